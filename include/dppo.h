@@ -6,7 +6,8 @@
  * factors so that the gradient stays unbiased, packs the retained sequences densely and trains on
  * them.  This library does, per batch:  group advantages -> candidate sets, pruning masks and
  * rescaling factors -> Dense Prompt Packing -> one sweep over the LM-head logits that yields the
- * loss and dlogits.
+ * loss and dlogits; and, for the frozen policies of that loss, the scoring of the sampled tokens (8-bit LM-head
+ * product, log-probs with entropy and alternatives).
  *
  * Conventions (all entry points)
  *  - Return value: 0 (DPPO_OK) or a negative dppo_error.  Nothing throws, aborts or prints.
@@ -336,6 +337,103 @@ int dppo_lmhead_grpo_loss(const dppo_lmhead_params* p, const void* hidden, const
                           const float* w, const int32_t* seg_map, void* dhidden, void* dW,
                           float* logp_out, float* lse_out, float* loss_out, void* workspace,
                           size_t workspace_bytes, int32_t* status, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Scoring: log-probs of GIVEN tokens, with the entropy of their distribution and its top alternatives.
+ * This is where the loss's logp_old and logp_ref come from (pi_theta_old and pi_ref of Eq. 1 at the sampled
+ * tokens), and what a training loop reports beside them.
+ *
+ * Row t, tau = temperature, m = max_v z_v, l = ln sum_v exp((z_v - m)/tau), p_v = exp((z_v - m)/tau - l):
+ *   lse = m/tau + l;   logp = (z_y - m)/tau - l;   entropy = l - sum_v p_v (z_v - m)/tau   (p ln p = 0 at p = 0)
+ *   alternatives: the top_k largest z_v in descending order, ties to the lower index, with their log-probs.
+ * Entries at -inf are masked: probability 0, never an alternative (a row with fewer than top_k others is filled
+ * up with id -1, log-prob -inf).  A row that its mask leaves empty has lse = logp = -inf, entropy 0.  A row with a
+ * NaN or +inf has NaN for all of these and ids -1.
+ */
+typedef struct {
+    int64_t T_max;          /* rows of logits / upper bound of tokens                                */
+    int32_t V;              /* vocabulary size                                                       */
+    int32_t dtype;          /* dppo_dtype of logits and dlogits                                      */
+    int64_t row_stride;     /* elements between consecutive rows (>= V; bytes a multiple of 16)      */
+    int32_t top_k;          /* alternatives per row, 0..32 (the backward ignores it)                 */
+    int32_t variant;        /* 0: the library picks the launch shape.  Tuning aid of the forward:
+                               C*10000 + threads: C = 1, 2, 4 or 8 CTAs per row with 128, 256 or 512
+                               threads each; 32: one warp per row                                    */
+    double temperature;     /* > 0                                                                   */
+} dppo_logprob_params;
+
+/*   logits       [T_max x row_stride] of dtype
+ *   target       i32 [T_max] token ids, or NULL (then logp_out is NULL)
+ *   n_tokens_dev i32 [1] true number of tokens T <= T_max on the device, or NULL (T = T_max);
+ *                rows >= T are neither read nor written, in any array
+ *   logp_out, entropy_out, lse_out   f32 [T_max] or NULL
+ *   top_ids      i32 [T_max x top_k], top_logp f32 [T_max x top_k]; NULL if and only if top_k = 0
+ *   stats        f32 [T_max x 4] or NULL: {m, l, entropy, 0} of each row for the backward call (m = -inf for a
+ *                row that its mask leaves empty)
+ * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED (logits base or row stride, stats base), UNSUPPORTED (dtype, variant).
+ * Device status: BAD_TARGET (the row's logp is 0; its other outputs are not affected).
+ */
+int dppo_token_logprobs(const dppo_logprob_params* p, const void* logits, const int32_t* target,
+                        const int32_t* n_tokens_dev, float* logp_out, float* entropy_out, float* lse_out,
+                        int32_t* top_ids, float* top_logp, float* stats, int32_t* status, void* stream);
+
+/* Gradient of the scoring call with respect to the logits, for a = dL/dlogp and b = dL/dentropy of each row:
+ *   dlogits[t, v] = (a ([v == y] - p_v) - b p_v (ln p_v + entropy)) / tau
+ * The probabilities are recomputed from the logits and the forward's stats: one read and one write of the rows.
+ * One below 2^-126 counts as 0.
+ *   dlogp, dentropy  f32 [T_max], either may be NULL (that term is absent); dlogp needs target
+ *   dlogits      same dtype / stride as logits; may alias logits (in place).  Columns at or past V are not written.
+ * A row that its mask leaves empty has a zero gradient.
+ * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED, UNSUPPORTED (dtype).  Device status: BAD_TARGET (the row is zero).
+ */
+int dppo_token_logprobs_backward(const dppo_logprob_params* p, const void* logits, const int32_t* target,
+                                 const int32_t* n_tokens_dev, const float* stats, const float* dlogp,
+                                 const float* dentropy, void* dlogits, int32_t* status, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Matrix product in 8-bit integers with one scale per token and one per output channel: the LM-head (or any
+ * projection) of a frozen policy whose log-probs are only scored.
+ *
+ * Quantisation of rows, symmetric: s = fl32(max_k |x_k| / 127), q_k = clamp(rint(fl32(x_k / s)), -127, 127) (ties to
+ * even); s = 0 gives q = 0.  A row with a NaN or an infinity gets s = NaN, q = 0, so that products with it are NaN.
+ */
+typedef struct {
+    int64_t rows_max;       /* rows of x                                                             */
+    int32_t K;              /* columns                                                               */
+    int32_t dtype;          /* dppo_dtype of x                                                       */
+    int64_t x_stride;       /* elements between rows of x (>= K; bytes a multiple of 16)             */
+    int64_t q_stride;       /* bytes between rows of q (>= K; a multiple of 16)                      */
+} dppo_quantize_params;
+
+/*   x   [rows_max x x_stride] of dtype;  q  i8 [rows_max x q_stride] out (columns at or past K are not written);
+ *   scale  f32 [rows_max] out;  n_rows_dev  i32 [1] true number of rows or NULL; rows past it are not touched
+ * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED, UNSUPPORTED (dtype).
+ */
+int dppo_quantize_rows_i8(const dppo_quantize_params* p, const void* x, int8_t* q, float* scale,
+                          const int32_t* n_rows_dev, int32_t* status, void* stream);
+
+/*   out[t, n] = fl32(fl32(x_scale[t] w_scale[n]) fl32(sum_k x[t, k] w[n, k])), rounded once more to a bf16 out.
+ * The sum is an exact 32-bit integer (K <= 131,071), so the result does not depend on the order of its terms. */
+typedef struct {
+    int64_t M_max;          /* rows of x / upper bound of tokens (below 2^31)                        */
+    int32_t N, K;           /* output channels; contraction length                                   */
+    int64_t x_stride, w_stride;   /* bytes between rows of x and of w (>= K; multiples of 16)        */
+    int64_t out_stride;     /* elements between rows of out (>= N)                                   */
+    int32_t out_dtype;      /* dppo_dtype of out                                                     */
+    int32_t variant;        /* 0: the library picks the kernel; 1 forces the CTA-pair tile kernel, 2 the
+                               kernel for few tokens (tuning aid).  101 / 102: the same two with the
+                               self-test of the bounded waits (see dppo_lmhead_params.variant): the call
+                               reports DPPO_STATUS_TIMEOUT, its output is unspecified                */
+} dppo_linear_i8_params;
+
+/*   x   i8 [M_max x x_stride], x_scale f32 [M_max];  w  i8 [N x w_stride], w_scale f32 [N]
+ *   out [M_max x out_stride] of out_dtype (no alignment beyond its element's)
+ *   n_rows_dev  i32 [1] true number of tokens on the device, or NULL; rows of out past it are not written
+ * Codes of -128 are allowed.  Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED (x, w: base or stride), UNSUPPORTED,
+ * CUDA (tensor-map creation).  Device status: TIMEOUT.
+ */
+int dppo_linear_i8(const dppo_linear_i8_params* p, const int8_t* x, const float* x_scale, const int8_t* w,
+                   const float* w_scale, void* out, const int32_t* n_rows_dev, int32_t* status, void* stream);
 
 #ifdef __cplusplus
 }

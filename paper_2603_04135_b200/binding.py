@@ -3,6 +3,9 @@
 Array arguments are torch tensors (their device pointer is passed), raw integer addresses, or None
 for the nullable ones.  Every function raises DppoError on a non-zero return code.  There is no
 fallback: if the library has not been built, importing this module raises.
+
+The scoring calls (token_logprobs, token_logprobs_backward, quantize_rows_i8, linear_i8) also check the tensors they
+are given: element type, on the current device, and large enough for the sizes in the params.
 """
 import ctypes
 import os
@@ -65,6 +68,26 @@ class LmheadParams(ctypes.Structure):
                 ("accumulate_dW", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class LogprobParams(ctypes.Structure):
+    _fields_ = [("T_max", ctypes.c_int64), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("row_stride", ctypes.c_int64), ("top_k", ctypes.c_int32), ("variant", ctypes.c_int32),
+                ("temperature", ctypes.c_double)]
+
+
+class QuantizeParams(ctypes.Structure):
+    _fields_ = [("rows_max", ctypes.c_int64), ("K", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64), ("q_stride", ctypes.c_int64)]
+
+
+class LinearI8Params(ctypes.Structure):
+    _fields_ = [("M_max", ctypes.c_int64), ("N", ctypes.c_int32), ("K", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
+                ("out_dtype", ctypes.c_int32), ("variant", ctypes.c_int32)]
+
+
+MAX_TOP_K = 32
+LINEAR_I8_WAIT_SELF_TEST = 100     # added to dppo_linear_i8_params.variant
+
 _vp = ctypes.c_void_p
 lib.dppo_version.restype = ctypes.c_int
 lib.dppo_last_error.restype = ctypes.c_char_p
@@ -97,6 +120,14 @@ lib.dppo_lmhead_workspace_bytes.restype = ctypes.c_size_t
 lib.dppo_lmhead_workspace_bytes.argtypes = [ctypes.POINTER(LmheadParams)]
 lib.dppo_lmhead_grpo_loss.restype = ctypes.c_int
 lib.dppo_lmhead_grpo_loss.argtypes = [ctypes.POINTER(LmheadParams)] + [_vp] * 16 + [ctypes.c_size_t, _vp, _vp]
+lib.dppo_token_logprobs.restype = ctypes.c_int
+lib.dppo_token_logprobs.argtypes = [ctypes.POINTER(LogprobParams)] + [_vp] * 11
+lib.dppo_token_logprobs_backward.restype = ctypes.c_int
+lib.dppo_token_logprobs_backward.argtypes = [ctypes.POINTER(LogprobParams)] + [_vp] * 9
+lib.dppo_quantize_rows_i8.restype = ctypes.c_int
+lib.dppo_quantize_rows_i8.argtypes = [ctypes.POINTER(QuantizeParams)] + [_vp] * 6
+lib.dppo_linear_i8.restype = ctypes.c_int
+lib.dppo_linear_i8.argtypes = [ctypes.POINTER(LinearI8Params)] + [_vp] * 8
 
 
 def _ptr(x):
@@ -105,6 +136,35 @@ def _ptr(x):
     if isinstance(x, torch.Tensor):
         return x.data_ptr()
     return int(x)
+
+
+_TORCH_DTYPE = {F32: torch.float32, BF16: torch.bfloat16}
+
+
+def _arr(x, name, device, dtype, rows, row_elems, stride=None):
+    """Device pointer of a [rows x row_elems] array.  A torch tensor is checked first: on `device` (the current
+    one), of `dtype`, laid out as the call will read it.  stride: elements between rows (None: dense)."""
+    if not isinstance(x, torch.Tensor):
+        return x
+    if x.dtype is not dtype:
+        raise DppoError(ERR_INVALID_ARG, "%s: dtype %s, expected %s" % (name, x.dtype, dtype))
+    if x.get_device() != device:
+        raise DppoError(ERR_INVALID_ARG, "%s: on %s, the current device is cuda:%d" % (name, x.device, device))
+    if rows > 0:
+        if stride is None:
+            if x.numel() < rows * row_elems or not x.is_contiguous():
+                raise DppoError(ERR_BAD_SHAPE, "%s: needs %d contiguous elements, got shape %s" % (name, rows * row_elems, tuple(x.shape)))
+        else:
+            have = x.untyped_storage().nbytes() // x.element_size() - x.storage_offset()
+            if have < (rows - 1) * stride + row_elems or (x.dim() == 2 and (x.stride(1) != 1 and x.shape[1] > 1
+                                                                            or x.stride(0) != stride and x.shape[0] > 1)):
+                raise DppoError(ERR_BAD_SHAPE, "%s: shape %s, strides %s do not hold %d rows of %d elements, %d apart"
+                                % (name, tuple(x.shape), x.stride(), rows, row_elems, stride))
+    return x.data_ptr()
+
+
+def _device():
+    return torch.cuda.current_device() if torch.cuda.is_available() else -1
 
 
 def _stream(stream):
@@ -210,3 +270,44 @@ def lmhead_grpo_loss(params, hidden, W, target, logp_old, logp_ref, cu_seqlens, 
 def sequence_log_ratio(logp, logp_old, cu_seqlens, S_max, out, status=None, stream=None):
     _check(lib.dppo_sequence_log_ratio(_ptr(logp), _ptr(logp_old), _ptr(cu_seqlens), S_max, _ptr(out), _ptr(status),
                                        _stream(stream)))
+
+
+def token_logprobs(params, logits, target, n_tokens_dev, logp_out, entropy_out, lse_out, top_ids, top_logp, stats,
+                   status=None, stream=None):
+    p, d, i32, f32 = params, _device(), torch.int32, torch.float32
+    T, k = p.T_max, p.top_k
+    _check(lib.dppo_token_logprobs(
+        ctypes.byref(p), _arr(logits, "logits", d, _TORCH_DTYPE.get(p.dtype), T, p.V, p.row_stride),
+        _arr(target, "target", d, i32, T, 1), _arr(n_tokens_dev, "n_tokens_dev", d, i32, 1, 1),
+        _arr(logp_out, "logp_out", d, f32, T, 1), _arr(entropy_out, "entropy_out", d, f32, T, 1),
+        _arr(lse_out, "lse_out", d, f32, T, 1), _arr(top_ids, "top_ids", d, i32, T, k),
+        _arr(top_logp, "top_logp", d, f32, T, k), _arr(stats, "stats", d, f32, T, 4), _arr(status, "status", d, i32, 1, 1),
+        _stream(stream)))
+
+
+def token_logprobs_backward(params, logits, target, n_tokens_dev, stats, dlogp, dentropy, dlogits, status=None,
+                            stream=None):
+    p, d, i32, f32 = params, _device(), torch.int32, torch.float32
+    T, dt = p.T_max, _TORCH_DTYPE.get(p.dtype)
+    _check(lib.dppo_token_logprobs_backward(
+        ctypes.byref(p), _arr(logits, "logits", d, dt, T, p.V, p.row_stride), _arr(target, "target", d, i32, T, 1),
+        _arr(n_tokens_dev, "n_tokens_dev", d, i32, 1, 1), _arr(stats, "stats", d, f32, T, 4),
+        _arr(dlogp, "dlogp", d, f32, T, 1), _arr(dentropy, "dentropy", d, f32, T, 1),
+        _arr(dlogits, "dlogits", d, dt, T, p.V, p.row_stride), _arr(status, "status", d, i32, 1, 1), _stream(stream)))
+
+
+def quantize_rows_i8(params, x, q, scale, n_rows_dev=None, status=None, stream=None):
+    p, d, M = params, _device(), params.rows_max
+    _check(lib.dppo_quantize_rows_i8(
+        ctypes.byref(p), _arr(x, "x", d, _TORCH_DTYPE.get(p.dtype), M, p.K, p.x_stride),
+        _arr(q, "q", d, torch.int8, M, p.K, p.q_stride), _arr(scale, "scale", d, torch.float32, M, 1),
+        _arr(n_rows_dev, "n_rows_dev", d, torch.int32, 1, 1), _arr(status, "status", d, torch.int32, 1, 1), _stream(stream)))
+
+
+def linear_i8(params, x, x_scale, w, w_scale, out, n_rows_dev=None, status=None, stream=None):
+    p, d, f32 = params, _device(), torch.float32
+    _check(lib.dppo_linear_i8(
+        ctypes.byref(p), _arr(x, "x", d, torch.int8, p.M_max, p.K, p.x_stride), _arr(x_scale, "x_scale", d, f32, p.M_max, 1),
+        _arr(w, "w", d, torch.int8, p.N, p.K, p.w_stride), _arr(w_scale, "w_scale", d, f32, p.N, 1),
+        _arr(out, "out", d, _TORCH_DTYPE.get(p.out_dtype), p.M_max, p.N, p.out_stride),
+        _arr(n_rows_dev, "n_rows_dev", d, torch.int32, 1, 1), _arr(status, "status", d, torch.int32, 1, 1), _stream(stream)))

@@ -1,0 +1,596 @@
+// Matrix product in 8-bit integers with one scale per token and one per output channel, on the 5th-generation tensor
+// cores: out[t, n] = (sx[t] sw[n]) sum_k x[t, k] w[n, k], the sum an exact int32 (tcgen05.mma kind::i8); and the
+// quantisation of rows that makes its operands.
+//
+// The weights take the M side of the tensor-core tile (TMEM lanes = output channels), the tokens its N side (TMEM
+// columns): a tile of 128 channels then fits any number of tokens from 16 up without wasted columns, and the epilogue,
+// whose thread holds one channel, writes 32 consecutive channels of a token per warp instruction whatever the row
+// pitch of the output (64 or 128 contiguous bytes, no alignment asked for).
+//
+// Two kernels:
+//   many tokens (tensor-core bound): persistent CTA pairs (cta_group::2), 256 channels x 256 tokens per tile, 128-byte K
+//     slabs through a six-stage TMA ring, two TMEM accumulators so that the epilogue of a tile runs under the next one's
+//     products; tiles are handed out so that the CTAs running together share their weights and their tokens in L2
+//   few tokens (bound by reading the weights): a CTA per 128 channels, 16 to 128 tokens, and the contraction split over
+//     the CTAs of a cluster when there are too few tiles to keep all SMs reading; the int32 partial sums are joined
+//     through distributed shared memory (exact, so the split changes no result)
+// Every wait is bounded; on a time-out the CTA reports DPPO_STATUS_TIMEOUT, leaves its loops, lets copies and products in
+// flight finish (bounded), frees its tensor memory and returns.
+#include "common.cuh"
+#include "grpo_loss.cuh"
+#include "tensor_core.cuh"
+
+namespace dppo {
+namespace i8 {
+
+constexpr int kBK = 128;                  // K slab: 128 codes = one 128-byte swizzle row
+constexpr int kTileM = 128;               // channels per CTA
+constexpr int kTileN = 256;               // tokens per tile of the pair kernel
+constexpr int kStages2 = 6;
+constexpr int kBytesA = kTileM * kBK;                        // 16 KB
+constexpr int kBytesB2 = kTileN / 2 * kBK;                   // 16 KB: this CTA's half of the token tile
+constexpr int kStageBytes2 = kBytesA + kBytesB2;
+constexpr int kThreads = 192;
+constexpr int kTokenGroup = 16;           // token tiles swept together (4096 tokens: 10 MB of codes at K = 2560)
+constexpr size_t kDynSmem2 = (size_t)kStages2 * kStageBytes2 + 1024;
+
+struct Args {
+    const float* x_scale;
+    const float* w_scale;
+    void* out;
+    const int32_t* n_rows_dev;
+    int32_t* status;
+    long long M_max, out_stride;
+    int N, n_ksteps, out_bf16;
+    unsigned long long wait_limit_ns;
+    int test_extra_tx;
+};
+
+// Instruction descriptor of kind::i8: D = s32, A = B = s8, both K-major.
+__host__ __device__ constexpr uint32_t idesc(int m, int n) {
+    return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+__device__ __forceinline__ long long true_rows(const Args& a) {
+    return a.n_rows_dev ? min((long long)max(*a.n_rows_dev, 0), a.M_max) : a.M_max;
+}
+
+// One output: the scales are multiplied first, each step rounded to f32, then to the output's type.
+__device__ __forceinline__ void store(const Args& a, long long t, int n, int32_t acc, float sx, float sw) {
+    const float v = __fmul_rn(__int2float_rn(acc), __fmul_rn(sx, sw));
+    if (a.out_bf16) reinterpret_cast<__nv_bfloat16*>(a.out)[t * a.out_stride + n] = __float2bfloat16_rn(v);
+    else reinterpret_cast<float*>(a.out)[t * a.out_stride + n] = v;
+}
+
+// ---- many tokens: CTA pairs ---------------------------------------------------------------------------
+struct Shared2 {
+    unsigned long long full[kStages2];
+    unsigned long long empty[kStages2];
+    unsigned long long acc_full[2];
+    unsigned long long acc_empty[2];      // the leader's copy counts 8 arrivals: 4 epilogue warps x 2 CTAs
+    unsigned long long drain;             // products in flight on an early way out
+    uint32_t tmem_base;
+    int abort;
+};
+
+// Tile j of this pair: token tiles are taken kTokenGroup at a time; within a group the token tiles of one channel tile
+// follow each other, so that every weight is fetched once per group and the group's codes stay in L2.
+__device__ __forceinline__ bool tile_of(uint32_t j, int n_m2, int n_tok, int& m2, int& n) {
+    const long long id = (long long)(blockIdx.x >> 1) + (long long)j * (gridDim.x >> 1);
+    if (id >= (long long)n_m2 * n_tok) return false;
+    const long long per = (long long)kTokenGroup * n_m2;
+    const int g = (int)(id / per), local = (int)(id - (long long)g * per);
+    const int n0 = g * kTokenGroup, width = min(kTokenGroup, n_tok - n0);
+    m2 = local / width;
+    n = n0 + local - m2 * width;
+    return true;
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+linear_i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const Args a) {
+    extern __shared__ unsigned char i8_raw[];
+    __shared__ Shared2 sh;
+    const uint32_t tiles = (lm_smem_u32(i8_raw) + 1023u) & ~1023u;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    uint32_t rank;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    const bool leader = rank == 0;
+    volatile int* abort_flag = &sh.abort;
+    const long long T = true_rows(a);
+    const int n_m2 = (a.N + 2 * kTileM - 1) / (2 * kTileM), n_tok = (int)((T + kTileN - 1) / kTileN);
+
+    if (tid == 0) {
+        sh.abort = 0;
+        for (int s = 0; s < kStages2; ++s) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(lm_smem_u32(&sh.full[s])));
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(lm_smem_u32(&sh.empty[s])));
+        }
+        for (int b = 0; b < 2; ++b) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(lm_smem_u32(&sh.acc_full[b])));
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 8;" :: "r"(lm_smem_u32(&sh.acc_empty[b])));
+        }
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(lm_smem_u32(&sh.drain)));
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                     :: "r"(lm_smem_u32(&sh.tmem_base)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    lm_cluster_sync();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem_base = sh.tmem_base;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ TMA producer (both CTAs)
+        if (lane == 0) {
+            uint32_t it = 0;
+            int m2, n;
+            for (uint32_t j = 0; tile_of(j, n_m2, n_tok, m2, n) && !*abort_flag; ++j) {
+                const int row_w = (2 * m2 + (int)rank) * kTileM, row_x = n * kTileN + (int)rank * (kTileN / 2);
+                for (int k = 0; k < a.n_ksteps; ++k, ++it) {
+                    const uint32_t s = it % kStages2, use = it / kStages2;
+                    if (use > 0 && !lm_wait(lm_smem_u32(&sh.empty[s]), (use - 1) & 1, abort_flag, a.wait_limit_ns)) break;
+                    const uint32_t bar_local = lm_smem_u32(&sh.full[s]), bar = bar_local & kPeerMask;
+                    const uint32_t dst = tiles + s * kStageBytes2;
+                    if (leader)                                        // the leader's barrier collects both CTAs' bytes
+                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;"
+                                     :: "r"(bar_local), "r"((uint32_t)(2 * kStageBytes2) + (it == 0 ? (uint32_t)a.test_extra_tx : 0u)) : "memory");
+                    lm_tma_2d_pair(dst, &map_w, bar, k * kBK, row_w, 0);
+                    lm_tma_2d_pair(dst + kBytesA, &map_x, bar, k * kBK, row_x, 0);
+                }
+            }
+            if (*abort_flag && leader) {                               // copies in flight get a bounded chance to land
+                const uint32_t pending = it < (uint32_t)kStages2 ? it : (uint32_t)kStages2;
+                for (uint32_t i = 0; i < pending; ++i) {
+                    const uint32_t i2 = it - 1 - i;
+                    lm_wait_plain(lm_smem_u32(&sh.full[i2 % kStages2]), (i2 / kStages2) & 1, a.wait_limit_ns);
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer (leader CTA only)
+        if (lane == 0 && leader) {
+            uint32_t it = 0;
+            int m2, n;
+            bool ok = true;
+            for (uint32_t j = 0; ok && tile_of(j, n_m2, n_tok, m2, n) && !*abort_flag; ++j) {
+                const uint32_t b = j & 1, use_b = j >> 1;
+                if (use_b > 0 && !lm_wait(lm_smem_u32(&sh.acc_empty[b]), (use_b - 1) & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t d_tmem = tmem_base + b * kTileN;
+                for (int k = 0; k < a.n_ksteps; ++k, ++it) {
+                    const uint32_t s = it % kStages2, use = it / kStages2;
+                    if (!lm_wait(lm_smem_u32(&sh.full[s]), use & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t dw = lm_smem_desc_k(tiles + s * kStageBytes2), dx = lm_smem_desc_k(tiles + s * kStageBytes2 + kBytesA);
+#pragma unroll
+                    for (int kk = 0; kk < kBK / 32; ++kk) {              // 32 codes of K per instruction
+                        const uint32_t accumulate = (k > 0 || kk > 0) ? 1u : 0u;
+                        asm volatile("{\n\t.reg .pred p;\n\t"
+                                     "setp.ne.b32 p, %4, 0;\n\t"
+                                     "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                                     :: "r"(d_tmem), "l"(dw + kk * 2), "l"(dx + kk * 2), "r"(idesc(2 * kTileM, kTileN)), "r"(accumulate) : "memory");
+                    }
+                    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                                 :: "r"(lm_smem_u32(&sh.empty[s])), "h"((unsigned short)3) : "memory");
+                }
+                if (!ok) break;
+                asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                             :: "r"(lm_smem_u32(&sh.acc_full[b])), "h"((unsigned short)3) : "memory");
+            }
+            if (!ok) {                                                 // products already issued finish before memory goes away
+                asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(lm_smem_u32(&sh.drain)) : "memory");
+                lm_wait_plain(lm_smem_u32(&sh.drain), 0, a.wait_limit_ns);
+            }
+        }
+    } else {
+        // ------------------------------------------------------------------ epilogue (warps 2..5, both CTAs)
+        const int q = warp & 3;                                          // TMEM lane quarter of this warp
+        int m2, n;
+        for (uint32_t j = 0; tile_of(j, n_m2, n_tok, m2, n); ++j) {
+            const int ch = (2 * m2 + (int)rank) * kTileM + q * 32 + lane;
+            const float sw = ch < a.N ? a.w_scale[ch] : 0.0f;
+            const uint32_t b = j & 1, use_b = j >> 1;
+            // warp-uniform outcome: the tcgen05.ld below must be executed by all 32 lanes together
+            if (!__all_sync(0xffffffffu, lm_wait(lm_smem_u32(&sh.acc_full[b]), use_b & 1, abort_flag, a.wait_limit_ns))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + b * kTileN;
+#pragma unroll 1
+            for (int c = 0; c < kTileN / 32; ++c) {
+                const long long t0 = (long long)n * kTileN + c * 32;
+                if (t0 >= T) break;
+                uint32_t v[32];
+                lm_tmem_load32(v, taddr + (uint32_t)(c * 32));
+                const float sx = t0 + lane < T ? a.x_scale[t0 + lane] : 0.0f;
+                const int nt = (int)min((long long)32, T - t0);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const float sxi = __shfl_sync(0xffffffffu, sx, i);
+                    if (i < nt && ch < a.N) store(a, t0 + i, ch, (int32_t)v[i], sxi, sw);
+                }
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0)                                               // the leader's MMA thread waits for all 8 warps
+                asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(lm_smem_u32(&sh.acc_empty[b]) & kPeerMask) : "memory");
+        }
+    }
+
+    // ---- common exit: both CTAs are done with tensor memory and with each other's barriers, then free
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    lm_cluster_sync();
+    if (tid == 0 && sh.abort) set_status(a.status, DPPO_STATUS_TIMEOUT);
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem_base), "r"(512u) : "memory");
+    }
+}
+
+// ---- few tokens: a CTA per 128 channels, K split over a cluster ---------------------------------------
+// Stages for two resident CTAs per SM.
+template <int kNB> __host__ __device__ constexpr int small_stages() { return kNB <= 16 ? 6 : kNB <= 32 ? 5 : kNB <= 64 ? 4 : 3; }
+template <int kNB> __host__ __device__ constexpr int small_stage_bytes() { return kBytesA + kNB * kBK; }
+template <int kNB> constexpr size_t small_smem() { return (size_t)small_stages<kNB>() * small_stage_bytes<kNB>() + 1024; }
+
+struct SharedSmall {
+    unsigned long long full[6];
+    unsigned long long empty[6];
+    unsigned long long done;
+    uint32_t tmem_base;
+    int abort;
+};
+
+// 16 or 32 columns of this thread's TMEM lane.
+__device__ __forceinline__ void tmem_load16(uint32_t (&v)[32], uint32_t taddr) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+                   "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                 : "r"(taddr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+template <int kNB>
+__global__ void __launch_bounds__(kThreads)
+linear_i8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const Args a, int n_ch, int split) {
+    constexpr int kStages = small_stages<kNB>(), kStageBytes = small_stage_bytes<kNB>();
+    constexpr int kCols = kNB < 32 ? 32 : kNB;
+    constexpr int kChunk = kNB < 32 ? kNB : 32;
+    extern __shared__ unsigned char i8_raw[];
+    __shared__ SharedSmall sh;
+    const uint32_t tiles = (lm_smem_u32(i8_raw) + 1023u) & ~1023u;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    volatile int* abort_flag = &sh.abort;
+    const long long T = true_rows(a);
+    const int part = (int)(blockIdx.x % (unsigned)split);                 // rank in the cluster: clusters are consecutive CTAs
+    const int id = (int)(blockIdx.x / (unsigned)split);
+    const int m = id % n_ch;
+    const long long t_tile = (long long)(id / n_ch) * kNB;
+    if (t_tile >= T) return;                                              // the whole cluster leaves together
+    const int k0 = (int)((long long)a.n_ksteps * part / split), k1 = (int)((long long)a.n_ksteps * (part + 1) / split);
+
+    if (tid == 0) {
+        sh.abort = 0;
+        for (int s = 0; s < kStages; ++s) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(lm_smem_u32(&sh.full[s])));
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(lm_smem_u32(&sh.empty[s])));
+        }
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(lm_smem_u32(&sh.done)));
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     :: "r"(lm_smem_u32(&sh.tmem_base)), "r"((uint32_t)kCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem_base = sh.tmem_base;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int it = 0;
+            for (int k = k0; k < k1; ++k, ++it) {
+                const int s = it % kStages, use = it / kStages;
+                if (use > 0 && !lm_wait(lm_smem_u32(&sh.empty[s]), (use - 1) & 1, abort_flag, a.wait_limit_ns)) break;
+                const uint32_t bar = lm_smem_u32(&sh.full[s]), dst = tiles + s * kStageBytes;
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;"
+                             :: "r"(bar), "r"((uint32_t)kStageBytes + (it == 0 ? (uint32_t)a.test_extra_tx : 0u)) : "memory");
+                lm_tma_2d(dst, &map_w, bar, k * kBK, m * kTileM, 0);
+                lm_tma_2d(dst + kBytesA, &map_x, bar, k * kBK, (int)t_tile, 0);
+            }
+            if (*abort_flag) {
+                const int pending = it < kStages ? it : kStages;
+                for (int i = 0; i < pending; ++i) {
+                    const int i2 = it - 1 - i;
+                    lm_wait_plain(lm_smem_u32(&sh.full[i2 % kStages]), (i2 / kStages) & 1, a.wait_limit_ns);
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            int it = 0;
+            for (int k = k0; k < k1; ++k, ++it) {
+                const int s = it % kStages, use = it / kStages;
+                if (!lm_wait(lm_smem_u32(&sh.full[s]), use & 1, abort_flag, a.wait_limit_ns)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint64_t dw = lm_smem_desc_k(tiles + s * kStageBytes), dx = lm_smem_desc_k(tiles + s * kStageBytes + kBytesA);
+#pragma unroll
+                for (int kk = 0; kk < kBK / 32; ++kk) {
+                    const uint32_t accumulate = (it > 0 || kk > 0) ? 1u : 0u;
+                    asm volatile("{\n\t.reg .pred p;\n\t"
+                                 "setp.ne.b32 p, %4, 0;\n\t"
+                                 "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                                 :: "r"(tmem_base), "l"(dw + kk * 2), "l"(dx + kk * 2), "r"(idesc(kTileM, kNB)), "r"(accumulate) : "memory");
+                }
+                asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(lm_smem_u32(&sh.empty[s])) : "memory");
+            }
+            // all products issued so far (on an early way out too: they finish before memory goes away)
+            asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(lm_smem_u32(&sh.done)) : "memory");
+            lm_wait_plain(lm_smem_u32(&sh.done), 0, a.wait_limit_ns);
+        }
+    }
+    // epilogue warps; the int32 sums of a split contraction go through shared memory: [token][channel], in the ring,
+    // which nothing reads or writes any more once `done` has completed
+    const int q = warp & 3, row = q * 32 + lane;
+    const int ch = m * kTileM + row;
+    bool live = false;
+    const float sw = warp >= 2 && ch < a.N ? a.w_scale[ch] : 0.0f;
+    if (warp >= 2) {
+        live = __all_sync(0xffffffffu, lm_wait(lm_smem_u32(&sh.done), 0, abort_flag, a.wait_limit_ns)) && !*abort_flag;
+        live = __all_sync(0xffffffffu, live);
+        if (live) {
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16);
+#pragma unroll 1
+            for (int c = 0; c < kNB / kChunk; ++c) {
+                const long long t0 = t_tile + c * kChunk;
+                if (t0 >= T) break;
+                uint32_t v[32];
+                if constexpr (kChunk == 16) tmem_load16(v, taddr); else lm_tmem_load32(v, taddr + (uint32_t)(c * 32));
+                if (split == 1) {
+                    const float sx = t0 + lane < T && lane < kChunk ? a.x_scale[t0 + lane] : 0.0f;
+                    const int nt = (int)min((long long)kChunk, T - t0);
+#pragma unroll
+                    for (int i = 0; i < kChunk; ++i) {
+                        const float sxi = __shfl_sync(0xffffffffu, sx, i);
+                        if (i < nt && ch < a.N) store(a, t0 + i, ch, (int32_t)v[i], sxi, sw);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kChunk; ++i)
+                        asm volatile("st.shared.b32 [%0], %1;" :: "r"(tiles + (uint32_t)((c * kChunk + i) * kTileM + row) * 4u), "r"(v[i]) : "memory");
+                }
+            }
+        }
+    }
+    if (split > 1) {
+        lm_cluster_sync();                                               // every CTA's sums are in its shared memory
+        if (live) {
+            for (int c = part; c < kNB && t_tile + c < T; c += split) {  // this CTA's share of the tokens
+                const uint32_t local = tiles + (uint32_t)(c * kTileM + row) * 4u;
+                int32_t sum = 0;
+                for (int r = 0; r < split; ++r) {
+                    uint32_t remote;
+                    int32_t x;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(local), "r"(r));
+                    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(x) : "r"(remote) : "memory");
+                    sum += x;
+                }
+                if (ch < a.N) store(a, t_tile + c, ch, sum, a.x_scale[t_tile + c], sw);
+            }
+        }
+        lm_cluster_sync();                                               // the others have read this CTA's shared memory
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (tid == 0 && sh.abort) set_status(a.status, DPPO_STATUS_TIMEOUT);
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem_base), "r"((uint32_t)kCols) : "memory");
+    }
+}
+
+// ---- quantisation of rows -----------------------------------------------------------------------------
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+struct QuantArgs {
+    const char* x;
+    int8_t* q;
+    float* scale;
+    const int32_t* n_rows_dev;
+    long long rows_max, x_row_bytes, q_stride;
+    int K;
+};
+
+__device__ __forceinline__ uint32_t code_of(float x, float s) {
+    const float v = rintf(__fdiv_rn(x, s));
+    return (uint32_t)(int32_t)fminf(fmaxf(v, -127.0f), 127.0f) & 0xffu;
+}
+
+constexpr int kQuantThreads = 128;
+
+// One CTA per row, two reads of it (the second out of L1 / L2): the maximum, then the codes.
+template <bool kBf16>
+__global__ void __launch_bounds__(kQuantThreads)
+quantize_rows_kernel(const QuantArgs a) {
+    constexpr int kPer = Elems<kBf16>::kPerVec;
+    __shared__ float red[kQuantThreads / 32];
+    const long long t = blockIdx.x;
+    const long long T = a.n_rows_dev ? min((long long)*a.n_rows_dev, a.rows_max) : a.rows_max;
+    if (t >= T) return;
+    const int tid = threadIdx.x;
+    const char* row = a.x + t * a.x_row_bytes;
+    const uint4* rv = reinterpret_cast<const uint4*>(row);
+    int8_t* q = a.q + t * a.q_stride;
+    const int nvec = a.K / kPer, tail = nvec * kPer + tid;
+    float amax = 0.0f;
+    for (int i = tid; i < nvec; i += kQuantThreads) {
+        float f[kPer];
+        Elems<kBf16>::unpack(rv[i], f);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) amax = max_nan(amax, fabsf(f[j]));
+    }
+    if (tail < a.K) amax = max_nan(amax, fabsf(Elems<kBf16>::load1(row, tail)));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    if ((tid & 31) == 0) red[tid >> 5] = amax;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kQuantThreads / 32; ++w) amax = max_nan(amax, red[w]);
+    const bool fine = amax < INFINITY;
+    const float s = fine ? __fdiv_rn(amax, 127.0f) : __int_as_float(0x7fffffff);
+    if (tid == 0) a.scale[t] = s;
+    const bool live = fine && s > 0.0f;
+    for (int i = tid; i < nvec; i += kQuantThreads) {
+        float f[kPer];
+        Elems<kBf16>::unpack(rv[i], f);
+        uint32_t w[kPer / 4];
+#pragma unroll
+        for (int j = 0; j < kPer; j += 4)
+            w[j / 4] = live ? code_of(f[j], s) | code_of(f[j + 1], s) << 8 | code_of(f[j + 2], s) << 16 | code_of(f[j + 3], s) << 24 : 0u;
+        if constexpr (kBf16) reinterpret_cast<uint2*>(q)[i] = make_uint2(w[0], w[1]);
+        else reinterpret_cast<uint32_t*>(q)[i] = w[0];
+    }
+    if (tail < a.K) q[tail] = live ? (int8_t)code_of(Elems<kBf16>::load1(row, tail), s) : (int8_t)0;
+}
+
+// ---- host side ---------------------------------------------------------------------------------------
+// i8 [rows x K] with row pitch `ld` bytes; boxes of 128 codes x box_rows rows, 128B swizzle, zeros outside.
+static int make_map(CUtensorMap* map, const void* base, long long rows, int K, long long ld, int box_rows) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return fail(DPPO_ERR_CUDA, "linear_i8: cuTensorMapEncodeTiled is not available from this driver");
+    const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld};
+    const cuuint32_t box[2] = {(cuuint32_t)kBK, (cuuint32_t)box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(DPPO_ERR_CUDA, "linear_i8: cuTensorMapEncodeTiled failed with %d", (int)r);
+    return DPPO_OK;
+}
+
+static int launch_pair(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
+    cudaError_t e = cudaFuncSetAttribute(linear_i8_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDynSmem2);
+    if (e != cudaSuccess) return cuda_fail(e, "linear_i8: shared memory attribute");
+    const long long work = (long long)((a.N + 255) / 256) * ((a.M_max + kTileN - 1) / kTileN), most = sm_count() / 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * (work < most ? work : most)), 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = kDynSmem2;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, linear_i8_pair_kernel, mw, mx, a);
+    if (e != cudaSuccess) return cuda_fail(e, "linear_i8 launch");
+    return DPPO_OK;
+}
+
+template <int kNB> static int launch_small(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
+    auto kernel = linear_i8_small_kernel<kNB>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)small_smem<kNB>());
+    if (e != cudaSuccess) return cuda_fail(e, "linear_i8: shared memory attribute");
+    const int n_ch = (a.N + kTileM - 1) / kTileM;
+    const long long tiles = (long long)n_ch * ((a.M_max + kNB - 1) / kNB);
+    int split = 1;                                                       // enough CTAs for two per SM, two slabs at least each
+    while (split < 8 && tiles * split * 2 <= 2ll * sm_count() && a.n_ksteps >= 4 * split) split *= 2;
+    if (tiles * split > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "linear_i8: too many tiles");
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles * split), 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = small_smem<kNB>();
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, kernel, mw, mx, a, n_ch, split);
+    if (e != cudaSuccess) return cuda_fail(e, "linear_i8 launch");
+    return DPPO_OK;
+}
+
+}  // namespace i8
+}  // namespace dppo
+
+extern "C" int dppo_quantize_rows_i8(const dppo_quantize_params* p, const void* x, int8_t* q, float* scale,
+                                     const int32_t* n_rows_dev, int32_t* status, void* stream) {
+    dppo::NvtxRange nvtx_range("dppo_quantize_rows_i8");
+    using namespace dppo;
+    (void)status;
+    if (!p) return fail(DPPO_ERR_INVALID_ARG, "quantize_rows_i8: NULL params");
+    if (p->rows_max < 0 || p->K < 1) return fail(DPPO_ERR_INVALID_ARG, "quantize_rows_i8: rows_max=%lld K=%d", (long long)p->rows_max, p->K);
+    if (p->dtype != DPPO_F32 && p->dtype != DPPO_BF16) return fail(DPPO_ERR_UNSUPPORTED, "quantize_rows_i8: dtype %d", p->dtype);
+    if (p->x_stride < p->K || p->q_stride < p->K)
+        return fail(DPPO_ERR_BAD_SHAPE, "quantize_rows_i8: strides %lld, %lld < K %d", (long long)p->x_stride, (long long)p->q_stride, p->K);
+    if (p->rows_max >= ((int64_t)1 << 31)) return fail(DPPO_ERR_BAD_SHAPE, "quantize_rows_i8: rows_max must be below 2^31");
+    const long long x_row_bytes = (long long)p->x_stride * (p->dtype == DPPO_BF16 ? 2 : 4);
+    if (p->rows_max == 0) return DPPO_OK;
+    if (!x || !q || !scale) return fail(DPPO_ERR_INVALID_ARG, "quantize_rows_i8: NULL array");
+    if (((uintptr_t)x & 15) || ((uintptr_t)q & 15) || x_row_bytes % 16 != 0 || p->q_stride % 16 != 0)
+        return fail(DPPO_ERR_MISALIGNED, "quantize_rows_i8: x / q base and row strides must be multiples of 16 bytes");
+    const i8::QuantArgs a = {(const char*)x, q, scale, n_rows_dev, p->rows_max, x_row_bytes, p->q_stride, p->K};
+    if (p->dtype == DPPO_BF16) i8::quantize_rows_kernel<true><<<(unsigned)p->rows_max, i8::kQuantThreads, 0, (cudaStream_t)stream>>>(a);
+    else i8::quantize_rows_kernel<false><<<(unsigned)p->rows_max, i8::kQuantThreads, 0, (cudaStream_t)stream>>>(a);
+    DPPO_CHECK_LAUNCH("quantize_rows_i8 launch");
+    return DPPO_OK;
+}
+
+extern "C" int dppo_linear_i8(const dppo_linear_i8_params* p, const int8_t* x, const float* x_scale, const int8_t* w,
+                              const float* w_scale, void* out, const int32_t* n_rows_dev, int32_t* status, void* stream) {
+    dppo::NvtxRange nvtx_range("dppo_linear_i8");
+    using namespace dppo;
+    if (!p) return fail(DPPO_ERR_INVALID_ARG, "linear_i8: NULL params");
+    if (p->M_max < 0 || p->N < 1 || p->K < 1)
+        return fail(DPPO_ERR_INVALID_ARG, "linear_i8: M_max=%lld N=%d K=%d", (long long)p->M_max, p->N, p->K);
+    if (p->out_dtype != DPPO_F32 && p->out_dtype != DPPO_BF16) return fail(DPPO_ERR_UNSUPPORTED, "linear_i8: out_dtype %d", p->out_dtype);
+    if (p->K > 131071) return fail(DPPO_ERR_BAD_SHAPE, "linear_i8: K=%d, the int32 sums are exact up to 131071", p->K);
+    if (p->N > 0x7fffff00) return fail(DPPO_ERR_BAD_SHAPE, "linear_i8: N=%d", p->N);
+    if (p->x_stride < p->K || p->w_stride < p->K || p->out_stride < p->N)
+        return fail(DPPO_ERR_BAD_SHAPE, "linear_i8: strides %lld, %lld, %lld for K=%d N=%d", (long long)p->x_stride, (long long)p->w_stride,
+                    (long long)p->out_stride, p->K, p->N);
+    if (p->M_max >= ((int64_t)1 << 31) - 256) return fail(DPPO_ERR_BAD_SHAPE, "linear_i8: M_max too large");
+    const int variant = p->variant >= 100 ? p->variant - 100 : p->variant;
+    if (variant < 0 || variant > 2 || p->variant == 100) return fail(DPPO_ERR_INVALID_ARG, "linear_i8: variant %d", p->variant);
+    if (p->M_max == 0) return DPPO_OK;
+    if (!x || !x_scale || !w || !w_scale || !out) return fail(DPPO_ERR_INVALID_ARG, "linear_i8: NULL array");
+    if (((uintptr_t)x & 15) || ((uintptr_t)w & 15) || p->x_stride % 16 != 0 || p->w_stride % 16 != 0)
+        return fail(DPPO_ERR_MISALIGNED, "linear_i8: x / w base and row strides must be multiples of 16 bytes");
+    if (p->x_stride >= (1ll << 40) || p->w_stride >= (1ll << 40)) return fail(DPPO_ERR_BAD_SHAPE, "linear_i8: strides of x and w must be below 2^40");
+
+    i8::Args a = {};
+    a.x_scale = x_scale; a.w_scale = w_scale; a.out = out; a.n_rows_dev = n_rows_dev; a.status = status;
+    a.M_max = p->M_max; a.out_stride = p->out_stride;
+    a.N = p->N; a.n_ksteps = (p->K + i8::kBK - 1) / i8::kBK; a.out_bf16 = p->out_dtype == DPPO_BF16;
+    a.wait_limit_ns = p->variant >= 100 ? kSelfTestWaitLimitNs : kDefaultWaitLimitNs;
+    a.test_extra_tx = p->variant >= 100 ? 16 : 0;
+    // The pair kernel from half a wave of its 256 x 256 tiles on; below that, and for up to 128 tokens, the other
+    const long long pair_tiles = (long long)((p->N + 255) / 256) * ((p->M_max + 255) / 256);
+    const bool pair = variant == 1 || (variant == 0 && p->M_max > 128 && pair_tiles * 4 >= sm_count());
+    const int nb = pair ? i8::kTileN / 2 : p->M_max <= 16 ? 16 : p->M_max <= 32 ? 32 : p->M_max <= 64 ? 64 : 128;
+    alignas(64) CUtensorMap mw, mx;
+    int rc = i8::make_map(&mw, w, p->N, p->K, p->w_stride, i8::kTileM);
+    if (rc == DPPO_OK) rc = i8::make_map(&mx, x, p->M_max, p->K, p->x_stride, nb);
+    if (rc != DPPO_OK) return rc;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (pair) return i8::launch_pair(mw, mx, a, s);
+    switch (nb) {
+        case 16: return i8::launch_small<16>(mw, mx, a, s);
+        case 32: return i8::launch_small<32>(mw, mx, a, s);
+        case 64: return i8::launch_small<64>(mw, mx, a, s);
+        default: return i8::launch_small<128>(mw, mx, a, s);
+    }
+}

@@ -1,0 +1,649 @@
+// Log-probs of given tokens with entropy and top alternatives, and their gradient with respect to the logits.
+//
+// Forward.  Per row: m = max z, S = sum e_v and Q = sum e_v (z_v - m) with e_v = 2^((z_v - m) c), c = log2(e)/tau;
+// then l = ln S, lse = m/tau + l, logp = (z_y - m)/tau - l and entropy = l - Q/(S tau) (both terms are >= 0: nothing
+// cancels on a peaked row).  One pass: every thread keeps an ONLINE (m, S, Q) over the 16-byte vectors it sees; a larger
+// maximum M rescales them, S' = S 2^((m-M)c), Q' = (Q + (m-M) S) 2^((m-M)c).  (z_v - m) is formed first and
+// scaled afterwards, so that rows of any magnitude (masks of the type's lowest value included) keep their differences.
+//
+// The alternatives cost the pass nothing.  A thread's running maximum is known anyway at the end of the row, and the
+// k-th largest of the threads' maxima, thr, is a lower bound of the k-th largest entry (k threads have an entry that
+// large): a thread whose maximum is below thr holds none of the top k.  So about k of the 128-512 threads' vectors
+// are read again (a few KB of the row, out of L2), entries >= thr become candidates, and a candidate's rank is the
+// number of candidates ahead of it in the order (value descending, index ascending).  Too many candidates (ties)
+// are met by rules that need no more memory: see select_top.
+//
+// A row is worked on by a TEAM: a warp (short rows), a CTA, or a cluster of CTAs that split the row and join through
+// distributed shared memory (few rows: a decode batch).
+//
+// Backward.  dz_v = ([v = y] a - p_v (a + b (ln p_v + H))) / tau, with p_v recomputed from the row's (m, l, H).  No
+// reduction: a streaming map, one read and one write per element.
+#include <cooperative_groups.h>
+
+#include "common.cuh"
+#include "grpo_loss.cuh"
+
+namespace dppo {
+using namespace packed;
+namespace cg = cooperative_groups;
+
+namespace logprob {
+
+constexpr int kMaxTop = 32;
+constexpr int kCand = 512;                // candidate buffer of a CTA-sized team
+constexpr int kCandWarp = 128;            // and of a warp-sized one
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kFar = -1e30f;            // differences are held at or above this: 0 * (-inf) never arises
+
+struct Args {
+    const char* logits;
+    const int32_t* target;
+    const int32_t* n_tokens_dev;
+    float *logp, *entropy, *lse;
+    int32_t* top_ids;
+    float* top_logp;
+    float4* stats;
+    int32_t* status;
+    long long T_max, row_bytes;
+    int V, k;
+    float c, inv_tau;
+};
+
+// What a thread (then a warp, a CTA, a cluster) has seen of a row.  m = the largest entry (kLowest if there is none but
+// -inf; then S = 0); bad: a NaN or +inf was among them.
+struct Part {
+    float m, S, Q;
+    int bad;
+};
+
+__device__ __forceinline__ void rescale(Part& p, float M, float c) {
+    const float d = fmaxf(p.m - M, kFar), f = ex2(d * c);
+    p.Q = (p.Q + d * p.S) * f;
+    p.S *= f;
+    p.m = M;
+}
+__device__ __forceinline__ void join(Part& p, Part o, float c) {
+    const float M = fmaxf(p.m, o.m);
+    rescale(p, M, c);
+    rescale(o, M, c);
+    p.S += o.S; p.Q += o.Q; p.bad |= o.bad;
+}
+__device__ __forceinline__ Part shfl_xor(const Part& p, int o) {
+    Part r;
+    r.m = __shfl_xor_sync(0xffffffffu, p.m, o); r.S = __shfl_xor_sync(0xffffffffu, p.S, o);
+    r.Q = __shfl_xor_sync(0xffffffffu, p.Q, o); r.bad = __shfl_xor_sync(0xffffffffu, p.bad, o);
+    return r;
+}
+
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// Largest entry of a vector (NaN if there is one).
+template <bool kBf16> __device__ __forceinline__ float vec_max(const uint4& q) {
+    if constexpr (kBf16) {
+        __nv_bfloat162 a = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&q.x), *reinterpret_cast<const __nv_bfloat162*>(&q.y));
+        a = __hmax2_nan(a, __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&q.z), *reinterpret_cast<const __nv_bfloat162*>(&q.w)));
+        return max_nan(__low2float(a), __high2float(a));
+    } else {
+        return max_nan(max_nan(__uint_as_float(q.x), __uint_as_float(q.y)), max_nan(__uint_as_float(q.z), __uint_as_float(q.w)));
+    }
+}
+
+__device__ __forceinline__ uint4 load_vec(const void* p) {
+    uint4 q;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "l"(p));
+    return q;
+}
+
+// The backward may write where it reads (in place): not the read-only path.
+__device__ __forceinline__ uint4 load_vec_rw(const void* p) {
+    uint4 q;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "l"(p) : "memory");
+    return q;
+}
+
+// Running sums of a thread: pairs, so that the packed f32x2 instructions take two elements at a time.
+struct Acc {
+    f32x2 S, Q;
+    float m;
+    int bad;
+};
+__device__ __forceinline__ void acc_init(Acc& a) { a.S = a.Q = pair_of(0.0f, 0.0f); a.m = kLowest; a.bad = 0; }
+__device__ __forceinline__ Part acc_part(const Acc& a) {
+    float s0, s1, q0, q1;
+    unpair(a.S, s0, s1); unpair(a.Q, q0, q1);
+    return {a.m, s0 + s1, q0 + q1, a.bad};
+}
+__device__ __forceinline__ void acc_grow(Acc& a, float vmax, float c) {
+    if (!(vmax < INFINITY)) { a.bad = 1; return; }                 // NaN or +inf: the row's results are NaN
+    const float d = fmaxf(a.m - vmax, kFar), f = ex2(d * c);
+    a.Q = mul2(fma2(pair_of(d, d), a.S, a.Q), pair_of(f, f));
+    a.S = mul2(a.S, pair_of(f, f));
+    a.m = vmax;
+}
+__device__ __forceinline__ void acc_pair(Acc& a, float z0, float z1, f32x2 nm2, f32x2 c2) {
+    float x0, x1, y0, y1;
+    unpair(add2(pair_of(z0, z1), nm2), x0, x1);
+    const f32x2 x = pair_of(fmaxf(x0, kFar), fmaxf(x1, kFar));
+    unpair(mul2(x, c2), y0, y1);
+    const f32x2 e = pair_of(ex2(y0), ex2(y1));
+    a.S = add2(a.S, e);
+    a.Q = fma2(e, x, a.Q);
+}
+template <bool kBf16> __device__ __forceinline__ void acc_vec(Acc& a, const uint4& q, float c) {
+    const float vmax = vec_max<kBf16>(q);
+    if (!(vmax <= a.m)) acc_grow(a, vmax, c);                      // rare after the first few vectors of a row
+    const f32x2 nm2 = pair_of(-a.m, -a.m), c2 = pair_of(c, c);
+    float f[Elems<kBf16>::kPerVec];
+    Elems<kBf16>::unpack(q, f);
+#pragma unroll
+    for (int i = 0; i < Elems<kBf16>::kPerVec; i += 2) acc_pair(a, f[i], f[i + 1], nm2, c2);
+}
+
+// Order of f32 values as unsigned numbers (-0 counts as +0; no NaN gets here).
+__device__ __forceinline__ uint32_t key_of(float z) {
+    const uint32_t b = __float_as_uint(z + 0.0f);
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t key) {
+    return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
+
+template <int kThreads, int kCap> struct TeamShared {
+    Part part[kThreads / 32];
+    Part row;
+    float tmax[kThreads];
+    int hot[kThreads];
+    int n_hot, n_cand, n_le;
+    float thr;
+    uint32_t ckey[kCap];
+    int cidx[kCap];
+    uint32_t lkey[kMaxTop];                // the team's own sorted list (joined over a cluster)
+    int lidx[kMaxTop];
+    int n_list;
+    int red[kThreads / 32];
+};
+
+template <int kThreads> __device__ __forceinline__ void team_sync() {
+    if constexpr (kThreads == 32) __syncwarp(); else __syncthreads();
+}
+
+// k-th largest (1-based) of n keys in shared memory, by one warp: the largest value that at least k keys reach, found bit
+// by bit from the top.  n <= 32 * kPer.
+template <int kPer> __device__ __forceinline__ uint32_t kth_largest(const float* v, int n, int k, int lane) {
+    uint32_t own[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) own[i] = (i * 32 + lane) < n ? key_of(v[i * 32 + lane]) : 0u;
+    uint32_t r = 0;
+#pragma unroll 1
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t t = r | (1u << bit);
+        int cnt = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) cnt += own[i] >= t ? 1 : 0;
+        cnt = __reduce_add_sync(0xffffffffu, cnt);
+        if (cnt >= k) r = t;
+        if (cnt == k) break;                                       // exactly the k largest reach t: t serves as well
+    }
+    return r;
+}
+
+// Entries of the row part [v0, v1) (in vectors) + tail [tail0, V) as a team sees them.
+struct Span {
+    const char* row;
+    int v0, v1, tail0, tail1;
+};
+
+// Calls f(value, index) for every entry of the part that this thread owns in the sweep's own layout.
+template <bool kBf16, int kThreads, class F> __device__ __forceinline__ void for_own(const Span& sp, int tid, F f) {
+    constexpr int kPer = Elems<kBf16>::kPerVec;
+    for (int i = sp.v0 + tid; i < sp.v1; i += kThreads) {
+        float z[kPer];
+        Elems<kBf16>::unpack(load_vec(sp.row + (size_t)i * 16), z);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) f(z[j], i * kPer + j);
+    }
+    if (sp.tail0 + tid < sp.tail1) f(Elems<kBf16>::load1(sp.row, sp.tail0 + tid), sp.tail0 + tid);
+}
+
+template <int kThreads, int kCap> __device__ __forceinline__ int team_count(TeamShared<kThreads, kCap>& sh, int cnt, int tid) {
+    cnt = __reduce_add_sync(0xffffffffu, cnt);
+    if constexpr (kThreads == 32) return cnt;
+    __syncthreads();                                               // red[] may still be read from the last call
+    if ((tid & 31) == 0) sh.red[tid >> 5] = cnt;
+    __syncthreads();
+    int s = 0;
+    for (int w = 0; w < kThreads / 32; ++w) s += sh.red[w];
+    return s;
+}
+
+// The team's top k of its part, sorted, into sh.lkey / lidx / n_list.  sh.tmax holds the threads' maxima.
+template <bool kBf16, int kThreads, int kCap>
+__device__ void select_top(TeamShared<kThreads, kCap>& sh, const Span& sp, int k, int tid) {
+    constexpr int kPer = Elems<kBf16>::kPerVec;
+    const int lane = tid & 31, warp = tid >> 5;
+    if (warp == 0) {
+        const uint32_t t = kth_largest<kThreads / 32>(sh.tmax, kThreads, k, lane);
+        // fewer than k threads hold anything: every entry above -inf is a candidate
+        if (lane == 0) { sh.thr = fmaxf(value_of(t), kLowest); sh.n_hot = 0; sh.n_cand = 0; }
+    }
+    team_sync<kThreads>();
+    float thr = sh.thr;
+    if (sh.tmax[tid] >= thr) sh.hot[atomicAdd(&sh.n_hot, 1)] = tid;
+    team_sync<kThreads>();
+    auto offer = [&](float z, int idx) {
+        if (z >= thr) {
+            const int at = atomicAdd(&sh.n_cand, 1);
+            if (at < kCap) { sh.ckey[at] = key_of(z); sh.cidx[at] = idx; }
+        }
+    };
+    const int n_hot = sh.n_hot;
+    for (int h = warp; h < n_hot; h += kThreads / 32) {            // a warp reads a hot thread's vectors
+        const int i0 = sp.v0 + sh.hot[h];
+        for (int i = i0 + lane * kThreads; i < sp.v1; i += 32 * kThreads) {
+            const uint4 q = load_vec(sp.row + (size_t)i * 16);
+            if (!(vec_max<kBf16>(q) >= thr)) continue;
+            float z[kPer];
+            Elems<kBf16>::unpack(q, z);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) offer(z[j], i * kPer + j);
+        }
+    }
+    if (sp.tail0 + tid < sp.tail1) offer(Elems<kBf16>::load1(sp.row, sp.tail0 + tid), sp.tail0 + tid);
+    team_sync<kThreads>();
+    int n = sh.n_cand;
+    if (n > kCap) {
+        // Too many entries at or above thr.  Mostly ties: fewer than kCap are ABOVE it.  Where that fails too, thr is raised
+        // to the k-th largest entry itself (bit by bit, a counting sweep per bit): at most k - 1 are above that.
+        auto count_above = [&](float t) {
+            int cnt = 0;
+            for_own<kBf16, kThreads>(sp, tid, [&](float z, int) { cnt += z > t ? 1 : 0; });
+            return team_count(sh, cnt, tid);
+        };
+        if (count_above(thr) > kCap - kMaxTop) {
+            uint32_t r = 0;
+            for (int bit = 31; bit >= 0; --bit) {
+                const uint32_t t = r | (1u << bit);
+                int cnt = 0;
+                for_own<kBf16, kThreads>(sp, tid, [&](float z, int) { cnt += z > -INFINITY && key_of(z) >= t ? 1 : 0; });
+                if (team_count(sh, cnt, tid) >= k) r = t;
+            }
+            thr = fmaxf(value_of(r), kLowest);
+        }
+        team_sync<kThreads>();
+        if (tid == 0) sh.n_cand = 0;
+        team_sync<kThreads>();
+        for_own<kBf16, kThreads>(sp, tid, [&](float z, int idx) {
+            if (z > thr) {
+                const int at = atomicAdd(&sh.n_cand, 1);
+                sh.ckey[at] = key_of(z); sh.cidx[at] = idx;        // at most kCap - kMaxTop of them
+            }
+        });
+        team_sync<kThreads>();
+        n = sh.n_cand;
+        team_sync<kThreads>();
+        if (warp == 0) {                                           // and the first k entries AT thr, in index order
+            int have = 0;
+            auto take = [&](bool hit, int idx) {
+                const uint32_t b = __ballot_sync(0xffffffffu, hit);
+                const int at = have + __popc(b & ((1u << lane) - 1u));
+                if (hit && at < k) { sh.ckey[n + at] = key_of(thr); sh.cidx[n + at] = idx; }
+                have += __popc(b);
+            };
+            for (int i = sp.v0 * kPer; i < sp.v1 * kPer && have < k; i += 32) {
+                const int idx = i + lane;
+                take(idx < sp.v1 * kPer && Elems<kBf16>::load1(sp.row, idx) == thr, idx);
+            }
+            if (have < k) take(sp.tail0 + lane < sp.tail1 && Elems<kBf16>::load1(sp.row, sp.tail0 + lane) == thr, sp.tail0 + lane);
+            if (lane == 0) sh.n_cand = n + (have < k ? have : k);
+        }
+        team_sync<kThreads>();
+        n = sh.n_cand;
+    }
+    for (int i = tid; i < n; i += kThreads) {                      // rank = candidates ahead of this one
+        const uint32_t key = sh.ckey[i];
+        const int idx = sh.cidx[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += sh.ckey[j] > key || (sh.ckey[j] == key && sh.cidx[j] < idx) ? 1 : 0;
+        if (rank < k) { sh.lkey[rank] = key; sh.lidx[rank] = idx; }
+    }
+    if (tid == 0) sh.n_list = n < k ? n : k;
+    team_sync<kThreads>();
+}
+
+// kCluster: the CTAs of a cluster split the row (blockIdx.x / cluster size = row).  Else kTeams teams per CTA, a row each.
+template <bool kBf16, int kThreads, int kTeams, bool kCluster>
+__global__ void __launch_bounds__(kThreads * kTeams)
+token_logprobs_kernel(const Args a) {
+    constexpr int kPer = Elems<kBf16>::kPerVec, kLog2Per = kBf16 ? 3 : 2;
+    constexpr int kCap = kThreads == 32 ? kCandWarp : kCand;
+    constexpr int kUnroll = 4;
+    __shared__ TeamShared<kThreads, kCap> shared[kTeams];
+    const int team = kTeams == 1 ? 0 : threadIdx.x / kThreads;
+    const int tid = kTeams == 1 ? threadIdx.x : threadIdx.x % kThreads;
+    const int lane = tid & 31, warp = tid >> 5;
+    TeamShared<kThreads, kCap>& sh = shared[team];
+    const long long T = a.n_tokens_dev ? min((long long)*a.n_tokens_dev, a.T_max) : a.T_max;
+    unsigned rank = 0, C = 1;
+    if constexpr (kCluster) { C = cg::this_cluster().num_blocks(); rank = cg::this_cluster().block_rank(); }
+    const long long t = kCluster ? (long long)(blockIdx.x / C) : (long long)blockIdx.x * kTeams + team;
+    if (t >= T) return;                                            // the whole team (and cluster) leaves together
+
+    const char* row = a.logits + t * a.row_bytes;
+    const int nvec = a.V >> kLog2Per;
+    Span sp;
+    sp.row = row;
+    sp.v0 = (int)((long long)nvec * rank / C);
+    sp.v1 = (int)((long long)nvec * (rank + 1) / C);
+    sp.tail0 = rank == C - 1 ? nvec << kLog2Per : a.V;
+    sp.tail1 = a.V;
+
+    // the given token: asked for while the row streams
+    float zy = 0.0f;
+    int y_state = 0;
+    if (rank == 0 && tid == 0 && a.target) {
+        const int y = a.target[t];
+        if (y < 0 || y >= a.V) y_state = DPPO_STATUS_BAD_TARGET;
+        else zy = Elems<kBf16>::load1(row, y);
+    }
+
+    Acc acc;
+    acc_init(acc);
+    int i = sp.v0 + tid;
+    for (; i + (kUnroll - 1) * kThreads < sp.v1; i += kUnroll * kThreads) {
+        uint4 q[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) q[u] = load_vec(row + (size_t)(i + u * kThreads) * 16);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) acc_vec<kBf16>(acc, q[u], a.c);
+    }
+    for (; i < sp.v1; i += kThreads) acc_vec<kBf16>(acc, load_vec(row + (size_t)i * 16), a.c);
+    if (sp.tail0 + tid < sp.tail1) {
+        const float z = Elems<kBf16>::load1(row, sp.tail0 + tid);
+        if (!(z <= acc.m)) acc_grow(acc, z, a.c);
+        acc_pair(acc, z, -INFINITY, pair_of(-acc.m, -acc.m), pair_of(a.c, a.c));
+    }
+
+    Part p = acc_part(acc);
+    if (a.k > 0) sh.tmax[tid] = p.S > 0.0f ? p.m : -INFINITY;      // nothing but -inf seen: not a maximum
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) join(p, shfl_xor(p, o), a.c);
+    if constexpr (kThreads > 32) {
+        if (lane == 0) sh.part[warp] = p;
+        __syncthreads();
+        if (warp == 0) {
+            p = lane < kThreads / 32 ? sh.part[lane] : Part{kLowest, 0.0f, 0.0f, 0};
+#pragma unroll
+            for (int o = kThreads / 64; o > 0; o >>= 1) join(p, shfl_xor(p, o), a.c);
+        }
+    }
+    if (tid == 0) sh.row = p;
+    team_sync<kThreads>();
+    if (a.k > 0 && !sh.row.bad) select_top<kBf16, kThreads, kCap>(sh, sp, a.k, tid);
+
+    if constexpr (kCluster) {
+        cg::cluster_group cl = cg::this_cluster();
+        cl.sync();                                                 // every CTA's part and list are in its shared memory
+        if (rank == 0) {
+            if (warp == 0) {
+                Part o = {kLowest, 0.0f, 0.0f, 0};
+                if (lane < (int)C) o = cl.map_shared_rank(&sh, lane)->row;
+#pragma unroll
+                for (int s = 16; s > 0; s >>= 1) join(o, shfl_xor(o, s), a.c);
+                if (lane == 0) sh.part[0] = o;
+            }
+            if (a.k > 0) {
+                // the lists side by side in the candidate buffer (C * k <= 8 * 32 < kCap), then rank by rank
+                if (tid == 0) sh.n_cand = 0;
+                __syncthreads();
+                for (int i = tid; i < (int)C * a.k; i += kThreads) {
+                    auto* o = cl.map_shared_rank(&sh, i / a.k);
+                    const int j = i % a.k;
+                    if (!o->row.bad && j < o->n_list) {
+                        const int at = atomicAdd(&sh.n_cand, 1);
+                        sh.ckey[at] = o->lkey[j]; sh.cidx[at] = o->lidx[j];
+                    }
+                }
+            }
+        }
+        cl.sync();                                                 // the other CTAs' shared memory has been read
+        if (rank != 0) return;
+        if (a.k > 0) {
+            const int n = sh.n_cand;
+            for (int i = tid; i < n; i += kThreads) {
+                const uint32_t key = sh.ckey[i];
+                const int idx = sh.cidx[i];
+                int ahead = 0;
+                for (int j = 0; j < n; ++j) ahead += sh.ckey[j] > key || (sh.ckey[j] == key && sh.cidx[j] < idx) ? 1 : 0;
+                if (ahead < a.k) { sh.lkey[ahead] = key; sh.lidx[ahead] = idx; }
+            }
+            if (tid == 0) sh.n_list = n < a.k ? n : a.k;
+        }
+        if (tid == 0) sh.row = sh.part[0];
+        __syncthreads();
+    }
+
+    // ---- outputs
+    const Part r = sh.row;
+    const bool empty = r.S == 0.0f && !r.bad;
+    const float nan = __int_as_float(0x7fffffff);
+    const float l = r.bad ? nan : empty ? 0.0f : logf(r.S);
+    if (tid == 0) {
+        const float H = r.bad ? nan : empty ? 0.0f : fmaxf(l - r.Q / r.S * a.inv_tau, 0.0f);
+        if (a.lse) a.lse[t] = r.bad ? nan : empty ? -INFINITY : fmaf(r.m, a.inv_tau, l);
+        if (a.entropy) a.entropy[t] = H;
+        if (a.stats) a.stats[t] = make_float4(r.bad ? nan : empty ? -INFINITY : r.m, l, H, 0.0f);
+        if (a.logp) {
+            if (y_state != 0) set_status(a.status, y_state);
+            a.logp[t] = y_state != 0 ? 0.0f : r.bad ? nan : empty ? -INFINITY : fmaf(zy - r.m, a.inv_tau, -l);
+        } else if (y_state != 0) {
+            set_status(a.status, y_state);
+        }
+    }
+    for (int j = tid; j < a.k; j += kThreads) {
+        const bool have = !r.bad && j < sh.n_list;
+        a.top_ids[t * a.k + j] = have ? sh.lidx[j] : -1;
+        a.top_logp[t * a.k + j] = have ? fmaf(value_of(sh.lkey[j]) - r.m, a.inv_tau, -l) : r.bad ? nan : -INFINITY;
+    }
+}
+
+// ---- backward -----------------------------------------------------------------------------------------
+struct BwdArgs {
+    const char* logits;
+    char* dlogits;
+    const int32_t* target;
+    const int32_t* n_tokens_dev;
+    const float4* stats;
+    const float *dlogp, *dentropy;
+    int32_t* status;
+    long long T_max, row_bytes;
+    int V, chunks, chunk_vecs;           // a row is taken in `chunks` pieces of chunk_vecs vectors
+    float c, inv_tau;
+};
+
+struct BwdRow {
+    float nm, l2n, a, b, bH;             // -m, -l log2(e), a / tau, b / tau, (a + b (H - l)) / tau
+    float bx;                            // b / tau^2: what (z - m) adds to the bracket
+    int y;
+};
+
+__device__ __forceinline__ float bwd_elem(float z, const BwdRow& r, float c) {
+    const float x = fmaxf(z + r.nm, kFar);
+    const float p = ex2(fmaf(x, c, r.l2n));
+    return -p * fmaf(x, r.bx, r.bH);
+}
+
+template <bool kBf16, int kThreads, int kTeams>
+__global__ void __launch_bounds__(kThreads * kTeams)
+token_logprobs_bwd_kernel(const BwdArgs a) {
+    constexpr int kPer = Elems<kBf16>::kPerVec, kLog2Per = kBf16 ? 3 : 2;
+    const int team = kTeams == 1 ? 0 : threadIdx.x / kThreads;
+    const int tid = kTeams == 1 ? threadIdx.x : threadIdx.x % kThreads;
+    const long long T = a.n_tokens_dev ? min((long long)*a.n_tokens_dev, a.T_max) : a.T_max;
+    const long long item = (long long)blockIdx.x * kTeams + team;
+    const long long t = a.chunks == 1 ? item : item / a.chunks;
+    const int chunk = a.chunks == 1 ? 0 : (int)(item - t * a.chunks);
+    if (t >= T) return;
+
+    const float4 st = a.stats[t];
+    const int y = a.target ? a.target[t] : 0;
+    const float da = a.dlogp ? a.dlogp[t] : 0.0f, db = a.dentropy ? a.dentropy[t] : 0.0f;
+    const bool bad_y = a.target && (y < 0 || y >= a.V);
+    const bool zero = bad_y || st.x == -INFINITY;
+    if (bad_y && tid == 0 && chunk == 0) set_status(a.status, DPPO_STATUS_BAD_TARGET);
+    BwdRow r;
+    r.nm = -st.x; r.l2n = -st.y * 1.4426950408889634f;
+    r.a = da * a.inv_tau; r.b = db * a.inv_tau;
+    r.bH = fmaf(r.b, st.z - st.y, r.a);
+    r.bx = r.b * a.inv_tau;
+    r.y = y;
+
+    const char* row = a.logits + t * a.row_bytes;
+    char* out = a.dlogits + t * a.row_bytes;
+    const int nvec = a.V >> kLog2Per;
+    const int v0 = chunk * a.chunk_vecs, v1 = min(nvec, v0 + a.chunk_vecs);
+    const int vy = a.dlogp && !zero ? y >> kLog2Per : -1;
+    for (int i = v0 + tid; i < v1; i += kThreads) {
+        float z[kPer];
+        Elems<kBf16>::unpack(load_vec_rw(row + (size_t)i * 16), z);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) z[j] = zero ? 0.0f : bwd_elem(z[j], r, a.c);
+        if (i == vy) {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) z[j] += j == (y & (kPer - 1)) ? r.a : 0.0f;
+        }
+        __stcs(reinterpret_cast<uint4*>(out) + i, Elems<kBf16>::pack(z));
+    }
+    const int tail = (nvec << kLog2Per) + tid;
+    if (chunk == a.chunks - 1 && tail < a.V) {
+        float g = zero ? 0.0f : bwd_elem(Elems<kBf16>::load1(row, tail), r, a.c);
+        if (a.dlogp && !zero && tail == y) g += r.a;
+        Elems<kBf16>::store1(out, tail, g);
+    }
+}
+
+// ---- host side ---------------------------------------------------------------------------------------
+template <bool kBf16, int kThreads, int kTeams, bool kCluster>
+static int launch_fwd(const Args& a, int C, cudaStream_t s) {
+    auto kernel = token_logprobs_kernel<kBf16, kThreads, kTeams, kCluster>;
+    cudaLaunchConfig_t cfg = {};
+    const long long teams = kCluster ? a.T_max * C : (a.T_max + kTeams - 1) / kTeams;
+    if (teams > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "token_logprobs: T_max=%lld needs too large a grid", a.T_max);
+    cfg.gridDim = dim3((unsigned)teams, 1, 1);
+    cfg.blockDim = dim3(kThreads * kTeams, 1, 1);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = kCluster ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
+    if (e != cudaSuccess) return cuda_fail(e, "token_logprobs launch");
+    return DPPO_OK;
+}
+
+template <bool kBf16> static int run_fwd(const Args& a, int variant, cudaStream_t s) {
+    int C = 1, threads = 256;
+    if (variant == 0) {
+        const int nvec = a.V >> (kBf16 ? 3 : 2);
+        if (nvec <= 512) { threads = 32; }
+        else {
+            while (C < 8 && a.T_max * C * 2 <= 2ll * sm_count() && nvec / (2 * C) >= 256) C *= 2;
+            threads = nvec / C >= 4096 ? 512 : 256;
+        }
+    } else if (variant == 32) {
+        threads = 32;
+    } else {
+        C = variant / 10000; threads = variant % 10000;
+    }
+    if (threads == 32 && C == 1) return launch_fwd<kBf16, 32, 8, false>(a, 1, s);
+    if (C == 1 && threads == 128) return launch_fwd<kBf16, 128, 1, false>(a, 1, s);
+    if (C == 1 && threads == 256) return launch_fwd<kBf16, 256, 1, false>(a, 1, s);
+    if (C == 1 && threads == 512) return launch_fwd<kBf16, 512, 1, false>(a, 1, s);
+    if (C == 2 || C == 4 || C == 8) {
+        if (threads == 128) return launch_fwd<kBf16, 128, 1, true>(a, C, s);
+        if (threads == 256) return launch_fwd<kBf16, 256, 1, true>(a, C, s);
+        if (threads == 512) return launch_fwd<kBf16, 512, 1, true>(a, C, s);
+    }
+    return fail(DPPO_ERR_UNSUPPORTED, "token_logprobs: variant %d", variant);
+}
+
+template <bool kBf16, int kThreads, int kTeams> static int launch_bwd(const BwdArgs& a, cudaStream_t s) {
+    const long long ctas = (a.T_max * a.chunks + kTeams - 1) / kTeams;
+    if (ctas > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "token_logprobs_backward: T_max=%lld needs too large a grid", a.T_max);
+    token_logprobs_bwd_kernel<kBf16, kThreads, kTeams><<<(unsigned)ctas, kThreads * kTeams, 0, s>>>(a);
+    DPPO_CHECK_LAUNCH("token_logprobs_backward launch");
+    return DPPO_OK;
+}
+
+template <bool kBf16> static int run_bwd(BwdArgs a, cudaStream_t s) {
+    const int nvec = a.V >> (kBf16 ? 3 : 2);
+    a.chunks = 1; a.chunk_vecs = nvec;
+    if (nvec <= 512) return launch_bwd<kBf16, 32, 8>(a, s);
+    a.chunk_vecs = 2048;
+    a.chunks = (nvec + a.chunk_vecs - 1) / a.chunk_vecs;
+    return launch_bwd<kBf16, 256, 1>(a, s);
+}
+
+// Checks that both calls make; 0 or the error.
+static int check(const dppo_logprob_params* p, const char* what, const void* logits, const void* other) {
+    if (!p) return fail(DPPO_ERR_INVALID_ARG, "%s: NULL params", what);
+    if (p->T_max < 0 || p->V < 1) return fail(DPPO_ERR_INVALID_ARG, "%s: T_max=%lld V=%d", what, (long long)p->T_max, p->V);
+    if (p->dtype != DPPO_F32 && p->dtype != DPPO_BF16) return fail(DPPO_ERR_UNSUPPORTED, "%s: dtype %d", what, p->dtype);
+    if (p->row_stride < p->V) return fail(DPPO_ERR_BAD_SHAPE, "%s: row_stride %lld < V %d", what, (long long)p->row_stride, p->V);
+    if (!(p->temperature > 0.0) || !(p->temperature < INFINITY)) return fail(DPPO_ERR_INVALID_ARG, "%s: temperature must be > 0", what);
+    if (p->T_max >= ((int64_t)1 << 31)) return fail(DPPO_ERR_BAD_SHAPE, "%s: T_max must be below 2^31", what);
+    const size_t esize = p->dtype == DPPO_BF16 ? 2 : 4;
+    if (p->T_max > 0 && !logits) return fail(DPPO_ERR_INVALID_ARG, "%s: NULL logits", what);
+    if (((uintptr_t)logits & 15) || ((uintptr_t)other & 15) || ((size_t)p->row_stride * esize) % 16 != 0)
+        return fail(DPPO_ERR_MISALIGNED, "%s: logits / dlogits / stats base and row stride must be multiples of 16 bytes", what);
+    return DPPO_OK;
+}
+
+}  // namespace logprob
+}  // namespace dppo
+
+extern "C" int dppo_token_logprobs(const dppo_logprob_params* p, const void* logits, const int32_t* target,
+                                   const int32_t* n_tokens_dev, float* logp_out, float* entropy_out, float* lse_out,
+                                   int32_t* top_ids, float* top_logp, float* stats, int32_t* status, void* stream) {
+    dppo::NvtxRange nvtx_range("dppo_token_logprobs");
+    using namespace dppo;
+    const int rc = logprob::check(p, "token_logprobs", logits, stats);
+    if (rc != DPPO_OK) return rc;
+    if (p->top_k < 0 || p->top_k > logprob::kMaxTop) return fail(DPPO_ERR_INVALID_ARG, "token_logprobs: top_k=%d (0..%d)", p->top_k, logprob::kMaxTop);
+    if (p->variant < 0) return fail(DPPO_ERR_INVALID_ARG, "token_logprobs: variant %d", p->variant);
+    if (p->T_max == 0) return DPPO_OK;
+    if ((p->top_k > 0) != (top_ids != nullptr) || (p->top_k > 0) != (top_logp != nullptr))
+        return fail(DPPO_ERR_INVALID_ARG, "token_logprobs: top_ids and top_logp go with top_k > 0");
+    if (logp_out && !target) return fail(DPPO_ERR_INVALID_ARG, "token_logprobs: logp_out without target");
+    logprob::Args a = {};
+    a.logits = (const char*)logits; a.target = target; a.n_tokens_dev = n_tokens_dev;
+    a.logp = logp_out; a.entropy = entropy_out; a.lse = lse_out; a.top_ids = top_ids; a.top_logp = top_logp;
+    a.stats = (float4*)stats; a.status = status;
+    a.T_max = p->T_max; a.row_bytes = (long long)p->row_stride * (p->dtype == DPPO_BF16 ? 2 : 4);
+    a.V = p->V; a.k = p->top_k;
+    a.c = (float)(1.4426950408889634 / p->temperature); a.inv_tau = (float)(1.0 / p->temperature);
+    return p->dtype == DPPO_BF16 ? logprob::run_fwd<true>(a, p->variant, (cudaStream_t)stream)
+                                 : logprob::run_fwd<false>(a, p->variant, (cudaStream_t)stream);
+}
+
+extern "C" int dppo_token_logprobs_backward(const dppo_logprob_params* p, const void* logits, const int32_t* target,
+                                            const int32_t* n_tokens_dev, const float* stats, const float* dlogp,
+                                            const float* dentropy, void* dlogits, int32_t* status, void* stream) {
+    dppo::NvtxRange nvtx_range("dppo_token_logprobs_backward");
+    using namespace dppo;
+    int rc = logprob::check(p, "token_logprobs_backward", logits, stats);
+    if (rc != DPPO_OK) return rc;
+    if (p->T_max == 0) return DPPO_OK;
+    if (!stats || !dlogits) return fail(DPPO_ERR_INVALID_ARG, "token_logprobs_backward: NULL stats or dlogits");
+    if ((uintptr_t)dlogits & 15) return fail(DPPO_ERR_MISALIGNED, "token_logprobs_backward: dlogits base must be a multiple of 16 bytes");
+    if (dlogp && !target) return fail(DPPO_ERR_INVALID_ARG, "token_logprobs_backward: dlogp without target");
+    logprob::BwdArgs a = {};
+    a.logits = (const char*)logits; a.dlogits = (char*)dlogits; a.target = target; a.n_tokens_dev = n_tokens_dev;
+    a.stats = (const float4*)stats; a.dlogp = dlogp; a.dentropy = dentropy; a.status = status;
+    a.T_max = p->T_max; a.row_bytes = (long long)p->row_stride * (p->dtype == DPPO_BF16 ? 2 : 4);
+    a.V = p->V;
+    a.c = (float)(1.4426950408889634 / p->temperature); a.inv_tau = (float)(1.0 / p->temperature);
+    return p->dtype == DPPO_BF16 ? logprob::run_bwd<true>(a, (cudaStream_t)stream) : logprob::run_bwd<false>(a, (cudaStream_t)stream);
+}

@@ -10,6 +10,18 @@ from . import binding as B
 from . import dp
 
 
+def quantize_rows_i8(x, status=None):
+    """8-bit codes and scales of the rows of x (bf16 or f32 [M, K] with rows on 16 bytes): (q int8 [M, K], scale f32 [M]), q a
+    view of rows padded to 16 bytes.  Weights are quantised once this way and kept; see DppoStep.score_hidden_i8."""
+    M, K = x.shape
+    ld = (K + 15) // 16 * 16
+    q = torch.zeros(M, ld, dtype=torch.int8, device=x.device)
+    scale = torch.zeros(M, dtype=torch.float32, device=x.device)
+    B.quantize_rows_i8(B.QuantizeParams(M, K, B.BF16 if x.dtype is torch.bfloat16 else B.F32, x.stride(0) if M > 1 else max(x.stride(0), K), ld),
+                       x, q, scale, status=status)
+    return q[:, :K], scale
+
+
 class DppoStep:
     """Buffers for a batch of P prompts x G completions and a loss sweep over at most T_max tokens.
 
@@ -104,6 +116,78 @@ class DppoStep:
         B.grpo_loss_fwd_bwd(self.loss_params, logits, target, logp_old, logp_ref, self.cu_seqlens,
                             self.counts[3:4], self.adv, self.w_seq, self.order, dlogits, self.logp_out,
                             self.lse_out, self.loss_out, self.loss_ws, self.loss_ws_bytes, self.status)
+
+    # -- scoring: where logp_old and logp_ref come from ---------------------------------------------
+    def _score_buffers(self, T, top_k, out):
+        """Buffers of a scoring call over T rows (reused when `out` is what an earlier call of the same sizes returned)."""
+        if out is not None:
+            return out
+        f32 = dict(dtype=torch.float32, device=self.device)
+        out = {n: torch.zeros(T, **f32) for n in ("logp", "entropy", "lse")}
+        out["stats"] = torch.zeros(T, 4, **f32)
+        out["top_ids"] = torch.full((T, top_k), -1, dtype=torch.int32, device=self.device)
+        out["top_logp"] = torch.zeros(T, top_k, **f32)
+        return out
+
+    def _score_call(self, logits, dtype, V, stride, target, n_tokens_dev, top_k, out, lo, hi):
+        prm = B.LogprobParams(hi - lo, V, dtype, stride, top_k, 0, self.loss_params.temperature)
+        part = {n: v[lo:hi] for n, v in out.items()}
+        B.token_logprobs(prm, logits, target, n_tokens_dev, part["logp"] if target is not None else None, part["entropy"],
+                         part["lse"], part["top_ids"] if top_k else None, part["top_logp"] if top_k else None,
+                         part["stats"], self.status)
+
+    def score(self, logits, target=None, top_k=0, row_stride=None, n_tokens_dev=None, out=None):
+        """Log-probs of the given tokens under the policy that made `logits` [T_max, V] (with the temperature of the
+        loss), their entropy and top_k alternatives: a dict of logp, entropy, lse [T_max], top_ids, top_logp
+        [T_max, top_k] and stats [T_max, 4] (for score_backward).  logp of a frozen policy is what loss() takes as
+        logp_old or logp_ref.  Rows past the token count (the packer's, or n_tokens_dev) are left as they were."""
+        out = self._score_buffers(self.T_max, top_k, out)
+        self._score_call(logits, self.loss_params.dtype, self.V, self.V if row_stride is None else row_stride, target,
+                         self.counts[3:4] if n_tokens_dev is None else n_tokens_dev, top_k, out, 0, self.T_max)
+        return out
+
+    def score_backward(self, logits, target, scored, dlogp=None, dentropy=None, dlogits=None, row_stride=None,
+                       n_tokens_dev=None):
+        """Gradient with respect to `logits` of a loss with the per-token derivatives dlogp and dentropy (f32 [T_max], either
+        may be None); `scored` is what score() returned.  Returns dlogits (`logits` itself for in place)."""
+        if dlogits is None:
+            dlogits = torch.zeros_like(logits)
+        stride = self.V if row_stride is None else row_stride
+        prm = B.LogprobParams(self.T_max, self.V, self.loss_params.dtype, stride, 0, 0, self.loss_params.temperature)
+        B.token_logprobs_backward(prm, logits, target, self.counts[3:4] if n_tokens_dev is None else n_tokens_dev,
+                                  scored["stats"], dlogp, dentropy, dlogits, self.status)
+        return dlogits
+
+    def score_hidden_i8(self, hidden, W_q, W_scale, target=None, top_k=0, n_tokens_dev=None, chunk_tokens=2048, out=None):
+        """The same scores from hidden states [T_max, H] (bf16 or f32, rows on 16 bytes) and a frozen policy's LM-head in
+        8 bits (quantize_rows_i8 of its [V, H] weight): rows quantised per token, product on the tensor cores, scores.
+        The tokens are taken chunk_tokens at a time through an f32 logits scratch of that many rows that this object
+        keeps; the whole [T_max, V] is never formed."""
+        T, H = hidden.shape
+        if T != self.T_max:
+            raise ValueError("hidden has %d rows, T_max is %d" % (T, self.T_max))
+        out = self._score_buffers(T, top_k, out)
+        if T == 0:
+            return out
+        V, C = W_scale.numel(), min(chunk_tokens, T)
+        ldq, ldv = (H + 15) // 16 * 16, (V + 3) // 4 * 4
+        need = (C, ldv, ldq)
+        if getattr(self, "_score_scratch_shape", None) != need:
+            self._score_scratch = (torch.zeros(C, ldv, dtype=torch.float32, device=self.device),
+                                   torch.zeros(C, ldq, dtype=torch.int8, device=self.device),
+                                   torch.zeros(C, dtype=torch.float32, device=self.device))
+            self._score_scratch_shape = need
+        logits, q, q_scale = self._score_scratch
+        T_dev = self.counts[3:4] if n_tokens_dev is None else n_tokens_dev
+        left = torch.clamp(T_dev - torch.arange(0, T, C, dtype=torch.int32, device=self.device), 0, C).to(torch.int32)
+        dtype = B.BF16 if hidden.dtype is torch.bfloat16 else B.F32
+        for i, lo in enumerate(range(0, T, C)):
+            hi, n = min(lo + C, T), left[i:i + 1]
+            B.quantize_rows_i8(B.QuantizeParams(hi - lo, H, dtype, hidden.stride(0), ldq), hidden[lo:hi], q, q_scale, n, self.status)
+            B.linear_i8(B.LinearI8Params(hi - lo, V, H, ldq, W_q.stride(0), ldv, B.F32), q, q_scale, W_q, W_scale, logits, n,
+                        self.status)
+            self._score_call(logits, B.F32, V, ldv, None if target is None else target[lo:hi], n, top_k, out, lo, hi)
+        return out
 
     def step_from_host(self, batch_host, token_host, dev_tokens, seed=0, step=0, dlogits=None):
         """The whole path from HOST buffers: copies the batch inputs and the token inputs (logits, targets,

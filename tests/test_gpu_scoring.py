@@ -1,0 +1,615 @@
+"""The scoring operators on the GPU against the float64 oracle.
+
+Tolerances.  u = 2^-24 is half an f32 step, relative.  A term e = 2^((z - m) c) carries the roundings of z - m, of c and of
+the product (3 u |x| for x = (z - m)/tau) and the 2-ulp exponential (4 u); a thread adds n of them one after the other and
+rescales its sums at most once per vector (5 u each: difference, product, exponential, two products), the joins of at most
+512 partial sums add 16 more roundings.  So S = sum e has a relative error of at most
+    eS = (3 E|x| + 3 + adds + 5 rescales + 16) u,   E|x| = sum p |x|,
+which is the absolute error of l = ln S besides l's own rounding; Q/S = -E|x| carries twice that.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import scoring
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2603_04135_b200 import binding
+    return binding
+
+
+def pad16(n, elem):
+    per = 16 // elem
+    return (n + per - 1) // per * per
+
+
+GUARD = 64
+
+
+class Fwd:
+    """Buffers of one forward call, every output between guard bands."""
+
+    def __init__(self, B, z, V, target, k, tau, variant=0, n_dev=None, status=None, skip=()):
+        T = z.shape[0]
+        self.T, self.k = T, k
+        f32 = dict(dtype=torch.float32, device="cuda")
+        self.raw = {n: torch.full((T * w + 2 * GUARD,), -7.5, **f32) for n, w in
+                    dict(logp=1, entropy=1, lse=1, stats=4, top_logp=k).items()}
+        self.raw["top_ids"] = torch.full((T * k + 2 * GUARD,), -77, dtype=torch.int32, device="cuda")
+        o = {n: r[GUARD:r.numel() - GUARD] for n, r in self.raw.items()}
+        self.status = torch.zeros(1, dtype=torch.int32, device="cuda") if status is None else status
+        prm = B.LogprobParams(T, V, B.BF16 if z.dtype is torch.bfloat16 else B.F32, z.stride(0), k, variant, tau)
+        g = lambda n: None if n in skip else o[n]
+        B.token_logprobs(prm, z, target, n_dev, g("logp") if target is not None else None, g("entropy"), g("lse"),
+                         o["top_ids"] if k else None, o["top_logp"] if k else None, g("stats"), self.status)
+        torch.cuda.synchronize()
+        self.dev = o
+        self.stats = o["stats"]
+
+    def host(self):
+        for n, r in self.raw.items():                                # nothing is written outside the arrays
+            want = -77 if n == "top_ids" else -7.5
+            assert bool((r[:GUARD] == want).all()) and bool((r[r.numel() - GUARD:] == want).all()), n
+        o = {n: v.cpu().numpy() for n, v in self.dev.items()}
+        o["stats"] = o["stats"].reshape(self.T, 4)
+        o["top_ids"], o["top_logp"] = (o[n].reshape(self.T, self.k) for n in ("top_ids", "top_logp"))
+        return o
+
+
+def row_eps(z, tau, V, variant):
+    """eS of each row (see above)."""
+    with np.errstate(all="ignore"):
+        m = z.max(axis=1, keepdims=True)
+        x = np.where(z > -np.inf, (z - m) / tau, 0.0)
+        e = np.where(z > -np.inf, np.exp(x), 0.0)
+        ex = np.abs(e * x).sum(1) / np.maximum(e.sum(1), 1e-300)
+    threads = 32 if (variant == 32 or (variant == 0 and V <= 4096)) else 128
+    n = math.ceil(V / threads)
+    return (3 * ex + 3 + n + 5 * n + 16) * U, ex, e.sum(1)
+
+
+def check(got, want, z, target, tau, V, k, variant=0, rows=None):
+    eS, ex, S = row_eps(z, tau, V, variant)
+    rows = range(z.shape[0]) if rows is None else rows
+    for t in rows:
+        m = z[t].max()
+        l = math.log(S[t]) if S[t] > 0 and math.isfinite(S[t]) else 0.0
+
+        def near(a, b, tol, what):
+            if abs(b) > 3.4028235677973366e38:                       # 2^128 - 2^103: rounds to an infinity in f32
+                b = math.copysign(math.inf, b)
+            if math.isnan(b):
+                assert math.isnan(a), (what, t, a, b)
+            elif math.isinf(b):
+                assert a == b, (what, t, a, b)
+            else:
+                assert abs(a - b) <= tol, (what, t, a, b, abs(a - b), tol)
+        base = eS[t] + 4 * U * abs(l)
+        near(got["lse"][t], want["lse"][t], base + 3 * U * abs(m) / tau + U * abs(want["lse"][t]), "lse")
+        near(got["entropy"][t], want["entropy"][t], base + ex[t] * (2 * eS[t] + 6 * U), "entropy")
+        if target is not None and math.isfinite(m):
+            d = abs(z[t, target[t]] - m) / tau if math.isfinite(z[t, target[t]]) else 0.0
+            near(got["logp"][t], want["logp"][t], base + 4 * U * d + U * abs(want["logp"][t]) if math.isfinite(want["logp"][t]) else 0, "logp")
+        elif target is not None:
+            near(got["logp"][t], want["logp"][t], 0, "logp")
+        assert list(got["top_ids"][t]) == list(want["top_ids"][t]), (t, got["top_ids"][t], want["top_ids"][t])
+        for j in range(k):
+            w = want["top_logp"][t, j]
+            near(got["top_logp"][t, j], w, base + (5 * U * (abs(w) + abs(l)) if math.isfinite(w) else 0), "top_logp")
+
+
+def make(T, V, dtype, seed, sigma=2.0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    z = torch.empty(T, pad16(V, 2 if dtype == "bf16" else 4), dtype=DT[dtype], device="cuda").normal_(0.0, sigma, generator=g)
+    y = torch.randint(0, V, (T,), generator=g, device="cuda", dtype=torch.int32)
+    return z, y
+
+
+def run(B, z, V, y, k, tau, variant=0):
+    got = Fwd(B, z, V, y, k, tau, variant).host()
+    zh = z[:, :V].double().cpu().numpy()
+    yh = None if y is None else y.cpu().numpy()
+    check(got, scoring.token_logprobs(zh, yh, k, tau), zh, yh, tau, V, k, variant)
+    return got
+
+
+# ---- forward ---------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T, V, k, tau", [
+    (1, 1, 1, 1.0), (3, 2, 5, 1.0), (2, 7, 7, 0.5), (5, 8, 3, 1.0), (9, 9, 0, 2.0), (17, 31, 32, 1.0), (4, 33, 32, 1.0),
+    (33, 255, 20, 0.7), (70, 1021, 5, 0.7), (8, 1024, 8, 1.0), (3, 2048, 20, 1.0), (3, 4095, 20, 1.3), (3, 4104, 20, 1.0),
+    (5, 8192, 32, 1.0), (2, 32001, 20, 1.0), (300, 5003, 4, 1.0), (1, 151936, 20, 1.0), (3, 151936, 32, 0.8)])
+def test_forward(B, T, V, k, tau, dtype):
+    z, y = make(T, V, dtype, T * 1000 + V)
+    run(B, z, V, y, k, tau)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("variant", [32, 10128, 10256, 10512, 20128, 20256, 20512, 40128, 40256, 40512, 80128, 80256, 80512])
+def test_every_launch_shape(B, variant, dtype):
+    for T, V in ((3, 5003), (2, 40), (1, 3)):                        # fewer vectors than CTAs too
+        z, y = make(T, V, dtype, V)
+        run(B, z, V, y, 20, 0.9, variant)
+
+
+def special_rows(V, dtype):
+    """Rows where a softmax or a selection goes wrong, as f32 [n, V]."""
+    g = torch.Generator().manual_seed(V)
+    low = torch.finfo(DT[dtype]).min
+    rnd = torch.empty(V).normal_(0, 2, generator=g)
+    rows = []
+    rows.append(torch.full((V,), -math.inf))                                    # a mask that leaves nothing
+    rows.append(torch.full((V,), float(low)))                                   # nothing but the type's lowest value
+    rows.append(torch.where(torch.rand(V, generator=g) < 0.9, torch.tensor(-math.inf), rnd))
+    rows.append(torch.where(torch.rand(V, generator=g) < 0.9, torch.tensor(float(low)), rnd))
+    r = torch.full((V,), -math.inf); r[V // 2] = 1.5; rows.append(r)            # one entry
+    r = torch.full((V,), float(low)); r[V - 1] = 3.0; rows.append(r)
+    r = rnd.clone(); r[V // 3] = math.nan; rows.append(r)
+    r = rnd.clone(); r[V - 1] = math.inf; rows.append(r)
+    r = torch.full((V,), -math.inf); r[0] = math.nan; rows.append(r)
+    rows.append(torch.zeros(V))                                                 # all tied
+    r = torch.zeros(V); r[::2] = -0.0; rows.append(r)                           # -0 ties with +0
+    rows.append(torch.full((V,), -3.25))
+    rows.append(torch.arange(V).float() / 7)                                    # the maximum grows all the way
+    rows.append(-torch.arange(V).float() / 7)
+    rows.append(torch.randint(-2, 3, (V,), generator=g).float())                # a handful of values
+    rows.append((torch.arange(V) % 37).float())
+    r = rnd * 0.01; r[: max(1, V // 2)] += 5; rows.append(r)                    # half of the row far above the rest
+    r = torch.zeros(V); r[torch.arange(V) % (512 * 8) < 24] = 1; r += rnd * 0.1; rows.append(r)   # three threads hold the large ones
+    r = torch.zeros(V); r[torch.arange(V) % (256 * 4) < 16] = 1; r += rnd * 0.1; rows.append(r)
+    r = torch.zeros(V); r[torch.arange(V) % (32 * 8) < 8] = 4; r += torch.arange(V) * 1e-3; rows.append(r)
+    rows.append(rnd * 1e4)                                                      # large magnitudes
+    rows.append(rnd + 3e4)
+    rows.append(rnd * 1e37)
+    rows.append(rnd * 1e-38)
+    return torch.stack(rows)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V, k, variant", [(9, 4, 0), (1000, 20, 0), (4099, 32, 0), (8200, 5, 0), (20000, 20, 10128), (20003, 20, 0),
+                                           (20003, 32, 10512), (20003, 7, 40256), (20003, 20, 80128), (20003, 32, 32)])
+def test_special_rows(B, V, k, variant, dtype):
+    rows = special_rows(V, dtype)
+    z = torch.zeros(rows.shape[0], pad16(V, 2 if dtype == "bf16" else 4), dtype=DT[dtype], device="cuda")
+    z[:, :V] = rows.to(DT[dtype])
+    y = torch.arange(rows.shape[0], dtype=torch.int32, device="cuda") * 7919 % V
+    run(B, z, V, y, k, 1.0, variant)
+    run(B, z, V, y, k, 0.25, variant)
+
+
+def test_forward_is_deterministic_and_stream_ordered(B):
+    z, y = make(64, 20003, "bf16", 5)
+    a = Fwd(B, z, 20003, y, 20, 1.0).host()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        b = Fwd(B, z, 20003, y, 20, 1.0).host()
+    for n in a:
+        assert np.array_equal(a[n].view(np.int32), b[n].view(np.int32)), n
+
+
+@pytest.mark.parametrize("V", [1021, 20000])
+def test_token_count_on_the_device_leaves_later_rows(B, V):
+    z, y = make(40, V, "bf16", 1)
+    z[23:] = math.nan
+    y[23:] = -5
+    for n in (0, 1, 23, 40):
+        n_dev = torch.tensor([n], dtype=torch.int32, device="cuda")
+        f = Fwd(B, z, V, y, 4, 1.0, n_dev=n_dev)
+        o = f.host()
+        m = min(n, 23)
+        zh = z[:m, :V].double().cpu().numpy()
+        check({k: v[:m] for k, v in o.items()}, scoring.token_logprobs(zh, y[:m].cpu().numpy(), 4, 1.0), zh, y[:m].cpu().numpy(), 1.0, V, 4)
+        for name in ("logp", "entropy", "lse", "stats", "top_logp"):
+            assert (o[name][n:] == -7.5).all(), name
+        assert (o["top_ids"][n:] == -77).all()
+        assert f.status.item() == (0 if n <= 23 else B.STATUS_BAD_TARGET)
+    many = torch.tensor([1000], dtype=torch.int32, device="cuda")          # more than T_max: T_max rows
+    assert np.isfinite(Fwd(B, z[:23], V, y[:23], 4, 1.0, n_dev=many).host()["logp"]).all()
+
+
+@pytest.mark.parametrize("V", [1021, 20000])
+def test_bad_targets_and_absent_outputs(B, V):
+    z, y = make(6, V, "f32", 2)
+    ref = Fwd(B, z, V, y, 3, 1.0).host()
+    y2 = y.clone()
+    y2[1], y2[4] = -1, V
+    f = Fwd(B, z, V, y2, 3, 1.0)
+    o = f.host()
+    assert f.status.item() == B.STATUS_BAD_TARGET and o["logp"][1] == 0 and o["logp"][4] == 0
+    keep = [0, 2, 3, 5]
+    assert np.array_equal(o["logp"][keep], ref["logp"][keep])
+    for n in ("entropy", "lse", "top_ids", "top_logp", "stats"):
+        assert np.array_equal(o[n], ref[n]), n
+    o = Fwd(B, z, V, None, 3, 1.0).host()                                  # no tokens given
+    assert (o["logp"] == -7.5).all() and np.array_equal(o["top_ids"], ref["top_ids"])
+    o = Fwd(B, z, V, y, 0, 1.0, skip=("entropy", "stats")).host()
+    assert (o["entropy"] == -7.5).all() and (o["stats"] == -7.5).all() and np.array_equal(o["logp"], ref["logp"])
+
+
+def test_rows_past_4_gib(B):
+    V, T = 151936, 9000                                                    # 5.5 GB of f32 logits
+    z = torch.zeros(T, V, dtype=torch.float32, device="cuda")
+    y = torch.full((T,), V - 1, dtype=torch.int32, device="cuda")
+    z[8999, V - 1] = 20.0
+    z[8998, 17] = 20.0
+    f = Fwd(B, z, V, y, 2, 1.0)
+    o = f.host()
+    l = math.log1p((V - 1) * math.exp(-20.0))
+    assert abs(o["logp"][8999] + l) < 1e-4 and abs(o["logp"][8998] + l + 20) < 1e-4 and abs(o["lse"][0] - math.log(V)) < 1e-4
+    assert o["top_ids"][8999].tolist() == [V - 1, 0] and o["top_ids"][8998].tolist() == [17, 0] and o["top_ids"][5].tolist() == [0, 1]
+    d = torch.zeros_like(z)
+    a = torch.ones(T, device="cuda")
+    B.token_logprobs_backward(B.LogprobParams(T, V, B.F32, V, 0, 0, 1.0), z, y, None, f.stats, a, None, d)
+    p = math.exp(o["logp"][8998] + 20)
+    assert abs(d[8998, 17].item() + p) < 1e-4 and abs(d[8998, V - 1].item() - 1) < 1e-4 and abs(d[8999, V - 1].item() - (1 - p)) < 1e-4
+
+
+# ---- backward --------------------------------------------------------------------------------------
+def check_grad(g, want, z, target, a, b, tau, dtype, V, variant=0):
+    """|error| <= p-relative part (the exponent: 3 u |x| + l's own error and rounding, the exponential) x |dz|, plus the
+    bracket's roundings x p, plus the token's own element, plus the output's rounding (half a step)."""
+    eS, ex, S = row_eps(z, tau, V, variant)
+    with np.errstate(all="ignore"):
+        m = z.max(axis=1, keepdims=True)
+        x = np.where(z > -np.inf, np.maximum((z - m) / tau, -1e6), 0.0)
+        l = np.log(np.maximum(S, 1e-300))[:, None]
+        p = np.where(z > -np.inf, np.exp(x - l), 0.0)
+        plnp = np.where(p > 0, p * np.where(p > 0, x - l, 0.0), 0.0)
+    H = -plnp.sum(1, keepdims=True)
+    aa = np.abs(a)[:, None] if a is not None else 0.0
+    bb = np.abs(b)[:, None] if b is not None else 0.0
+    e = eS[:, None]
+    bracket = aa + bb * (np.abs(np.where(p > 0, x - l, 0.0)) + H)
+    tol = p / tau * (bracket * (3 * U * np.abs(x) + e + 4 * U * np.abs(l) + 16 * U)
+                     + bb * (8 * U * (np.abs(x) + np.abs(l) + H) + 3 * e + ex[:, None] * (2 * e + 6 * U)) + 4 * U * aa)
+    if a is not None:
+        tol[np.arange(len(target)), target] += 6 * U * np.abs(a) / tau
+    half = 2.0 ** -8 if dtype == "bf16" else U
+    # a probability below the smallest normal f32, 2^-126, counts as 0: the element then lacks p x bracket / tau
+    tol = tol * (1 + half) + half * np.abs(want) + 2.0 ** -126 * (1 + bracket / tau)
+    bad = np.abs(g - want) > tol
+    assert not bad.any(), (np.argwhere(bad)[:3], g[bad][:3], want[bad][:3], tol[bad][:3])
+
+
+def backward(B, z, V, y, a, b, tau, in_place=False, n_dev=None, status=None):
+    f = Fwd(B, z, V, y, 0, tau, n_dev=n_dev)
+    out = z if in_place else torch.full_like(z, 9.0)
+    prm = B.LogprobParams(z.shape[0], V, B.BF16 if z.dtype is torch.bfloat16 else B.F32, z.stride(0), 0, 0, tau)
+    B.token_logprobs_backward(prm, z, y, n_dev, f.stats, a, b, out, status)
+    torch.cuda.synchronize()
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T, V, tau, terms", [(1, 1, 1.0, "ab"), (3, 9, 0.5, "ab"), (5, 31, 1.0, "a"), (70, 1021, 0.7, "ab"), (4, 4096, 1.0, "b"),
+                                              (3, 4104, 1.0, "ab"), (2, 16392, 1.3, "ab"), (2, 32001, 1.0, "a"), (2, 151936, 1.0, "ab"), (3, 40, 1.0, "")])
+def test_backward(B, T, V, tau, terms, dtype):
+    z, y = make(T, V, dtype, V + T)
+    a = torch.randn(T, device="cuda") if "a" in terms else None
+    b = torch.randn(T, device="cuda") if "b" in terms else None
+    zh = z[:, :V].double().cpu().numpy()
+    ah, bh = (None if v is None else v.double().cpu().numpy() for v in (a, b))
+    want = scoring.token_logprobs_backward(zh, y.cpu().numpy(), ah, bh, tau)
+    out = backward(B, z, V, y, a, b, tau)
+    check_grad(out[:, :V].double().cpu().numpy(), want, zh, y.cpu().numpy(), ah, bh, tau, dtype, V)
+    assert bool((out[:, V:] == 9.0).all())                                 # the padding of the rows is left alone
+    pad = z[:, V:].clone()
+    same = backward(B, z, V, y, a, b, tau, in_place=True)
+    assert torch.equal(same[:, :V], out[:, :V]) and torch.equal(z[:, V:], pad)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [9, 1000, 8200])
+def test_backward_special_rows(B, V, dtype):
+    rows = special_rows(V, dtype)
+    keep = [i for i in range(rows.shape[0]) if not torch.isnan(rows[i]).any() and not torch.isposinf(rows[i]).any()]
+    rows = rows[keep]
+    z = torch.zeros(rows.shape[0], pad16(V, 2 if dtype == "bf16" else 4), dtype=DT[dtype], device="cuda")
+    z[:, :V] = rows.to(DT[dtype])
+    T = z.shape[0]
+    zh = z[:, :V].double().cpu().numpy()
+    yh = np.array([int(np.argmax(zh[t] > -np.inf)) for t in range(T)])      # a token that the mask allows, where there is one
+    y = torch.tensor(yh, dtype=torch.int32, device="cuda")
+    a, b = torch.randn(T, device="cuda"), torch.randn(T, device="cuda")
+    want = scoring.token_logprobs_backward(zh, yh, a.double().cpu().numpy(), b.double().cpu().numpy(), 1.0)
+    got = backward(B, z, V, y, a, b, 1.0)[:, :V].double().cpu().numpy()
+    assert (got[0] == 0).all() and (got[zh == -np.inf] == 0).all()
+    check_grad(got, want, zh, yh, a.double().cpu().numpy(), b.double().cpu().numpy(), 1.0, dtype, V)
+
+
+def test_backward_of_invalid_rows_is_nan(B):
+    z, y = make(2, 500, "f32", 3)
+    z[0, 7] = math.nan
+    z[1, 9] = math.inf
+    one = torch.ones(2, device="cuda")
+    assert bool(torch.isnan(backward(B, z, 500, y, one, one, 1.0)[:, :500]).all())
+
+
+@pytest.mark.parametrize("V", [500, 20000])
+def test_backward_bad_target_and_token_count(B, V):
+    z, y = make(8, V, "f32", 4)
+    y[2], y[5] = -3, V + 1
+    a = torch.ones(8, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    n_dev = torch.tensor([7], dtype=torch.int32, device="cuda")
+    out = backward(B, z, V, y, a, a, 1.0, n_dev=n_dev, status=status)
+    assert status.item() == B.STATUS_BAD_TARGET
+    assert bool((out[2, :V] == 0).all()) and bool((out[5, :V] == 0).all()) and bool((out[7] == 9.0).all())
+    assert bool((out[0, :V] != 9.0).all())
+
+
+def test_gradient_against_differences(B):
+    """<dz, d> against central differences of the oracle's value: the error of the difference is at most h^2/6 |f'''| with
+    |f'''| <= 6 (sum |a| + |b| (ln V + 6)) for |d| <= 1, tau = 1; h = 2^-8."""
+    T, V, h = 4, 600, 2.0 ** -8
+    z, y = make(T, V, "f32", 11)
+    a, b, d = torch.randn(T), torch.randn(T), torch.rand(T, V) * 2 - 1
+    g = backward(B, z, V, y, a.cuda(), b.cuda(), 1.0)[:, :V].double().cpu()
+    zh, yh = z[:, :V].double().cpu().numpy(), y.cpu().numpy()
+
+    def f(x):
+        r = scoring.token_logprobs(x, yh, 0, 1.0)
+        return (a.double().numpy() * r["logp"] + b.double().numpy() * r["entropy"]).sum()
+    diff = (f(zh + h * d.double().numpy()) - f(zh - h * d.double().numpy())) / (2 * h)
+    bound = h * h * float((a.abs() + b.abs() * (math.log(V) + 6)).sum())
+    assert abs(float((g * d.double()).sum()) - diff) <= bound + 1e-4 * float((a.abs() + b.abs() * 8).sum())
+
+
+# ---- 8-bit product: exact, bit for bit --------------------------------------------------------------
+def f32_product(q, qs, w, ws):
+    acc = (q.double() @ w.double().t()).cpu().numpy()                      # |sum| < 2^31: exact in f64
+    s = (qs.cpu().numpy()[:, None] * ws.cpu().numpy()[None, :]).astype(np.float32)
+    with np.errstate(over="ignore", invalid="ignore"):
+        return (acc.astype(np.float32) * s).astype(np.float32)
+
+
+def codes(rows, K, ld, seed, full=False):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randint(-128, 128, (rows, ld), generator=g, device="cuda", dtype=torch.int32).to(torch.int8)
+
+
+@pytest.mark.parametrize("out_dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M, N, K, variant", [
+    (1, 1, 1, 0), (1, 5, 3, 0), (3, 128, 128, 0), (16, 129, 127, 0), (17, 300, 129, 0), (1, 4096, 2560, 0), (5, 100, 4097, 0),
+    (33, 1000, 640, 0), (64, 4096, 4096, 0), (100, 257, 700, 0), (128, 640, 256, 0), (129, 640, 256, 0), (300, 130, 2000, 0),
+    (257, 20000, 384, 0), (700, 3001, 513, 0), (1003, 5003, 2563, 0), (5000, 700, 200, 0), (1, 151936, 64, 0),
+    (1, 1, 1, 1), (7, 300, 129, 1), (300, 513, 640, 1), (300, 513, 640, 2), (20, 64, 131071, 0), (130, 256, 131071, 1)])
+def test_linear_i8(B, M, N, K, variant, out_dtype):
+    ldx, ldw, ldo = (K + 15) // 16 * 16, (K + 15) // 16 * 16 + 16, N + 3
+    x, w = codes(M, K, ldx, M + K), codes(N, K, ldw, N + K + 1)
+    xs = torch.rand(M, device="cuda") * 0.01
+    ws = torch.rand(N, device="cuda") * 0.01
+    out = torch.full((M + 2, ldo), 5.0, dtype=DT[out_dtype], device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.linear_i8(B.LinearI8Params(M, N, K, ldx, ldw, ldo, B.BF16 if out_dtype == "bf16" else B.F32, variant), x, xs, w, ws, out, status=status)
+    torch.cuda.synchronize()
+    assert status.item() == 0
+    want = torch.from_numpy(f32_product(x[:, :K], xs, w[:, :K], ws)).to(DT[out_dtype])
+    assert torch.equal(out[:M, :N].cpu(), want)
+    assert bool((out[:M, N:] == 5.0).all()) and bool((out[M:] == 5.0).all())
+
+
+@pytest.mark.parametrize("M, variant", [(1, 2), (16, 2), (40, 2), (100, 2), (256, 1), (256, 2)])
+def test_linear_i8_extreme_sums(B, M, variant):
+    """Every product is (-128)^2 or -128 * 127: the sums reach the ends of int32."""
+    K, N = 131071, 130
+    ld = 131072
+    x = torch.full((M, ld), -128, dtype=torch.int8, device="cuda")
+    w = torch.full((N, ld), -128, dtype=torch.int8, device="cuda")
+    w[1::2] = 127
+    out = torch.zeros(M, N, device="cuda")
+    one = torch.ones(max(M, N), device="cuda")
+    B.linear_i8(B.LinearI8Params(M, N, K, ld, ld, N, B.F32, variant), x, one, w, one, out)
+    assert bool((out[:, 0::2] == np.float32(16384 * K)).all()) and bool((out[:, 1::2] == np.float32(-128 * 127 * K)).all())
+
+
+@pytest.mark.parametrize("M, variant", [(40, 0), (300, 1), (300, 2)])
+def test_linear_i8_token_count_on_the_device(B, M, variant):
+    N, K = 300, 256
+    x, w = codes(M, K, K, 1), codes(N, K, K, 2)
+    xs, ws = torch.rand(M, device="cuda"), torch.rand(N, device="cuda")
+    want = torch.from_numpy(f32_product(x, xs, w, ws))
+    for n in (0, 1, M // 2, M, M + 9):
+        n_dev = torch.tensor([n], dtype=torch.int32, device="cuda")
+        out = torch.full((M, N), 5.0, device="cuda")
+        B.linear_i8(B.LinearI8Params(M, N, K, K, K, N, B.F32, variant), x, xs, w, ws, out, n_dev)
+        m = min(n, M)
+        assert torch.equal(out[:m].cpu(), want[:m]) and bool((out[m:] == 5.0).all())
+
+
+def test_linear_i8_scales_that_are_no_numbers(B):
+    x, w = codes(4, 64, 64, 1), codes(32, 64, 64, 2)
+    xs, ws = torch.ones(4, device="cuda"), torch.ones(32, device="cuda")
+    xs[1], ws[3] = math.nan, math.inf
+    out = torch.zeros(4, 32, device="cuda")
+    B.linear_i8(B.LinearI8Params(4, 32, 64, 64, 64, 32, B.F32), x, xs, w, ws, out)
+    nan = torch.isnan(out)
+    assert bool(nan[1].all()) and not bool(nan[0, :3].any()) and bool(torch.isinf(out[0, 3]) | torch.isnan(out[0, 3]))
+
+
+@pytest.mark.parametrize("variant", [101, 102])
+def test_linear_i8_bounded_waits(B, variant):
+    x, w = codes(200, 256, 256, 1), codes(300, 256, 256, 2)
+    xs, ws = torch.ones(200, device="cuda"), torch.ones(300, device="cuda")
+    out = torch.zeros(200, 300, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.linear_i8(B.LinearI8Params(200, 300, 256, 256, 256, 300, B.F32, variant), x, xs, w, ws, out, status=status)
+    torch.cuda.synchronize()
+    assert status.item() == B.STATUS_TIMEOUT
+    status.zero_()                                                          # the device goes on working
+    B.linear_i8(B.LinearI8Params(200, 300, 256, 256, 256, 300, B.F32, variant - 100), x, xs, w, ws, out, status=status)
+    assert status.item() == 0 and torch.equal(out.cpu(), torch.from_numpy(f32_product(x, xs, w, ws)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M, K", [(1, 1), (3, 7), (5, 8), (2, 129), (9, 2560), (4, 4097), (2, 30001), (300, 64)])
+def test_quantize_rows(B, M, K, dtype):
+    ldx, ldq = pad16(K, 2 if dtype == "bf16" else 4), (K + 15) // 16 * 16 + 16
+    x = torch.empty(M, ldx, device="cuda").normal_(0, 3).to(DT[dtype])
+    x[:, K:] = math.nan                                                     # the rows' padding is not looked at
+    if M > 2:
+        x[0, :K] = 0
+        x[1, K // 2] = math.inf
+        x[2, :K] = torch.arange(K, device="cuda").to(DT[dtype]) * 0.5
+    if M > 4:
+        x[3, K - 1] = math.nan
+        x[4, :K] = 1e-42                                                    # the scale underflows
+    q = torch.full((M + 1, ldq), 99, dtype=torch.int8, device="cuda")
+    s = torch.full((M + 1,), 5.0, device="cuda")
+    B.quantize_rows_i8(B.QuantizeParams(M, K, B.BF16 if dtype == "bf16" else B.F32, ldx, ldq), x, q, s)
+    wq, ws = scoring.quantize_rows_i8(x[:, :K].float().cpu().numpy())
+    assert np.array_equal(q[:M, :K].cpu().numpy(), wq) and np.array_equal(s[:M].cpu().numpy(), ws, equal_nan=True)
+    assert bool((q[:M, K:] == 99).all()) and bool((q[M] == 99).all()) and s[M].item() == 5.0
+    n_dev = torch.tensor([M // 2], dtype=torch.int32, device="cuda")
+    q.fill_(99)
+    B.quantize_rows_i8(B.QuantizeParams(M, K, B.BF16 if dtype == "bf16" else B.F32, ldx, ldq), x, q, s, n_dev)
+    assert np.array_equal(q[:M // 2, :K].cpu().numpy(), wq[:M // 2]) and bool((q[M // 2:] == 99).all())
+
+
+# ---- together, as a step uses them ------------------------------------------------------------------
+def make_step(V, T, dtype="f32", n=None):
+    from paper_2603_04135_b200.step import DppoStep
+    st = DppoStep(2, 2, 512, 4, 0.0, 0.0, V, dtype, T, temperature=0.9)
+    st.counts[3] = T if n is None else n
+    return st
+
+
+@pytest.mark.parametrize("T, n, chunk", [(50, 50, 16), (50, 33, 16), (300, 290, 2048), (1, 1, 2048)])
+def test_step_scores_hidden_states(B, T, n, chunk):
+    """hidden -> codes -> product -> scores, against the oracle on the same codes: the f32 logits carry 3 roundings."""
+    from paper_2603_04135_b200.step import quantize_rows_i8
+    H, V, k = 136, 1003, 6
+    st = make_step(V, T, n=n)
+    hidden = torch.randn(T, H, device="cuda").to(torch.bfloat16)
+    W = torch.randn(V, H, device="cuda").to(torch.bfloat16) / math.sqrt(H) * 2
+    Wq, Ws = quantize_rows_i8(W)
+    y = torch.randint(0, V, (T,), device="cuda", dtype=torch.int32)
+    got = st.score_hidden_i8(hidden, Wq, Ws, y, top_k=k, chunk_tokens=chunk)
+    again = st.score_hidden_i8(hidden, Wq, Ws, y, top_k=k, chunk_tokens=chunk, out={x: v.clone() for x, v in got.items()})
+    assert st.status.item() == 0
+    q, s = scoring.quantize_rows_i8(hidden.float().cpu().numpy())
+    wq, ws = scoring.quantize_rows_i8(W.float().cpu().numpy())
+    assert np.array_equal(wq, Wq.cpu().numpy())
+    z = f32_product(torch.from_numpy(q).cuda(), torch.from_numpy(s), torch.from_numpy(wq).cuda(), torch.from_numpy(ws)).astype(np.float64)[:n]
+    want = scoring.token_logprobs(z, y.cpu().numpy(), k, 0.9)
+    o = {x: v.cpu().numpy() for x, v in got.items()}
+    check({x: v[:n] for x, v in o.items()}, want, z, y.cpu().numpy(), 0.9, V, k)
+    assert (o["logp"][n:] == 0).all() and (o["top_ids"][n:] == -1).all()
+    for x in got:
+        assert torch.equal(got[x], again[x]), x
+
+
+def test_step_scores_feed_the_loss_and_its_gradient(B):
+    """score() of the current policy as logp_old makes every ratio 1 in the loss sweep; score_backward with
+    dlogp = -A W is then the gradient that the loss sweep writes (beta = 0)."""
+    from paper_2603_04135_b200 import synth
+    from paper_2603_04135_b200.step import DppoStep
+    w = synth.WORKLOADS["config0"]
+    batch = synth.make_batch(w, 0)
+    T_max = int(batch.loss_len.sum())
+    st = DppoStep(w.P, w.G, w.L_row, w.N_win, 0.0, 0.0, w.V, w.dtype, T_max, beta=0.0)
+    st.set_batch(batch.rewards, batch.unit_len, batch.loss_len)
+    st.prune_pack()
+    T = st.n_tokens()
+    tok = synth.make_token_inputs(w, T_max, 0, device="cuda:0")
+    scored = st.score(tok.logits, tok.target, top_k=4)
+    d_loss = torch.zeros_like(tok.logits)
+    st.loss(tok.logits, tok.target, scored["logp"], scored["logp"], d_loss)
+    assert st.status.item() == 0
+    assert torch.allclose(st.logp_out[:T], scored["logp"][:T], rtol=0, atol=2e-5) and torch.allclose(st.lse_out[:T], scored["lse"][:T], rtol=0, atol=2e-5)
+    cu = st.cu_seqlens.cpu().numpy()
+    order = st.order.cpu().numpy()
+    dlogp = torch.zeros(T_max)
+    for s in range(int(st.counts[0])):
+        lo, hi, unit = int(cu[s]), int(cu[s + 1]), int(order[s])
+        if hi > lo:
+            dlogp[lo:hi] = -float(st.adv[unit]) * float(st.w_seq[unit]) / (hi - lo)
+    d = st.score_backward(tok.logits, tok.target, scored, dlogp=dlogp.cuda())
+    # both are f32 evaluations of the same expression: the ratio exp(logp - logp_old) is 1 within 2e-5
+    scale = float(dlogp.abs().max())
+    assert float((d[:T] - d_loss[:T]).abs().max()) <= 4e-5 * scale
+    st.score_backward(tok.logits, tok.target, scored, dlogp=dlogp.cuda(), dlogits=tok.logits)        # in place
+    assert torch.equal(tok.logits[:T], d[:T])
+
+
+def test_captured_and_replayed(B):
+    V, T, H, k = 4001, 24, 256, 5
+    ld = pad16(V, 4)
+    x = torch.randn(T, H, device="cuda")
+    W = codes(V, H, H, 3)
+    ws = torch.rand(V, device="cuda") * 1e-3
+    f32 = dict(dtype=torch.float32, device="cuda")
+    q, s, z, dz = torch.zeros(T, H, dtype=torch.int8, device="cuda"), torch.zeros(T, **f32), torch.zeros(T, ld, **f32), torch.zeros(T, ld, **f32)
+    y = torch.randint(0, V, (T,), device="cuda", dtype=torch.int32)
+    logp, H_, lse, stats = torch.zeros(T, **f32), torch.zeros(T, **f32), torch.zeros(T, **f32), torch.zeros(T, 4, **f32)
+    ids, tl = torch.zeros(T, k, dtype=torch.int32, device="cuda"), torch.zeros(T, k, **f32)
+    a = torch.ones(T, **f32)
+
+    def work():
+        B.quantize_rows_i8(B.QuantizeParams(T, H, B.F32, H, H), x, q, s)
+        B.linear_i8(B.LinearI8Params(T, V, H, H, H, ld, B.F32), q, s, W, ws, z)
+        prm = B.LogprobParams(T, V, B.F32, ld, k, 0, 1.0)
+        B.token_logprobs(prm, z, y, None, logp, H_, lse, ids, tl, stats)
+        B.token_logprobs_backward(prm, z, y, None, stats, a, a, dz)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        work()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work()
+    for seed in (1, 2):
+        torch.manual_seed(seed)
+        x.copy_(torch.randn(T, H, device="cuda"))
+        outs = (q, s, z, logp, H_, lse, ids, tl, dz)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [o.clone() for o in outs]
+        for o in outs:
+            o.zero_()
+        work()
+        torch.cuda.synchronize()
+        for r, o in zip(replayed, outs):
+            assert torch.equal(r, o)
+
+
+def test_calls_on_two_streams_at_once(B):
+    """Nothing is shared between calls: the same work on two streams at a time gives what it gives alone."""
+    V, T, K, N = 20003, 37, 640, 3000
+    z, y = make(T, V, "bf16", 9)
+    x, w = codes(T, K, K, 1), codes(N, K, K, 2)
+    xs, ws = torch.rand(T, device="cuda"), torch.rand(N, device="cuda")
+
+    def work():
+        o = torch.zeros(T, N, device="cuda")
+        logp, ids, tl = torch.zeros(T, device="cuda"), torch.zeros(T, 8, dtype=torch.int32, device="cuda"), torch.zeros(T, 8, device="cuda")
+        return o, logp, ids, tl
+
+    def go(b):
+        B.linear_i8(B.LinearI8Params(T, N, K, K, K, N, B.F32), x, xs, w, ws, b[0])
+        B.token_logprobs(B.LogprobParams(T, V, B.BF16, z.stride(0), 8, 0, 1.0), z, y, None, b[1], None, None, b[2], b[3], None)
+    alone = work()
+    go(alone)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    bufs = [[work() for _ in range(8)] for _ in streams]
+    torch.cuda.synchronize()
+    for i in range(8):
+        for s, bs in zip(streams, bufs):
+            with torch.cuda.stream(s):
+                go(bs[i])
+    torch.cuda.synchronize()
+    for bs in bufs:
+        for b in bs:
+            for got, want in zip(b, alone):
+                assert torch.equal(got, want)
