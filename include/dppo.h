@@ -394,8 +394,8 @@ int dppo_token_logprobs_backward(const dppo_logprob_params* p, const void* logit
  * Matrix product in 8-bit integers with one scale per token and one per output channel: the LM-head (or any
  * projection) of a frozen policy whose log-probs are only scored.
  *
- * Quantisation of rows, symmetric: s = fl32(max_k |x_k| / 127), q_k = clamp(rint(fl32(x_k / s)), -127, 127) (ties to
- * even); s = 0 gives q = 0.  A row with a NaN or an infinity gets s = NaN, q = 0, so that products with it are NaN.
+ * Quantisation of rows, symmetric: s = fl32(max_k |x_k| fl32(1/127)), q_k = clamp(rint(fl32(x_k / s)), -127, 127)
+ * (ties to even); s = 0 gives q = 0.  A row with a NaN or an infinity gets s = NaN, q = 0, so that products with it are NaN.
  */
 typedef struct {
     int64_t rows_max;       /* rows of x                                                             */

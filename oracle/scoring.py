@@ -63,7 +63,7 @@ def quantize_rows_i8(x):
     x = x.astype(np.float32)
     amax = np.abs(x).max(axis=1)
     with np.errstate(all="ignore"):
-        s = (amax / np.float32(127.0)).astype(np.float32)
+        s = (amax * (np.float32(1.0) / np.float32(127.0))).astype(np.float32)
         q = np.rint((x / s[:, None]).astype(np.float32))
     fine = np.isfinite(amax)
     live = fine & (s > 0)

@@ -163,13 +163,19 @@ def _arr(x, name, device, dtype, rows, row_elems, stride=None):
     return x.data_ptr()
 
 
+_cuda = None                        # whether there is a CUDA device; asked once
+
+
 def _device():
-    return torch.cuda.current_device() if torch.cuda.is_available() else -1
+    global _cuda
+    if _cuda is None:
+        _cuda = torch.cuda.is_available()
+    return torch.cuda.current_device() if _cuda else -1
 
 
 def _stream(stream):
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
+        return torch.cuda.current_stream().cuda_stream if _device() >= 0 else None
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
     return int(stream)

@@ -450,7 +450,7 @@ quantize_rows_kernel(const QuantArgs a) {
 #pragma unroll
     for (int w = 0; w < kQuantThreads / 32; ++w) amax = max_nan(amax, red[w]);
     const bool fine = amax < INFINITY;
-    const float s = fine ? __fdiv_rn(amax, 127.0f) : __int_as_float(0x7fffffff);
+    const float s = fine ? __fmul_rn(amax, 1.0f / 127.0f) : __int_as_float(0x7fffffff);
     if (tid == 0) a.scale[t] = s;
     const bool live = fine && s > 0.0f;
     for (int i = tid; i < nvec; i += kQuantThreads) {
