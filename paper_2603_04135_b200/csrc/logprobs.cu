@@ -62,17 +62,17 @@ __device__ __forceinline__ void rescale(Part& p, float M, float c) {
     p.S *= f;
     p.m = M;
 }
-__device__ __forceinline__ void join(Part& p, Part o, float c) {
-    const float M = fmaxf(p.m, o.m);
-    rescale(p, M, c);
-    rescale(o, M, c);
-    p.S += o.S; p.Q += o.Q; p.bad |= o.bad;
-}
-__device__ __forceinline__ Part shfl_xor(const Part& p, int o) {
-    Part r;
-    r.m = __shfl_xor_sync(0xffffffffu, p.m, o); r.S = __shfl_xor_sync(0xffffffffu, p.S, o);
-    r.Q = __shfl_xor_sync(0xffffffffu, p.Q, o); r.bad = __shfl_xor_sync(0xffffffffu, p.bad, o);
+// The parts of a warp's lanes as one, in every lane: the maximum first, one rescale per lane, then the sums.
+__device__ __forceinline__ float warp_max_f32(float v) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
     return r;
+}
+__device__ __forceinline__ Part warp_join(Part p, float c) {
+    rescale(p, warp_max_f32(p.m), c);
+    p.S = warp_sum(p.S); p.Q = warp_sum(p.Q);
+    p.bad = __any_sync(0xffffffffu, p.bad);
+    return p;
 }
 
 __device__ __forceinline__ float max_nan(float a, float b) {
@@ -151,6 +151,12 @@ __device__ __forceinline__ float value_of(uint32_t key) {
     return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
 }
 
+// An entry as one number: larger = ahead in the order (value descending, index ascending).
+typedef unsigned long long Entry;
+__device__ __forceinline__ Entry entry_of(float z, int idx) { return (Entry)key_of(z) << 32 | (uint32_t)~idx; }
+__device__ __forceinline__ float entry_value(Entry e) { return value_of((uint32_t)(e >> 32)); }
+__device__ __forceinline__ int entry_index(Entry e) { return (int)~(uint32_t)e; }
+
 template <int kThreads, int kCap> struct TeamShared {
     Part part[kThreads / 32];
     Part row;
@@ -158,10 +164,8 @@ template <int kThreads, int kCap> struct TeamShared {
     int hot[kThreads];
     int n_hot, n_cand, n_le;
     float thr;
-    uint32_t ckey[kCap];
-    int cidx[kCap];
-    uint32_t lkey[kMaxTop];                // the team's own sorted list (joined over a cluster)
-    int lidx[kMaxTop];
+    Entry cand[kCap];
+    Entry list[kMaxTop];                   // the team's own sorted list (joined over a cluster)
     int n_list;
     int red[kThreads / 32];
 };
@@ -170,24 +174,43 @@ template <int kThreads> __device__ __forceinline__ void team_sync() {
     if constexpr (kThreads == 32) __syncwarp(); else __syncthreads();
 }
 
-// k-th largest (1-based) of n keys in shared memory, by one warp: the largest value that at least k keys reach, found bit
-// by bit from the top.  n <= 32 * kPer.
-template <int kPer> __device__ __forceinline__ uint32_t kth_largest(const float* v, int n, int k, int lane) {
-    uint32_t own[kPer];
+// A lower bound, as a key, of the k-th largest (1-based) of 32 * kPer keys (kPer per lane) that at least k of them reach:
+// found bit by bit below the bits that all keys share, by counting; exact to kBits bits of the key (bf16 values have no
+// more than 16, for f32 a slightly low bound costs a few more candidates).
+template <int kPer, int kBits> __device__ __forceinline__ uint32_t kth_largest(const uint32_t (&own)[kPer], int k) {
+    uint32_t hi = own[0], lo = own[0];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) own[i] = (i * 32 + lane) < n ? key_of(v[i * 32 + lane]) : 0u;
-    uint32_t r = 0;
+    for (int i = 1; i < kPer; ++i) { hi = max(hi, own[i]); lo = min(lo, own[i]); }
+    hi = __reduce_max_sync(0xffffffffu, hi); lo = __reduce_min_sync(0xffffffffu, lo);
+    const int top = 31 - __clz(hi ^ lo);                           // -1: all keys alike
+    uint32_t r = top < 0 ? hi : hi & ~((2u << top) - 1u);
 #pragma unroll 1
-    for (int bit = 31; bit >= 0; --bit) {
+    for (int bit = top; bit >= 32 - kBits; --bit) {
         const uint32_t t = r | (1u << bit);
         int cnt = 0;
+        if constexpr (kPer == 1) {
+            cnt = __popc(__ballot_sync(0xffffffffu, own[0] >= t));
+        } else {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) cnt += own[i] >= t ? 1 : 0;
-        cnt = __reduce_add_sync(0xffffffffu, cnt);
+            for (int i = 0; i < kPer; ++i) cnt += own[i] >= t ? 1 : 0;
+            cnt = __reduce_add_sync(0xffffffffu, cnt);
+        }
         if (cnt >= k) r = t;
         if (cnt == k) break;                                       // exactly the k largest reach t: t serves as well
     }
     return r;
+}
+
+// The list of the top k of n entries in shared memory, by the threads tid = 0 .. stride - 1: an entry's place is the number
+// of entries ahead of it.
+__device__ __forceinline__ void rank_entries(const Entry* cand, int n, int k, Entry* list, int tid, int stride) {
+    for (int i = tid; i < n; i += stride) {
+        const Entry e = cand[i];
+        int ahead = 0;
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) ahead += cand[j] > e ? 1 : 0;
+        if (ahead < k) list[ahead] = e;
+    }
 }
 
 // Entries of the row part [v0, v1) (in vectors) + tail [tail0, V) as a team sees them.
@@ -225,7 +248,10 @@ __device__ void select_top(TeamShared<kThreads, kCap>& sh, const Span& sp, int k
     constexpr int kPer = Elems<kBf16>::kPerVec;
     const int lane = tid & 31, warp = tid >> 5;
     if (warp == 0) {
-        const uint32_t t = kth_largest<kThreads / 32>(sh.tmax, kThreads, k, lane);
+        uint32_t own[kThreads / 32];
+#pragma unroll
+        for (int i = 0; i < kThreads / 32; ++i) own[i] = key_of(sh.tmax[i * 32 + lane]);
+        const uint32_t t = kth_largest<kThreads / 32, kBf16 ? 16 : 20>(own, k);
         // fewer than k threads hold anything: every entry above -inf is a candidate
         if (lane == 0) { sh.thr = fmaxf(value_of(t), kLowest); sh.n_hot = 0; sh.n_cand = 0; }
     }
@@ -236,7 +262,7 @@ __device__ void select_top(TeamShared<kThreads, kCap>& sh, const Span& sp, int k
     auto offer = [&](float z, int idx) {
         if (z >= thr) {
             const int at = atomicAdd(&sh.n_cand, 1);
-            if (at < kCap) { sh.ckey[at] = key_of(z); sh.cidx[at] = idx; }
+            if (at < kCap) sh.cand[at] = entry_of(z, idx);
         }
     };
     const int n_hot = sh.n_hot;
@@ -278,7 +304,7 @@ __device__ void select_top(TeamShared<kThreads, kCap>& sh, const Span& sp, int k
         for_own<kBf16, kThreads>(sp, tid, [&](float z, int idx) {
             if (z > thr) {
                 const int at = atomicAdd(&sh.n_cand, 1);
-                sh.ckey[at] = key_of(z); sh.cidx[at] = idx;        // at most kCap - kMaxTop of them
+                sh.cand[at] = entry_of(z, idx);                    // at most kCap - kMaxTop of them
             }
         });
         team_sync<kThreads>();
@@ -289,7 +315,7 @@ __device__ void select_top(TeamShared<kThreads, kCap>& sh, const Span& sp, int k
             auto take = [&](bool hit, int idx) {
                 const uint32_t b = __ballot_sync(0xffffffffu, hit);
                 const int at = have + __popc(b & ((1u << lane) - 1u));
-                if (hit && at < k) { sh.ckey[n + at] = key_of(thr); sh.cidx[n + at] = idx; }
+                if (hit && at < k) sh.cand[n + at] = entry_of(thr, idx);
                 have += __popc(b);
             };
             for (int i = sp.v0 * kPer; i < sp.v1 * kPer && have < k; i += 32) {
@@ -302,15 +328,123 @@ __device__ void select_top(TeamShared<kThreads, kCap>& sh, const Span& sp, int k
         team_sync<kThreads>();
         n = sh.n_cand;
     }
-    for (int i = tid; i < n; i += kThreads) {                      // rank = candidates ahead of this one
-        const uint32_t key = sh.ckey[i];
-        const int idx = sh.cidx[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += sh.ckey[j] > key || (sh.ckey[j] == key && sh.cidx[j] < idx) ? 1 : 0;
-        if (rank < k) { sh.lkey[rank] = key; sh.lidx[rank] = idx; }
-    }
+    rank_entries(sh.cand, n, k, sh.list, tid, kThreads);
     if (tid == 0) sh.n_list = n < k ? n : k;
     team_sync<kThreads>();
+}
+
+// The outputs of row t, by the threads tid = 0 .. stride - 1 of a team (thread 0 holds the given token's logit zy).
+__device__ __forceinline__ void write_row(const Args& a, long long t, const Part r, const Entry* list, int n_list, float zy,
+                                          int y_state, int tid, int stride) {
+    const bool empty = r.S == 0.0f && !r.bad;
+    const float nan = __int_as_float(0x7fffffff);
+    const float l = r.bad ? nan : empty ? 0.0f : logf(r.S);
+    if (tid == 0) {
+        const float H = r.bad ? nan : empty ? 0.0f : fmaxf(l - r.Q / r.S * a.inv_tau, 0.0f);
+        if (a.lse) a.lse[t] = r.bad ? nan : empty ? -INFINITY : fmaf(r.m, a.inv_tau, l);
+        if (a.entropy) a.entropy[t] = H;
+        if (a.stats) a.stats[t] = make_float4(r.bad ? nan : empty ? -INFINITY : r.m, l, H, 0.0f);
+        if (y_state != 0) set_status(a.status, y_state);
+        if (a.logp) a.logp[t] = y_state != 0 ? 0.0f : r.bad ? nan : empty ? -INFINITY : fmaf(zy - r.m, a.inv_tau, -l);
+    }
+    for (int j = tid; j < a.k; j += stride) {
+        const bool have = !r.bad && j < n_list;
+        const Entry e = have ? list[j] : 0;
+        a.top_ids[t * a.k + j] = have ? entry_index(e) : -1;
+        a.top_logp[t * a.k + j] = have ? fmaf(entry_value(e) - r.m, a.inv_tau, -l) : r.bad ? nan : -INFINITY;
+    }
+}
+
+// Short rows: a warp per row, the whole row in registers (kVecs vectors per lane), so the maximum is known before the
+// exponentials and the candidates are picked out of the registers.
+template <bool kBf16, int kVecs, int kTeams>
+__global__ void __launch_bounds__(32 * kTeams)
+token_logprobs_warp_kernel(const Args a) {
+    constexpr int kPer = Elems<kBf16>::kPerVec, kLog2Per = kBf16 ? 3 : 2;
+    __shared__ TeamShared<32, kCandWarp> shared[kTeams];
+    const int team = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    TeamShared<32, kCandWarp>& sh = shared[team];
+    const long long T = a.n_tokens_dev ? min((long long)*a.n_tokens_dev, a.T_max) : a.T_max;
+    const long long t = (long long)blockIdx.x * kTeams + team;
+    if (t >= T) return;
+    const char* row = a.logits + t * a.row_bytes;
+    const int nvec = a.V >> kLog2Per, tail = (nvec << kLog2Per) + lane;
+
+    constexpr uint32_t kNone = kBf16 ? 0xff80ff80u : 0xff800000u;  // -inf
+    uint4 q[kVecs];
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) {
+        q[u] = make_uint4(kNone, kNone, kNone, kNone);
+        if (u * 32 + lane < nvec) q[u] = load_vec(row + (size_t)(u * 32 + lane) * 16);
+    }
+    const float zt = tail < a.V ? Elems<kBf16>::load1(row, tail) : -INFINITY;
+    float zy = 0.0f;
+    int y_state = 0;
+    if (lane == 0 && a.target) {
+        const int y = a.target[t];
+        if (y < 0 || y >= a.V) y_state = DPPO_STATUS_BAD_TARGET;
+        else zy = Elems<kBf16>::load1(row, y);
+    }
+    float mx = zt;                                                 // this lane's maximum (NaN if it has one)
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) mx = max_nan(mx, vec_max<kBf16>(q[u]));
+    Part p;
+    p.bad = __any_sync(0xffffffffu, !(mx < INFINITY));
+    p.m = fmaxf(warp_max_f32(mx), kLowest);
+    const f32x2 nm2 = pair_of(-p.m, -p.m), c2 = pair_of(a.c, a.c);
+    Acc acc;
+    acc.S = acc.Q = pair_of(0.0f, 0.0f);
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) {
+        float f[kPer];
+        Elems<kBf16>::unpack(q[u], f);
+#pragma unroll
+        for (int j = 0; j < kPer; j += 2) acc_pair(acc, f[j], f[j + 1], nm2, c2);
+    }
+    acc_pair(acc, zt, -INFINITY, nm2, c2);
+    float s0, s1, q0, q1;
+    unpair(acc.S, s0, s1); unpair(acc.Q, q0, q1);
+    p.S = warp_sum(s0 + s1); p.Q = warp_sum(q0 + q1);
+
+    int n = 0;
+    if (a.k > 0 && !p.bad) {
+        const uint32_t own[1] = {key_of(mx)};
+        const float thr = fmaxf(value_of(kth_largest<1, kBf16 ? 16 : 20>(own, a.k)), kLowest);
+        if (lane == 0) sh.n_cand = 0;
+        __syncwarp();
+        if (mx >= thr) {
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u) {
+                float f[kPer];
+                Elems<kBf16>::unpack(q[u], f);
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) {
+                    if (f[j] >= thr) {
+                        const int at = atomicAdd(&sh.n_cand, 1);
+                        if (at < kCandWarp) sh.cand[at] = entry_of(f[j], (u * 32 + lane) * kPer + j);
+                    }
+                }
+            }
+            if (zt >= thr) {
+                const int at = atomicAdd(&sh.n_cand, 1);
+                if (at < kCandWarp) sh.cand[at] = entry_of(zt, tail);
+            }
+        }
+        __syncwarp();
+        n = sh.n_cand;
+        if (n <= kCandWarp) {
+            rank_entries(sh.cand, n, a.k, sh.list, lane, 32);
+            n = min(n, a.k);
+        } else {                                                   // ties: the rules of select_top, from memory
+            sh.tmax[lane] = mx;
+            __syncwarp();
+            const Span sp = {row, 0, nvec, nvec << kLog2Per, a.V};
+            select_top<kBf16, 32, kCandWarp>(sh, sp, a.k, lane);
+            n = sh.n_list;
+        }
+        __syncwarp();
+    }
+    write_row(a, t, p, sh.list, n, zy, y_state, lane, 32);
 }
 
 // kCluster: the CTAs of a cluster split the row (blockIdx.x / cluster size = row).  Else kTeams teams per CTA, a row each.
@@ -368,16 +502,11 @@ token_logprobs_kernel(const Args a) {
 
     Part p = acc_part(acc);
     if (a.k > 0) sh.tmax[tid] = p.S > 0.0f ? p.m : -INFINITY;      // nothing but -inf seen: not a maximum
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) join(p, shfl_xor(p, o), a.c);
+    p = warp_join(p, a.c);
     if constexpr (kThreads > 32) {
         if (lane == 0) sh.part[warp] = p;
         __syncthreads();
-        if (warp == 0) {
-            p = lane < kThreads / 32 ? sh.part[lane] : Part{kLowest, 0.0f, 0.0f, 0};
-#pragma unroll
-            for (int o = kThreads / 64; o > 0; o >>= 1) join(p, shfl_xor(p, o), a.c);
-        }
+        if (warp == 0) p = warp_join(lane < kThreads / 32 ? sh.part[lane] : Part{kLowest, 0.0f, 0.0f, 0}, a.c);
     }
     if (tid == 0) sh.row = p;
     team_sync<kThreads>();
@@ -390,8 +519,7 @@ token_logprobs_kernel(const Args a) {
             if (warp == 0) {
                 Part o = {kLowest, 0.0f, 0.0f, 0};
                 if (lane < (int)C) o = cl.map_shared_rank(&sh, lane)->row;
-#pragma unroll
-                for (int s = 16; s > 0; s >>= 1) join(o, shfl_xor(o, s), a.c);
+                o = warp_join(o, a.c);
                 if (lane == 0) sh.part[0] = o;
             }
             if (a.k > 0) {
@@ -403,7 +531,7 @@ token_logprobs_kernel(const Args a) {
                     const int j = i % a.k;
                     if (!o->row.bad && j < o->n_list) {
                         const int at = atomicAdd(&sh.n_cand, 1);
-                        sh.ckey[at] = o->lkey[j]; sh.cidx[at] = o->lidx[j];
+                        sh.cand[at] = o->list[j];
                     }
                 }
             }
@@ -412,41 +540,14 @@ token_logprobs_kernel(const Args a) {
         if (rank != 0) return;
         if (a.k > 0) {
             const int n = sh.n_cand;
-            for (int i = tid; i < n; i += kThreads) {
-                const uint32_t key = sh.ckey[i];
-                const int idx = sh.cidx[i];
-                int ahead = 0;
-                for (int j = 0; j < n; ++j) ahead += sh.ckey[j] > key || (sh.ckey[j] == key && sh.cidx[j] < idx) ? 1 : 0;
-                if (ahead < a.k) { sh.lkey[ahead] = key; sh.lidx[ahead] = idx; }
-            }
+            rank_entries(sh.cand, n, a.k, sh.list, tid, kThreads);
             if (tid == 0) sh.n_list = n < a.k ? n : a.k;
         }
         if (tid == 0) sh.row = sh.part[0];
         __syncthreads();
     }
 
-    // ---- outputs
-    const Part r = sh.row;
-    const bool empty = r.S == 0.0f && !r.bad;
-    const float nan = __int_as_float(0x7fffffff);
-    const float l = r.bad ? nan : empty ? 0.0f : logf(r.S);
-    if (tid == 0) {
-        const float H = r.bad ? nan : empty ? 0.0f : fmaxf(l - r.Q / r.S * a.inv_tau, 0.0f);
-        if (a.lse) a.lse[t] = r.bad ? nan : empty ? -INFINITY : fmaf(r.m, a.inv_tau, l);
-        if (a.entropy) a.entropy[t] = H;
-        if (a.stats) a.stats[t] = make_float4(r.bad ? nan : empty ? -INFINITY : r.m, l, H, 0.0f);
-        if (a.logp) {
-            if (y_state != 0) set_status(a.status, y_state);
-            a.logp[t] = y_state != 0 ? 0.0f : r.bad ? nan : empty ? -INFINITY : fmaf(zy - r.m, a.inv_tau, -l);
-        } else if (y_state != 0) {
-            set_status(a.status, y_state);
-        }
-    }
-    for (int j = tid; j < a.k; j += kThreads) {
-        const bool have = !r.bad && j < sh.n_list;
-        a.top_ids[t * a.k + j] = have ? sh.lidx[j] : -1;
-        a.top_logp[t * a.k + j] = have ? fmaf(value_of(sh.lkey[j]) - r.m, a.inv_tau, -l) : r.bad ? nan : -INFINITY;
-    }
+    write_row(a, t, sh.row, sh.list, sh.n_list, zy, y_state, tid, kThreads);
 }
 
 // ---- backward -----------------------------------------------------------------------------------------
@@ -479,6 +580,7 @@ template <bool kBf16, int kThreads, int kTeams>
 __global__ void __launch_bounds__(kThreads * kTeams)
 token_logprobs_bwd_kernel(const BwdArgs a) {
     constexpr int kPer = Elems<kBf16>::kPerVec, kLog2Per = kBf16 ? 3 : 2;
+    constexpr int kUnroll = 4;
     const int team = kTeams == 1 ? 0 : threadIdx.x / kThreads;
     const int tid = kTeams == 1 ? threadIdx.x : threadIdx.x % kThreads;
     const long long T = a.n_tokens_dev ? min((long long)*a.n_tokens_dev, a.T_max) : a.T_max;
@@ -505,9 +607,9 @@ token_logprobs_bwd_kernel(const BwdArgs a) {
     const int nvec = a.V >> kLog2Per;
     const int v0 = chunk * a.chunk_vecs, v1 = min(nvec, v0 + a.chunk_vecs);
     const int vy = a.dlogp && !zero ? y >> kLog2Per : -1;
-    for (int i = v0 + tid; i < v1; i += kThreads) {
+    auto put = [&](const uint4& q, int i) {
         float z[kPer];
-        Elems<kBf16>::unpack(load_vec_rw(row + (size_t)i * 16), z);
+        Elems<kBf16>::unpack(q, z);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) z[j] = zero ? 0.0f : bwd_elem(z[j], r, a.c);
         if (i == vy) {
@@ -515,7 +617,16 @@ token_logprobs_bwd_kernel(const BwdArgs a) {
             for (int j = 0; j < kPer; ++j) z[j] += j == (y & (kPer - 1)) ? r.a : 0.0f;
         }
         __stcs(reinterpret_cast<uint4*>(out) + i, Elems<kBf16>::pack(z));
+    };
+    int i = v0 + tid;
+    for (; i + (kUnroll - 1) * kThreads < v1; i += kUnroll * kThreads) {       // all loads of a round before its stores
+        uint4 q[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) q[u] = load_vec_rw(row + (size_t)(i + u * kThreads) * 16);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) put(q[u], i + u * kThreads);
     }
+    for (; i < v1; i += kThreads) put(load_vec_rw(row + (size_t)i * 16), i);
     const int tail = (nvec << kLog2Per) + tid;
     if (chunk == a.chunks - 1 && tail < a.V) {
         float g = zero ? 0.0f : bwd_elem(Elems<kBf16>::load1(row, tail), r, a.c);
@@ -543,19 +654,32 @@ static int launch_fwd(const Args& a, int C, cudaStream_t s) {
     return DPPO_OK;
 }
 
+template <bool kBf16, int kVecs> static int launch_warp(const Args& a, cudaStream_t s) {
+    constexpr int kTeams = 8;
+    token_logprobs_warp_kernel<kBf16, kVecs, kTeams><<<(unsigned)((a.T_max + kTeams - 1) / kTeams), 32 * kTeams, 0, s>>>(a);
+    DPPO_CHECK_LAUNCH("token_logprobs launch");
+    return DPPO_OK;
+}
+
 template <bool kBf16> static int run_fwd(const Args& a, int variant, cudaStream_t s) {
     int C = 1, threads = 256;
     if (variant == 0) {
         const int nvec = a.V >> (kBf16 ? 3 : 2);
-        if (nvec <= 512) { threads = 32; }
+        if (nvec <= 256) { threads = 32; }
         else {
             while (C < 8 && a.T_max * C * 2 <= 2ll * sm_count() && nvec / (2 * C) >= 256) C *= 2;
-            threads = nvec / C >= 4096 ? 512 : 256;
+            threads = C == 1 && nvec <= 2048 ? 128 : 256;
         }
     } else if (variant == 32) {
         threads = 32;
     } else {
         C = variant / 10000; threads = variant % 10000;
+    }
+    if (threads == 32 && C == 1) {
+        const int nvec = a.V >> (kBf16 ? 3 : 2);
+        if (nvec <= 128) return launch_warp<kBf16, 4>(a, s);
+        if (nvec <= 256) return launch_warp<kBf16, 8>(a, s);
+        if (nvec <= 512) return launch_warp<kBf16, 16>(a, s);
     }
     if (threads == 32 && C == 1) return launch_fwd<kBf16, 32, 8, false>(a, 1, s);
     if (C == 1 && threads == 128) return launch_fwd<kBf16, 128, 1, false>(a, 1, s);

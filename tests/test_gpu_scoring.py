@@ -175,7 +175,7 @@ def special_rows(V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("V, k, variant", [(9, 4, 0), (1000, 20, 0), (4099, 32, 0), (8200, 5, 0), (20000, 20, 10128), (20003, 20, 0),
+@pytest.mark.parametrize("V, k, variant", [(9, 4, 0), (1000, 20, 0), (1500, 20, 0), (2001, 32, 0), (3500, 8, 0), (4099, 32, 0), (8200, 5, 0), (20000, 20, 10128), (20003, 20, 0),
                                            (20003, 32, 10512), (20003, 7, 40256), (20003, 20, 80128), (20003, 32, 32)])
 def test_special_rows(B, V, k, variant, dtype):
     rows = special_rows(V, dtype)
