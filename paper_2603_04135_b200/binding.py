@@ -154,7 +154,7 @@ def _arr(x, name, device, dtype, rows, row_elems, stride=None):
         if stride is None:
             if x.numel() < rows * row_elems or not x.is_contiguous():
                 raise DppoError(ERR_BAD_SHAPE, "%s: needs %d contiguous elements, got shape %s" % (name, rows * row_elems, tuple(x.shape)))
-        else:
+        elif x.stride() != (stride, 1) or x.shape[0] < rows or x.shape[1] < row_elems:     # else the plain case: rows of a matrix
             have = x.untyped_storage().nbytes() // x.element_size() - x.storage_offset()
             if have < (rows - 1) * stride + row_elems or (x.dim() == 2 and (x.stride(1) != 1 and x.shape[1] > 1
                                                                             or x.stride(0) != stride and x.shape[0] > 1)):
@@ -173,9 +173,18 @@ def _device():
     return torch.cuda.current_device() if _cuda else -1
 
 
+def _current_stream(device):
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+# the same without the stream object that current_stream() builds (3 us of a small call)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream)
+
+
 def _stream(stream):
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream if _device() >= 0 else None
+        device = _device()
+        return _current_stream(device) if device >= 0 else None
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
     return int(stream)

@@ -505,10 +505,22 @@ static int make_map(CUtensorMap* map, const void* base, long long rows, int K, l
     return DPPO_OK;
 }
 
+// Raises a kernel's shared-memory limit once per device.
+template <class Kernel> static int raise_smem(Kernel kernel, size_t bytes, bool (&done)[64]) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); dev = -1; }
+    if (dev >= 0 && done[dev]) return DPPO_OK;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != cudaSuccess) { cudaGetLastError(); return cuda_fail(e, "linear_i8: shared memory attribute"); }
+    if (dev >= 0) done[dev] = true;
+    return DPPO_OK;
+}
+
 template <bool kBf16> static int launch_pair(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
     auto kernel = linear_i8_pair_kernel<kBf16>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDynSmem2);
-    if (e != cudaSuccess) return cuda_fail(e, "linear_i8: shared memory attribute");
+    static bool raised[64];
+    const int rc = raise_smem(kernel, kDynSmem2, raised);
+    if (rc != DPPO_OK) return rc;
     const long long work = (long long)((a.N + 255) / 256) * ((a.M_max + kTileN - 1) / kTileN), most = sm_count() / 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(2 * (work < most ? work : most)), 1, 1);
@@ -519,15 +531,16 @@ template <bool kBf16> static int launch_pair(const CUtensorMap& mw, const CUtens
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, kernel, mw, mx, a);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, mw, mx, a);
     if (e != cudaSuccess) return cuda_fail(e, "linear_i8 launch");
     return DPPO_OK;
 }
 
 template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
     auto kernel = linear_i8_small_kernel<kNB, kBf16>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)small_smem<kNB>());
-    if (e != cudaSuccess) return cuda_fail(e, "linear_i8: shared memory attribute");
+    static bool raised[64];
+    const int rc = raise_smem(kernel, small_smem<kNB>(), raised);
+    if (rc != DPPO_OK) return rc;
     const int n_ch = (a.N + kTileM - 1) / kTileM;
     const long long tiles = (long long)n_ch * ((a.M_max + kNB - 1) / kNB);
     int split = 1;                                                       // enough CTAs for two per SM, two slabs at least each
@@ -542,7 +555,7 @@ template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, co
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, kernel, mw, mx, a, n_ch, split);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, mw, mx, a, n_ch, split);
     if (e != cudaSuccess) return cuda_fail(e, "linear_i8 launch");
     return DPPO_OK;
 }
