@@ -27,7 +27,7 @@ namespace i8 {
 
 constexpr int kBK = 128;                  // K slab: 128 codes = one 128-byte swizzle row
 constexpr int kTileM = 128;               // channels per CTA
-constexpr int kTileN = 256;               // tokens per tile of the pair kernel
+constexpr int kTileN = 256;               // most tokens per tile of the pair kernel
 constexpr int kStages2 = 6;
 constexpr int kBytesA = kTileM * kBK;                        // 16 KB
 constexpr int kBytesB2 = kTileN / 2 * kBK;                   // 16 KB: this CTA's half of the token tile
@@ -44,6 +44,7 @@ struct Args {
     int32_t* status;
     long long M_max, out_stride;
     int N, n_ksteps, out_bf16;
+    int tile_n;                           // pair kernel: tokens per tile, a multiple of 32 up to 256
     unsigned long long wait_limit_ns;
     int test_extra_tx;
 };
@@ -94,6 +95,10 @@ __device__ __forceinline__ void store_column(const Args& a, long long t0, long l
     }
 }
 
+// The product may be launched while the kernel before it (the quantisation of its rows) still runs: nothing is read from
+// global memory before that kernel has completed.
+__device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // ---- many tokens: CTA pairs ---------------------------------------------------------------------------
 struct Shared2 {
     unsigned long long full[kStages2];
@@ -129,8 +134,7 @@ linear_i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     const bool leader = rank == 0;
     volatile int* abort_flag = &sh.abort;
-    const long long T = true_rows(a);
-    const int n_m2 = (a.N + 2 * kTileM - 1) / (2 * kTileM), n_tok = (int)((T + kTileN - 1) / kTileN);
+    const int n_m2 = (a.N + 2 * kTileM - 1) / (2 * kTileM);
 
     if (tid == 0) {
         sh.abort = 0;
@@ -156,14 +160,18 @@ linear_i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     lm_cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = sh.tmem_base;
+    wait_for_previous_kernel();
+    const long long T = true_rows(a);
+    const int n_tok = (int)((T + a.tile_n - 1) / a.tile_n);
 
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer (both CTAs)
         if (lane == 0) {
+            const uint32_t stage_bytes = 2u * (uint32_t)(kBytesA + a.tile_n / 2 * kBK);
             uint32_t it = 0;
             int m2, n;
             for (uint32_t j = 0; tile_of(j, n_m2, n_tok, m2, n) && !*abort_flag; ++j) {
-                const int row_w = (2 * m2 + (int)rank) * kTileM, row_x = n * kTileN + (int)rank * (kTileN / 2);
+                const int row_w = (2 * m2 + (int)rank) * kTileM, row_x = n * a.tile_n + (int)rank * (a.tile_n / 2);
                 for (int k = 0; k < a.n_ksteps; ++k, ++it) {
                     const uint32_t s = it % kStages2, use = it / kStages2;
                     if (use > 0 && !lm_wait(lm_smem_u32(&sh.empty[s]), (use - 1) & 1, abort_flag, a.wait_limit_ns)) break;
@@ -171,7 +179,7 @@ linear_i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                     const uint32_t dst = tiles + s * kStageBytes2;
                     if (leader)                                        // the leader's barrier collects both CTAs' bytes
                         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;"
-                                     :: "r"(bar_local), "r"((uint32_t)(2 * kStageBytes2) + (it == 0 ? (uint32_t)a.test_extra_tx : 0u)) : "memory");
+                                     :: "r"(bar_local), "r"(stage_bytes + (it == 0 ? (uint32_t)a.test_extra_tx : 0u)) : "memory");
                     lm_tma_2d_pair(dst, &map_w, bar, k * kBK, row_w, 0);
                     lm_tma_2d_pair(dst + kBytesA, &map_x, bar, k * kBK, row_x, 0);
                 }
@@ -187,6 +195,7 @@ linear_i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer (leader CTA only)
         if (lane == 0 && leader) {
+            const uint32_t desc = idesc(2 * kTileM, a.tile_n);
             uint32_t it = 0;
             int m2, n;
             bool ok = true;
@@ -206,7 +215,7 @@ linear_i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                         asm volatile("{\n\t.reg .pred p;\n\t"
                                      "setp.ne.b32 p, %4, 0;\n\t"
                                      "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
-                                     :: "r"(d_tmem), "l"(dw + kk * 2), "l"(dx + kk * 2), "r"(idesc(2 * kTileM, kTileN)), "r"(accumulate) : "memory");
+                                     :: "r"(d_tmem), "l"(dw + kk * 2), "l"(dx + kk * 2), "r"(desc), "r"(accumulate) : "memory");
                     }
                     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                                  :: "r"(lm_smem_u32(&sh.empty[s])), "h"((unsigned short)3) : "memory");
@@ -233,8 +242,8 @@ linear_i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + b * kTileN;
 #pragma unroll 1
-            for (int c = 0; c < kTileN / 32; ++c) {
-                const long long t0 = (long long)n * kTileN + c * 32;
+            for (int c = 0; c < a.tile_n / 32; ++c) {
+                const long long t0 = (long long)n * a.tile_n + c * 32;
                 if (t0 >= T) break;
                 uint32_t v[32];
                 lm_tmem_load32(v, taddr + (uint32_t)(c * 32));
@@ -294,12 +303,10 @@ linear_i8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
     const uint32_t tiles = (lm_smem_u32(i8_raw) + 1023u) & ~1023u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     volatile int* abort_flag = &sh.abort;
-    const long long T = true_rows(a);
     const int part = (int)(blockIdx.x % (unsigned)split);                 // rank in the cluster: clusters are consecutive CTAs
     const int id = (int)(blockIdx.x / (unsigned)split);
     const int m = id % n_ch;
     const long long t_tile = (long long)(id / n_ch) * kNB;
-    if (t_tile >= T) return;                                              // the whole cluster leaves together
     const int k0 = (int)((long long)a.n_ksteps * part / split), k1 = (int)((long long)a.n_ksteps * (part + 1) / split);
 
     if (tid == 0) {
@@ -312,6 +319,9 @@ linear_i8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
+    wait_for_previous_kernel();
+    const long long T = true_rows(a);
+    if (t_tile >= T) return;                                              // the whole cluster leaves together
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                      :: "r"(lm_smem_u32(&sh.tmem_base)), "r"((uint32_t)kCols) : "memory");
@@ -442,14 +452,42 @@ __device__ __forceinline__ uint32_t code_of(float x, float s) {
     return (uint32_t)(int32_t)fminf(fmaxf(v, -127.0f), 127.0f) & 0xffu;
 }
 
+// The codes of kPer values (4 per word).  x / s lies within 4e-5 of x * r, r = fl(1/s) (|x / s| <= 127.1, relative errors of r and
+// of the quotient 2^-24 each), so unless x * r is that close to a tie, both round to the same integer; adding 1.5 * 2^23 rounds
+// to it and leaves it in the low bits.  A vector with such a value is divided out (one in thousands).  The division alone
+// held the kernel to 3.1 TB/s on 16,384 x 4,096 bf16.
+// quick: s is large enough for r to be a normal number.
+template <int kPer> __device__ __forceinline__ void codes_of(const float (&f)[kPer], float s, float r, bool quick, bool live, uint32_t (&w)[kPer / 4]) {
+    constexpr float kMagic = 12582912.0f;
+    float t[kPer], far = quick ? 0.0f : 1.0f;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        t[j] = fmaf(f[j], r, kMagic);
+        far = fmaxf(far, fabsf(fmaf(f[j], r, kMagic - t[j])));
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; j += 4) {
+        const uint32_t lo = __byte_perm(__float_as_uint(t[j]), __float_as_uint(t[j + 1]), 0x0040);
+        const uint32_t hi = __byte_perm(__float_as_uint(t[j + 2]), __float_as_uint(t[j + 3]), 0x0040);
+        w[j / 4] = __byte_perm(lo, hi, 0x5410);
+    }
+    if (!(far < 0.4999f)) {
+#pragma unroll
+        for (int j = 0; j < kPer; j += 4)
+            w[j / 4] = live ? code_of(f[j], s) | code_of(f[j + 1], s) << 8 | code_of(f[j + 2], s) << 16 | code_of(f[j + 3], s) << 24 : 0u;
+    }
+}
+
 constexpr int kQuantThreads = 128;
 
-// One CTA per row, two reads of it (the second out of L1 / L2): the maximum, then the codes.
-template <bool kBf16>
+// One CTA per row: the maximum, then the codes.  Rows of up to kVecs vectors per thread stay in registers in between; longer
+// ones are read a second time (out of L2).
+template <bool kBf16, int kVecs>
 __global__ void __launch_bounds__(kQuantThreads)
 quantize_rows_kernel(const QuantArgs a) {
     constexpr int kPer = Elems<kBf16>::kPerVec;
     __shared__ float red[kQuantThreads / 32];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // a product may set itself up meanwhile
     const long long t = blockIdx.x;
     const long long T = a.n_rows_dev ? min((long long)*a.n_rows_dev, a.rows_max) : a.rows_max;
     if (t >= T) return;
@@ -458,14 +496,21 @@ quantize_rows_kernel(const QuantArgs a) {
     const uint4* rv = reinterpret_cast<const uint4*>(row);
     int8_t* q = a.q + t * a.q_stride;
     const int nvec = a.K / kPer, tail = nvec * kPer + tid;
+    uint4 v[kVecs];
     float amax = 0.0f;
-    for (int i = tid; i < nvec; i += kQuantThreads) {
+    auto look = [&](const uint4& x) {
         float f[kPer];
-        Elems<kBf16>::unpack(rv[i], f);
+        Elems<kBf16>::unpack(x, f);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) amax = max_nan(amax, fabsf(f[j]));
-    }
-    if (tail < a.K) amax = max_nan(amax, fabsf(Elems<kBf16>::load1(row, tail)));
+    };
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) v[u] = u * kQuantThreads + tid < nvec ? rv[u * kQuantThreads + tid] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) look(v[u]);
+    for (int i = kVecs * kQuantThreads + tid; i < nvec; i += kQuantThreads) look(rv[i]);
+    const float xt = tail < a.K ? Elems<kBf16>::load1(row, tail) : 0.0f;
+    amax = max_nan(amax, fabsf(xt));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
     if ((tid & 31) == 0) red[tid >> 5] = amax;
@@ -476,17 +521,21 @@ quantize_rows_kernel(const QuantArgs a) {
     const float s = fine ? __fmul_rn(amax, 1.0f / 127.0f) : __int_as_float(0x7fffffff);
     if (tid == 0) a.scale[t] = s;
     const bool live = fine && s > 0.0f;
-    for (int i = tid; i < nvec; i += kQuantThreads) {
+    const bool quick = s > 1e-30f;
+    const float r = quick ? __fdiv_rn(1.0f, s) : 0.0f;
+    auto put = [&](const uint4& x, int i) {
         float f[kPer];
-        Elems<kBf16>::unpack(rv[i], f);
+        Elems<kBf16>::unpack(x, f);
         uint32_t w[kPer / 4];
-#pragma unroll
-        for (int j = 0; j < kPer; j += 4)
-            w[j / 4] = live ? code_of(f[j], s) | code_of(f[j + 1], s) << 8 | code_of(f[j + 2], s) << 16 | code_of(f[j + 3], s) << 24 : 0u;
+        codes_of<kPer>(f, s, r, quick, live, w);
         if constexpr (kBf16) reinterpret_cast<uint2*>(q)[i] = make_uint2(w[0], w[1]);
         else reinterpret_cast<uint32_t*>(q)[i] = w[0];
-    }
-    if (tail < a.K) q[tail] = live ? (int8_t)code_of(Elems<kBf16>::load1(row, tail), s) : (int8_t)0;
+    };
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u)
+        if (u * kQuantThreads + tid < nvec) put(v[u], u * kQuantThreads + tid);
+    for (int i = kVecs * kQuantThreads + tid; i < nvec; i += kQuantThreads) put(rv[i], i);
+    if (tail < a.K) q[tail] = live ? (int8_t)code_of(xt, s) : (int8_t)0;
 }
 
 // ---- host side ---------------------------------------------------------------------------------------
@@ -516,21 +565,42 @@ template <class Kernel> static int raise_smem(Kernel kernel, size_t bytes, bool 
     return DPPO_OK;
 }
 
+// Clusters of `cluster` CTAs, started as soon as the kernel before lets dependents go (see wait_for_previous_kernel).
+static void set_attributes(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[2], int cluster) {
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+}
+
+// Tokens per tile of the pair kernel: the tile that needs the least time over whole waves of pairs.  A K slab of a tile costs
+// about (256 + tile) units: a tile of 256 keeps the tensor cores and the operand fetches equally busy, a narrower one is bound
+// by fetching the weights' 16 KB.  (1,003 x 5,003 x 2,563: 140 tiles of 160 in two waves instead of 80 of 256 in two.)
+static int pair_tile(long long M, int N) {
+    const long long n_m2 = (N + 255) / 256, pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
+    int best = kTileN;
+    long long best_cost = 0;
+    for (int tn = kTileN; tn >= 64; tn -= 32) {
+        const long long tiles = n_m2 * ((M + tn - 1) / tn), cost = (tiles + pairs - 1) / pairs * (256 + tn);
+        if (best_cost == 0 || cost < best_cost) { best = tn; best_cost = cost; }
+    }
+    return best;
+}
+
 template <bool kBf16> static int launch_pair(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
     auto kernel = linear_i8_pair_kernel<kBf16>;
     static bool raised[64];
     const int rc = raise_smem(kernel, kDynSmem2, raised);
     if (rc != DPPO_OK) return rc;
-    const long long work = (long long)((a.N + 255) / 256) * ((a.M_max + kTileN - 1) / kTileN), most = sm_count() / 2;
+    const long long work = (long long)((a.N + 255) / 256) * ((a.M_max + a.tile_n - 1) / a.tile_n), most = sm_count() / 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(2 * (work < most ? work : most)), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
     cfg.dynamicSmemBytes = kDynSmem2;
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = 1;
+    cudaLaunchAttribute attr[2];
+    set_attributes(cfg, attr, 2);
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, mw, mx, a);
     if (e != cudaSuccess) return cuda_fail(e, "linear_i8 launch");
     return DPPO_OK;
@@ -551,10 +621,8 @@ template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, co
     cfg.blockDim = dim3(kThreads, 1, 1);
     cfg.dynamicSmemBytes = small_smem<kNB>();
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = 1;
+    cudaLaunchAttribute attr[2];
+    set_attributes(cfg, attr, split);
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, mw, mx, a, n_ch, split);
     if (e != cudaSuccess) return cuda_fail(e, "linear_i8 launch");
     return DPPO_OK;
@@ -590,8 +658,8 @@ extern "C" int dppo_quantize_rows_i8(const dppo_quantize_params* p, const void* 
     if (((uintptr_t)x & 15) || ((uintptr_t)q & 15) || x_row_bytes % 16 != 0 || p->q_stride % 16 != 0)
         return fail(DPPO_ERR_MISALIGNED, "quantize_rows_i8: x / q base and row strides must be multiples of 16 bytes");
     const i8::QuantArgs a = {(const char*)x, q, scale, n_rows_dev, p->rows_max, x_row_bytes, p->q_stride, p->K};
-    if (p->dtype == DPPO_BF16) i8::quantize_rows_kernel<true><<<(unsigned)p->rows_max, i8::kQuantThreads, 0, (cudaStream_t)stream>>>(a);
-    else i8::quantize_rows_kernel<false><<<(unsigned)p->rows_max, i8::kQuantThreads, 0, (cudaStream_t)stream>>>(a);
+    if (p->dtype == DPPO_BF16) i8::quantize_rows_kernel<true, 4><<<(unsigned)p->rows_max, i8::kQuantThreads, 0, (cudaStream_t)stream>>>(a);
+    else i8::quantize_rows_kernel<false, 8><<<(unsigned)p->rows_max, i8::kQuantThreads, 0, (cudaStream_t)stream>>>(a);
     DPPO_CHECK_LAUNCH("quantize_rows_i8 launch");
     return DPPO_OK;
 }
@@ -627,7 +695,8 @@ extern "C" int dppo_linear_i8(const dppo_linear_i8_params* p, const int8_t* x, c
     // The pair kernel from half a wave of its 256 x 256 tiles on; below that, and for up to 128 tokens, the other
     const long long pair_tiles = (long long)((p->N + 255) / 256) * ((p->M_max + 255) / 256);
     const bool pair = variant == 1 || (variant == 0 && p->M_max > 128 && pair_tiles * 4 >= sm_count());
-    const int nb = pair ? i8::kTileN / 2 : p->M_max <= 16 ? 16 : p->M_max <= 32 ? 32 : p->M_max <= 64 ? 64 : 128;
+    a.tile_n = pair ? i8::pair_tile(p->M_max, p->N) : 0;
+    const int nb = pair ? a.tile_n / 2 : p->M_max <= 16 ? 16 : p->M_max <= 32 ? 32 : p->M_max <= 64 ? 64 : 128;
     alignas(64) CUtensorMap mw, mx;
     int rc = i8::make_map(&mw, w, p->N, p->K, p->w_stride, i8::kTileM);
     if (rc == DPPO_OK) rc = i8::make_map(&mx, x, p->M_max, p->K, p->x_stride, nb);

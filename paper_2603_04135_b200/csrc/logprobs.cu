@@ -188,17 +188,26 @@ template <int kPer, int kBits> __device__ __forceinline__ uint32_t kth_largest(c
     for (int bit = top; bit >= 32 - kBits; --bit) {
         const uint32_t t = r | (1u << bit);
         int cnt = 0;
-        if constexpr (kPer == 1) {
-            cnt = __popc(__ballot_sync(0xffffffffu, own[0] >= t));
-        } else {
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) cnt += own[i] >= t ? 1 : 0;
-            cnt = __reduce_add_sync(0xffffffffu, cnt);
-        }
+        for (int i = 0; i < kPer; ++i) cnt += own[i] >= t ? 1 : 0;
+        cnt = __reduce_add_sync(0xffffffffu, cnt);
         if (cnt >= k) r = t;
         if (cnt == k) break;                                       // exactly the k largest reach t: t serves as well
     }
     return r;
+}
+
+// The k-th largest of the lanes' values (those that are equal count together), at least kLowest.
+__device__ __forceinline__ float kth_of_lanes(float v, int k) {
+    float m = kLowest;
+#pragma unroll 1
+    for (int have = 0; have < k;) {
+        m = warp_max_f32(v);
+        if (!(m > kLowest)) return kLowest;
+        have += __popc(__ballot_sync(0xffffffffu, v == m));
+        v = v == m ? -INFINITY : v;
+    }
+    return m;
 }
 
 // The list of the top k of n entries in shared memory, by the threads tid = 0 .. stride - 1: an entry's place is the number
@@ -333,137 +342,169 @@ __device__ void select_top(TeamShared<kThreads, kCap>& sh, const Span& sp, int k
     team_sync<kThreads>();
 }
 
-// The outputs of row t, by the threads tid = 0 .. stride - 1 of a team (thread 0 holds the given token's logit zy).
-__device__ __forceinline__ void write_row(const Args& a, long long t, const Part r, const Entry* list, int n_list, float zy,
-                                          int y_state, int tid, int stride) {
-    const bool empty = r.S == 0.0f && !r.bad;
+// The outputs of a row from its sums.
+struct RowOut {
+    float l, H;
+};
+__device__ __forceinline__ bool is_empty(const Part& r) { return r.S == 0.0f && !r.bad; }
+__device__ __forceinline__ RowOut row_out(const Args& a, const Part& r) {
     const float nan = __int_as_float(0x7fffffff);
-    const float l = r.bad ? nan : empty ? 0.0f : logf(r.S);
-    if (tid == 0) {
-        const float H = r.bad ? nan : empty ? 0.0f : fmaxf(l - r.Q / r.S * a.inv_tau, 0.0f);
-        if (a.lse) a.lse[t] = r.bad ? nan : empty ? -INFINITY : fmaf(r.m, a.inv_tau, l);
-        if (a.entropy) a.entropy[t] = H;
-        if (a.stats) a.stats[t] = make_float4(r.bad ? nan : empty ? -INFINITY : r.m, l, H, 0.0f);
-        if (y_state != 0) set_status(a.status, y_state);
-        if (a.logp) a.logp[t] = y_state != 0 ? 0.0f : r.bad ? nan : empty ? -INFINITY : fmaf(zy - r.m, a.inv_tau, -l);
-    }
-    for (int j = tid; j < a.k; j += stride) {
-        const bool have = !r.bad && j < n_list;
-        const Entry e = have ? list[j] : 0;
-        a.top_ids[t * a.k + j] = have ? entry_index(e) : -1;
-        a.top_logp[t * a.k + j] = have ? fmaf(entry_value(e) - r.m, a.inv_tau, -l) : r.bad ? nan : -INFINITY;
-    }
+    if (r.bad) return {nan, nan};
+    if (is_empty(r)) return {0.0f, 0.0f};
+    const float l = logf(r.S);
+    return {l, fmaxf(l - r.Q / r.S * a.inv_tau, 0.0f)};
+}
+__device__ __forceinline__ void write_scalars(const Args& a, long long t, const Part& r, const RowOut& o, float zy, int y_state) {
+    const bool empty = is_empty(r);                                // a bad row's l is NaN, and so is what is formed with it
+    if (a.lse) a.lse[t] = empty ? -INFINITY : r.bad ? o.l : fmaf(r.m, a.inv_tau, o.l);
+    if (a.entropy) a.entropy[t] = o.H;
+    if (a.stats) a.stats[t] = make_float4(r.bad ? o.l : empty ? -INFINITY : r.m, o.l, o.H, 0.0f);
+    if (y_state != 0) set_status(a.status, y_state);
+    if (a.logp) a.logp[t] = y_state != 0 ? 0.0f : r.bad ? o.l : empty ? -INFINITY : fmaf(zy - r.m, a.inv_tau, -o.l);
+}
+__device__ __forceinline__ void write_top(const Args& a, long long t, int j, float m, float l, int bad, const Entry* list, int n_list) {
+    const bool have = !bad && j < n_list;
+    const Entry e = have ? list[j] : 0;
+    a.top_ids[t * a.k + j] = have ? entry_index(e) : -1;
+    a.top_logp[t * a.k + j] = have ? fmaf(entry_value(e) - m, a.inv_tau, -l) : bad ? l : -INFINITY;
 }
 
-// Short rows: a warp per row, the whole row in registers (kVecs vectors per lane), so the maximum is known before the
-// exponentials and the candidates are picked out of the registers.
+// Short rows: a warp per row at a time, the whole row in registers (kVecs vectors per lane), so the maximum is known before
+// the exponentials and the candidates are picked out of the registers.  What such a row costs is instructions (871 per row
+// of 1,021 f32 in a form that treated candidates and outputs entry by entry: 26 us for 20,011 rows), so:
+// the vectors that hold a candidate (a few of the row's) go through shared memory, one lane per entry; a warp takes up to 8
+// consecutive rows, and the scalar outputs of all of them are formed in one pass, a lane per row.
+constexpr int kMaxRun = 8;
+constexpr int kHotVecs = 64;
+struct WarpShared {
+    TeamShared<32, kCandWarp> team;
+    uint4 hot[kHotVecs];
+    int hot_vec[kHotVecs];
+    Entry list[kMaxRun][kMaxTop];
+};
+
 template <bool kBf16, int kVecs, int kTeams>
 __global__ void __launch_bounds__(32 * kTeams)
-token_logprobs_warp_kernel(const Args a) {
+token_logprobs_warp_kernel(const Args a, int run) {
     constexpr int kPer = Elems<kBf16>::kPerVec, kLog2Per = kBf16 ? 3 : 2;
-    __shared__ TeamShared<32, kCandWarp> shared[kTeams];
-    const int team = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    TeamShared<32, kCandWarp>& sh = shared[team];
+    constexpr uint32_t kNone = kBf16 ? 0xff80ff80u : 0xff800000u;  // -inf
+    __shared__ WarpShared shared[kTeams];
+    const int lane = threadIdx.x & 31;
+    WarpShared& ws = shared[threadIdx.x >> 5];
     const long long T = a.n_tokens_dev ? min((long long)*a.n_tokens_dev, a.T_max) : a.T_max;
-    const long long t = (long long)blockIdx.x * kTeams + team;
-    if (t >= T) return;
-    const char* row = a.logits + t * a.row_bytes;
+    const long long t0 = ((long long)blockIdx.x * kTeams + (threadIdx.x >> 5)) * run;
+    if (t0 >= T) return;
+    const int n_rows = (int)min((long long)run, T - t0);
     const int nvec = a.V >> kLog2Per, tail = (nvec << kLog2Per) + lane;
 
-    constexpr uint32_t kNone = kBf16 ? 0xff80ff80u : 0xff800000u;  // -inf
-    uint4 q[kVecs];
-#pragma unroll
-    for (int u = 0; u < kVecs; ++u) {
-        q[u] = make_uint4(kNone, kNone, kNone, kNone);
-        if (u * 32 + lane < nvec) q[u] = load_vec(row + (size_t)(u * 32 + lane) * 16);
-    }
-    const float zt = tail < a.V ? Elems<kBf16>::load1(row, tail) : -INFINITY;
+    // lane r: the given token of row t0 + r, and (below) the row's sums
     float zy = 0.0f;
-    int y_state = 0;
-    if (lane == 0 && a.target) {
-        const int y = a.target[t];
+    int y_state = 0, my_list = 0;
+    Part mine = {kLowest, 0.0f, 0.0f, 0};
+    if (lane < n_rows && a.target) {
+        const int y = a.target[t0 + lane];
         if (y < 0 || y >= a.V) y_state = DPPO_STATUS_BAD_TARGET;
-        else zy = Elems<kBf16>::load1(row, y);
+        else zy = Elems<kBf16>::load1(a.logits + (t0 + lane) * a.row_bytes, y);
     }
-    float mx = zt;                                                 // this lane's maximum (NaN if it has one)
+#pragma unroll 1
+    for (int r = 0; r < n_rows; ++r) {
+        const char* row = a.logits + (t0 + r) * a.row_bytes;
+        uint4 q[kVecs];
 #pragma unroll
-    for (int u = 0; u < kVecs; ++u) mx = max_nan(mx, vec_max<kBf16>(q[u]));
-    Part p;
-    p.bad = __any_sync(0xffffffffu, !(mx < INFINITY));
-    p.m = fmaxf(warp_max_f32(mx), kLowest);
-    const f32x2 nm2 = pair_of(-p.m, -p.m), c2 = pair_of(a.c, a.c);
-    Acc acc;
-    acc.S = acc.Q = pair_of(0.0f, 0.0f);
+        for (int u = 0; u < kVecs; ++u) {
+            q[u] = make_uint4(kNone, kNone, kNone, kNone);
+            if (u * 32 + lane < nvec) q[u] = load_vec(row + (size_t)(u * 32 + lane) * 16);
+        }
+        const float zt = tail < a.V ? Elems<kBf16>::load1(row, tail) : -INFINITY;
+        float vm[kVecs], mx = zt;                                  // the vectors' maxima, the lane's (NaN if it has one)
 #pragma unroll
-    for (int u = 0; u < kVecs; ++u) {
-        float f[kPer];
-        Elems<kBf16>::unpack(q[u], f);
+        for (int u = 0; u < kVecs; ++u) { vm[u] = vec_max<kBf16>(q[u]); mx = max_nan(mx, vm[u]); }
+        Part p;
+        p.bad = __any_sync(0xffffffffu, !(mx < INFINITY));
+        p.m = fmaxf(warp_max_f32(mx), kLowest);
+        const f32x2 nm2 = pair_of(-p.m, -p.m), c2 = pair_of(a.c, a.c);
+        Acc acc;
+        acc.S = acc.Q = pair_of(0.0f, 0.0f);
 #pragma unroll
-        for (int j = 0; j < kPer; j += 2) acc_pair(acc, f[j], f[j + 1], nm2, c2);
-    }
-    acc_pair(acc, zt, -INFINITY, nm2, c2);
-    float s0, s1, q0, q1;
-    unpair(acc.S, s0, s1); unpair(acc.Q, q0, q1);
-    p.S = warp_sum(s0 + s1); p.Q = warp_sum(q0 + q1);
+        for (int u = 0; u < kVecs; ++u) {
+            float f[kPer];
+            Elems<kBf16>::unpack(q[u], f);
+#pragma unroll
+            for (int j = 0; j < kPer; j += 2) acc_pair(acc, f[j], f[j + 1], nm2, c2);
+        }
+        acc_pair(acc, zt, -INFINITY, nm2, c2);
+        float s0, s1, q0, q1;
+        unpair(acc.S, s0, s1); unpair(acc.Q, q0, q1);
+        p.S = warp_sum(s0 + s1); p.Q = warp_sum(q0 + q1);
 
-    int n = 0;
-    if (a.k > 0 && !p.bad) {
-        const uint32_t own[1] = {key_of(mx)};
-        const float thr = fmaxf(value_of(kth_largest<1, kBf16 ? 16 : 20>(own, a.k)), kLowest);
-        if (lane == 0) sh.n_cand = 0;
-        __syncwarp();
-        if (mx >= thr) {
+        int n = 0;
+        if (a.k > 0 && !p.bad) {
+            const float thr = kth_of_lanes(mx, a.k);
+            const uint32_t below = (1u << lane) - 1u;
+            int n_hot = 0;
 #pragma unroll
             for (int u = 0; u < kVecs; ++u) {
-                float f[kPer];
-                Elems<kBf16>::unpack(q[u], f);
-#pragma unroll
-                for (int j = 0; j < kPer; ++j) {
-                    if (f[j] >= thr) {
-                        const int at = atomicAdd(&sh.n_cand, 1);
-                        if (at < kCandWarp) sh.cand[at] = entry_of(f[j], (u * 32 + lane) * kPer + j);
-                    }
-                }
+                const uint32_t b = __ballot_sync(0xffffffffu, vm[u] >= thr);
+                if (b == 0) continue;
+                const int at = n_hot + __popc(b & below);
+                if (vm[u] >= thr && at < kHotVecs) { ws.hot[at] = q[u]; ws.hot_vec[at] = u * 32 + lane; }
+                n_hot += __popc(b);
             }
-            if (zt >= thr) {
-                const int at = atomicAdd(&sh.n_cand, 1);
-                if (at < kCandWarp) sh.cand[at] = entry_of(zt, tail);
-            }
-        }
-        __syncwarp();
-        n = sh.n_cand;
-        if (n <= kCandWarp) {
-            rank_entries(sh.cand, n, a.k, sh.list, lane, 32);
-            n = min(n, a.k);
-        } else {                                                   // ties: the rules of select_top, from memory
-            sh.tmax[lane] = mx;
             __syncwarp();
-            const Span sp = {row, 0, nvec, nvec << kLog2Per, a.V};
-            select_top<kBf16, 32, kCandWarp>(sh, sp, a.k, lane);
-            n = sh.n_list;
+            n = n_hot > kHotVecs ? kCandWarp + 1 : 0;
+            for (int i = 0; i < n_hot * kPer && n <= kCandWarp; i += 32) {         // a lane per entry
+                const int e = i + lane, h = e >> kLog2Per, j = e & (kPer - 1);
+                const float z = e < n_hot * kPer ? Elems<kBf16>::load1(&ws.hot[h], j) : -INFINITY;
+                const uint32_t b = __ballot_sync(0xffffffffu, z >= thr);
+                const int at = n + __popc(b & below);
+                if (z >= thr && at < kCandWarp) ws.team.cand[at] = entry_of(z, ws.hot_vec[h] * kPer + j);
+                n += __popc(b);
+            }
+            const uint32_t b = __ballot_sync(0xffffffffu, zt >= thr);
+            if (b) {
+                const int at = n + __popc(b & below);
+                if (zt >= thr && at < kCandWarp) ws.team.cand[at] = entry_of(zt, tail);
+                n += __popc(b);
+            }
+            __syncwarp();
+            if (n <= kCandWarp) {
+                rank_entries(ws.team.cand, n, a.k, ws.list[r], lane, 32);
+                n = min(n, a.k);
+            } else {                                               // ties: the rules of select_top, from memory
+                ws.team.tmax[lane] = mx;
+                __syncwarp();
+                const Span sp = {row, 0, nvec, nvec << kLog2Per, a.V};
+                select_top<kBf16, 32, kCandWarp>(ws.team, sp, a.k, lane);
+                n = ws.team.n_list;
+                if (lane < n) ws.list[r][lane] = ws.team.list[lane];
+            }
+            __syncwarp();
         }
-        __syncwarp();
+        if (lane == r) { mine = p; my_list = n; }
     }
-    write_row(a, t, p, sh.list, n, zy, y_state, lane, 32);
+
+    const RowOut o = row_out(a, mine);
+    if (lane < n_rows) write_scalars(a, t0 + lane, mine, o, zy, y_state);
+    for (int r = 0; r < n_rows; ++r) {
+        const float m = __shfl_sync(0xffffffffu, mine.m, r), l = __shfl_sync(0xffffffffu, o.l, r);
+        const int bad = __shfl_sync(0xffffffffu, mine.bad, r), n = __shfl_sync(0xffffffffu, my_list, r);
+        if (lane < a.k) write_top(a, t0 + r, lane, m, l, bad, ws.list[r], n);
+    }
 }
 
-// kCluster: the CTAs of a cluster split the row (blockIdx.x / cluster size = row).  Else kTeams teams per CTA, a row each.
-template <bool kBf16, int kThreads, int kTeams, bool kCluster>
-__global__ void __launch_bounds__(kThreads * kTeams)
+// A CTA per row; kCluster: the CTAs of a cluster split it (blockIdx.x / cluster size = row).
+template <bool kBf16, int kThreads, bool kCluster>
+__global__ void __launch_bounds__(kThreads)
 token_logprobs_kernel(const Args a) {
     constexpr int kPer = Elems<kBf16>::kPerVec, kLog2Per = kBf16 ? 3 : 2;
-    constexpr int kCap = kThreads == 32 ? kCandWarp : kCand;
     constexpr int kUnroll = 4;
-    __shared__ TeamShared<kThreads, kCap> shared[kTeams];
-    const int team = kTeams == 1 ? 0 : threadIdx.x / kThreads;
-    const int tid = kTeams == 1 ? threadIdx.x : threadIdx.x % kThreads;
-    const int lane = tid & 31, warp = tid >> 5;
-    TeamShared<kThreads, kCap>& sh = shared[team];
+    __shared__ TeamShared<kThreads, kCand> sh;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const long long T = a.n_tokens_dev ? min((long long)*a.n_tokens_dev, a.T_max) : a.T_max;
     unsigned rank = 0, C = 1;
     if constexpr (kCluster) { C = cg::this_cluster().num_blocks(); rank = cg::this_cluster().block_rank(); }
-    const long long t = kCluster ? (long long)(blockIdx.x / C) : (long long)blockIdx.x * kTeams + team;
-    if (t >= T) return;                                            // the whole team (and cluster) leaves together
+    const long long t = (long long)(blockIdx.x / C);
+    if (t >= T) return;                                            // the whole cluster leaves together
 
     const char* row = a.logits + t * a.row_bytes;
     const int nvec = a.V >> kLog2Per;
@@ -503,14 +544,12 @@ token_logprobs_kernel(const Args a) {
     Part p = acc_part(acc);
     if (a.k > 0) sh.tmax[tid] = p.S > 0.0f ? p.m : -INFINITY;      // nothing but -inf seen: not a maximum
     p = warp_join(p, a.c);
-    if constexpr (kThreads > 32) {
-        if (lane == 0) sh.part[warp] = p;
-        __syncthreads();
-        if (warp == 0) p = warp_join(lane < kThreads / 32 ? sh.part[lane] : Part{kLowest, 0.0f, 0.0f, 0}, a.c);
-    }
+    if (lane == 0) sh.part[warp] = p;
+    __syncthreads();
+    if (warp == 0) p = warp_join(lane < kThreads / 32 ? sh.part[lane] : Part{kLowest, 0.0f, 0.0f, 0}, a.c);
     if (tid == 0) sh.row = p;
-    team_sync<kThreads>();
-    if (a.k > 0 && !sh.row.bad) select_top<kBf16, kThreads, kCap>(sh, sp, a.k, tid);
+    __syncthreads();
+    if (a.k > 0 && !sh.row.bad) select_top<kBf16, kThreads, kCand>(sh, sp, a.k, tid);
 
     if constexpr (kCluster) {
         cg::cluster_group cl = cg::this_cluster();
@@ -547,7 +586,12 @@ token_logprobs_kernel(const Args a) {
         __syncthreads();
     }
 
-    write_row(a, t, sh.row, sh.list, sh.n_list, zy, y_state, tid, kThreads);
+    if (warp == 0) {                                               // k <= 32: one warp writes all
+        const Part r = sh.row;
+        const RowOut o = row_out(a, r);
+        if (lane == 0) write_scalars(a, t, r, o, zy, y_state);
+        if (lane < a.k) write_top(a, t, lane, r.m, o.l, r.bad, sh.list, sh.n_list);
+    }
 }
 
 // ---- backward -----------------------------------------------------------------------------------------
@@ -636,38 +680,46 @@ token_logprobs_bwd_kernel(const BwdArgs a) {
 }
 
 // ---- host side ---------------------------------------------------------------------------------------
-template <bool kBf16, int kThreads, int kTeams, bool kCluster>
+template <bool kBf16, int kThreads, bool kCluster>
 static int launch_fwd(const Args& a, int C, cudaStream_t s) {
-    auto kernel = token_logprobs_kernel<kBf16, kThreads, kTeams, kCluster>;
+    auto kernel = token_logprobs_kernel<kBf16, kThreads, kCluster>;
+    if (!kCluster) {
+        kernel<<<(unsigned)a.T_max, kThreads, 0, s>>>(a);
+        DPPO_CHECK_LAUNCH("token_logprobs launch");
+        return DPPO_OK;
+    }
+    if (a.T_max * C > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "token_logprobs: T_max=%lld needs too large a grid", a.T_max);
     cudaLaunchConfig_t cfg = {};
-    const long long teams = kCluster ? a.T_max * C : (a.T_max + kTeams - 1) / kTeams;
-    if (teams > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "token_logprobs: T_max=%lld needs too large a grid", a.T_max);
-    cfg.gridDim = dim3((unsigned)teams, 1, 1);
-    cfg.blockDim = dim3(kThreads * kTeams, 1, 1);
+    cfg.gridDim = dim3((unsigned)(a.T_max * C), 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = kCluster ? 1 : 0;
+    cfg.attrs = attr; cfg.numAttrs = 1;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
     if (e != cudaSuccess) return cuda_fail(e, "token_logprobs launch");
     return DPPO_OK;
 }
 
 template <bool kBf16, int kVecs> static int launch_warp(const Args& a, cudaStream_t s) {
-    constexpr int kTeams = 8;
-    token_logprobs_warp_kernel<kBf16, kVecs, kTeams><<<(unsigned)((a.T_max + kTeams - 1) / kTeams), 32 * kTeams, 0, s>>>(a);
+    constexpr int kTeams = 4;
+    // as many rows per warp as make one wave of warps (about 32 resident per SM), 8 at most
+    const long long wave = 32ll * sm_count(), per = (a.T_max + wave - 1) / wave;
+    const int run = (int)(per < 1 ? 1 : per > kMaxRun ? kMaxRun : per);
+    const long long warps = (a.T_max + run - 1) / run;
+    token_logprobs_warp_kernel<kBf16, kVecs, kTeams><<<(unsigned)((warps + kTeams - 1) / kTeams), 32 * kTeams, 0, s>>>(a, run);
     DPPO_CHECK_LAUNCH("token_logprobs launch");
     return DPPO_OK;
 }
 
 template <bool kBf16> static int run_fwd(const Args& a, int variant, cudaStream_t s) {
+    const int nvec = a.V >> (kBf16 ? 3 : 2);
     int C = 1, threads = 256;
     if (variant == 0) {
-        const int nvec = a.V >> (kBf16 ? 3 : 2);
         if (nvec <= 256) { threads = 32; }
         else {
-            while (C < 8 && a.T_max * C * 2 <= 2ll * sm_count() && nvec / (2 * C) >= 256) C *= 2;
+            while (C < 8 && a.T_max * C * 2 <= 3ll * sm_count() && nvec / (2 * C) >= 256) C *= 2;
             threads = C == 1 && nvec <= 2048 ? 128 : 256;
         }
     } else if (variant == 32) {
@@ -676,19 +728,16 @@ template <bool kBf16> static int run_fwd(const Args& a, int variant, cudaStream_
         C = variant / 10000; threads = variant % 10000;
     }
     if (threads == 32 && C == 1) {
-        const int nvec = a.V >> (kBf16 ? 3 : 2);
         if (nvec <= 128) return launch_warp<kBf16, 4>(a, s);
         if (nvec <= 256) return launch_warp<kBf16, 8>(a, s);
-        if (nvec <= 512) return launch_warp<kBf16, 16>(a, s);
     }
-    if (threads == 32 && C == 1) return launch_fwd<kBf16, 32, 8, false>(a, 1, s);
-    if (C == 1 && threads == 128) return launch_fwd<kBf16, 128, 1, false>(a, 1, s);
-    if (C == 1 && threads == 256) return launch_fwd<kBf16, 256, 1, false>(a, 1, s);
-    if (C == 1 && threads == 512) return launch_fwd<kBf16, 512, 1, false>(a, 1, s);
+    if (C == 1 && threads == 128) return launch_fwd<kBf16, 128, false>(a, 1, s);
+    if (C == 1 && threads == 256) return launch_fwd<kBf16, 256, false>(a, 1, s);
+    if (C == 1 && threads == 512) return launch_fwd<kBf16, 512, false>(a, 1, s);
     if (C == 2 || C == 4 || C == 8) {
-        if (threads == 128) return launch_fwd<kBf16, 128, 1, true>(a, C, s);
-        if (threads == 256) return launch_fwd<kBf16, 256, 1, true>(a, C, s);
-        if (threads == 512) return launch_fwd<kBf16, 512, 1, true>(a, C, s);
+        if (threads == 128) return launch_fwd<kBf16, 128, true>(a, C, s);
+        if (threads == 256) return launch_fwd<kBf16, 256, true>(a, C, s);
+        if (threads == 512) return launch_fwd<kBf16, 512, true>(a, C, s);
     }
     return fail(DPPO_ERR_UNSUPPORTED, "token_logprobs: variant %d", variant);
 }

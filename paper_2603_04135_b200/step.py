@@ -12,9 +12,9 @@ from . import dp
 
 def quantize_rows_i8(x, status=None):
     """8-bit codes and scales of the rows of x (bf16 or f32 [M, K] with rows on 16 bytes): (q int8 [M, K], scale f32 [M]), q a
-    view of rows padded to 16 bytes.  Weights are quantised once this way and kept; see DppoStep.score_hidden_i8."""
+    view of padded rows.  Weights are quantised once this way and kept; see DppoStep.score_hidden_i8."""
     M, K = x.shape
-    ld = (K + 15) // 16 * 16
+    ld = (K + 127) // 128 * 128            # whole 128-byte lines: the product's slabs then never straddle two
     q = torch.zeros(M, ld, dtype=torch.int8, device=x.device)
     scale = torch.zeros(M, dtype=torch.float32, device=x.device)
     B.quantize_rows_i8(B.QuantizeParams(M, K, B.BF16 if x.dtype is torch.bfloat16 else B.F32, x.stride(0) if M > 1 else max(x.stride(0), K), ld),
@@ -170,7 +170,7 @@ class DppoStep:
         if T == 0:
             return out
         V, C = W_scale.numel(), min(chunk_tokens, T)
-        ldq, ldv = (H + 15) // 16 * 16, (V + 3) // 4 * 4
+        ldq, ldv = (H + 127) // 128 * 128, (V + 3) // 4 * 4
         need = (C, ldv, ldq)
         if getattr(self, "_score_scratch_shape", None) != need:
             self._score_scratch = (torch.zeros(C, ldv, dtype=torch.float32, device=self.device),

@@ -71,7 +71,7 @@ def row_eps(z, tau, V, variant):
         x = np.where(z > -np.inf, (z - m) / tau, 0.0)
         e = np.where(z > -np.inf, np.exp(x), 0.0)
         ex = np.abs(e * x).sum(1) / np.maximum(e.sum(1), 1e-300)
-    threads = 32 if (variant == 32 or (variant == 0 and V <= 4096)) else 128
+    threads = 32 if (variant == 32 or (variant == 0 and V <= 2055)) else 128      # up to 256 vectors (and a tail): a warp
     n = math.ceil(V / threads)
     return (3 * ex + 3 + n + 5 * n + 16) * U, ex, e.sum(1)
 
@@ -136,7 +136,7 @@ def test_forward(B, T, V, k, tau, dtype):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("variant", [32, 10128, 10256, 10512, 20128, 20256, 20512, 40128, 40256, 40512, 80128, 80256, 80512])
 def test_every_launch_shape(B, variant, dtype):
-    for T, V in ((3, 5003), (2, 40), (1, 3)):                        # fewer vectors than CTAs too
+    for T, V in ((3, 1001 if variant == 32 else 5003), (2, 40), (1, 3)):          # fewer vectors than CTAs too
         z, y = make(T, V, dtype, V)
         run(B, z, V, y, 20, 0.9, variant)
 
@@ -176,7 +176,7 @@ def special_rows(V, dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V, k, variant", [(9, 4, 0), (1000, 20, 0), (1500, 20, 0), (2001, 32, 0), (3500, 8, 0), (4099, 32, 0), (8200, 5, 0), (20000, 20, 10128), (20003, 20, 0),
-                                           (20003, 32, 10512), (20003, 7, 40256), (20003, 20, 80128), (20003, 32, 32)])
+                                           (20003, 32, 10512), (20003, 7, 40256), (20003, 20, 80128), (1027, 32, 32)])
 def test_special_rows(B, V, k, variant, dtype):
     rows = special_rows(V, dtype)
     z = torch.zeros(rows.shape[0], pad16(V, 2 if dtype == "bf16" else 4), dtype=DT[dtype], device="cuda")
@@ -252,6 +252,30 @@ def test_rows_past_4_gib(B):
     B.token_logprobs_backward(B.LogprobParams(T, V, B.F32, V, 0, 0, 1.0), z, y, None, f.stats, a, None, d)
     p = math.exp(o["logp"][8998] + 20)
     assert abs(d[8998, 17].item() + p) < 1e-4 and abs(d[8998, V - 1].item() - 1) < 1e-4 and abs(d[8999, V - 1].item() - (1 - p)) < 1e-4
+
+
+@pytest.mark.parametrize("T, V, dtype", [(4737, 37, "bf16"), (20011, 260, "f32"), (40001, 9, "f32"), (9000, 1500, "bf16")])
+def test_many_short_rows(B, T, V, dtype):
+    """A warp takes several rows here: every row is what it is in a call of its own."""
+    z, y = make(T, V, dtype, T)
+    y[T - 3] = -1
+    f = Fwd(B, z, V, y, 6, 1.0)
+    o = f.host()
+    assert f.status.item() == B.STATUS_BAD_TARGET
+    few = [0, 1, 7, 8, 4735, T // 2, T - 3, T - 2, T - 1]
+    for t in few:
+        one = Fwd(B, z[t:t + 1], V, y[t:t + 1], 6, 1.0).host()
+        for n in o:
+            assert np.array_equal(o[n][t:t + 1], one[n]), (n, t)
+    z64 = z[:, :V].double()
+    lnp = torch.log_softmax(z64, 1)
+    ok = torch.arange(T) != T - 3
+    want = lnp.gather(1, y.clamp_min(0).long()[:, None])[:, 0].cpu()
+    # row_eps at its largest here: E|x| < 10, V / 32 < 48, and 4 u |l| + 4 u |x_y| + u |logp| < 150 u
+    tol = (3 * 10 + 6 * 48 + 19 + 150) * U
+    assert float((torch.from_numpy(o["logp"]).double() - want)[ok].abs().max()) < tol
+    key = torch.sort(z64, dim=1, descending=True, stable=True)
+    assert torch.equal(torch.from_numpy(o["top_ids"]).long(), key.indices[:, :6].cpu())
 
 
 # ---- backward --------------------------------------------------------------------------------------
@@ -399,6 +423,35 @@ def test_linear_i8(B, M, N, K, variant, out_dtype):
     assert bool((out[:M, N:] == 5.0).all()) and bool((out[M:] == 5.0).all())
 
 
+@pytest.mark.parametrize("M", [33, 64, 65, 96, 128, 160, 192, 224, 250, 256, 480])
+def test_linear_i8_every_token_tile(B, M):
+    """594 channel tiles: the pair kernel takes the token tile that holds M with the least waves (64, 96, ... 256)."""
+    N, K = 151936, 48
+    x, w = codes(M, K, K, M), codes(N, K, K, 7)
+    xs, ws = torch.rand(M, device="cuda"), torch.rand(N, device="cuda")
+    out = torch.zeros(M, N, device="cuda")
+    B.linear_i8(B.LinearI8Params(M, N, K, K, K, N, B.F32, 1), x, xs, w, ws, out)
+    assert torch.equal(out.cpu(), torch.from_numpy(f32_product(x, xs, w, ws)))
+
+
+def test_quantize_then_product_is_ordered(B):
+    """The product starts setting up while the quantisation runs: it must still see all of its rows, call after call."""
+    M, N, K = 3000, 512, 1024
+    w = codes(N, K, K, 7)
+    ws = torch.rand(N, device="cuda")
+    xs = [torch.randn(M, K, device="cuda") * (i + 1) for i in range(4)]
+    q, s = torch.zeros(M, K, dtype=torch.int8, device="cuda"), torch.zeros(M, device="cuda")
+    outs = [torch.zeros(M, N, device="cuda") for _ in xs]
+    for _ in range(3):
+        for x, out in zip(xs, outs):
+            B.quantize_rows_i8(B.QuantizeParams(M, K, B.F32, K, K), x, q, s)
+            B.linear_i8(B.LinearI8Params(M, N, K, K, K, N, B.F32), q, s, w, ws, out)
+    for x, out in zip(xs, outs):
+        wq, wsc = scoring.quantize_rows_i8(x.cpu().numpy())
+        want = f32_product(torch.from_numpy(wq).cuda(), torch.from_numpy(wsc), w, ws)
+        assert torch.equal(out.cpu(), torch.from_numpy(want))
+
+
 @pytest.mark.parametrize("M, variant", [(1, 2), (16, 2), (40, 2), (100, 2), (256, 1), (256, 2)])
 def test_linear_i8_extreme_sums(B, M, variant):
     """Every product is (-128)^2 or -128 * 127: the sums reach the ends of int32."""
@@ -452,7 +505,7 @@ def test_linear_i8_bounded_waits(B, variant):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("M, K", [(1, 1), (3, 7), (5, 8), (2, 129), (9, 2560), (4, 4097), (2, 30001), (300, 64)])
+@pytest.mark.parametrize("M, K", [(1, 1), (3, 7), (5, 8), (2, 129), (9, 2560), (4, 4097), (2, 30001), (300, 64), (5000, 1000), (2, 4096), (6, 4104)])
 def test_quantize_rows(B, M, K, dtype):
     ldx, ldq = pad16(K, 2 if dtype == "bf16" else 4), (K + 15) // 16 * 16 + 16
     x = torch.empty(M, ldx, device="cuda").normal_(0, 3).to(DT[dtype])
@@ -460,7 +513,7 @@ def test_quantize_rows(B, M, K, dtype):
     if M > 2:
         x[0, :K] = 0
         x[1, K // 2] = math.inf
-        x[2, :K] = torch.arange(K, device="cuda").to(DT[dtype]) * 0.5
+        x[2, :K] = (torch.arange(K, device="cuda") % 255 - 127).to(DT[dtype]) * 0.5      # many exact ties
     if M > 4:
         x[3, K - 1] = math.nan
         x[4, :K] = 1e-42                                                    # the scale underflows
