@@ -407,17 +407,37 @@ linear_i8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
     if (split > 1) {
         lm_cluster_sync();                                               // every CTA's sums are in its shared memory
         if (live) {
-            for (int c = part; c < kNB && t_tile + c < T; c += split) {  // this CTA's share of the tokens
-                const uint32_t local = tiles + (uint32_t)(c * kTileM + row) * 4u;
-                int32_t sum = 0;
-                for (int r = 0; r < split; ++r) {
-                    uint32_t remote;
-                    int32_t x;
-                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(local), "r"(r));
-                    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(x) : "r"(remote) : "memory");
-                    sum += x;
+            // this CTA's share of the tokens: part, part + split, ...; a batch's loads are all under way before the first is used
+            // (one token at a time, each waits out the latency of its remote reads: 128 tokens 31 us instead of 14)
+            constexpr int kBatch = 8;
+            const int n_tok = (int)min((long long)kNB, T - t_tile);
+            for (int c0 = part; c0 < n_tok; c0 += kBatch * split) {
+                int32_t sum[kBatch];
+                float sx[kBatch];
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    sum[i] = 0;
+                    sx[i] = c0 + i * split < n_tok ? a.x_scale[t_tile + c0 + i * split] : 0.0f;
                 }
-                if (ch < a.N) store<kBf16>(a, t_tile + c, ch, value_of(sum, a.x_scale[t_tile + c], sw));
+                for (int i0 = 0; i0 < split; ++i0) {                     // every CTA starts with another one's memory
+                    const int r = (part + i0) & (split - 1);
+                    int32_t x[kBatch];
+                    uint32_t remote;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(tiles + (uint32_t)row * 4u), "r"(r));
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i) {
+                        const int c = c0 + i * split;
+                        x[i] = 0;
+                        if (c < n_tok)
+                            asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(x[i]) : "r"(remote + (uint32_t)(c * kTileM) * 4u) : "memory");
+                    }
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i) sum[i] += x[i];
+                }
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i)
+                    if (c0 + i * split < n_tok && ch < a.N)
+                        store<kBf16>(a, t_tile + c0 + i * split, ch, value_of(sum[i], sx[i], sw));
             }
         }
         lm_cluster_sync();                                               // the others have read this CTA's shared memory
@@ -574,18 +594,34 @@ static void set_attributes(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[
     cfg.attrs = attr; cfg.numAttrs = 2;
 }
 
-// Tokens per tile of the pair kernel: the tile that needs the least time over whole waves of pairs.  A K slab of a tile costs
-// about (256 + tile) units: a tile of 256 keeps the tensor cores and the operand fetches equally busy, a narrower one is bound
-// by fetching the weights' 16 KB.  (1,003 x 5,003 x 2,563: 140 tiles of 160 in two waves instead of 80 of 256 in two.)
-static int pair_tile(long long M, int N) {
+// ---- which kernel, which tile ----
+// Both kernels' times in microseconds, from sweeps over N = 64 to 151,936, K = 64 to 9,728 and 1 to 1,003 tokens: the choice
+// they give was the faster one or within 5 % of it at nine shapes of ten, and 20 % off at worst.
+//
+// Pair kernel: whole waves of tiles; a 128-code slab of a tile costs about (256 + tokens) ns: 256 tokens keep the tensor cores
+// and the operand fetches equally busy, fewer are bound by fetching the weights' 16 KB.  The token tile is the one with the
+// least time (1,003 x 5,003 x 2,563: 140 tiles of 160 in two waves instead of 80 of 256 in two; 27 -> 23 us).
+static double pair_time(long long M, int N, int n_ksteps, int* tile) {
     const long long n_m2 = (N + 255) / 256, pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
-    int best = kTileN;
-    long long best_cost = 0;
+    double best = 0.0;
     for (int tn = kTileN; tn >= 64; tn -= 32) {
-        const long long tiles = n_m2 * ((M + tn - 1) / tn), cost = (tiles + pairs - 1) / pairs * (256 + tn);
-        if (best_cost == 0 || cost < best_cost) { best = tn; best_cost = cost; }
+        const long long tiles = n_m2 * ((M + tn - 1) / tn), waves = (tiles + pairs - 1) / pairs;
+        const double t = 4.2 + 1e-3 * (double)waves * n_ksteps * (256 + tn);
+        if (best == 0.0 || t < best) { best = t; *tile = tn; }
     }
     return best;
+}
+// The other: the contraction is split while two CTAs per SM have room and each keeps two slabs; the join costs a few
+// microseconds (64 tokens: 2), more than it gains only where there are few slabs.
+static double small_time(long long M, int N, int n_ksteps, int* tokens, int* split) {
+    const int nb = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    const long long tiles = (long long)((N + kTileM - 1) / kTileM) * ((M + nb - 1) / nb), sms = sm_count();
+    int sp = 1;
+    while (sp < 8 && tiles * sp * 2 <= 2 * sms && n_ksteps >= 4 * sp) sp *= 2;
+    *tokens = nb; *split = sp;
+    const double waves = (double)((tiles * sp + 2 * sms - 1) / (2 * sms)), load = (double)(tiles * sp) / (double)sms;
+    const double shared = waves > 1.0 ? 1.5 : load * 0.75 > 1.0 ? load * 0.75 : 1.0;          // two CTAs on an SM slow each other
+    return 3.6 + waves * ((n_ksteps + sp - 1) / sp) * (0.2 + 0.0024 * nb) * shared + (sp > 1 ? 0.6 + 0.03 * nb : 0.0);
 }
 
 template <bool kBf16> static int launch_pair(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
@@ -606,15 +642,13 @@ template <bool kBf16> static int launch_pair(const CUtensorMap& mw, const CUtens
     return DPPO_OK;
 }
 
-template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
+template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, int split, cudaStream_t s) {
     auto kernel = linear_i8_small_kernel<kNB, kBf16>;
     static bool raised[64];
     const int rc = raise_smem(kernel, small_smem<kNB>(), raised);
     if (rc != DPPO_OK) return rc;
     const int n_ch = (a.N + kTileM - 1) / kTileM;
     const long long tiles = (long long)n_ch * ((a.M_max + kNB - 1) / kNB);
-    int split = 1;                                                       // enough CTAs for two per SM, two slabs at least each
-    while (split < 8 && tiles * split * 2 <= 2ll * sm_count() && a.n_ksteps >= 4 * split) split *= 2;
     if (tiles * split > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "linear_i8: too many tiles");
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * split), 1, 1);
@@ -628,13 +662,13 @@ template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, co
     return DPPO_OK;
 }
 
-template <bool kBf16> static int launch(bool pair, int nb, const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
+template <bool kBf16> static int launch(bool pair, int nb, int split, const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
     if (pair) return launch_pair<kBf16>(mw, mx, a, s);
     switch (nb) {
-        case 16: return launch_small<16, kBf16>(mw, mx, a, s);
-        case 32: return launch_small<32, kBf16>(mw, mx, a, s);
-        case 64: return launch_small<64, kBf16>(mw, mx, a, s);
-        default: return launch_small<128, kBf16>(mw, mx, a, s);
+        case 16: return launch_small<16, kBf16>(mw, mx, a, split, s);
+        case 32: return launch_small<32, kBf16>(mw, mx, a, split, s);
+        case 64: return launch_small<64, kBf16>(mw, mx, a, split, s);
+        default: return launch_small<128, kBf16>(mw, mx, a, split, s);
     }
 }
 
@@ -692,15 +726,14 @@ extern "C" int dppo_linear_i8(const dppo_linear_i8_params* p, const int8_t* x, c
     a.N = p->N; a.n_ksteps = (p->K + i8::kBK - 1) / i8::kBK; a.out_bf16 = p->out_dtype == DPPO_BF16;
     a.wait_limit_ns = p->variant >= 100 ? kSelfTestWaitLimitNs : kDefaultWaitLimitNs;
     a.test_extra_tx = p->variant >= 100 ? 16 : 0;
-    // The pair kernel from half a wave of its 256 x 256 tiles on; below that, and for up to 128 tokens, the other
-    const long long pair_tiles = (long long)((p->N + 255) / 256) * ((p->M_max + 255) / 256);
-    const bool pair = variant == 1 || (variant == 0 && p->M_max > 128 && pair_tiles * 4 >= sm_count());
-    a.tile_n = pair ? i8::pair_tile(p->M_max, p->N) : 0;
-    const int nb = pair ? a.tile_n / 2 : p->M_max <= 16 ? 16 : p->M_max <= 32 ? 32 : p->M_max <= 64 ? 64 : 128;
+    int nb = 0, split = 1;
+    const double t_pair = i8::pair_time(p->M_max, p->N, a.n_ksteps, &a.tile_n), t_small = i8::small_time(p->M_max, p->N, a.n_ksteps, &nb, &split);
+    const bool pair = variant == 1 || (variant == 0 && t_pair < t_small);
+    if (pair) nb = a.tile_n / 2;
     alignas(64) CUtensorMap mw, mx;
     int rc = i8::make_map(&mw, w, p->N, p->K, p->w_stride, i8::kTileM);
     if (rc == DPPO_OK) rc = i8::make_map(&mx, x, p->M_max, p->K, p->x_stride, nb);
     if (rc != DPPO_OK) return rc;
     cudaStream_t s = (cudaStream_t)stream;
-    return a.out_bf16 ? i8::launch<true>(pair, nb, mw, mx, a, s) : i8::launch<false>(pair, nb, mw, mx, a, s);
+    return a.out_bf16 ? i8::launch<true>(pair, nb, split, mw, mx, a, s) : i8::launch<false>(pair, nb, split, mw, mx, a, s);
 }
