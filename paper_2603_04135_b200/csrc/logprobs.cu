@@ -1,10 +1,9 @@
 // Log-probs of given tokens with entropy and top alternatives, and their gradient with respect to the logits.
 //
-// Forward.  Per row: m = max z, S = sum e_v and Q = sum e_v (z_v - m) with e_v = 2^((z_v - m) c), c = log2(e)/tau;
-// then l = ln S, lse = m/tau + l, logp = (z_y - m)/tau - l and entropy = l - Q/(S tau) (both terms are >= 0: nothing
+// Forward.  Per row: m = max z, S = sum e_v and Q = sum e_v y_v with y_v = (z_v - m) c, e_v = 2^y_v, c = log2(e)/tau;
+// then l = ln S, lse = m/tau + l, logp = (z_y - m)/tau - l and entropy = l - ln2 Q/S (both terms are >= 0: nothing
 // cancels on a peaked row).  One pass: every thread keeps an ONLINE (m, S, Q) over the 16-byte vectors it sees; a larger
-// maximum M rescales them, S' = S 2^((m-M)c), Q' = (Q + (m-M) S) 2^((m-M)c).  (z_v - m) is formed first and
-// scaled afterwards, so that rows of any magnitude (masks of the type's lowest value included) keep their differences.
+// maximum M moves them by D = (m - M) c: S' = S 2^D, Q' = (Q + D S) 2^D.
 //
 // The alternatives cost the pass nothing.  A thread's running maximum is known anyway at the end of the row, and the
 // k-th largest of the threads' maxima, thr, is a lower bound of the k-th largest entry (k threads have an entry that
@@ -20,6 +19,8 @@
 // reduction: a streaming map, one read and one write per element.
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 #include "grpo_loss.cuh"
 
@@ -33,7 +34,7 @@ constexpr int kMaxTop = 32;
 constexpr int kCand = 512;                // candidate buffer of a CTA-sized team
 constexpr int kCandWarp = 128;            // and of a warp-sized one
 constexpr float kLowest = -3.402823466e38f;
-constexpr float kFar = -1e30f;            // differences are held at or above this: 0 * (-inf) never arises
+constexpr float kFar = -2000.0f;          // exponents are held at or above this (2^-2000 is 0): 0 * (-inf) never arises
 
 struct Args {
     const char* logits;
@@ -57,8 +58,8 @@ struct Part {
 };
 
 __device__ __forceinline__ void rescale(Part& p, float M, float c) {
-    const float d = fmaxf(p.m - M, kFar), f = ex2(d * c);
-    p.Q = (p.Q + d * p.S) * f;
+    const float D = fmaxf((p.m - M) * c, kFar), f = ex2(D);
+    p.Q = fmaf(D, p.S, p.Q) * f;
     p.S *= f;
     p.m = M;
 }
@@ -105,41 +106,115 @@ __device__ __forceinline__ uint4 load_vec_rw(const void* p) {
 }
 
 // Running sums of a thread: pairs, so that the packed f32x2 instructions take two elements at a time.
+//
+// What bounds a long sweep is the 1000 W limit (at 6 TB/s of bf16 logits the clock falls from 1.9 to 1.6 GHz), so what
+// counts is how little is done per element.  On ordinary rows ("quick") the exponent is one fma, y' = z c - r with
+// r = fl(m c); all sums of the thread then carry the same shift res = m c - r (exact in f32), which comes out when m grows
+// and at the end of the row.  bf16 entries so low that their exponential is 0 are lifted to m + kFar / c by a packed
+// maximum, two per instruction.  Rows of other magnitudes (|m c| > 2^20: masks of the type's lowest value with
+// nothing above, logits of 10^6) take the differences z - m first, so they keep them.
 struct Acc {
     f32x2 S, Q;
-    float m;
-    int bad;
+    float m, nr, res;                     // maximum; -r and m c - r (0 unless quick)
+    uint32_t m2, low2;                    // bf16 pairs: the maximum, and what lower entries are lifted to
+    int quick, bad;
 };
-__device__ __forceinline__ void acc_init(Acc& a) { a.S = a.Q = pair_of(0.0f, 0.0f); a.m = kLowest; a.bad = 0; }
+__device__ __forceinline__ uint32_t bf16_pair(__nv_bfloat16 x) {
+    const __nv_bfloat162 p = __halves2bfloat162(x, x);
+    return *reinterpret_cast<const uint32_t*>(&p);
+}
+// The frame of maximum m.
+__device__ __forceinline__ void acc_frame(Acc& a, float m, float c) {
+    const float r = m * c;
+    a.quick = fabsf(r) <= 1048576.0f && fabsf(m) <= 1e37f;
+    a.m = m; a.nr = -r;
+    a.res = a.quick ? fmaf(m, c, -r) : 0.0f;
+    a.m2 = bf16_pair(__float2bfloat16_rn(m));                      // exact where the entries are bf16
+    a.low2 = bf16_pair(__float2bfloat16_rd(m + kFar / c));
+}
+__device__ __forceinline__ void acc_init(Acc& a, float m, float c) {
+    a.S = a.Q = pair_of(0.0f, 0.0f); a.bad = 0;
+    acc_frame(a, m, c);
+}
 __device__ __forceinline__ Part acc_part(const Acc& a) {
     float s0, s1, q0, q1;
     unpair(a.S, s0, s1); unpair(a.Q, q0, q1);
-    return {a.m, s0 + s1, q0 + q1, a.bad};
+    const float S = s0 + s1, f = ex2(-a.res);
+    return {a.m, S * f, fmaf(-a.res, S, q0 + q1) * f, a.bad};
 }
 __device__ __forceinline__ void acc_grow(Acc& a, float vmax, float c) {
     if (!(vmax < INFINITY)) { a.bad = 1; return; }                 // NaN or +inf: the row's results are NaN
-    const float d = fmaxf(a.m - vmax, kFar), f = ex2(d * c);
-    a.Q = mul2(fma2(pair_of(d, d), a.S, a.Q), pair_of(f, f));
+    const float x = (a.m - vmax) * c, res = a.res;
+    acc_frame(a, vmax, c);
+    const float D = fmaxf(x + (a.res - res), kFar), f = ex2(D);
+    a.Q = mul2(fma2(pair_of(D, D), a.S, a.Q), pair_of(f, f));
     a.S = mul2(a.S, pair_of(f, f));
-    a.m = vmax;
 }
-__device__ __forceinline__ void acc_pair(Acc& a, float z0, float z1, f32x2 nm2, f32x2 c2) {
-    float x0, x1, y0, y1;
-    unpair(add2(pair_of(z0, z1), nm2), x0, x1);
-    const f32x2 x = pair_of(fmaxf(x0, kFar), fmaxf(x1, kFar));
-    unpair(mul2(x, c2), y0, y1);
+__device__ __forceinline__ void acc_add(Acc& a, f32x2 y) {
+    float y0, y1;
+    unpair(y, y0, y1);
     const f32x2 e = pair_of(ex2(y0), ex2(y1));
     a.S = add2(a.S, e);
-    a.Q = fma2(e, x, a.Q);
+    a.Q = fma2(e, y, a.Q);
 }
-template <bool kBf16> __device__ __forceinline__ void acc_vec(Acc& a, const uint4& q, float c) {
-    const float vmax = vec_max<kBf16>(q);
-    if (!(vmax <= a.m)) acc_grow(a, vmax, c);                      // rare after the first few vectors of a row
-    const f32x2 nm2 = pair_of(-a.m, -a.m), c2 = pair_of(c, c);
-    float f[Elems<kBf16>::kPerVec];
-    Elems<kBf16>::unpack(q, f);
+__device__ __forceinline__ void acc_add_far(Acc& a, f32x2 y) {     // y may be -inf
+    float y0, y1;
+    unpair(y, y0, y1);
+    acc_add(a, pair_of(fmaxf(y0, kFar), fmaxf(y1, kFar)));
+}
+__device__ __forceinline__ void acc_pair_slow(Acc& a, float z0, float z1, float c) {
+    acc_add_far(a, mul2(add2(pair_of(z0, z1), pair_of(-a.m, -a.m)), pair_of(c, c)));
+}
+// kN vectors in the frame of a maximum that none of them exceeds.
+template <bool kBf16, int kN> __device__ __forceinline__ void acc_sum(Acc& a, const uint4 (&q)[kN], float c) {
+    if (a.quick) {                                                 // one test per kN vectors: what follows is a straight line
+        const f32x2 c2 = pair_of(c, c), nr2 = pair_of(a.nr, a.nr);
 #pragma unroll
-    for (int i = 0; i < Elems<kBf16>::kPerVec; i += 2) acc_pair(a, f[i], f[i + 1], nm2, c2);
+        for (int u = 0; u < kN; ++u) {
+            const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+            if constexpr (kBf16) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const __nv_bfloat162 z = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]), *reinterpret_cast<const __nv_bfloat162*>(&a.low2));
+                    const uint32_t b = *reinterpret_cast<const uint32_t*>(&z);
+                    acc_add(a, fma2(pair_of(__uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u)), c2, nr2));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) acc_add_far(a, fma2(pair_of(__uint_as_float(w[i]), __uint_as_float(w[i + 1])), c2, nr2));
+            }
+        }
+    } else {
+#pragma unroll 1
+        for (int u = 0; u < kN; ++u) {
+            uint4 v = q[0];                                        // selects: q stays in registers
+#pragma unroll
+            for (int j = 1; j < kN; ++j) v = u == j ? q[j] : v;
+            float f[Elems<kBf16>::kPerVec];
+            Elems<kBf16>::unpack(v, f);
+#pragma unroll
+            for (int i = 0; i < Elems<kBf16>::kPerVec; i += 2) acc_pair_slow(a, f[i], f[i + 1], c);
+        }
+    }
+}
+// kN vectors; a larger maximum (or a NaN) is rare after the first few of a row.
+template <bool kBf16, int kN> __device__ __forceinline__ void acc_vecs(Acc& a, const uint4 (&q)[kN], float c) {
+    if constexpr (kBf16) {
+        __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162*>(&q[0].x);
+#pragma unroll
+        for (int u = 0; u < kN; ++u) {
+            const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+#pragma unroll
+            for (int i = u == 0 ? 1 : 0; i < 4; ++i) x = __hmax2_nan(x, *reinterpret_cast<const __nv_bfloat162*>(&w[i]));
+        }
+        if (!__hble2(x, *reinterpret_cast<const __nv_bfloat162*>(&a.m2))) acc_grow(a, max_nan(__low2float(x), __high2float(x)), c);
+    } else {
+        float vmax = vec_max<false>(q[0]);
+#pragma unroll
+        for (int u = 1; u < kN; ++u) vmax = max_nan(vmax, vec_max<false>(q[u]));
+        if (!(vmax <= a.m)) acc_grow(a, vmax, c);
+    }
+    acc_sum<kBf16, kN>(a, q, c);
 }
 
 // Order of f32 values as unsigned numbers (-0 counts as +0; no NaN gets here).
@@ -352,7 +427,7 @@ __device__ __forceinline__ RowOut row_out(const Args& a, const Part& r) {
     if (r.bad) return {nan, nan};
     if (is_empty(r)) return {0.0f, 0.0f};
     const float l = logf(r.S);
-    return {l, fmaxf(l - r.Q / r.S * a.inv_tau, 0.0f)};
+    return {l, fmaxf(l - r.Q / r.S * 0.6931471805599453f, 0.0f)};
 }
 __device__ __forceinline__ void write_scalars(const Args& a, long long t, const Part& r, const RowOut& o, float zy, int y_state) {
     const bool empty = is_empty(r);                                // a bad row's l is NaN, and so is what is formed with it
@@ -422,20 +497,15 @@ token_logprobs_warp_kernel(const Args a, int run) {
         Part p;
         p.bad = __any_sync(0xffffffffu, !(mx < INFINITY));
         p.m = fmaxf(warp_max_f32(mx), kLowest);
-        const f32x2 nm2 = pair_of(-p.m, -p.m), c2 = pair_of(a.c, a.c);
         Acc acc;
-        acc.S = acc.Q = pair_of(0.0f, 0.0f);
-#pragma unroll
-        for (int u = 0; u < kVecs; ++u) {
-            float f[kPer];
-            Elems<kBf16>::unpack(q[u], f);
-#pragma unroll
-            for (int j = 0; j < kPer; j += 2) acc_pair(acc, f[j], f[j + 1], nm2, c2);
+        acc_init(acc, p.m, a.c);
+        acc_sum<kBf16, kVecs>(acc, q, a.c);
+        Part own = acc_part(acc);
+        if (zt > -INFINITY) {
+            const float y = fmaxf((zt - p.m) * a.c, kFar), e = ex2(y);
+            own.S += e; own.Q = fmaf(e, y, own.Q);
         }
-        acc_pair(acc, zt, -INFINITY, nm2, c2);
-        float s0, s1, q0, q1;
-        unpair(acc.S, s0, s1); unpair(acc.Q, q0, q1);
-        p.S = warp_sum(s0 + s1); p.Q = warp_sum(q0 + q1);
+        p.S = warp_sum(own.S); p.Q = warp_sum(own.Q);
 
         int n = 0;
         if (a.k > 0 && !p.bad) {
@@ -525,20 +595,23 @@ token_logprobs_kernel(const Args a) {
     }
 
     Acc acc;
-    acc_init(acc);
+    acc_init(acc, kLowest, a.c);
     int i = sp.v0 + tid;
     for (; i + (kUnroll - 1) * kThreads < sp.v1; i += kUnroll * kThreads) {
         uint4 q[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) q[u] = load_vec(row + (size_t)(i + u * kThreads) * 16);
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) acc_vec<kBf16>(acc, q[u], a.c);
+        acc_vecs<kBf16, kUnroll>(acc, q, a.c);
     }
-    for (; i < sp.v1; i += kThreads) acc_vec<kBf16>(acc, load_vec(row + (size_t)i * 16), a.c);
+    for (; i < sp.v1; i += kThreads) {
+        const uint4 q[1] = {load_vec(row + (size_t)i * 16)};
+        acc_vecs<kBf16, 1>(acc, q, a.c);
+    }
     if (sp.tail0 + tid < sp.tail1) {
         const float z = Elems<kBf16>::load1(row, sp.tail0 + tid);
         if (!(z <= acc.m)) acc_grow(acc, z, a.c);
-        acc_pair(acc, z, -INFINITY, pair_of(-acc.m, -acc.m), pair_of(a.c, a.c));
+        acc_add_far(acc, acc.quick ? fma2(pair_of(z, -INFINITY), pair_of(a.c, a.c), pair_of(acc.nr, acc.nr))
+                                   : mul2(add2(pair_of(z, -INFINITY), pair_of(-acc.m, -acc.m)), pair_of(a.c, a.c)));
     }
 
     Part p = acc_part(acc);
@@ -608,16 +681,23 @@ struct BwdArgs {
     float c, inv_tau;
 };
 
+// dz = -p (A + X x), x = z - m, p = 2^(x c - l log2(e)), A = (a + b (H - l)) / tau, X = b / tau^2.
 struct BwdRow {
-    float nm, l2n, a, b, bH;             // -m, -l log2(e), a / tau, b / tau, (a + b (H - l)) / tau
-    float bx;                            // b / tau^2: what (z - m) adds to the bracket
-    int y;
+    float nm, l2n, nA, nX;               // -m, -l log2(e), -A, -X
+    float far;                           // x is held at or above this: p is 0 there
+    uint32_t low2;                       // bf16 pair: m + far, or -inf where that is beyond the type
 };
 
-__device__ __forceinline__ float bwd_elem(float z, const BwdRow& r, float c) {
-    const float x = fmaxf(z + r.nm, kFar);
-    const float p = ex2(fmaf(x, c, r.l2n));
-    return -p * fmaf(x, r.bx, r.bH);
+__device__ __forceinline__ f32x2 bwd_pair(float z0, float z1, const BwdRow& r, float c, bool lift) {
+    f32x2 x = add2(pair_of(z0, z1), pair_of(r.nm, r.nm));
+    if (lift) {
+        float x0, x1;
+        unpair(x, x0, x1);
+        x = pair_of(fmaxf(x0, r.far), fmaxf(x1, r.far));
+    }
+    float y0, y1;
+    unpair(fma2(x, pair_of(c, c), pair_of(r.l2n, r.l2n)), y0, y1);
+    return mul2(pair_of(ex2(y0), ex2(y1)), fma2(x, pair_of(r.nX, r.nX), pair_of(r.nA, r.nA)));
 }
 
 template <bool kBf16, int kThreads, int kTeams>
@@ -641,41 +721,65 @@ token_logprobs_bwd_kernel(const BwdArgs a) {
     if (bad_y && tid == 0 && chunk == 0) set_status(a.status, DPPO_STATUS_BAD_TARGET);
     BwdRow r;
     r.nm = -st.x; r.l2n = -st.y * 1.4426950408889634f;
-    r.a = da * a.inv_tau; r.b = db * a.inv_tau;
-    r.bH = fmaf(r.b, st.z - st.y, r.a);
-    r.bx = r.b * a.inv_tau;
-    r.y = y;
+    const float ga = da * a.inv_tau, gb = db * a.inv_tau;
+    r.nA = -fmaf(gb, st.z - st.y, ga);
+    r.nX = -gb * a.inv_tau;
+    r.far = fmaxf(kFar / a.c, -1e30f);
+    r.low2 = bf16_pair(__float2bfloat16_rd(st.x + r.far));
+    // bf16 entries are lifted by a packed maximum before they are unpacked, unless the bound is beyond the type
+    const bool lift = !kBf16 || !(fabsf(st.x) <= 1e37f);
 
     const char* row = a.logits + t * a.row_bytes;
     char* out = a.dlogits + t * a.row_bytes;
-    const int nvec = a.V >> kLog2Per;
+    const int nvec = a.V >> kLog2Per, tail0 = nvec << kLog2Per;
     const int v0 = chunk * a.chunk_vecs, v1 = min(nvec, v0 + a.chunk_vecs);
-    const int vy = a.dlogp && !zero ? y >> kLog2Per : -1;
-    auto put = [&](const uint4& q, int i) {
+    // the given token's element is formed apart and stored by the thread that stores its vector, after that
+    const int vy = y >> kLog2Per;
+    const bool mine = a.dlogp && !zero && (y < tail0 ? vy >= v0 && vy < v1 && (vy - v0) % kThreads == tid
+                                                     : chunk == a.chunks - 1 && y - tail0 == tid);
+    const float zy = mine ? Elems<kBf16>::load1(row, y) : 0.0f;
+
+    auto put = [&](uint4 q, int i, auto lift_f32) {
+        if constexpr (kBf16 && !decltype(lift_f32)::value) {
+            uint32_t* w[4] = {&q.x, &q.y, &q.z, &q.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const __nv_bfloat162 h = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(w[j]), *reinterpret_cast<const __nv_bfloat162*>(&r.low2));
+                *w[j] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+        }
         float z[kPer];
         Elems<kBf16>::unpack(q, z);
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) z[j] = zero ? 0.0f : bwd_elem(z[j], r, a.c);
-        if (i == vy) {
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) z[j] += j == (y & (kPer - 1)) ? r.a : 0.0f;
-        }
+        for (int j = 0; j < kPer; j += 2) unpair(bwd_pair(z[j], z[j + 1], r, a.c, decltype(lift_f32)::value), z[j], z[j + 1]);
         __stcs(reinterpret_cast<uint4*>(out) + i, Elems<kBf16>::pack(z));
     };
-    int i = v0 + tid;
-    for (; i + (kUnroll - 1) * kThreads < v1; i += kUnroll * kThreads) {       // all loads of a round before its stores
-        uint4 q[kUnroll];
+    auto sweep = [&](auto lift_f32) {
+        int i = v0 + tid;
+        for (; i + (kUnroll - 1) * kThreads < v1; i += kUnroll * kThreads) {   // all loads of a round before its stores
+            uint4 q[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) q[u] = load_vec_rw(row + (size_t)(i + u * kThreads) * 16);
+            for (int u = 0; u < kUnroll; ++u) q[u] = load_vec_rw(row + (size_t)(i + u * kThreads) * 16);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) put(q[u], i + u * kThreads);
+            for (int u = 0; u < kUnroll; ++u) put(q[u], i + u * kThreads, lift_f32);
+        }
+        for (; i < v1; i += kThreads) put(load_vec_rw(row + (size_t)i * 16), i, lift_f32);
+    };
+    if (zero) {
+        for (int i = v0 + tid; i < v1; i += kThreads) __stcs(reinterpret_cast<uint4*>(out) + i, make_uint4(0u, 0u, 0u, 0u));
+    } else if (lift) {
+        sweep(std::true_type());
+    } else {
+        sweep(std::false_type());
     }
-    for (; i < v1; i += kThreads) put(load_vec_rw(row + (size_t)i * 16), i);
-    const int tail = (nvec << kLog2Per) + tid;
-    if (chunk == a.chunks - 1 && tail < a.V) {
-        float g = zero ? 0.0f : bwd_elem(Elems<kBf16>::load1(row, tail), r, a.c);
-        if (a.dlogp && !zero && tail == y) g += r.a;
-        Elems<kBf16>::store1(out, tail, g);
+    float g, unused;
+    if (chunk == a.chunks - 1 && tail0 + tid < a.V) {
+        unpair(bwd_pair(Elems<kBf16>::load1(row, tail0 + tid), 0.0f, r, a.c, true), g, unused);
+        Elems<kBf16>::store1(out, tail0 + tid, zero ? 0.0f : g);
+    }
+    if (mine) {
+        unpair(bwd_pair(zy, 0.0f, r, a.c, true), g, unused);
+        Elems<kBf16>::store1(out, y, g + ga);
     }
 }
 
