@@ -141,6 +141,15 @@ def test_every_launch_shape(B, variant, dtype):
         run(B, z, V, y, 20, 0.9, variant)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V, variant", [(151936, 10128), (151936, 10256), (300001, 10128), (131077, 20128), (600003, 10256)])
+def test_more_rounds_than_slots(B, V, variant, dtype):
+    """Rows of more rounds than there are slots for their maxima: several rounds share one."""
+    z, y = make(2, V, dtype, V)
+    z[1, :V] = z[1, :V].round()                                      # and with many ties
+    run(B, z, V, y, 20, 1.0, variant)
+
+
 def special_rows(V, dtype):
     """Rows where a softmax or a selection goes wrong, as f32 [n, V]."""
     g = torch.Generator().manual_seed(V)
@@ -176,7 +185,7 @@ def special_rows(V, dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V, k, variant", [(9, 4, 0), (1000, 20, 0), (1500, 20, 0), (2001, 32, 0), (3500, 8, 0), (4099, 32, 0), (8200, 5, 0), (20000, 20, 10128), (20003, 20, 0),
-                                           (20003, 32, 10512), (20003, 7, 40256), (20003, 20, 80128), (1027, 32, 32)])
+                                           (20003, 32, 10512), (20003, 7, 40256), (20003, 20, 80128), (1027, 32, 32), (150003, 20, 10128)])
 def test_special_rows(B, V, k, variant, dtype):
     rows = special_rows(V, dtype)
     z = torch.zeros(rows.shape[0], pad16(V, 2 if dtype == "bf16" else 4), dtype=DT[dtype], device="cuda")
