@@ -358,7 +358,7 @@ typedef struct {
     int32_t top_k;          /* alternatives per row, 0..32 (the backward ignores it)                 */
     int32_t variant;        /* 0: the library picks the launch shape.  Tuning aid of the forward:
                                C*10000 + threads: C = 1, 2, 4 or 8 CTAs per row with 128, 256 or 512
-                               threads each; 32: one warp per row (rows of up to 4 KB)               */
+                               threads each; 32: one warp per row                                    */
     double temperature;     /* > 0                                                                   */
 } dppo_logprob_params;
 

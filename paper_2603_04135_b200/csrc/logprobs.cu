@@ -33,7 +33,7 @@ namespace logprob {
 
 constexpr int kMaxTop = 32;
 constexpr int kCand = 512;                // candidate buffer of a CTA-sized team
-constexpr int kCandWarp = 128;            // and of a warp-sized one
+constexpr int kCandWarp = 256;            // and of a warp-sized one
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kFar = -2000.0f;          // exponents are held at or above this (2^-2000 is 0): 0 * (-inf) never arises
 
@@ -120,6 +120,11 @@ struct Acc {
     uint32_t m2, low2;                    // bf16 pairs: the maximum, and what lower entries are lifted to
     int quick, bad;
 };
+// The least bf16 value that is not below x (a NaN or a value beyond the type: no matter, its row is NaN or x is not exceeded).
+__device__ __forceinline__ __nv_bfloat16 bf16_up(float x) {
+    const uint32_t b = __float_as_uint(x);
+    return __ushort_as_bfloat16((unsigned short)((b + ((int32_t)b < 0 ? 0u : 0xffffu)) >> 16));
+}
 __device__ __forceinline__ uint32_t bf16_pair(__nv_bfloat16 x) {
     const __nv_bfloat162 p = __halves2bfloat162(x, x);
     return *reinterpret_cast<const uint32_t*>(&p);
@@ -216,11 +221,18 @@ template <bool kBf16, int kN> __device__ __forceinline__ __nv_bfloat16 acc_vecs(
         float vmax = vec_max<false>(q[0]);
 #pragma unroll
         for (int u = 1; u < kN; ++u) vmax = max_nan(vmax, vec_max<false>(q[u]));
-        top = __float2bfloat16_ru(vmax);
+        top = bf16_up(vmax);
         if (!(vmax <= a.m)) acc_grow(a, vmax, c);
     }
     acc_sum<kBf16, kN>(a, q, c);
     return top;
+}
+
+// One entry (-inf: nothing).
+__device__ __forceinline__ void acc_one(Acc& a, float z, float c) {
+    if (!(z <= a.m)) acc_grow(a, z, c);
+    const f32x2 z2 = pair_of(z, -INFINITY), c2 = pair_of(c, c);
+    acc_add_far(a, a.quick ? fma2(z2, c2, pair_of(a.nr, a.nr)) : mul2(add2(z2, pair_of(-a.m, -a.m)), c2));
 }
 
 // Order of f32 values as unsigned numbers (-0 counts as +0; no NaN gets here).
@@ -474,17 +486,26 @@ __device__ __forceinline__ void write_top(const Args& a, long long t, int j, flo
     a.top_logp[t * a.k + j] = have ? fmaf(entry_value(e) - m, a.inv_tau, -l) : bad ? l : -INFINITY;
 }
 
-// Short rows: a warp per row at a time, the whole row in registers (kVecs vectors per lane), so the maximum is known before
-// the exponentials and the candidates are picked out of the registers.  What such a row costs is instructions (871 per row
-// of 1,021 f32 in a form that treated candidates and outputs entry by entry: 26 us for 20,011 rows), so:
-// the vectors that hold a candidate (a few of the row's) go through shared memory, one lane per entry; a warp takes up to 8
-// consecutive rows, and the scalar outputs of all of them are formed in one pass, a lane per row.
+// Short rows: a warp per row at a time.  Rows of up to 32 kVecs vectors are held in registers (kVecs vectors per lane), so the
+// maximum is known before the exponentials and the candidates are picked out of the registers; longer ones (kVecs = 0) are
+// swept in rounds, as a CTA does it, without a CTA's five barriers per row.
+// What such a row costs is instructions (871 per row of 1,021 f32 in a form that treated candidates and outputs entry by
+// entry: 26 us for 20,011 rows), so: the vectors that hold a candidate (a few of the row's) go through shared memory, one lane
+// per entry; a warp takes several consecutive rows, and the scalar outputs of all of them are formed in one pass, a lane
+// per row.
 constexpr int kMaxRun = 8;
 constexpr int kHotVecs = 64;
-struct WarpShared {
+template <bool kSweep> struct WarpShared;
+template <> struct WarpShared<false> {
     TeamShared<32, kCandWarp> team;
     uint4 hot[kHotVecs];
     int hot_vec[kHotVecs];
+    Entry list[kMaxRun][kMaxTop];
+};
+template <> struct WarpShared<true> {
+    TeamShared<32, kCandWarp> team;
+    __nv_bfloat16 best[kSlots][32];
+    int group[kMaxGroups];                 // slot * 32 + lane
     Entry list[kMaxRun][kMaxTop];
 };
 
@@ -493,14 +514,17 @@ __global__ void __launch_bounds__(32 * kTeams)
 token_logprobs_warp_kernel(const Args a, int run) {
     constexpr int kPer = Elems<kBf16>::kPerVec, kLog2Per = kBf16 ? 3 : 2;
     constexpr uint32_t kNone = kBf16 ? 0xff80ff80u : 0xff800000u;  // -inf
-    __shared__ WarpShared shared[kTeams];
+    __shared__ WarpShared<kVecs == 0> shared[kTeams];
     const int lane = threadIdx.x & 31;
-    WarpShared& ws = shared[threadIdx.x >> 5];
+    auto& ws = shared[threadIdx.x >> 5];
     const long long T = a.n_tokens_dev ? min((long long)*a.n_tokens_dev, a.T_max) : a.T_max;
     const long long t0 = ((long long)blockIdx.x * kTeams + (threadIdx.x >> 5)) * run;
     if (t0 >= T) return;
     const int n_rows = (int)min((long long)run, T - t0);
     const int nvec = a.V >> kLog2Per, tail = (nvec << kLog2Per) + lane;
+    const int n_rounds = (nvec + kRound * 32 - 1) / (kRound * 32);
+    int shift = 0;
+    while (n_rounds > kSlots << shift) ++shift;
 
     // lane r: the given token of row t0 + r, and (below) the row's sums
     float zy = 0.0f;
@@ -514,69 +538,122 @@ token_logprobs_warp_kernel(const Args a, int run) {
 #pragma unroll 1
     for (int r = 0; r < n_rows; ++r) {
         const char* row = a.logits + (t0 + r) * a.row_bytes;
-        uint4 q[kVecs];
-#pragma unroll
-        for (int u = 0; u < kVecs; ++u) {
-            q[u] = make_uint4(kNone, kNone, kNone, kNone);
-            if (u * 32 + lane < nvec) q[u] = load_vec(row + (size_t)(u * 32 + lane) * 16);
-        }
         const float zt = tail < a.V ? Elems<kBf16>::load1(row, tail) : -INFINITY;
-        float vm[kVecs], mx = zt;                                  // the vectors' maxima, the lane's (NaN if it has one)
-#pragma unroll
-        for (int u = 0; u < kVecs; ++u) { vm[u] = vec_max<kBf16>(q[u]); mx = max_nan(mx, vm[u]); }
+        uint4 q[kVecs > 0 ? kVecs : kRound];
+        float vm[kVecs > 0 ? kVecs : 1];                           // the vectors' maxima
+        float mx;                                                  // the lane's
         Part p;
-        p.bad = __any_sync(0xffffffffu, !(mx < INFINITY));
-        p.m = fmaxf(warp_max_f32(mx), kLowest);
-        Acc acc;
-        acc_init(acc, p.m, a.c);
-        acc_sum<kBf16, kVecs>(acc, q, a.c);
-        Part own = acc_part(acc);
-        if (zt > -INFINITY) {
-            const float y = fmaxf((zt - p.m) * a.c, kFar), e = ex2(y);
-            own.S += e; own.Q = fmaf(e, y, own.Q);
+        if constexpr (kVecs > 0) {
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u) {
+                q[u] = make_uint4(kNone, kNone, kNone, kNone);
+                if (u * 32 + lane < nvec) q[u] = load_vec(row + (size_t)(u * 32 + lane) * 16);
+            }
+            mx = zt;
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u) { vm[u] = vec_max<kBf16>(q[u]); mx = max_nan(mx, vm[u]); }
+            p.bad = __any_sync(0xffffffffu, !(mx < INFINITY));
+            p.m = fmaxf(warp_max_f32(mx), kLowest);
+            Acc acc;
+            acc_init(acc, p.m, a.c);
+            acc_sum<kBf16, kVecs>(acc, q, a.c);
+            Part own = acc_part(acc);
+            if (zt > -INFINITY) {
+                const float y = fmaxf((zt - p.m) * a.c, kFar), e = ex2(y);
+                own.S += e; own.Q = fmaf(e, y, own.Q);
+            }
+            p.S = warp_sum(own.S); p.Q = warp_sum(own.Q);
+        } else {
+            Acc acc;
+            acc_init(acc, kLowest, a.c);
+#pragma unroll 1
+            for (int it = 0; it < n_rounds; ++it) {
+                const int i = it * (kRound * 32) + lane;
+                if ((it + 1) * (kRound * 32) <= nvec) {
+#pragma unroll
+                    for (int u = 0; u < kRound; ++u) q[u] = load_vec(row + (size_t)(i + u * 32) * 16);
+                } else {                                           // the row's last vectors
+#pragma unroll
+                    for (int u = 0; u < kRound; ++u)
+                        q[u] = i + u * 32 < nvec ? load_vec(row + (size_t)(i + u * 32) * 16) : make_uint4(kNone, kNone, kNone, kNone);
+                }
+                __nv_bfloat16 top = acc_vecs<kBf16, kRound>(acc, q, a.c);
+                if (a.k > 0) {
+                    __nv_bfloat16* best = &ws.best[it >> shift][lane];
+                    if (it & ((1 << shift) - 1)) top = __hmax(top, *best);
+                    *best = top;
+                }
+            }
+            acc_one(acc, zt, a.c);
+            p = acc_part(acc);
+            mx = p.S > 0.0f ? p.m : -INFINITY;
+            p = warp_join(p, a.c);
         }
-        p.S = warp_sum(own.S); p.Q = warp_sum(own.Q);
 
         int n = 0;
         if (a.k > 0 && !p.bad) {
             const float thr = kth_of_lanes(mx, a.k);
             const uint32_t below = (1u << lane) - 1u;
-            int n_hot = 0;
-#pragma unroll
-            for (int u = 0; u < kVecs; ++u) {
-                const uint32_t b = __ballot_sync(0xffffffffu, vm[u] >= thr);
-                if (b == 0) continue;
-                const int at = n_hot + __popc(b & below);
-                if (vm[u] >= thr && at < kHotVecs) { ws.hot[at] = q[u]; ws.hot_vec[at] = u * 32 + lane; }
-                n_hot += __popc(b);
-            }
-            __syncwarp();
-            n = n_hot > kHotVecs ? kCandWarp + 1 : 0;
-            for (int i = 0; i < n_hot * kPer && n <= kCandWarp; i += 32) {         // a lane per entry
-                const int e = i + lane, h = e >> kLog2Per, j = e & (kPer - 1);
-                const float z = e < n_hot * kPer ? Elems<kBf16>::load1(&ws.hot[h], j) : -INFINITY;
+            auto offer = [&](float z, int idx) {                   // by all lanes together
                 const uint32_t b = __ballot_sync(0xffffffffu, z >= thr);
                 const int at = n + __popc(b & below);
-                if (z >= thr && at < kCandWarp) ws.team.cand[at] = entry_of(z, ws.hot_vec[h] * kPer + j);
+                if (z >= thr && at < kCandWarp) ws.team.cand[at] = entry_of(z, idx);
                 n += __popc(b);
+            };
+            if constexpr (kVecs > 0) {
+                int n_hot = 0;
+#pragma unroll
+                for (int u = 0; u < kVecs; ++u) {
+                    const uint32_t b = __ballot_sync(0xffffffffu, vm[u] >= thr);
+                    if (b == 0) continue;
+                    const int at = n_hot + __popc(b & below);
+                    if (vm[u] >= thr && at < kHotVecs) { ws.hot[at] = q[u]; ws.hot_vec[at] = u * 32 + lane; }
+                    n_hot += __popc(b);
+                }
+                __syncwarp();
+                n = n_hot > kHotVecs ? kCandWarp + 1 : 0;
+                for (int i = 0; i < n_hot * kPer && n <= kCandWarp; i += 32) {     // a lane per entry
+                    const int e = i + lane, h = e >> kLog2Per, j = e & (kPer - 1);
+                    const bool in = e < n_hot * kPer;
+                    offer(in ? Elems<kBf16>::load1(&ws.hot[h], j) : -INFINITY, in ? ws.hot_vec[h] * kPer + j : 0);
+                }
+            } else {
+                const int n_slots = (n_rounds + (1 << shift) - 1) >> shift, log2_vecs = 2 + shift;
+                int n_group = 0;
+                for (int s = 0; s < n_slots; ++s) {
+                    const bool hit = __bfloat162float(ws.best[s][lane]) >= thr;
+                    const uint32_t b = __ballot_sync(0xffffffffu, hit);
+                    const int at = n_group + __popc(b & below);
+                    if (hit && at < kMaxGroups) ws.group[at] = s * 32 + lane;
+                    n_group += __popc(b);
+                }
+                __syncwarp();
+                n = n_group > kMaxGroups ? kCandWarp + 1 : 0;
+                for (int i0 = 0; i0 < n_group << log2_vecs && n <= kCandWarp; i0 += 32) {      // a lane per vector
+                    const int i = i0 + lane;
+                    uint4 v = make_uint4(kNone, kNone, kNone, kNone);
+                    int at = 0;
+                    if (i < n_group << log2_vecs) {
+                        const int g = ws.group[i >> log2_vecs];
+                        at = (((g >> 5) << log2_vecs) + (i & ((1 << log2_vecs) - 1))) * 32 + (g & 31);
+                        if (at < nvec) v = load_vec(row + (size_t)at * 16);
+                    }
+                    float z[kPer];
+                    Elems<kBf16>::unpack(v, z);
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j)
+                        if (__any_sync(0xffffffffu, z[j] >= thr)) offer(z[j], at * kPer + j);
+                }
             }
-            const uint32_t b = __ballot_sync(0xffffffffu, zt >= thr);
-            if (b) {
-                const int at = n + __popc(b & below);
-                if (zt >= thr && at < kCandWarp) ws.team.cand[at] = entry_of(zt, tail);
-                n += __popc(b);
-            }
+            if (__any_sync(0xffffffffu, zt >= thr)) offer(zt, tail);
             __syncwarp();
-            if (n <= kCandWarp) {
-                rank_entries(ws.team.cand, n, a.k, ws.list[r], lane, 32);
-                n = min(n, a.k);
-            } else {                                               // ties
+            if (n > kCandWarp) {                                   // ties
                 const Span sp = {row, 0, nvec, nvec << kLog2Per, a.V};
                 collect_ties<kBf16, 32, kCandWarp>(ws.team, sp, a.k, thr, lane);
                 n = ws.team.n_cand;
-                rank_entries(ws.team.cand, n, a.k, ws.list[r], lane, 32);
-                n = min(n, a.k);
             }
+            rank_entries(ws.team.cand, n, a.k, ws.list[r], lane, 32);
+            n = min(n, a.k);
             __syncwarp();
         }
         if (lane == r) { mine = p; my_list = n; }
@@ -646,12 +723,7 @@ token_logprobs_kernel(const Args a) {
             *best = top;
         }
     }
-    if (sp.tail0 + tid < sp.tail1) {
-        const float z = Elems<kBf16>::load1(row, sp.tail0 + tid);
-        if (!(z <= acc.m)) acc_grow(acc, z, a.c);
-        acc_add_far(acc, acc.quick ? fma2(pair_of(z, -INFINITY), pair_of(a.c, a.c), pair_of(acc.nr, acc.nr))
-                                   : mul2(add2(pair_of(z, -INFINITY), pair_of(-acc.m, -acc.m)), pair_of(a.c, a.c)));
-    }
+    if (sp.tail0 + tid < sp.tail1) acc_one(acc, Elems<kBf16>::load1(row, sp.tail0 + tid), a.c);
 
     Part p = acc_part(acc);
     if (a.k > 0) sh.tmax[tid] = p.S > 0.0f ? p.m : -INFINITY;      // nothing but -inf seen: not a maximum
@@ -865,10 +937,16 @@ template <bool kBf16> static int run_fwd(const Args& a, int variant, cudaStream_
     const int nvec = a.V >> (kBf16 ? 3 : 2);
     int C = 1, threads = 256;
     if (variant == 0) {
-        if (nvec <= 256) { threads = 32; }
+        // Rows of up to 4 KB: a warp each (20,011 x 1,021 f32: 22 us, a CTA each 68), up to 24 KB where there are enough of them
+        // to fill the SMs with warps (8,192 x 8,192 bf16: 33 us against 42; 1,000 of them: 9.7 against 8.3).  Longer rows, or
+        // fewer: a CTA each, small CTAs where there are many of them (8,192 x 151,936 bf16: 128 threads 416 us, 256 449;
+        // 2,003 x 151,936 f32: 212 against 199); few rows: split over a cluster, up to about three CTAs per SM
+        // (1 row of 151,936: 1 CTA 16.9 us, 8 CTAs 10.0; 300 rows: 1 CTA 31.6, 2 CTAs 38.7).
+        const long long sms = sm_count();
+        if (nvec <= 256 || (nvec <= 1536 && a.T_max >= 13 * sms)) { threads = 32; }
         else {
-            while (C < 8 && a.T_max * C * 2 <= 3ll * sm_count() && nvec / (2 * C) >= 256) C *= 2;
-            threads = C == 1 && nvec <= 2048 ? 128 : 256;
+            while (C < 8 && a.T_max * C * 2 <= 3 * sms && nvec / (2 * C) >= 256) C *= 2;
+            threads = C == 1 && (nvec <= 2048 || a.T_max >= 24 * sms) ? 128 : 256;
         }
     } else if (variant == 32) {
         threads = 32;
@@ -878,6 +956,7 @@ template <bool kBf16> static int run_fwd(const Args& a, int variant, cudaStream_
     if (threads == 32 && C == 1) {
         if (nvec <= 128) return launch_warp<kBf16, 4>(a, s);
         if (nvec <= 256) return launch_warp<kBf16, 8>(a, s);
+        return launch_warp<kBf16, 0>(a, s);
     }
     if (C == 1 && threads == 128) return launch_fwd<kBf16, 128, false>(a, 1, s);
     if (C == 1 && threads == 256) return launch_fwd<kBf16, 256, false>(a, 1, s);
