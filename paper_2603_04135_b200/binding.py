@@ -139,28 +139,44 @@ def _ptr(x):
 
 
 _TORCH_DTYPE = {F32: torch.float32, BF16: torch.bfloat16}
+_Tensor, _f32, _i32, _i8 = torch.Tensor, torch.float32, torch.int32, torch.int8
 
 
-def _arr(x, name, device, dtype, rows, row_elems, stride=None):
-    """Device pointer of a [rows x row_elems] array.  A torch tensor is checked first: on `device` (the current
-    one), of `dtype`, laid out as the call will read it.  stride: elements between rows (None: dense)."""
-    if not isinstance(x, torch.Tensor):
+def _arr(x, name, device, dtype, n):
+    """Device pointer of n dense elements.  A torch tensor is checked: of `dtype`, on `device` (the current one), large
+    enough.  The plain case is one expression: these checks are on the path of calls that take 10 us."""
+    if x.__class__ is _Tensor and x.dtype is dtype and x.get_device() == device and x.numel() >= n and x.is_contiguous():
+        return x.data_ptr()
+    if not isinstance(x, _Tensor):
         return x
+    _check_kind(x, name, device, dtype)
+    if n > 0 and (x.numel() < n or not x.is_contiguous()):
+        raise DppoError(ERR_BAD_SHAPE, "%s: needs %d contiguous elements, got shape %s, strides %s" % (name, n, tuple(x.shape), x.stride()))
+    return x.data_ptr()
+
+
+def _mat(x, name, device, dtype, rows, cols, stride):
+    """The same for [rows x cols] with `stride` elements between rows."""
+    if (x.__class__ is _Tensor and x.dtype is dtype and x.get_device() == device and x.stride() == (stride, 1)
+            and x.shape[0] >= rows and x.shape[1] >= cols):
+        return x.data_ptr()
+    if not isinstance(x, _Tensor):
+        return x
+    _check_kind(x, name, device, dtype)
+    if rows > 0:
+        have = x.untyped_storage().nbytes() // x.element_size() - x.storage_offset()
+        if have < (rows - 1) * stride + cols or (x.dim() == 2 and (x.stride(1) != 1 and x.shape[1] > 1
+                                                                   or x.stride(0) != stride and x.shape[0] > 1)):
+            raise DppoError(ERR_BAD_SHAPE, "%s: shape %s, strides %s do not hold %d rows of %d elements, %d apart"
+                            % (name, tuple(x.shape), x.stride(), rows, cols, stride))
+    return x.data_ptr()
+
+
+def _check_kind(x, name, device, dtype):
     if x.dtype is not dtype:
         raise DppoError(ERR_INVALID_ARG, "%s: dtype %s, expected %s" % (name, x.dtype, dtype))
     if x.get_device() != device:
         raise DppoError(ERR_INVALID_ARG, "%s: on %s, the current device is cuda:%d" % (name, x.device, device))
-    if rows > 0:
-        if stride is None:
-            if x.numel() < rows * row_elems or not x.is_contiguous():
-                raise DppoError(ERR_BAD_SHAPE, "%s: needs %d contiguous elements, got shape %s" % (name, rows * row_elems, tuple(x.shape)))
-        elif x.stride() != (stride, 1) or x.shape[0] < rows or x.shape[1] < row_elems:     # else the plain case: rows of a matrix
-            have = x.untyped_storage().nbytes() // x.element_size() - x.storage_offset()
-            if have < (rows - 1) * stride + row_elems or (x.dim() == 2 and (x.stride(1) != 1 and x.shape[1] > 1
-                                                                            or x.stride(0) != stride and x.shape[0] > 1)):
-                raise DppoError(ERR_BAD_SHAPE, "%s: shape %s, strides %s do not hold %d rows of %d elements, %d apart"
-                                % (name, tuple(x.shape), x.stride(), rows, row_elems, stride))
-    return x.data_ptr()
 
 
 _cuda = None                        # whether there is a CUDA device; asked once
@@ -289,40 +305,42 @@ def sequence_log_ratio(logp, logp_old, cu_seqlens, S_max, out, status=None, stre
 
 def token_logprobs(params, logits, target, n_tokens_dev, logp_out, entropy_out, lse_out, top_ids, top_logp, stats,
                    status=None, stream=None):
-    p, d, i32, f32 = params, _device(), torch.int32, torch.float32
-    T, k = p.T_max, p.top_k
+    p, d = params, _device()
+    T, V = p.T_max, p.V
+    k = p.top_k * T
     _check(lib.dppo_token_logprobs(
-        ctypes.byref(p), _arr(logits, "logits", d, _TORCH_DTYPE.get(p.dtype), T, p.V, p.row_stride),
-        _arr(target, "target", d, i32, T, 1), _arr(n_tokens_dev, "n_tokens_dev", d, i32, 1, 1),
-        _arr(logp_out, "logp_out", d, f32, T, 1), _arr(entropy_out, "entropy_out", d, f32, T, 1),
-        _arr(lse_out, "lse_out", d, f32, T, 1), _arr(top_ids, "top_ids", d, i32, T, k),
-        _arr(top_logp, "top_logp", d, f32, T, k), _arr(stats, "stats", d, f32, T, 4), _arr(status, "status", d, i32, 1, 1),
+        ctypes.byref(p), _mat(logits, "logits", d, _TORCH_DTYPE.get(p.dtype), T, V, p.row_stride),
+        _arr(target, "target", d, _i32, T), _arr(n_tokens_dev, "n_tokens_dev", d, _i32, 1), _arr(logp_out, "logp_out", d, _f32, T),
+        _arr(entropy_out, "entropy_out", d, _f32, T), _arr(lse_out, "lse_out", d, _f32, T), _arr(top_ids, "top_ids", d, _i32, k),
+        _arr(top_logp, "top_logp", d, _f32, k), _arr(stats, "stats", d, _f32, 4 * T), _arr(status, "status", d, _i32, 1),
         _stream(stream)))
 
 
 def token_logprobs_backward(params, logits, target, n_tokens_dev, stats, dlogp, dentropy, dlogits, status=None,
                             stream=None):
-    p, d, i32, f32 = params, _device(), torch.int32, torch.float32
-    T, dt = p.T_max, _TORCH_DTYPE.get(p.dtype)
+    p, d = params, _device()
+    T, V, dt, ld = p.T_max, p.V, _TORCH_DTYPE.get(p.dtype), p.row_stride
     _check(lib.dppo_token_logprobs_backward(
-        ctypes.byref(p), _arr(logits, "logits", d, dt, T, p.V, p.row_stride), _arr(target, "target", d, i32, T, 1),
-        _arr(n_tokens_dev, "n_tokens_dev", d, i32, 1, 1), _arr(stats, "stats", d, f32, T, 4),
-        _arr(dlogp, "dlogp", d, f32, T, 1), _arr(dentropy, "dentropy", d, f32, T, 1),
-        _arr(dlogits, "dlogits", d, dt, T, p.V, p.row_stride), _arr(status, "status", d, i32, 1, 1), _stream(stream)))
+        ctypes.byref(p), _mat(logits, "logits", d, dt, T, V, ld), _arr(target, "target", d, _i32, T),
+        _arr(n_tokens_dev, "n_tokens_dev", d, _i32, 1), _arr(stats, "stats", d, _f32, 4 * T), _arr(dlogp, "dlogp", d, _f32, T),
+        _arr(dentropy, "dentropy", d, _f32, T), _mat(dlogits, "dlogits", d, dt, T, V, ld), _arr(status, "status", d, _i32, 1),
+        _stream(stream)))
 
 
 def quantize_rows_i8(params, x, q, scale, n_rows_dev=None, status=None, stream=None):
-    p, d, M = params, _device(), params.rows_max
+    p, d = params, _device()
+    M, K = p.rows_max, p.K
     _check(lib.dppo_quantize_rows_i8(
-        ctypes.byref(p), _arr(x, "x", d, _TORCH_DTYPE.get(p.dtype), M, p.K, p.x_stride),
-        _arr(q, "q", d, torch.int8, M, p.K, p.q_stride), _arr(scale, "scale", d, torch.float32, M, 1),
-        _arr(n_rows_dev, "n_rows_dev", d, torch.int32, 1, 1), _arr(status, "status", d, torch.int32, 1, 1), _stream(stream)))
+        ctypes.byref(p), _mat(x, "x", d, _TORCH_DTYPE.get(p.dtype), M, K, p.x_stride), _mat(q, "q", d, _i8, M, K, p.q_stride),
+        _arr(scale, "scale", d, _f32, M), _arr(n_rows_dev, "n_rows_dev", d, _i32, 1), _arr(status, "status", d, _i32, 1),
+        _stream(stream)))
 
 
 def linear_i8(params, x, x_scale, w, w_scale, out, n_rows_dev=None, status=None, stream=None):
-    p, d, f32 = params, _device(), torch.float32
+    p, d = params, _device()
+    M, N, K = p.M_max, p.N, p.K
     _check(lib.dppo_linear_i8(
-        ctypes.byref(p), _arr(x, "x", d, torch.int8, p.M_max, p.K, p.x_stride), _arr(x_scale, "x_scale", d, f32, p.M_max, 1),
-        _arr(w, "w", d, torch.int8, p.N, p.K, p.w_stride), _arr(w_scale, "w_scale", d, f32, p.N, 1),
-        _arr(out, "out", d, _TORCH_DTYPE.get(p.out_dtype), p.M_max, p.N, p.out_stride),
-        _arr(n_rows_dev, "n_rows_dev", d, torch.int32, 1, 1), _arr(status, "status", d, torch.int32, 1, 1), _stream(stream)))
+        ctypes.byref(p), _mat(x, "x", d, _i8, M, K, p.x_stride), _arr(x_scale, "x_scale", d, _f32, M),
+        _mat(w, "w", d, _i8, N, K, p.w_stride), _arr(w_scale, "w_scale", d, _f32, N),
+        _mat(out, "out", d, _TORCH_DTYPE.get(p.out_dtype), M, N, p.out_stride), _arr(n_rows_dev, "n_rows_dev", d, _i32, 1),
+        _arr(status, "status", d, _i32, 1), _stream(stream)))

@@ -95,10 +95,6 @@ __device__ __forceinline__ void store_column(const Args& a, long long t0, long l
     }
 }
 
-// The product may be launched while the kernel before it (the quantisation of its rows) still runs: nothing is read from
-// global memory before that kernel has completed.
-__device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
 // ---- many tokens: CTA pairs ---------------------------------------------------------------------------
 struct Shared2 {
     unsigned long long full[kStages2];
@@ -160,7 +156,7 @@ linear_i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     lm_cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = sh.tmem_base;
-    wait_for_previous_kernel();
+    enter_kernel();
     const long long T = true_rows(a);
     const int n_tok = (int)((T + a.tile_n - 1) / a.tile_n);
 
@@ -319,7 +315,7 @@ linear_i8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    wait_for_previous_kernel();
+    enter_kernel();
     const long long T = true_rows(a);
     if (t_tile >= T) return;                                              // the whole cluster leaves together
     if (warp == 1) {
@@ -507,7 +503,7 @@ __global__ void __launch_bounds__(kQuantThreads)
 quantize_rows_kernel(const QuantArgs a) {
     constexpr int kPer = Elems<kBf16>::kPerVec;
     __shared__ float red[kQuantThreads / 32];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // a product may set itself up meanwhile
+    enter_kernel();
     const long long t = blockIdx.x;
     const long long T = a.n_rows_dev ? min((long long)*a.n_rows_dev, a.rows_max) : a.rows_max;
     if (t >= T) return;
@@ -585,15 +581,6 @@ template <class Kernel> static int raise_smem(Kernel kernel, size_t bytes, bool 
     return DPPO_OK;
 }
 
-// Clusters of `cluster` CTAs, started as soon as the kernel before lets dependents go (see wait_for_previous_kernel).
-static void set_attributes(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[2], int cluster) {
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr; cfg.numAttrs = 2;
-}
-
 // ---- which kernel, which tile ----
 // Both kernels' times in microseconds, from sweeps over N = 64 to 151,936, K = 64 to 9,728 and 1 to 1,003 tokens: the choice
 // they give was the faster one or within 5 % of it at nine shapes of ten, and 20 % off at worst.
@@ -630,16 +617,7 @@ template <bool kBf16> static int launch_pair(const CUtensorMap& mw, const CUtens
     const int rc = raise_smem(kernel, kDynSmem2, raised);
     if (rc != DPPO_OK) return rc;
     const long long work = (long long)((a.N + 255) / 256) * ((a.M_max + a.tile_n - 1) / a.tile_n), most = sm_count() / 2;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(2 * (work < most ? work : most)), 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = kDynSmem2;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
-    set_attributes(cfg, attr, 2);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, mw, mx, a);
-    if (e != cudaSuccess) return cuda_fail(e, "linear_i8 launch");
-    return DPPO_OK;
+    return launch_after("linear_i8 launch", kernel, 2 * (work < most ? work : most), kThreads, kDynSmem2, s, 2, mw, mx, a);
 }
 
 template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, int split, cudaStream_t s) {
@@ -650,16 +628,7 @@ template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, co
     const int n_ch = (a.N + kTileM - 1) / kTileM;
     const long long tiles = (long long)n_ch * ((a.M_max + kNB - 1) / kNB);
     if (tiles * split > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "linear_i8: too many tiles");
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(tiles * split), 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = small_smem<kNB>();
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
-    set_attributes(cfg, attr, split);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, mw, mx, a, n_ch, split);
-    if (e != cudaSuccess) return cuda_fail(e, "linear_i8 launch");
-    return DPPO_OK;
+    return launch_after("linear_i8 launch", kernel, tiles * split, kThreads, small_smem<kNB>(), s, split, mw, mx, a, n_ch, split);
 }
 
 template <bool kBf16> static int launch(bool pair, int nb, int split, const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
@@ -692,10 +661,8 @@ extern "C" int dppo_quantize_rows_i8(const dppo_quantize_params* p, const void* 
     if (((uintptr_t)x & 15) || ((uintptr_t)q & 15) || x_row_bytes % 16 != 0 || p->q_stride % 16 != 0)
         return fail(DPPO_ERR_MISALIGNED, "quantize_rows_i8: x / q base and row strides must be multiples of 16 bytes");
     const i8::QuantArgs a = {(const char*)x, q, scale, n_rows_dev, p->rows_max, x_row_bytes, p->q_stride, p->K};
-    if (p->dtype == DPPO_BF16) i8::quantize_rows_kernel<true, 4><<<(unsigned)p->rows_max, i8::kQuantThreads, 0, (cudaStream_t)stream>>>(a);
-    else i8::quantize_rows_kernel<false, 8><<<(unsigned)p->rows_max, i8::kQuantThreads, 0, (cudaStream_t)stream>>>(a);
-    DPPO_CHECK_LAUNCH("quantize_rows_i8 launch");
-    return DPPO_OK;
+    auto kernel = p->dtype == DPPO_BF16 ? i8::quantize_rows_kernel<true, 4> : i8::quantize_rows_kernel<false, 8>;
+    return launch_after("quantize_rows_i8 launch", kernel, p->rows_max, i8::kQuantThreads, 0, (cudaStream_t)stream, 1, a);
 }
 
 extern "C" int dppo_linear_i8(const dppo_linear_i8_params* p, const int8_t* x, const float* x_scale, const int8_t* w,

@@ -517,6 +517,7 @@ token_logprobs_warp_kernel(const Args a, int run) {
     __shared__ WarpShared<kVecs == 0> shared[kTeams];
     const int lane = threadIdx.x & 31;
     auto& ws = shared[threadIdx.x >> 5];
+    enter_kernel();
     const long long T = a.n_tokens_dev ? min((long long)*a.n_tokens_dev, a.T_max) : a.T_max;
     const long long t0 = ((long long)blockIdx.x * kTeams + (threadIdx.x >> 5)) * run;
     if (t0 >= T) return;
@@ -675,6 +676,7 @@ token_logprobs_kernel(const Args a) {
     constexpr int kLog2Per = kBf16 ? 3 : 2;
     __shared__ CtaShared<kThreads> sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    wait_for_previous();
     const long long T = a.n_tokens_dev ? min((long long)*a.n_tokens_dev, a.T_max) : a.T_max;
     unsigned rank = 0, C = 1;
     if constexpr (kCluster) { C = cg::this_cluster().num_blocks(); rank = cg::this_cluster().block_rank(); }
@@ -743,38 +745,49 @@ token_logprobs_kernel(const Args a) {
     if constexpr (kCluster) {
         cg::cluster_group cl = cg::this_cluster();
         cl.sync();                                                 // every CTA's part and list are in its shared memory
-        if (rank == 0) {
-            if (warp == 0) {
-                Part o = {kLowest, 0.0f, 0.0f, 0};
-                if (lane < (int)C) o = cl.map_shared_rank(&sh, lane)->row;
-                o = warp_join(o, a.c);
-                if (lane == 0) sh.part[0] = o;
-            }
-            if (a.k > 0) {
-                // the lists side by side in the candidate buffer (C * k <= 8 * 32 < kCap), then rank by rank
-                if (tid == 0) sh.n_cand = 0;
-                __syncthreads();
-                for (int i = tid; i < (int)C * a.k; i += kThreads) {
-                    auto* o = cl.map_shared_rank(&sh, i / a.k);
-                    const int j = i % a.k;
-                    if (!o->row.bad && j < o->n_list) {
-                        const int at = atomicAdd(&sh.n_cand, 1);
-                        sh.cand[at] = o->list[j];
-                    }
-                }
+        if (rank != 0) {                                           // ... which lasts until the first CTA has read it
+            let_next_start();
+            cl.sync();
+            return;
+        }
+        if (warp == 0) {
+            Part o = {kLowest, 0.0f, 0.0f, 0};
+            if (lane < (int)C) o = cl.map_shared_rank(&sh, lane)->row;
+            o = warp_join(o, a.c);
+            if (lane == 0) sh.part[0] = o;
+        }
+        if (a.k > 0) {                                             // the sorted lists side by side, 0 past the end of each
+            for (int i = tid; i < (int)C * kMaxTop; i += kThreads) {
+                const CtaShared<kThreads>* o = cl.map_shared_rank(&sh, i / kMaxTop);
+                sh.cand[i] = !o->row.bad && i % kMaxTop < o->n_list ? o->list[i % kMaxTop] : 0;
             }
         }
-        cl.sync();                                                 // the other CTAs' shared memory has been read
-        if (rank != 0) return;
+        cl.barrier_arrive();                                       // the others may go
+        __syncthreads();
         if (a.k > 0) {
-            const int n = sh.n_cand;
-            rank_entries(sh.cand, n, a.k, sh.list, tid, kThreads);
-            if (tid == 0) sh.n_list = n < a.k ? n : a.k;
+            if (tid == 0) sh.n_list = 0;
+            __syncthreads();
+            for (int i = tid; i < (int)C * kMaxTop; i += kThreads) {
+                const Entry e = sh.cand[i];
+                if (e == 0) continue;
+                int ahead = i % kMaxTop;                           // in its own list; in the others, by bisection
+                for (int c = 0; c < (int)C; ++c) {
+                    if (c == i / kMaxTop) continue;
+                    const Entry* l = sh.cand + c * kMaxTop;
+                    int n = 0;
+#pragma unroll
+                    for (int step = kMaxTop / 2; step > 0; step >>= 1) n += l[n + step - 1] > e ? step : 0;
+                    ahead += n + (l[n] > e ? 1 : 0);
+                }
+                if (ahead < a.k) { sh.list[ahead] = e; atomicMax(&sh.n_list, ahead + 1); }
+            }
         }
         if (tid == 0) sh.row = sh.part[0];
         __syncthreads();
+        cl.barrier_wait();
     }
 
+    let_next_start();
     if (warp == 0) {                                               // k <= 32: one warp writes all
         const Part r = sh.row;
         const RowOut o = row_out(a, r);
@@ -823,6 +836,7 @@ token_logprobs_bwd_kernel(const BwdArgs a) {
     constexpr int kUnroll = kThreads == 32 ? 4 : 8;
     const int team = kTeams == 1 ? 0 : threadIdx.x / kThreads;
     const int tid = kTeams == 1 ? threadIdx.x : threadIdx.x % kThreads;
+    enter_kernel();
     const long long T = a.n_tokens_dev ? min((long long)*a.n_tokens_dev, a.T_max) : a.T_max;
     const long long item = (long long)blockIdx.x * kTeams + team;
     const long long t = a.chunks == 1 ? item : item / a.chunks;
@@ -904,22 +918,10 @@ template <bool kBf16, int kThreads, bool kCluster>
 static int launch_fwd(const Args& a, int C, cudaStream_t s) {
     auto kernel = token_logprobs_kernel<kBf16, kThreads, kCluster>;
     if (!kCluster) {
-        kernel<<<(unsigned)a.T_max, kThreads, 0, s>>>(a);
-        DPPO_CHECK_LAUNCH("token_logprobs launch");
-        return DPPO_OK;
+        return launch_after("token_logprobs launch", kernel, a.T_max, kThreads, 0, s, 1, a);
     }
     if (a.T_max * C > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "token_logprobs: T_max=%lld needs too large a grid", a.T_max);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.T_max * C), 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
-    if (e != cudaSuccess) return cuda_fail(e, "token_logprobs launch");
-    return DPPO_OK;
+    return launch_after("token_logprobs launch", kernel, a.T_max * C, kThreads, 0, s, C, a);
 }
 
 template <bool kBf16, int kVecs> static int launch_warp(const Args& a, cudaStream_t s) {
@@ -928,9 +930,8 @@ template <bool kBf16, int kVecs> static int launch_warp(const Args& a, cudaStrea
     const long long wave = 32ll * sm_count(), per = (a.T_max + wave - 1) / wave;
     const int run = (int)(per < 1 ? 1 : per > kMaxRun ? kMaxRun : per);
     const long long warps = (a.T_max + run - 1) / run;
-    token_logprobs_warp_kernel<kBf16, kVecs, kTeams><<<(unsigned)((warps + kTeams - 1) / kTeams), 32 * kTeams, 0, s>>>(a, run);
-    DPPO_CHECK_LAUNCH("token_logprobs launch");
-    return DPPO_OK;
+    return launch_after("token_logprobs launch", token_logprobs_warp_kernel<kBf16, kVecs, kTeams>, (warps + kTeams - 1) / kTeams, 32 * kTeams,
+                        0, s, 1, a, run);
 }
 
 template <bool kBf16> static int run_fwd(const Args& a, int variant, cudaStream_t s) {
@@ -972,9 +973,7 @@ template <bool kBf16> static int run_fwd(const Args& a, int variant, cudaStream_
 template <bool kBf16, int kThreads, int kTeams> static int launch_bwd(const BwdArgs& a, cudaStream_t s) {
     const long long ctas = (a.T_max * a.chunks + kTeams - 1) / kTeams;
     if (ctas > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "token_logprobs_backward: T_max=%lld needs too large a grid", a.T_max);
-    token_logprobs_bwd_kernel<kBf16, kThreads, kTeams><<<(unsigned)ctas, kThreads * kTeams, 0, s>>>(a);
-    DPPO_CHECK_LAUNCH("token_logprobs_backward launch");
-    return DPPO_OK;
+    return launch_after("token_logprobs_backward launch", token_logprobs_bwd_kernel<kBf16, kThreads, kTeams>, ctas, kThreads * kTeams, 0, s, 1, a);
 }
 
 template <bool kBf16> static int run_bwd(BwdArgs a, cudaStream_t s) {

@@ -675,3 +675,34 @@ def test_calls_on_two_streams_at_once(B):
         for b in bs:
             for got, want in zip(b, alone):
                 assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("T, V, dtype", [(1, 20000, "bf16"), (40, 20000, "bf16"), (3000, 300, "f32"), (4000, 4001, "f32")])
+def test_dependent_calls_back_to_back(B, T, V, dtype):
+    """A call may be set up while the one before it runs: chains in which each reads what the last wrote (in place, into
+    shared buffers) give what the same calls give with a wait after each."""
+    z0, y = make(T, V, dtype, T + V)
+    f32 = dict(dtype=torch.float32, device="cuda")
+
+    def chain(wait):
+        z = z0.clone()
+        logp, H, lse, stats = torch.zeros(T, **f32), torch.zeros(T, **f32), torch.zeros(T, **f32), torch.zeros(T, 4, **f32)
+        ids, tl = torch.zeros(T, 6, dtype=torch.int32, device="cuda"), torch.zeros(T, 6, **f32)
+        n_dev = torch.tensor([T], dtype=torch.int32, device="cuda")
+        kept = []
+        torch.cuda.synchronize()
+        for i in range(6):
+            prm = B.LogprobParams(T, V, B.BF16 if dtype == "bf16" else B.F32, z.stride(0), 6, 0, 1.0)
+            B.token_logprobs(prm, z, y, n_dev, logp, H, lse, ids, tl, stats)
+            if wait:
+                torch.cuda.synchronize()
+            B.token_logprobs_backward(prm, z, y, n_dev, stats, logp, H, z)        # in place: the next call's logits
+            if wait:
+                torch.cuda.synchronize()
+            if i % 2:
+                z.mul_(3.0).add_(0.25)                                            # a kernel that knows nothing of it
+                kept += [x.clone() for x in (logp, H, lse, ids, tl, z)]
+        torch.cuda.synchronize()
+        return kept
+    for a, b in zip(chain(True), chain(False)):
+        assert torch.equal(a, b)
