@@ -299,17 +299,30 @@ template <int kPer, int kBits> __device__ __forceinline__ uint32_t kth_largest(c
     return r;
 }
 
-// The k-th largest of the lanes' values (those that are equal count together), at least kLowest.
-__device__ __forceinline__ float kth_of_lanes(float v, int k) {
-    float m = kLowest;
+// The k-th largest of the lanes' values, at least kLowest: for a small k by taking the largest away k times (those that are
+// equal go together), else out of the sorted values (a bitonic network over the lanes, 15 exchanges).
+__device__ __forceinline__ float kth_of_lanes(float v, int k, int lane) {
+    if (k <= 6) {
+        float m = kLowest;
 #pragma unroll 1
-    for (int have = 0; have < k;) {
-        m = warp_max_f32(v);
-        if (!(m > kLowest)) return kLowest;
-        have += __popc(__ballot_sync(0xffffffffu, v == m));
-        v = v == m ? -INFINITY : v;
+        for (int have = 0; have < k;) {
+            m = warp_max_f32(v);
+            if (!(m > kLowest)) return kLowest;
+            have += __popc(__ballot_sync(0xffffffffu, v == m));
+            v = v == m ? -INFINITY : v;
+        }
+        return m;
     }
-    return m;
+#pragma unroll
+    for (int size = 2; size <= 32; size <<= 1) {
+#pragma unroll
+        for (int step = size >> 1; step > 0; step >>= 1) {
+            const float o = __shfl_xor_sync(0xffffffffu, v, step);
+            const bool larger = ((lane & step) == 0) == ((lane & size) == 0);     // descending overall
+            v = larger ? fmaxf(v, o) : fminf(v, o);
+        }
+    }
+    return fmaxf(__shfl_sync(0xffffffffu, v, k - 1), kLowest);
 }
 
 // The list of the top k of n entries in shared memory, by the threads tid = 0 .. stride - 1: an entry's place is the number
@@ -593,7 +606,7 @@ token_logprobs_warp_kernel(const Args a, int run) {
 
         int n = 0;
         if (a.k > 0 && !p.bad) {
-            const float thr = kth_of_lanes(mx, a.k);
+            const float thr = kth_of_lanes(mx, a.k, lane);
             const uint32_t below = (1u << lane) - 1u;
             auto offer = [&](float z, int idx) {                   // by all lanes together
                 const uint32_t b = __ballot_sync(0xffffffffu, z >= thr);
@@ -829,11 +842,10 @@ __device__ __forceinline__ f32x2 bwd_pair(float z0, float z1, const BwdRow& r, f
     return mul2(pair_of(ex2(y0), ex2(y1)), fma2(x, pair_of(r.nX, r.nX), pair_of(r.nA, r.nA)));
 }
 
-template <bool kBf16, int kThreads, int kTeams>
+template <bool kBf16, int kThreads, int kTeams, int kUnroll>
 __global__ void __launch_bounds__(kThreads * kTeams)
 token_logprobs_bwd_kernel(const BwdArgs a) {
     constexpr int kPer = Elems<kBf16>::kPerVec, kLog2Per = kBf16 ? 3 : 2;
-    constexpr int kUnroll = kThreads == 32 ? 4 : 8;
     const int team = kTeams == 1 ? 0 : threadIdx.x / kThreads;
     const int tid = kTeams == 1 ? threadIdx.x : threadIdx.x % kThreads;
     enter_kernel();
@@ -885,15 +897,22 @@ token_logprobs_bwd_kernel(const BwdArgs a) {
         __stcs(reinterpret_cast<uint4*>(out) + i, Elems<kBf16>::pack(z));
     };
     auto sweep = [&](auto lift_f32) {
-        int i = v0 + tid;
-        for (; i + (kUnroll - 1) * kThreads < v1; i += kUnroll * kThreads) {   // all loads of a round before its stores
+        for (int i = v0 + tid; i - tid < v1; i += kUnroll * kThreads) {        // all loads of a round before its stores
             uint4 q[kUnroll];
+            if (i - tid + kUnroll * kThreads <= v1) {
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) q[u] = load_vec_rw(row + (size_t)(i + u * kThreads) * 16);
+                for (int u = 0; u < kUnroll; ++u) q[u] = load_vec_rw(row + (size_t)(i + u * kThreads) * 16);
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) put(q[u], i + u * kThreads, lift_f32);
+                for (int u = 0; u < kUnroll; ++u) put(q[u], i + u * kThreads, lift_f32);
+            } else {
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u)
+                    if (i + u * kThreads < v1) q[u] = load_vec_rw(row + (size_t)(i + u * kThreads) * 16);
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u)
+                    if (i + u * kThreads < v1) put(q[u], i + u * kThreads, lift_f32);
+            }
         }
-        for (; i < v1; i += kThreads) put(load_vec_rw(row + (size_t)i * 16), i, lift_f32);
     };
     if (zero) {
         for (int i = v0 + tid; i < v1; i += kThreads) __stcs(reinterpret_cast<uint4*>(out) + i, make_uint4(0u, 0u, 0u, 0u));
@@ -955,6 +974,8 @@ template <bool kBf16> static int run_fwd(const Args& a, int variant, cudaStream_
         C = variant / 10000; threads = variant % 10000;
     }
     if (threads == 32 && C == 1) {
+        if (nvec <= 32) return launch_warp<kBf16, 1>(a, s);
+        if (nvec <= 64) return launch_warp<kBf16, 2>(a, s);
         if (nvec <= 128) return launch_warp<kBf16, 4>(a, s);
         if (nvec <= 256) return launch_warp<kBf16, 8>(a, s);
         return launch_warp<kBf16, 0>(a, s);
@@ -970,21 +991,25 @@ template <bool kBf16> static int run_fwd(const Args& a, int variant, cudaStream_
     return fail(DPPO_ERR_UNSUPPORTED, "token_logprobs: variant %d", variant);
 }
 
-template <bool kBf16, int kThreads, int kTeams> static int launch_bwd(const BwdArgs& a, cudaStream_t s) {
+template <bool kBf16, int kThreads, int kTeams, int kUnroll> static int launch_bwd(const BwdArgs& a, cudaStream_t s) {
     const long long ctas = (a.T_max * a.chunks + kTeams - 1) / kTeams;
     if (ctas > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "token_logprobs_backward: T_max=%lld needs too large a grid", a.T_max);
-    return launch_after("token_logprobs_backward launch", token_logprobs_bwd_kernel<kBf16, kThreads, kTeams>, ctas, kThreads * kTeams, 0, s, 1, a);
+    return launch_after("token_logprobs_backward launch", token_logprobs_bwd_kernel<kBf16, kThreads, kTeams, kUnroll>, ctas, kThreads * kTeams, 0, s, 1, a);
 }
 
 template <bool kBf16> static int run_bwd(BwdArgs a, cudaStream_t s) {
     const int nvec = a.V >> (kBf16 ? 3 : 2);
     a.chunks = 1; a.chunk_vecs = nvec;
-    if (nvec <= 512) return launch_bwd<kBf16, 32, 8>(a, s);
+    // a warp per row of up to 8 KB, its loads in rounds of four (20,011 x 1,021 f32: 27 us = 6.0 TB/s; rounds of two 30,
+    // of eight 28); a round does not go past the end of a very short one (100,000 x 128 bf16: 46 us in rounds of four)
+    if (nvec <= 32) return launch_bwd<kBf16, 32, 4, 1>(a, s);
+    if (nvec <= 64) return launch_bwd<kBf16, 32, 4, 2>(a, s);
+    if (nvec <= 512) return launch_bwd<kBf16, 32, 4, 4>(a, s);
     // longer rows: a CTA of 128 threads per 1024 vectors, every thread's eight loads before its first store.  8,192 rows of
     // 151,936 bf16 entries 739 us (6.7 TB/s read and written); 256 threads with four loads 830, 512 threads 988.
     a.chunk_vecs = 1024;
     a.chunks = (nvec + a.chunk_vecs - 1) / a.chunk_vecs;
-    return launch_bwd<kBf16, 128, 1>(a, s);
+    return launch_bwd<kBf16, 128, 1, 8>(a, s);
 }
 
 // Checks that both calls make; 0 or the error.
