@@ -9,7 +9,7 @@
 //
 // Two kernels:
 //   many tokens (tensor-core bound): persistent CTA pairs (cta_group::2), 256 channels x 256 tokens per tile, 128-byte K
-//     slabs through a six-stage TMA ring, two TMEM accumulators so that the epilogue of a tile runs under the next one's
+//     slabs through a TMA ring of 224 KB, two TMEM accumulators so that the epilogue of a tile runs under the next one's
 //     products; tiles are handed out so that the CTAs running together share their weights and their tokens in L2
 //   few tokens (bound by reading the weights): a CTA per 128 channels, 16 to 128 tokens, and the contraction split over
 //     the CTAs of a cluster when there are too few tiles to keep all SMs reading; the int32 partial sums are joined
@@ -28,13 +28,13 @@ namespace i8 {
 constexpr int kBK = 128;                  // K slab: 128 codes = one 128-byte swizzle row
 constexpr int kTileM = 128;               // channels per CTA
 constexpr int kTileN = 256;               // most tokens per tile of the pair kernel
-constexpr int kStages2 = 6;
+constexpr int kMaxStages = 12;
 constexpr int kBytesA = kTileM * kBK;                        // 16 KB
-constexpr int kBytesB2 = kTileN / 2 * kBK;                   // 16 KB: this CTA's half of the token tile
-constexpr int kStageBytes2 = kBytesA + kBytesB2;
-constexpr int kThreads = 192;
+constexpr int kThreads = 320;              // producer warp, MMA warp, 8 epilogue warps (two per TMEM lane quarter)
 constexpr int kTokenGroup = 16;           // token tiles swept together (4096 tokens: 10 MB of codes at K = 2560)
-constexpr size_t kDynSmem2 = (size_t)kStages2 * kStageBytes2 + 1024;
+constexpr int kRingBytes = 7 * (kBytesA + kTileN / 2 * kBK);   // pair kernel: 7 stages of the largest tile, more of smaller ones
+constexpr size_t kDynSmem2 = (size_t)kRingBytes + 1024;
+static_assert(kDynSmem2 + 512 <= 232448, "the ring must fit one CTA's shared memory");
 
 struct Args {
     const float* x_scale;
@@ -97,10 +97,10 @@ __device__ __forceinline__ void store_column(const Args& a, long long t0, long l
 
 // ---- many tokens: CTA pairs ---------------------------------------------------------------------------
 struct Shared2 {
-    unsigned long long full[kStages2];
-    unsigned long long empty[kStages2];
+    unsigned long long full[kMaxStages];
+    unsigned long long empty[kMaxStages];
     unsigned long long acc_full[2];
-    unsigned long long acc_empty[2];      // the leader's copy counts 8 arrivals: 4 epilogue warps x 2 CTAs
+    unsigned long long acc_empty[2];      // the leader's copy counts 16 arrivals: 8 epilogue warps x 2 CTAs
     unsigned long long drain;             // products in flight on an early way out
     uint32_t tmem_base;
     int abort;
@@ -131,16 +131,19 @@ linear_i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     const bool leader = rank == 0;
     volatile int* abort_flag = &sh.abort;
     const int n_m2 = (a.N + 2 * kTileM - 1) / (2 * kTileM);
+    // a stage: 128 codes of K of this CTA's 128 channels and of its half of the token tile
+    const uint32_t stage_bytes = (uint32_t)(kBytesA + a.tile_n / 2 * kBK);
+    const uint32_t stages = min((uint32_t)kMaxStages, (uint32_t)kRingBytes / stage_bytes);
 
     if (tid == 0) {
         sh.abort = 0;
-        for (int s = 0; s < kStages2; ++s) {
+        for (uint32_t s = 0; s < stages; ++s) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(lm_smem_u32(&sh.full[s])));
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(lm_smem_u32(&sh.empty[s])));
         }
         for (int b = 0; b < 2; ++b) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(lm_smem_u32(&sh.acc_full[b])));
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], 8;" :: "r"(lm_smem_u32(&sh.acc_empty[b])));
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 16;" :: "r"(lm_smem_u32(&sh.acc_empty[b])));
         }
         asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(lm_smem_u32(&sh.drain)));
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -163,28 +166,26 @@ linear_i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer (both CTAs)
         if (lane == 0) {
-            const uint32_t stage_bytes = 2u * (uint32_t)(kBytesA + a.tile_n / 2 * kBK);
-            uint32_t it = 0;
+            uint32_t it = 0, s = 0, use = 0;
             int m2, n;
             for (uint32_t j = 0; tile_of(j, n_m2, n_tok, m2, n) && !*abort_flag; ++j) {
                 const int row_w = (2 * m2 + (int)rank) * kTileM, row_x = n * a.tile_n + (int)rank * (a.tile_n / 2);
-                for (int k = 0; k < a.n_ksteps; ++k, ++it) {
-                    const uint32_t s = it % kStages2, use = it / kStages2;
+                for (int k = 0; k < a.n_ksteps; ++k, ++it, s = s + 1 == stages ? 0 : s + 1, use += s == 0 ? 1 : 0) {
                     if (use > 0 && !lm_wait(lm_smem_u32(&sh.empty[s]), (use - 1) & 1, abort_flag, a.wait_limit_ns)) break;
                     const uint32_t bar_local = lm_smem_u32(&sh.full[s]), bar = bar_local & kPeerMask;
-                    const uint32_t dst = tiles + s * kStageBytes2;
+                    const uint32_t dst = tiles + s * stage_bytes;
                     if (leader)                                        // the leader's barrier collects both CTAs' bytes
                         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;"
-                                     :: "r"(bar_local), "r"(stage_bytes + (it == 0 ? (uint32_t)a.test_extra_tx : 0u)) : "memory");
+                                     :: "r"(bar_local), "r"(2 * stage_bytes + (it == 0 ? (uint32_t)a.test_extra_tx : 0u)) : "memory");
                     lm_tma_2d_pair(dst, &map_w, bar, k * kBK, row_w, 0);
                     lm_tma_2d_pair(dst + kBytesA, &map_x, bar, k * kBK, row_x, 0);
                 }
             }
             if (*abort_flag && leader) {                               // copies in flight get a bounded chance to land
-                const uint32_t pending = it < (uint32_t)kStages2 ? it : (uint32_t)kStages2;
+                const uint32_t pending = it < stages ? it : stages;
                 for (uint32_t i = 0; i < pending; ++i) {
                     const uint32_t i2 = it - 1 - i;
-                    lm_wait_plain(lm_smem_u32(&sh.full[i2 % kStages2]), (i2 / kStages2) & 1, a.wait_limit_ns);
+                    lm_wait_plain(lm_smem_u32(&sh.full[i2 % stages]), (i2 / stages) & 1, a.wait_limit_ns);
                 }
             }
         }
@@ -192,7 +193,7 @@ linear_i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         // ------------------------------------------------------------------ MMA issuer (leader CTA only)
         if (lane == 0 && leader) {
             const uint32_t desc = idesc(2 * kTileM, a.tile_n);
-            uint32_t it = 0;
+            uint32_t s = 0, use = 0;
             int m2, n;
             bool ok = true;
             for (uint32_t j = 0; ok && tile_of(j, n_m2, n_tok, m2, n) && !*abort_flag; ++j) {
@@ -200,11 +201,10 @@ linear_i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 if (use_b > 0 && !lm_wait(lm_smem_u32(&sh.acc_empty[b]), (use_b - 1) & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t d_tmem = tmem_base + b * kTileN;
-                for (int k = 0; k < a.n_ksteps; ++k, ++it) {
-                    const uint32_t s = it % kStages2, use = it / kStages2;
+                for (int k = 0; k < a.n_ksteps; ++k, s = s + 1 == stages ? 0 : s + 1, use += s == 0 ? 1 : 0) {
                     if (!lm_wait(lm_smem_u32(&sh.full[s]), use & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t dw = lm_smem_desc_k(tiles + s * kStageBytes2), dx = lm_smem_desc_k(tiles + s * kStageBytes2 + kBytesA);
+                    const uint64_t dw = lm_smem_desc_k(tiles + s * stage_bytes), dx = lm_smem_desc_k(tiles + s * stage_bytes + kBytesA);
 #pragma unroll
                     for (int kk = 0; kk < kBK / 32; ++kk) {              // 32 codes of K per instruction
                         const uint32_t accumulate = (k > 0 || kk > 0) ? 1u : 0u;
@@ -226,8 +226,8 @@ linear_i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             }
         }
     } else {
-        // ------------------------------------------------------------------ epilogue (warps 2..5, both CTAs)
-        const int q = warp & 3;                                          // TMEM lane quarter of this warp
+        // ------------------------------------------------------------------ epilogue (warps 2..9, both CTAs)
+        const int q = warp & 3, half = (warp - 2) >> 2;                  // TMEM lane quarter of this warp; which blocks of 32 tokens
         int m2, n;
         for (uint32_t j = 0; tile_of(j, n_m2, n_tok, m2, n); ++j) {
             const int ch = (2 * m2 + (int)rank) * kTileM + q * 32 + lane;
@@ -238,7 +238,7 @@ linear_i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + b * kTileN;
 #pragma unroll 1
-            for (int c = 0; c < a.tile_n / 32; ++c) {
+            for (int c = half; c < a.tile_n / 32; c += 2) {
                 const long long t0 = (long long)n * a.tile_n + c * 32;
                 if (t0 >= T) break;
                 uint32_t v[32];
@@ -248,7 +248,7 @@ linear_i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0)                                               // the leader's MMA thread waits for all 8 warps
+            if (lane == 0)                                               // the leader's MMA thread waits for all 16 warps
                 asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(lm_smem_u32(&sh.acc_empty[b]) & kPeerMask) : "memory");
         }
     }
@@ -374,6 +374,7 @@ linear_i8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
     // epilogue warps; the int32 sums of a split contraction go through shared memory: [token][channel], in the ring,
     // which nothing reads or writes any more once `done` has completed
     const int q = warp & 3, row = q * 32 + lane;
+    const int half = (warp - 2) >> 2, halves = (int)(blockDim.x - 64) >> 7;         // one or two warps per lane quarter share the tokens
     const int ch = m * kTileM + row;
     bool live = false;
     const float sw = warp >= 2 && ch < a.N ? a.w_scale[ch] : 0.0f;
@@ -384,7 +385,7 @@ linear_i8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16);
 #pragma unroll 1
-            for (int c = 0; c < kNB / kChunk; ++c) {
+            for (int c = half; c < kNB / kChunk; c += halves) {
                 const long long t0 = t_tile + c * kChunk;
                 if (t0 >= T) break;
                 uint32_t v[32];
@@ -405,15 +406,16 @@ linear_i8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
         if (live) {
             // this CTA's share of the tokens: part, part + split, ...; a batch's loads are all under way before the first is used
             // (one token at a time, each waits out the latency of its remote reads: 128 tokens 31 us instead of 14)
-            constexpr int kBatch = 8;
+            constexpr int kBatch = 4;
             const int n_tok = (int)min((long long)kNB, T - t_tile);
-            for (int c0 = part; c0 < n_tok; c0 += kBatch * split) {
+            const int step = halves * split;
+            for (int c0 = part + half * split; c0 < n_tok; c0 += kBatch * step) {
                 int32_t sum[kBatch];
                 float sx[kBatch];
 #pragma unroll
                 for (int i = 0; i < kBatch; ++i) {
                     sum[i] = 0;
-                    sx[i] = c0 + i * split < n_tok ? a.x_scale[t_tile + c0 + i * split] : 0.0f;
+                    sx[i] = c0 + i * step < n_tok ? a.x_scale[t_tile + c0 + i * step] : 0.0f;
                 }
                 for (int i0 = 0; i0 < split; ++i0) {                     // every CTA starts with another one's memory
                     const int r = (part + i0) & (split - 1);
@@ -422,7 +424,7 @@ linear_i8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
                     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(tiles + (uint32_t)row * 4u), "r"(r));
 #pragma unroll
                     for (int i = 0; i < kBatch; ++i) {
-                        const int c = c0 + i * split;
+                        const int c = c0 + i * step;
                         x[i] = 0;
                         if (c < n_tok)
                             asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(x[i]) : "r"(remote + (uint32_t)(c * kTileM) * 4u) : "memory");
@@ -432,8 +434,8 @@ linear_i8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
                 }
 #pragma unroll
                 for (int i = 0; i < kBatch; ++i)
-                    if (c0 + i * split < n_tok && ch < a.N)
-                        store<kBf16>(a, t_tile + c0 + i * split, ch, value_of(sum[i], sx[i], sw));
+                    if (c0 + i * step < n_tok && ch < a.N)
+                        store<kBf16>(a, t_tile + c0 + i * step, ch, value_of(sum[i], sx[i], sw));
             }
         }
         lm_cluster_sync();                                               // the others have read this CTA's shared memory
@@ -628,7 +630,10 @@ template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, co
     const int n_ch = (a.N + kTileM - 1) / kTileM;
     const long long tiles = (long long)n_ch * ((a.M_max + kNB - 1) / kNB);
     if (tiles * split > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "linear_i8: too many tiles");
-    return launch_after("linear_i8 launch", kernel, tiles * split, kThreads, small_smem<kNB>(), s, split, mw, mx, a, n_ch, split);
+    // four more epilogue warps where they have work: they shorten a join or a wide epilogue (16 x 1,024 x 1,024: 5.3 -> 4.7 us)
+    // and only cost their launch elsewhere (1 x 151,936 x 2,560: 62 -> 65)
+    const int threads = split > 1 || kNB >= 64 ? kThreads : kThreads - 128;
+    return launch_after("linear_i8 launch", kernel, tiles * split, threads, small_smem<kNB>(), s, split, mw, mx, a, n_ch, split);
 }
 
 template <bool kBf16> static int launch(bool pair, int nb, int split, const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
