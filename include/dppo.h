@@ -352,14 +352,14 @@ int dppo_lmhead_grpo_loss(const dppo_lmhead_params* p, const void* hidden, const
  */
 typedef struct {
     int64_t T_max;          /* rows of logits / upper bound of tokens                                */
-    int32_t V;              /* vocabulary size                                                       */
+    int32_t V;              /* vocabulary size, up to 2^30                                           */
     int32_t dtype;          /* dppo_dtype of logits and dlogits                                      */
     int64_t row_stride;     /* elements between consecutive rows (>= V; bytes a multiple of 16)      */
     int32_t top_k;          /* alternatives per row, 0..32 (the backward ignores it)                 */
     int32_t variant;        /* 0: the library picks the launch shape.  Tuning aid of the forward:
                                C*10000 + threads: C = 1, 2, 4 or 8 CTAs per row with 128, 256 or 512
                                threads each; 32: one warp per row                                    */
-    double temperature;     /* > 0                                                                   */
+    double temperature;     /* 1e-30 .. 1e30                                                         */
 } dppo_logprob_params;
 
 /*   logits       [T_max x row_stride] of dtype

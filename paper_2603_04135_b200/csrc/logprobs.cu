@@ -866,7 +866,7 @@ token_logprobs_bwd_kernel(const BwdArgs a) {
     const float ga = da * a.inv_tau, gb = db * a.inv_tau;
     r.nA = -fmaf(gb, st.z - st.y, ga);
     r.nX = -gb * a.inv_tau;
-    r.far = fmaxf(kFar / a.c, -1e30f);
+    r.far = kFar / a.c;
     r.low2 = bf16_pair(__float2bfloat16_rd(st.x + r.far));
     // bf16 entries are lifted by a packed maximum before they are unpacked, unless the bound is beyond the type
     const bool lift = !kBf16 || !(fabsf(st.x) <= 1e37f);
@@ -1018,7 +1018,8 @@ static int check(const dppo_logprob_params* p, const char* what, const void* log
     if (p->T_max < 0 || p->V < 1) return fail(DPPO_ERR_INVALID_ARG, "%s: T_max=%lld V=%d", what, (long long)p->T_max, p->V);
     if (p->dtype != DPPO_F32 && p->dtype != DPPO_BF16) return fail(DPPO_ERR_UNSUPPORTED, "%s: dtype %d", what, p->dtype);
     if (p->row_stride < p->V) return fail(DPPO_ERR_BAD_SHAPE, "%s: row_stride %lld < V %d", what, (long long)p->row_stride, p->V);
-    if (!(p->temperature > 0.0) || !(p->temperature < INFINITY)) return fail(DPPO_ERR_INVALID_ARG, "%s: temperature must be > 0", what);
+    if (!(p->temperature >= 1e-30) || !(p->temperature <= 1e30)) return fail(DPPO_ERR_INVALID_ARG, "%s: temperature must be in [1e-30, 1e30]", what);
+    if (p->V > (1 << 30)) return fail(DPPO_ERR_BAD_SHAPE, "%s: V=%d, the limit is 2^30", what, p->V);
     if (p->T_max >= ((int64_t)1 << 31)) return fail(DPPO_ERR_BAD_SHAPE, "%s: T_max must be below 2^31", what);
     const size_t esize = p->dtype == DPPO_BF16 ? 2 : 4;
     if (p->T_max > 0 && !logits) return fail(DPPO_ERR_INVALID_ARG, "%s: NULL logits", what);
