@@ -157,9 +157,8 @@ def _arr(x, name, device, dtype, n):
 
 def _mat(x, name, device, dtype, rows, cols, stride):
     """The same for [rows x cols] with `stride` elements between rows."""
-    if (x.__class__ is _Tensor and x.dtype is dtype and x.get_device() == device and x.stride() == (stride, 1)
-            and x.shape[0] >= rows and x.shape[1] >= cols):
-        return x.data_ptr()
+    if x.__class__ is _Tensor and x.dtype is dtype and x.get_device() == device and x.stride() == (stride, 1) and x.numel() >= rows * stride:
+        return x.data_ptr()                      # whole rows
     if not isinstance(x, _Tensor):
         return x
     _check_kind(x, name, device, dtype)

@@ -32,6 +32,7 @@ namespace cg = cooperative_groups;
 namespace logprob {
 
 constexpr int kMaxTop = 32;
+constexpr int kMaxCluster = 8;
 constexpr int kCand = 512;                // candidate buffer of a CTA-sized team
 constexpr int kCandWarp = 256;            // and of a warp-sized one
 constexpr float kLowest = -3.402823466e38f;
@@ -284,17 +285,23 @@ template <int kPer, int kBits> __device__ __forceinline__ uint32_t kth_largest(c
 #pragma unroll
     for (int i = 1; i < kPer; ++i) { hi = max(hi, own[i]); lo = min(lo, own[i]); }
     hi = __reduce_max_sync(0xffffffffu, hi); lo = __reduce_min_sync(0xffffffffu, lo);
-    const int top = 31 - __clz(hi ^ lo);                           // -1: all keys alike
-    uint32_t r = top < 0 ? hi : hi & ~((2u << top) - 1u);
+    int bit = 31 - __clz(hi ^ lo);                                 // -1: all keys alike
+    uint32_t r = bit < 0 ? hi : hi & ~((2u << bit) - 1u);
+    // two bits a step: the three counts are under way together
 #pragma unroll 1
-    for (int bit = top; bit >= 32 - kBits; --bit) {
-        const uint32_t t = r | (1u << bit);
-        int cnt = 0;
+    for (bit -= 1; bit + 1 >= 32 - kBits; bit -= 2) {
+        const uint32_t unit = bit >= 0 ? 1u << bit : 0u;           // bit < 0: the last step has one bit left
+        const uint32_t t1 = r + unit, t2 = r + (bit >= 0 ? unit << 1 : 1u), t3 = t2 + unit;
+        int c1 = 0, c2 = 0, c3 = 0;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) cnt += own[i] >= t ? 1 : 0;
-        cnt = __reduce_add_sync(0xffffffffu, cnt);
-        if (cnt >= k) r = t;
-        if (cnt == k) break;                                       // exactly the k largest reach t: t serves as well
+        for (int i = 0; i < kPer; ++i) {
+            c1 += own[i] >= t1 ? 1 : 0; c2 += own[i] >= t2 ? 1 : 0; c3 += own[i] >= t3 ? 1 : 0;
+        }
+        c1 = __reduce_add_sync(0xffffffffu, c1); c2 = __reduce_add_sync(0xffffffffu, c2); c3 = __reduce_add_sync(0xffffffffu, c3);
+        if (c3 >= k) { r = t3; c1 = c3; }
+        else if (c2 >= k) { r = t2; c1 = c2; }
+        else if (c1 >= k) r = t1;
+        if (c1 == k) break;                                        // exactly the k largest reach r
     }
     return r;
 }
@@ -435,11 +442,14 @@ __device__ __forceinline__ void select_top(CtaShared<kThreads>& sh, const Span& 
     constexpr int kPer = Elems<kBf16>::kPerVec;
     const float thr = sh.thr;
     if (sh.tmax[tid] >= thr) {
-        for (int s = 0; s < n_slots; ++s)
-            if (__bfloat162float(sh.best[s][tid]) >= thr) {
-                const int at = atomicAdd(&sh.n_group, 1);
-                if (at < kMaxGroups) sh.group[at] = s * kThreads + tid;
-            }
+        uint32_t hits = 0;                                         // all loads before the first atomic
+#pragma unroll
+        for (int s = 0; s < kSlots; ++s)
+            if (s < n_slots && __bfloat162float(sh.best[s][tid]) >= thr) hits |= 1u << s;
+        for (; hits != 0; hits &= hits - 1) {
+            const int at = atomicAdd(&sh.n_group, 1);
+            if (at < kMaxGroups) sh.group[at] = (__ffs(hits) - 1) * kThreads + tid;
+        }
     }
     __syncthreads();
     auto offer = [&](float z, int idx) {
@@ -757,11 +767,23 @@ token_logprobs_kernel(const Args a) {
 
     if constexpr (kCluster) {
         cg::cluster_group cl = cg::this_cluster();
+        if (a.k > 0 && tid < kMaxTop && (sh.row.bad || tid >= sh.n_list)) sh.list[tid] = 0;      // 0 past the end of the list
         cl.sync();                                                 // every CTA's part and list are in its shared memory
         if (rank != 0) {                                           // ... which lasts until the first CTA has read it
             let_next_start();
             cl.sync();
             return;
+        }
+        // the sorted lists side by side (a thread holds its entry too), and the sums: one round of remote reads
+        constexpr int kMine = kMaxCluster * kMaxTop / kThreads > 0 ? kMaxCluster * kMaxTop / kThreads : 1;
+        Entry mine[kMine];
+        if (a.k > 0) {
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                const int at = i * kThreads + tid;
+                mine[i] = 0;
+                if (at < (int)C * kMaxTop) mine[i] = cl.map_shared_rank(&sh, at / kMaxTop)->list[at % kMaxTop];
+            }
         }
         if (warp == 0) {
             Part o = {kLowest, 0.0f, 0.0f, 0};
@@ -769,34 +791,34 @@ token_logprobs_kernel(const Args a) {
             o = warp_join(o, a.c);
             if (lane == 0) sh.part[0] = o;
         }
-        if (a.k > 0) {                                             // the sorted lists side by side, 0 past the end of each
-            for (int i = tid; i < (int)C * kMaxTop; i += kThreads) {
-                const CtaShared<kThreads>* o = cl.map_shared_rank(&sh, i / kMaxTop);
-                sh.cand[i] = !o->row.bad && i % kMaxTop < o->n_list ? o->list[i % kMaxTop] : 0;
-            }
+        if (a.k > 0) {
+#pragma unroll
+            for (int i = 0; i < kMine; ++i)
+                if (i * kThreads + tid < kMaxCluster * kMaxTop) sh.cand[i * kThreads + tid] = mine[i];
         }
         cl.barrier_arrive();                                       // the others may go
         __syncthreads();
+        if (tid == 0) { sh.row = sh.part[0]; sh.n_list = 0; }
+        __syncthreads();
         if (a.k > 0) {
-            if (tid == 0) sh.n_list = 0;
-            __syncthreads();
-            for (int i = tid; i < (int)C * kMaxTop; i += kThreads) {
-                const Entry e = sh.cand[i];
-                if (e == 0) continue;
-                int ahead = i % kMaxTop;                           // in its own list; in the others, by bisection
-                for (int c = 0; c < (int)C; ++c) {
-                    if (c == i / kMaxTop) continue;
-                    const Entry* l = sh.cand + c * kMaxTop;
-                    int n = 0;
 #pragma unroll
-                    for (int step = kMaxTop / 2; step > 0; step >>= 1) n += l[n + step - 1] > e ? step : 0;
-                    ahead += n + (l[n] > e ? 1 : 0);
-                }
+            for (int i = 0; i < kMine; ++i) {
+                const Entry e = mine[i];
+                if (e == 0) continue;
+                // entries ahead: by bisection of every list, its own included (all lists a step at a time)
+                int n[kMaxCluster], ahead = 0;
+#pragma unroll
+                for (int c = 0; c < kMaxCluster; ++c) n[c] = c * kMaxTop;
+#pragma unroll
+                for (int step = kMaxTop / 2; step > 0; step >>= 1)
+#pragma unroll
+                    for (int c = 0; c < kMaxCluster; ++c) n[c] += sh.cand[n[c] + step - 1] > e ? step : 0;
+#pragma unroll
+                for (int c = 0; c < kMaxCluster; ++c) ahead += n[c] - c * kMaxTop + (sh.cand[n[c]] > e ? 1 : 0);
                 if (ahead < a.k) { sh.list[ahead] = e; atomicMax(&sh.n_list, ahead + 1); }
             }
+            __syncthreads();
         }
-        if (tid == 0) sh.row = sh.part[0];
-        __syncthreads();
         cl.barrier_wait();
     }
 
@@ -958,15 +980,19 @@ template <bool kBf16> static int run_fwd(const Args& a, int variant, cudaStream_
     int C = 1, threads = 256;
     if (variant == 0) {
         // Rows of up to 4 KB: a warp each (20,011 x 1,021 f32: 22 us, a CTA each 68), up to 24 KB where there are enough of them
-        // to fill the SMs with warps (8,192 x 8,192 bf16: 33 us against 42; 1,000 of them: 9.7 against 8.3).  Longer rows, or
-        // fewer: a CTA each, small CTAs where there are many of them (8,192 x 151,936 bf16: 128 threads 416 us, 256 449;
-        // 2,003 x 151,936 f32: 212 against 199); few rows: split over a cluster, up to about three CTAs per SM
-        // (1 row of 151,936: 1 CTA 16.9 us, 8 CTAs 10.0; 300 rows: 1 CTA 31.6, 2 CTAs 38.7).
+        // to fill the SMs with warps (8,192 x 8,192 bf16: 33 us against 42; 1,000 of them: 12 against 7.6).  Longer rows, or
+        // fewer: a CTA each, small CTAs where there are many (8,192 x 151,936 bf16: 128 threads 416 us, 256 449; 2,003 x
+        // 151,936 f32: 212 against 199).  No more rows than SMs: one CTA up to 80 KB (32,000 bf16: 6.1 us, split in two
+        // or more 6.5 and up: the join costs two to three), longer ones split over a cluster, up to two or three CTAs per SM
+        // (1 row of 151,936 bf16: 12.4 us in one CTA, 8.0 in eight; 100 rows: 16.4, 13.8 in four, 20.7 in eight).
         const long long sms = sm_count();
-        if (nvec <= 256 || (nvec <= 1536 && a.T_max >= 13 * sms)) { threads = 32; }
-        else {
-            while (C < 8 && a.T_max * C * 2 <= 3 * sms && nvec / (2 * C) >= 256) C *= 2;
-            threads = C == 1 && (nvec <= 2048 || a.T_max >= 24 * sms) ? 128 : 256;
+        if (nvec <= 256 || (nvec <= 1536 && a.T_max >= 13 * sms)) {
+            threads = 32;
+        } else if (nvec <= 5120 || a.T_max * 2 > 3 * sms) {
+            threads = nvec <= 1024 || a.T_max >= 24 * sms || (nvec <= 2048 && a.T_max > sms) ? 128 : nvec > 2048 && a.T_max <= sms ? 512 : 256;
+        } else {
+            C = a.T_max * 8 <= 2 * sms ? 8 : a.T_max * 4 <= 3 * sms ? 4 : nvec <= 16384 && a.T_max <= sms ? 1 : 2;
+            threads = C <= 2 && a.T_max <= sms ? 512 : 256;
         }
     } else if (variant == 32) {
         threads = 32;
