@@ -16,6 +16,8 @@ Side modes (each prints its own lines and is not part of the default run):
   --prune-pack-sweep            density / timing table of the pruning and packing sweep shape
   --profile-case loss           a self-contained run of the loss sweep for timing and profiler captures
                                 (--rows --vocab --dtype --iters --in-place --full-call --back-to-back --variant)
+  --profile-case score, linear  the same for the scoring call (--rows --vocab --dtype --top-k --backward --variant) and the
+                                8-bit product (--tokens --hidden --vocab --variant)
   --profile-case lmhead         the same for the fused LM-head (--tokens --hidden --vocab --iters --backward --variant)
 """
 import argparse
@@ -309,6 +311,57 @@ def time_row_length(dtype, V, rows, dev, iters=8, warmup=3):
 
 
 # --------------------------------------------------------------------------------------- profile cases
+def run_score_case(args):
+    """`score`: dppo_token_logprobs (or, with --backward, its gradient) on --rows rows of --vocab logits;  `linear`:
+    dppo_quantize_rows_i8 + dppo_linear_i8 on --tokens tokens, --hidden wide, --vocab channels, bf16 out."""
+    from paper_2603_04135_b200 import binding as B
+    torch.cuda.set_device(0)
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    if args.profile_case == "linear":
+        M, K, N = args.tokens, args.hidden, args.vocab
+        ld = -(-K // 128) * 128
+        x = torch.empty(M, -(-K // 8) * 8, device="cuda").normal_(generator=gen).to(torch.bfloat16)
+        w = torch.randint(-127, 128, (N, ld), device="cuda", generator=gen, dtype=torch.int8)
+        q, qs = torch.zeros(M, ld, dtype=torch.int8, device="cuda"), torch.zeros(M, device="cuda")
+        ws, out = torch.rand(N, device="cuda", generator=gen), torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+        work, unit = 2.0 * M * N * K, "TOP/s"
+
+        def call():
+            B.quantize_rows_i8(B.QuantizeParams(M, K, B.BF16, x.shape[1], ld), x, q, qs, status=status)
+            B.linear_i8(B.LinearI8Params(M, N, K, ld, ld, N, B.BF16, args.variant), q, qs, w, ws, out, status=status)
+    else:
+        T, V, dt = args.rows, args.vocab, torch.bfloat16 if args.dtype == "bf16" else torch.float32
+        per16 = 16 // dt.itemsize
+        z = torch.empty(T, -(-V // per16) * per16, dtype=dt, device="cuda").normal_(0.0, 2.0, generator=gen)
+        y = torch.randint(0, V, (T,), device="cuda", generator=gen, dtype=torch.int32)
+        logp, ent, lse, stats = (torch.zeros(T, *n, device="cuda") for n in ((), (), (), (4,)))
+        ids, top = torch.zeros(T, args.top_k, dtype=torch.int32, device="cuda"), torch.zeros(T, args.top_k, device="cuda")
+        prm = B.LogprobParams(T, V, B.BF16 if dt is torch.bfloat16 else B.F32, z.shape[1], args.top_k, args.variant, 1.0)
+        dz = torch.empty_like(z) if args.backward else None
+        work, unit = (2.0 if args.backward else 1.0) * T * V * dt.itemsize * 1e-3, "GB/s"
+
+        def forward():
+            B.token_logprobs(prm, z, y, None, logp, ent, lse, ids if args.top_k else None, top if args.top_k else None, stats, status)
+
+        def call():
+            if args.backward:
+                B.token_logprobs_backward(prm, z, y, None, stats, logp, ent, dz, status)
+            else:
+                forward()
+        forward()
+    for it in range(args.iters):
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        call()
+        e1.record()
+        torch.cuda.synchronize()
+        ms = e0.elapsed_time(e1)
+        print("iter %d: %.4f ms  %.1f %s  status %d" % (it, ms, work / ms / (1e9 if unit == "TOP/s" else 1e3), unit, status.item()))
+    assert status.item() == 0
+    return 0
+
+
 def run_profile_case(args):
     """A small, self-contained run of one entry point for timing and profiler captures: prints the event-timed
     duration of each call.  `loss`: dppo_grpo_loss_fwd_bwd on --rows token rows of the large-vocabulary workload
@@ -676,7 +729,7 @@ def main():
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--no-lmhead", action="store_true", help="skip the fused LM-head measurement")
     ap.add_argument("--no-modes", action="store_true", help="skip the forward-only / in-place / sequence-ratio timings")
-    ap.add_argument("--profile-case", choices=["loss", "lmhead"], help="instead of the benchmark: a small self-contained run")
+    ap.add_argument("--profile-case", choices=["loss", "lmhead", "score", "linear"], help="instead of the benchmark: a small self-contained run")
     ap.add_argument("--rows", type=int, default=8192)
     ap.add_argument("--tokens", type=int, default=16384)
     ap.add_argument("--hidden", type=int, default=2560)
@@ -685,17 +738,20 @@ def main():
     ap.add_argument("--iters", type=int, default=3)
     ap.add_argument("--seqs", type=int, default=16)
     ap.add_argument("--variant", type=int, default=0, help="kernel variant of the profile case (see include/dppo.h)")
+    ap.add_argument("--top-k", type=int, default=0, help="score profile case: alternatives per row")
     ap.add_argument("--in-place", action="store_true")
     ap.add_argument("--forward-only", action="store_true")
     ap.add_argument("--full-call", action="store_true")
     ap.add_argument("--back-to-back", action="store_true", help="enqueue all iterations before synchronising")
-    ap.add_argument("--backward", action="store_true", help="lmhead profile case: also dhidden and dW")
+    ap.add_argument("--backward", action="store_true", help="lmhead profile case: also dhidden and dW; score: the gradient")
     ap.add_argument("--no-clock-sampling", action="store_true", help="do not poll nvidia-smi during the timed region")
     ap.add_argument("--prune-pack-sweep", action="store_true",
                     help="instead of the benchmark: density and timing table of the pruning / packing sweep shape")
     args = ap.parse_args()
     if args.prune_pack_sweep:
         sys.exit(run_prune_pack_sweep(args))
+    if args.profile_case in ("score", "linear"):
+        sys.exit(run_score_case(args))
     if args.profile_case:
         sys.exit(run_profile_case(args))
     if args.impl == "ours" and args.warmup < 3:

@@ -517,6 +517,7 @@ __device__ __forceinline__ void write_top(const Args& a, long long t, int j, flo
 // per entry; a warp takes several consecutive rows, and the scalar outputs of all of them are formed in one pass, a lane
 // per row.
 constexpr int kMaxRun = 8;
+constexpr int kWarpCtas = 7;               // resident CTAs (of four warps) per SM
 constexpr int kHotVecs = 64;
 template <bool kSweep> struct WarpShared;
 template <> struct WarpShared<false> {
@@ -533,7 +534,7 @@ template <> struct WarpShared<true> {
 };
 
 template <bool kBf16, int kVecs, int kTeams>
-__global__ void __launch_bounds__(32 * kTeams)
+__global__ void __launch_bounds__(32 * kTeams, kWarpCtas)                 // 28 warps per SM: 32 spill, 24 leave latencies uncovered
 token_logprobs_warp_kernel(const Args a, int run) {
     constexpr int kPer = Elems<kBf16>::kPerVec, kLog2Per = kBf16 ? 3 : 2;
     constexpr uint32_t kNone = kBf16 ? 0xff80ff80u : 0xff800000u;  // -inf
@@ -967,9 +968,17 @@ static int launch_fwd(const Args& a, int C, cudaStream_t s) {
 
 template <bool kBf16, int kVecs> static int launch_warp(const Args& a, cudaStream_t s) {
     constexpr int kTeams = 4;
-    // as many rows per warp as make one wave of warps (about 32 resident per SM), 8 at most
-    const long long wave = 32ll * sm_count(), per = (a.T_max + wave - 1) / wave;
-    const int run = (int)(per < 1 ? 1 : per > kMaxRun ? kMaxRun : per);
+    // Rows per warp: one where they are fewer than two waves of warps, else what takes the fewest rows one after the other, in
+    // whole waves (20,011 x 1,021 f32: 5 rows a warp, one wave, 22 us; 4 rows, 1.2 waves, 27; 5,000: 1 row 8.0, 2 rows 9.3).
+    const long long wave = (long long)kWarpCtas * kTeams * sm_count();
+    int run = 1;
+    if (a.T_max > 2 * wave) {
+        long long best = 0;
+        for (int r = 1; r <= kMaxRun; ++r) {
+            const long long rows = ((a.T_max + r - 1) / r + wave - 1) / wave * r;
+            if (best == 0 || rows <= best) { best = rows; run = r; }
+        }
+    }
     const long long warps = (a.T_max + run - 1) / run;
     return launch_after("token_logprobs launch", token_logprobs_warp_kernel<kBf16, kVecs, kTeams>, (warps + kTeams - 1) / kTeams, 32 * kTeams,
                         0, s, 1, a, run);

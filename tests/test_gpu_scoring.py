@@ -726,3 +726,28 @@ def test_dependent_calls_back_to_back(B, T, V, dtype):
         return kept
     for a, b in zip(chain(True), chain(False)):
         assert torch.equal(a, b)
+
+
+def test_events_between_calls_are_kept(B):
+    """A call that may be set up early still waits for another stream's event (and a copy) in front of it."""
+    V, T = 5003, 20
+    z, y = make(T, V, "f32", 1)
+    z2, _ = make(T, V, "f32", 2)
+    want = Fwd(B, z2, V, y, 4, 1.0).host()
+    prm = B.LogprobParams(T, V, B.F32, z.stride(0), 0, 0, 1.0)
+    one, stats, dz = torch.ones(T, device="cuda"), torch.zeros(T, 4, device="cuda"), torch.zeros_like(z)
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        buf = z.clone()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)                            # about 10 ms
+            buf.copy_(z2)
+            done = torch.cuda.Event()
+            done.record()
+        B.token_logprobs(prm, z, y, None, one, None, None, None, None, stats)          # lets its successor start early
+        torch.cuda.current_stream().wait_event(done)
+        f = Fwd(B, buf, V, y, 4, 1.0)
+        got = f.host()
+        for n in want:
+            assert np.array_equal(got[n], want[n]), n
