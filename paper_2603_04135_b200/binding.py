@@ -145,6 +145,8 @@ _Tensor, _f32, _i32, _i8 = torch.Tensor, torch.float32, torch.int32, torch.int8
 def _arr(x, name, device, dtype, n):
     """Device pointer of n dense elements.  A torch tensor is checked: of `dtype`, on `device` (the current one), large
     enough.  The plain case is one expression: these checks are on the path of calls that take 10 us."""
+    if x is None:
+        return None
     if x.__class__ is _Tensor and x.dtype is dtype and x.get_device() == device and x.numel() >= n and x.is_contiguous():
         return x.data_ptr()
     if not isinstance(x, _Tensor):
@@ -185,15 +187,12 @@ def _device():
     global _cuda
     if _cuda is None:
         _cuda = torch.cuda.is_available()
-    return torch.cuda.current_device() if _cuda else -1
+    return _get_device() if _cuda else -1
 
 
-def _current_stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
-
-
-# the same without the stream object that current_stream() builds (3 us of a small call)
-_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream)
+# torch.cuda.current_device() and current_stream().cuda_stream without their Python layers (3 us of a small call)
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 def _stream(stream):
@@ -307,39 +306,48 @@ def token_logprobs(params, logits, target, n_tokens_dev, logp_out, entropy_out, 
     p, d = params, _device()
     T, V = p.T_max, p.V
     k = p.top_k * T
-    _check(lib.dppo_token_logprobs(
+    rc = lib.dppo_token_logprobs(
         ctypes.byref(p), _mat(logits, "logits", d, _TORCH_DTYPE.get(p.dtype), T, V, p.row_stride),
         _arr(target, "target", d, _i32, T), _arr(n_tokens_dev, "n_tokens_dev", d, _i32, 1), _arr(logp_out, "logp_out", d, _f32, T),
         _arr(entropy_out, "entropy_out", d, _f32, T), _arr(lse_out, "lse_out", d, _f32, T), _arr(top_ids, "top_ids", d, _i32, k),
         _arr(top_logp, "top_logp", d, _f32, k), _arr(stats, "stats", d, _f32, 4 * T), _arr(status, "status", d, _i32, 1),
-        _stream(stream)))
+        _current_stream(d) if stream is None and d >= 0 else _stream(stream))
+    if rc != 0:
+        _check(rc)
 
 
 def token_logprobs_backward(params, logits, target, n_tokens_dev, stats, dlogp, dentropy, dlogits, status=None,
                             stream=None):
     p, d = params, _device()
     T, V, dt, ld = p.T_max, p.V, _TORCH_DTYPE.get(p.dtype), p.row_stride
-    _check(lib.dppo_token_logprobs_backward(
+    rc = lib.dppo_token_logprobs_backward(
         ctypes.byref(p), _mat(logits, "logits", d, dt, T, V, ld), _arr(target, "target", d, _i32, T),
         _arr(n_tokens_dev, "n_tokens_dev", d, _i32, 1), _arr(stats, "stats", d, _f32, 4 * T), _arr(dlogp, "dlogp", d, _f32, T),
         _arr(dentropy, "dentropy", d, _f32, T), _mat(dlogits, "dlogits", d, dt, T, V, ld), _arr(status, "status", d, _i32, 1),
-        _stream(stream)))
+        _current_stream(d) if stream is None and d >= 0 else _stream(stream))
+    if rc != 0:
+        _check(rc)
 
 
 def quantize_rows_i8(params, x, q, scale, n_rows_dev=None, status=None, stream=None):
     p, d = params, _device()
     M, K = p.rows_max, p.K
-    _check(lib.dppo_quantize_rows_i8(
+    rc = lib.dppo_quantize_rows_i8(
         ctypes.byref(p), _mat(x, "x", d, _TORCH_DTYPE.get(p.dtype), M, K, p.x_stride), _mat(q, "q", d, _i8, M, K, p.q_stride),
         _arr(scale, "scale", d, _f32, M), _arr(n_rows_dev, "n_rows_dev", d, _i32, 1), _arr(status, "status", d, _i32, 1),
-        _stream(stream)))
+        _current_stream(d) if stream is None and d >= 0 else _stream(stream))
+    if rc != 0:
+        _check(rc)
 
 
 def linear_i8(params, x, x_scale, w, w_scale, out, n_rows_dev=None, status=None, stream=None):
     p, d = params, _device()
     M, N, K = p.M_max, p.N, p.K
-    _check(lib.dppo_linear_i8(
+    rc = lib.dppo_linear_i8(
         ctypes.byref(p), _mat(x, "x", d, _i8, M, K, p.x_stride), _arr(x_scale, "x_scale", d, _f32, M),
         _mat(w, "w", d, _i8, N, K, p.w_stride), _arr(w_scale, "w_scale", d, _f32, N),
         _mat(out, "out", d, _TORCH_DTYPE.get(p.out_dtype), M, N, p.out_stride), _arr(n_rows_dev, "n_rows_dev", d, _i32, 1),
-        _arr(status, "status", d, _i32, 1), _stream(stream)))
+        _arr(status, "status", d, _i32, 1),
+        _current_stream(d) if stream is None and d >= 0 else _stream(stream))
+    if rc != 0:
+        _check(rc)
