@@ -359,7 +359,7 @@ typedef struct {
     int32_t variant;        /* 0: the library picks the launch shape.  Tuning aid of the forward:
                                C*10000 + threads: C = 1, 2, 4 or 8 CTAs per row with 128, 256 or 512
                                threads each; 32: one warp per row                                    */
-    double temperature;     /* 1e-30 .. 1e30                                                         */
+    double temperature;     /* 1e-6 .. 1e6                                                           */
 } dppo_logprob_params;
 
 /*   logits       [T_max x row_stride] of dtype

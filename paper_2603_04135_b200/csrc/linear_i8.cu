@@ -220,7 +220,7 @@ linear_i8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                              :: "r"(lm_smem_u32(&sh.acc_full[b])), "h"((unsigned short)3) : "memory");
             }
-            if (!ok) {                                                 // products already issued finish before memory goes away
+            if (!ok || *abort_flag) {                                  // products already issued finish before memory goes away
                 asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(lm_smem_u32(&sh.drain)) : "memory");
                 lm_wait_plain(lm_smem_u32(&sh.drain), 0, a.wait_limit_ns);
             }
@@ -402,6 +402,7 @@ linear_i8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
         }
     }
     if (split > 1) {
+        __syncwarp();
         lm_cluster_sync();                                               // every CTA's sums are in its shared memory
         if (live) {
             // this CTA's share of the tokens: part, part + split, ...; a batch's loads are all under way before the first is used

@@ -5,13 +5,12 @@
 // cancels on a peaked row).  One pass: every thread keeps an ONLINE (m, S, Q) over the 16-byte vectors it sees; a larger
 // maximum M moves them by D = (m - M) c: S' = S 2^D, Q' = (Q + D S) 2^D.
 //
-// The alternatives cost the pass nothing.  A thread's running maximum is known anyway at the end of the row, and the
+// The alternatives need no second pass.  A thread's running maximum is known anyway at the end of the row, and the
 // k-th largest of the threads' maxima, thr, is a lower bound of the k-th largest entry (k threads have an entry that
 // large): a thread whose maximum is below thr holds none of the top k.  Each thread also leaves the maximum of every round of
 // its sweep (4 vectors) in shared memory, so about k such groups of vectors are read again (a few KB of the row), entries
 // >= thr become candidates, and a candidate's rank is the number of candidates ahead of it in the order (value
-// descending, index ascending).  Too many candidates (ties)
-// are met by rules that need no more memory: see collect_ties.
+// descending, index ascending).  Too many candidates (ties) are met by rules that need no more memory: see collect_ties.
 //
 // A row is worked on by a TEAM: a warp (short rows), a CTA, or a cluster of CTAs that split the row and join through
 // distributed shared memory (few rows: a decode batch).
@@ -1053,7 +1052,7 @@ static int check(const dppo_logprob_params* p, const char* what, const void* log
     if (p->T_max < 0 || p->V < 1) return fail(DPPO_ERR_INVALID_ARG, "%s: T_max=%lld V=%d", what, (long long)p->T_max, p->V);
     if (p->dtype != DPPO_F32 && p->dtype != DPPO_BF16) return fail(DPPO_ERR_UNSUPPORTED, "%s: dtype %d", what, p->dtype);
     if (p->row_stride < p->V) return fail(DPPO_ERR_BAD_SHAPE, "%s: row_stride %lld < V %d", what, (long long)p->row_stride, p->V);
-    if (!(p->temperature >= 1e-30) || !(p->temperature <= 1e30)) return fail(DPPO_ERR_INVALID_ARG, "%s: temperature must be in [1e-30, 1e30]", what);
+    if (!(p->temperature >= 1e-6) || !(p->temperature <= 1e6)) return fail(DPPO_ERR_INVALID_ARG, "%s: temperature must be in [1e-6, 1e6]", what);
     if (p->V > (1 << 30)) return fail(DPPO_ERR_BAD_SHAPE, "%s: V=%d, the limit is 2^30", what, p->V);
     if (p->T_max >= ((int64_t)1 << 31)) return fail(DPPO_ERR_BAD_SHAPE, "%s: T_max must be below 2^31", what);
     const size_t esize = p->dtype == DPPO_BF16 ? 2 : 4;

@@ -143,7 +143,7 @@ def test_every_launch_shape(B, variant, dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V", [1000, 20003])
-@pytest.mark.parametrize("tau", [1e-30, 1e-3, 1e3, 1e30])
+@pytest.mark.parametrize("tau", [1e-6, 1e-3, 1e3, 1e6])
 def test_extreme_temperatures(B, V, tau, dtype):
     """Temperatures at which the distribution is a single token, or uniform; masked entries too."""
     z, y = make(4, V, dtype, 17)
@@ -153,12 +153,11 @@ def test_extreme_temperatures(B, V, tau, dtype):
     z[3, ::3] = float(torch.finfo(DT[dtype]).min)
     z[1, int(y[1])] = 1.0
     run(B, z, V, y, 5, tau)
-    if tau >= 1e-3:                                                  # |dz| ~ 1/tau^2 stays within f32
-        a, b = torch.randn(4, device="cuda"), torch.randn(4, device="cuda")
-        zh, yh = z[:, :V].double().cpu().numpy(), y.cpu().numpy()
-        want = scoring.token_logprobs_backward(zh, yh, a.double().cpu().numpy(), b.double().cpu().numpy(), tau)
-        check_grad(backward(B, z, V, y, a, b, tau)[:, :V].double().cpu().numpy(), want, zh, yh, a.double().cpu().numpy(),
-                   b.double().cpu().numpy(), tau, dtype, V)
+    a, b = torch.randn(4, device="cuda"), torch.randn(4, device="cuda")
+    zh, yh = z[:, :V].double().cpu().numpy(), y.cpu().numpy()
+    want = scoring.token_logprobs_backward(zh, yh, a.double().cpu().numpy(), b.double().cpu().numpy(), tau)
+    check_grad(backward(B, z, V, y, a, b, tau)[:, :V].double().cpu().numpy(), want, zh, yh, a.double().cpu().numpy(),
+               b.double().cpu().numpy(), tau, dtype, V)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

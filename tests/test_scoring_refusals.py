@@ -28,7 +28,7 @@ P = 1 << 20      # an aligned address that is only looked at
     ((4, 8, 1, 12, 0, 0, 1.0), B.ERR_MISALIGNED), ((4, 8, 1, 8, 33, 0, 1.0), B.ERR_INVALID_ARG),
     ((4, 8, 1, 8, -1, 0, 1.0), B.ERR_INVALID_ARG), ((4, 8, 1, 8, 0, 0, 0.0), B.ERR_INVALID_ARG),
     ((4, 8, 1, 8, 0, 0, float("nan")), B.ERR_INVALID_ARG), ((4, 8, 1, 8, 0, 0, float("inf")), B.ERR_INVALID_ARG),
-    ((4, 8, 1, 8, 0, 0, 1e-31), B.ERR_INVALID_ARG), ((4, 8, 1, 8, 0, 0, -1.0), B.ERR_INVALID_ARG),
+    ((4, 8, 1, 8, 0, 0, 1e-7), B.ERR_INVALID_ARG), ((4, 8, 1, 8, 0, 0, 1e7), B.ERR_INVALID_ARG), ((4, 8, 1, 8, 0, 0, -1.0), B.ERR_INVALID_ARG),
     ((4, (1 << 30) + 8, 1, (1 << 30) + 8, 0, 0, 1.0), B.ERR_BAD_SHAPE), ((4, 8, 1, 8, 0, -1, 1.0), B.ERR_INVALID_ARG), ((4, 8, 1, 8, 0, 30256, 1.0), B.ERR_UNSUPPORTED),
     ((4, 8, 1, 8, 0, 7, 1.0), B.ERR_UNSUPPORTED), ((1 << 31, 8, 1, 8, 0, 0, 1.0), B.ERR_BAD_SHAPE)])
 def test_logprobs_params(prm, want):
