@@ -5,7 +5,9 @@ for the nullable ones.  Every function raises DppoError on a non-zero return cod
 fallback: if the library has not been built, importing this module raises.
 
 The scoring calls (token_logprobs, token_logprobs_backward, quantize_rows_i8, linear_i8) also check the tensors they
-are given: element type, on the current device, and large enough for the sizes in the params.
+are given: element type, on the current device, and large enough for the sizes in the params.  Their plain case (torch
+tensors in the exact layout, the current stream) is checked and marshalled in native code (_marshal.so); anything else, and a
+tree where that module has not been built, takes the same checks here.
 """
 import ctypes
 import os
@@ -301,53 +303,76 @@ def sequence_log_ratio(logp, logp_old, cu_seqlens, S_max, out, status=None, stre
                                        _stream(stream)))
 
 
+try:
+    from . import _marshal as _native
+    _native.bind(LogprobParams, QuantizeParams, LinearI8Params,
+                 *(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.dppo_token_logprobs, lib.dppo_token_logprobs_backward,
+                                                                   lib.dppo_quantize_rows_i8, lib.dppo_linear_i8)))
+except ImportError:
+    class _native:                   # noqa: N801  (stands in for the module: nothing is the plain case)
+        token_logprobs = token_logprobs_backward = quantize_rows_i8 = linear_i8 = staticmethod(lambda *a: None)
+
+
+def _done(rc):
+    """Whether the native marshalling has made the call (rc: its return code, None where it was not the plain case)."""
+    if rc is None:
+        return False
+    _check(rc)
+    return True
+
+
 def token_logprobs(params, logits, target, n_tokens_dev, logp_out, entropy_out, lse_out, top_ids, top_logp, stats,
                    status=None, stream=None):
+    rc = _native.token_logprobs(params, logits, target, n_tokens_dev, logp_out, entropy_out, lse_out, top_ids, top_logp, stats,
+                                status, stream)
+    if rc == 0 or _done(rc):
+        return
     p, d = params, _device()
     T, V = p.T_max, p.V
     k = p.top_k * T
-    rc = lib.dppo_token_logprobs(
+    _check(lib.dppo_token_logprobs(
         ctypes.byref(p), _mat(logits, "logits", d, _TORCH_DTYPE.get(p.dtype), T, V, p.row_stride),
         _arr(target, "target", d, _i32, T), _arr(n_tokens_dev, "n_tokens_dev", d, _i32, 1), _arr(logp_out, "logp_out", d, _f32, T),
         _arr(entropy_out, "entropy_out", d, _f32, T), _arr(lse_out, "lse_out", d, _f32, T), _arr(top_ids, "top_ids", d, _i32, k),
         _arr(top_logp, "top_logp", d, _f32, k), _arr(stats, "stats", d, _f32, 4 * T), _arr(status, "status", d, _i32, 1),
-        _current_stream(d) if stream is None and d >= 0 else _stream(stream))
-    if rc != 0:
-        _check(rc)
+        _stream(stream)))
 
 
 def token_logprobs_backward(params, logits, target, n_tokens_dev, stats, dlogp, dentropy, dlogits, status=None,
                             stream=None):
+    rc = _native.token_logprobs_backward(params, logits, target, n_tokens_dev, stats, dlogp, dentropy, dlogits, status, stream)
+    if rc == 0 or _done(rc):
+        return
     p, d = params, _device()
     T, V, dt, ld = p.T_max, p.V, _TORCH_DTYPE.get(p.dtype), p.row_stride
-    rc = lib.dppo_token_logprobs_backward(
+    _check(lib.dppo_token_logprobs_backward(
         ctypes.byref(p), _mat(logits, "logits", d, dt, T, V, ld), _arr(target, "target", d, _i32, T),
         _arr(n_tokens_dev, "n_tokens_dev", d, _i32, 1), _arr(stats, "stats", d, _f32, 4 * T), _arr(dlogp, "dlogp", d, _f32, T),
         _arr(dentropy, "dentropy", d, _f32, T), _mat(dlogits, "dlogits", d, dt, T, V, ld), _arr(status, "status", d, _i32, 1),
-        _current_stream(d) if stream is None and d >= 0 else _stream(stream))
-    if rc != 0:
-        _check(rc)
+        _stream(stream)))
 
 
 def quantize_rows_i8(params, x, q, scale, n_rows_dev=None, status=None, stream=None):
+    rc = _native.quantize_rows_i8(params, x, q, scale, n_rows_dev, status, stream)
+    if rc == 0 or _done(rc):
+        return
     p, d = params, _device()
     M, K = p.rows_max, p.K
-    rc = lib.dppo_quantize_rows_i8(
+    _check(lib.dppo_quantize_rows_i8(
         ctypes.byref(p), _mat(x, "x", d, _TORCH_DTYPE.get(p.dtype), M, K, p.x_stride), _mat(q, "q", d, _i8, M, K, p.q_stride),
         _arr(scale, "scale", d, _f32, M), _arr(n_rows_dev, "n_rows_dev", d, _i32, 1), _arr(status, "status", d, _i32, 1),
-        _current_stream(d) if stream is None and d >= 0 else _stream(stream))
-    if rc != 0:
-        _check(rc)
+        _stream(stream)))
 
 
 def linear_i8(params, x, x_scale, w, w_scale, out, n_rows_dev=None, status=None, stream=None):
+    rc = _native.linear_i8(params, x, x_scale, w, w_scale, out, n_rows_dev, status, stream)
+    if rc == 0 or _done(rc):
+        return
     p, d = params, _device()
     M, N, K = p.M_max, p.N, p.K
-    rc = lib.dppo_linear_i8(
+    _check(lib.dppo_linear_i8(
         ctypes.byref(p), _mat(x, "x", d, _i8, M, K, p.x_stride), _arr(x_scale, "x_scale", d, _f32, M),
         _mat(w, "w", d, _i8, N, K, p.w_stride), _arr(w_scale, "w_scale", d, _f32, N),
         _mat(out, "out", d, _TORCH_DTYPE.get(p.out_dtype), M, N, p.out_stride), _arr(n_rows_dev, "n_rows_dev", d, _i32, 1),
         _arr(status, "status", d, _i32, 1),
-        _current_stream(d) if stream is None and d >= 0 else _stream(stream))
-    if rc != 0:
-        _check(rc)
+        _stream(stream)))

@@ -1,4 +1,5 @@
-"""Builds libdppo.so (sm_100a) in-tree with nvcc.  `python -m paper_2603_04135_b200.build`."""
+"""Builds libdppo.so (sm_100a, nvcc) and the binding's argument marshalling (_marshal.so, host compiler) in-tree.
+`python -m paper_2603_04135_b200.build`."""
 import os
 import subprocess
 import sys
@@ -9,6 +10,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libdppo.so")
+MARSHAL = os.path.join(PKG, "_marshal.so")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]
@@ -60,5 +62,29 @@ def build_library(force=False, verbose=False):
     return LIB
 
 
+def build_marshal(force=False):
+    """Compile csrc/marshal.cpp against this interpreter's and torch's headers.  Returns the module's path."""
+    src = os.path.join(CSRC, "marshal.cpp")
+    if not force and not _stale(MARSHAL, [src, os.path.join(ROOT, "include", "dppo.h")]):
+        return MARSHAL
+    import sysconfig
+
+    import torch
+    tdir = os.path.dirname(torch.__file__)
+    tlib = os.path.join(tdir, "lib")
+    cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.sep in _nvcc() else "/usr/local/cuda"
+    inc = [os.path.join(tdir, "include"), os.path.join(tdir, "include", "torch", "csrc", "api", "include"),
+           os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-I" + os.path.join(ROOT, "include"),
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)]
+    cmd += [x for p in inc for x in ("-isystem", p)]
+    cmd += [src, "-o", MARSHAL, "-L" + tlib, "-Wl,-rpath," + tlib, "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("host compiler failed: %s\n%s\n%s" % (" ".join(cmd), r.stdout, r.stderr))
+    return MARSHAL
+
+
 if __name__ == "__main__":
+    print(build_marshal(force="--force" in sys.argv))
     print(build_library(force="--force" in sys.argv, verbose="-v" in sys.argv))

@@ -7,6 +7,7 @@ rescales its sums at most once per vector (5 u each: difference, product, expone
     eS = (3 E|x| + 3 + adds + 5 rescales + 16) u,   E|x| = sum p |x|,
 which is the absolute error of l = ln S besides l's own rounding; Q/S = -E|x| carries twice that.
 """
+import ctypes
 import math
 
 import numpy as np
@@ -750,3 +751,71 @@ def test_events_between_calls_are_kept(B):
         got = f.host()
         for n in want:
             assert np.array_equal(got[n], want[n]), n
+
+
+def test_native_marshalling_takes_the_plain_case_only(B):
+    """The plain case is marshalled natively; addresses, parameters, views and explicit streams go through Python and do the
+    same; what is wrong is named by the same errors either way."""
+    T, V, k = 6, 1003, 3
+    z, y = make(T, V, "f32", 3)
+    f = lambda *s: torch.zeros(*s, device="cuda")
+    logp, ent, lse, stats, tl = f(T), f(T), f(T), f(T, 4), f(T, k)
+    ids = torch.zeros(T, k, dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    prm = B.LogprobParams(T, V, B.F32, z.stride(0), k, 0, 1.0)
+    plain = (z, y, None, logp, ent, lse, ids, tl, stats)
+    native = getattr(B._native, "__name__", "").endswith("_marshal")
+    assert B._native.token_logprobs(prm, *plain, status, None) == (0 if native else None)
+    B.token_logprobs(prm, *plain, status)
+    want = [t.clone() for t in (logp, ent, lse, ids, tl, stats)]
+    others = [((z[:, :V],) + plain[1:], None), ((torch.nn.Parameter(z),) + plain[1:], None), (plain, torch.cuda.current_stream()),
+              ((z.data_ptr(), y.data_ptr(), None) + tuple(t.data_ptr() for t in plain[3:]), None)]
+    for args, stream in others:
+        for t in (logp, ent, lse, ids, tl, stats):
+            t.zero_()
+        assert B._native.token_logprobs(prm, *args, status, stream) is None
+        B.token_logprobs(prm, *args, status, stream=stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, (logp, ent, lse, ids, tl, stats)))
+
+    def code(prm, *args):
+        with pytest.raises(B.DppoError) as e:
+            B.token_logprobs(prm, *args, status)
+        return e.value.code
+    assert code(prm, z.double(), *plain[1:]) == B.ERR_INVALID_ARG
+    assert code(prm, z.cpu(), *plain[1:]) == B.ERR_INVALID_ARG
+    assert code(prm, z[:5].clone(), *plain[1:]) == B.ERR_BAD_SHAPE
+    assert code(prm, z, y[:5].clone(), *plain[2:]) == B.ERR_BAD_SHAPE
+    assert code(prm, z, y, None, f(2 * T)[::2], *plain[4:]) == B.ERR_BAD_SHAPE
+    assert code(prm, None, *plain[1:]) == B.ERR_INVALID_ARG
+    assert code(B.LogprobParams(T, V, B.F32, z.stride(0), k, 77, 1.0), *plain) == B.ERR_UNSUPPORTED
+    assert code(B.LogprobParams(T, V, 9, z.stride(0), k, 0, 1.0), *plain) in (B.ERR_UNSUPPORTED, B.ERR_INVALID_ARG)
+    with pytest.raises((AttributeError, ctypes.ArgumentError)):          # the params of another call
+        B.token_logprobs(B.LinearI8Params(T, V, 64, 64, 64, V, 0), *plain, status)
+    assert status.item() == 0
+
+
+def test_calls_from_two_threads(B):
+    """Two Python threads, a stream each, the same work at the same time."""
+    import threading
+    V, T = 20003, 31
+    z, y = make(T, V, "bf16", 12)
+    want = Fwd(B, z, V, y, 8, 1.0).host()
+    got, errors = {}, []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(30):
+                    got[i] = Fwd(B, z, V, y, 8, 1.0).host()
+        except Exception as e:                                       # noqa: BLE001  (reported by the main thread)
+            errors.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    for o in got.values():
+        for n in want:
+            assert np.array_equal(o[n].view(np.int32), want[n].view(np.int32)), n
