@@ -337,7 +337,7 @@ __device__ __forceinline__ void rank_entries(const Entry* cand, int n, int k, En
     for (int i = tid; i < n; i += stride) {
         const Entry e = cand[i];
         int ahead = 0;
-#pragma unroll 8
+#pragma unroll 4
         for (int j = 0; j < n; ++j) ahead += cand[j] > e ? 1 : 0;
         if (ahead < k) list[ahead] = e;
     }
@@ -441,14 +441,12 @@ __device__ __forceinline__ void select_top(CtaShared<kThreads>& sh, const Span& 
     constexpr int kPer = Elems<kBf16>::kPerVec;
     const float thr = sh.thr;
     if (sh.tmax[tid] >= thr) {
-        uint32_t hits = 0;                                         // all loads before the first atomic
-#pragma unroll
-        for (int s = 0; s < kSlots; ++s)
-            if (s < n_slots && __bfloat162float(sh.best[s][tid]) >= thr) hits |= 1u << s;
-        for (; hits != 0; hits &= hits - 1) {
-            const int at = atomicAdd(&sh.n_group, 1);
+        uint32_t hits = 0;                                         // the loads before the first atomic
+#pragma unroll 4
+        for (int s = 0; s < n_slots; ++s) hits |= __bfloat162float(sh.best[s][tid]) >= thr ? 1u << s : 0u;
+        int at = atomicAdd(&sh.n_group, __popc(hits));
+        for (; hits != 0; hits &= hits - 1, ++at)
             if (at < kMaxGroups) sh.group[at] = (__ffs(hits) - 1) * kThreads + tid;
-        }
     }
     __syncthreads();
     auto offer = [&](float z, int idx) {
@@ -465,11 +463,19 @@ __device__ __forceinline__ void select_top(CtaShared<kThreads>& sh, const Span& 
             const int v = sp.v0 + ((slot << log2_vecs) + (i & ((1 << log2_vecs) - 1))) * kThreads + thread;
             if (v >= sp.v1) continue;
             const uint4 q = load_vec(sp.row + (size_t)v * 16);
-            if (!(vec_max<kBf16>(q) >= thr)) continue;
             float z[kPer];
             Elems<kBf16>::unpack(q, z);
+            int cnt = 0;
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) offer(z[j], v * kPer + j);
+            for (int j = 0; j < kPer; ++j) cnt += z[j] >= thr ? 1 : 0;
+            if (cnt == 0) continue;
+            int at = atomicAdd(&sh.n_cand, cnt);                   // one per vector
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (z[j] >= thr) {
+                    if (at < kCand) sh.cand[at] = entry_of(z[j], v * kPer + j);
+                    ++at;
+                }
         }
         if (sp.tail0 + tid < sp.tail1) offer(Elems<kBf16>::load1(sp.row, sp.tail0 + tid), sp.tail0 + tid);
     }
@@ -703,15 +709,16 @@ token_logprobs_kernel(const Args a) {
     const long long T = a.n_tokens_dev ? min((long long)*a.n_tokens_dev, a.T_max) : a.T_max;
     unsigned rank = 0, C = 1;
     if constexpr (kCluster) { C = cg::this_cluster().num_blocks(); rank = cg::this_cluster().block_rank(); }
-    const long long t = (long long)(blockIdx.x / C);
+    const int log2C = 31 - __clz((int)C);                          // C = 1, 2, 4 or 8
+    const long long t = (long long)(blockIdx.x >> log2C);
     if (t >= T) return;                                            // the whole cluster leaves together
 
     const char* row = a.logits + t * a.row_bytes;
     const int nvec = a.V >> kLog2Per;
     Span sp;
     sp.row = row;
-    sp.v0 = (int)((long long)nvec * rank / C);
-    sp.v1 = (int)((long long)nvec * (rank + 1) / C);
+    sp.v0 = (int)((long long)nvec * rank >> log2C);
+    sp.v1 = (int)((long long)nvec * (rank + 1) >> log2C);
     sp.tail0 = rank == C - 1 ? nvec << kLog2Per : a.V;
     sp.tail1 = a.V;
 
@@ -823,11 +830,11 @@ token_logprobs_kernel(const Args a) {
     }
 
     let_next_start();
-    if (warp == 0) {                                               // k <= 32: one warp writes all
+    if (warp < 2) {                                                // k <= 32: a warp for the scalars, one for the alternatives
         const Part r = sh.row;
         const RowOut o = row_out(a, r);
-        if (lane == 0) write_scalars(a, t, r, o, zy, y_state);
-        if (lane < a.k) write_top(a, t, lane, r.m, o.l, r.bad, sh.list, sh.n_list);
+        if (tid == 0) write_scalars(a, t, r, o, zy, y_state);
+        if (warp == 1 && lane < a.k) write_top(a, t, lane, r.m, o.l, r.bad, sh.list, sh.n_list);
     }
 }
 
