@@ -990,24 +990,62 @@ template <bool kBf16, int kVecs> static int launch_warp(const Args& a, cudaStrea
                         0, s, 1, a, run);
 }
 
+// The launch shape of the CTA and cluster kernels: CTAs per row and threads per CTA.  `n` below is the CTAs that the fullest SM
+// gets; 2, 5 and 10 CTAs of 512, 256 and 128 threads fit on one (48 registers a thread).
+struct Shape { int C, threads; };
+
+static Shape row_shape(long long T, int nvec, bool alternatives) {
+    const long long sms = sm_count();
+    auto per_sm = [&](long long ctas) { return (ctas + sms - 1) / sms; };
+    if (nvec <= 512) return {1, 128};
+    // Rows over 80 KB (64 KB for a few without alternatives) are split over a cluster where they do not fill the SMs evenly.
+    // The time in us: the rows' share that the fullest SM reads, at 30 KB/us (12 % slower when a single CTA has the SM), and
+    // the join, which costs more with alternatives.  (48 rows of 256,000 f32: 12.2 in eight CTAs, 17.7 in four; 90: 20.4 in
+    // four; 300: 50.7 in two, 65.9 in one; 444 are even: one.  Over 260 random shapes of 1 to 12,000 rows of 1,200 to 260,000
+    // entries this rule and the one for warps take a shape 0.6 % from the best of all, 16 % at worst.)
+    const bool very_long = nvec >= (alternatives ? 30000 : 12000);
+    int C = 1;
+    if (nvec > 5120 || (nvec > 4096 && !alternatives && 8 * T <= sms)) {
+        constexpr float kJoin[4] = {0.f, 0.5f, 1.0f, 0.5f}, kJoinAlternatives[4] = {0.f, 1.4f, 1.6f, 1.5f};
+        float best = 0;
+        for (int i = 0; i < 4; ++i) {
+            const long long n = per_sm(T << i);
+            // A cluster's CTAs start together, so close to full SMs the last clusters wait (183 x 160,597 f32: 34 us in four CTAs,
+            // 29 in two), and three CTAs per SM crowd each other in the selection (48 x 151,936 bf16 out of L2, 8 alternatives:
+            // 10.2 us in eight CTAs, 9.4 in four).
+            const int quarters = i < 3 ? 21 - i : very_long || !alternatives ? 16 : 8;       // of an SM's count of CTAs
+            if (i > 0 && 4 * (T << i) > quarters * sms) break;
+            const float t = (float)n / (float)(1 << i) * (n == 1 ? 1.12f : 1.f) * (float)nvec * (16.f / 30e3f)
+                          + (alternatives ? kJoinAlternatives[i] : kJoin[i]);
+            if (i == 0 || t < best) { best = t; C = 1 << i; }
+        }
+    }
+    const long long n = per_sm(T * C);
+    if (C == 8) return {C, very_long && 4 * T * C <= 7 * sms ? 512 : 256};
+    if (C == 4) return {C, n <= 2 && (very_long || !alternatives) ? 512 : 256};
+    if (C == 2) return {C, n <= 2 ? 512 : 256};
+    // One CTA per row: the largest that leave every SM's rows resident at once (1,000 x 151,936 f32: 96 us with 128 threads, 106
+    // with 256; 296: 30.6 with 512, 40.3 with 256); in many waves the smallest (8,192 x 151,936 bf16: 416 against 449).
+    // Shorter rows give a large CTA too little to do for its reductions (148 x 16,384 bf16 with alternatives: 256 threads).
+    if (nvec <= 1024) return {1, n <= 3 ? 256 : 128};
+    if (nvec <= 2048) return {1, n <= 2 && !alternatives ? 512 : n <= 4 ? 256 : 128};
+    return {1, n <= 2 ? 512 : n <= 5 ? 256 : n <= 10 || n >= 24 ? 128 : 256};
+}
+
 template <bool kBf16> static int run_fwd(const Args& a, int variant, cudaStream_t s) {
     const int nvec = a.V >> (kBf16 ? 3 : 2);
     int C = 1, threads = 256;
     if (variant == 0) {
-        // Rows of up to 4 KB: a warp each (20,011 x 1,021 f32: 22 us, a CTA each 68), up to 24 KB where there are enough of them
-        // to fill the SMs with warps (8,192 x 8,192 bf16: 33 us against 42; 1,000 of them: 12 against 7.6).  Longer rows, or
-        // fewer: a CTA each, small CTAs where there are many (8,192 x 151,936 bf16: 128 threads 416 us, 256 449; 2,003 x
-        // 151,936 f32: 212 against 199).  No more rows than SMs: one CTA up to 80 KB (32,000 bf16: 6.1 us, split in two
-        // or more 6.5 and up: the join costs two to three), longer ones split over a cluster, up to two or three CTAs per SM
-        // (1 row of 151,936 bf16: 12.4 us in one CTA, 8.0 in eight; 100 rows: 16.4, 13.8 in four, 20.7 in eight).
+        // Rows of up to 4 KB: a warp each (20,011 x 1,021 f32: 22 us, a CTA each 68).  Up to 20 KB where there are enough of them
+        // to fill the SMs with warps (20,000 x 2,048 f32, 8 alternatives: 41 us against 66; 1,000 of them: 8.1 against 6.1;
+        // 20,000 x 5,120: 83 against 96, 2,000 of them 15.6 against 14.4; 20,000 x 6,144: no gain either way), without
+        // alternatives up to 12 KB (20,000 x 2,800: 46 against 52; 6,000 x 4,096: 23 against 20).
         const long long sms = sm_count();
-        if (nvec <= 256 || (nvec <= 1536 && a.T_max >= 13 * sms)) {
+        if (nvec <= 256 || (nvec <= 768 && a.T_max >= 13 * sms) || (nvec <= 1280 && a.k > 0 && a.T_max >= 20 * sms)) {
             threads = 32;
-        } else if (nvec <= 5120 || a.T_max * 2 > 3 * sms) {
-            threads = nvec <= 1024 || a.T_max >= 24 * sms || (nvec <= 2048 && a.T_max > sms) ? 128 : nvec > 2048 && a.T_max <= sms ? 512 : 256;
         } else {
-            C = a.T_max * 8 <= 2 * sms ? 8 : a.T_max * 4 <= 3 * sms ? 4 : nvec <= 16384 && a.T_max <= sms ? 1 : 2;
-            threads = C <= 2 && a.T_max <= sms ? 512 : 256;
+            const Shape sh = row_shape(a.T_max, nvec, a.k > 0);
+            C = sh.C; threads = sh.threads;
         }
     } else if (variant == 32) {
         threads = 32;

@@ -142,6 +142,19 @@ def test_every_launch_shape(B, variant, dtype):
         run(B, z, V, y, 20, 0.9, variant)
 
 
+@pytest.mark.parametrize("k", [0, 9])
+@pytest.mark.parametrize("T", [19, 37, 49, 61, 91, 149, 184, 300, 371, 500, 745, 1490])
+def test_many_row_shapes(B, T, k):
+    """Counts of rows for which the library picks every split of a row and size of a CTA; first, last and some rows between."""
+    for V, dtype in ((50003, "f32"), (17003, "bf16"), (6001, "f32")):
+        z, y = make(T, V, dtype, T + V)
+        z[1, 7:] = -math.inf
+        got = Fwd(B, z, V, y, k, 0.8).host()
+        pick = sorted({0, 1, 2, T // 3, T // 2, T - 2, T - 1})
+        zh, yh = z[pick, :V].double().cpu().numpy(), y.cpu().numpy()[pick]
+        check({n: v[pick] for n, v in got.items()}, scoring.token_logprobs(zh, yh, k, 0.8), zh, yh, 0.8, V, k)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V", [1000, 20003])
 @pytest.mark.parametrize("tau", [1e-6, 1e-3, 1e3, 1e6])
