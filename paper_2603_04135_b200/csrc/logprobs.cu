@@ -1078,17 +1078,45 @@ template <bool kBf16, int kThreads, int kTeams, int kUnroll> static int launch_b
 
 template <bool kBf16> static int run_bwd(BwdArgs a, cudaStream_t s) {
     const int nvec = a.V >> (kBf16 ? 3 : 2);
+    const long long sms = sm_count(), T = a.T_max;
     a.chunks = 1; a.chunk_vecs = nvec;
-    // a warp per row of up to 8 KB, its loads in rounds of four (20,011 x 1,021 f32: 27 us = 6.0 TB/s; rounds of two 30,
-    // of eight 28); a round does not go past the end of a very short one (100,000 x 128 bf16: 46 us in rounds of four)
-    if (nvec <= 32) return launch_bwd<kBf16, 32, 4, 1>(a, s);
-    if (nvec <= 64) return launch_bwd<kBf16, 32, 4, 2>(a, s);
-    if (nvec <= 512) return launch_bwd<kBf16, 32, 4, 4>(a, s);
-    // longer rows: a CTA of 128 threads per 1024 vectors, every thread's eight loads before its first store.  8,192 rows of
-    // 151,936 bf16 entries 739 us (6.7 TB/s read and written); 256 threads with four loads 830, 512 threads 988.
-    a.chunk_vecs = 1024;
-    a.chunks = (nvec + a.chunk_vecs - 1) / a.chunk_vecs;
-    return launch_bwd<kBf16, 128, 1, 8>(a, s);
+    // A warp per row of up to 5 KB, its loads in rounds of four (20,011 x 1,021 f32: 27 us = 6.0 TB/s; rounds of two 30, of
+    // eight 28); a round does not go past the end of a very short one (100,000 x 128 bf16: 46 us in rounds of four).  Fewer
+    // rows than the SMs have places for warps go the quicker way below (300 x 2,000 bf16: 3.0 us in warps, 2.3).
+    if (nvec <= 64 || (nvec <= 320 && T > (nvec <= 128 ? 3 : 8) * sms)) {
+        if (nvec <= 32) return launch_bwd<kBf16, 32, 4, 1>(a, s);
+        if (nvec <= 64) return launch_bwd<kBf16, 32, 4, 2>(a, s);
+        return launch_bwd<kBf16, 32, 4, 4>(a, s);
+    }
+    // Longer rows in chunks, a CTA each, every thread's loads before its first store.
+    auto cut = [&](int limit, int unit) {                          // equal chunks, of whole units
+        a.chunks = (nvec + limit - 1) / limit;
+        a.chunk_vecs = ((nvec + a.chunks - 1) / a.chunks + unit - 1) / unit * unit;
+        a.chunks = (nvec + a.chunk_vecs - 1) / a.chunk_vecs;
+    };
+    // Little work, where latency counts: 128 threads of four loads (1,000 x 4,096 bf16 4.7 us, 7.6 with a warp per row; 64 x
+    // 75,968 f32 8.2, 9.0 with the next), then for bf16, which has twice the exponentials in a load, 64 threads of eight (40 x
+    // 151,936: 5.4 us, 5.8 with the one before).
+    if (T * nvec < (nvec < 1024 || kBf16 ? 3 : 9) * sms * 1024) {
+        cut(512, 64);
+        return launch_bwd<kBf16, 128, 1, 4>(a, s);
+    }
+    if (kBf16 && T * nvec < 9 * sms * 1024) {
+        a.chunk_vecs = 512;
+        a.chunks = (nvec + 511) / 512;
+        return launch_bwd<kBf16, 64, 1, 8>(a, s);
+    }
+    // Much: bf16 in 1024 vectors by 128 threads of eight loads, where that leaves no half-empty last chunk (8,192 x 151,936
+    // 739 us, 6.7 TB/s read and written; 256 threads of four loads 830, 512 threads 988; 16,000 x 15,200 155, 162 with the next);
+    if (kBf16 && nvec > 512 && (nvec >= 8192 || nvec % 1024 == 0 || nvec % 1024 >= 600)) {
+        a.chunk_vecs = 1024;
+        a.chunks = (nvec + 1023) / 1024;
+        return launch_bwd<kBf16, 128, 1, 8>(a, s);
+    }
+    // otherwise equal chunks of up to 512 by 64 threads of eight (16,000 x 10,000 bf16 107 us, 118 with the one before; 4,000 x
+    // 75,968 f32 366, 377).
+    cut(512, 1);
+    return launch_bwd<kBf16, 64, 1, 8>(a, s);
 }
 
 // Checks that both calls make; 0 or the error.

@@ -374,6 +374,26 @@ def test_backward(B, T, V, tau, terms, dtype):
     assert torch.equal(same[:, :V], out[:, :V]) and torch.equal(z[:, V:], pad)
 
 
+@pytest.mark.parametrize("T, V, dtype", [(100, 1000, "bf16"), (2000, 1000, "bf16"), (3000, 1203, "f32"), (1500, 2603, "bf16"), (1500, 5003, "bf16"), (1500, 2501, "f32"),
+                                         (1200, 9603, "bf16"), (700, 17003, "bf16"), (60, 200003, "bf16"), (300, 20001, "f32")])
+def test_backward_many_row_shapes(B, T, V, dtype):
+    """Counts of rows for which the library takes every cut of a row and size of a CTA; sampled rows, masked ones and in place too."""
+    z, y = make(T, V, dtype, T + V)
+    z[2, 5:] = -math.inf
+    z[3] = -math.inf                                                       # an empty row
+    y[2], y[0], y[T - 1] = 3, V - 1, V // 2
+    a, b = torch.randn(T, device="cuda"), torch.randn(T, device="cuda")
+    pick = sorted({0, 1, 2, 3, T // 3, T // 2, T - 2, T - 1})
+    zh, yh, ah, bh = (v.cpu().numpy()[pick] for v in (z[:, :V].double(), y, a.double(), b.double()))
+    want = scoring.token_logprobs_backward(zh, yh, ah, bh, 0.8)
+    out = backward(B, z, V, y, a, b, 0.8)
+    check_grad(out[:, :V].double().cpu().numpy()[pick], want, zh, yh, ah, bh, 0.8, dtype, V)
+    assert bool((out[:, V:] == 9.0).all()) and bool((out[3, :V] == 0).all())
+    pad = z[:, V:].clone()
+    same = backward(B, z, V, y, a, b, 0.8, in_place=True)
+    assert torch.equal(same[:, :V], out[:, :V]) and torch.equal(z[:, V:], pad)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V", [9, 1000, 8200])
 def test_backward_special_rows(B, V, dtype):
