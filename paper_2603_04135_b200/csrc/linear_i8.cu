@@ -497,20 +497,18 @@ template <int kPer> __device__ __forceinline__ void codes_of(const float (&f)[kP
     }
 }
 
-constexpr int kQuantThreads = 128;
-
-// One CTA per row: the maximum, then the codes.  Rows of up to kVecs vectors per thread stay in registers in between; longer
-// ones are read a second time (out of L2).
-template <bool kBf16, int kVecs>
-__global__ void __launch_bounds__(kQuantThreads)
+// A team of kThreads per row: the maximum, then the codes.  Rows of up to kVecs vectors per thread stay in registers in between;
+// longer ones are read a second time (out of L2).
+template <bool kBf16, int kThreads, int kVecs>
+__global__ void __launch_bounds__(kThreads < 128 ? 128 : kThreads)
 quantize_rows_kernel(const QuantArgs a) {
-    constexpr int kPer = Elems<kBf16>::kPerVec;
-    __shared__ float red[kQuantThreads / 32];
+    constexpr int kPer = Elems<kBf16>::kPerVec, kTeams = kThreads < 128 ? 128 / kThreads : 1;
+    __shared__ float red[kThreads / 32];
     enter_kernel();
-    const long long t = blockIdx.x;
+    const int tid = kTeams == 1 ? threadIdx.x : threadIdx.x % kThreads;
+    const long long t = kTeams == 1 ? (long long)blockIdx.x : (long long)blockIdx.x * kTeams + threadIdx.x / kThreads;
     const long long T = a.n_rows_dev ? min((long long)*a.n_rows_dev, a.rows_max) : a.rows_max;
     if (t >= T) return;
-    const int tid = threadIdx.x;
     const char* row = a.x + t * a.x_row_bytes;
     const uint4* rv = reinterpret_cast<const uint4*>(row);
     int8_t* q = a.q + t * a.q_stride;
@@ -524,18 +522,30 @@ quantize_rows_kernel(const QuantArgs a) {
         for (int j = 0; j < kPer; ++j) amax = max_nan(amax, fabsf(f[j]));
     };
 #pragma unroll
-    for (int u = 0; u < kVecs; ++u) v[u] = u * kQuantThreads + tid < nvec ? rv[u * kQuantThreads + tid] : make_uint4(0u, 0u, 0u, 0u);
+    for (int u = 0; u < kVecs; ++u) v[u] = u * kThreads + tid < nvec ? rv[u * kThreads + tid] : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
     for (int u = 0; u < kVecs; ++u) look(v[u]);
-    for (int i = kVecs * kQuantThreads + tid; i < nvec; i += kQuantThreads) look(rv[i]);
+    // the rest in rounds of kVecs loads; zeros do not move a maximum of magnitudes
+    auto rest = [&](auto use) {
+        for (int i = kVecs * kThreads + tid; i < nvec; i += kVecs * kThreads) {
+            uint4 x[kVecs];
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u) x[u] = i + u * kThreads < nvec ? rv[i + u * kThreads] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u) use(x[u], i + u * kThreads);
+        }
+    };
+    rest([&](const uint4& x, int) { look(x); });
     const float xt = tail < a.K ? Elems<kBf16>::load1(row, tail) : 0.0f;
     amax = max_nan(amax, fabsf(xt));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    if ((tid & 31) == 0) red[tid >> 5] = amax;
-    __syncthreads();
+    if constexpr (kThreads > 32) {
+        if ((tid & 31) == 0) red[tid >> 5] = amax;
+        __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kQuantThreads / 32; ++w) amax = max_nan(amax, red[w]);
+        for (int w = 0; w < kThreads / 32; ++w) amax = max_nan(amax, red[w]);
+    }
     const bool fine = amax < INFINITY;
     const float s = fine ? __fmul_rn(amax, 1.0f / 127.0f) : __int_as_float(0x7fffffff);
     if (tid == 0) a.scale[t] = s;
@@ -552,8 +562,8 @@ quantize_rows_kernel(const QuantArgs a) {
     };
 #pragma unroll
     for (int u = 0; u < kVecs; ++u)
-        if (u * kQuantThreads + tid < nvec) put(v[u], u * kQuantThreads + tid);
-    for (int i = kVecs * kQuantThreads + tid; i < nvec; i += kQuantThreads) put(rv[i], i);
+        if (u * kThreads + tid < nvec) put(v[u], u * kThreads + tid);
+    rest([&](const uint4& x, int i) { if (i < nvec) put(x, i); });
     if (tail < a.K) q[tail] = live ? (int8_t)code_of(xt, s) : (int8_t)0;
 }
 
@@ -571,6 +581,38 @@ static int make_map(CUtensorMap* map, const void* base, long long rows, int K, l
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return fail(DPPO_ERR_CUDA, "linear_i8: cuTensorMapEncodeTiled failed with %d", (int)r);
     return DPPO_OK;
+}
+
+template <bool kBf16, int kThreads, int kVecs> static int launch_quantize(const QuantArgs& a, cudaStream_t s) {
+    constexpr int kCta = kThreads < 128 ? 128 : kThreads, kTeams = kCta / kThreads;
+    return launch_after("quantize_rows_i8 launch", quantize_rows_kernel<kBf16, kThreads, kVecs>, (a.rows_max + kTeams - 1) / kTeams, kCta, 0, s, 1, a);
+}
+
+// Which team per row, by its length in vectors: the row in registers where that takes no more than eight loads a thread, small
+// teams where the rows are many (the reduction and the launch of each CTA count), large ones where they are few and a row's
+// latency counts.  bf16: 16,000 x 1,024 14 us with warps, 19 with 128 threads of one load, 26 of four; 64 x 4,096 2.3 with 512
+// threads, 3.1 with 128, 16,000 of them 81 and 44; 1,000 x 16,384 17 with 512, 22 with 128.  f32, whose loads bring half the
+// work, in eight: 16,000 x 4,096 48 us (6.8 TB/s), 65 in four with a second read; 16,000 x 8,192 93 with 256 threads, 135 with
+// 128 of four.  Longer rows are read twice whatever the team (1,000 x 28,672 bf16: 28 us in rounds of two, 31 of four).
+template <bool kBf16> static int run_quantize(const QuantArgs& a, cudaStream_t s) {
+    const int nvec = a.K / Elems<kBf16>::kPerVec;
+    const long long M = a.rows_max, sms = sm_count();
+    if (nvec <= 64 && M >= 4 * sms) return launch_quantize<kBf16, 32, 4>(a, s);
+    if (nvec <= 128 && M >= 13 * sms) return launch_quantize<kBf16, 32, 4>(a, s);
+    if (nvec <= 128) return launch_quantize<kBf16, 128, 1>(a, s);
+    if constexpr (kBf16) {
+        if (nvec <= 256) return launch_quantize<kBf16, 128, 2>(a, s);
+        if (nvec <= 512) return M <= 2 * sms ? launch_quantize<kBf16, 512, 1>(a, s) : launch_quantize<kBf16, 128, 4>(a, s);
+        if (nvec <= 1024) return M <= 4 * sms ? launch_quantize<kBf16, 512, 2>(a, s) : launch_quantize<kBf16, 256, 4>(a, s);
+        if (nvec <= 2048) return M <= 8 * sms ? launch_quantize<kBf16, 512, 4>(a, s) : launch_quantize<kBf16, 256, 4>(a, s);
+        return launch_quantize<kBf16, 512, 2>(a, s);
+    } else {
+        if (nvec <= 256) return M >= 13 * sms ? launch_quantize<kBf16, 32, 8>(a, s) : launch_quantize<kBf16, 128, 2>(a, s);
+        if (nvec <= 512) return launch_quantize<kBf16, 128, 4>(a, s);
+        if (nvec <= 1024) return M <= 2 * sms ? launch_quantize<kBf16, 512, 2>(a, s) : launch_quantize<kBf16, 128, 8>(a, s);
+        if (nvec <= 2048) return launch_quantize<kBf16, 256, 8>(a, s);
+        return launch_quantize<kBf16, 512, 8>(a, s);
+    }
 }
 
 // Raises a kernel's shared-memory limit once per device.
@@ -667,8 +709,7 @@ extern "C" int dppo_quantize_rows_i8(const dppo_quantize_params* p, const void* 
     if (((uintptr_t)x & 15) || ((uintptr_t)q & 15) || x_row_bytes % 16 != 0 || p->q_stride % 16 != 0)
         return fail(DPPO_ERR_MISALIGNED, "quantize_rows_i8: x / q base and row strides must be multiples of 16 bytes");
     const i8::QuantArgs a = {(const char*)x, q, scale, n_rows_dev, p->rows_max, x_row_bytes, p->q_stride, p->K};
-    auto kernel = p->dtype == DPPO_BF16 ? i8::quantize_rows_kernel<true, 4> : i8::quantize_rows_kernel<false, 8>;
-    return launch_after("quantize_rows_i8 launch", kernel, p->rows_max, i8::kQuantThreads, 0, (cudaStream_t)stream, 1, a);
+    return p->dtype == DPPO_BF16 ? i8::run_quantize<true>(a, (cudaStream_t)stream) : i8::run_quantize<false>(a, (cudaStream_t)stream);
 }
 
 extern "C" int dppo_linear_i8(const dppo_linear_i8_params* p, const int8_t* x, const float* x_scale, const int8_t* w,

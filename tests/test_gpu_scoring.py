@@ -567,7 +567,8 @@ def test_linear_i8_bounded_waits(B, variant):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("M, K", [(1, 1), (3, 7), (5, 8), (2, 129), (9, 2560), (4, 4097), (2, 30001), (300, 64), (5000, 1000), (2, 4096), (6, 4104)])
+@pytest.mark.parametrize("M, K", [(1, 1), (3, 7), (5, 8), (2, 129), (9, 2560), (4, 4097), (2, 30001), (300, 64), (5000, 1000), (2, 4096), (6, 4104),
+                                  (700, 500), (2001, 1003), (1000, 2005), (300, 4001), (20, 4003), (700, 7001), (701, 8200), (1300, 16003), (300, 12001), (40, 40003)])
 def test_quantize_rows(B, M, K, dtype):
     ldx, ldq = pad16(K, 2 if dtype == "bf16" else 4), (K + 15) // 16 * 16 + 16
     x = torch.empty(M, ldx, device="cuda").normal_(0, 3).to(DT[dtype])
