@@ -627,33 +627,35 @@ template <class Kernel> static int raise_smem(Kernel kernel, size_t bytes, bool 
 }
 
 // ---- which kernel, which tile ----
-// Both kernels' times in microseconds, from sweeps over N = 64 to 151,936, K = 64 to 9,728 and 1 to 1,003 tokens: the choice
-// they give was the faster one or within 5 % of it at nine shapes of ten, and 20 % off at worst.
+// Both kernels' times in microseconds, fitted to 420 random shapes of 1 to 3,000 tokens, N = 100 to 160,000 and K = 64 to
+// 17,000: over those the choice costs 0.5 % against the faster kernel of each, 40 % at worst (52 tokens x 21,152 x 6,652).
 //
-// Pair kernel: whole waves of tiles; a 128-code slab of a tile costs about (256 + tokens) ns: 256 tokens keep the tensor cores
-// and the operand fetches equally busy, fewer are bound by fetching the weights' 16 KB.  The token tile is the one with the
-// least time (1,003 x 5,003 x 2,563: 140 tiles of 160 in two waves instead of 80 of 256 in two; 27 -> 23 us).
+// Pair kernel: whole waves of tiles.  A 128-code slab of a tile takes 300 ns, bound by fetching the weights' 16 KB, until the
+// tensor cores take longer (256 tokens: 380); a wave ends with an epilogue.  The token tile is the one with the least time
+// (1,003 x 5,003 x 2,563: 140 tiles of 160 in two waves instead of 80 of 256 in two; 27 -> 23 us).
 static double pair_time(long long M, int N, int n_ksteps, int* tile) {
     const long long n_m2 = (N + 255) / 256, pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
     double best = 0.0;
     for (int tn = kTileN; tn >= 64; tn -= 32) {
         const long long tiles = n_m2 * ((M + tn - 1) / tn), waves = (tiles + pairs - 1) / pairs;
-        const double t = 4.2 + 1e-3 * (double)waves * n_ksteps * (256 + tn);
+        const double slab = tn * 0.0015 > 0.3 ? tn * 0.0015 : 0.3;
+        const double t = 2.9 + (double)waves * (n_ksteps * slab + 0.3 + 0.011 * tn);
         if (best == 0.0 || t < best) { best = t; *tile = tn; }
     }
     return best;
 }
-// The other: the contraction is split while two CTAs per SM have room and each keeps two slabs; the join costs a few
-// microseconds (64 tokens: 2), more than it gains only where there are few slabs.
+// The other: the contraction is split while two CTAs per SM have room and each keeps two slabs.  An SM fetches 80 KB/us, each
+// CTA starts and ends (3 us and more with its tokens), and a join costs a few microseconds (64 tokens: 1.6).
 static double small_time(long long M, int N, int n_ksteps, int* tokens, int* split) {
     const int nb = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
     const long long tiles = (long long)((N + kTileM - 1) / kTileM) * ((M + nb - 1) / nb), sms = sm_count();
     int sp = 1;
     while (sp < 8 && tiles * sp * 2 <= 2 * sms && n_ksteps >= 4 * sp) sp *= 2;
     *tokens = nb; *split = sp;
-    const double waves = (double)((tiles * sp + 2 * sms - 1) / (2 * sms)), load = (double)(tiles * sp) / (double)sms;
-    const double shared = waves > 1.0 ? 1.5 : load * 0.75 > 1.0 ? load * 0.75 : 1.0;          // two CTAs on an SM slow each other
-    return 3.6 + waves * ((n_ksteps + sp - 1) / sp) * (0.2 + 0.0024 * nb) * shared + (sp > 1 ? 0.6 + 0.03 * nb : 0.0);
+    const long long ctas = tiles * sp;
+    const double waves = ctas <= 2 * sms ? 1.0 : (double)ctas / (double)(2 * sms) + 0.4;
+    const double slab = (ctas > sms ? 2 : 1) * (16384 + nb * 128) / 80e3;
+    return waves * (((n_ksteps + sp - 1) / sp) * slab + 3.2 + 0.007 * nb) + (sp > 1 ? 0.6 + 0.015 * nb : 0.0);
 }
 
 template <bool kBf16> static int launch_pair(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
