@@ -398,8 +398,8 @@ int dppo_token_logprobs_backward(const dppo_logprob_params* p, const void* logit
  * (ties to even); s = 0 gives q = 0.  A row with a NaN or an infinity gets s = NaN, q = 0, so that products with it are NaN.
  */
 typedef struct {
-    int64_t rows_max;       /* rows of x                                                             */
-    int32_t K;              /* columns                                                               */
+    int64_t rows_max;       /* rows of x (below 2^31)                                                */
+    int32_t K;              /* columns, up to 2^30                                                   */
     int32_t dtype;          /* dppo_dtype of x                                                       */
     int64_t x_stride;       /* elements between rows of x (>= K; bytes a multiple of 16)             */
     int64_t q_stride;       /* bytes between rows of q (>= K; a multiple of 16)                      */

@@ -705,6 +705,7 @@ extern "C" int dppo_quantize_rows_i8(const dppo_quantize_params* p, const void* 
     if (p->x_stride < p->K || p->q_stride < p->K)
         return fail(DPPO_ERR_BAD_SHAPE, "quantize_rows_i8: strides %lld, %lld < K %d", (long long)p->x_stride, (long long)p->q_stride, p->K);
     if (p->rows_max >= ((int64_t)1 << 31)) return fail(DPPO_ERR_BAD_SHAPE, "quantize_rows_i8: rows_max must be below 2^31");
+    if (p->K > (1 << 30)) return fail(DPPO_ERR_BAD_SHAPE, "quantize_rows_i8: K=%d, the limit is 2^30", p->K);
     const long long x_row_bytes = (long long)p->x_stride * (p->dtype == DPPO_BF16 ? 2 : 4);
     if (p->rows_max == 0) return DPPO_OK;
     if (!x || !q || !scale) return fail(DPPO_ERR_INVALID_ARG, "quantize_rows_i8: NULL array");

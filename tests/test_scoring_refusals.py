@@ -68,6 +68,7 @@ def test_quantize_params():
     assert code(q, B.QuantizeParams(4, 8, 1, 8, 16), P, P + 1, P) == B.ERR_MISALIGNED
     assert code(q, B.QuantizeParams(4, 8, 1, 8, 16), None, P, P) == B.ERR_INVALID_ARG
     assert code(q, B.QuantizeParams(1 << 31, 8, 1, 8, 16), P, P, P) == B.ERR_BAD_SHAPE
+    assert code(q, B.QuantizeParams(4, (1 << 30) + 8, 1, (1 << 30) + 8, (1 << 30) + 16), P, P, P) == B.ERR_BAD_SHAPE    # column indices pass 31 bits
     q(B.QuantizeParams(0, 8, 1, 8, 16), None, None, None)
 
 
