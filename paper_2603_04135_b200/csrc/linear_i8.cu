@@ -657,18 +657,28 @@ static double pair_time(long long M, int N, int n_ksteps, int* tile) {
     }
     return best;
 }
-// The other: the contraction is split while two CTAs per SM have room and each keeps two slabs.  An SM fetches 80 KB/us, each
-// CTA starts and ends (3 us and more with its tokens), and a join costs a few microseconds (64 tokens: 1.6).
+// The other, with the split of the contraction that takes least (400 random shapes: 1 % from the best on average; splitting
+// until there are two CTAs per SM was 5 %: 64 x 4,096 x 4,096 in four 7.8 us, in eight 9.0).  A slab costs its latency, or,
+// where two CTAs share an SM, what the SM can fetch (75 KB/us); each CTA starts and ends, later with a second one beside it;
+// a join grows with the CTAs that take part and with the tokens.
 static double small_time(long long M, int N, int n_ksteps, int* tokens, int* split) {
     const int nb = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
     const long long tiles = (long long)((N + kTileM - 1) / kTileM) * ((M + nb - 1) / nb), sms = sm_count();
-    int sp = 1;
-    while (sp < 8 && tiles * sp * 2 <= 2 * sms && n_ksteps >= 4 * sp) sp *= 2;
-    *tokens = nb; *split = sp;
-    const long long ctas = tiles * sp;
-    const double waves = ctas <= 2 * sms ? 1.0 : (double)ctas / (double)(2 * sms) + 0.4;
-    const double slab = (ctas > sms ? 2 : 1) * (16384 + nb * 128) / 80e3;
-    return waves * (((n_ksteps + sp - 1) / sp) * slab + 3.2 + 0.007 * nb) + (sp > 1 ? 0.6 + 0.015 * nb : 0.0);
+    const double latency = 0.25 + 0.00075 * nb, fetch = 2 * (16384 + nb * 128) / 75e3;
+    double best = 0.0;
+    for (int sp = 1, i = 0; sp <= 8; sp *= 2, ++i) {
+        constexpr double kJoin[4] = {0.0, 0.3, 0.4, 0.9};
+        const long long ctas = tiles * sp;
+        if (sp > 1 && (ctas > 2 * sms || n_ksteps < sp)) break;
+        const bool two = ctas > sms;
+        const double waves = ctas <= 2 * sms ? 1.0 : (double)ctas / (double)(2 * sms) + 0.4;
+        const double slab = two && fetch > latency ? fetch : latency;
+        const double t = waves * (((n_ksteps + sp - 1) / sp) * slab + 3.0 + 0.0075 * nb) + (two ? 1.8 : 0.0)
+                       + (sp > 1 ? kJoin[i] + 0.017 * nb : 0.0);
+        if (best == 0.0 || t < best) { best = t; *split = sp; }
+    }
+    *tokens = nb;
+    return best;
 }
 
 template <bool kBf16> static int launch_pair(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
