@@ -156,6 +156,14 @@ __device__ __forceinline__ void acc_grow(Acc& a, float vmax, float c) {
     a.Q = mul2(fma2(pair_of(D, D), a.S, a.Q), pair_of(f, f));
     a.S = mul2(a.S, pair_of(f, f));
 }
+// The lanes of a warp together, so that they keep one maximum: a larger one then turns up a few times per row, not in nearly
+// every round in some lane (a thread's r-th round holds its largest entry so far with probability 1 / r), and lanes that have
+// seen nothing but masked entries have a frame all the same.
+__device__ __forceinline__ void acc_grow_warp(Acc& a, float vmax, float c) {
+    if (!(vmax < INFINITY)) { a.bad = 1; vmax = -INFINITY; }
+    const float m = warp_max_f32(vmax);
+    if (m > a.m) acc_grow(a, m, c);
+}
 __device__ __forceinline__ void acc_add(Acc& a, f32x2 y) {
     float y0, y1;
     unpair(y, y0, y1);
@@ -171,8 +179,8 @@ __device__ __forceinline__ void acc_add_far(Acc& a, f32x2 y) {     // y may be -
 __device__ __forceinline__ void acc_pair_slow(Acc& a, float z0, float z1, float c) {
     acc_add_far(a, mul2(add2(pair_of(z0, z1), pair_of(-a.m, -a.m)), pair_of(c, c)));
 }
-// kN vectors in the frame of a maximum that none of them exceeds.
-template <bool kBf16, int kN> __device__ __forceinline__ void acc_sum(Acc& a, const uint4 (&q)[kN], float c) {
+// kN vectors in the frame of a maximum that none of them exceeds.  some: one of them is above -inf.
+template <bool kBf16, int kN> __device__ __forceinline__ void acc_sum(Acc& a, const uint4 (&q)[kN], float c, bool some) {
     if (a.quick) {                                                 // one test per kN vectors: what follows is a straight line
         const f32x2 c2 = pair_of(c, c), nr2 = pair_of(a.nr, a.nr);
 #pragma unroll
@@ -190,7 +198,7 @@ template <bool kBf16, int kN> __device__ __forceinline__ void acc_sum(Acc& a, co
                 for (int i = 0; i < 4; i += 2) acc_add_far(a, fma2(pair_of(__uint_as_float(w[i]), __uint_as_float(w[i + 1])), c2, nr2));
             }
         }
-    } else {
+    } else if (some) {
 #pragma unroll 1
         for (int u = 0; u < kN; ++u) {
             uint4 v = q[0];                                        // selects: q stays in registers
@@ -203,10 +211,11 @@ template <bool kBf16, int kN> __device__ __forceinline__ void acc_sum(Acc& a, co
         }
     }
 }
-// kN vectors; a larger maximum (or a NaN) is rare after the first few of a row.  Returns their largest entry as bf16, rounded
-// up (NaN where there is one).
-template <bool kBf16, int kN> __device__ __forceinline__ __nv_bfloat16 acc_vecs(Acc& a, const uint4 (&q)[kN], float c) {
+// kN vectors, by a whole warp; a larger maximum (or a NaN) is rare after the first few of a row.  Returns their largest entry
+// as bf16, rounded up (NaN where there is one); own: the thread's largest so far.
+template <bool kBf16, int kN> __device__ __forceinline__ __nv_bfloat16 acc_vecs(Acc& a, const uint4 (&q)[kN], float c, float& own) {
     __nv_bfloat16 top;
+    float vmax;
     if constexpr (kBf16) {
         __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162*>(&q[0].x);
 #pragma unroll
@@ -216,15 +225,17 @@ template <bool kBf16, int kN> __device__ __forceinline__ __nv_bfloat16 acc_vecs(
             for (int i = u == 0 ? 1 : 0; i < 4; ++i) x = __hmax2_nan(x, *reinterpret_cast<const __nv_bfloat162*>(&w[i]));
         }
         top = __hmax_nan(__low2bfloat16(x), __high2bfloat16(x));
-        if (!__hble2(x, *reinterpret_cast<const __nv_bfloat162*>(&a.m2))) acc_grow(a, __bfloat162float(top), c);
+        vmax = __bfloat162float(top);
+        if (__any_sync(0xffffffffu, !__hble2(x, *reinterpret_cast<const __nv_bfloat162*>(&a.m2)))) acc_grow_warp(a, vmax, c);
     } else {
-        float vmax = vec_max<false>(q[0]);
+        vmax = vec_max<false>(q[0]);
 #pragma unroll
         for (int u = 1; u < kN; ++u) vmax = max_nan(vmax, vec_max<false>(q[u]));
         top = bf16_up(vmax);
-        if (!(vmax <= a.m)) acc_grow(a, vmax, c);
+        if (__any_sync(0xffffffffu, !(vmax <= a.m))) acc_grow_warp(a, vmax, c);
     }
-    acc_sum<kBf16, kN>(a, q, c);
+    own = fmaxf(own, vmax);
+    acc_sum<kBf16, kN>(a, q, c, vmax > -INFINITY);
     return top;
 }
 
@@ -586,7 +597,7 @@ token_logprobs_warp_kernel(const Args a, int run) {
             p.m = fmaxf(warp_max_f32(mx), kLowest);
             Acc acc;
             acc_init(acc, p.m, a.c);
-            acc_sum<kBf16, kVecs>(acc, q, a.c);
+            acc_sum<kBf16, kVecs>(acc, q, a.c, mx > -INFINITY);
             Part own = acc_part(acc);
             if (zt > -INFINITY) {
                 const float y = fmaxf((zt - p.m) * a.c, kFar), e = ex2(y);
@@ -596,6 +607,7 @@ token_logprobs_warp_kernel(const Args a, int run) {
         } else {
             Acc acc;
             acc_init(acc, kLowest, a.c);
+            mx = zt;
 #pragma unroll 1
             for (int it = 0; it < n_rounds; ++it) {
                 const int i = it * (kRound * 32) + lane;
@@ -607,7 +619,7 @@ token_logprobs_warp_kernel(const Args a, int run) {
                     for (int u = 0; u < kRound; ++u)
                         q[u] = i + u * 32 < nvec ? load_vec(row + (size_t)(i + u * 32) * 16) : make_uint4(kNone, kNone, kNone, kNone);
                 }
-                __nv_bfloat16 top = acc_vecs<kBf16, kRound>(acc, q, a.c);
+                __nv_bfloat16 top = acc_vecs<kBf16, kRound>(acc, q, a.c, mx);
                 if (a.k > 0) {
                     __nv_bfloat16* best = &ws.best[it >> shift][lane];
                     if (it & ((1 << shift) - 1)) top = __hmax(top, *best);
@@ -615,9 +627,7 @@ token_logprobs_warp_kernel(const Args a, int run) {
                 }
             }
             acc_one(acc, zt, a.c);
-            p = acc_part(acc);
-            mx = p.S > 0.0f ? p.m : -INFINITY;
-            p = warp_join(p, a.c);
+            p = warp_join(acc_part(acc), a.c);
         }
 
         int n = 0;
@@ -733,6 +743,7 @@ token_logprobs_kernel(const Args a) {
 
     Acc acc;
     acc_init(acc, kLowest, a.c);
+    float own = -INFINITY;                                         // the thread's largest entry
     constexpr uint32_t kNone = kBf16 ? 0xff80ff80u : 0xff800000u;  // -inf
     const int n_rounds = (sp.v1 - sp.v0 + kRound * kThreads - 1) / (kRound * kThreads);
     int shift = 0;
@@ -748,18 +759,20 @@ token_logprobs_kernel(const Args a) {
             for (int u = 0; u < kRound; ++u)
                 q[u] = i + u * kThreads < sp.v1 ? load_vec(row + (size_t)(i + u * kThreads) * 16) : make_uint4(kNone, kNone, kNone, kNone);
         }
-        __nv_bfloat16 top = acc_vecs<kBf16, kRound>(acc, q, a.c);
+        __nv_bfloat16 top = acc_vecs<kBf16, kRound>(acc, q, a.c, own);
         if (a.k > 0) {
             __nv_bfloat16* best = &sh.best[it >> shift][tid];
             if (it & ((1 << shift) - 1)) top = __hmax(top, *best);
             *best = top;
         }
     }
-    if (sp.tail0 + tid < sp.tail1) acc_one(acc, Elems<kBf16>::load1(row, sp.tail0 + tid), a.c);
-
-    Part p = acc_part(acc);
-    if (a.k > 0) sh.tmax[tid] = p.S > 0.0f ? p.m : -INFINITY;      // nothing but -inf seen: not a maximum
-    p = warp_join(p, a.c);
+    if (sp.tail0 + tid < sp.tail1) {
+        const float z = Elems<kBf16>::load1(row, sp.tail0 + tid);
+        acc_one(acc, z, a.c);
+        own = fmaxf(own, z);
+    }
+    if (a.k > 0) sh.tmax[tid] = own;
+    Part p = warp_join(acc_part(acc), a.c);
     if (lane == 0) sh.part[warp] = p;
     __syncthreads();
     if (warp == 0) {                                               // two warps at a time: the row's sums, the threshold
