@@ -142,6 +142,30 @@ def test_every_launch_shape(B, variant, dtype):
         run(B, z, V, y, 20, 0.9, variant)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V, variant", [(8203, 0), (8203, 32), (20003, 10128), (20003, 10512), (151936, 10256), (151936, 0), (151937, 40256)])
+def test_maxima_that_move(B, V, variant, dtype):
+    """Rows whose maximum grows all along, or that most threads see nothing of: the lanes of a warp share their maximum."""
+    lowest = float(torch.finfo(DT[dtype]).min)
+    g = torch.Generator().manual_seed(V)
+    z = torch.full((9, pad16(V, 2 if dtype == "bf16" else 4)), 7.0)
+    z[0, :V] = torch.linspace(-30, 30, V)
+    z[1, :V] = torch.linspace(30, -30, V)
+    z[2, :V] = -math.inf
+    z[2, V - 3:] = torch.tensor([1.0, 2.0, -5.0] + [0.0] * (z.shape[1] - V))
+    z[3, :V] = torch.randn(V, generator=g).masked_fill(torch.rand(V, generator=g) < 0.99, -math.inf)
+    z[4, :V] = torch.full((V,), -math.inf).masked_fill(torch.rand(V, generator=g) < 0.01, lowest)
+    z[5, :V] = torch.full((V,), lowest).masked_fill(torch.rand(V, generator=g) < 0.5, -math.inf)
+    z[5, V // 2] = 3.0
+    z[6, :V] = torch.linspace(-400, 400, V)[torch.randperm(V, generator=g)]
+    z[7, :V] = torch.where(torch.arange(V) // 8 % 32 == 5, torch.linspace(-9, 9, V), torch.tensor(-math.inf))     # one lane of each warp
+    z[8, :V] = lowest
+    z[8, V // 3] = -math.inf
+    z = z.to(DT[dtype]).cuda()
+    y = torch.tensor([5, V - 1, V - 2, 0, 1, V // 2, 7, 40, V // 3], dtype=torch.int32, device="cuda")
+    run(B, z, V, y, 7, 0.9, variant)
+
+
 @pytest.mark.parametrize("k", [0, 9])
 @pytest.mark.parametrize("T", [19, 37, 49, 61, 91, 149, 184, 300, 371, 500, 745, 1490])
 def test_many_row_shapes(B, T, k):
