@@ -869,7 +869,7 @@ struct BwdArgs {
 struct BwdRow {
     float nm, l2n, nA, nX;               // -m, -l log2(e), -A, -X
     float far;                           // x is held at or above this: p is 0 there
-    uint32_t low2;                       // bf16 pair: m + far, or -inf where that is beyond the type
+    uint32_t low2;                       // bf16 pair: m + far, rounded down
 };
 
 __device__ __forceinline__ f32x2 bwd_pair(float z0, float z1, const BwdRow& r, float c, bool lift) {
@@ -910,8 +910,10 @@ token_logprobs_bwd_kernel(const BwdArgs a) {
     r.nX = -gb * a.inv_tau;
     r.far = kFar / a.c;
     r.low2 = bf16_pair(__float2bfloat16_rd(st.x + r.far));
-    // bf16 entries are lifted by a packed maximum before they are unpacked, unless the bound is beyond the type
-    const bool lift = !kBf16 || !(fabsf(st.x) <= 1e37f);
+    // bf16 entries are lifted by a packed maximum before they are unpacked, where m + far lies well below m (the forward's quick
+    // frame: |far / m| >= 2^-9.1).  Of a maximum further from zero, far rounds away, low2 would be m itself and every entry, masked
+    // ones too, would count as the maximum: there (and for f32) the differences come first and are held at far.
+    const bool lift = !kBf16 || !(fabsf(st.x * a.c) <= 1048576.0f && fabsf(st.x) <= 1e37f);
 
     const char* row = a.logits + t * a.row_bytes;
     char* out = a.dlogits + t * a.row_bytes;

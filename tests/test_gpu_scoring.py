@@ -877,3 +877,36 @@ def test_calls_from_two_threads(B):
     for o in got.values():
         for n in want:
             assert np.array_equal(o[n].view(np.int32), want[n].view(np.int32)), n
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [9, 1000, 8200])
+@pytest.mark.parametrize("m, tau", [(-1e30, 1.0), (-1e12, 1.0), (1e11, 1.0), (1e36, 1.0), (7e5, 1.0), (7.5e5, 1.0), (-7.5e5, 1.0), (-1e9, 0.01),
+                                    (1e8, 1e-3), (33024.0, 1e-6), (4e4, 1e-6), (-1e11, 1e6)])
+def test_backward_of_a_maximum_far_from_zero(B, m, tau, V, dtype):
+    """Rows whose maximum is large against the temperature: entries below it, masked ones too, keep their own probability
+    (0 here: `lower` is more than 104 tau below m)."""
+    m = float(torch.tensor(m).to(DT[dtype]))
+    g = torch.Generator().manual_seed(V)
+    kind = torch.randint(0, 4, (5, V), generator=g)
+    lower = float(torch.tensor(m - abs(m) * 2.0 ** -6).to(DT[dtype]))
+    rows = torch.where(kind == 0, m, torch.where(kind == 1, lower, torch.tensor(-math.inf)))
+    rows[0] = m
+    rows[0, V // 2:] = -math.inf
+    rows[1] = -math.inf
+    rows[1, V - 1] = m                                                     # one token
+    rows[2] = lower
+    rows[2, V // 3] = m
+    rows[3, 0], rows[4, 1] = m, m
+    rows[4, V - 2] = lower                                                 # the given token is not the most likely one
+    z = torch.zeros(5, pad16(V, 2 if dtype == "bf16" else 4), dtype=DT[dtype], device="cuda")
+    z[:, :V] = rows.to(DT[dtype])
+    yh = np.array([0, V - 1, V // 3, 0, V - 2])
+    a, b = torch.randn(5, device="cuda"), torch.randn(5, device="cuda")
+    zh = z[:, :V].double().cpu().numpy()
+    ah, bh = a.double().cpu().numpy(), b.double().cpu().numpy()
+    want = scoring.token_logprobs_backward(zh, yh, ah, bh, tau)
+    out = backward(B, z, V, torch.tensor(yh, dtype=torch.int32, device="cuda"), a, b, tau)
+    got = out[:, :V].double().cpu().numpy()
+    assert (got[zh == -np.inf] == 0).all()
+    check_grad(got, want, zh, yh, ah, bh, tau, dtype, V)
