@@ -160,19 +160,38 @@ def _arr(x, name, device, dtype, n):
 
 
 def _mat(x, name, device, dtype, rows, cols, stride):
-    """The same for [rows x cols] with `stride` elements between rows."""
-    if x.__class__ is _Tensor and x.dtype is dtype and x.get_device() == device and x.stride() == (stride, 1) and x.numel() >= rows * stride:
-        return x.data_ptr()                      # whole rows
+    """The same for [rows x cols] with `stride` elements between rows: the tensor itself must hold them, not only its storage."""
+    if (x.__class__ is _Tensor and x.dtype is dtype and x.get_device() == device and x.stride() == (stride, 1)
+            and x.shape[0] >= rows and x.shape[1] >= cols):
+        return x.data_ptr()
     if not isinstance(x, _Tensor):
         return x
     _check_kind(x, name, device, dtype)
-    if rows > 0:
-        have = x.untyped_storage().nbytes() // x.element_size() - x.storage_offset()
-        if have < (rows - 1) * stride + cols or (x.dim() == 2 and (x.stride(1) != 1 and x.shape[1] > 1
-                                                                   or x.stride(0) != stride and x.shape[0] > 1)):
-            raise DppoError(ERR_BAD_SHAPE, "%s: shape %s, strides %s do not hold %d rows of %d elements, %d apart"
-                            % (name, tuple(x.shape), x.stride(), rows, cols, stride))
+    if rows > 0 and not _holds_rows(x, rows, cols, stride):
+        raise DppoError(ERR_BAD_SHAPE, "%s: shape %s, strides %s do not hold %d rows of %d elements, %d apart"
+                        % (name, tuple(x.shape), x.stride(), rows, cols, stride))
     return x.data_ptr()
+
+
+def _holds_rows(x, rows, cols, stride):
+    """Whether x, of any rank, holds `rows` rows of `cols` elements that lie `stride` apart."""
+    if x.dim() == 2 and x.shape[0] > 1 and x.stride(0) != stride:
+        return False
+    runs = []                                    # x as few dimensions as its strides allow: [size, stride], outermost first
+    for n, s in zip(x.shape, x.stride()):
+        if n == 1:
+            continue
+        if runs and runs[-1][1] == n * s:
+            runs[-1] = [runs[-1][0] * n, s]
+        else:
+            runs.append([n, s])
+    if len(runs) == 2 and runs[1][1] == 1:       # rows of their own
+        (r, pitch), (c, _) = runs
+        return (pitch == stride or rows == 1) and r >= rows and c >= cols
+    if len(runs) == 1 and runs[0][1] == stride and cols == 1:
+        return runs[0][0] >= rows
+    dense = not runs or len(runs) == 1 and runs[0][1] == 1
+    return dense and x.numel() >= (rows - 1) * stride + cols
 
 
 def _check_kind(x, name, device, dtype):

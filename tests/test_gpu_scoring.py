@@ -910,3 +910,40 @@ def test_backward_of_a_maximum_far_from_zero(B, m, tau, V, dtype):
     got = out[:, :V].double().cpu().numpy()
     assert (got[zh == -np.inf] == 0).all()
     check_grad(got, want, zh, yh, ah, bh, tau, dtype, V)
+
+
+def test_matrices_of_other_ranks_and_slices(B):
+    """A matrix is taken in any shape whose own elements are the rows; rows of its storage that were not passed are refused, and
+    not written."""
+    T, V, ld, k = 10, 1003, 1008, 3
+    z, y = make(T, V, "bf16", 21)
+    assert z.shape[1] == ld
+    want = Fwd(B, z, V, y, k, 1.0).host()
+    prm = B.LogprobParams(T, V, B.BF16, ld, k, 0, 1.0)
+    f = lambda *s: torch.zeros(*s, device="cuda")
+    stats, a = f(T, 4), torch.ones(T, device="cuda")
+    dz = torch.full_like(z, 9.0)
+
+    def call(logits):
+        logp, ids, tl = f(T), torch.zeros(T, k, dtype=torch.int32, device="cuda"), f(T, k)
+        B.token_logprobs(prm, logits, y, None, logp, None, None, ids, tl, stats)
+        return logp.cpu().numpy(), ids.cpu().numpy()
+    for logits in (z, z[:, :V], z.view(2, 5, ld), z.view(2, 5, ld)[:, :, :V], z.view(-1), z.view(T, 1, ld)):
+        logp, ids = call(logits)
+        assert np.array_equal(logp, want["logp"]) and np.array_equal(ids, want["top_ids"])
+    B.token_logprobs_backward(prm, z, y, None, stats, a, None, dz)
+    grad = dz[:, :V].clone()
+    seqs = torch.full((2, 6, ld), 9.0, dtype=z.dtype, device="cuda")
+    for dlogits in (dz.view(2, 5, ld), dz.view(2, 5, ld)[:, :, :V]):
+        dz.fill_(9.0)
+        B.token_logprobs_backward(prm, z.view(2, 5, ld), y, None, stats, a, None, dlogits)
+        assert torch.equal(dz[:, :V], grad)
+    for wrong in (seqs[:, :-1], seqs[:, 1:], seqs.view(12, ld)[:9], seqs.view(12, ld)[:9, :V], seqs.view(-1)[:9 * ld]):
+        for args in ((wrong, dz), (z, wrong)):
+            with pytest.raises(B.DppoError) as e:
+                B.token_logprobs_backward(prm, args[0], y, None, stats, a, None, args[1])
+            assert e.value.code == B.ERR_BAD_SHAPE
+        with pytest.raises(B.DppoError):
+            call(wrong)
+    torch.cuda.synchronize()
+    assert bool((seqs == 9.0).all())

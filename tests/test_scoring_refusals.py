@@ -104,3 +104,68 @@ def test_binding_checks_tensors():
     assert code(B.token_logprobs, prm, torch.zeros(8, 4, dtype=torch.bfloat16).t(), P, None, P, P, P, None, None, P) == B.ERR_BAD_SHAPE
     assert code(B.token_logprobs, prm, z, torch.zeros(3, dtype=torch.int32), None, P, P, P, None, None, P) == B.ERR_BAD_SHAPE
     assert code(B.token_logprobs, prm, z, torch.zeros(8, dtype=torch.int32)[::2], None, P, P, P, None, None, P) == B.ERR_BAD_SHAPE
+
+
+cpu_only = pytest.mark.skipif(torch.cuda.is_available(), reason="looks at CPU tensors, which are on no current device there")
+BF = torch.bfloat16
+
+
+def not_held():
+    """(tensor, rows, cols, stride): the tensor itself does not hold the rows, though its storage may."""
+    buf = torch.zeros(8, 16, dtype=BF)
+    seqs = torch.zeros(2, 5, 16, dtype=BF)
+    return [
+        (seqs[:, :-1], 8, 16, 16),                               # shifted by one: the second sequence's rows are elsewhere
+        (seqs[:, 1:], 8, 16, 16),
+        (seqs.transpose(0, 1), 10, 16, 16), (seqs.permute(2, 0, 1), 10, 16, 16),
+        (torch.zeros(256, dtype=BF)[::2], 8, 16, 16),
+        (buf[:5], 8, 16, 16), (buf[:5, :12], 8, 12, 16), (buf[3:, :12], 6, 12, 16),      # rows that were not passed
+        (buf[:, :10], 8, 12, 16),                                # columns that were not passed
+        (buf[:1], 2, 16, 16), (buf[0], 2, 16, 16), (buf.view(-1)[:100], 8, 16, 16),
+        (buf.view(2, 4, 16)[:1], 8, 16, 16), (seqs[:, :, :12], 11, 12, 16),
+        (buf.view(4, 32), 8, 16, 16), (buf.view(16, 8), 8, 16, 16),
+        (buf[:1].expand(8, 16), 8, 16, 16), (buf.t(), 8, 8, 8), (buf[:, ::2], 8, 8, 16), (buf[::2], 4, 16, 16),
+        (torch.zeros(40, dtype=BF).as_strided((2, 32), (8, 1)), 8, 8, 8),                # windows that overlap: 40 elements, 64 asked for
+        (torch.zeros(0, 16, dtype=BF), 1, 16, 16), (torch.zeros(8, 0, dtype=BF), 8, 16, 16)]
+
+
+def held():
+    buf, seqs = torch.zeros(8, 16, dtype=BF), torch.zeros(2, 5, 16, dtype=BF)
+    return [
+        (buf, 8, 16, 16), (buf, 5, 12, 16), (buf[:5], 5, 16, 16), (buf[:, :12], 8, 12, 16), (buf[3:, :12], 5, 12, 16), (buf[::2], 4, 16, 32),
+        (buf[2:3, :12], 1, 12, 16), (buf[2:3], 1, 12, 12), (buf[0], 1, 16, 16), (buf.view(-1), 8, 16, 16), (buf.view(-1)[:124], 8, 12, 16),
+        (buf.view(1, -1), 8, 16, 16), (seqs, 10, 16, 16), (seqs[:, :, :12], 10, 12, 16), (seqs[:1, :4], 4, 16, 16), (seqs[0, 1:], 4, 16, 16),
+        (buf.view(8, 1, 16), 8, 16, 16), (buf.view(8, 4, 4), 8, 16, 16), (buf.view(8, 4, 4)[:, :3], 8, 12, 16), (buf[:, :1], 8, 1, 16),
+        (buf[:5], 0, 16, 16)]
+
+
+@cpu_only
+@pytest.mark.parametrize("case", range(len(not_held())))
+def test_binding_refuses_tensors_that_do_not_hold_the_rows(case):
+    x, rows, cols, stride = not_held()[case]
+    assert code(B._mat, x, "x", -1, BF, rows, cols, stride) == B.ERR_BAD_SHAPE
+
+
+@cpu_only
+@pytest.mark.parametrize("case", range(len(held())))
+def test_binding_takes_tensors_that_hold_the_rows(case):
+    x, rows, cols, stride = held()[case]
+    assert B._mat(x, "x", -1, BF, rows, cols, stride) == x.data_ptr()
+
+
+@cpu_only
+def test_every_matrix_argument_is_checked():
+    """As input and as output, of each call: rows behind the tensor that is passed are not touched."""
+    buf = torch.zeros(8, 16, dtype=BF)
+    codes = torch.zeros(8, 16, dtype=torch.int8)
+    prm = B.LogprobParams(8, 16, B.BF16, 16, 0, 0, 1.0)
+    assert code(B.token_logprobs, prm, buf[:5], P, None, P, P, P, None, None, P) == B.ERR_BAD_SHAPE
+    assert code(B.token_logprobs_backward, prm, buf[:5], P, None, P, P, P, buf) == B.ERR_BAD_SHAPE
+    assert code(B.token_logprobs_backward, prm, buf, P, None, P, P, P, buf[:5]) == B.ERR_BAD_SHAPE
+    q = B.QuantizeParams(8, 16, B.BF16, 16, 16)
+    assert code(B.quantize_rows_i8, q, buf[:5], codes, P) == B.ERR_BAD_SHAPE
+    assert code(B.quantize_rows_i8, q, buf, codes[:5], P) == B.ERR_BAD_SHAPE
+    lin = B.LinearI8Params(8, 8, 16, 16, 16, 16, B.BF16)
+    assert code(B.linear_i8, lin, codes[:5], P, codes, P, buf) == B.ERR_BAD_SHAPE
+    assert code(B.linear_i8, lin, codes, P, codes[:5], P, buf) == B.ERR_BAD_SHAPE
+    assert code(B.linear_i8, lin, codes, P, codes, P, buf[:5]) == B.ERR_BAD_SHAPE
