@@ -119,8 +119,13 @@ class DppoStep:
 
     # -- scoring: where logp_old and logp_ref come from ---------------------------------------------
     def _score_buffers(self, T, top_k, out):
-        """Buffers of a scoring call over T rows (reused when `out` is what an earlier call of the same sizes returned)."""
+        """Buffers of a scoring call over T rows: new ones, or `out`, what an earlier call with the same top_k returned."""
         if out is not None:
+            row, k = (T,), (T, top_k)
+            for n, want in (("logp", row), ("entropy", row), ("lse", row), ("stats", (T, 4)), ("top_ids", k), ("top_logp", k)):
+                have = out[n].shape if n in out else want
+                if have != want and (len(have) != len(want) or have[1:] != want[1:] or have[0] < T):
+                    raise ValueError("out: %s has shape %s, this call needs %s" % (n, tuple(have), want))
             return out
         f32 = dict(dtype=torch.float32, device=self.device)
         out = {n: torch.zeros(T, **f32) for n in ("logp", "entropy", "lse")}
@@ -140,7 +145,8 @@ class DppoStep:
         """Log-probs of the given tokens under the policy that made `logits` [T_max, V] (with the temperature of the
         loss), their entropy and top_k alternatives: a dict of logp, entropy, lse [T_max], top_ids, top_logp
         [T_max, top_k] and stats [T_max, 4] (for score_backward).  logp of a frozen policy is what loss() takes as
-        logp_old or logp_ref.  Rows past the token count (the packer's, or n_tokens_dev) are left as they were."""
+        logp_old or logp_ref.  Rows past the token count (the packer's, or n_tokens_dev) are left as they were.  `out`: the
+        dict of an earlier call with the same top_k, to be written again (ValueError where its shapes do not fit)."""
         out = self._score_buffers(self.T_max, top_k, out)
         self._score_call(logits, self.loss_params.dtype, self.V, self.V if row_stride is None else row_stride, target,
                          self.counts[3:4] if n_tokens_dev is None else n_tokens_dev, top_k, out, 0, self.T_max)

@@ -1,0 +1,48 @@
+"""What DppoStep's scoring methods hand to the library, with the library's calls replaced by recorders (CPU)."""
+import types
+
+import pytest
+import torch
+
+from paper_2603_04135_b200 import binding as B
+from paper_2603_04135_b200 import step as S
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Every call of the binding's scoring functions as (name, arguments); tensors are kept alive."""
+    seen = []
+    for name in ("token_logprobs", "token_logprobs_backward", "quantize_rows_i8", "linear_i8"):
+        monkeypatch.setattr(B, name, lambda *a, _n=name, **k: seen.append((_n, a)))
+    return seen
+
+
+def make(T_max, V, dtype=B.F32):
+    st = S.DppoStep.__new__(S.DppoStep)                              # the constructor asks for a GPU
+    st.V, st.T_max, st.device = V, T_max, torch.device("cpu")
+    st.counts = torch.tensor([0, 0, 0, T_max], dtype=torch.int32)
+    st.status = torch.zeros(1, dtype=torch.int32)
+    st.loss_params = types.SimpleNamespace(dtype=dtype, temperature=1.0)
+    return st
+
+
+def test_scores_into_earlier_outputs(calls):
+    st = make(6, 16)
+    z, y = torch.zeros(6, 16), torch.zeros(6, dtype=torch.int32)
+    out = st.score(z, y, top_k=3)
+    assert st.score(z, y, top_k=3, out=out) is out
+    assert [c[1][7].data_ptr() for c in calls] == [out["top_ids"].data_ptr()] * 2
+    plain = st.score(z, y)
+    assert st.score(z, None, out=plain) is plain
+    longer = {n: torch.zeros(9, *v.shape[1:], dtype=v.dtype) for n, v in out.items()}      # more rows than T_max
+    assert st.score(z, y, top_k=3, out=longer) is longer
+    n = len(calls)
+    for k in (0, 2, 4, 8):                                           # ids of another pitch would come out scrambled, of 0 stale
+        with pytest.raises(ValueError):
+            st.score(z, y, top_k=k, out=out)
+    for name in ("logp", "entropy", "lse", "stats", "top_ids", "top_logp"):
+        with pytest.raises(ValueError):
+            st.score(z, y, top_k=3, out=dict(out, **{name: out[name][:5]}))
+    with pytest.raises(ValueError):
+        st.score(z, y, top_k=3, out=dict(out, top_logp=torch.zeros(18)))
+    assert len(calls) == n
