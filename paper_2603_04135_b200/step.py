@@ -172,6 +172,9 @@ class DppoStep:
         T, H = hidden.shape
         if T != self.T_max:
             raise ValueError("hidden has %d rows, T_max is %d" % (T, self.T_max))
+        if W_q.shape != (W_scale.numel(), H):
+            raise ValueError("W_q has shape %s; %d scales and hidden states %d wide need (%d, %d)"
+                             % (tuple(W_q.shape), W_scale.numel(), H, W_scale.numel(), H))
         out = self._score_buffers(T, top_k, out)
         if T == 0:
             return out

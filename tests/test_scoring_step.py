@@ -46,3 +46,21 @@ def test_scores_into_earlier_outputs(calls):
     with pytest.raises(ValueError):
         st.score(z, y, top_k=3, out=dict(out, top_logp=torch.zeros(18)))
     assert len(calls) == n
+
+
+def frozen_head(V, H):
+    W_q = torch.zeros(V, (H + 127) // 128 * 128, dtype=torch.int8)[:, :H]
+    return W_q, torch.ones(V)
+
+
+def test_weights_of_another_width_are_refused(calls):
+    st = make(6, 40)
+    hidden = torch.zeros(6, 128)
+    st.score_hidden_i8(hidden, *frozen_head(40, 128))
+    assert [c[0] for c in calls] == ["quantize_rows_i8", "linear_i8", "token_logprobs"]
+    W_q, W_scale = frozen_head(40, 100)                              # padded to 128 columns: the codes of 100 pass as 128
+    for args in ((hidden, W_q, W_scale), (hidden, *frozen_head(40, 256)), (hidden, frozen_head(41, 128)[0], torch.ones(40)),
+                 (hidden, frozen_head(39, 128)[0], torch.ones(40)), (hidden, torch.zeros(40 * 128, dtype=torch.int8), torch.ones(40))):
+        with pytest.raises(ValueError):
+            st.score_hidden_i8(*args)
+    assert len(calls) == 3
