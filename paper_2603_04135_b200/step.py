@@ -167,8 +167,8 @@ class DppoStep:
     def score_hidden_i8(self, hidden, W_q, W_scale, target=None, top_k=0, n_tokens_dev=None, chunk_tokens=2048, out=None):
         """The same scores from hidden states [T_max, H] (bf16 or f32, rows on 16 bytes) and a frozen policy's LM-head in
         8 bits (quantize_rows_i8 of its [V, H] weight): rows quantised per token, product on the tensor cores, scores.
-        The tokens are taken chunk_tokens at a time through an f32 logits scratch of that many rows that this object
-        keeps; the whole [T_max, V] is never formed."""
+        The tokens are taken chunk_tokens at a time through an f32 logits scratch of that many rows, allocated for the call;
+        the whole [T_max, V] is never formed."""
         T, H = hidden.shape
         if T != self.T_max:
             raise ValueError("hidden has %d rows, T_max is %d" % (T, self.T_max))
@@ -180,15 +180,16 @@ class DppoStep:
             return out
         V, C = W_scale.numel(), min(chunk_tokens, T)
         ldq, ldv = (H + 127) // 128 * 128, (V + 3) // 4 * 4
-        need = (C, ldv, ldq)
-        if getattr(self, "_score_scratch_shape", None) != need:
-            self._score_scratch = (torch.zeros(C, ldv, dtype=torch.float32, device=self.device),
-                                   torch.zeros(C, ldq, dtype=torch.int8, device=self.device),
-                                   torch.zeros(C, dtype=torch.float32, device=self.device))
-            self._score_scratch_shape = need
-        logits, q, q_scale = self._score_scratch
+        # of this call alone, so that calls on several streams, or captured ones, do not write each other's; nothing of it is read
+        # before it is written
+        logits = torch.empty(C, ldv, dtype=torch.float32, device=self.device)
+        q = torch.empty(C, ldq, dtype=torch.int8, device=self.device)
+        q_scale = torch.empty(C, dtype=torch.float32, device=self.device)
         T_dev = self.counts[3:4] if n_tokens_dev is None else n_tokens_dev
-        left = torch.clamp(T_dev - torch.arange(0, T, C, dtype=torch.int32, device=self.device), 0, C).to(torch.int32)
+        if T <= C and T_dev.dtype is torch.int32 and T_dev.dim() == 1:
+            left = T_dev                         # one chunk: the kernels bound the count by the rows themselves
+        else:
+            left = torch.clamp(T_dev - torch.arange(0, T, C, dtype=torch.int32, device=self.device), 0, C).to(torch.int32)
         dtype = B.BF16 if hidden.dtype is torch.bfloat16 else B.F32
         for i, lo in enumerate(range(0, T, C)):
             hi, n = min(lo + C, T), left[i:i + 1]

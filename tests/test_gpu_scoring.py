@@ -947,3 +947,81 @@ def test_matrices_of_other_ranks_and_slices(B):
             call(wrong)
     torch.cuda.synchronize()
     assert bool((seqs == 9.0).all())
+
+
+def hidden_case(V, H, T, seed):
+    from paper_2603_04135_b200.step import quantize_rows_i8
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    hidden = torch.empty(T, H, device="cuda").normal_(0, 1, generator=g).to(torch.bfloat16)
+    W_q, W_scale = quantize_rows_i8(torch.empty(V, H, device="cuda").normal_(0, 0.1, generator=g))
+    return hidden, W_q, W_scale, torch.randint(0, V, (T,), device="cuda", dtype=torch.int32, generator=g)
+
+
+def test_hidden_states_scored_on_two_streams_at_once(B):
+    """Two frozen policies side by side, each on its own stream, give what they give alone."""
+    V, H, T = 20003, 256, 700
+    st = make_step(V, T)
+    cases = [hidden_case(V, H, T, s) for s in (1, 2)]
+    alone = {n: [st.score_hidden_i8(*c, top_k=4, chunk_tokens=n) for c in cases] for n in (300, 128)}    # each sums in its own order
+    streams = [torch.cuda.Stream() for _ in cases]
+    outs = [[{n: torch.zeros_like(v) for n, v in alone[300][0].items()} for _ in range(6)] for _ in cases]
+    torch.cuda.synchronize()
+    for i in range(6):
+        for s, c, o in zip(streams, cases, outs):
+            with torch.cuda.stream(s):
+                st.score_hidden_i8(*c, top_k=4, chunk_tokens=300 if i % 3 else 128, out=o[i])
+    torch.cuda.synchronize()
+    assert st.status.item() == 0
+    for j, os in enumerate(outs):
+        for i, o in enumerate(os):
+            for n, v in alone[300 if i % 3 else 128][j].items():
+                assert torch.equal(o[n], v), (i, j, n)
+
+
+def test_hidden_states_scored_in_two_graphs(B):
+    """Two captured calls replayed on two streams at once, with eager calls of other sizes in between."""
+    V, H, T = 8003, 256, 300
+    st = make_step(V, T)
+    cases = [hidden_case(V, H, T, s) for s in (3, 4)]
+    want = [st.score_hidden_i8(*c, top_k=4) for c in cases]
+    outs = [{n: torch.zeros_like(v) for n, v in w.items()} for w in want]
+    torch.cuda.synchronize()
+    graphs = []
+    for c, o in zip(cases, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            st.score_hidden_i8(*c, top_k=4, out=o)
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for i in range(4):
+        for o in outs:
+            for v in o.values():
+                v.zero_()
+        st.score_hidden_i8(*cases[0], top_k=2, chunk_tokens=64 + 32 * i)
+        torch.cuda.synchronize()
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+                g.replay()
+        torch.cuda.synchronize()
+        for w, o in zip(want, outs):
+            for n in w:
+                assert torch.equal(o[n], w[n]), n
+    assert st.status.item() == 0
+
+
+@pytest.mark.parametrize("n", [-3, 0, 1, 40, 1000])
+def test_hidden_states_of_any_token_count(B, n):
+    """A count on the device beyond the rows, none or below none, in one chunk and in several, as i32 [1], i32 [] and i64 [1]."""
+    V, H, T = 1003, 128, 41
+    st = make_step(V, T)
+    c = hidden_case(V, H, T, 5)
+    full = st.score_hidden_i8(*c, top_k=3)
+    m = min(max(n, 0), T)
+    for chunk in (2048, 41, 16):
+        for count in (torch.tensor([n], dtype=torch.int32, device="cuda"), torch.tensor(n, dtype=torch.int32, device="cuda"),
+                      torch.tensor([n], device="cuda")):
+            got = st.score_hidden_i8(*c, top_k=3, n_tokens_dev=count, chunk_tokens=chunk)
+            for name, v in got.items():
+                assert torch.equal(v[:m], full[name][:m]), name
+                assert bool((v[m:] == (-1 if name == "top_ids" else 0)).all()), name
+    assert st.status.item() == 0

@@ -64,3 +64,20 @@ def test_weights_of_another_width_are_refused(calls):
         with pytest.raises(ValueError):
             st.score_hidden_i8(*args)
     assert len(calls) == 3
+
+
+def test_calls_share_no_scratch(calls):
+    """Two calls may be under way at once (two streams), or be replayed later (captured): each has codes, scales and logits of
+    its own."""
+    st = make(6, 40)
+    hidden = torch.zeros(6, 128)
+    st.score_hidden_i8(hidden, *frozen_head(40, 128), chunk_tokens=4)
+    first = [a for _, a in calls]                                    # the recorder keeps the tensors: their memory is not free
+    del calls[:]
+    st.score_hidden_i8(hidden, *frozen_head(40, 128), chunk_tokens=4)
+    second = [a for _, a in calls]
+    assert len(first) == len(second) == 6
+    for i, names in ((0, (2, 3)), (1, (1, 2, 5)), (2, (1,))):        # codes and scales; codes, scales and logits; logits
+        for j in names:
+            assert first[i][j].data_ptr() != second[i][j].data_ptr()
+            assert first[i][j].data_ptr() == first[i + 3][j].data_ptr()          # the chunks of a call follow each other
