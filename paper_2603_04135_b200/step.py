@@ -155,9 +155,13 @@ class DppoStep:
     def score_backward(self, logits, target, scored, dlogp=None, dentropy=None, dlogits=None, row_stride=None,
                        n_tokens_dev=None):
         """Gradient with respect to `logits` of a loss with the per-token derivatives dlogp and dentropy (f32 [T_max], either
-        may be None); `scored` is what score() returned.  Returns dlogits (`logits` itself for in place)."""
-        if dlogits is None:
+        may be None); `scored` is what score() returned.  Returns dlogits (`logits` itself for in place; a new tensor of the
+        logits' shape and strides if None)."""
+        if dlogits is None and logits.is_contiguous():
             dlogits = torch.zeros_like(logits)
+        elif dlogits is None:                    # rows that are padded: the same pitch
+            extent = 1 + sum((n - 1) * s for n, s in zip(logits.shape, logits.stride())) if logits.numel() else 0
+            dlogits = logits.new_zeros(extent).as_strided(logits.shape, logits.stride())
         stride = self.V if row_stride is None else row_stride
         prm = B.LogprobParams(self.T_max, self.V, self.loss_params.dtype, stride, 0, 0, self.loss_params.temperature)
         B.token_logprobs_backward(prm, logits, target, self.counts[3:4] if n_tokens_dev is None else n_tokens_dev,

@@ -1025,3 +1025,22 @@ def test_hidden_states_of_any_token_count(B, n):
                 assert torch.equal(v[:m], full[name][:m]), name
                 assert bool((v[m:] == (-1 if name == "top_ids" else 0)).all()), name
     assert st.status.item() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_step_gradient_of_padded_rows(B, dtype):
+    """score and score_backward on a [T, V] view of rows padded to 16 bytes, an odd vocabulary."""
+    T, V = 9, 1003
+    st = make_step(V, T, dtype)
+    z, y = make(T, V, dtype, 30)
+    z[:, V:] = math.nan                                              # the padding is not looked at
+    a, b = torch.randn(T, device="cuda"), torch.randn(T, device="cuda")
+    zh, yh = z[:, :V].double().cpu().numpy(), y.cpu().numpy()
+    ah, bh = a.double().cpu().numpy(), b.double().cpu().numpy()
+    want = scoring.token_logprobs_backward(zh, yh, ah, bh, 0.9)
+    for logits in (z[:, :V], z):
+        scored = st.score(logits, y, top_k=2, row_stride=z.shape[1])
+        d = st.score_backward(logits, y, scored, dlogp=a, dentropy=b, row_stride=z.shape[1])
+        assert d.shape == logits.shape and d.stride() == logits.stride() and bool((d[:, V:] == 0).all())
+        check_grad(d[:, :V].double().cpu().numpy(), want, zh, yh, ah, bh, 0.9, dtype, V)
+    assert st.status.item() == 0

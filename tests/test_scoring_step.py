@@ -81,3 +81,26 @@ def test_calls_share_no_scratch(calls):
         for j in names:
             assert first[i][j].data_ptr() != second[i][j].data_ptr()
             assert first[i][j].data_ptr() == first[i + 3][j].data_ptr()          # the chunks of a call follow each other
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradient_is_laid_out_as_the_logits_are(calls, dtype):
+    """score_backward without dlogits: a result with the logits' shape and row pitch, also of rows that are padded."""
+    T, V, ld = 6, 1003, 1008
+    st = make(T, V, B.BF16 if dtype is torch.bfloat16 else B.F32)
+    buf, y, one = torch.zeros(T, ld, dtype=dtype), torch.zeros(T, dtype=torch.int32), torch.ones(T)
+    scored = dict(stats=torch.zeros(T, 4))
+    more = torch.zeros(T + 3, ld, dtype=dtype)
+    for logits in (buf[:, :V], buf, buf.view(2, 3, ld), buf.view(2, 3, ld)[:, :, :V], buf.view(-1), more[:, :V], more[2:-1, :V]):
+        got = st.score_backward(logits, y, scored, dlogp=one, row_stride=ld)
+        assert got.shape == logits.shape and got.dtype is dtype and not bool(got.any())
+        assert calls[-1][0] == "token_logprobs_backward" and calls[-1][1][7] is got
+        for x in (logits, got):                                      # what the binding then asks of both
+            assert B._mat(x, "x", x.get_device(), dtype, T, V, ld) == x.data_ptr()
+        if logits.dim() > 1:
+            assert got.stride() == logits.stride()
+    st1 = make(1, V)
+    row = torch.zeros(1, ld)[:, :V]
+    assert st1.score_backward(row, y[:1], scored, dlogp=one[:1], row_stride=ld).shape == row.shape
+    mine = torch.zeros(T, ld, dtype=dtype)
+    assert st.score_backward(buf, y, scored, dlogp=one, dlogits=mine, row_stride=ld) is mine
