@@ -93,6 +93,9 @@ __device__ __forceinline__ void lm_tma_2d_pair(uint32_t dst, const CUtensorMap* 
                      :: "r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
 }
 
+// Instructions marked .aligned want the warp's lanes together.  After code that some lanes leave early (rows or channels past
+// the end), or that one lane runs alone, only a __syncwarp() promises that: callers of these helpers see to it.
+
 // 32 consecutive f32 columns of this thread's TMEM lane (its tile row) into registers.
 __device__ __forceinline__ void lm_tmem_load32(uint32_t (&v)[32], uint32_t taddr) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "

@@ -1044,3 +1044,21 @@ def test_step_gradient_of_padded_rows(B, dtype):
         assert d.shape == logits.shape and d.stride() == logits.stride() and bool((d[:, V:] == 0).all())
         check_grad(d[:, :V].double().cpu().numpy(), want, zh, yh, ah, bh, 0.9, dtype, V)
     assert st.status.item() == 0
+
+
+@pytest.mark.parametrize("variant", [1, 2])
+@pytest.mark.parametrize("N", [1, 31, 33, 97, 129, 255, 257, 383])
+def test_linear_i8_last_channels(B, N, variant):
+    """Some lanes of a warp have no channel, or a block of tokens is the last: the others' sums are read all the same, in
+    contractions of one CTA, of a cluster and of a pair, call after call."""
+    for M, K in ((1, 130), (15, 1024), (47, 4096), (130, 515), (300, 640)):
+        x, w = codes(M, K, (K + 15) // 16 * 16, M), codes(N, K, (K + 15) // 16 * 16, N)
+        xs, ws = torch.rand(M, device="cuda"), torch.rand(N, device="cuda")
+        out = torch.full((M + 1, N + 5), 5.0, device="cuda")
+        prm = B.LinearI8Params(M, N, K, x.shape[1], w.shape[1], N + 5, B.F32, variant)
+        want = torch.from_numpy(f32_product(x[:, :K], xs, w[:, :K], ws))
+        for _ in range(3):
+            out[:M, :N] = 0
+            B.linear_i8(prm, x, xs, w, ws, out)
+            assert torch.equal(out[:M, :N].cpu(), want)
+        assert bool((out[M:] == 5.0).all()) and bool((out[:, N:] == 5.0).all())
