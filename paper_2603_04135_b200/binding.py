@@ -14,6 +14,8 @@ import os
 
 import torch
 
+from . import build
+
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdppo.so")
 if not os.path.exists(_LIB_PATH):
     raise ImportError("libdppo.so is not built: run `python -m paper_2603_04135_b200.build` "
@@ -322,14 +324,26 @@ def sequence_log_ratio(logp, logp_old, cu_seqlens, S_max, out, status=None, stre
                                        _stream(stream)))
 
 
-try:
-    from . import _marshal as _native
-    _native.bind(LogprobParams, QuantizeParams, LinearI8Params,
-                 *(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.dppo_token_logprobs, lib.dppo_token_logprobs_backward,
-                                                                   lib.dppo_quantize_rows_i8, lib.dppo_linear_i8)))
-except ImportError:
-    class _native:                   # noqa: N801  (stands in for the module: nothing is the plain case)
-        token_logprobs = token_logprobs_backward = quantize_rows_i8 = linear_i8 = staticmethod(lambda *a: None)
+class _NoNative:
+    """Stands in for the native marshalling: nothing is the plain case."""
+    token_logprobs = token_logprobs_backward = quantize_rows_i8 = linear_i8 = staticmethod(lambda *a: None)
+
+
+def _load_native():
+    """The native marshalling, if it was built for this interpreter and this torch: it reads their structures."""
+    try:
+        from . import _marshal
+    except ImportError:
+        return _NoNative
+    if getattr(_marshal, "built_for", None) != build.built_for():
+        return _NoNative
+    _marshal.bind(LogprobParams, QuantizeParams, LinearI8Params,
+                  *(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.dppo_token_logprobs, lib.dppo_token_logprobs_backward,
+                                                                    lib.dppo_quantize_rows_i8, lib.dppo_linear_i8)))
+    return _marshal
+
+
+_native = _load_native()
 
 
 def _done(rc):

@@ -11,6 +11,7 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libdppo.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")
+MARSHAL_STAMP = os.path.join(OBJ, "marshal.stamp")       # what MARSHAL was built for
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]
@@ -62,10 +63,20 @@ def build_library(force=False, verbose=False):
     return LIB
 
 
+def built_for():
+    """The interpreter and torch whose layouts a module compiled now relies on."""
+    import torch
+    return "%s torch %s" % (sys.implementation.cache_tag, torch.__version__)
+
+
 def build_marshal(force=False):
     """Compile csrc/marshal.cpp against this interpreter's and torch's headers.  Returns the module's path."""
     src = os.path.join(CSRC, "marshal.cpp")
-    if not force and not _stale(MARSHAL, [src, os.path.join(ROOT, "include", "dppo.h")]):
+    stamp = None
+    if os.path.exists(MARSHAL_STAMP):
+        with open(MARSHAL_STAMP) as f:
+            stamp = f.read()
+    if not force and stamp == built_for() and not _stale(MARSHAL, [src, os.path.join(ROOT, "include", "dppo.h")]):
         return MARSHAL
     import sysconfig
 
@@ -76,12 +87,15 @@ def build_marshal(force=False):
     inc = [os.path.join(tdir, "include"), os.path.join(tdir, "include", "torch", "csrc", "api", "include"),
            os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-I" + os.path.join(ROOT, "include"),
-           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)]
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), '-DDPPO_BUILT_FOR="%s"' % built_for()]
     cmd += [x for p in inc for x in ("-isystem", p)]
     cmd += [src, "-o", MARSHAL, "-L" + tlib, "-Wl,-rpath," + tlib, "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("host compiler failed: %s\n%s\n%s" % (" ".join(cmd), r.stdout, r.stderr))
+    os.makedirs(OBJ, exist_ok=True)
+    with open(MARSHAL_STAMP, "w") as f:
+        f.write(built_for())
     return MARSHAL
 
 

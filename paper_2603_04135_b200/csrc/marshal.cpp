@@ -163,4 +163,9 @@ PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods,
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__marshal(void) { return PyModule_Create(&kModule); }
+// built_for: the interpreter and torch whose layouts this code relies on; the binding uses it with no other.
+PyMODINIT_FUNC PyInit__marshal(void) {
+    PyObject* m = PyModule_Create(&kModule);
+    if (m && PyModule_AddStringConstant(m, "built_for", DPPO_BUILT_FOR) != 0) { Py_DECREF(m); return nullptr; }
+    return m;
+}
