@@ -1062,3 +1062,43 @@ def test_linear_i8_last_channels(B, N, variant):
             B.linear_i8(prm, x, xs, w, ws, out)
             assert torch.equal(out[:M, :N].cpu(), want)
         assert bool((out[M:] == 5.0).all()) and bool((out[:, N:] == 5.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V, variant", [(1021, 0), (1021, 32), (8203, 32), (20003, 0), (20003, 10512), (50304, 20256), (151936, 0), (151937, 10128),
+                                        (151937, 40256), (151937, 80512)])
+def test_every_entry_counts_once(B, V, variant, dtype):
+    """Rows of n entries at 0 and nothing else that counts (-inf, the type's lowest value, -5,000): 2^0 = 1 is exact, so are
+    sums of up to 2^24 ones, and 2^-5000 is 0.  What is left is logf's error of one step, 2 U l for l = ln n, where one entry
+    lost or counted twice moves l by 1 / n > 6e-6.  The gradient's exponent has l's error (2 U l) and three roundings
+    (log2(e), product, fma: 3 U l), the exponential 4 U, the product with a and the sum at the token one each."""
+    lowest = float(torch.finfo(DT[dtype]).min)
+    g = torch.Generator().manual_seed(V)
+    live = [torch.ones(V, dtype=torch.bool), torch.rand(V, generator=g) < 0.5, torch.arange(V) < V - 1, torch.arange(V) > 0,
+            torch.arange(V) % 977 == 5, torch.arange(V) == V - 1, torch.rand(V, generator=g) < 0.9]
+    T = len(live)
+    z = torch.zeros(T, pad16(V, 2 if dtype == "bf16" else 4))
+    for t, on in enumerate(live):
+        other = torch.tensor([-math.inf, lowest, -5000.0])[torch.randint(0, 3, (V,), generator=g)]
+        z[t, :V] = torch.where(on, torch.tensor(0.0), other)
+    n = torch.stack([on.sum() for on in live]).double().numpy()
+    y = torch.tensor([int(torch.nonzero(on)[-1]) for on in live], dtype=torch.int32, device="cuda")
+    z = z.to(DT[dtype]).cuda()
+    f = Fwd(B, z, V, y, 3, 1.0, variant)
+    o, l = f.host(), np.log(n)
+    for got, want in ((o["lse"], l), (o["entropy"], l), (o["logp"], -l), (o["top_logp"][:, 0], -l)):
+        assert (np.abs(got - want) <= 2 * U * l).all(), (got - want, l)
+    first = [torch.nonzero(on)[:3, 0].tolist() for on in live]
+    assert [[i for i, p in zip(ids, lp) if p > -100] for ids, lp in zip(o["top_ids"].tolist(), o["top_logp"].tolist())] == first
+    a = torch.randn(T, device="cuda")
+    dz = torch.full_like(z, 9.0)
+    B.token_logprobs_backward(B.LogprobParams(T, V, B.BF16 if dtype == "bf16" else B.F32, z.stride(0), 0, 0, 1.0), z, y, None, f.stats, a, None, dz)
+    ah, got = a.double().cpu().numpy(), dz[:, :V].double().cpu().numpy()
+    half = 2.0 ** -8 if dtype == "bf16" else 0.0                           # f32: the product's rounding is the output's
+    for t, on in enumerate(live):
+        p = on.double().numpy() / n[t]
+        want = -ah[t] * p
+        tol = np.abs(want) * (5 * l[t] + 6) * U
+        want[int(y[t])] += ah[t]
+        tol[int(y[t])] += 2 * U * abs(ah[t])
+        assert (np.abs(got[t] - want) <= tol * (1 + half) + half * np.abs(want)).all(), t
