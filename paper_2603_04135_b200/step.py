@@ -136,7 +136,7 @@ class DppoStep:
 
     def _score_call(self, logits, dtype, V, stride, target, n_tokens_dev, top_k, out, lo, hi):
         prm = B.LogprobParams(hi - lo, V, dtype, stride, top_k, 0, self.loss_params.temperature)
-        part = {n: v[lo:hi] for n, v in out.items()}
+        part = {n: v[lo:hi] for n, v in out.items()} if lo > 0 else out
         B.token_logprobs(prm, logits, target, n_tokens_dev, part["logp"] if target is not None else None, part["entropy"],
                          part["lse"], part["top_ids"] if top_k else None, part["top_logp"] if top_k else None,
                          part["stats"], self.status)
