@@ -435,6 +435,57 @@ typedef struct {
 int dppo_linear_i8(const dppo_linear_i8_params* p, const int8_t* x, const float* x_scale, const int8_t* w,
                    const float* w_scale, void* out, const int32_t* n_rows_dev, int32_t* status, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Distillation from a teacher's top log-probs (what dppo_token_logprobs returns for another policy: top_ids, top_logp).
+ *
+ * Row t lists top_k tokens i_j with the teacher's log-probs; an id of -1 is no entry.  p_j = exp(top_logp_j), s = softmax(z / tau)
+ * of the student's logits z, sigma = the sum of s over the tokens that are not listed.
+ *   loss = sum_j p_j (ln p_j - ln s_{i_j})          p ln p = 0 at p = 0
+ *   mode GIVEN: as it stands;  NORMALIZED: with p_j / sum_j p_j in place of p_j;
+ *   REST: plus r (ln r - ln sigma) for the teacher's remainder r = 1 - sum_j p_j; an r up to 2^-16 counts as 0 (that is the
+ *         rounding of f32 log-probs)
+ *   dloss/dz_v = (G s_v - sum_{j: i_j = v} p_j - [v not listed] s_v r / sigma) / tau,   G = sum_j p_j + r  (r = 0 but in REST)
+ * A token listed twice counts with both log-probs, and once in sigma.  A row without entries has loss 0 and a zero gradient.
+ * Logits at -inf are masked: probability 0; a listed one with p > 0 makes the loss +inf (its gradient stays finite).  A row that
+ * its mask leaves empty has lse = -inf, loss +inf (0 if all p are 0) and a zero gradient.  A row with a NaN or +inf has NaN for
+ * all of these.  sigma is summed from its own terms, not taken as 1 minus the others.
+ */
+typedef enum { DPPO_DISTILL_GIVEN = 0, DPPO_DISTILL_NORMALIZED = 1, DPPO_DISTILL_REST = 2 } dppo_distill_mode;
+
+typedef struct {
+    int64_t T_max;          /* rows of logits / upper bound of tokens                                */
+    int32_t V;              /* vocabulary size, up to 2^20                                           */
+    int32_t dtype;          /* dppo_dtype of logits and dlogits                                      */
+    int64_t row_stride;     /* elements between consecutive rows (>= V; bytes a multiple of 16)      */
+    int32_t top_k;          /* teacher entries per row, 1..128                                       */
+    int32_t mode;           /* dppo_distill_mode                                                     */
+    double temperature;     /* of the student, 1e-6 .. 1e6; the teacher's log-probs are taken as they are */
+} dppo_distill_params;
+
+/*   logits       [T_max x row_stride] of dtype: the student's
+ *   top_ids      i32 [T_max x top_k], top_logp f32 [T_max x top_k]
+ *   n_tokens_dev i32 [1] true number of tokens T <= T_max on the device, or NULL (T = T_max);
+ *                rows >= T are neither read nor written, in any array
+ *   weight       f32 [T_max] or NULL (1): dL/dloss of each row, for dlogits; the loss is written without it
+ *   loss_out, lse_out   f32 [T_max] or NULL
+ *   stats        f32 [T_max x 4]: {m, S, G, r / sigma} of each row for the backward call (m the largest logit, S = sum_v
+ *                exp((z_v - m) / tau)); may be NULL without dlogits
+ *   dlogits      NULL (loss alone), or the gradient in the same call: same dtype / stride as logits; may alias logits (in
+ *                place).  Columns at or past V are not written.
+ * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED (logits, dlogits, stats: base or row stride), UNSUPPORTED (dtype).
+ * Device status: BAD_TARGET (an id below -1 or at or past V: the row's loss is 0 and its gradient zero).
+ */
+int dppo_distill_topk(const dppo_distill_params* p, const void* logits, const int32_t* top_ids, const float* top_logp,
+                      const int32_t* n_tokens_dev, const float* weight, float* loss_out, float* lse_out, float* stats,
+                      void* dlogits, int32_t* status, void* stream);
+
+/* The gradient alone, for dloss = dL/dloss of each row (f32 [T_max], NULL: 1) and the stats of a dppo_distill_topk call with the
+ * same arguments: one read and one write of the rows.  dlogits may alias logits.  Errors and status as above.
+ */
+int dppo_distill_topk_backward(const dppo_distill_params* p, const void* logits, const int32_t* top_ids, const float* top_logp,
+                               const int32_t* n_tokens_dev, const float* stats, const float* dloss, void* dlogits,
+                               int32_t* status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -89,6 +89,14 @@ class LinearI8Params(ctypes.Structure):
                 ("out_dtype", ctypes.c_int32), ("variant", ctypes.c_int32)]
 
 
+class DistillParams(ctypes.Structure):
+    _fields_ = [("T_max", ctypes.c_int64), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("row_stride", ctypes.c_int64), ("top_k", ctypes.c_int32), ("mode", ctypes.c_int32),
+                ("temperature", ctypes.c_double)]
+
+
+DISTILL_GIVEN, DISTILL_NORMALIZED, DISTILL_REST = 0, 1, 2
+MAX_LISTED = 128
 MAX_TOP_K = 32
 LINEAR_I8_WAIT_SELF_TEST = 100     # added to dppo_linear_i8_params.variant
 
@@ -132,6 +140,10 @@ lib.dppo_quantize_rows_i8.restype = ctypes.c_int
 lib.dppo_quantize_rows_i8.argtypes = [ctypes.POINTER(QuantizeParams)] + [_vp] * 6
 lib.dppo_linear_i8.restype = ctypes.c_int
 lib.dppo_linear_i8.argtypes = [ctypes.POINTER(LinearI8Params)] + [_vp] * 8
+lib.dppo_distill_topk.restype = ctypes.c_int
+lib.dppo_distill_topk.argtypes = [ctypes.POINTER(DistillParams)] + [_vp] * 11
+lib.dppo_distill_topk_backward.restype = ctypes.c_int
+lib.dppo_distill_topk_backward.argtypes = [ctypes.POINTER(DistillParams)] + [_vp] * 9
 
 
 def _ptr(x):
@@ -409,3 +421,22 @@ def linear_i8(params, x, x_scale, w, w_scale, out, n_rows_dev=None, status=None,
         _mat(out, "out", d, _TORCH_DTYPE.get(p.out_dtype), M, N, p.out_stride), _arr(n_rows_dev, "n_rows_dev", d, _i32, 1),
         _arr(status, "status", d, _i32, 1),
         _stream(stream)))
+
+
+def distill_topk(params, logits, top_ids, top_logp, n_tokens_dev, weight, loss_out, lse_out, stats, dlogits, status=None, stream=None):
+    p, d = params, _device()
+    T, V, dt, ld, k = p.T_max, p.V, _TORCH_DTYPE.get(p.dtype), p.row_stride, p.T_max * p.top_k
+    _check(lib.dppo_distill_topk(
+        ctypes.byref(p), _mat(logits, "logits", d, dt, T, V, ld), _arr(top_ids, "top_ids", d, _i32, k), _arr(top_logp, "top_logp", d, _f32, k),
+        _arr(n_tokens_dev, "n_tokens_dev", d, _i32, 1), _arr(weight, "weight", d, _f32, T), _arr(loss_out, "loss_out", d, _f32, T),
+        _arr(lse_out, "lse_out", d, _f32, T), _arr(stats, "stats", d, _f32, 4 * T), _mat(dlogits, "dlogits", d, dt, T, V, ld),
+        _arr(status, "status", d, _i32, 1), _stream(stream)))
+
+
+def distill_topk_backward(params, logits, top_ids, top_logp, n_tokens_dev, stats, dloss, dlogits, status=None, stream=None):
+    p, d = params, _device()
+    T, V, dt, ld, k = p.T_max, p.V, _TORCH_DTYPE.get(p.dtype), p.row_stride, p.T_max * p.top_k
+    _check(lib.dppo_distill_topk_backward(
+        ctypes.byref(p), _mat(logits, "logits", d, dt, T, V, ld), _arr(top_ids, "top_ids", d, _i32, k), _arr(top_logp, "top_logp", d, _f32, k),
+        _arr(n_tokens_dev, "n_tokens_dev", d, _i32, 1), _arr(stats, "stats", d, _f32, 4 * T), _arr(dloss, "dloss", d, _f32, T),
+        _mat(dlogits, "dlogits", d, dt, T, V, ld), _arr(status, "status", d, _i32, 1), _stream(stream)))

@@ -1,0 +1,568 @@
+// Distillation from a teacher's top log-probs: the loss of each token and its gradient with respect to the student's logits.
+//
+// The teacher lists K <= 128 tokens i_j of a row with log-probs; p_j = exp of those (mode NORMALIZED: over their sum), and in
+// mode REST r = 1 - sum p_j is its probability of everything else.  With the student's s = softmax(z / tau) and sigma = the
+// sum of s over what is not listed:
+//     loss = sum_j p_j (ln p_j - ln s_{i_j}) [+ r (ln r - ln sigma)]
+//     dloss/dz_v = (G s_v - sum_{j: i_j = v} p_j - [v not listed] s_v r / sigma) / tau,      G = sum_j p_j [+ r]
+// sigma of a peaked student is small: as 1 - sum s_{i_j} it would have no digits left, so the listed entries are kept OUT of
+// the running sum, and S = S_rest + sum_listed exp((z - m) / tau).
+//
+// Forward alone (distill_forward_kernel): the row streams through registers once, bound by HBM.  Which vectors hold listed entries stands
+// in a bitmap in shared memory, four words per warp and round, so an ordinary round pays one 16-byte shared load and a
+// test; the marked vectors are left out there, and a warp of its own (which also fetches the teacher's entries and their logits)
+// adds the unlisted entries of each from the vector itself.
+//
+// Gradient (distill_backward_kernel): a map over the row from the forward's {m, S, G, r / sigma}; the listed entries are written
+// afterwards.
+#include <cooperative_groups.h>
+
+#include <type_traits>
+
+#include "common.cuh"
+#include "grpo_loss.cuh"
+#include "row_sweep.cuh"
+
+namespace dppo {
+using namespace packed;
+namespace cg = cooperative_groups;
+
+namespace distill {
+using namespace sweep;
+
+constexpr int kMaxListed = 128;
+constexpr int kMaxCluster = 8;
+constexpr int kMaxV = 1 << 20;
+constexpr double kLeastRest = 1.0 / 65536.0;       // a remainder up to this is the rounding of f32 log-probs: it counts as none
+constexpr uint32_t kAll = 0xffffffffu;
+
+struct Args {
+    const char* logits;
+    const int32_t* ids;
+    const float* logp;
+    const int32_t* n_tokens_dev;
+    const float* weight;                           // gradient: dL/dloss of each row, or NULL (1)
+    float *loss, *lse;
+    float4* stats;
+    const float4* stats_in;
+    char* dlogits;
+    int32_t* status;
+    long long T_max, row_bytes;
+    int V, k, mode, in_place;
+    int chunks, chunk_vecs;                        // gradient: a row is taken in `chunks` pieces of chunk_vecs vectors
+    float c;
+    double inv_tau;
+};
+
+__device__ __forceinline__ long long rows_of(const Args& a) {
+    return a.n_tokens_dev ? min((long long)*a.n_tokens_dev, a.T_max) : a.T_max;
+}
+
+// ---- the teacher's entries of a row, by a warp: entry i * 32 + lane in slot i of a lane ------------------
+template <int kPer> struct Listed {
+    int id[kPer];                                  // -1: no entry
+    double p[kPer];                                // 0 where there is none
+    float z[kPer];                                 // the student's logit, -inf where there is none
+    bool first[kPer];                              // no earlier entry has this id
+    bool bad;                                      // (all lanes) an id outside [-1, V)
+};
+
+template <int kPer> __device__ __forceinline__ void listed_ids(const Args& a, long long t, int lane, Listed<kPer>& e, float (&lp)[kPer]) {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int j = i * 32 + lane;
+        e.id[i] = j < a.k ? a.ids[t * a.k + j] : -1;
+        lp[i] = j < a.k ? a.logp[t * a.k + j] : -INFINITY;
+        bad = bad || e.id[i] < -1 || e.id[i] >= a.V;
+        if (e.id[i] < 0 || e.id[i] >= a.V) e.id[i] = -1;
+    }
+    e.bad = __any_sync(kAll, bad);
+}
+template <bool kBf16, int kPer> __device__ __forceinline__ void listed_logits(const char* row, Listed<kPer>& e) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) e.z[i] = e.id[i] >= 0 ? Elems<kBf16>::load1(row, e.id[i]) : -INFINITY;
+}
+template <int kPer> __device__ __forceinline__ void listed_probs(const float (&lp)[kPer], Listed<kPer>& e) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) e.p[i] = e.id[i] >= 0 ? exp((double)lp[i]) : 0.0;
+}
+// Which entries are the first with their id.  together: their p, added up in the order of the entries, goes to the first.
+template <int kPer> __device__ __forceinline__ void listed_first(const Args& a, int lane, Listed<kPer>& e, bool together) {
+    if constexpr (kPer == 1) {                     // mostly no id comes twice
+        const unsigned peers = __match_any_sync(kAll, e.id[0]);
+        e.first[0] = e.id[0] >= 0 && __ffs(peers) - 1 == lane;
+        if (!__any_sync(kAll, e.id[0] >= 0 && !e.first[0])) return;
+    }
+    double sum[kPer];
+    bool first[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) { sum[i] = 0.0; first[i] = e.id[i] >= 0; }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+#pragma unroll 1
+        for (int l = 0; l < 32 && i * 32 + l < a.k; ++l) {
+            const int o = __shfl_sync(kAll, e.id[i], l);
+            const double po = together ? __shfl_sync(kAll, e.p[i], l) : 0.0;
+#pragma unroll
+            for (int n = 0; n < kPer; ++n) {
+                if (o != e.id[n]) continue;
+                sum[n] += po;
+                if (i * 32 + l < n * 32 + lane) first[n] = false;
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        e.first[i] = first[i];
+        if (together) e.p[i] = sum[i];             // of an entry that is not the first: not used again
+    }
+}
+__device__ __forceinline__ double warp_sum_f64(double v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
+    return v;
+}
+
+// ---- the row's loss from its parts ---------------------------------------------------------------------
+struct RowOut {                                    // in every lane
+    float m, S, G, share;                          // what the backward call reads
+    double norm;                                   // the listed p times this are the loss's p
+    float loss, lse;
+    bool zero;                                     // no gradient: an empty row or a bad id
+};
+// rest: the row without its listed entries.  The exponentials of the listed ones go to ej.
+template <int kPer> __device__ __forceinline__ RowOut row_finish(const Args& a, const Listed<kPer>& e, const float (&lp)[kPer], const Part& rest, float (&ej)[kPer]) {
+    float zmax = kLowest;
+    bool bad = rest.bad;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        bad = bad || !(e.z[i] < INFINITY);
+        if (e.z[i] < INFINITY) zmax = fmaxf(zmax, e.z[i]);
+    }
+    bad = __any_sync(kAll, bad);
+    const float M = fmaxf(rest.m, warp_max_f32(zmax));
+    const float Sr = rest.S > 0.0f ? rest.S * ex2((rest.m - M) * a.c) : 0.0f;
+    float Sl = 0.0f;
+    double P = 0.0, B = 0.0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const double y = ((double)e.z[i] - (double)M) * a.inv_tau;
+        ej[i] = e.id[i] >= 0 ? ex2((e.z[i] - M) * a.c) : 0.0f;
+        if (e.first[i]) Sl += ej[i];
+        P += e.p[i];
+        if (e.p[i] != 0.0) B += e.p[i] * ((double)lp[i] - y);
+    }
+    Sl = warp_sum(Sl); P = warp_sum_f64(P); B = warp_sum_f64(B);
+    const double S = (double)Sr + (double)Sl, l = log(S);
+    RowOut o;
+    o.norm = 1.0;
+    double G = P, r = 0.0, loss;
+    const bool empty = !(S > 0.0) && !bad;
+    if (a.mode == DPPO_DISTILL_NORMALIZED) {
+        o.norm = P > 0.0 ? 1.0 / P : 0.0;
+        G = P > 0.0 ? 1.0 : P;                     // a NaN stays one
+        loss = P > 0.0 ? B / P - log(P) + l : P;
+    } else {
+        loss = P != 0.0 ? B + P * l : 0.0;
+        if (a.mode == DPPO_DISTILL_REST) {
+            r = 1.0 - P > kLeastRest ? 1.0 - P : 0.0;
+            G = P + r;
+            if (r > 0.0) loss += r * (log(r) - (log((double)Sr) - l));
+        }
+    }
+    if (empty) loss = P > 0.0 ? INFINITY : P != 0.0 ? P : 0.0;
+    const float nan = __int_as_float(0x7fffffff);
+    o.m = bad ? nan : empty ? -INFINITY : M;
+    o.S = (float)S; o.G = (float)G;
+    o.share = r > 0.0 ? (float)(r * S / (double)Sr) : 0.0f;
+    if (bad) o.S = o.G = o.share = nan;
+    o.loss = bad ? nan : e.bad ? 0.0f : (float)loss;
+    o.lse = bad ? nan : empty ? -INFINITY : (float)((double)M * a.inv_tau + l);
+    o.zero = e.bad || empty;
+    if (e.bad) { o.G = 0.0f; o.share = 0.0f; }
+    return o;
+}
+__device__ __forceinline__ void row_write(const Args& a, long long t, const RowOut& o, bool bad_id, int lane) {
+    if (lane != 0) return;
+    if (a.loss) a.loss[t] = o.loss;
+    if (a.lse) a.lse[t] = o.lse;
+    if (a.stats) a.stats[t] = make_float4(o.m, o.S, o.G, o.share);
+    if (bad_id) set_status(a.status, DPPO_STATUS_BAD_TARGET);
+}
+
+// ---- forward: a CTA per row, or the CTAs of a cluster ---------------------------------------------------
+template <int kThreads> struct FwdShared {
+    Part part[kThreads / 32];
+    Part row;
+    unsigned tail_listed;                          // of the V % kPerVec entries behind the last vector
+};
+
+// Words of the bitmap of a part of n vectors.
+template <int kThreads> __host__ __device__ constexpr int bitmap_words(int n) {
+    return (n + kRound * kThreads - 1) / (kRound * kThreads) * (kRound * kThreads / 32);
+}
+
+template <bool kBf16, int kThreads, int kPer, bool kCluster>
+__global__ void __launch_bounds__(kThreads + 32)
+distill_forward_kernel(const Args a) {
+    constexpr int kLog2 = kBf16 ? 3 : 2, kPerVec = 1 << kLog2, kWarps = kThreads / 32;
+    extern __shared__ uint4 bitmap[];
+    __shared__ FwdShared<kThreads> sh;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    wait_for_previous();
+    const long long T = rows_of(a);
+    unsigned rank = 0, C = 1;
+    if constexpr (kCluster) { C = cg::this_cluster().num_blocks(); rank = cg::this_cluster().block_rank(); }
+    const int log2C = 31 - __clz((int)C);
+    const long long t = (long long)(blockIdx.x >> log2C);
+    if (t >= T) return;                                            // the whole cluster leaves together
+    const char* row = a.logits + t * a.row_bytes;
+    const int nvec = a.V >> kLog2;
+    const int v0 = (int)((long long)nvec * rank >> log2C), v1 = (int)((long long)nvec * (rank + 1) >> log2C);
+    const bool last = rank == C - 1;
+    const int n_rounds = (v1 - v0 + kRound * kThreads - 1) / (kRound * kThreads);
+
+    Listed<kPer> e;
+    float lp[kPer];
+    uint4 q[kRound];
+    auto load = [&](int it) {
+        const int i = v0 + it * (kRound * kThreads) + tid;
+        if (i - tid + kRound * kThreads <= v1) {
+#pragma unroll
+            for (int u = 0; u < kRound; ++u) q[u] = load_vec(row + (size_t)(i + u * kThreads) * 16);
+        } else {                                                   // the part's last vectors
+#pragma unroll
+            for (int u = 0; u < kRound; ++u)
+                q[u] = i + u * kThreads < v1 ? load_vec(row + (size_t)(i + u * kThreads) * 16) : masked_vec<kBf16>();
+        }
+    };
+    for (int i = tid; i < bitmap_words<kThreads>(v1 - v0) / 4; i += kThreads + 32) bitmap[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (tid == 0) sh.tail_listed = 0;
+    if (warp == kWarps) listed_ids<kPer>(a, t, lane, e, lp);
+    __syncthreads();
+    if (warp == kWarps) {
+        uint32_t* words = reinterpret_cast<uint32_t*>(bitmap);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int v = e.id[i] >> kLog2, rel = v - v0;
+            if (e.id[i] < 0) continue;
+            if (v >= nvec) {
+                atomicOr(&sh.tail_listed, 1u << (e.id[i] & (kPerVec - 1)));
+            } else if (rel >= 0 && v < v1) {
+                const int it = rel / (kRound * kThreads), u = rel / kThreads % kRound, w = rel % kThreads >> 5;
+                atomicOr(&words[(it * kWarps + w) * kRound + u], 1u << (rel & 31));
+            }
+        }
+    } else if (n_rounds > 0) {
+        load(0);                                                   // under way while the bitmap is finished
+    }
+    __syncthreads();
+
+    if (warp < kWarps) {
+        Sum acc;
+        sum_init(acc, kLowest, a.c);
+        for (int it = 0; it < n_rounds; ++it) {
+            if (it > 0) load(it);
+            const uint4 b = bitmap[it * kWarps + warp];
+            if (b.x | b.y | b.z | b.w) {
+                const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int u = 0; u < kRound; ++u)
+                    if (w[u] >> lane & 1u) q[u] = masked_vec<kBf16>();
+            }
+            sum_vecs<kBf16, kRound>(acc, q, a.c);
+        }
+        Part p = sum_part(acc);
+        if (last && (nvec << kLog2) + tid < a.V && !(sh.tail_listed >> tid & 1u)) part_one(p, Elems<kBf16>::load1(row, (nvec << kLog2) + tid), a.c);
+        p = part_warp(p, a.c);
+        if (lane == 0) sh.part[warp] = p;
+    }
+    Part hot = part_none();                                        // the unlisted entries of the marked vectors
+    if (warp == kWarps) {
+        listed_probs<kPer>(lp, e);
+        listed_logits<kBf16, kPer>(row, e);
+        int vec[kPer];
+        unsigned out[kPer];
+        uint4 hv[kPer];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int v = e.id[i] >> kLog2;
+            vec[i] = e.id[i] >= 0 && v >= v0 && v < v1 ? v : -1;
+            out[i] = 0;
+            if (vec[i] >= 0) hv[i] = load_vec(row + (size_t)v * 16);
+        }
+        // the first entry of each marked vector takes it, without what any entry lists there
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+#pragma unroll 1
+            for (int l = 0; l < 32 && i * 32 + l < a.k; ++l) {
+                const int o = __shfl_sync(kAll, e.id[i], l);
+#pragma unroll
+                for (int n = 0; n < kPer; ++n) {
+                    if (o < 0 || (o >> kLog2) != vec[n]) continue;
+                    out[n] |= 1u << (o & (kPerVec - 1));
+                    if (i * 32 + l < n * 32 + lane) out[n] |= 1u << 31;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (vec[i] < 0 || out[i] >> 31) continue;
+            float f[kPerVec];
+            Elems<kBf16>::unpack(hv[i], f);
+#pragma unroll
+            for (int j = 0; j < kPerVec; ++j)
+                if (!(out[i] >> j & 1u)) part_one(hot, f[j], a.c);
+        }
+        listed_first<kPer>(a, lane, e, false);
+    }
+    __syncthreads();
+    Part rest = part_none();
+    if (warp == kWarps) {
+        if (lane < kWarps) {                                       // kWarps <= 16: one part per lane, then the two joined
+            const Part o = sh.part[lane];
+            const float M = fmaxf(o.m, hot.m);
+            Part x = o;
+            part_to(x, M, a.c); part_to(hot, M, a.c);
+            rest = {M, x.S + hot.S, x.bad | hot.bad};
+        } else {
+            rest = hot;
+        }
+        rest = part_warp(rest, a.c);
+    }
+    if constexpr (kCluster) {
+        cg::cluster_group cl = cg::this_cluster();
+        if (warp == kWarps && lane == 0) sh.row = rest;
+        cl.sync();                                                 // every CTA's part is in its shared memory
+        if (rank != 0) {                                           // ... which lasts until the first CTA has read it
+            let_next_start();
+            cl.sync();
+            return;
+        }
+        if (warp == kWarps) {
+            rest = lane < (int)C ? cl.map_shared_rank(&sh, lane)->row : part_none();
+            rest = part_warp(rest, a.c);
+        }
+        cl.sync();
+    }
+    let_next_start();
+    if (warp == kWarps) {
+        float ej[kPer];
+        const RowOut o = row_finish<kPer>(a, e, lp, rest, ej);
+        row_write(a, t, o, e.bad, lane);
+    }
+}
+
+// ---- gradient from the forward's statistics ---------------------------------------------------------------
+template <bool kBf16, int kThreads, int kTeams, int kUnroll, int kPer>
+__global__ void __launch_bounds__(kThreads * kTeams)
+distill_backward_kernel(const Args a) {
+    constexpr int kPerVec = Elems<kBf16>::kPerVec, kLog2 = kBf16 ? 3 : 2;
+    const int team = kTeams == 1 ? 0 : threadIdx.x / kThreads;
+    const int tid = kTeams == 1 ? threadIdx.x : threadIdx.x % kThreads, lane = tid & 31;
+    enter_kernel();
+    const long long T = rows_of(a);
+    const long long item = (long long)blockIdx.x * kTeams + team;
+    const long long t = a.chunks == 1 ? item : item / a.chunks;
+    const int chunk = a.chunks == 1 ? 0 : (int)(item - t * a.chunks);
+    if (t >= T) return;                                            // a team is a warp, or the whole CTA
+    const char* row = a.logits + t * a.row_bytes;
+    char* out = a.dlogits + t * a.row_bytes;
+    const int nvec = a.V >> kLog2, tail0 = nvec << kLog2;
+    const int v0 = chunk * a.chunk_vecs, v1 = min(nvec, v0 + a.chunk_vecs);
+    const bool last = chunk == a.chunks - 1;
+    const float4 st = a.stats_in[t];
+    const float wt = (float)((a.weight ? (double)a.weight[t] : 1.0) * a.inv_tau);
+
+    // what is listed in this piece: its ids now, the rest when the sweep is done (in place: its logits before anything is written)
+    Listed<kPer> e;
+    float lp[kPer];
+    if (tid < 32) {
+        listed_ids<kPer>(a, t, lane, e, lp);
+        if (a.in_place) listed_logits<kBf16, kPer>(row, e);
+    }
+    if (a.in_place) { if constexpr (kThreads == 32) __syncwarp(); else __syncthreads(); }
+
+    const bool empty = st.x == -INFINITY;
+    const float inv = st.y > 0.0f || st.y != st.y ? 1.0f / st.y : 0.0f;
+    // share = inf: nothing unlisted has a probability, so nothing is multiplied by it
+    const float coef = empty || st.w == INFINITY ? 0.0f : wt * (st.z - st.w) * inv;
+    const bool zero = empty || coef == 0.0f;
+    const f32x2 c2 = pair_of(a.c, a.c), g2 = pair_of(coef, coef);
+    const float r = st.x * a.c;
+    const bool quick = fabsf(r) <= 1048576.0f && fabsf(st.x) <= 1e37f;             // as in the forward's sum
+    const f32x2 nr2 = pair_of(-r, -r), nm2 = pair_of(-st.x, -st.x);
+    const float res = quick ? fmaf(st.x, a.c, -r) : 0.0f;
+    const f32x2 gq2 = pair_of(coef * ex2(-res), coef * ex2(-res));
+    auto put = [&](const uint4& q, int i, auto is_quick) {
+        float z[kPerVec];
+        Elems<kBf16>::unpack(q, z);
+#pragma unroll
+        for (int j = 0; j < kPerVec; j += 2) {
+            float y0, y1;
+            if constexpr (decltype(is_quick)::value) unpair(fma2(pair_of(z[j], z[j + 1]), c2, nr2), y0, y1);
+            else unpair(mul2(add2(pair_of(z[j], z[j + 1]), nm2), c2), y0, y1);
+            unpair(mul2(pair_of(ex2(y0), ex2(y1)), decltype(is_quick)::value ? gq2 : g2), z[j], z[j + 1]);
+        }
+        __stcs(reinterpret_cast<uint4*>(out) + i, Elems<kBf16>::pack(z));
+    };
+    auto sweep = [&](auto is_quick) {
+        for (int i = v0 + tid; i - tid < v1; i += kUnroll * kThreads) {        // all loads of a round before its stores
+            uint4 q[kUnroll];
+            if (i - tid + kUnroll * kThreads <= v1) {
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) q[u] = load_vec_rw(row + (size_t)(i + u * kThreads) * 16);
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) put(q[u], i + u * kThreads, is_quick);
+            } else {
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u)
+                    if (i + u * kThreads < v1) q[u] = load_vec_rw(row + (size_t)(i + u * kThreads) * 16);
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u)
+                    if (i + u * kThreads < v1) put(q[u], i + u * kThreads, is_quick);
+            }
+        }
+    };
+    if (zero) {
+        for (int i = v0 + tid; i < v1; i += kThreads) __stcs(reinterpret_cast<uint4*>(out) + i, make_uint4(0u, 0u, 0u, 0u));
+    } else if (quick) {
+        sweep(std::true_type());
+    } else {
+        sweep(std::false_type());
+    }
+    if (last && tail0 + tid < a.V) {
+        const float z = Elems<kBf16>::load1(row, tail0 + tid);
+        Elems<kBf16>::store1(out, tail0 + tid, zero ? 0.0f : coef * ex2((z - st.x) * a.c));
+    }
+    if constexpr (kThreads == 32) __syncwarp(); else __syncthreads();          // the listed entries' places have been written
+    if (tid >= 32) return;
+    if (e.bad) {
+        if (lane == 0 && chunk == 0) set_status(a.status, DPPO_STATUS_BAD_TARGET);
+        return;                                                    // G = 0: the row is zero
+    }
+    bool here = false;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) here = here || (e.id[i] >= 0 && ((e.id[i] >> kLog2) >= nvec ? last : (e.id[i] >> kLog2) >= v0 && (e.id[i] >> kLog2) < v1));
+    if (empty || !__any_sync(kAll, here)) return;
+    if (!a.in_place) listed_logits<kBf16, kPer>(row, e);
+    listed_probs<kPer>(lp, e);
+    double norm = 1.0;
+    if (a.mode == DPPO_DISTILL_NORMALIZED) {
+        double P = 0.0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) P += e.p[i];
+        P = warp_sum_f64(P);
+        norm = P > 0.0 ? 1.0 / P : 0.0;
+    }
+    listed_first<kPer>(a, lane, e, true);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int v = e.id[i] >> kLog2;
+        if (!e.first[i] || !(v >= nvec ? last : v >= v0 && v < v1)) continue;
+        const float s = ex2((e.z[i] - st.x) * a.c) * inv;
+        Elems<kBf16>::store1(out, e.id[i], wt * (float)((double)s * (double)st.z - e.p[i] * norm));
+    }
+}
+
+// ---- host side -------------------------------------------------------------------------------------------
+template <bool kBf16, int kThreads, int kPer, bool kCluster> static int launch_fwd(const Args& a, int C, cudaStream_t s) {
+    auto kernel = distill_forward_kernel<kBf16, kThreads, kPer, kCluster>;
+    const int nvec = a.V >> (kBf16 ? 3 : 2);
+    const size_t smem = (size_t)bitmap_words<kThreads>((nvec + C - 1) / C) * 4;       // 32 KB at kMaxV
+    if (a.T_max * C > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "distill_topk: T_max=%lld needs too large a grid", a.T_max);
+    return launch_after("distill_topk launch", kernel, a.T_max * C, kThreads + 32, smem, s, kCluster ? C : 1, a);
+}
+
+template <bool kBf16, int kPer> static int run_fwd(const Args& a, cudaStream_t s) {
+    const int nvec = a.V >> (kBf16 ? 3 : 2);
+    const long long sms = sm_count();
+    int C = 1;
+    if (nvec > 4096)
+        while (C < kMaxCluster && a.T_max * C < 2 * sms) C *= 2;
+    if (nvec <= 512) return launch_fwd<kBf16, 128, kPer, false>(a, 1, s);
+    if (C == 1) return launch_fwd<kBf16, 128, kPer, false>(a, 1, s);
+    return launch_fwd<kBf16, 256, kPer, true>(a, C, s);
+}
+
+template <bool kBf16, int kThreads, int kTeams, int kUnroll, int kPer> static int launch_bwd(const Args& a, cudaStream_t s) {
+    const long long ctas = (a.T_max * a.chunks + kTeams - 1) / kTeams;
+    if (ctas > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "distill_topk_backward: T_max=%lld needs too large a grid", a.T_max);
+    return launch_after("distill_topk_backward launch", distill_backward_kernel<kBf16, kThreads, kTeams, kUnroll, kPer>, ctas, kThreads * kTeams, 0, s, 1, a);
+}
+
+template <bool kBf16, int kPer> static int run_bwd(Args a, cudaStream_t s) {
+    const int nvec = a.V >> (kBf16 ? 3 : 2);
+    a.chunks = 1; a.chunk_vecs = nvec;
+    if (nvec <= 320) return launch_bwd<kBf16, 32, 4, 4, kPer>(a, s);
+    a.chunk_vecs = 512;
+    a.chunks = (nvec + 511) / 512;
+    return launch_bwd<kBf16, 128, 1, 4, kPer>(a, s);
+}
+
+// Checks that both calls make; 0 or the error.
+static int check(const dppo_distill_params* p, const char* what, const void* logits, const void* top_ids, const void* top_logp, const void* stats,
+                 const void* dlogits) {
+    if (!p) return fail(DPPO_ERR_INVALID_ARG, "%s: NULL params", what);
+    if (p->T_max < 0 || p->V < 1) return fail(DPPO_ERR_INVALID_ARG, "%s: T_max=%lld V=%d", what, (long long)p->T_max, p->V);
+    if (p->dtype != DPPO_F32 && p->dtype != DPPO_BF16) return fail(DPPO_ERR_UNSUPPORTED, "%s: dtype %d", what, p->dtype);
+    if (p->row_stride < p->V) return fail(DPPO_ERR_BAD_SHAPE, "%s: row_stride %lld < V %d", what, (long long)p->row_stride, p->V);
+    if (!(p->temperature >= 1e-6) || !(p->temperature <= 1e6)) return fail(DPPO_ERR_INVALID_ARG, "%s: temperature must be in [1e-6, 1e6]", what);
+    if (p->V > kMaxV) return fail(DPPO_ERR_BAD_SHAPE, "%s: V=%d, the limit is 2^20", what, p->V);
+    if (p->T_max >= ((int64_t)1 << 31)) return fail(DPPO_ERR_BAD_SHAPE, "%s: T_max must be below 2^31", what);
+    if (p->top_k < 1 || p->top_k > kMaxListed) return fail(DPPO_ERR_INVALID_ARG, "%s: top_k=%d (1..%d)", what, p->top_k, kMaxListed);
+    if (p->mode < DPPO_DISTILL_GIVEN || p->mode > DPPO_DISTILL_REST) return fail(DPPO_ERR_INVALID_ARG, "%s: mode %d", what, p->mode);
+    const size_t esize = p->dtype == DPPO_BF16 ? 2 : 4;
+    if (((uintptr_t)logits & 15) || ((uintptr_t)stats & 15) || ((uintptr_t)dlogits & 15) || ((size_t)p->row_stride * esize) % 16 != 0)
+        return fail(DPPO_ERR_MISALIGNED, "%s: logits / dlogits / stats base and row stride must be multiples of 16 bytes", what);
+    if (p->T_max > 0 && (!logits || !top_ids || !top_logp)) return fail(DPPO_ERR_INVALID_ARG, "%s: NULL logits, top_ids or top_logp", what);
+    return DPPO_OK;
+}
+
+static Args args_of(const dppo_distill_params* p, const void* logits, const int32_t* top_ids, const float* top_logp, const int32_t* n_tokens_dev,
+                    const float* weight, void* dlogits, int32_t* status) {
+    Args a = {};
+    a.logits = (const char*)logits; a.ids = top_ids; a.logp = top_logp; a.n_tokens_dev = n_tokens_dev; a.weight = weight;
+    a.dlogits = (char*)dlogits; a.status = status;
+    a.T_max = p->T_max; a.row_bytes = (long long)p->row_stride * (p->dtype == DPPO_BF16 ? 2 : 4);
+    a.V = p->V; a.k = p->top_k; a.mode = p->mode; a.in_place = dlogits == logits;
+    a.c = (float)(1.4426950408889634 / p->temperature); a.inv_tau = 1.0 / p->temperature;
+    return a;
+}
+
+template <bool kBf16> static int run_fwd_k(const Args& a, cudaStream_t s) { return a.k <= 32 ? run_fwd<kBf16, 1>(a, s) : run_fwd<kBf16, 4>(a, s); }
+template <bool kBf16> static int run_bwd_k(const Args& a, cudaStream_t s) { return a.k <= 32 ? run_bwd<kBf16, 1>(a, s) : run_bwd<kBf16, 4>(a, s); }
+
+}  // namespace distill
+}  // namespace dppo
+
+extern "C" int dppo_distill_topk(const dppo_distill_params* p, const void* logits, const int32_t* top_ids, const float* top_logp,
+                                 const int32_t* n_tokens_dev, const float* weight, float* loss_out, float* lse_out, float* stats,
+                                 void* dlogits, int32_t* status, void* stream) {
+    dppo::NvtxRange nvtx_range("dppo_distill_topk");
+    using namespace dppo;
+    const int rc = distill::check(p, "distill_topk", logits, top_ids, top_logp, stats, dlogits);
+    if (rc != DPPO_OK || p->T_max == 0) return rc;
+    if (dlogits && !stats) return fail(DPPO_ERR_INVALID_ARG, "distill_topk: dlogits without stats");
+    if (weight && !dlogits) return fail(DPPO_ERR_INVALID_ARG, "distill_topk: weight without dlogits");
+    distill::Args a = distill::args_of(p, logits, top_ids, top_logp, n_tokens_dev, weight, dlogits, status);
+    a.loss = loss_out; a.lse = lse_out; a.stats = (float4*)stats; a.stats_in = (const float4*)stats;
+    cudaStream_t s = (cudaStream_t)stream;
+    const int f = p->dtype == DPPO_BF16 ? distill::run_fwd_k<true>(a, s) : distill::run_fwd_k<false>(a, s);
+    if (f != DPPO_OK || !dlogits) return f;
+    return p->dtype == DPPO_BF16 ? distill::run_bwd_k<true>(a, s) : distill::run_bwd_k<false>(a, s);
+}
+
+extern "C" int dppo_distill_topk_backward(const dppo_distill_params* p, const void* logits, const int32_t* top_ids, const float* top_logp,
+                                          const int32_t* n_tokens_dev, const float* stats, const float* dloss, void* dlogits,
+                                          int32_t* status, void* stream) {
+    dppo::NvtxRange nvtx_range("dppo_distill_topk_backward");
+    using namespace dppo;
+    const int rc = distill::check(p, "distill_topk_backward", logits, top_ids, top_logp, stats, dlogits);
+    if (rc != DPPO_OK || p->T_max == 0) return rc;
+    if (!stats || !dlogits) return fail(DPPO_ERR_INVALID_ARG, "distill_topk_backward: NULL stats or dlogits");
+    distill::Args a = distill::args_of(p, logits, top_ids, top_logp, n_tokens_dev, dloss, dlogits, status);
+    a.stats_in = (const float4*)stats;
+    return p->dtype == DPPO_BF16 ? distill::run_bwd_k<true>(a, (cudaStream_t)stream) : distill::run_bwd_k<false>(a, (cudaStream_t)stream);
+}
