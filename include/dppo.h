@@ -486,6 +486,47 @@ int dppo_distill_topk_backward(const dppo_distill_params* p, const void* logits,
                                const int32_t* n_tokens_dev, const float* stats, const float* dloss, void* dlogits,
                                int32_t* status, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Verification of drafted tokens (an earlier completion, a smaller model's proposal) against the target policy, from given random
+ * numbers: the accepted tokens and the one after them are distributed as the target's own samples.
+ *
+ * Sequence b has the drafts y_j, j < n, n = cu_drafts[b + 1] - cu_drafts[b], at cu_drafts[b] + j; rows of the target (and of its outputs)
+ * lie at cu_drafts[b] + b + j, j = 0 .. n: one more than drafts.  p_j = softmax(target row / temperature); q_j = softmax(draft row /
+ * draft_temperature), or, without draft logits, 1 at y_j (drafts copied from somewhere).
+ *   y_j is accepted while u_j q_j(y_j) < p_j(y_j).
+ *   After a first rejection at j the next token is argmax_v max(p_j(v) - q_j(v), 0) / e_b(v) (if p_j <= q_j everywhere:
+ *   argmax_v p_j(v) / e_b(v)), after n acceptances argmax_v p_n(v) / e_b(v); ties to the lower index.  With independent u uniform
+ *   in [0, 1) and e exponential that is a sample.
+ *   tokens_out: the accepted drafts, the next token, then -1;  logp_out: their log-probs under the target, then 0.
+ * Logits at -inf are masked.  A draft row that its mask leaves empty has q = 0.  At a row with a NaN or +inf, the target's or the draft's,
+ * the sequence ends: next token -1, log-prob NaN.  A target row that its mask leaves empty: next token -1, log-prob -inf.
+ */
+typedef struct {
+    int64_t T_max;          /* drafts of all sequences, upper bound                                  */
+    int32_t n_seqs;
+    int32_t V;              /* vocabulary size, up to 2^30                                           */
+    int32_t dtype;          /* dppo_dtype of both policies' logits                                   */
+    int64_t target_stride, draft_stride;  /* elements between rows (>= V; bytes a multiple of 16)    */
+    int64_t noise_stride;   /* elements between rows of noise (>= V; a multiple of 4)                */
+    double temperature, draft_temperature;      /* 1e-6 .. 1e6                                       */
+} dppo_verify_params;
+
+size_t dppo_verify_drafts_workspace_bytes(const dppo_verify_params* p);
+
+/*   target_logits [(T_max + n_seqs) x target_stride], draft_logits [T_max x draft_stride] or NULL, of dtype
+ *   drafts        i32 [T_max];  cu_drafts i32 [n_seqs + 1], non-decreasing from 0, the last at most T_max; rows past the last
+ *                 sequence are neither read nor written
+ *   uniforms      f32 [T_max] in [0, 1);  noise f32 [n_seqs x noise_stride], positive
+ *   n_accepted    i32 [n_seqs] out;  tokens_out i32, logp_out f32 [T_max + n_seqs] out
+ *   workspace     at least dppo_verify_drafts_workspace_bytes, 16-byte aligned
+ * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED, UNSUPPORTED (dtype), WORKSPACE_TOO_SMALL.
+ * Device status: BAD_TARGET (a drafted id outside [0, V) is rejected), BAD_SEGMENTS (cu_drafts decreases, or ends past T_max: such a
+ * sequence has n_accepted 0 and no other output).
+ */
+int dppo_verify_drafts(const dppo_verify_params* p, const void* target_logits, const void* draft_logits, const int32_t* drafts,
+                       const int32_t* cu_drafts, const float* uniforms, const float* noise, int32_t* n_accepted, int32_t* tokens_out,
+                       float* logp_out, void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -95,6 +95,12 @@ class DistillParams(ctypes.Structure):
                 ("temperature", ctypes.c_double)]
 
 
+class VerifyParams(ctypes.Structure):
+    _fields_ = [("T_max", ctypes.c_int64), ("n_seqs", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("target_stride", ctypes.c_int64), ("draft_stride", ctypes.c_int64), ("noise_stride", ctypes.c_int64),
+                ("temperature", ctypes.c_double), ("draft_temperature", ctypes.c_double)]
+
+
 DISTILL_GIVEN, DISTILL_NORMALIZED, DISTILL_REST = 0, 1, 2
 MAX_LISTED = 128
 MAX_TOP_K = 32
@@ -144,6 +150,10 @@ lib.dppo_distill_topk.restype = ctypes.c_int
 lib.dppo_distill_topk.argtypes = [ctypes.POINTER(DistillParams)] + [_vp] * 11
 lib.dppo_distill_topk_backward.restype = ctypes.c_int
 lib.dppo_distill_topk_backward.argtypes = [ctypes.POINTER(DistillParams)] + [_vp] * 9
+lib.dppo_verify_drafts_workspace_bytes.restype = ctypes.c_size_t
+lib.dppo_verify_drafts_workspace_bytes.argtypes = [ctypes.POINTER(VerifyParams)]
+lib.dppo_verify_drafts.restype = ctypes.c_int
+lib.dppo_verify_drafts.argtypes = [ctypes.POINTER(VerifyParams)] + [_vp] * 10 + [ctypes.c_size_t, _vp, _vp]
 
 
 def _ptr(x):
@@ -440,3 +450,20 @@ def distill_topk_backward(params, logits, top_ids, top_logp, n_tokens_dev, stats
         ctypes.byref(p), _mat(logits, "logits", d, dt, T, V, ld), _arr(top_ids, "top_ids", d, _i32, k), _arr(top_logp, "top_logp", d, _f32, k),
         _arr(n_tokens_dev, "n_tokens_dev", d, _i32, 1), _arr(stats, "stats", d, _f32, 4 * T), _arr(dloss, "dloss", d, _f32, T),
         _mat(dlogits, "dlogits", d, dt, T, V, ld), _arr(status, "status", d, _i32, 1), _stream(stream)))
+
+
+def verify_drafts_workspace_bytes(params):
+    return lib.dppo_verify_drafts_workspace_bytes(ctypes.byref(params))
+
+
+def verify_drafts(params, target_logits, draft_logits, drafts, cu_drafts, uniforms, noise, n_accepted, tokens_out, logp_out, workspace,
+                  workspace_bytes, status=None, stream=None):
+    p, d = params, _device()
+    T, B, V, dt = p.T_max, p.n_seqs, p.V, _TORCH_DTYPE.get(p.dtype)
+    _check(lib.dppo_verify_drafts(
+        ctypes.byref(p), _mat(target_logits, "target_logits", d, dt, T + B, V, p.target_stride),
+        _mat(draft_logits, "draft_logits", d, dt, T, V, p.draft_stride), _arr(drafts, "drafts", d, _i32, T),
+        _arr(cu_drafts, "cu_drafts", d, _i32, B + 1), _arr(uniforms, "uniforms", d, _f32, T),
+        _mat(noise, "noise", d, _f32, B, V, p.noise_stride), _arr(n_accepted, "n_accepted", d, _i32, B),
+        _arr(tokens_out, "tokens_out", d, _i32, T + B), _arr(logp_out, "logp_out", d, _f32, T + B),
+        _arr(workspace, "workspace", d, torch.uint8, workspace_bytes), workspace_bytes, _arr(status, "status", d, _i32, 1), _stream(stream)))

@@ -85,7 +85,7 @@ template <bool kBf16, int kPer> __device__ __forceinline__ void listed_logits(co
 }
 template <int kPer> __device__ __forceinline__ void listed_probs(const float (&lp)[kPer], Listed<kPer>& e) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) e.p[i] = e.id[i] >= 0 ? exp((double)lp[i]) : 0.0;
+    for (int i = 0; i < kPer; ++i) e.p[i] = e.id[i] >= 0 ? exp64((double)lp[i]) : 0.0;
 }
 // Which entries are the first with their id.  together: their p, added up in the order of the entries, goes to the first.
 template <int kPer> __device__ __forceinline__ void listed_first(const Args& a, int lane, Listed<kPer>& e, bool together) {
@@ -154,28 +154,28 @@ template <int kPer> __device__ __forceinline__ RowOut row_finish(const Args& a, 
         if (e.p[i] != 0.0) B += e.p[i] * ((double)lp[i] - y);
     }
     Sl = warp_sum(Sl); P = warp_sum_f64(P); B = warp_sum_f64(B);
-    const double S = (double)Sr + (double)Sl, l = log(S);
+    const double S = (double)Sr + (double)Sl, l = log64(S);
     RowOut o;
     o.norm = 1.0;
     double G = P, r = 0.0, loss;
     const bool empty = !(S > 0.0) && !bad;
     if (a.mode == DPPO_DISTILL_NORMALIZED) {
-        o.norm = P > 0.0 ? 1.0 / P : 0.0;
+        o.norm = P > 0.0 ? inv64(P) : 0.0;
         G = P > 0.0 ? 1.0 : P;                     // a NaN stays one
-        loss = P > 0.0 ? B / P - log(P) + l : P;
+        loss = P > 0.0 ? B * o.norm - log64(P) + l : P;
     } else {
         loss = P != 0.0 ? B + P * l : 0.0;
         if (a.mode == DPPO_DISTILL_REST) {
             r = 1.0 - P > kLeastRest ? 1.0 - P : 0.0;
             G = P + r;
-            if (r > 0.0) loss += r * (log(r) - (log((double)Sr) - l));
+            if (r > 0.0) loss += r * (log64(r) - (log64((double)Sr) - l));
         }
     }
     if (empty) loss = P > 0.0 ? INFINITY : P != 0.0 ? P : 0.0;
     const float nan = __int_as_float(0x7fffffff);
     o.m = bad ? nan : empty ? -INFINITY : M;
     o.S = (float)S; o.G = (float)G;
-    o.share = r > 0.0 ? (float)(r * S / (double)Sr) : 0.0f;
+    o.share = r > 0.0 ? (float)r * (float)S / Sr : 0.0f;
     if (bad) o.S = o.G = o.share = nan;
     o.loss = bad ? nan : e.bad ? 0.0f : (float)loss;
     o.lse = bad ? nan : empty ? -INFINITY : (float)((double)M * a.inv_tau + l);
@@ -454,7 +454,7 @@ distill_backward_kernel(const Args a) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) P += e.p[i];
         P = warp_sum_f64(P);
-        norm = P > 0.0 ? 1.0 / P : 0.0;
+        norm = P > 0.0 ? inv64(P) : 0.0;
     }
     listed_first<kPer>(a, lane, e, true);
 #pragma unroll

@@ -171,5 +171,31 @@ __device__ __forceinline__ void part_one(Part& p, float z, float c) {
     p.S += ex2((z - p.m) * c);
 }
 
+// ---- a row's scalars in 64 bits, short of the library's full precision -----------------------------------
+// e^x for x <= 700 to a relative 2^-36: x = n ln 2 + f with |f| <= ln 2 / 2, the Taylor series of e^f to f^9 / 9! (remainder
+// f^10 / 10! < 7e-12), in two halves that are under way together, and n added to the exponent.  Below -700 it is 0.
+__device__ __forceinline__ double exp64(double x) {
+    if (!(x >= -700.0)) return x != x ? x : 0.0;
+    const double n = rint(x * 1.4426950408889634);
+    const double f = fma(n, -0.6931471805599453, x), f2 = f * f;
+    const double even = fma(fma(fma(fma(1.0 / 40320, f2, 1.0 / 720), f2, 1.0 / 24), f2, 0.5), f2, 1.0);
+    const double odd = fma(fma(fma(fma(1.0 / 362880, f2, 1.0 / 5040), f2, 1.0 / 120), f2, 1.0 / 6), f2, 1.0);
+    const double r = fma(odd, f, even);
+    return __hiloint2double(__double2hiint(r) + ((int)n << 20), __double2loint(r));
+}
+// ln x of a normal f32's range (or of 0, infinity, NaN) to 1e-11: one step of Newton's method from the f32 logarithm,
+// l = l0 + d - d^2 / 2 with d = x e^-l0 - 1.
+__device__ __forceinline__ double log64(double x) {
+    const float l0 = logf((float)x);
+    if (!(fabsf(l0) < 1e3f)) return (double)l0;
+    const double d = fma(x, exp64(-(double)l0), -1.0);
+    return (double)l0 + fma(-0.5 * d, d, d);
+}
+// 1 / x to 2^-46 of it, for x in the range of normal f32 values: Newton's step from the f32 quotient.
+__device__ __forceinline__ double inv64(double x) {
+    const double y = (double)(1.0f / (float)x);
+    return y * fma(-x, y, 2.0);
+}
+
 }  // namespace sweep
 }  // namespace dppo
