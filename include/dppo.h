@@ -527,6 +527,60 @@ int dppo_verify_drafts(const dppo_verify_params* p, const void* target_logits, c
                        const int32_t* cu_drafts, const float* uniforms, const float* noise, int32_t* n_accepted, int32_t* tokens_out,
                        float* logp_out, void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Matrix product in 8-bit floating point (e4m3) with a scale for each block of 128 of the contraction: the LM-head (or any projection)
+ * of a frozen policy or teacher.  Finer scales than dppo_linear_i8's: a channel far larger than the others costs only its own
+ * block digits.
+ *
+ * Quantisation of a block (block_rows = 1: 128 columns of a row; 128: 128 rows x 128 columns; less at the edges):
+ * s = max(fl32(max |x| fl32(1/448)), 2^-126), q = e4m3(fl32(x / s)) (nearest, ties to even, held at +-448).  A block with a NaN or an
+ * infinity gets s = NaN, q = 0, so that products with it are NaN.
+ */
+typedef struct {
+    int64_t rows_max;       /* rows of x (below 2^31)                                                */
+    int32_t K;              /* columns, up to 2^30                                                   */
+    int32_t dtype;          /* dppo_dtype of x                                                       */
+    int64_t x_stride;       /* elements between rows of x (>= K; bytes a multiple of 16)             */
+    int64_t q_stride;       /* bytes between rows of q (>= K; a multiple of 16)                      */
+    int64_t scale_stride;   /* block_rows = 1: elements between the scales of consecutive blocks of columns (>= rows_max);
+                               128: between those of consecutive blocks of rows (>= ceil(K / 128))   */
+    int32_t block_rows;     /* 1 or 128                                                              */
+} dppo_quantize_f8_params;
+
+/*   x   [rows_max x x_stride] of dtype;  q  e4m3 [rows_max x q_stride] out (columns at or past K are not written)
+ *   scale  f32 out, block_rows = 1: [ceil(K / 128) x scale_stride], the scales of a block of columns side by side for the rows;
+ *          128: [ceil(rows_max / 128) x scale_stride]
+ *   n_rows_dev  i32 [1] true number of rows or NULL; rows (and blocks) past it are not touched
+ * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED, UNSUPPORTED (dtype, block_rows).
+ */
+int dppo_quantize_f8(const dppo_quantize_f8_params* p, const void* x, uint8_t* q, float* scale, const int32_t* n_rows_dev,
+                     int32_t* status, void* stream);
+
+/*   out[t, n] = sum_B x_scale[B, t] w_scale[n / 128, B] sum_{k in block B} x[t, k] w[n, k], the blocks' sums and their sum in f32,
+ * rounded once more to a bf16 out.  The order of the sums is a function of the sizes alone. */
+typedef struct {
+    int64_t M_max;          /* rows of x / upper bound of tokens (below 2^31)                        */
+    int32_t N, K;           /* output channels; contraction length                                   */
+    int64_t x_stride, w_stride;   /* bytes between rows of x and of w (>= K; multiples of 16)        */
+    int64_t out_stride;     /* elements between rows of out (>= N)                                   */
+    int64_t x_scale_stride; /* elements between rows of x_scale (>= M_max)                           */
+    int64_t w_scale_stride; /* elements between rows of w_scale (>= ceil(K / 128))                   */
+    int32_t out_dtype;      /* dppo_dtype of out                                                     */
+    int32_t variant;        /* 0: the library picks the kernel; 1 forces the CTA-pair tile kernel, 2 the
+                               kernel for few tokens (tuning aid).  101 / 102: the same two with the
+                               self-test of the bounded waits (see dppo_lmhead_params.variant): the call
+                               reports DPPO_STATUS_TIMEOUT, its output is unspecified                */
+} dppo_linear_f8_params;
+
+/*   x   e4m3 [M_max x x_stride], x_scale f32 [ceil(K / 128) x x_scale_stride];  w  e4m3 [N x w_stride], w_scale f32
+ *   [ceil(N / 128) x w_scale_stride]: as dppo_quantize_f8 leaves them
+ *   out [M_max x out_stride] of out_dtype (no alignment beyond its element's)
+ *   n_rows_dev  i32 [1] true number of tokens on the device, or NULL; rows of out past it are not written
+ * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED (x, w: base or stride), UNSUPPORTED, CUDA (tensor-map creation).  Device status: TIMEOUT.
+ */
+int dppo_linear_f8(const dppo_linear_f8_params* p, const uint8_t* x, const float* x_scale, const uint8_t* w, const float* w_scale,
+                   void* out, const int32_t* n_rows_dev, int32_t* status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -101,10 +101,25 @@ class VerifyParams(ctypes.Structure):
                 ("temperature", ctypes.c_double), ("draft_temperature", ctypes.c_double)]
 
 
+class QuantizeF8Params(ctypes.Structure):
+    _fields_ = [("rows_max", ctypes.c_int64), ("K", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64), ("q_stride", ctypes.c_int64), ("scale_stride", ctypes.c_int64),
+                ("block_rows", ctypes.c_int32)]
+
+
+class LinearF8Params(ctypes.Structure):
+    _fields_ = [("M_max", ctypes.c_int64), ("N", ctypes.c_int32), ("K", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
+                ("x_scale_stride", ctypes.c_int64), ("w_scale_stride", ctypes.c_int64),
+                ("out_dtype", ctypes.c_int32), ("variant", ctypes.c_int32)]
+
+
 DISTILL_GIVEN, DISTILL_NORMALIZED, DISTILL_REST = 0, 1, 2
 MAX_LISTED = 128
 MAX_TOP_K = 32
 LINEAR_I8_WAIT_SELF_TEST = 100     # added to dppo_linear_i8_params.variant
+LINEAR_F8_WAIT_SELF_TEST = 100     # added to dppo_linear_f8_params.variant
+F8_BLOCK = 128
 
 _vp = ctypes.c_void_p
 lib.dppo_version.restype = ctypes.c_int
@@ -154,6 +169,10 @@ lib.dppo_verify_drafts_workspace_bytes.restype = ctypes.c_size_t
 lib.dppo_verify_drafts_workspace_bytes.argtypes = [ctypes.POINTER(VerifyParams)]
 lib.dppo_verify_drafts.restype = ctypes.c_int
 lib.dppo_verify_drafts.argtypes = [ctypes.POINTER(VerifyParams)] + [_vp] * 10 + [ctypes.c_size_t, _vp, _vp]
+lib.dppo_quantize_f8.restype = ctypes.c_int
+lib.dppo_quantize_f8.argtypes = [ctypes.POINTER(QuantizeF8Params)] + [_vp] * 6
+lib.dppo_linear_f8.restype = ctypes.c_int
+lib.dppo_linear_f8.argtypes = [ctypes.POINTER(LinearF8Params)] + [_vp] * 8
 
 
 def _ptr(x):
@@ -165,7 +184,7 @@ def _ptr(x):
 
 
 _TORCH_DTYPE = {F32: torch.float32, BF16: torch.bfloat16}
-_Tensor, _f32, _i32, _i8 = torch.Tensor, torch.float32, torch.int32, torch.int8
+_Tensor, _f32, _i32, _i8, _f8 = torch.Tensor, torch.float32, torch.int32, torch.int8, torch.float8_e4m3fn
 
 
 def _arr(x, name, device, dtype, n):
@@ -467,3 +486,23 @@ def verify_drafts(params, target_logits, draft_logits, drafts, cu_drafts, unifor
         _mat(noise, "noise", d, _f32, B, V, p.noise_stride), _arr(n_accepted, "n_accepted", d, _i32, B),
         _arr(tokens_out, "tokens_out", d, _i32, T + B), _arr(logp_out, "logp_out", d, _f32, T + B),
         _arr(workspace, "workspace", d, torch.uint8, workspace_bytes), workspace_bytes, _arr(status, "status", d, _i32, 1), _stream(stream)))
+
+
+def quantize_f8(params, x, q, scale, n_rows_dev=None, status=None, stream=None):
+    p, d = params, _device()
+    M, K, blocks = p.rows_max, p.K, (p.K + 127) // 128
+    rows, cols = (blocks, M) if p.block_rows == 1 else ((M + 127) // 128, blocks)
+    _check(lib.dppo_quantize_f8(
+        ctypes.byref(p), _mat(x, "x", d, _TORCH_DTYPE.get(p.dtype), M, K, p.x_stride), _mat(q, "q", d, _f8, M, K, p.q_stride),
+        _mat(scale, "scale", d, _f32, rows, cols, p.scale_stride), _arr(n_rows_dev, "n_rows_dev", d, _i32, 1),
+        _arr(status, "status", d, _i32, 1), _stream(stream)))
+
+
+def linear_f8(params, x, x_scale, w, w_scale, out, n_rows_dev=None, status=None, stream=None):
+    p, d = params, _device()
+    M, N, K, blocks = p.M_max, p.N, p.K, (p.K + 127) // 128
+    _check(lib.dppo_linear_f8(
+        ctypes.byref(p), _mat(x, "x", d, _f8, M, K, p.x_stride), _mat(x_scale, "x_scale", d, _f32, blocks, M, p.x_scale_stride),
+        _mat(w, "w", d, _f8, N, K, p.w_stride), _mat(w_scale, "w_scale", d, _f32, (N + 127) // 128, blocks, p.w_scale_stride),
+        _mat(out, "out", d, _TORCH_DTYPE.get(p.out_dtype), M, N, p.out_stride), _arr(n_rows_dev, "n_rows_dev", d, _i32, 1),
+        _arr(status, "status", d, _i32, 1), _stream(stream)))

@@ -1,0 +1,875 @@
+// Matrix product in 8-bit floating point (e4m3) with a scale for each block of 128 of the contraction, on the 5th-generation
+// tensor cores: out[t, n] = sum_B sx[B, t] sw[n / 128, B] sum_{k in B} x[t, k] w[n, k]; and the quantisation that makes its
+// operands (a scale per token and 128 values; per 128 x 128 of the weights).
+//
+// A block of 128 codes is one 128-byte swizzle row: one stage of the TMA ring, four instructions (tcgen05.mma kind::f8f6f4, f32
+// accumulation) into a tensor-memory accumulator of its own.  The epilogue warps read that accumulator back while the next
+// block's products run, and add it, times its scales, to f32 sums in their registers: acc += v * (sx sw), packed two tokens at a time.
+// The weights take the M side (TMEM lanes = output channels): a CTA's 128 channels share one weight scale per block, so the
+// factors of a block are one number per token, formed by a warp of its own and read by the epilogue as shared-memory broadcasts; and 32
+// consecutive channels of a token are written per warp instruction whatever the row pitch of the output.
+//
+// Two kernels, as for the 8-bit integer product: CTA pairs (cta_group::2), 256 channels x up to 256 tokens, for many tokens; a CTA
+// per 128 channels with the contraction split over a cluster for few (partial sums joined in a fixed order through distributed
+// shared memory).  Every wait is bounded; on a time-out the CTA reports DPPO_STATUS_TIMEOUT, leaves its loops, lets copies and products
+// in flight finish (bounded), frees its tensor memory and returns.
+#include <cuda_fp8.h>
+
+#include <type_traits>
+
+#include "common.cuh"
+#include "grpo_loss.cuh"
+#include "tensor_core.cuh"
+
+namespace dppo {
+using namespace packed;
+
+namespace f8 {
+
+constexpr int kBK = 128;                  // codes of a block = of a stage
+constexpr int kTileM = 128;               // channels per CTA
+constexpr int kTileN = 256;               // most tokens per tile of the pair kernel
+constexpr int kBytesA = kTileM * kBK;
+constexpr int kMaxStages = 12;
+constexpr int kSlots = 8;                 // blocks whose factors are in shared memory
+constexpr int kBatch = 4;                 // blocks whose scales are under way together
+constexpr int kThreads = 384;             // producer, MMA, scale and one idle warp; 8 epilogue warps (two per TMEM lane quarter)
+constexpr int kTokenGroup = 16;           // token tiles swept together
+constexpr int kRingBytes = 6 * (kBytesA + kTileN / 2 * kBK);
+constexpr size_t kDynSmem2 = (size_t)kRingBytes + 1024;
+
+struct Args {
+    const float* x_scale;
+    const float* w_scale;
+    void* out;
+    const int32_t* n_rows_dev;
+    int32_t* status;
+    long long M_max, out_stride, xs_stride, ws_stride;
+    int N, n_ksteps, out_bf16;
+    int tile_n;                           // pair kernel: tokens per tile, a multiple of 32 up to 256
+    unsigned long long wait_limit_ns;
+    int test_extra_tx;
+};
+
+// Instruction descriptor of kind::f8f6f4: D = f32, A = B = e4m3, both K-major.
+__host__ __device__ constexpr uint32_t idesc(int m, int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
+
+__device__ __forceinline__ long long true_rows(const Args& a) {
+    return a.n_rows_dev ? min((long long)max(*a.n_rows_dev, 0), a.M_max) : a.M_max;
+}
+__device__ __forceinline__ void init_bar(unsigned long long* bar, int count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(lm_smem_u32(bar)), "r"(count));
+}
+
+// kCount consecutive tokens t0 .. of this lane's channel.
+template <bool kBf16, int kCount> __device__ __forceinline__ void store_tokens(const Args& a, long long t0, long long T, int ch, const f32x2* acc) {
+    typedef typename std::conditional<kBf16, __nv_bfloat16, float>::type Out;
+    const int nt = (int)min((long long)kCount, T - t0);
+    if (ch >= a.N) return;
+    Out* p = reinterpret_cast<Out*>(a.out) + t0 * a.out_stride + ch;
+#pragma unroll
+    for (int i = 0; i < kCount; i += 2) {
+        float x0, x1;
+        unpair(acc[i / 2], x0, x1);
+        Out o0, o1;
+        if constexpr (kBf16) { const __nv_bfloat162 h = __floats2bfloat162_rn(x0, x1); o0 = h.x; o1 = h.y; } else { o0 = x0; o1 = x1; }
+        if (i < nt) p[0] = o0;
+        if (i + 1 < nt) p[a.out_stride] = o1;
+        p += 2 * a.out_stride;
+    }
+}
+
+// acc += v * f for 32 tokens; f in shared memory.
+__device__ __forceinline__ void add_block(f32x2* acc, const uint32_t (&v)[32], uint32_t f) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) {
+        f32x2 f0, f1;
+        asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(f0), "=l"(f1) : "r"(f + i * 4));
+        acc[i / 2] = fma2(pair_of(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), f0, acc[i / 2]);
+        acc[i / 2 + 1] = fma2(pair_of(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), f1, acc[i / 2 + 1]);
+    }
+}
+
+// ---- many tokens: CTA pairs ---------------------------------------------------------------------------
+struct Shared2 {
+    alignas(16) float4 factor[kSlots][kTileN / 4];
+    unsigned long long full[kMaxStages];
+    unsigned long long empty[kMaxStages];
+    unsigned long long acc_full[2];
+    unsigned long long acc_empty[2];      // the leader's copy counts 16 arrivals: 8 epilogue warps x 2 CTAs
+    unsigned long long f_full[kSlots];
+    unsigned long long f_empty[kSlots];
+    unsigned long long drain;             // products in flight on an early way out
+    uint32_t tmem_base;
+    int abort;
+};
+static_assert(kDynSmem2 + sizeof(Shared2) <= 232448, "the ring must fit one CTA's shared memory");
+
+// Tile j of this pair: token tiles are taken kTokenGroup at a time; within a group the token tiles of one channel tile
+// follow each other, so that every weight is fetched once per group and the group's codes stay in L2.
+__device__ __forceinline__ bool tile_of(uint32_t j, int n_m2, int n_tok, int& m2, int& n) {
+    const long long id = (long long)(blockIdx.x >> 1) + (long long)j * (gridDim.x >> 1);
+    if (id >= (long long)n_m2 * n_tok) return false;
+    const long long per = (long long)kTokenGroup * n_m2;
+    const int g = (int)(id / per), local = (int)(id - (long long)g * per);
+    const int n0 = g * kTokenGroup, width = min(kTokenGroup, n_tok - n0);
+    m2 = local / width;
+    n = n0 + local - m2 * width;
+    return true;
+}
+
+template <bool kBf16>
+__global__ void __launch_bounds__(kThreads, 1)
+linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const Args a) {
+    extern __shared__ unsigned char f8_raw[];
+    __shared__ Shared2 sh;
+    const uint32_t tiles = (lm_smem_u32(f8_raw) + 1023u) & ~1023u;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    uint32_t rank;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    const bool leader = rank == 0;
+    volatile int* abort_flag = &sh.abort;
+    const int n_m2 = (a.N + 2 * kTileM - 1) / (2 * kTileM);
+    // a stage: 128 codes of K of this CTA's 128 channels and of its half of the token tile
+    const uint32_t stage_bytes = (uint32_t)(kBytesA + a.tile_n / 2 * kBK);
+    const uint32_t stages = min((uint32_t)kMaxStages, (uint32_t)kRingBytes / stage_bytes);
+
+    if (tid == 0) {
+        sh.abort = 0;
+        for (uint32_t s = 0; s < stages; ++s) { init_bar(&sh.full[s], 1); init_bar(&sh.empty[s], 1); }
+        for (int b = 0; b < 2; ++b) { init_bar(&sh.acc_full[b], 1); init_bar(&sh.acc_empty[b], 16); }
+        for (int b = 0; b < kSlots; ++b) { init_bar(&sh.f_full[b], 1); init_bar(&sh.f_empty[b], 8); }
+        init_bar(&sh.drain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                     :: "r"(lm_smem_u32(&sh.tmem_base)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    __syncwarp();
+    lm_cluster_sync();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem_base = sh.tmem_base;
+    enter_kernel();
+    const long long T = true_rows(a);
+    const int n_tok = (int)((T + a.tile_n - 1) / a.tile_n);
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ TMA producer (both CTAs)
+        if (lane == 0) {
+            uint32_t it = 0, s = 0, use = 0;
+            int m2, n;
+            for (uint32_t j = 0; tile_of(j, n_m2, n_tok, m2, n) && !*abort_flag; ++j) {
+                const int row_w = (2 * m2 + (int)rank) * kTileM, row_x = n * a.tile_n + (int)rank * (a.tile_n / 2);
+                for (int k = 0; k < a.n_ksteps; ++k, ++it, s = s + 1 == stages ? 0 : s + 1, use += s == 0 ? 1 : 0) {
+                    if (use > 0 && !lm_wait(lm_smem_u32(&sh.empty[s]), (use - 1) & 1, abort_flag, a.wait_limit_ns)) break;
+                    const uint32_t bar_local = lm_smem_u32(&sh.full[s]), bar = bar_local & kPeerMask;
+                    const uint32_t dst = tiles + s * stage_bytes;
+                    if (leader)                                        // the leader's barrier collects both CTAs' bytes
+                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;"
+                                     :: "r"(bar_local), "r"(2 * stage_bytes + (it == 0 ? (uint32_t)a.test_extra_tx : 0u)) : "memory");
+                    lm_tma_2d_pair(dst, &map_w, bar, k * kBK, row_w, 0);
+                    lm_tma_2d_pair(dst + kBytesA, &map_x, bar, k * kBK, row_x, 0);
+                }
+            }
+            if (*abort_flag && leader) {                               // copies in flight get a bounded chance to land
+                const uint32_t pending = it < stages ? it : stages;
+                for (uint32_t i = 0; i < pending; ++i) {
+                    const uint32_t i2 = it - 1 - i;
+                    lm_wait_plain(lm_smem_u32(&sh.full[i2 % stages]), (i2 / stages) & 1, a.wait_limit_ns);
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer (leader CTA only)
+        if (lane == 0 && leader) {
+            const uint32_t desc = idesc(2 * kTileM, a.tile_n);
+            uint32_t s = 0, use = 0, it = 0;
+            int m2, n;
+            bool ok = true;
+            for (uint32_t j = 0; ok && tile_of(j, n_m2, n_tok, m2, n) && !*abort_flag; ++j) {
+                for (int k = 0; k < a.n_ksteps; ++k, ++it, s = s + 1 == stages ? 0 : s + 1, use += s == 0 ? 1 : 0) {
+                    const uint32_t b = it & 1, use_b = it >> 1;
+                    if (use_b > 0 && !lm_wait(lm_smem_u32(&sh.acc_empty[b]), (use_b - 1) & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
+                    if (!lm_wait(lm_smem_u32(&sh.full[s]), use & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t d_tmem = tmem_base + b * kTileN;
+                    const uint64_t dw = lm_smem_desc_k(tiles + s * stage_bytes), dx = lm_smem_desc_k(tiles + s * stage_bytes + kBytesA);
+#pragma unroll
+                    for (int kk = 0; kk < kBK / 32; ++kk) {              // 32 codes of K per instruction
+                        asm volatile("{\n\t.reg .pred p;\n\t"
+                                     "setp.ne.b32 p, %4, 0;\n\t"
+                                     "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+                                     :: "r"(d_tmem), "l"(dw + kk * 2), "l"(dx + kk * 2), "r"(desc), "r"(kk > 0 ? 1u : 0u) : "memory");
+                    }
+                    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                                 :: "r"(lm_smem_u32(&sh.acc_full[b])), "h"((unsigned short)3) : "memory");
+                    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                                 :: "r"(lm_smem_u32(&sh.empty[s])), "h"((unsigned short)3) : "memory");
+                }
+            }
+            if (!ok || *abort_flag) {                                  // products already issued finish before memory goes away
+                asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(lm_smem_u32(&sh.drain)) : "memory");
+                lm_wait_plain(lm_smem_u32(&sh.drain), 0, a.wait_limit_ns);
+            }
+        }
+    } else if (warp == 2) {
+        // ------------------------------------------------------------------ factors of the blocks: 8 tokens per lane
+        uint32_t it = 0;
+        int m2, n;
+        bool ok = true;
+        for (uint32_t j = 0; ok && tile_of(j, n_m2, n_tok, m2, n); ++j) {
+            const float* sw = a.w_scale + (long long)(2 * m2 + (int)rank) * a.ws_stride;
+            const bool live = (2 * m2 + (int)rank) * kTileM < a.N;
+            const long long t0 = (long long)n * a.tile_n + lane * 4;
+            for (int k0 = 0; ok && k0 < a.n_ksteps; k0 += kBatch) {
+                float f[kBatch][8];
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    const float* p = a.x_scale + (long long)(k0 + i) * a.xs_stride + t0;
+                    const float w = live && k0 + i < a.n_ksteps ? sw[k0 + i] : 0.0f;
+#pragma unroll
+                    for (int h = 0; h < 8; ++h) {
+                        const int t = h < 4 ? h : 124 + h;                   // tokens 4 lane .. and 128 + 4 lane ..
+                        f[i][h] = k0 + i < a.n_ksteps && t0 + t < T ? p[t] * w : 0.0f;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    if (k0 + i >= a.n_ksteps) break;
+                    const uint32_t slot = it % kSlots, use = it / kSlots;
+                    if (use > 0 && !__all_sync(0xffffffffu, lm_wait(lm_smem_u32(&sh.f_empty[slot]), (use - 1) & 1, abort_flag, a.wait_limit_ns))) { ok = false; break; }
+                    sh.factor[slot][lane] = make_float4(f[i][0], f[i][1], f[i][2], f[i][3]);
+                    sh.factor[slot][32 + lane] = make_float4(f[i][4], f[i][5], f[i][6], f[i][7]);
+                    __syncwarp();
+                    if (lane == 0) lm_arrive(lm_smem_u32(&sh.f_full[slot]));
+                    ++it;
+                }
+            }
+        }
+    } else if (warp >= 4) {
+        // ------------------------------------------------------------------ epilogue (warps 4..11, both CTAs)
+        const int q = warp & 3, half = (warp - 4) >> 2;                  // TMEM lane quarter of this warp; which blocks of 32 tokens
+        uint32_t it = 0;
+        int m2, n;
+        bool ok = true;
+        for (uint32_t j = 0; ok && tile_of(j, n_m2, n_tok, m2, n); ++j) {
+            f32x2 acc[64];
+#pragma unroll
+            for (int i = 0; i < 64; ++i) acc[i] = 0ull;
+#pragma unroll 1
+            for (int k = 0; k < a.n_ksteps; ++k, ++it) {
+                const uint32_t b = it & 1, use_b = it >> 1, slot = it % kSlots;
+                // warp-uniform outcome: the tcgen05.ld below must be executed by all 32 lanes together
+                ok = __all_sync(0xffffffffu, lm_wait(lm_smem_u32(&sh.f_full[slot]), (it / kSlots) & 1, abort_flag, a.wait_limit_ns) &&
+                                             lm_wait(lm_smem_u32(&sh.acc_full[b]), use_b & 1, abort_flag, a.wait_limit_ns));
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + b * kTileN, f = lm_smem_u32(&sh.factor[slot][0]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int col = (2 * c + half) * 32;
+                    if (col < a.tile_n) {
+                        uint32_t v[32];
+                        lm_tmem_load32(v, taddr + (uint32_t)col);
+                        add_block(acc + c * 16, v, f + (uint32_t)col * 4u);
+                    }
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {                                         // the leader's MMA thread waits for all 16 warps
+                    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(lm_smem_u32(&sh.acc_empty[b]) & kPeerMask) : "memory");
+                    lm_arrive(lm_smem_u32(&sh.f_empty[slot]));
+                }
+            }
+            if (!ok) break;
+            const int ch = (2 * m2 + (int)rank) * kTileM + q * 32 + lane;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const long long t0 = (long long)n * a.tile_n + (2 * c + half) * 32;
+                if ((2 * c + half) * 32 < a.tile_n && t0 < T) store_tokens<kBf16, 32>(a, t0, T, ch, acc + c * 16);
+            }
+            __syncwarp();                                                // lanes without a channel went ahead; the next load wants all
+        }
+    }
+
+    // ---- common exit: both CTAs are done with tensor memory and with each other's barriers, then free
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    __syncwarp();
+    lm_cluster_sync();
+    if (tid == 0 && sh.abort) set_status(a.status, DPPO_STATUS_TIMEOUT);
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem_base), "r"(512u) : "memory");
+    }
+}
+
+// ---- few tokens: a CTA per 128 channels, K split over a cluster ---------------------------------------
+template <int kNB> struct Small {
+    static constexpr int kStages = kNB <= 16 ? 6 : kNB <= 32 ? 5 : kNB <= 64 ? 4 : 6;        // two CTAs per SM, but one of 128 tokens
+    static constexpr int kPerSm = kNB <= 64 ? 2 : 1;
+    static constexpr int kStageBytes = kBytesA + kNB * kBK;
+    static constexpr int kPitch = kNB < 32 ? 32 : kNB;                                       // TMEM columns between accumulators
+    static constexpr int kBufs = 256 / kPitch > 8 ? 8 : 256 / kPitch;
+    static constexpr int kHalves = kNB >= 64 ? 2 : 1;                                        // epilogue warps per lane quarter
+    static constexpr int kThreads = 128 + kHalves * 128;
+    static constexpr int kCols = kNB / kHalves;                                              // tokens of an epilogue warp
+    static constexpr int kChunk = kCols < 32 ? kCols : 32;
+    static constexpr size_t kDynSmem = (size_t)kStages * kStageBytes + 1024;
+    struct Shared {
+        alignas(16) float factor[kSlots][kNB];
+        unsigned long long full[kStages];
+        unsigned long long empty[kStages];
+        unsigned long long acc_full[kBufs];
+        unsigned long long acc_empty[kBufs];
+        unsigned long long f_full[kSlots];
+        unsigned long long f_empty[kSlots];
+        unsigned long long done;
+        uint32_t tmem_base;
+        int abort;
+    };
+};
+
+// 16 columns of this thread's TMEM lane.
+__device__ __forceinline__ void tmem_load16(uint32_t (&v)[16], uint32_t taddr) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+                   "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                 : "r"(taddr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+template <int kNB, bool kBf16>
+__global__ void __launch_bounds__(Small<kNB>::kThreads, Small<kNB>::kPerSm)
+linear_f8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const Args a, int n_ch, int split) {
+    typedef Small<kNB> S;
+    extern __shared__ unsigned char f8_raw[];
+    __shared__ typename S::Shared sh;
+    const uint32_t tiles = (lm_smem_u32(f8_raw) + 1023u) & ~1023u;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    volatile int* abort_flag = &sh.abort;
+    const int part = (int)(blockIdx.x % (unsigned)split);                 // rank in the cluster: clusters are consecutive CTAs
+    const int id = (int)(blockIdx.x / (unsigned)split);
+    const int m = id % n_ch;
+    const long long t_tile = (long long)(id / n_ch) * kNB;
+    const int k0 = (int)((long long)a.n_ksteps * part / split), k1 = (int)((long long)a.n_ksteps * (part + 1) / split);
+
+    if (tid == 0) {
+        sh.abort = 0;
+        for (int s = 0; s < S::kStages; ++s) { init_bar(&sh.full[s], 1); init_bar(&sh.empty[s], 1); }
+        for (int b = 0; b < S::kBufs; ++b) { init_bar(&sh.acc_full[b], 1); init_bar(&sh.acc_empty[b], 4 * S::kHalves); }
+        for (int b = 0; b < kSlots; ++b) { init_bar(&sh.f_full[b], 1); init_bar(&sh.f_empty[b], 4 * S::kHalves); }
+        init_bar(&sh.done, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    enter_kernel();
+    const long long T = true_rows(a);
+    if (t_tile >= T) return;                                              // the whole cluster leaves together
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     :: "r"(lm_smem_u32(&sh.tmem_base)), "r"(256u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem_base = sh.tmem_base;
+
+    const int q = warp & 3, row = q * 32 + lane, half = (warp - 4) >> 2;
+    const int ch = m * kTileM + row;
+    f32x2 acc[S::kCols / 2];
+    bool live = false;
+    if (warp == 0) {
+        if (lane == 0) {
+            int it = 0;
+            for (int k = k0; k < k1; ++k, ++it) {
+                const int s = it % S::kStages, use = it / S::kStages;
+                if (use > 0 && !lm_wait(lm_smem_u32(&sh.empty[s]), (use - 1) & 1, abort_flag, a.wait_limit_ns)) break;
+                const uint32_t bar = lm_smem_u32(&sh.full[s]), dst = tiles + s * S::kStageBytes;
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;"
+                             :: "r"(bar), "r"((uint32_t)S::kStageBytes + (it == 0 ? (uint32_t)a.test_extra_tx : 0u)) : "memory");
+                lm_tma_2d(dst, &map_w, bar, k * kBK, m * kTileM, 0);
+                lm_tma_2d(dst + kBytesA, &map_x, bar, k * kBK, (int)t_tile, 0);
+            }
+            if (*abort_flag) {
+                const int pending = it < S::kStages ? it : S::kStages;
+                for (int i = 0; i < pending; ++i) {
+                    const int i2 = it - 1 - i;
+                    lm_wait_plain(lm_smem_u32(&sh.full[i2 % S::kStages]), (i2 / S::kStages) & 1, a.wait_limit_ns);
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            int it = 0;
+            for (int k = k0; k < k1; ++k, ++it) {
+                const int s = it % S::kStages, use = it / S::kStages, b = it % S::kBufs, use_b = it / S::kBufs;
+                if (use_b > 0 && !lm_wait(lm_smem_u32(&sh.acc_empty[b]), (use_b - 1) & 1, abort_flag, a.wait_limit_ns)) break;
+                if (!lm_wait(lm_smem_u32(&sh.full[s]), use & 1, abort_flag, a.wait_limit_ns)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint64_t dw = lm_smem_desc_k(tiles + s * S::kStageBytes), dx = lm_smem_desc_k(tiles + s * S::kStageBytes + kBytesA);
+#pragma unroll
+                for (int kk = 0; kk < kBK / 32; ++kk) {
+                    asm volatile("{\n\t.reg .pred p;\n\t"
+                                 "setp.ne.b32 p, %4, 0;\n\t"
+                                 "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+                                 :: "r"(tmem_base + (uint32_t)(b * S::kPitch)), "l"(dw + kk * 2), "l"(dx + kk * 2), "r"(idesc(kTileM, kNB)), "r"(kk > 0 ? 1u : 0u) : "memory");
+                }
+                asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(lm_smem_u32(&sh.acc_full[b])) : "memory");
+                asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(lm_smem_u32(&sh.empty[s])) : "memory");
+            }
+            // all products issued so far (on an early way out too: they finish before memory goes away)
+            asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(lm_smem_u32(&sh.done)) : "memory");
+            lm_wait_plain(lm_smem_u32(&sh.done), 0, a.wait_limit_ns);
+        }
+    } else if (warp == 2) {
+        constexpr int kPer = kNB < 32 ? 1 : kNB / 32;
+        const float* sw = a.w_scale + (long long)m * a.ws_stride;
+        uint32_t it = 0;
+        bool ok = true;
+        for (int k = k0; ok && k < k1; k += kBatch) {
+            float f[kBatch][kPer];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const float w = k + i < k1 ? sw[k + i] : 0.0f;
+#pragma unroll
+                for (int h = 0; h < kPer; ++h) {
+                    const long long t = t_tile + h * 32 + lane;
+                    f[i][h] = k + i < k1 && t < T && h * 32 + lane < kNB ? a.x_scale[(long long)(k + i) * a.xs_stride + t] * w : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                if (k + i >= k1) break;
+                const uint32_t slot = it % kSlots, use = it / kSlots;
+                if (use > 0 && !__all_sync(0xffffffffu, lm_wait(lm_smem_u32(&sh.f_empty[slot]), (use - 1) & 1, abort_flag, a.wait_limit_ns))) { ok = false; break; }
+#pragma unroll
+                for (int h = 0; h < kPer; ++h)
+                    if (h * 32 + lane < kNB) sh.factor[slot][h * 32 + lane] = f[i][h];
+                __syncwarp();
+                if (lane == 0) lm_arrive(lm_smem_u32(&sh.f_full[slot]));
+                ++it;
+            }
+        }
+    } else if (warp >= 4) {
+#pragma unroll
+        for (int i = 0; i < S::kCols / 2; ++i) acc[i] = 0ull;
+        live = true;
+        uint32_t it = 0;
+#pragma unroll 1
+        for (int k = k0; k < k1; ++k, ++it) {
+            const uint32_t b = it % S::kBufs, slot = it % kSlots;
+            live = __all_sync(0xffffffffu, lm_wait(lm_smem_u32(&sh.f_full[slot]), (it / kSlots) & 1, abort_flag, a.wait_limit_ns) &&
+                                           lm_wait(lm_smem_u32(&sh.acc_full[b]), (it / S::kBufs) & 1, abort_flag, a.wait_limit_ns));
+            if (!live) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + b * S::kPitch + (uint32_t)(half * S::kCols);
+            const uint32_t f = lm_smem_u32(&sh.factor[slot][half * S::kCols]);
+#pragma unroll
+            for (int c = 0; c < S::kCols / S::kChunk; ++c) {
+                if constexpr (S::kChunk == 32) {
+                    uint32_t v[32];
+                    lm_tmem_load32(v, taddr + (uint32_t)(c * 32));
+                    add_block(acc + c * 16, v, f + (uint32_t)(c * 32) * 4u);
+                } else {
+                    uint32_t v[16];
+                    tmem_load16(v, taddr);
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        f32x2 f0, f1;
+                        asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(f0), "=l"(f1) : "r"(f + i * 4));
+                        acc[i / 2] = fma2(pair_of(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), f0, acc[i / 2]);
+                        acc[i / 2 + 1] = fma2(pair_of(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), f1, acc[i / 2 + 1]);
+                    }
+                }
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) { lm_arrive(lm_smem_u32(&sh.acc_empty[b])); lm_arrive(lm_smem_u32(&sh.f_empty[slot])); }
+        }
+        live = live && !__any_sync(0xffffffffu, *abort_flag);
+        if (live) {
+            if (split == 1) {
+#pragma unroll
+                for (int c = 0; c < S::kCols / S::kChunk; ++c) {
+                    const long long t0 = t_tile + half * S::kCols + c * S::kChunk;
+                    if (t0 < T) store_tokens<kBf16, S::kChunk>(a, t0, T, ch, acc + c * S::kChunk / 2);
+                }
+            } else {
+                // partial sums to shared memory, [token][channel], in the ring: nothing reads or writes that any more, the last
+                // block's products being complete
+#pragma unroll
+                for (int i = 0; i < S::kCols; i += 2) {
+                    float x0, x1;
+                    unpair(acc[i / 2], x0, x1);
+                    const uint32_t at = tiles + (uint32_t)((half * S::kCols + i) * kTileM + row) * 4u;
+                    asm volatile("st.shared.f32 [%0], %1;" :: "r"(at), "f"(x0) : "memory");
+                    asm volatile("st.shared.f32 [%0], %1;" :: "r"(at + kTileM * 4u), "f"(x1) : "memory");
+                }
+            }
+        }
+        __syncwarp();
+    }
+    if (split > 1) {
+        __syncwarp();
+        lm_cluster_sync();                                               // every CTA's sums are in its shared memory
+        if (live) {
+            // this CTA's share of the tokens: part, part + split, ...; all of a token's partial sums are under way together
+            const int n_tok = (int)min((long long)kNB, T - t_tile);
+            for (int c = part + half * split; c < n_tok; c += S::kHalves * split) {
+                float x[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    x[r] = 0.0f;
+                    if (r < split) {
+                        uint32_t remote;
+                        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(tiles + (uint32_t)(c * kTileM + row) * 4u), "r"(r));
+                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x[r]) : "r"(remote) : "memory");
+                    }
+                }
+                const float y = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+                if (ch < a.N) {
+                    if constexpr (kBf16) reinterpret_cast<__nv_bfloat16*>(a.out)[(t_tile + c) * a.out_stride + ch] = __float2bfloat16_rn(y);
+                    else reinterpret_cast<float*>(a.out)[(t_tile + c) * a.out_stride + ch] = y;
+                }
+            }
+        }
+        __syncwarp();
+        lm_cluster_sync();                                               // the others have read this CTA's shared memory
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (tid == 0 && sh.abort) set_status(a.status, DPPO_STATUS_TIMEOUT);
+    if (warp == 1) {
+        __syncwarp();
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem_base), "r"(256u) : "memory");
+    }
+}
+
+// ---- quantisation -------------------------------------------------------------------------------------
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+struct QuantArgs {
+    const char* x;
+    uint8_t* q;
+    float* scale;
+    const int32_t* n_rows_dev;
+    long long rows_max, x_row_bytes, q_stride, scale_stride;
+    int K, n_blocks;
+};
+
+// Two codes.
+__device__ __forceinline__ uint32_t codes2(float a, float b) { return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3); }
+// What a block's maximum makes of it: its scale, and the reciprocal's neighbours.
+struct Scale {
+    float s, lo, hi;
+    bool fine;                            // no NaN or infinity in the block
+};
+__device__ __forceinline__ Scale scale_of(float amax) {
+    Scale r;
+    r.fine = amax < INFINITY;
+    r.s = r.fine ? fmaxf(__fmul_rn(amax, 1.0f / 448.0f), 1.17549435e-38f) : __int_as_float(0x7fffffff);
+    const float inv = __fdiv_rn(1.0f, r.s);
+    r.lo = inv * (1.0f - 0x1p-21f);
+    r.hi = inv * (1.0f + 0x1p-21f);
+    return r;
+}
+// The codes of kPer values, 4 per word.  The quotient x / s lies strictly between x lo and x hi (the roundings of 1 / s and of the
+// products are 2^-24 each), and rounding to a code is monotonous: where both ends have the same code, so has the quotient.  A
+// vector where they differ (one in ten thousand) is divided out.
+template <int kPer> __device__ __forceinline__ void codes_of(const float (&f)[kPer], const Scale& sc, uint32_t (&w)[kPer / 4]) {
+    uint32_t diff = 0;
+    const f32x2 lo = pair_of(sc.lo, sc.lo), hi = pair_of(sc.hi, sc.hi);
+#pragma unroll
+    for (int j = 0; j < kPer; j += 4) {
+        float a0, a1, a2, a3, b0, b1, b2, b3;
+        unpair(mul2(pair_of(f[j], f[j + 1]), lo), a0, a1);
+        unpair(mul2(pair_of(f[j + 2], f[j + 3]), lo), a2, a3);
+        unpair(mul2(pair_of(f[j], f[j + 1]), hi), b0, b1);
+        unpair(mul2(pair_of(f[j + 2], f[j + 3]), hi), b2, b3);
+        w[j / 4] = codes2(a0, a1) | codes2(a2, a3) << 16;
+        diff |= w[j / 4] ^ (codes2(b0, b1) | codes2(b2, b3) << 16);
+    }
+    if (diff != 0 || !sc.fine) {
+#pragma unroll
+        for (int j = 0; j < kPer; j += 4)
+            w[j / 4] = sc.fine ? codes2(__fdiv_rn(f[j], sc.s), __fdiv_rn(f[j + 1], sc.s)) | codes2(__fdiv_rn(f[j + 2], sc.s), __fdiv_rn(f[j + 3], sc.s)) << 16 : 0u;
+    }
+}
+// kPer values of a row from element e0 on; 0 past its end.  Whole vectors in one load.
+template <bool kBf16> __device__ __forceinline__ uint4 load_part(const char* row, int e0, int K) {
+    constexpr int kPer = Elems<kBf16>::kPerVec;
+    if (e0 + kPer <= K) return *reinterpret_cast<const uint4*>(row + (size_t)e0 * (16 / kPer));
+    float f[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) f[j] = e0 + j < K ? Elems<kBf16>::load1(row, e0 + j) : 0.0f;
+    return Elems<kBf16>::pack(f);
+}
+template <bool kBf16> __device__ __forceinline__ float amax_vec(const uint4& v) {
+    constexpr int kPer = Elems<kBf16>::kPerVec;
+    float f[kPer], m = 0.0f;
+    Elems<kBf16>::unpack(v, f);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) m = max_nan(m, fabsf(f[j]));
+    return m;
+}
+template <bool kBf16> __device__ __forceinline__ void store_codes(uint8_t* row, int e0, int K, const uint4& v, const Scale& sc) {
+    constexpr int kPer = Elems<kBf16>::kPerVec;
+    float f[kPer];
+    uint32_t w[kPer / 4];
+    Elems<kBf16>::unpack(v, f);
+    codes_of<kPer>(f, sc, w);
+    if (e0 + kPer <= K) {
+        if constexpr (kBf16) *reinterpret_cast<uint2*>(row + e0) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<uint32_t*>(row + e0) = w[0];
+    } else {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j)
+            if (e0 + j < K) row[e0 + j] = (uint8_t)(w[j / 4] >> (8 * (j & 3)));
+    }
+}
+
+// A scale per row and 128 columns: 16 lanes (bf16) or 32 (f32) hold a block, one vector each; kUnroll blocks of a row at a time.
+template <bool kBf16, int kUnroll> __global__ void __launch_bounds__(128) quantize_f8_rows_kernel(const QuantArgs a, int groups) {
+    constexpr int kPer = Elems<kBf16>::kPerVec, kTeam = kBK / kPer, kTeams = 128 / kTeam;
+    enter_kernel();
+    const long long T = a.n_rows_dev ? min((long long)*a.n_rows_dev, a.rows_max) : a.rows_max;
+    const long long item = (long long)blockIdx.x * kTeams + threadIdx.x / kTeam;
+    const long long t = item / groups;
+    const int b0 = (int)(item - t * groups) * kUnroll, l = threadIdx.x % kTeam;
+    const bool live = t < T;
+    const char* row = a.x + t * a.x_row_bytes;
+    uint4 v[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+        const int e0 = (b0 + u) * kBK + l * kPer;
+        v[u] = live && b0 + u < a.n_blocks && e0 < a.K ? load_part<kBf16>(row, e0, a.K) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+        float m = amax_vec<kBf16>(v[u]);
+#pragma unroll
+        for (int o = kTeam / 2; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+        const Scale sc = scale_of(m);
+        const int e0 = (b0 + u) * kBK + l * kPer;
+        if (live && b0 + u < a.n_blocks) {
+            if (l == 0) a.scale[(long long)(b0 + u) * a.scale_stride + t] = sc.s;
+            if (e0 < a.K) store_codes<kBf16>(a.q + t * a.q_stride, e0, a.K, v[u], sc);
+        }
+    }
+}
+
+// A scale per 128 x 128: a CTA holds the block in registers.
+template <bool kBf16> __global__ void __launch_bounds__(256) quantize_f8_blocks_kernel(const QuantArgs a) {
+    constexpr int kPer = Elems<kBf16>::kPerVec, kTeam = kBK / kPer, kRows = 256 / kTeam, kVecs = kBK / kRows;
+    __shared__ float red[8];
+    enter_kernel();
+    const long long T = a.n_rows_dev ? min((long long)*a.n_rows_dev, a.rows_max) : a.rows_max;
+    const long long br = blockIdx.x / (unsigned)a.n_blocks, r0 = br * kBK + threadIdx.x / kTeam;
+    const int bk = (int)(blockIdx.x - br * a.n_blocks), e0 = bk * kBK + (int)(threadIdx.x % kTeam) * kPer;
+    if (br * kBK >= T) return;
+    uint4 v[kVecs];
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        const long long t = r0 + i * kRows;
+        v[i] = t < T && e0 < a.K ? load_part<kBf16>(a.x + t * a.x_row_bytes, e0, a.K) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) m = max_nan(m, amax_vec<kBf16>(v[i]));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 8; ++w) m = max_nan(m, red[w]);
+    const Scale sc = scale_of(m);
+    if (threadIdx.x == 0) a.scale[br * a.scale_stride + bk] = sc.s;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        const long long t = r0 + i * kRows;
+        if (t < T && e0 < a.K) store_codes<kBf16>(a.q + t * a.q_stride, e0, a.K, v[i], sc);
+    }
+}
+
+// ---- host side ---------------------------------------------------------------------------------------
+template <bool kBf16> static int run_quantize(const QuantArgs& a, int block_rows, cudaStream_t s) {
+    if (block_rows == 1) {
+        constexpr int kUnroll = 4, kTeams = kBf16 ? 8 : 4;
+        const int groups = (a.n_blocks + kUnroll - 1) / kUnroll;
+        const long long ctas = (a.rows_max * groups + kTeams - 1) / kTeams;
+        if (ctas > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "quantize_f8: too many blocks");
+        return launch_after("quantize_f8 launch", quantize_f8_rows_kernel<kBf16, kUnroll>, ctas, 128, 0, s, 1, a, groups);
+    }
+    const long long ctas = (a.rows_max + kBK - 1) / kBK * a.n_blocks;
+    if (ctas > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "quantize_f8: too many blocks");
+    return launch_after("quantize_f8 launch", quantize_f8_blocks_kernel<kBf16>, ctas, 256, 0, s, 1, a);
+}
+
+// e4m3 [rows x K] with row pitch `ld` bytes; boxes of 128 codes x box_rows rows, 128B swizzle, zeros outside.
+static int make_map(CUtensorMap* map, const void* base, long long rows, int K, long long ld, int box_rows) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return fail(DPPO_ERR_CUDA, "linear_f8: cuTensorMapEncodeTiled is not available from this driver");
+    const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld};
+    const cuuint32_t box[2] = {(cuuint32_t)kBK, (cuuint32_t)box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(DPPO_ERR_CUDA, "linear_f8: cuTensorMapEncodeTiled failed with %d", (int)r);
+    return DPPO_OK;
+}
+
+// Raises a kernel's shared-memory limit once per device.
+template <class Kernel> static int raise_smem(Kernel kernel, size_t bytes, bool (&done)[64]) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); dev = -1; }
+    if (dev >= 0 && done[dev]) return DPPO_OK;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != cudaSuccess) { cudaGetLastError(); return cuda_fail(e, "linear_f8: shared memory attribute"); }
+    if (dev >= 0) done[dev] = true;
+    return DPPO_OK;
+}
+
+// ---- which kernel, which tile: both kernels' times in microseconds ----
+static double pair_time(long long M, int N, int n_ksteps, int* tile) {
+    const long long n_m2 = (N + 255) / 256, pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
+    double best = 0.0;
+    for (int tn = kTileN; tn >= 64; tn -= 32) {
+        const long long tiles = n_m2 * ((M + tn - 1) / tn), waves = (tiles + pairs - 1) / pairs;
+        const double slab = tn * 0.0018 > 0.3 ? tn * 0.0018 : 0.3;
+        const double t = 2.9 + (double)waves * (n_ksteps * slab + 0.3 + 0.011 * tn);
+        if (best == 0.0 || t < best) { best = t; *tile = tn; }
+    }
+    return best;
+}
+static double small_time(long long M, int N, int n_ksteps, int* tokens, int* split) {
+    const int nb = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    const long long tiles = (long long)((N + kTileM - 1) / kTileM) * ((M + nb - 1) / nb), sms = sm_count();
+    const double latency = 0.25 + 0.00075 * nb, fetch = 2 * (16384 + nb * 128) / 75e3;
+    double best = 0.0;
+    for (int sp = 1, i = 0; sp <= 8; sp *= 2, ++i) {
+        constexpr double kJoin[4] = {0.0, 0.3, 0.4, 0.9};
+        const long long ctas = tiles * sp;
+        if (sp > 1 && (ctas > 2 * sms || n_ksteps < sp)) break;
+        const bool two = ctas > sms;
+        const double waves = ctas <= 2 * sms ? 1.0 : (double)ctas / (double)(2 * sms) + 0.4;
+        const double slab = two && fetch > latency ? fetch : latency;
+        const double t = waves * (((n_ksteps + sp - 1) / sp) * slab + 3.0 + 0.0075 * nb) + (two ? 1.8 : 0.0)
+                       + (sp > 1 ? kJoin[i] + 0.017 * nb : 0.0);
+        if (best == 0.0 || t < best) { best = t; *split = sp; }
+    }
+    *tokens = nb;
+    return best;
+}
+
+template <bool kBf16> static int launch_pair(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
+    auto kernel = linear_f8_pair_kernel<kBf16>;
+    static bool raised[64];
+    const int rc = raise_smem(kernel, kDynSmem2, raised);
+    if (rc != DPPO_OK) return rc;
+    const long long work = (long long)((a.N + 255) / 256) * ((a.M_max + a.tile_n - 1) / a.tile_n), most = sm_count() / 2;
+    return launch_after("linear_f8 launch", kernel, 2 * (work < most ? work : most), kThreads, kDynSmem2, s, 2, mw, mx, a);
+}
+
+template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, int split, cudaStream_t s) {
+    auto kernel = linear_f8_small_kernel<kNB, kBf16>;
+    static bool raised[64];
+    const int rc = raise_smem(kernel, Small<kNB>::kDynSmem, raised);
+    if (rc != DPPO_OK) return rc;
+    const int n_ch = (a.N + kTileM - 1) / kTileM;
+    const long long tiles = (long long)n_ch * ((a.M_max + kNB - 1) / kNB);
+    if (tiles * split > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "linear_f8: too many tiles");
+    return launch_after("linear_f8 launch", kernel, tiles * split, Small<kNB>::kThreads, Small<kNB>::kDynSmem, s, split, mw, mx, a, n_ch, split);
+}
+
+template <bool kBf16> static int launch(bool pair, int nb, int split, const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
+    if (pair) return launch_pair<kBf16>(mw, mx, a, s);
+    switch (nb) {
+        case 16: return launch_small<16, kBf16>(mw, mx, a, split, s);
+        case 32: return launch_small<32, kBf16>(mw, mx, a, split, s);
+        case 64: return launch_small<64, kBf16>(mw, mx, a, split, s);
+        default: return launch_small<128, kBf16>(mw, mx, a, split, s);
+    }
+}
+
+}  // namespace f8
+}  // namespace dppo
+
+extern "C" int dppo_quantize_f8(const dppo_quantize_f8_params* p, const void* x, uint8_t* q, float* scale,
+                                const int32_t* n_rows_dev, int32_t* status, void* stream) {
+    dppo::NvtxRange nvtx_range("dppo_quantize_f8");
+    using namespace dppo;
+    (void)status;
+    if (!p) return fail(DPPO_ERR_INVALID_ARG, "quantize_f8: NULL params");
+    if (p->rows_max < 0 || p->K < 1) return fail(DPPO_ERR_INVALID_ARG, "quantize_f8: rows_max=%lld K=%d", (long long)p->rows_max, p->K);
+    if (p->dtype != DPPO_F32 && p->dtype != DPPO_BF16) return fail(DPPO_ERR_UNSUPPORTED, "quantize_f8: dtype %d", p->dtype);
+    if (p->block_rows != 1 && p->block_rows != 128) return fail(DPPO_ERR_UNSUPPORTED, "quantize_f8: block_rows %d (1 or 128)", p->block_rows);
+    if (p->K > (1 << 30)) return fail(DPPO_ERR_BAD_SHAPE, "quantize_f8: K=%d, the limit is 2^30", p->K);
+    if (p->rows_max >= ((int64_t)1 << 31)) return fail(DPPO_ERR_BAD_SHAPE, "quantize_f8: rows_max must be below 2^31");
+    const int n_blocks = (p->K + f8::kBK - 1) / f8::kBK;
+    if (p->x_stride < p->K || p->q_stride < p->K || p->scale_stride < (p->block_rows == 1 ? p->rows_max : (int64_t)n_blocks))
+        return fail(DPPO_ERR_BAD_SHAPE, "quantize_f8: strides %lld, %lld, %lld for %lld rows of K=%d", (long long)p->x_stride, (long long)p->q_stride,
+                    (long long)p->scale_stride, (long long)p->rows_max, p->K);
+    const long long x_row_bytes = (long long)p->x_stride * (p->dtype == DPPO_BF16 ? 2 : 4);
+    if (p->rows_max == 0) return DPPO_OK;
+    if (!x || !q || !scale) return fail(DPPO_ERR_INVALID_ARG, "quantize_f8: NULL array");
+    if (((uintptr_t)x & 15) || ((uintptr_t)q & 15) || x_row_bytes % 16 != 0 || p->q_stride % 16 != 0)
+        return fail(DPPO_ERR_MISALIGNED, "quantize_f8: x / q base and row strides must be multiples of 16 bytes");
+    const f8::QuantArgs a = {(const char*)x, q, scale, n_rows_dev, p->rows_max, x_row_bytes, p->q_stride, p->scale_stride, p->K, n_blocks};
+    return p->dtype == DPPO_BF16 ? f8::run_quantize<true>(a, p->block_rows, (cudaStream_t)stream) : f8::run_quantize<false>(a, p->block_rows, (cudaStream_t)stream);
+}
+
+extern "C" int dppo_linear_f8(const dppo_linear_f8_params* p, const uint8_t* x, const float* x_scale, const uint8_t* w,
+                              const float* w_scale, void* out, const int32_t* n_rows_dev, int32_t* status, void* stream) {
+    dppo::NvtxRange nvtx_range("dppo_linear_f8");
+    using namespace dppo;
+    if (!p) return fail(DPPO_ERR_INVALID_ARG, "linear_f8: NULL params");
+    if (p->M_max < 0 || p->N < 1 || p->K < 1)
+        return fail(DPPO_ERR_INVALID_ARG, "linear_f8: M_max=%lld N=%d K=%d", (long long)p->M_max, p->N, p->K);
+    if (p->out_dtype != DPPO_F32 && p->out_dtype != DPPO_BF16) return fail(DPPO_ERR_UNSUPPORTED, "linear_f8: out_dtype %d", p->out_dtype);
+    if (p->K > (1 << 30)) return fail(DPPO_ERR_BAD_SHAPE, "linear_f8: K=%d, the limit is 2^30", p->K);
+    if (p->N > 0x7fffff00) return fail(DPPO_ERR_BAD_SHAPE, "linear_f8: N=%d", p->N);
+    const int n_blocks = (p->K + f8::kBK - 1) / f8::kBK;
+    if (p->x_stride < p->K || p->w_stride < p->K || p->out_stride < p->N || p->x_scale_stride < p->M_max || p->w_scale_stride < n_blocks)
+        return fail(DPPO_ERR_BAD_SHAPE, "linear_f8: strides %lld, %lld, %lld, %lld, %lld for M_max=%lld N=%d K=%d", (long long)p->x_stride,
+                    (long long)p->w_stride, (long long)p->out_stride, (long long)p->x_scale_stride, (long long)p->w_scale_stride, (long long)p->M_max, p->N, p->K);
+    if (p->M_max >= ((int64_t)1 << 31) - 256) return fail(DPPO_ERR_BAD_SHAPE, "linear_f8: M_max too large");
+    const int variant = p->variant >= 100 ? p->variant - 100 : p->variant;
+    if (variant < 0 || variant > 2 || p->variant == 100) return fail(DPPO_ERR_INVALID_ARG, "linear_f8: variant %d", p->variant);
+    if (p->M_max == 0) return DPPO_OK;
+    if (!x || !x_scale || !w || !w_scale || !out) return fail(DPPO_ERR_INVALID_ARG, "linear_f8: NULL array");
+    if (((uintptr_t)x & 15) || ((uintptr_t)w & 15) || p->x_stride % 16 != 0 || p->w_stride % 16 != 0)
+        return fail(DPPO_ERR_MISALIGNED, "linear_f8: x / w base and row strides must be multiples of 16 bytes");
+    if (p->x_stride >= (1ll << 40) || p->w_stride >= (1ll << 40)) return fail(DPPO_ERR_BAD_SHAPE, "linear_f8: strides of x and w must be below 2^40");
+
+    f8::Args a = {};
+    a.x_scale = x_scale; a.w_scale = w_scale; a.out = out; a.n_rows_dev = n_rows_dev; a.status = status;
+    a.M_max = p->M_max; a.out_stride = p->out_stride; a.xs_stride = p->x_scale_stride; a.ws_stride = p->w_scale_stride;
+    a.N = p->N; a.n_ksteps = n_blocks; a.out_bf16 = p->out_dtype == DPPO_BF16;
+    a.wait_limit_ns = p->variant >= 100 ? kSelfTestWaitLimitNs : kDefaultWaitLimitNs;
+    a.test_extra_tx = p->variant >= 100 ? 16 : 0;
+    int nb = 0, split = 1;
+    const double t_pair = f8::pair_time(p->M_max, p->N, n_blocks, &a.tile_n), t_small = f8::small_time(p->M_max, p->N, n_blocks, &nb, &split);
+    const bool pair = variant == 1 || (variant == 0 && t_pair < t_small);
+    if (pair) nb = a.tile_n / 2;
+    alignas(64) CUtensorMap mw, mx;
+    int rc = f8::make_map(&mw, w, p->N, p->K, p->w_stride, f8::kTileM);
+    if (rc == DPPO_OK) rc = f8::make_map(&mx, x, p->M_max, p->K, p->x_stride, nb);
+    if (rc != DPPO_OK) return rc;
+    cudaStream_t s = (cudaStream_t)stream;
+    return a.out_bf16 ? f8::launch<true>(pair, nb, split, mw, mx, a, s) : f8::launch<false>(pair, nb, split, mw, mx, a, s);
+}
