@@ -563,7 +563,7 @@ typedef struct {
     int32_t N, K;           /* output channels; contraction length                                   */
     int64_t x_stride, w_stride;   /* bytes between rows of x and of w (>= K; multiples of 16)        */
     int64_t out_stride;     /* elements between rows of out (>= N)                                   */
-    int64_t x_scale_stride; /* elements between rows of x_scale (>= M_max)                           */
+    int64_t x_scale_stride; /* elements between rows of x_scale (>= M_max; a multiple of 4)          */
     int64_t w_scale_stride; /* elements between rows of w_scale (>= ceil(K / 128))                   */
     int32_t out_dtype;      /* dppo_dtype of out                                                     */
     int32_t variant;        /* 0: the library picks the kernel; 1 forces the CTA-pair tile kernel, 2 the
@@ -576,7 +576,8 @@ typedef struct {
  *   [ceil(N / 128) x w_scale_stride]: as dppo_quantize_f8 leaves them
  *   out [M_max x out_stride] of out_dtype (no alignment beyond its element's)
  *   n_rows_dev  i32 [1] true number of tokens on the device, or NULL; rows of out past it are not written
- * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED (x, w: base or stride), UNSUPPORTED, CUDA (tensor-map creation).  Device status: TIMEOUT.
+ * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED (x, w, x_scale: base or stride), UNSUPPORTED, CUDA (tensor-map creation).  Device status:
+ * TIMEOUT.
  */
 int dppo_linear_f8(const dppo_linear_f8_params* p, const uint8_t* x, const float* x_scale, const uint8_t* w, const float* w_scale,
                    void* out, const int32_t* n_rows_dev, int32_t* status, void* stream);

@@ -4,14 +4,20 @@
 //
 // A block of 128 codes is one 128-byte swizzle row: one stage of the TMA ring, four instructions (tcgen05.mma kind::f8f6f4, f32
 // accumulation) into a tensor-memory accumulator of its own.  The epilogue warps read that accumulator back while the next
-// block's products run, and add it, times its scales, to f32 sums in their registers: acc += v * (sx sw), packed two tokens at a time.
-// The weights take the M side (TMEM lanes = output channels): a CTA's 128 channels share one weight scale per block, so the
-// factors of a block are one number per token, formed by a warp of its own and read by the epilogue as shared-memory broadcasts; and 32
-// consecutive channels of a token are written per warp instruction whatever the row pitch of the output.
+// block's products run, and add it, times its scales, to f32 sums in their registers.
 //
-// Two kernels, as for the 8-bit integer product: CTA pairs (cta_group::2), 256 channels x up to 256 tokens, for many tokens; a CTA
-// per 128 channels with the contraction split over a cluster for few (partial sums joined in a fixed order through distributed
-// shared memory).  Every wait is bounded; on a time-out the CTA reports DPPO_STATUS_TIMEOUT, leaves its loops, lets copies and products
+// Two kernels.
+//   many tokens: persistent CTA pairs (cta_group::2), 256 tokens x up to 256 channels per tile.  The tokens take the M side (TMEM lanes): a
+//     thread of the epilogue then holds 128 channels of one token, which share one weight scale, so a block's factor is ONE number per
+//     thread.  That matters because shared memory is what the tensor cores read their operands from: with the channels on the
+//     lanes the factors came as 16 shared-memory loads per warp and block, and the products waited for the epilogue (2,048 x 2,560
+//     x 151,936: 1,260 us).  The outputs are transposed through shared memory, once per tile.
+//   few tokens (bound by reading the weights): a CTA per 128 channels, 16 to 128 tokens on the N side, so that few tokens waste
+//     nothing; the contraction is split over the CTAs of a cluster when there are too few tiles to keep all SMs reading, and the
+//     partial sums are joined in a fixed order through distributed shared memory.  The tokens' scales of a block travel with its codes,
+//     through a ring of their own that is longer than the codes' (kSlots > stages + accumulators + 1): a slot is then read
+//     long before its turn comes again, with no barrier.
+// Every wait is bounded; on a time-out the CTA reports DPPO_STATUS_TIMEOUT, leaves its loops, lets copies and products
 // in flight finish (bounded), frees its tensor memory and returns.
 #include <cuda_fp8.h>
 
@@ -27,16 +33,17 @@ using namespace packed;
 namespace f8 {
 
 constexpr int kBK = 128;                  // codes of a block = of a stage
-constexpr int kTileM = 128;               // channels per CTA
-constexpr int kTileN = 256;               // most tokens per tile of the pair kernel
+constexpr int kTileM = 128;               // rows of the M side per CTA
+constexpr int kTileN = 256;               // most channels per tile of the pair kernel
 constexpr int kBytesA = kTileM * kBK;
-constexpr int kMaxStages = 12;
-constexpr int kSlots = 8;                 // blocks whose factors are in shared memory
-constexpr int kBatch = 4;                 // blocks whose scales are under way together
-constexpr int kThreads = 384;             // producer, MMA, scale and one idle warp; 8 epilogue warps (two per TMEM lane quarter)
-constexpr int kTokenGroup = 16;           // token tiles swept together
+constexpr int kMaxStages = 9;
+constexpr int kSlots = 16;                // few tokens: blocks whose token scales are in shared memory
+constexpr int kEpiWarps = 8;              // pair kernel: two per TMEM lane quarter, half of the tile's channels each
+constexpr int kThreads = 128 + 32 * kEpiWarps;     // producer, MMA and two idle warps before them
+constexpr int kTokenGroup = 8;            // token tiles swept together (2,048 tokens: 5 MB of codes at K = 2,560)
 constexpr int kRingBytes = 6 * (kBytesA + kTileN / 2 * kBK);
-constexpr size_t kDynSmem2 = (size_t)kRingBytes + 1024;
+constexpr int kStageOut = 2048;           // 64 bytes of outputs of 32 tokens: what an epilogue warp transposes at a time
+constexpr size_t kDynSmem2 = (size_t)kRingBytes + kEpiWarps * kStageOut + 1024;
 
 struct Args {
     const float* x_scale;
@@ -46,7 +53,8 @@ struct Args {
     int32_t* status;
     long long M_max, out_stride, xs_stride, ws_stride;
     int N, n_ksteps, out_bf16;
-    int tile_n;                           // pair kernel: tokens per tile, a multiple of 32 up to 256
+    int tile_n;                           // pair kernel: channels per tile, 64, 128 or 256
+    int vec_out;                          // out: base and rows on 16 bytes
     unsigned long long wait_limit_ns;
     int test_extra_tx;
 };
@@ -61,44 +69,99 @@ __device__ __forceinline__ void init_bar(unsigned long long* bar, int count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(lm_smem_u32(bar)), "r"(count));
 }
 
+// A warp's bounded wait: warp-uniform outcome, since what follows is executed by all 32 lanes together.
+__device__ __forceinline__ bool warp_wait(unsigned long long* bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns) {
+    return __all_sync(0xffffffffu, lm_wait(lm_smem_u32(bar), parity, abort_flag, limit_ns));
+}
+
 // kCount consecutive tokens t0 .. of this lane's channel.
-template <bool kBf16, int kCount> __device__ __forceinline__ void store_tokens(const Args& a, long long t0, long long T, int ch, const f32x2* acc) {
+template <bool kBf16, int kCount> __device__ __forceinline__ void store_tokens(const Args& a, long long t0, long long T, int ch, const float* acc) {
     typedef typename std::conditional<kBf16, __nv_bfloat16, float>::type Out;
     const int nt = (int)min((long long)kCount, T - t0);
     if (ch >= a.N) return;
     Out* p = reinterpret_cast<Out*>(a.out) + t0 * a.out_stride + ch;
 #pragma unroll
-    for (int i = 0; i < kCount; i += 2) {
-        float x0, x1;
-        unpair(acc[i / 2], x0, x1);
-        Out o0, o1;
-        if constexpr (kBf16) { const __nv_bfloat162 h = __floats2bfloat162_rn(x0, x1); o0 = h.x; o1 = h.y; } else { o0 = x0; o1 = x1; }
-        if (i < nt) p[0] = o0;
-        if (i + 1 < nt) p[a.out_stride] = o1;
-        p += 2 * a.out_stride;
+    for (int i = 0; i < kCount; ++i) {
+        Out o;
+        if constexpr (kBf16) o = __float2bfloat16_rn(acc[i]); else o = acc[i];
+        if (i < nt) *p = o;
+        p += a.out_stride;
     }
 }
 
-// acc += v * f for 32 tokens; f in shared memory.
-__device__ __forceinline__ void add_block(f32x2* acc, const uint32_t (&v)[32], uint32_t f) {
+// 32 columns of this thread's TMEM lane, asked for; columns_wait waits for every load of the thread, and nothing that uses
+// the registers moves ahead of it.
+__device__ __forceinline__ void columns_load(uint32_t (&v)[32], uint32_t taddr) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+                   "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+                   "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+                   "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+                 : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void columns_wait(uint32_t (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                   "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]),
+                   "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]),
+                   "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31]) :: "memory");
+}
+// 64 bytes of outputs (16 f32 or 32 bf16 channels from ch on) of each of the warp's 32 tokens t0 + lane: through shared memory (`stage`,
+// this warp's), where piece p of a token's 64 bytes is at 64 lane + 16 (p ^ (lane / 2 mod 4)), without bank conflicts.
+template <bool kBf16> __device__ __forceinline__ void store_piece(const Args& a, long long t0, long long T, int ch, int lane, const f32x2* acc, uint32_t stage) {
+    typedef typename std::conditional<kBf16, __nv_bfloat16, float>::type Out;
+    constexpr int kPer = 16 / (int)sizeof(Out);
+    __syncwarp();                                                        // the piece before this one has been read
 #pragma unroll
-    for (int i = 0; i < 32; i += 4) {
-        f32x2 f0, f1;
-        asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(f0), "=l"(f1) : "r"(f + i * 4));
-        acc[i / 2] = fma2(pair_of(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), f0, acc[i / 2]);
-        acc[i / 2 + 1] = fma2(pair_of(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), f1, acc[i / 2 + 1]);
+    for (int p = 0; p < 4; ++p) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x0, x1;
+            if constexpr (kBf16) {
+                unpair(acc[4 * p + i], x0, x1);
+                const __nv_bfloat162 h = __floats2bfloat162_rn(x0, x1);
+                w[i] = *reinterpret_cast<const uint32_t*>(&h);
+            } else {
+                unpair(acc[2 * p + i / 2], x0, x1);
+                w[i] = __float_as_uint(i & 1 ? x1 : x0);
+            }
+        }
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                     :: "r"(stage + (uint32_t)(lane * 64 + ((p ^ (lane >> 1 & 3)) * 16))), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    }
+    __syncwarp();
+    const int c = ch + (lane & 3) * kPer;
+    Out* out = reinterpret_cast<Out*>(a.out) + t0 * a.out_stride + c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int t = i * 8 + (lane >> 2);
+        uint4 v;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                     : "r"(stage + (uint32_t)(t * 64 + (((lane & 3) ^ (t >> 1 & 3)) * 16))) : "memory");
+        if (t0 + t >= T) continue;
+        if (a.vec_out && c + kPer <= a.N) {
+            *reinterpret_cast<uint4*>(out + t * a.out_stride) = v;
+        } else {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                if (c + e >= a.N) continue;
+                if constexpr (kBf16) out[t * a.out_stride + e] = __ushort_as_bfloat16((unsigned short)(w[e >> 1] >> (16 * (e & 1))));
+                else out[t * a.out_stride + e] = __uint_as_float(w[e]);
+            }
+        }
     }
 }
 
 // ---- many tokens: CTA pairs ---------------------------------------------------------------------------
 struct Shared2 {
-    alignas(16) float4 factor[kSlots][kTileN / 4];
     unsigned long long full[kMaxStages];
     unsigned long long empty[kMaxStages];
     unsigned long long acc_full[2];
-    unsigned long long acc_empty[2];      // the leader's copy counts 16 arrivals: 8 epilogue warps x 2 CTAs
-    unsigned long long f_full[kSlots];
-    unsigned long long f_empty[kSlots];
+    unsigned long long acc_empty[2];      // the leader's copy counts the epilogue warps of both CTAs
     unsigned long long drain;             // products in flight on an early way out
     uint32_t tmem_base;
     int abort;
@@ -107,14 +170,14 @@ static_assert(kDynSmem2 + sizeof(Shared2) <= 232448, "the ring must fit one CTA'
 
 // Tile j of this pair: token tiles are taken kTokenGroup at a time; within a group the token tiles of one channel tile
 // follow each other, so that every weight is fetched once per group and the group's codes stay in L2.
-__device__ __forceinline__ bool tile_of(uint32_t j, int n_m2, int n_tok, int& m2, int& n) {
+__device__ __forceinline__ bool tile_of(uint32_t j, int n_ch, int n_tok, int& ch, int& tok) {
     const long long id = (long long)(blockIdx.x >> 1) + (long long)j * (gridDim.x >> 1);
-    if (id >= (long long)n_m2 * n_tok) return false;
-    const long long per = (long long)kTokenGroup * n_m2;
+    if (id >= (long long)n_ch * n_tok) return false;
+    const long long per = (long long)kTokenGroup * n_ch;
     const int g = (int)(id / per), local = (int)(id - (long long)g * per);
-    const int n0 = g * kTokenGroup, width = min(kTokenGroup, n_tok - n0);
-    m2 = local / width;
-    n = n0 + local - m2 * width;
+    const int t0 = g * kTokenGroup, width = min(kTokenGroup, n_tok - t0);
+    ch = local / width;
+    tok = t0 + local - ch * width;
     return true;
 }
 
@@ -129,16 +192,15 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     const bool leader = rank == 0;
     volatile int* abort_flag = &sh.abort;
-    const int n_m2 = (a.N + 2 * kTileM - 1) / (2 * kTileM);
-    // a stage: 128 codes of K of this CTA's 128 channels and of its half of the token tile
+    const int n_ch = (a.N + a.tile_n - 1) / a.tile_n;
+    // a stage: 128 codes of K of this CTA's 128 tokens and of its half of the channels
     const uint32_t stage_bytes = (uint32_t)(kBytesA + a.tile_n / 2 * kBK);
     const uint32_t stages = min((uint32_t)kMaxStages, (uint32_t)kRingBytes / stage_bytes);
 
     if (tid == 0) {
         sh.abort = 0;
         for (uint32_t s = 0; s < stages; ++s) { init_bar(&sh.full[s], 1); init_bar(&sh.empty[s], 1); }
-        for (int b = 0; b < 2; ++b) { init_bar(&sh.acc_full[b], 1); init_bar(&sh.acc_empty[b], 16); }
-        for (int b = 0; b < kSlots; ++b) { init_bar(&sh.f_full[b], 1); init_bar(&sh.f_empty[b], 8); }
+        for (int b = 0; b < 2; ++b) { init_bar(&sh.acc_full[b], 1); init_bar(&sh.acc_empty[b], 2 * kEpiWarps); }
         init_bar(&sh.drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -156,15 +218,17 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     const uint32_t tmem_base = sh.tmem_base;
     enter_kernel();
     const long long T = true_rows(a);
-    const int n_tok = (int)((T + a.tile_n - 1) / a.tile_n);
+    const int n_tok = (int)((T + 2 * kTileM - 1) / (2 * kTileM));
 
+    // registers: launched with 168 a thread, 64,512 in all; 128 x 72 + 256 x 216 are as many
+    if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer (both CTAs)
         if (lane == 0) {
             uint32_t it = 0, s = 0, use = 0;
-            int m2, n;
-            for (uint32_t j = 0; tile_of(j, n_m2, n_tok, m2, n) && !*abort_flag; ++j) {
-                const int row_w = (2 * m2 + (int)rank) * kTileM, row_x = n * a.tile_n + (int)rank * (a.tile_n / 2);
+            int ch, tok;
+            for (uint32_t j = 0; tile_of(j, n_ch, n_tok, ch, tok) && !*abort_flag; ++j) {
+                const int row_x = (2 * tok + (int)rank) * kTileM, row_w = ch * a.tile_n + (int)rank * (a.tile_n / 2);
                 for (int k = 0; k < a.n_ksteps; ++k, ++it, s = s + 1 == stages ? 0 : s + 1, use += s == 0 ? 1 : 0) {
                     if (use > 0 && !lm_wait(lm_smem_u32(&sh.empty[s]), (use - 1) & 1, abort_flag, a.wait_limit_ns)) break;
                     const uint32_t bar_local = lm_smem_u32(&sh.full[s]), bar = bar_local & kPeerMask;
@@ -172,8 +236,8 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                     if (leader)                                        // the leader's barrier collects both CTAs' bytes
                         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;"
                                      :: "r"(bar_local), "r"(2 * stage_bytes + (it == 0 ? (uint32_t)a.test_extra_tx : 0u)) : "memory");
-                    lm_tma_2d_pair(dst, &map_w, bar, k * kBK, row_w, 0);
-                    lm_tma_2d_pair(dst + kBytesA, &map_x, bar, k * kBK, row_x, 0);
+                    lm_tma_2d_pair(dst, &map_x, bar, k * kBK, row_x, 0);
+                    lm_tma_2d_pair(dst + kBytesA, &map_w, bar, k * kBK, row_w, 0);
                 }
             }
             if (*abort_flag && leader) {                               // copies in flight get a bounded chance to land
@@ -189,22 +253,22 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         if (lane == 0 && leader) {
             const uint32_t desc = idesc(2 * kTileM, a.tile_n);
             uint32_t s = 0, use = 0, it = 0;
-            int m2, n;
+            int ch, tok;
             bool ok = true;
-            for (uint32_t j = 0; ok && tile_of(j, n_m2, n_tok, m2, n) && !*abort_flag; ++j) {
+            for (uint32_t j = 0; ok && tile_of(j, n_ch, n_tok, ch, tok) && !*abort_flag; ++j) {
                 for (int k = 0; k < a.n_ksteps; ++k, ++it, s = s + 1 == stages ? 0 : s + 1, use += s == 0 ? 1 : 0) {
                     const uint32_t b = it & 1, use_b = it >> 1;
-                    if (use_b > 0 && !lm_wait(lm_smem_u32(&sh.acc_empty[b]), (use_b - 1) & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
                     if (!lm_wait(lm_smem_u32(&sh.full[s]), use & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
+                    if (use_b > 0 && !lm_wait(lm_smem_u32(&sh.acc_empty[b]), (use_b - 1) & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t d_tmem = tmem_base + b * kTileN;
-                    const uint64_t dw = lm_smem_desc_k(tiles + s * stage_bytes), dx = lm_smem_desc_k(tiles + s * stage_bytes + kBytesA);
+                    const uint64_t dx = lm_smem_desc_k(tiles + s * stage_bytes), dw = lm_smem_desc_k(tiles + s * stage_bytes + kBytesA);
 #pragma unroll
                     for (int kk = 0; kk < kBK / 32; ++kk) {              // 32 codes of K per instruction
                         asm volatile("{\n\t.reg .pred p;\n\t"
                                      "setp.ne.b32 p, %4, 0;\n\t"
                                      "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-                                     :: "r"(d_tmem), "l"(dw + kk * 2), "l"(dx + kk * 2), "r"(desc), "r"(kk > 0 ? 1u : 0u) : "memory");
+                                     :: "r"(d_tmem), "l"(dx + kk * 2), "l"(dw + kk * 2), "r"(desc), "r"(kk > 0 ? 1u : 0u) : "memory");
                     }
                     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                                  :: "r"(lm_smem_u32(&sh.acc_full[b])), "h"((unsigned short)3) : "memory");
@@ -217,83 +281,71 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 lm_wait_plain(lm_smem_u32(&sh.drain), 0, a.wait_limit_ns);
             }
         }
-    } else if (warp == 2) {
-        // ------------------------------------------------------------------ factors of the blocks: 8 tokens per lane
-        uint32_t it = 0;
-        int m2, n;
-        bool ok = true;
-        for (uint32_t j = 0; ok && tile_of(j, n_m2, n_tok, m2, n); ++j) {
-            const float* sw = a.w_scale + (long long)(2 * m2 + (int)rank) * a.ws_stride;
-            const bool live = (2 * m2 + (int)rank) * kTileM < a.N;
-            const long long t0 = (long long)n * a.tile_n + lane * 4;
-            for (int k0 = 0; ok && k0 < a.n_ksteps; k0 += kBatch) {
-                float f[kBatch][8];
-#pragma unroll
-                for (int i = 0; i < kBatch; ++i) {
-                    const float* p = a.x_scale + (long long)(k0 + i) * a.xs_stride + t0;
-                    const float w = live && k0 + i < a.n_ksteps ? sw[k0 + i] : 0.0f;
-#pragma unroll
-                    for (int h = 0; h < 8; ++h) {
-                        const int t = h < 4 ? h : 124 + h;                   // tokens 4 lane .. and 128 + 4 lane ..
-                        f[i][h] = k0 + i < a.n_ksteps && t0 + t < T ? p[t] * w : 0.0f;
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < kBatch; ++i) {
-                    if (k0 + i >= a.n_ksteps) break;
-                    const uint32_t slot = it % kSlots, use = it / kSlots;
-                    if (use > 0 && !__all_sync(0xffffffffu, lm_wait(lm_smem_u32(&sh.f_empty[slot]), (use - 1) & 1, abort_flag, a.wait_limit_ns))) { ok = false; break; }
-                    sh.factor[slot][lane] = make_float4(f[i][0], f[i][1], f[i][2], f[i][3]);
-                    sh.factor[slot][32 + lane] = make_float4(f[i][4], f[i][5], f[i][6], f[i][7]);
-                    __syncwarp();
-                    if (lane == 0) lm_arrive(lm_smem_u32(&sh.f_full[slot]));
-                    ++it;
-                }
-            }
-        }
     } else if (warp >= 4) {
         // ------------------------------------------------------------------ epilogue (warps 4..11, both CTAs)
-        const int q = warp & 3, half = (warp - 4) >> 2;                  // TMEM lane quarter of this warp; which blocks of 32 tokens
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        const int q = warp & 3, half = (warp - 4) >> 2;                  // TMEM lane quarter of this warp; which half of the channels
+        const int blocks = a.tile_n / 64, first = half * (a.tile_n / 2); // blocks of 32 channels, the first of them
+        const uint32_t stage = tiles + (uint32_t)kRingBytes + (uint32_t)((warp - 4) * kStageOut);
         uint32_t it = 0;
-        int m2, n;
+        int ch, tok;
         bool ok = true;
-        for (uint32_t j = 0; ok && tile_of(j, n_m2, n_tok, m2, n); ++j) {
+        for (uint32_t j = 0; ok && tile_of(j, n_ch, n_tok, ch, tok); ++j) {
+            const long long t0 = (2ll * tok + (int)rank) * kTileM + q * 32;
+            const int ch0 = ch * a.tile_n + first;
+            // this thread's factors, asked for two blocks ahead; 0 for rows and channels past the end
+            const bool live = t0 + lane < T && ch0 < a.N;
+            const float* xs = a.x_scale + (live ? t0 + lane : 0);
+            const float* ws = a.w_scale + (live ? (long long)(ch0 / kBK) * a.ws_stride : 0);
+            float sx[2] = {0.0f, 0.0f}, sw[2] = {0.0f, 0.0f};
+            if (live) {
+                sx[0] = xs[0]; sw[0] = ws[0];
+                if (a.n_ksteps > 1) { sx[1] = xs[a.xs_stride]; sw[1] = ws[1]; }
+            }
             f32x2 acc[64];
 #pragma unroll
             for (int i = 0; i < 64; ++i) acc[i] = 0ull;
 #pragma unroll 1
             for (int k = 0; k < a.n_ksteps; ++k, ++it) {
-                const uint32_t b = it & 1, use_b = it >> 1, slot = it % kSlots;
-                // warp-uniform outcome: the tcgen05.ld below must be executed by all 32 lanes together
-                ok = __all_sync(0xffffffffu, lm_wait(lm_smem_u32(&sh.f_full[slot]), (it / kSlots) & 1, abort_flag, a.wait_limit_ns) &&
-                                             lm_wait(lm_smem_u32(&sh.acc_full[b]), use_b & 1, abort_flag, a.wait_limit_ns));
+                const uint32_t b = it & 1, use_b = it >> 1;
+                const float f1 = sx[0] * sw[0];
+                const f32x2 f = pair_of(f1, f1);
+                sx[0] = sx[1]; sw[0] = sw[1];
+                if (live && k + 2 < a.n_ksteps) { sx[1] = xs[(k + 2) * a.xs_stride]; sw[1] = ws[k + 2]; }
+                ok = warp_wait(&sh.acc_full[b], use_b & 1, abort_flag, a.wait_limit_ns);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + b * kTileN, f = lm_smem_u32(&sh.factor[slot][0]);
+                const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + b * kTileN + (uint32_t)first;
+                uint32_t v[2][32];
+                columns_load(v[0], taddr);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    const int col = (2 * c + half) * 32;
-                    if (col < a.tile_n) {
-                        uint32_t v[32];
-                        lm_tmem_load32(v, taddr + (uint32_t)col);
-                        add_block(acc + c * 16, v, f + (uint32_t)col * 4u);
+                    if (c < blocks) {                                    // a block's loads run under the one before it
+                        columns_wait(v[c & 1]);
+                        if (c + 1 < blocks) {
+                            columns_load(v[(c + 1) & 1], taddr + (uint32_t)((c + 1) * 32));
+                        } else {                                         // all read: the leader's MMA thread waits for every epilogue warp
+                            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                            __syncwarp();
+                            if (lane == 0)
+                                asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(lm_smem_u32(&sh.acc_empty[b]) & kPeerMask) : "memory");
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            acc[16 * c + i] = fma2(pair_of(__uint_as_float(v[c & 1][2 * i]), __uint_as_float(v[c & 1][2 * i + 1])), f, acc[16 * c + i]);
                     }
-                }
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) {                                         // the leader's MMA thread waits for all 16 warps
-                    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(lm_smem_u32(&sh.acc_empty[b]) & kPeerMask) : "memory");
-                    lm_arrive(lm_smem_u32(&sh.f_empty[slot]));
                 }
             }
             if (!ok) break;
-            const int ch = (2 * m2 + (int)rank) * kTileM + q * 32 + lane;
+            if (t0 < T) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const long long t0 = (long long)n * a.tile_n + (2 * c + half) * 32;
-                if ((2 * c + half) * 32 < a.tile_n && t0 < T) store_tokens<kBf16, 32>(a, t0, T, ch, acc + c * 16);
+                for (int c = 0; c < 4; ++c) {
+                    if (c >= blocks || ch0 + 32 * c >= a.N) break;
+                    store_piece<kBf16>(a, t0, T, ch0 + 32 * c, lane, acc + 16 * c, stage);
+                    if constexpr (!kBf16) store_piece<kBf16>(a, t0, T, ch0 + 32 * c + 16, lane, acc + 16 * c + 8, stage);
+                }
             }
-            __syncwarp();                                                // lanes without a channel went ahead; the next load wants all
+            __syncwarp();
         }
     }
 
@@ -320,15 +372,14 @@ template <int kNB> struct Small {
     static constexpr int kThreads = 128 + kHalves * 128;
     static constexpr int kCols = kNB / kHalves;                                              // tokens of an epilogue warp
     static constexpr int kChunk = kCols < 32 ? kCols : 32;
-    static constexpr size_t kDynSmem = (size_t)kStages * kStageBytes + 1024;
+    static constexpr int kSlotBytes = kNB * 4 < 128 ? 128 : kNB * 4;
+    static constexpr size_t kDynSmem = (size_t)kStages * kStageBytes + kSlots * kSlotBytes + 1024;
+    static_assert(kStages + kBufs + 1 < kSlots, "a slot's turn comes again too soon");
     struct Shared {
-        alignas(16) float factor[kSlots][kNB];
         unsigned long long full[kStages];
         unsigned long long empty[kStages];
         unsigned long long acc_full[kBufs];
         unsigned long long acc_empty[kBufs];
-        unsigned long long f_full[kSlots];
-        unsigned long long f_empty[kSlots];
         unsigned long long done;
         uint32_t tmem_base;
         int abort;
@@ -347,11 +398,12 @@ __device__ __forceinline__ void tmem_load16(uint32_t (&v)[16], uint32_t taddr) {
 
 template <int kNB, bool kBf16>
 __global__ void __launch_bounds__(Small<kNB>::kThreads, Small<kNB>::kPerSm)
-linear_f8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const Args a, int n_ch, int split) {
+linear_f8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_s,
+                       const Args a, int n_ch, int split) {
     typedef Small<kNB> S;
     extern __shared__ unsigned char f8_raw[];
     __shared__ typename S::Shared sh;
-    const uint32_t tiles = (lm_smem_u32(f8_raw) + 1023u) & ~1023u;
+    const uint32_t tiles = (lm_smem_u32(f8_raw) + 1023u) & ~1023u, slots = tiles + (uint32_t)(S::kStages * S::kStageBytes);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     volatile int* abort_flag = &sh.abort;
     const int part = (int)(blockIdx.x % (unsigned)split);                 // rank in the cluster: clusters are consecutive CTAs
@@ -364,7 +416,6 @@ linear_f8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
         sh.abort = 0;
         for (int s = 0; s < S::kStages; ++s) { init_bar(&sh.full[s], 1); init_bar(&sh.empty[s], 1); }
         for (int b = 0; b < S::kBufs; ++b) { init_bar(&sh.acc_full[b], 1); init_bar(&sh.acc_empty[b], 4 * S::kHalves); }
-        for (int b = 0; b < kSlots; ++b) { init_bar(&sh.f_full[b], 1); init_bar(&sh.f_empty[b], 4 * S::kHalves); }
         init_bar(&sh.done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -384,7 +435,7 @@ linear_f8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
 
     const int q = warp & 3, row = q * 32 + lane, half = (warp - 4) >> 2;
     const int ch = m * kTileM + row;
-    f32x2 acc[S::kCols / 2];
+    float acc[S::kCols];
     bool live = false;
     if (warp == 0) {
         if (lane == 0) {
@@ -394,9 +445,10 @@ linear_f8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
                 if (use > 0 && !lm_wait(lm_smem_u32(&sh.empty[s]), (use - 1) & 1, abort_flag, a.wait_limit_ns)) break;
                 const uint32_t bar = lm_smem_u32(&sh.full[s]), dst = tiles + s * S::kStageBytes;
                 asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;"
-                             :: "r"(bar), "r"((uint32_t)S::kStageBytes + (it == 0 ? (uint32_t)a.test_extra_tx : 0u)) : "memory");
+                             :: "r"(bar), "r"((uint32_t)(S::kStageBytes + kNB * 4) + (it == 0 ? (uint32_t)a.test_extra_tx : 0u)) : "memory");
                 lm_tma_2d(dst, &map_w, bar, k * kBK, m * kTileM, 0);
                 lm_tma_2d(dst + kBytesA, &map_x, bar, k * kBK, (int)t_tile, 0);
+                lm_tma_2d(slots + (uint32_t)(it % kSlots * S::kSlotBytes), &map_s, bar, (int)t_tile, k, 0);
             }
             if (*abort_flag) {
                 const int pending = it < S::kStages ? it : S::kStages;
@@ -429,70 +481,42 @@ linear_f8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
             asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(lm_smem_u32(&sh.done)) : "memory");
             lm_wait_plain(lm_smem_u32(&sh.done), 0, a.wait_limit_ns);
         }
-    } else if (warp == 2) {
-        constexpr int kPer = kNB < 32 ? 1 : kNB / 32;
-        const float* sw = a.w_scale + (long long)m * a.ws_stride;
-        uint32_t it = 0;
-        bool ok = true;
-        for (int k = k0; ok && k < k1; k += kBatch) {
-            float f[kBatch][kPer];
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                const float w = k + i < k1 ? sw[k + i] : 0.0f;
-#pragma unroll
-                for (int h = 0; h < kPer; ++h) {
-                    const long long t = t_tile + h * 32 + lane;
-                    f[i][h] = k + i < k1 && t < T && h * 32 + lane < kNB ? a.x_scale[(long long)(k + i) * a.xs_stride + t] * w : 0.0f;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                if (k + i >= k1) break;
-                const uint32_t slot = it % kSlots, use = it / kSlots;
-                if (use > 0 && !__all_sync(0xffffffffu, lm_wait(lm_smem_u32(&sh.f_empty[slot]), (use - 1) & 1, abort_flag, a.wait_limit_ns))) { ok = false; break; }
-#pragma unroll
-                for (int h = 0; h < kPer; ++h)
-                    if (h * 32 + lane < kNB) sh.factor[slot][h * 32 + lane] = f[i][h];
-                __syncwarp();
-                if (lane == 0) lm_arrive(lm_smem_u32(&sh.f_full[slot]));
-                ++it;
-            }
-        }
     } else if (warp >= 4) {
 #pragma unroll
-        for (int i = 0; i < S::kCols / 2; ++i) acc[i] = 0ull;
+        for (int i = 0; i < S::kCols; ++i) acc[i] = 0.0f;
         live = true;
+        const float* ws = a.w_scale + (long long)m * a.ws_stride;
+        float next_sw = k0 < k1 ? ws[k0] : 0.0f;
         uint32_t it = 0;
 #pragma unroll 1
         for (int k = k0; k < k1; ++k, ++it) {
-            const uint32_t b = it % S::kBufs, slot = it % kSlots;
-            live = __all_sync(0xffffffffu, lm_wait(lm_smem_u32(&sh.f_full[slot]), (it / kSlots) & 1, abort_flag, a.wait_limit_ns) &&
-                                           lm_wait(lm_smem_u32(&sh.acc_full[b]), (it / S::kBufs) & 1, abort_flag, a.wait_limit_ns));
+            const uint32_t b = it % S::kBufs;
+            const float sw = next_sw;
+            if (k + 1 < k1) next_sw = ws[k + 1];
+            live = warp_wait(&sh.acc_full[b], (it / S::kBufs) & 1, abort_flag, a.wait_limit_ns);
             if (!live) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + b * S::kPitch + (uint32_t)(half * S::kCols);
-            const uint32_t f = lm_smem_u32(&sh.factor[slot][half * S::kCols]);
+            const uint32_t f = slots + it % kSlots * S::kSlotBytes + (uint32_t)(half * S::kCols * 4);
 #pragma unroll
             for (int c = 0; c < S::kCols / S::kChunk; ++c) {
-                if constexpr (S::kChunk == 32) {
-                    uint32_t v[32];
-                    lm_tmem_load32(v, taddr + (uint32_t)(c * 32));
-                    add_block(acc + c * 16, v, f + (uint32_t)(c * 32) * 4u);
-                } else {
-                    uint32_t v[16];
-                    tmem_load16(v, taddr);
+                uint32_t v[S::kChunk];
+                if constexpr (S::kChunk == 32) lm_tmem_load32(v, taddr + (uint32_t)(c * 32)); else tmem_load16(v, taddr);
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        f32x2 f0, f1;
-                        asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(f0), "=l"(f1) : "r"(f + i * 4));
-                        acc[i / 2] = fma2(pair_of(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), f0, acc[i / 2]);
-                        acc[i / 2 + 1] = fma2(pair_of(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), f1, acc[i / 2 + 1]);
-                    }
+                for (int i = 0; i < S::kChunk; i += 4) {
+                    float4 sx;
+                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(sx.x), "=f"(sx.y), "=f"(sx.z), "=f"(sx.w)
+                                 : "r"(f + (uint32_t)(c * S::kChunk + i) * 4u) : "memory");
+                    float* o = acc + c * S::kChunk + i;
+                    o[0] = fmaf(__uint_as_float(v[i]), sx.x * sw, o[0]);
+                    o[1] = fmaf(__uint_as_float(v[i + 1]), sx.y * sw, o[1]);
+                    o[2] = fmaf(__uint_as_float(v[i + 2]), sx.z * sw, o[2]);
+                    o[3] = fmaf(__uint_as_float(v[i + 3]), sx.w * sw, o[3]);
                 }
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            if (lane == 0) { lm_arrive(lm_smem_u32(&sh.acc_empty[b])); lm_arrive(lm_smem_u32(&sh.f_empty[slot])); }
+            if (lane == 0) lm_arrive(lm_smem_u32(&sh.acc_empty[b]));
         }
         live = live && !__any_sync(0xffffffffu, *abort_flag);
         if (live) {
@@ -500,19 +524,14 @@ linear_f8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
 #pragma unroll
                 for (int c = 0; c < S::kCols / S::kChunk; ++c) {
                     const long long t0 = t_tile + half * S::kCols + c * S::kChunk;
-                    if (t0 < T) store_tokens<kBf16, S::kChunk>(a, t0, T, ch, acc + c * S::kChunk / 2);
+                    if (t0 < T) store_tokens<kBf16, S::kChunk>(a, t0, T, ch, acc + c * S::kChunk);
                 }
             } else {
                 // partial sums to shared memory, [token][channel], in the ring: nothing reads or writes that any more, the last
                 // block's products being complete
 #pragma unroll
-                for (int i = 0; i < S::kCols; i += 2) {
-                    float x0, x1;
-                    unpair(acc[i / 2], x0, x1);
-                    const uint32_t at = tiles + (uint32_t)((half * S::kCols + i) * kTileM + row) * 4u;
-                    asm volatile("st.shared.f32 [%0], %1;" :: "r"(at), "f"(x0) : "memory");
-                    asm volatile("st.shared.f32 [%0], %1;" :: "r"(at + kTileM * 4u), "f"(x1) : "memory");
-                }
+                for (int i = 0; i < S::kCols; ++i)
+                    asm volatile("st.shared.f32 [%0], %1;" :: "r"(tiles + (uint32_t)((half * S::kCols + i) * kTileM + row) * 4u), "f"(acc[i]) : "memory");
             }
         }
         __syncwarp();
@@ -733,6 +752,21 @@ static int make_map(CUtensorMap* map, const void* base, long long rows, int K, l
     return DPPO_OK;
 }
 
+// The tokens' scales, f32 [blocks x tokens] with `ld` elements between blocks: boxes of `tokens` of one block.
+static int make_scale_map(CUtensorMap* map, const float* base, long long rows, int blocks, long long ld, int tokens) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return fail(DPPO_ERR_CUDA, "linear_f8: cuTensorMapEncodeTiled is not available from this driver");
+    const cuuint64_t dims[2] = {(cuuint64_t)rows, (cuuint64_t)blocks};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld * 4};
+    const cuuint32_t box[2] = {(cuuint32_t)tokens, 1};
+    const cuuint32_t estr[2] = {1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<float*>(base), dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(DPPO_ERR_CUDA, "linear_f8: cuTensorMapEncodeTiled failed with %d", (int)r);
+    return DPPO_OK;
+}
+
 // Raises a kernel's shared-memory limit once per device.
 template <class Kernel> static int raise_smem(Kernel kernel, size_t bytes, bool (&done)[64]) {
     int dev = 0;
@@ -746,10 +780,10 @@ template <class Kernel> static int raise_smem(Kernel kernel, size_t bytes, bool 
 
 // ---- which kernel, which tile: both kernels' times in microseconds ----
 static double pair_time(long long M, int N, int n_ksteps, int* tile) {
-    const long long n_m2 = (N + 255) / 256, pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
+    const long long n_tok = (M + 255) / 256, pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
     double best = 0.0;
-    for (int tn = kTileN; tn >= 64; tn -= 32) {
-        const long long tiles = n_m2 * ((M + tn - 1) / tn), waves = (tiles + pairs - 1) / pairs;
+    for (int tn = kTileN; tn >= 64; tn /= 2) {
+        const long long tiles = n_tok * ((N + tn - 1) / tn), waves = (tiles + pairs - 1) / pairs;
         const double slab = tn * 0.0018 > 0.3 ? tn * 0.0018 : 0.3;
         const double t = 2.9 + (double)waves * (n_ksteps * slab + 0.3 + 0.011 * tn);
         if (best == 0.0 || t < best) { best = t; *tile = tn; }
@@ -781,11 +815,11 @@ template <bool kBf16> static int launch_pair(const CUtensorMap& mw, const CUtens
     static bool raised[64];
     const int rc = raise_smem(kernel, kDynSmem2, raised);
     if (rc != DPPO_OK) return rc;
-    const long long work = (long long)((a.N + 255) / 256) * ((a.M_max + a.tile_n - 1) / a.tile_n), most = sm_count() / 2;
+    const long long work = (long long)((a.N + a.tile_n - 1) / a.tile_n) * ((a.M_max + 2 * kTileM - 1) / (2 * kTileM)), most = sm_count() / 2;
     return launch_after("linear_f8 launch", kernel, 2 * (work < most ? work : most), kThreads, kDynSmem2, s, 2, mw, mx, a);
 }
 
-template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, int split, cudaStream_t s) {
+template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, const CUtensorMap& mx, const CUtensorMap& ms, const Args& a, int split, cudaStream_t s) {
     auto kernel = linear_f8_small_kernel<kNB, kBf16>;
     static bool raised[64];
     const int rc = raise_smem(kernel, Small<kNB>::kDynSmem, raised);
@@ -793,16 +827,16 @@ template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, co
     const int n_ch = (a.N + kTileM - 1) / kTileM;
     const long long tiles = (long long)n_ch * ((a.M_max + kNB - 1) / kNB);
     if (tiles * split > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "linear_f8: too many tiles");
-    return launch_after("linear_f8 launch", kernel, tiles * split, Small<kNB>::kThreads, Small<kNB>::kDynSmem, s, split, mw, mx, a, n_ch, split);
+    return launch_after("linear_f8 launch", kernel, tiles * split, Small<kNB>::kThreads, Small<kNB>::kDynSmem, s, split, mw, mx, ms, a, n_ch, split);
 }
 
-template <bool kBf16> static int launch(bool pair, int nb, int split, const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
+template <bool kBf16> static int launch(bool pair, int nb, int split, const CUtensorMap& mw, const CUtensorMap& mx, const CUtensorMap& ms, const Args& a, cudaStream_t s) {
     if (pair) return launch_pair<kBf16>(mw, mx, a, s);
     switch (nb) {
-        case 16: return launch_small<16, kBf16>(mw, mx, a, split, s);
-        case 32: return launch_small<32, kBf16>(mw, mx, a, split, s);
-        case 64: return launch_small<64, kBf16>(mw, mx, a, split, s);
-        default: return launch_small<128, kBf16>(mw, mx, a, split, s);
+        case 16: return launch_small<16, kBf16>(mw, mx, ms, a, split, s);
+        case 32: return launch_small<32, kBf16>(mw, mx, ms, a, split, s);
+        case 64: return launch_small<64, kBf16>(mw, mx, ms, a, split, s);
+        default: return launch_small<128, kBf16>(mw, mx, ms, a, split, s);
     }
 }
 
@@ -852,9 +886,10 @@ extern "C" int dppo_linear_f8(const dppo_linear_f8_params* p, const uint8_t* x, 
     if (variant < 0 || variant > 2 || p->variant == 100) return fail(DPPO_ERR_INVALID_ARG, "linear_f8: variant %d", p->variant);
     if (p->M_max == 0) return DPPO_OK;
     if (!x || !x_scale || !w || !w_scale || !out) return fail(DPPO_ERR_INVALID_ARG, "linear_f8: NULL array");
-    if (((uintptr_t)x & 15) || ((uintptr_t)w & 15) || p->x_stride % 16 != 0 || p->w_stride % 16 != 0)
-        return fail(DPPO_ERR_MISALIGNED, "linear_f8: x / w base and row strides must be multiples of 16 bytes");
-    if (p->x_stride >= (1ll << 40) || p->w_stride >= (1ll << 40)) return fail(DPPO_ERR_BAD_SHAPE, "linear_f8: strides of x and w must be below 2^40");
+    if (((uintptr_t)x & 15) || ((uintptr_t)w & 15) || ((uintptr_t)x_scale & 15) || p->x_stride % 16 != 0 || p->w_stride % 16 != 0 || p->x_scale_stride % 4 != 0)
+        return fail(DPPO_ERR_MISALIGNED, "linear_f8: x / w / x_scale base and row strides must be multiples of 16 bytes");
+    if (p->x_stride >= (1ll << 40) || p->w_stride >= (1ll << 40) || p->x_scale_stride >= (1ll << 38))
+        return fail(DPPO_ERR_BAD_SHAPE, "linear_f8: strides of x, w and x_scale must be below 2^40 bytes");
 
     f8::Args a = {};
     a.x_scale = x_scale; a.w_scale = w_scale; a.out = out; a.n_rows_dev = n_rows_dev; a.status = status;
@@ -865,11 +900,12 @@ extern "C" int dppo_linear_f8(const dppo_linear_f8_params* p, const uint8_t* x, 
     int nb = 0, split = 1;
     const double t_pair = f8::pair_time(p->M_max, p->N, n_blocks, &a.tile_n), t_small = f8::small_time(p->M_max, p->N, n_blocks, &nb, &split);
     const bool pair = variant == 1 || (variant == 0 && t_pair < t_small);
-    if (pair) nb = a.tile_n / 2;
-    alignas(64) CUtensorMap mw, mx;
-    int rc = f8::make_map(&mw, w, p->N, p->K, p->w_stride, f8::kTileM);
-    if (rc == DPPO_OK) rc = f8::make_map(&mx, x, p->M_max, p->K, p->x_stride, nb);
+    a.vec_out = ((uintptr_t)out & 15) == 0 && p->out_stride * (a.out_bf16 ? 2 : 4) % 16 == 0;
+    alignas(64) CUtensorMap mw, mx, ms;
+    int rc = f8::make_map(&mw, w, p->N, p->K, p->w_stride, pair ? a.tile_n / 2 : f8::kTileM);
+    if (rc == DPPO_OK) rc = f8::make_map(&mx, x, p->M_max, p->K, p->x_stride, pair ? f8::kTileM : nb);
+    if (rc == DPPO_OK && !pair) rc = f8::make_scale_map(&ms, x_scale, p->M_max, n_blocks, p->x_scale_stride, nb);
     if (rc != DPPO_OK) return rc;
     cudaStream_t s = (cudaStream_t)stream;
-    return a.out_bf16 ? f8::launch<true>(pair, nb, split, mw, mx, a, s) : f8::launch<false>(pair, nb, split, mw, mx, a, s);
+    return a.out_bf16 ? f8::launch<true>(pair, nb, split, mw, mx, ms, a, s) : f8::launch<false>(pair, nb, split, mw, mx, ms, a, s);
 }

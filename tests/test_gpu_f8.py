@@ -31,7 +31,7 @@ def quantize(B, x, K, rows, n_dev=None, extra=0):
     M = x.shape[0]
     kb = (K + 127) // 128
     q = torch.full((M + 1, pad(K, 16) + 16 * extra), 0x55, dtype=torch.uint8, device="cuda")
-    s = torch.full((kb + 1, M + extra) if rows == 1 else ((M + 127) // 128 + 1, kb + extra), -7.5, device="cuda")
+    s = torch.full((kb + 1, pad(M, 4) + 4 * extra) if rows == 1 else ((M + 127) // 128 + 1, kb + extra), -7.5, device="cuda")
     B.quantize_f8(B.QuantizeF8Params(M, K, B.BF16 if x.dtype is torch.bfloat16 else B.F32, x.stride(0), q.stride(0), s.stride(0), rows), x,
                   q.view(F8), s, n_dev)
     return q, s
