@@ -14,9 +14,9 @@
 //     x 151,936: 1,260 us).  The outputs are transposed through shared memory, once per tile.
 //   few tokens (bound by reading the weights): a CTA per 128 channels, 16 to 128 tokens on the N side, so that few tokens waste
 //     nothing; the contraction is split over the CTAs of a cluster when there are too few tiles to keep all SMs reading, and the
-//     partial sums are joined in a fixed order through distributed shared memory.  The tokens' scales of a block travel with its codes,
-//     through a ring of their own that is longer than the codes' (kSlots > stages + accumulators + 1): a slot is then read
-//     long before its turn comes again, with no barrier.
+//     partial sums are joined in a fixed order through distributed shared memory.
+// The tokens' scales of a block travel with its codes, through a ring of their own that is longer than the codes' (kSlots > stages +
+// accumulators + 1): a slot is then read long before its turn comes again, with no barrier.
 // Every wait is bounded; on a time-out the CTA reports DPPO_STATUS_TIMEOUT, leaves its loops, lets copies and products
 // in flight finish (bounded), frees its tensor memory and returns.
 #include <cuda_fp8.h>
@@ -36,14 +36,15 @@ constexpr int kBK = 128;                  // codes of a block = of a stage
 constexpr int kTileM = 128;               // rows of the M side per CTA
 constexpr int kTileN = 256;               // most channels per tile of the pair kernel
 constexpr int kBytesA = kTileM * kBK;
-constexpr int kMaxStages = 9;
-constexpr int kSlots = 16;                // few tokens: blocks whose token scales are in shared memory
+constexpr int kMaxStages = 9;             // + 2 accumulators + 1 < kSlots
+constexpr int kSlots = 16;                // blocks whose token scales are in shared memory
 constexpr int kEpiWarps = 8;              // pair kernel: two per TMEM lane quarter, half of the tile's channels each
 constexpr int kThreads = 128 + 32 * kEpiWarps;     // producer, MMA and two idle warps before them
 constexpr int kTokenGroup = 8;            // token tiles swept together (2,048 tokens: 5 MB of codes at K = 2,560)
 constexpr int kRingBytes = 6 * (kBytesA + kTileN / 2 * kBK);
 constexpr int kStageOut = 2048;           // 64 bytes of outputs of 32 tokens: what an epilogue warp transposes at a time
-constexpr size_t kDynSmem2 = (size_t)kRingBytes + kEpiWarps * kStageOut + 1024;
+constexpr int kSlotBytes2 = kTileM * 4;   // pair kernel: of this CTA's tokens
+constexpr size_t kDynSmem2 = (size_t)kRingBytes + kEpiWarps * kStageOut + kSlots * kSlotBytes2 + 1024;
 
 struct Args {
     const float* x_scale;
@@ -183,10 +184,11 @@ __device__ __forceinline__ bool tile_of(uint32_t j, int n_ch, int n_tok, int& ch
 
 template <bool kBf16>
 __global__ void __launch_bounds__(kThreads, 1)
-linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const Args a) {
+linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_s,
+                      const Args a) {
     extern __shared__ unsigned char f8_raw[];
     __shared__ Shared2 sh;
-    const uint32_t tiles = (lm_smem_u32(f8_raw) + 1023u) & ~1023u;
+    const uint32_t tiles = (lm_smem_u32(f8_raw) + 1023u) & ~1023u, slots = tiles + (uint32_t)(kRingBytes + kEpiWarps * kStageOut);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     uint32_t rank;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -235,9 +237,10 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                     const uint32_t dst = tiles + s * stage_bytes;
                     if (leader)                                        // the leader's barrier collects both CTAs' bytes
                         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;"
-                                     :: "r"(bar_local), "r"(2 * stage_bytes + (it == 0 ? (uint32_t)a.test_extra_tx : 0u)) : "memory");
+                                     :: "r"(bar_local), "r"(2 * (stage_bytes + (uint32_t)kSlotBytes2) + (it == 0 ? (uint32_t)a.test_extra_tx : 0u)) : "memory");
                     lm_tma_2d_pair(dst, &map_x, bar, k * kBK, row_x, 0);
                     lm_tma_2d_pair(dst + kBytesA, &map_w, bar, k * kBK, row_w, 0);
+                    lm_tma_2d_pair(slots + (it % kSlots) * kSlotBytes2, &map_s, bar, row_x, k, 0);
                 }
             }
             if (*abort_flag && leader) {                               // copies in flight get a bounded chance to land
@@ -293,31 +296,26 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         for (uint32_t j = 0; ok && tile_of(j, n_ch, n_tok, ch, tok); ++j) {
             const long long t0 = (2ll * tok + (int)rank) * kTileM + q * 32;
             const int ch0 = ch * a.tile_n + first;
-            // this thread's factors, asked for two blocks ahead; 0 for rows and channels past the end
-            const bool live = t0 + lane < T && ch0 < a.N;
-            const float* xs = a.x_scale + (live ? t0 + lane : 0);
-            const float* ws = a.w_scale + (live ? (long long)(ch0 / kBK) * a.ws_stride : 0);
-            float sx[2] = {0.0f, 0.0f}, sw[2] = {0.0f, 0.0f};
-            if (live) {
-                sx[0] = xs[0]; sw[0] = ws[0];
-                if (a.n_ksteps > 1) { sx[1] = xs[a.xs_stride]; sw[1] = ws[1]; }
-            }
+            // the channels' scales of 32 blocks, one per lane; 0 past the last channel
+            const float* ws = a.w_scale + (ch0 < a.N ? (long long)(ch0 / kBK) * a.ws_stride : 0);
+            float sw32 = 0.0f;
             f32x2 acc[64];
 #pragma unroll
             for (int i = 0; i < 64; ++i) acc[i] = 0ull;
+            const uint32_t lanes = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)first;
+            uint32_t v[2][32];
+            ok = warp_wait(&sh.acc_full[it & 1], (it >> 1) & 1, abort_flag, a.wait_limit_ns);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            columns_load(v[0], lanes + (it & 1) * kTileN);
 #pragma unroll 1
             for (int k = 0; k < a.n_ksteps; ++k, ++it) {
-                const uint32_t b = it & 1, use_b = it >> 1;
-                const float f1 = sx[0] * sw[0];
+                const uint32_t b = it & 1, taddr = lanes + b * kTileN;
+                if ((k & 31) == 0) sw32 = ch0 < a.N && k + lane < a.n_ksteps ? ws[k + lane] : 0.0f;
+                float sx;
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(sx) : "r"(slots + (it % kSlots) * kSlotBytes2 + (uint32_t)((q * 32 + lane) * 4)) : "memory");
+                const float f1 = sx * __shfl_sync(0xffffffffu, sw32, k & 31);
                 const f32x2 f = pair_of(f1, f1);
-                sx[0] = sx[1]; sw[0] = sw[1];
-                if (live && k + 2 < a.n_ksteps) { sx[1] = xs[(k + 2) * a.xs_stride]; sw[1] = ws[k + 2]; }
-                ok = warp_wait(&sh.acc_full[b], use_b & 1, abort_flag, a.wait_limit_ns);
-                if (!ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + b * kTileN + (uint32_t)first;
-                uint32_t v[2][32];
-                columns_load(v[0], taddr);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     if (c < blocks) {                                    // a block's loads run under the one before it
@@ -329,11 +327,25 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                             __syncwarp();
                             if (lane == 0)
                                 asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(lm_smem_u32(&sh.acc_empty[b]) & kPeerMask) : "memory");
+                            if (c == 3 && k + 1 < a.n_ksteps) {          // the next accumulator's first columns, under this one's last sums
+                                ok = warp_wait(&sh.acc_full[b ^ 1], ((it + 1) >> 1) & 1, abort_flag, a.wait_limit_ns);
+                                if (ok) {
+                                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                                    columns_load(v[0], lanes + (b ^ 1) * kTileN);
+                                }
+                            }
                         }
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
                             acc[16 * c + i] = fma2(pair_of(__uint_as_float(v[c & 1][2 * i]), __uint_as_float(v[c & 1][2 * i + 1])), f, acc[16 * c + i]);
                     }
+                }
+                if (!ok) break;
+                if (blocks < 4 && k + 1 < a.n_ksteps) {                  // narrow tiles: no registers to spare before
+                    ok = warp_wait(&sh.acc_full[b ^ 1], ((it + 1) >> 1) & 1, abort_flag, a.wait_limit_ns);
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    columns_load(v[0], lanes + (b ^ 1) * kTileN);
                 }
             }
             if (!ok) break;
@@ -810,13 +822,13 @@ static double small_time(long long M, int N, int n_ksteps, int* tokens, int* spl
     return best;
 }
 
-template <bool kBf16> static int launch_pair(const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, cudaStream_t s) {
+template <bool kBf16> static int launch_pair(const CUtensorMap& mw, const CUtensorMap& mx, const CUtensorMap& ms, const Args& a, cudaStream_t s) {
     auto kernel = linear_f8_pair_kernel<kBf16>;
     static bool raised[64];
     const int rc = raise_smem(kernel, kDynSmem2, raised);
     if (rc != DPPO_OK) return rc;
     const long long work = (long long)((a.N + a.tile_n - 1) / a.tile_n) * ((a.M_max + 2 * kTileM - 1) / (2 * kTileM)), most = sm_count() / 2;
-    return launch_after("linear_f8 launch", kernel, 2 * (work < most ? work : most), kThreads, kDynSmem2, s, 2, mw, mx, a);
+    return launch_after("linear_f8 launch", kernel, 2 * (work < most ? work : most), kThreads, kDynSmem2, s, 2, mw, mx, ms, a);
 }
 
 template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, const CUtensorMap& mx, const CUtensorMap& ms, const Args& a, int split, cudaStream_t s) {
@@ -831,7 +843,7 @@ template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, co
 }
 
 template <bool kBf16> static int launch(bool pair, int nb, int split, const CUtensorMap& mw, const CUtensorMap& mx, const CUtensorMap& ms, const Args& a, cudaStream_t s) {
-    if (pair) return launch_pair<kBf16>(mw, mx, a, s);
+    if (pair) return launch_pair<kBf16>(mw, mx, ms, a, s);
     switch (nb) {
         case 16: return launch_small<16, kBf16>(mw, mx, ms, a, split, s);
         case 32: return launch_small<32, kBf16>(mw, mx, ms, a, split, s);
@@ -904,7 +916,7 @@ extern "C" int dppo_linear_f8(const dppo_linear_f8_params* p, const uint8_t* x, 
     alignas(64) CUtensorMap mw, mx, ms;
     int rc = f8::make_map(&mw, w, p->N, p->K, p->w_stride, pair ? a.tile_n / 2 : f8::kTileM);
     if (rc == DPPO_OK) rc = f8::make_map(&mx, x, p->M_max, p->K, p->x_stride, pair ? f8::kTileM : nb);
-    if (rc == DPPO_OK && !pair) rc = f8::make_scale_map(&ms, x_scale, p->M_max, n_blocks, p->x_scale_stride, nb);
+    if (rc == DPPO_OK) rc = f8::make_scale_map(&ms, x_scale, p->M_max, n_blocks, p->x_scale_stride, pair ? f8::kTileM : nb);
     if (rc != DPPO_OK) return rc;
     cudaStream_t s = (cudaStream_t)stream;
     return a.out_bf16 ? f8::launch<true>(pair, nb, split, mw, mx, ms, a, s) : f8::launch<false>(pair, nb, split, mw, mx, ms, a, s);
