@@ -11,7 +11,7 @@
 //     thread of the epilogue then holds 128 channels of one token, which share one weight scale, so a block's factor is ONE number per
 //     thread.  That matters because shared memory is what the tensor cores read their operands from: with the channels on the
 //     lanes the factors came as 16 shared-memory loads per warp and block, and the products waited for the epilogue (2,048 x 2,560
-//     x 151,936: 1,260 us).  The outputs are transposed through shared memory, once per tile.
+//     x 151,936: 1,260 us).  A tile's outputs leave through shared memory by tiled copies that run under the next tile's products.
 //   few tokens (bound by reading the weights): a CTA per 128 channels, 16 to 128 tokens on the N side, so that few tokens waste
 //     nothing; the contraction is split over the CTAs of a cluster when there are too few tiles to keep all SMs reading, and the
 //     partial sums are joined in a fixed order through distributed shared memory.
@@ -41,8 +41,8 @@ constexpr int kSlots = 16;                // blocks whose token scales are in sh
 constexpr int kEpiWarps = 8;              // pair kernel: two per TMEM lane quarter, half of the tile's channels each
 constexpr int kThreads = 128 + 32 * kEpiWarps;     // producer, MMA and two idle warps before them
 constexpr int kTokenGroup = 8;            // token tiles swept together (2,048 tokens: 5 MB of codes at K = 2,560)
-constexpr int kRingBytes = 6 * (kBytesA + kTileN / 2 * kBK);
-constexpr int kStageOut = 2048;           // 64 bytes of outputs of 32 tokens: what an epilogue warp transposes at a time
+constexpr int kRingBytes = 4 * (kBytesA + kTileN / 2 * kBK);
+constexpr int kStageOut = 8192;           // an epilogue warp's outputs on their way: 256 bytes of each of its 32 tokens
 constexpr int kSlotBytes2 = kTileM * 4;   // pair kernel: of this CTA's tokens
 constexpr size_t kDynSmem2 = (size_t)kRingBytes + kEpiWarps * kStageOut + kSlots * kSlotBytes2 + 1024;
 
@@ -72,6 +72,7 @@ __device__ __forceinline__ void init_bar(unsigned long long* bar, int count) {
 
 // A warp's bounded wait: warp-uniform outcome, since what follows is executed by all 32 lanes together.
 __device__ __forceinline__ bool warp_wait(unsigned long long* bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns) {
+    if (__all_sync(0xffffffffu, lm_try(lm_smem_u32(bar), parity))) return true;
     return __all_sync(0xffffffffu, lm_wait(lm_smem_u32(bar), parity, abort_flag, limit_ns));
 }
 
@@ -109,8 +110,8 @@ __device__ __forceinline__ void columns_wait(uint32_t (&v)[32]) {
                    "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]),
                    "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31]) :: "memory");
 }
-// 64 bytes of outputs (16 f32 or 32 bf16 channels from ch on) of each of the warp's 32 tokens t0 + lane: through shared memory (`stage`,
-// this warp's), where piece p of a token's 64 bytes is at 64 lane + 16 (p ^ (lane / 2 mod 4)), without bank conflicts.
+// Tiles at the edges, and outputs whose rows are not on 16 bytes: 64 bytes (16 f32 or 32 bf16 channels from ch on) of each of the warp's
+// 32 tokens t0 + lane, through shared memory (`stage`, this warp's), where piece p of a token's 64 bytes is at 64 lane + 16 (p ^ (lane / 2 mod 4)), without bank conflicts.
 template <bool kBf16> __device__ __forceinline__ void store_piece(const Args& a, long long t0, long long T, int ch, int lane, const f32x2* acc, uint32_t stage) {
     typedef typename std::conditional<kBf16, __nv_bfloat16, float>::type Out;
     constexpr int kPer = 16 / (int)sizeof(Out);
@@ -157,6 +158,29 @@ template <bool kBf16> __device__ __forceinline__ void store_piece(const Args& a,
     }
 }
 
+// 256 bytes of outputs (64 f32 or 128 bf16 channels) of each of the warp's 32 tokens, in two boxes of 128 bytes laid out as a
+// 128B-swizzled tiled copy reads them.
+template <bool kBf16> __device__ __forceinline__ void stage_boxes(int lane, const f32x2* acc, uint32_t stage) {
+#pragma unroll
+    for (int p = 0; p < 16; ++p) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x0, x1;
+            if constexpr (kBf16) {
+                unpair(acc[4 * p + i], x0, x1);
+                const __nv_bfloat162 h = __floats2bfloat162_rn(x0, x1);
+                w[i] = *reinterpret_cast<const uint32_t*>(&h);
+            } else {
+                unpair(acc[2 * p + i / 2], x0, x1);
+                w[i] = __float_as_uint(i & 1 ? x1 : x0);
+            }
+        }
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                     :: "r"(stage + (uint32_t)((p >> 3) * 4096 + lane * 128 + (((p & 7) ^ (lane & 7)) * 16))), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    }
+}
+
 // ---- many tokens: CTA pairs ---------------------------------------------------------------------------
 struct Shared2 {
     unsigned long long full[kMaxStages];
@@ -185,7 +209,7 @@ __device__ __forceinline__ bool tile_of(uint32_t j, int n_ch, int n_tok, int& ch
 template <bool kBf16>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_s,
-                      const Args a) {
+                      const __grid_constant__ CUtensorMap map_out, const Args a) {
     extern __shared__ unsigned char f8_raw[];
     __shared__ Shared2 sh;
     const uint32_t tiles = (lm_smem_u32(f8_raw) + 1023u) & ~1023u, slots = tiles + (uint32_t)(kRingBytes + kEpiWarps * kStageOut);
@@ -262,7 +286,7 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 for (int k = 0; k < a.n_ksteps; ++k, ++it, s = s + 1 == stages ? 0 : s + 1, use += s == 0 ? 1 : 0) {
                     const uint32_t b = it & 1, use_b = it >> 1;
                     if (!lm_wait(lm_smem_u32(&sh.full[s]), use & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
-                    if (use_b > 0 && !lm_wait(lm_smem_u32(&sh.acc_empty[b]), (use_b - 1) & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
+                    if (use_b > 0 && !lm_wait_soon(lm_smem_u32(&sh.acc_empty[b]), (use_b - 1) & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t d_tmem = tmem_base + b * kTileN;
                     const uint64_t dx = lm_smem_desc_k(tiles + s * stage_bytes), dw = lm_smem_desc_k(tiles + s * stage_bytes + kBytesA);
@@ -308,6 +332,7 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             columns_load(v[0], lanes + (it & 1) * kTileN);
+            if (blocks > 1) columns_load(v[1], lanes + (it & 1) * kTileN + 32u);
 #pragma unroll 1
             for (int k = 0; k < a.n_ksteps; ++k, ++it) {
                 const uint32_t b = it & 1, taddr = lanes + b * kTileN;
@@ -316,40 +341,60 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 asm volatile("ld.shared.f32 %0, [%1];" : "=f"(sx) : "r"(slots + (it % kSlots) * kSlotBytes2 + (uint32_t)((q * 32 + lane) * 4)) : "memory");
                 const float f1 = sx * __shfl_sync(0xffffffffu, sw32, k & 31);
                 const f32x2 f = pair_of(f1, f1);
+                auto add = [&](int c, const uint32_t (&w)[32]) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    if (c < blocks) {                                    // a block's loads run under the one before it
-                        columns_wait(v[c & 1]);
-                        if (c + 1 < blocks) {
-                            columns_load(v[(c + 1) & 1], taddr + (uint32_t)((c + 1) * 32));
-                        } else {                                         // all read: the leader's MMA thread waits for every epilogue warp
-                            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                            __syncwarp();
-                            if (lane == 0)
-                                asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(lm_smem_u32(&sh.acc_empty[b]) & kPeerMask) : "memory");
-                            if (c == 3 && k + 1 < a.n_ksteps) {          // the next accumulator's first columns, under this one's last sums
-                                ok = warp_wait(&sh.acc_full[b ^ 1], ((it + 1) >> 1) & 1, abort_flag, a.wait_limit_ns);
-                                if (ok) {
-                                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                                    columns_load(v[0], lanes + (b ^ 1) * kTileN);
-                                }
-                            }
-                        }
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            acc[16 * c + i] = fma2(pair_of(__uint_as_float(v[c & 1][2 * i]), __uint_as_float(v[c & 1][2 * i + 1])), f, acc[16 * c + i]);
-                    }
+                    for (int i = 0; i < 16; ++i)
+                        acc[16 * c + i] = fma2(pair_of(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1])), f, acc[16 * c + i]);
+                };
+                // two blocks of columns under way at a time; the next accumulator's first two before this one's last sums are done
+                columns_wait(v[0]);
+                columns_wait(v[1]);
+                if (blocks == 4) {
+                    add(0, v[0]);
+                    columns_load(v[0], taddr + 64u);
+                    add(1, v[1]);
+                    columns_load(v[1], taddr + 96u);
+                    columns_wait(v[0]);
+                    columns_wait(v[1]);
                 }
-                if (!ok) break;
-                if (blocks < 4 && k + 1 < a.n_ksteps) {                  // narrow tiles: no registers to spare before
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0)                                           // all read: the leader's MMA thread waits for every epilogue warp
+                    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(lm_smem_u32(&sh.acc_empty[b]) & kPeerMask) : "memory");
+                const bool more = k + 1 < a.n_ksteps;
+                if (more) {
                     ok = warp_wait(&sh.acc_full[b ^ 1], ((it + 1) >> 1) & 1, abort_flag, a.wait_limit_ns);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    columns_load(v[0], lanes + (b ^ 1) * kTileN);
                 }
+                const uint32_t next = lanes + (b ^ 1) * kTileN;
+                if (blocks == 4) add(2, v[0]); else add(0, v[0]);
+                if (more) columns_load(v[0], next);
+                if (blocks == 4) add(3, v[1]); else if (blocks == 2) add(1, v[1]);
+                if (more && blocks > 1) columns_load(v[1], next + 32u);
             }
             if (!ok) break;
-            if (t0 < T) {
+            if (a.vec_out && blocks > 1 && t0 + 32 <= T) {
+                constexpr int kBox = kBf16 ? 64 : 32;                    // channels of a box
+#pragma unroll
+                for (int r = 0; r < (kBf16 ? 1 : 2); ++r) {
+                    if (2 * r * kBox >= a.tile_n / 2 || ch0 + 2 * r * kBox >= a.N) break;
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    __syncwarp();                                        // the boxes before these have been read
+                    stage_boxes<kBf16>(lane, acc + 32 * r, stage);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+#pragma unroll
+                        for (int g = 2 * r; g < 2 * r + 2; ++g)
+                            if (g * kBox < a.tile_n / 2 && ch0 + g * kBox < a.N)
+                                asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
+                                             :: "l"(&map_out), "r"(ch0 + g * kBox), "r"((int)t0), "r"(stage + (uint32_t)((g & 1) * 4096)) : "memory");
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
+                }
+            } else if (t0 < T) {
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     if (c >= blocks || ch0 + 32 * c >= a.N) break;
@@ -359,6 +404,8 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             }
             __syncwarp();
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");      // all outputs are written
+        __syncwarp();
     }
 
     // ---- common exit: both CTAs are done with tensor memory and with each other's barriers, then free
@@ -779,6 +826,21 @@ static int make_scale_map(CUtensorMap* map, const float* base, long long rows, i
     return DPPO_OK;
 }
 
+// The outputs, boxes of 128 bytes x 32 tokens, 128B swizzle (written: nothing outside them).
+static int make_out_map(CUtensorMap* map, void* base, long long rows, int N, long long ld, bool bf16) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return fail(DPPO_ERR_CUDA, "linear_f8: cuTensorMapEncodeTiled is not available from this driver");
+    const cuuint64_t dims[2] = {(cuuint64_t)N, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld * (bf16 ? 2 : 4)};
+    const cuuint32_t box[2] = {bf16 ? 64u : 32u, 32};
+    const cuuint32_t estr[2] = {1, 1};
+    const CUresult r = fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(DPPO_ERR_CUDA, "linear_f8: cuTensorMapEncodeTiled failed with %d", (int)r);
+    return DPPO_OK;
+}
+
 // Raises a kernel's shared-memory limit once per device.
 template <class Kernel> static int raise_smem(Kernel kernel, size_t bytes, bool (&done)[64]) {
     int dev = 0;
@@ -822,13 +884,13 @@ static double small_time(long long M, int N, int n_ksteps, int* tokens, int* spl
     return best;
 }
 
-template <bool kBf16> static int launch_pair(const CUtensorMap& mw, const CUtensorMap& mx, const CUtensorMap& ms, const Args& a, cudaStream_t s) {
+template <bool kBf16> static int launch_pair(const CUtensorMap& mw, const CUtensorMap& mx, const CUtensorMap& ms, const CUtensorMap& mo, const Args& a, cudaStream_t s) {
     auto kernel = linear_f8_pair_kernel<kBf16>;
     static bool raised[64];
     const int rc = raise_smem(kernel, kDynSmem2, raised);
     if (rc != DPPO_OK) return rc;
     const long long work = (long long)((a.N + a.tile_n - 1) / a.tile_n) * ((a.M_max + 2 * kTileM - 1) / (2 * kTileM)), most = sm_count() / 2;
-    return launch_after("linear_f8 launch", kernel, 2 * (work < most ? work : most), kThreads, kDynSmem2, s, 2, mw, mx, ms, a);
+    return launch_after("linear_f8 launch", kernel, 2 * (work < most ? work : most), kThreads, kDynSmem2, s, 2, mw, mx, ms, mo, a);
 }
 
 template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, const CUtensorMap& mx, const CUtensorMap& ms, const Args& a, int split, cudaStream_t s) {
@@ -842,8 +904,9 @@ template <int kNB, bool kBf16> static int launch_small(const CUtensorMap& mw, co
     return launch_after("linear_f8 launch", kernel, tiles * split, Small<kNB>::kThreads, Small<kNB>::kDynSmem, s, split, mw, mx, ms, a, n_ch, split);
 }
 
-template <bool kBf16> static int launch(bool pair, int nb, int split, const CUtensorMap& mw, const CUtensorMap& mx, const CUtensorMap& ms, const Args& a, cudaStream_t s) {
-    if (pair) return launch_pair<kBf16>(mw, mx, ms, a, s);
+template <bool kBf16> static int launch(bool pair, int nb, int split, const CUtensorMap& mw, const CUtensorMap& mx, const CUtensorMap& ms, const CUtensorMap& mo,
+                                        const Args& a, cudaStream_t s) {
+    if (pair) return launch_pair<kBf16>(mw, mx, ms, mo, a, s);
     switch (nb) {
         case 16: return launch_small<16, kBf16>(mw, mx, ms, a, split, s);
         case 32: return launch_small<32, kBf16>(mw, mx, ms, a, split, s);
@@ -912,12 +975,13 @@ extern "C" int dppo_linear_f8(const dppo_linear_f8_params* p, const uint8_t* x, 
     int nb = 0, split = 1;
     const double t_pair = f8::pair_time(p->M_max, p->N, n_blocks, &a.tile_n), t_small = f8::small_time(p->M_max, p->N, n_blocks, &nb, &split);
     const bool pair = variant == 1 || (variant == 0 && t_pair < t_small);
-    a.vec_out = ((uintptr_t)out & 15) == 0 && p->out_stride * (a.out_bf16 ? 2 : 4) % 16 == 0;
-    alignas(64) CUtensorMap mw, mx, ms;
+    a.vec_out = ((uintptr_t)out & 15) == 0 && p->out_stride * (a.out_bf16 ? 2 : 4) % 16 == 0 && p->out_stride < (1ll << 36);
+    alignas(64) CUtensorMap mw, mx, ms, mo = {};
     int rc = f8::make_map(&mw, w, p->N, p->K, p->w_stride, pair ? a.tile_n / 2 : f8::kTileM);
     if (rc == DPPO_OK) rc = f8::make_map(&mx, x, p->M_max, p->K, p->x_stride, pair ? f8::kTileM : nb);
     if (rc == DPPO_OK) rc = f8::make_scale_map(&ms, x_scale, p->M_max, n_blocks, p->x_scale_stride, pair ? f8::kTileM : nb);
+    if (rc == DPPO_OK && pair && a.vec_out) rc = f8::make_out_map(&mo, out, p->M_max, p->N, p->out_stride, a.out_bf16 != 0);
     if (rc != DPPO_OK) return rc;
     cudaStream_t s = (cudaStream_t)stream;
-    return a.out_bf16 ? f8::launch<true>(pair, nb, split, mw, mx, ms, a, s) : f8::launch<false>(pair, nb, split, mw, mx, ms, a, s);
+    return a.out_bf16 ? f8::launch<true>(pair, nb, split, mw, mx, ms, mo, a, s) : f8::launch<false>(pair, nb, split, mw, mx, ms, mo, a, s);
 }
