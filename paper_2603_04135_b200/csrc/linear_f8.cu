@@ -39,7 +39,7 @@ constexpr int kBytesA = kTileM * kBK;
 constexpr int kMaxStages = 9;             // + 2 accumulators + 1 < kSlots
 constexpr int kSlots = 16;                // blocks whose token scales are in shared memory
 constexpr int kEpiWarps = 8;              // pair kernel: two per TMEM lane quarter, half of the tile's channels each
-constexpr int kThreads = 128 + 32 * kEpiWarps;     // producer, MMA and two idle warps before them
+constexpr int kThreads = 128 + 32 * kEpiWarps;     // producer, MMA, watch and one idle warp before them
 constexpr int kTokenGroup = 8;            // token tiles swept together (2,048 tokens: 5 MB of codes at K = 2,560)
 constexpr int kRingBytes = 4 * (kBytesA + kTileN / 2 * kBK);
 constexpr int kStageOut = 8192;           // an epilogue warp's outputs on their way: 256 bytes of each of its 32 tokens
@@ -308,6 +308,22 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 lm_wait_plain(lm_smem_u32(&sh.drain), 0, a.wait_limit_ns);
             }
         }
+    } else if (warp == 2) {
+        // ------------------------------------------------------------------ watch (both CTAs): hands finished accumulators on to the epilogue
+        // The epilogue's warps wait at a hardware barrier, which costs a tenth of a look at an mbarrier while the tensor cores keep
+        // shared memory busy (250 cycles, of 650 that a block's products take).  This warp meets them there at every accumulator, so
+        // neither side is ever more than one ahead.  After a time-out it no longer looks before it goes there: the epilogue runs to
+        // its end, over whatever is there.
+        uint32_t it = 0;
+        int ch, tok;
+        for (uint32_t j = 0; tile_of(j, n_ch, n_tok, ch, tok); ++j) {
+            for (int k = 0; k < a.n_ksteps; ++k, ++it) {
+                if (!*abort_flag) lm_wait(lm_smem_u32(&sh.acc_full[it & 1]), (it >> 1) & 1, abort_flag, a.wait_limit_ns);
+                __syncwarp();
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                asm volatile("bar.sync 1, %0;" :: "n"(32 + 32 * kEpiWarps) : "memory");
+            }
+        }
     } else if (warp >= 4) {
         // ------------------------------------------------------------------ epilogue (warps 4..11, both CTAs)
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
@@ -316,29 +332,32 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         const uint32_t stage = tiles + (uint32_t)kRingBytes + (uint32_t)((warp - 4) * kStageOut);
         uint32_t it = 0;
         int ch, tok;
-        bool ok = true;
-        for (uint32_t j = 0; ok && tile_of(j, n_ch, n_tok, ch, tok); ++j) {
+        auto handed_on = [&]() {
+            asm volatile("bar.sync 1, %0;" :: "n"(32 + 32 * kEpiWarps) : "memory");
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        };
+        for (uint32_t j = 0; tile_of(j, n_ch, n_tok, ch, tok); ++j) {
             const long long t0 = (2ll * tok + (int)rank) * kTileM + q * 32;
             const int ch0 = ch * a.tile_n + first;
             // the channels' scales of 32 blocks, one per lane; 0 past the last channel
             const float* ws = a.w_scale + (ch0 < a.N ? (long long)(ch0 / kBK) * a.ws_stride : 0);
-            float sw32 = 0.0f;
+            float sw32 = ch0 < a.N && lane < a.n_ksteps ? ws[lane] : 0.0f;
             f32x2 acc[64];
 #pragma unroll
             for (int i = 0; i < 64; ++i) acc[i] = 0ull;
             const uint32_t lanes = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)first;
+            const uint32_t my_slot = slots + (uint32_t)((q * 32 + lane) * 4);
+            float sx;                                                    // the token's scale, asked for a block ahead
+            auto ask_scale = [&](uint32_t n) { asm volatile("ld.shared.f32 %0, [%1];" : "=f"(sx) : "r"(my_slot + (n % kSlots) * kSlotBytes2) : "memory"); };
             uint32_t v[2][32];
-            ok = warp_wait(&sh.acc_full[it & 1], (it >> 1) & 1, abort_flag, a.wait_limit_ns);
-            if (!ok) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            handed_on();
             columns_load(v[0], lanes + (it & 1) * kTileN);
             if (blocks > 1) columns_load(v[1], lanes + (it & 1) * kTileN + 32u);
+            ask_scale(it);
 #pragma unroll 1
             for (int k = 0; k < a.n_ksteps; ++k, ++it) {
                 const uint32_t b = it & 1, taddr = lanes + b * kTileN;
-                if ((k & 31) == 0) sw32 = ch0 < a.N && k + lane < a.n_ksteps ? ws[k + lane] : 0.0f;
-                float sx;
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(sx) : "r"(slots + (it % kSlots) * kSlotBytes2 + (uint32_t)((q * 32 + lane) * 4)) : "memory");
+                if ((k & 31) == 0 && k > 0) sw32 = ch0 < a.N && k + lane < a.n_ksteps ? ws[k + lane] : 0.0f;
                 const float f1 = sx * __shfl_sync(0xffffffffu, sw32, k & 31);
                 const f32x2 f = pair_of(f1, f1);
                 auto add = [&](int c, const uint32_t (&w)[32]) {
@@ -358,14 +377,13 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                     columns_wait(v[1]);
                 }
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
                 if (lane == 0)                                           // all read: the leader's MMA thread waits for every epilogue warp
                     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(lm_smem_u32(&sh.acc_empty[b]) & kPeerMask) : "memory");
+                __syncwarp();
                 const bool more = k + 1 < a.n_ksteps;
                 if (more) {
-                    ok = warp_wait(&sh.acc_full[b ^ 1], ((it + 1) >> 1) & 1, abort_flag, a.wait_limit_ns);
-                    if (!ok) break;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    handed_on();
+                    ask_scale(it + 1);
                 }
                 const uint32_t next = lanes + (b ^ 1) * kTileN;
                 if (blocks == 4) add(2, v[0]); else add(0, v[0]);
@@ -373,7 +391,6 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 if (blocks == 4) add(3, v[1]); else if (blocks == 2) add(1, v[1]);
                 if (more && blocks > 1) columns_load(v[1], next + 32u);
             }
-            if (!ok) break;
             if (a.vec_out && blocks > 1 && t0 + 32 <= T) {
                 constexpr int kBox = kBf16 ? 64 : 32;                    // channels of a box
 #pragma unroll

@@ -139,6 +139,16 @@ def test_many_tiles(B, variant):
     check_product(y, M, K, N, q, qs, p, ps)
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", [(512, 700, 1024), (300, 5000, 1000), (257, 256, 4056)])
+def test_aligned_outputs(B, out, M, K, N):
+    """Rows of the output on 16 bytes: whole tiles leave by tiled copies."""
+    q, qs, p, ps = make(B, M, K, N, 9)
+    for pitch in (0, 8):
+        y, _ = product(B, M, K, N, q, qs, p, ps, out, 1, pitch=pitch)
+        check_product(y, M, K, N, q, qs, p, ps)
+
+
 @pytest.mark.parametrize("variant", [1, 2])
 @pytest.mark.parametrize("rows", [0, 1, 100, 299])
 def test_true_count_on_the_device(B, rows, variant):
