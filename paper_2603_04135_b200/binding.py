@@ -4,8 +4,9 @@ Array arguments are torch tensors (their device pointer is passed), raw integer 
 for the nullable ones.  Every function raises DppoError on a non-zero return code.  There is no
 fallback: if the library has not been built, importing this module raises.
 
-The scoring calls (token_logprobs, token_logprobs_backward, quantize_rows_i8, linear_i8) also check the tensors they
-are given: element type, on the current device, and large enough for the sizes in the params.  Their plain case (torch
+The scoring calls (token_logprobs, token_logprobs_backward, quantize_rows_i8, linear_i8), the distillation and verification
+calls (distill_topk, distill_topk_backward, verify_drafts) and the block-scaled product (quantize_f8, linear_f8) also check the
+tensors they are given: element type, on the current device, and large enough for the sizes in the params.  Their plain case (torch
 tensors in the exact layout, the current stream) is checked and marshalled in native code (_marshal.so); anything else, and a
 tree where that module has not been built, takes the same checks here.
 """
@@ -368,6 +369,7 @@ def sequence_log_ratio(logp, logp_old, cu_seqlens, S_max, out, status=None, stre
 class _NoNative:
     """Stands in for the native marshalling: nothing is the plain case."""
     token_logprobs = token_logprobs_backward = quantize_rows_i8 = linear_i8 = staticmethod(lambda *a: None)
+    distill_topk = distill_topk_backward = verify_drafts = quantize_f8 = linear_f8 = token_logprobs
 
 
 def _load_native():
@@ -378,9 +380,10 @@ def _load_native():
         return _NoNative
     if getattr(_marshal, "built_for", None) != build.built_for():
         return _NoNative
-    _marshal.bind(LogprobParams, QuantizeParams, LinearI8Params,
-                  *(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.dppo_token_logprobs, lib.dppo_token_logprobs_backward,
-                                                                    lib.dppo_quantize_rows_i8, lib.dppo_linear_i8)))
+    _marshal.bind((LogprobParams, QuantizeParams, LinearI8Params, DistillParams, VerifyParams, QuantizeF8Params, LinearF8Params),
+                  tuple(ctypes.cast(f, ctypes.c_void_p).value for f in (
+                      lib.dppo_token_logprobs, lib.dppo_token_logprobs_backward, lib.dppo_quantize_rows_i8, lib.dppo_linear_i8,
+                      lib.dppo_distill_topk, lib.dppo_distill_topk_backward, lib.dppo_verify_drafts, lib.dppo_quantize_f8, lib.dppo_linear_f8)))
     return _marshal
 
 
@@ -453,6 +456,9 @@ def linear_i8(params, x, x_scale, w, w_scale, out, n_rows_dev=None, status=None,
 
 
 def distill_topk(params, logits, top_ids, top_logp, n_tokens_dev, weight, loss_out, lse_out, stats, dlogits, status=None, stream=None):
+    rc = _native.distill_topk(params, logits, top_ids, top_logp, n_tokens_dev, weight, loss_out, lse_out, stats, dlogits, status, stream)
+    if rc == 0 or _done(rc):
+        return
     p, d = params, _device()
     T, V, dt, ld, k = p.T_max, p.V, _TORCH_DTYPE.get(p.dtype), p.row_stride, p.T_max * p.top_k
     _check(lib.dppo_distill_topk(
@@ -463,6 +469,9 @@ def distill_topk(params, logits, top_ids, top_logp, n_tokens_dev, weight, loss_o
 
 
 def distill_topk_backward(params, logits, top_ids, top_logp, n_tokens_dev, stats, dloss, dlogits, status=None, stream=None):
+    rc = _native.distill_topk_backward(params, logits, top_ids, top_logp, n_tokens_dev, stats, dloss, dlogits, status, stream)
+    if rc == 0 or _done(rc):
+        return
     p, d = params, _device()
     T, V, dt, ld, k = p.T_max, p.V, _TORCH_DTYPE.get(p.dtype), p.row_stride, p.T_max * p.top_k
     _check(lib.dppo_distill_topk_backward(
@@ -477,6 +486,10 @@ def verify_drafts_workspace_bytes(params):
 
 def verify_drafts(params, target_logits, draft_logits, drafts, cu_drafts, uniforms, noise, n_accepted, tokens_out, logp_out, workspace,
                   workspace_bytes, status=None, stream=None):
+    rc = _native.verify_drafts(params, target_logits, draft_logits, drafts, cu_drafts, uniforms, noise, n_accepted, tokens_out, logp_out,
+                               workspace, workspace_bytes, status, stream)
+    if rc == 0 or _done(rc):
+        return
     p, d = params, _device()
     T, B, V, dt = p.T_max, p.n_seqs, p.V, _TORCH_DTYPE.get(p.dtype)
     _check(lib.dppo_verify_drafts(
@@ -489,6 +502,9 @@ def verify_drafts(params, target_logits, draft_logits, drafts, cu_drafts, unifor
 
 
 def quantize_f8(params, x, q, scale, n_rows_dev=None, status=None, stream=None):
+    rc = _native.quantize_f8(params, x, q, scale, n_rows_dev, status, stream)
+    if rc == 0 or _done(rc):
+        return
     p, d = params, _device()
     M, K, blocks = p.rows_max, p.K, (p.K + 127) // 128
     rows, cols = (blocks, M) if p.block_rows == 1 else ((M + 127) // 128, blocks)
@@ -499,6 +515,9 @@ def quantize_f8(params, x, q, scale, n_rows_dev=None, status=None, stream=None):
 
 
 def linear_f8(params, x, x_scale, w, w_scale, out, n_rows_dev=None, status=None, stream=None):
+    rc = _native.linear_f8(params, x, x_scale, w, w_scale, out, n_rows_dev, status, stream)
+    if rc == 0 or _done(rc):
+        return
     p, d = params, _device()
     M, N, K, blocks = p.M_max, p.N, p.K, (p.K + 127) // 128
     _check(lib.dppo_linear_f8(

@@ -286,7 +286,7 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 for (int k = 0; k < a.n_ksteps; ++k, ++it, s = s + 1 == stages ? 0 : s + 1, use += s == 0 ? 1 : 0) {
                     const uint32_t b = it & 1, use_b = it >> 1;
                     if (!lm_wait(lm_smem_u32(&sh.full[s]), use & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
-                    if (use_b > 0 && !lm_wait_soon(lm_smem_u32(&sh.acc_empty[b]), (use_b - 1) & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
+                    if (use_b > 0 && !lm_wait(lm_smem_u32(&sh.acc_empty[b]), (use_b - 1) & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t d_tmem = tmem_base + b * kTileN;
                     const uint64_t dx = lm_smem_desc_k(tiles + s * stage_bytes), dw = lm_smem_desc_k(tiles + s * stage_bytes + kBytesA);

@@ -1,5 +1,5 @@
-// Argument marshalling of the scoring calls for the Python binding: the plain case (torch tensors, laid out as the call
-// reads them) in native code.  What a call of a few microseconds on the device costs on the host is mostly the look at nine
+// Argument marshalling of the scoring, distillation and verification calls and the 8-bit products for the Python binding: the plain case
+// (torch tensors, laid out as the call reads them) in native code.  What a call of a few microseconds on the device costs on the host is mostly the look at nine
 // tensors through Python (3.5 us of 7); here it is a tenth of that.
 //
 // Each function takes the params object and the call's arguments in the order of binding.py, checks every tensor (exact
@@ -17,11 +17,19 @@
 
 namespace {
 
-PyTypeObject *g_logprob_type, *g_quantize_type, *g_linear_type;
+// The params classes and the library's entry points, in the order of bind()'s arguments.
+enum { kLogprob, kQuantize, kLinear, kDistill, kVerify, kQuantizeF8, kLinearF8, kTypes };
+PyTypeObject* g_type[kTypes];
 decltype(&dppo_token_logprobs) g_logprobs;
 decltype(&dppo_token_logprobs_backward) g_backward;
 decltype(&dppo_quantize_rows_i8) g_quantize;
 decltype(&dppo_linear_i8) g_linear;
+decltype(&dppo_distill_topk) g_distill;
+decltype(&dppo_distill_topk_backward) g_distill_backward;
+decltype(&dppo_verify_drafts) g_verify;
+decltype(&dppo_quantize_f8) g_quantize_f8;
+decltype(&dppo_linear_f8) g_linear_f8;
+constexpr int kFunctions = 9;
 
 struct NotPlain {};
 
@@ -84,7 +92,7 @@ template <class F> PyObject* guarded(PyObject* const* args, Py_ssize_t n, Py_ssi
 
 PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(a, n, 12, [&](int d, void* stream) {
-        const auto p = params_of<dppo_logprob_params>(a[0], g_logprob_type);
+        const auto p = params_of<dppo_logprob_params>(a[0], g_type[kLogprob]);
         const int64_t T = p.T_max, k = T * p.top_k;
         const void* logits = matrix(a[1], element(p.dtype), d, T, p.row_stride);
         const auto* target = dense<int32_t>(a[2], at::kInt, d, T);
@@ -99,7 +107,7 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 PyObject* token_logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(a, n, 10, [&](int d, void* stream) {
-        const auto p = params_of<dppo_logprob_params>(a[0], g_logprob_type);
+        const auto p = params_of<dppo_logprob_params>(a[0], g_type[kLogprob]);
         const int64_t T = p.T_max;
         const void* logits = matrix(a[1], element(p.dtype), d, T, p.row_stride);
         const auto* target = dense<int32_t>(a[2], at::kInt, d, T);
@@ -114,7 +122,7 @@ PyObject* token_logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 PyObject* quantize_rows_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(a, n, 7, [&](int d, void* stream) {
-        const auto p = params_of<dppo_quantize_params>(a[0], g_quantize_type);
+        const auto p = params_of<dppo_quantize_params>(a[0], g_type[kQuantize]);
         const void* x = matrix(a[1], element(p.dtype), d, p.rows_max, p.x_stride);
         auto* q = static_cast<int8_t*>(matrix(a[2], at::kChar, d, p.rows_max, p.q_stride));
         auto* scale = dense<float>(a[3], at::kFloat, d, p.rows_max);
@@ -126,7 +134,7 @@ PyObject* quantize_rows_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 PyObject* linear_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(a, n, 9, [&](int d, void* stream) {
-        const auto p = params_of<dppo_linear_i8_params>(a[0], g_linear_type);
+        const auto p = params_of<dppo_linear_i8_params>(a[0], g_type[kLinear]);
         const auto* x = static_cast<const int8_t*>(matrix(a[1], at::kChar, d, p.M_max, p.x_stride));
         const auto* xs = dense<float>(a[2], at::kFloat, d, p.M_max);
         const auto* w = static_cast<const int8_t*>(matrix(a[3], at::kChar, d, p.N, p.w_stride));
@@ -138,17 +146,109 @@ PyObject* linear_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// bind(LogprobParams, QuantizeParams, LinearI8Params, addresses of the four entry points in the order above)
+PyObject* distill_topk(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, 12, [&](int d, void* stream) {
+        const auto p = params_of<dppo_distill_params>(a[0], g_type[kDistill]);
+        const int64_t T = p.T_max, k = T * p.top_k;
+        const void* logits = matrix(a[1], element(p.dtype), d, T, p.row_stride);
+        const auto* ids = dense<int32_t>(a[2], at::kInt, d, k);
+        const auto *top_logp = dense<float>(a[3], at::kFloat, d, k), *weight = dense<float>(a[5], at::kFloat, d, T);
+        const auto* n_dev = dense<int32_t>(a[4], at::kInt, d, 1);
+        auto *loss = dense<float>(a[6], at::kFloat, d, T), *lse = dense<float>(a[7], at::kFloat, d, T), *stats = dense<float>(a[8], at::kFloat, d, 4 * T);
+        void* dlogits = matrix(a[9], element(p.dtype), d, T, p.row_stride);
+        auto* status = dense<int32_t>(a[10], at::kInt, d, 1);
+        return [=] { return g_distill(&p, logits, ids, top_logp, n_dev, weight, loss, lse, stats, dlogits, status, stream); };
+    });
+}
+
+PyObject* distill_topk_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, 10, [&](int d, void* stream) {
+        const auto p = params_of<dppo_distill_params>(a[0], g_type[kDistill]);
+        const int64_t T = p.T_max, k = T * p.top_k;
+        const void* logits = matrix(a[1], element(p.dtype), d, T, p.row_stride);
+        const auto* ids = dense<int32_t>(a[2], at::kInt, d, k);
+        const auto* top_logp = dense<float>(a[3], at::kFloat, d, k);
+        const auto* n_dev = dense<int32_t>(a[4], at::kInt, d, 1);
+        const auto *stats = dense<float>(a[5], at::kFloat, d, 4 * T), *dloss = dense<float>(a[6], at::kFloat, d, T);
+        void* dlogits = matrix(a[7], element(p.dtype), d, T, p.row_stride);
+        auto* status = dense<int32_t>(a[8], at::kInt, d, 1);
+        return [=] { return g_distill_backward(&p, logits, ids, top_logp, n_dev, stats, dloss, dlogits, status, stream); };
+    });
+}
+
+PyObject* verify_drafts(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, 14, [&](int d, void* stream) {
+        const auto p = params_of<dppo_verify_params>(a[0], g_type[kVerify]);
+        const int64_t T = p.T_max, B = p.n_seqs;
+        const void* target = matrix(a[1], element(p.dtype), d, T + B, p.target_stride);
+        const void* draft = matrix(a[2], element(p.dtype), d, T, p.draft_stride);
+        const auto *drafts = dense<int32_t>(a[3], at::kInt, d, T), *cu = dense<int32_t>(a[4], at::kInt, d, B + 1);
+        const auto* u = dense<float>(a[5], at::kFloat, d, T);
+        const auto* noise = static_cast<const float*>(matrix(a[6], at::kFloat, d, B, p.noise_stride));
+        auto *n_acc = dense<int32_t>(a[7], at::kInt, d, B), *tokens = dense<int32_t>(a[8], at::kInt, d, T + B);
+        auto* logp = dense<float>(a[9], at::kFloat, d, T + B);
+        const int64_t bytes = PyLong_AsLongLong(a[11]);
+        if (bytes < 0) { PyErr_Clear(); throw NotPlain(); }
+        auto* ws = dense<uint8_t>(a[10], at::kByte, d, bytes);
+        auto* status = dense<int32_t>(a[12], at::kInt, d, 1);
+        return [=] { return g_verify(&p, target, draft, drafts, cu, u, noise, n_acc, tokens, logp, ws, (size_t)bytes, status, stream); };
+    });
+}
+
+PyObject* quantize_f8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, 7, [&](int d, void* stream) {
+        const auto p = params_of<dppo_quantize_f8_params>(a[0], g_type[kQuantizeF8]);
+        const int64_t blocks = (p.K + 127ll) / 128;
+        const void* x = matrix(a[1], element(p.dtype), d, p.rows_max, p.x_stride);
+        auto* q = static_cast<uint8_t*>(matrix(a[2], at::kFloat8_e4m3fn, d, p.rows_max, p.q_stride));
+        auto* scale = static_cast<float*>(matrix(a[3], at::kFloat, d, p.block_rows == 1 ? blocks : (p.rows_max + 127) / 128, p.scale_stride));
+        const auto* n_dev = dense<int32_t>(a[4], at::kInt, d, 1);
+        auto* status = dense<int32_t>(a[5], at::kInt, d, 1);
+        return [=] { return g_quantize_f8(&p, x, q, scale, n_dev, status, stream); };
+    });
+}
+
+PyObject* linear_f8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, 9, [&](int d, void* stream) {
+        const auto p = params_of<dppo_linear_f8_params>(a[0], g_type[kLinearF8]);
+        const auto* x = static_cast<const uint8_t*>(matrix(a[1], at::kFloat8_e4m3fn, d, p.M_max, p.x_stride));
+        const auto* xs = static_cast<const float*>(matrix(a[2], at::kFloat, d, (p.K + 127ll) / 128, p.x_scale_stride));
+        const auto* w = static_cast<const uint8_t*>(matrix(a[3], at::kFloat8_e4m3fn, d, p.N, p.w_stride));
+        const auto* ws = static_cast<const float*>(matrix(a[4], at::kFloat, d, (p.N + 127ll) / 128, p.w_scale_stride));
+        void* out = matrix(a[5], element(p.out_dtype), d, p.M_max, p.out_stride);
+        const auto* n_dev = dense<int32_t>(a[6], at::kInt, d, 1);
+        auto* status = dense<int32_t>(a[7], at::kInt, d, 1);
+        return [=] { return g_linear_f8(&p, x, xs, w, ws, out, n_dev, status, stream); };
+    });
+}
+
+// bind(params classes, addresses of the entry points), each a tuple in the order above
 PyObject* bind(PyObject*, PyObject* args) {
-    unsigned long long f[4];
-    PyObject *a, *b, *c;
-    if (!PyArg_ParseTuple(args, "O!O!O!KKKK", &PyType_Type, &a, &PyType_Type, &b, &PyType_Type, &c, &f[0], &f[1], &f[2], &f[3])) return nullptr;
-    Py_INCREF(a); Py_INCREF(b); Py_INCREF(c);
-    g_logprob_type = (PyTypeObject*)a; g_quantize_type = (PyTypeObject*)b; g_linear_type = (PyTypeObject*)c;
+    PyObject *types, *functions;
+    if (!PyArg_ParseTuple(args, "O!O!", &PyTuple_Type, &types, &PyTuple_Type, &functions)) return nullptr;
+    if (PyTuple_GET_SIZE(types) != kTypes || PyTuple_GET_SIZE(functions) != kFunctions) {
+        PyErr_SetString(PyExc_ValueError, "bind: another number of classes or functions");
+        return nullptr;
+    }
+    unsigned long long f[kFunctions];
+    for (int i = 0; i < kFunctions; ++i) {
+        f[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(functions, i));
+        if (PyErr_Occurred()) return nullptr;
+    }
+    for (int i = 0; i < kTypes; ++i) {
+        PyObject* t = PyTuple_GET_ITEM(types, i);
+        Py_INCREF(t);
+        g_type[i] = (PyTypeObject*)t;
+    }
     g_logprobs = reinterpret_cast<decltype(g_logprobs)>(f[0]);
     g_backward = reinterpret_cast<decltype(g_backward)>(f[1]);
     g_quantize = reinterpret_cast<decltype(g_quantize)>(f[2]);
     g_linear = reinterpret_cast<decltype(g_linear)>(f[3]);
+    g_distill = reinterpret_cast<decltype(g_distill)>(f[4]);
+    g_distill_backward = reinterpret_cast<decltype(g_distill_backward)>(f[5]);
+    g_verify = reinterpret_cast<decltype(g_verify)>(f[6]);
+    g_quantize_f8 = reinterpret_cast<decltype(g_quantize_f8)>(f[7]);
+    g_linear_f8 = reinterpret_cast<decltype(g_linear_f8)>(f[8]);
     Py_RETURN_NONE;
 }
 
@@ -158,6 +258,11 @@ PyMethodDef kMethods[] = {
     {"token_logprobs_backward", (PyCFunction)(void (*)(void))token_logprobs_backward, METH_FASTCALL, nullptr},
     {"quantize_rows_i8", (PyCFunction)(void (*)(void))quantize_rows_i8, METH_FASTCALL, nullptr},
     {"linear_i8", (PyCFunction)(void (*)(void))linear_i8, METH_FASTCALL, nullptr},
+    {"distill_topk", (PyCFunction)(void (*)(void))distill_topk, METH_FASTCALL, nullptr},
+    {"distill_topk_backward", (PyCFunction)(void (*)(void))distill_topk_backward, METH_FASTCALL, nullptr},
+    {"verify_drafts", (PyCFunction)(void (*)(void))verify_drafts, METH_FASTCALL, nullptr},
+    {"quantize_f8", (PyCFunction)(void (*)(void))quantize_f8, METH_FASTCALL, nullptr},
+    {"linear_f8", (PyCFunction)(void (*)(void))linear_f8, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

@@ -38,15 +38,6 @@ __device__ __forceinline__ bool lm_wait(uint32_t bar, uint32_t parity, volatile 
     }
 }
 
-// The same where the waiting thread is what others wait for next: a look at the clock takes about as long as a stage of such a
-// pipeline, so it comes after tries that mostly succeed.
-__device__ __forceinline__ bool lm_wait_soon(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns) {
-#pragma unroll 1
-    for (int i = 0; i < 64; ++i)
-        if (lm_try(bar, parity)) return true;
-    return lm_wait(bar, parity, abort_flag, limit_ns);
-}
-
 // Bounded wait that ignores the abort flag (used on the way out).
 __device__ __forceinline__ bool lm_wait_plain(uint32_t bar, uint32_t parity, unsigned long long limit_ns) {
     if (lm_try(bar, parity)) return true;

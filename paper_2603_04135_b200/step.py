@@ -22,6 +22,19 @@ def quantize_rows_i8(x, status=None):
     return q[:, :K], scale
 
 
+def quantize_f8(x, block_rows=128, status=None):
+    """8-bit floating-point codes (e4m3) and block scales of x (bf16 or f32 [M, K] with rows on 16 bytes): (q float8_e4m3fn [M, K], a
+    view of padded rows, scale f32).  block_rows 128: weights, a scale per 128 x 128, [ceil(M / 128), ceil(K / 128)]; quantised
+    once this way and kept, see DppoStep.score_hidden_f8.  1: tokens, a scale per row and 128 columns, [ceil(K / 128), M] (a view)."""
+    M, K = x.shape
+    ld, kb = (K + 127) // 128 * 128, (K + 127) // 128
+    q = torch.zeros(M, ld, dtype=torch.float8_e4m3fn, device=x.device)
+    scale = torch.zeros(kb, (M + 3) // 4 * 4, device=x.device) if block_rows == 1 else torch.zeros((M + 127) // 128, kb, device=x.device)
+    B.quantize_f8(B.QuantizeF8Params(M, K, B.BF16 if x.dtype is torch.bfloat16 else B.F32, x.stride(0) if M > 1 else max(x.stride(0), K), ld,
+                                     scale.stride(0) if scale.numel() else max(kb, 1), block_rows), x, q, scale, status=status)
+    return q[:, :K], scale[:, :M] if block_rows == 1 else scale
+
+
 class DppoStep:
     """Buffers for a batch of P prompts x G completions and a loss sweep over at most T_max tokens.
 
@@ -152,16 +165,21 @@ class DppoStep:
                          self.counts[3:4] if n_tokens_dev is None else n_tokens_dev, top_k, out, 0, self.T_max)
         return out
 
+    @staticmethod
+    def _zeros_like_rows(logits):
+        """A gradient's tensor: the logits' shape and, where rows are padded, their pitch."""
+        if logits.is_contiguous():
+            return torch.zeros_like(logits)
+        extent = 1 + sum((n - 1) * s for n, s in zip(logits.shape, logits.stride())) if logits.numel() else 0
+        return logits.new_zeros(extent).as_strided(logits.shape, logits.stride())
+
     def score_backward(self, logits, target, scored, dlogp=None, dentropy=None, dlogits=None, row_stride=None,
                        n_tokens_dev=None):
         """Gradient with respect to `logits` of a loss with the per-token derivatives dlogp and dentropy (f32 [T_max], either
         may be None); `scored` is what score() returned.  Returns dlogits (`logits` itself for in place; a new tensor of the
         logits' shape and strides if None)."""
-        if dlogits is None and logits.is_contiguous():
-            dlogits = torch.zeros_like(logits)
-        elif dlogits is None:                    # rows that are padded: the same pitch
-            extent = 1 + sum((n - 1) * s for n, s in zip(logits.shape, logits.stride())) if logits.numel() else 0
-            dlogits = logits.new_zeros(extent).as_strided(logits.shape, logits.stride())
+        if dlogits is None:
+            dlogits = self._zeros_like_rows(logits)
         stride = self.V if row_stride is None else row_stride
         prm = B.LogprobParams(self.T_max, self.V, self.loss_params.dtype, stride, 0, 0, self.loss_params.temperature)
         B.token_logprobs_backward(prm, logits, target, self.counts[3:4] if n_tokens_dev is None else n_tokens_dev,
@@ -189,11 +207,7 @@ class DppoStep:
         logits = torch.empty(C, ldv, dtype=torch.float32, device=self.device)
         q = torch.empty(C, ldq, dtype=torch.int8, device=self.device)
         q_scale = torch.empty(C, dtype=torch.float32, device=self.device)
-        T_dev = self.counts[3:4] if n_tokens_dev is None else n_tokens_dev
-        if T <= C and T_dev.dtype is torch.int32 and T_dev.dim() == 1:
-            left = T_dev                         # one chunk: the kernels bound the count by the rows themselves
-        else:
-            left = torch.clamp(T_dev - torch.arange(0, T, C, dtype=torch.int32, device=self.device), 0, C).to(torch.int32)
+        left = self._left(T, C, n_tokens_dev)
         dtype = B.BF16 if hidden.dtype is torch.bfloat16 else B.F32
         for i, lo in enumerate(range(0, T, C)):
             hi, n = min(lo + C, T), left[i:i + 1]
@@ -201,6 +215,107 @@ class DppoStep:
             B.linear_i8(B.LinearI8Params(hi - lo, V, H, ldq, W_q.stride(0), ldv, B.F32), q, q_scale, W_q, W_scale, logits, n,
                         self.status)
             self._score_call(logits, B.F32, V, ldv, None if target is None else target[lo:hi], n, top_k, out, lo, hi)
+        return out
+
+    def _left(self, T, C, n_tokens_dev):
+        """True tokens in each chunk of C of T rows, on the device."""
+        T_dev = self.counts[3:4] if n_tokens_dev is None else n_tokens_dev
+        if T <= C and T_dev.dtype is torch.int32 and T_dev.dim() == 1:
+            return T_dev                         # one chunk: the kernels bound the count by the rows themselves
+        return torch.clamp(T_dev - torch.arange(0, T, C, dtype=torch.int32, device=self.device), 0, C).to(torch.int32)
+
+    def score_hidden_f8(self, hidden, W_q, W_scale, target=None, top_k=0, n_tokens_dev=None, chunk_tokens=2048, out=None):
+        """score_hidden_i8 with the LM-head in 8-bit floating point and a scale per 128 x 128 (quantize_f8 of its [V, H] weight): hidden
+        states with a few channels far larger than the others keep their digits.  Chunks and scratch as there."""
+        T, H = hidden.shape
+        if T != self.T_max:
+            raise ValueError("hidden has %d rows, T_max is %d" % (T, self.T_max))
+        V, kb = W_q.shape[0], (H + 127) // 128
+        if W_q.shape[1] != H or W_scale.shape != ((V + 127) // 128, kb):
+            raise ValueError("W_q has shape %s, W_scale %s; hidden states %d wide need (V, %d) and (ceil(V / 128), %d)"
+                             % (tuple(W_q.shape), tuple(W_scale.shape), H, H, kb))
+        out = self._score_buffers(T, top_k, out)
+        if T == 0:
+            return out
+        C = min(chunk_tokens, T)
+        ldq, ldv, lds = kb * 128, (V + 3) // 4 * 4, (C + 3) // 4 * 4
+        logits = torch.empty(C, ldv, dtype=torch.float32, device=self.device)          # of this call alone, as there
+        q = torch.empty(C, ldq, dtype=torch.float8_e4m3fn, device=self.device)
+        q_scale = torch.empty(kb, lds, dtype=torch.float32, device=self.device)
+        left = self._left(T, C, n_tokens_dev)
+        dtype = B.BF16 if hidden.dtype is torch.bfloat16 else B.F32
+        for i, lo in enumerate(range(0, T, C)):
+            hi, n = min(lo + C, T), left[i:i + 1]
+            B.quantize_f8(B.QuantizeF8Params(hi - lo, H, dtype, hidden.stride(0), ldq, lds, 1), hidden[lo:hi], q, q_scale, n, self.status)
+            B.linear_f8(B.LinearF8Params(hi - lo, V, H, ldq, W_q.stride(0), ldv, lds, W_scale.stride(0), B.F32), q, q_scale, W_q, W_scale,
+                        logits, n, self.status)
+            self._score_call(logits, B.F32, V, ldv, None if target is None else target[lo:hi], n, top_k, out, lo, hi)
+        return out
+
+    # -- distillation: a teacher's alternatives (score(..., top_k) of its logits) as the target ----------------
+    _DISTILL = {"given": B.DISTILL_GIVEN, "normalized": B.DISTILL_NORMALIZED, "rest": B.DISTILL_REST}
+
+    def _distill_params(self, logits, top_ids, mode, row_stride):
+        if mode not in self._DISTILL:
+            raise ValueError("mode %r: one of %s" % (mode, ", ".join(sorted(self._DISTILL))))
+        if top_ids.dim() != 2 or top_ids.shape[0] < self.T_max:
+            raise ValueError("top_ids has shape %s, T_max is %d" % (tuple(top_ids.shape), self.T_max))
+        return B.DistillParams(self.T_max, self.V, self.loss_params.dtype, self.V if row_stride is None else row_stride, top_ids.shape[1],
+                               self._DISTILL[mode], self.loss_params.temperature)
+
+    def distill(self, logits, top_ids, top_logp, mode="rest", weight=None, dlogits=None, row_stride=None, n_tokens_dev=None, out=None):
+        """Distillation loss of `logits` [T_max, V] (the student's, with the temperature of the loss) against a teacher's tokens and their
+        log-probs, [T_max, K] each (ids of -1: no entry): a dict of loss, lse [T_max] and stats [T_max, 4] (for distill_backward).
+        mode "given": the log-probs as they stand, "normalized": over their sum, "rest": with the remainder as one more outcome.
+        dlogits (`logits` itself for in place): the gradient of sum(weight * loss) in the same call (weight f32 [T_max], None: ones).
+        Rows past the token count (the packer's, or n_tokens_dev) are left as they were.  `out`: the dict of an earlier call."""
+        prm = self._distill_params(logits, top_ids, mode, row_stride)
+        T = self.T_max
+        if out is None:
+            f32 = dict(dtype=torch.float32, device=self.device)
+            out = {"loss": torch.zeros(T, **f32), "lse": torch.zeros(T, **f32), "stats": torch.zeros(T, 4, **f32)}
+        for n, want in (("loss", ()), ("lse", ()), ("stats", (4,))):
+            if out[n].shape[1:] != want or out[n].dim() != len(want) + 1 or out[n].shape[0] < T:
+                raise ValueError("out: %s has shape %s, this call needs %s" % (n, tuple(out[n].shape), (T,) + want))
+        B.distill_topk(prm, logits, top_ids, top_logp, self.counts[3:4] if n_tokens_dev is None else n_tokens_dev, weight, out["loss"],
+                       out["lse"], out["stats"], dlogits, self.status)
+        return out
+
+    def distill_backward(self, logits, top_ids, top_logp, distilled, dloss=None, mode="rest", dlogits=None, row_stride=None, n_tokens_dev=None):
+        """Gradient with respect to `logits` for the per-token derivatives dloss (f32 [T_max], None: ones); `distilled` is what distill()
+        returned for the same arguments.  Returns dlogits (`logits` itself for in place; a new tensor of its shape and strides if None)."""
+        prm = self._distill_params(logits, top_ids, mode, row_stride)
+        if dlogits is None:
+            dlogits = self._zeros_like_rows(logits)
+        B.distill_topk_backward(prm, logits, top_ids, top_logp, self.counts[3:4] if n_tokens_dev is None else n_tokens_dev,
+                                distilled["stats"], dloss, dlogits, self.status)
+        return dlogits
+
+    # -- verification: which tokens of earlier completions (or of a draft model) stand under this policy --------
+    def verify(self, target_logits, drafts, cu_drafts, draft_logits=None, draft_temperature=None, uniforms=None, noise=None, generator=None,
+               out=None):
+        """The tokens of n sequences that stand under the policy that made `target_logits`, and the next one of each.  drafts i32 [T],
+        cu_drafts i32 [n + 1]; target_logits [T + n, V] has one more row than drafts for each sequence, draft_logits [T, V] the
+        distributions that the drafts were drawn from (None: they were copied, e.g. from an earlier epoch's completion).  uniforms f32
+        [T] and noise f32 [n, V] (exponential, rows on 16 bytes) are drawn from `generator` where they are None.  Returns a dict: n_accepted
+        i32 [n], tokens i32 and logp f32 [T + n] (the accepted drafts, the next token, then -1 and 0), and the call's workspace.  logp is
+        what loss() takes as logp_old for those tokens.  `out`: the dict of an earlier call of the same sizes."""
+        T, n, V, dev = drafts.numel(), cu_drafts.numel() - 1, self.V, self.device
+        per = 8 if self.loss_params.dtype == B.BF16 else 4
+        stride = lambda x, m: x.stride(0) if x.shape[0] > 1 else (max(V, x.stride(0)) + m - 1) // m * m
+        if uniforms is None:
+            uniforms = torch.rand(T, device=dev, generator=generator)
+        if noise is None:
+            noise = torch.empty(n, (V + 3) // 4 * 4, device=dev).exponential_(generator=generator)
+        prm = B.VerifyParams(T, n, V, self.loss_params.dtype, stride(target_logits, per), stride(draft_logits, per) if draft_logits is not None else 0,
+                             stride(noise, 4), self.loss_params.temperature,
+                             self.loss_params.temperature if draft_temperature is None else draft_temperature)
+        need = B.verify_drafts_workspace_bytes(prm)
+        if out is None:
+            out = {"n_accepted": torch.zeros(n, dtype=torch.int32, device=dev), "tokens": torch.full((T + n,), -1, dtype=torch.int32, device=dev),
+                   "logp": torch.zeros(T + n, device=dev), "workspace": torch.empty(need, dtype=torch.uint8, device=dev)}
+        B.verify_drafts(prm, target_logits, draft_logits, drafts, cu_drafts, uniforms, noise, out["n_accepted"], out["tokens"], out["logp"],
+                        out["workspace"], need, self.status)
         return out
 
     def step_from_host(self, batch_host, token_host, dev_tokens, seed=0, step=0, dlogits=None):
