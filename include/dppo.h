@@ -469,7 +469,8 @@ typedef struct {
  *   weight       f32 [T_max] or NULL (1): dL/dloss of each row, for dlogits; the loss is written without it
  *   loss_out, lse_out   f32 [T_max] or NULL
  *   stats        f32 [T_max x 4]: {m, S, G, r / sigma} of each row for the backward call (m the largest logit, S = sum_v
- *                exp((z_v - m) / tau)); may be NULL without dlogits
+ *                exp((z_v - m) / tau); -log2(r / sigma - G) in place of r / sigma where r / sigma - G is above 16); may be NULL without
+ *                dlogits
  *   dlogits      NULL (loss alone), or the gradient in the same call: same dtype / stride as logits; may alias logits (in
  *                place).  Columns at or past V are not written.
  * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED (logits, dlogits, stats: base or row stride), UNSUPPORTED (dtype).

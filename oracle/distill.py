@@ -43,15 +43,16 @@ def distill_topk(z, top_ids, top_logp, mode, temperature):
             loss = float((p[on] * (lp[on] - lns[ids[on]])).sum())
         listed = np.zeros(V, dtype=bool)
         listed[ids] = True
-        rest = e[~listed].sum()
-        out["sigma"][t] = rest / S
+        out["sigma"][t] = e[~listed].sum() / S
+        xr = x[~listed]                                              # the unlisted ones relative to their own maximum
+        mr = xr.max() if xr.size else -np.inf
+        er = np.exp(xr - mr) if mr > -np.inf else np.zeros(xr.size)
         dz = s * (P + r)
         np.subtract.at(dz, ids, p)
         if r > 0:
-            with np.errstate(divide="ignore"):
-                loss += r * (np.log(r) - np.log(rest / S))
-            if rest > 0:
-                dz[~listed] -= r * e[~listed] / rest
+            loss += r * (np.log(r) - (np.log(er.sum()) + mr - np.log(S))) if mr > -np.inf else np.inf
+            if mr > -np.inf:
+                dz[~listed] -= r * er / er.sum()
         out["loss"][t] = loss
         out["dz"][t] = dz / temperature
     return out

@@ -13,8 +13,12 @@
 // test; the marked vectors are left out there, and a warp of its own (which also fetches the teacher's entries and their logits)
 // adds the unlisted entries of each from the vector itself.
 //
-// Gradient (distill_backward_kernel): a map over the row from the forward's {m, S, G, r / sigma}; the listed entries are written
-// afterwards.
+// Loss and gradient together (distill_step_kernel): one read and one write of the row.  A row's slices lie in the shared memory of the CTAs
+// of a cluster; the listed entries are set to -inf there, the exponentials replace the logits (as fp16 pairs for bf16 rows), and once the
+// row's sums are known the slices leave scaled; the listed entries are written last.  Short rows (distill_warp_kernel) do the same in
+// a warp's registers.
+//
+// Gradient alone (distill_backward_kernel): a map over the row from the forward's {m, S, G, r / sigma}; the listed entries last here too.
 #include <cooperative_groups.h>
 
 #include <type_traits>
@@ -126,10 +130,11 @@ __device__ __forceinline__ double warp_sum_f64(double v) {
 
 // ---- the row's loss from its parts ---------------------------------------------------------------------
 struct RowOut {                                    // in every lane
-    float m, S, G, share;                          // what the backward call reads
+    float m, S, G, share;                          // what the backward call reads; share: r / sigma, or -log2(r / sigma - G) where that is above 16
+    float to_rest;                                 // gradient of an unlisted entry: its exponential relative to the unlisted entries' maximum times this
     double norm;                                   // the listed p times this are the loss's p
     float loss, lse;
-    bool zero;                                     // no gradient: an empty row or a bad id
+    bool zero;                                     // no gradient of the listed entries: an empty row or a bad id
 };
 // rest: the row without its listed entries.  The exponentials of the listed ones go to ej.
 template <int kPer> __device__ __forceinline__ RowOut row_finish(const Args& a, const Listed<kPer>& e, const float (&lp)[kPer], const Part& rest, float (&ej)[kPer]) {
@@ -142,7 +147,9 @@ template <int kPer> __device__ __forceinline__ RowOut row_finish(const Args& a, 
     }
     bad = __any_sync(kAll, bad);
     const float M = fmaxf(rest.m, warp_max_f32(zmax));
-    const float Sr = rest.S > 0.0f ? rest.S * ex2((rest.m - M) * a.c) : 0.0f;
+    // the unlisted sum relative to M may underflow; its logarithm does not
+    const double down = ((double)rest.m - (double)M) * a.inv_tau;
+    const float shrink = rest.S > 0.0f ? ex2((rest.m - M) * a.c) : 0.0f, Sr = rest.S * shrink;
     float Sl = 0.0f;
     double P = 0.0, B = 0.0;
 #pragma unroll
@@ -157,7 +164,7 @@ template <int kPer> __device__ __forceinline__ RowOut row_finish(const Args& a, 
     const double S = (double)Sr + (double)Sl, l = log64(S);
     RowOut o;
     o.norm = 1.0;
-    double G = P, r = 0.0, loss;
+    double G = P, r = 0.0, loss, ln_share = 0.0;
     const bool empty = !(S > 0.0) && !bad;
     if (a.mode == DPPO_DISTILL_NORMALIZED) {
         o.norm = P > 0.0 ? inv64(P) : 0.0;
@@ -168,19 +175,35 @@ template <int kPer> __device__ __forceinline__ RowOut row_finish(const Args& a, 
         if (a.mode == DPPO_DISTILL_REST) {
             r = 1.0 - P > kLeastRest ? 1.0 - P : 0.0;
             G = P + r;
-            if (r > 0.0) loss += r * (log64(r) - (log64((double)Sr) - l));
+            if (r > 0.0) {
+                ln_share = rest.S > 0.0f ? log64(r) - (log64((double)rest.S) + down) + l : INFINITY;
+                loss += r * ln_share;
+            }
         }
     }
     if (empty) loss = P > 0.0 ? INFINITY : P != 0.0 ? P : 0.0;
     const float nan = __int_as_float(0x7fffffff);
     o.m = bad ? nan : empty ? -INFINITY : M;
     o.S = (float)S; o.G = (float)G;
-    o.share = r > 0.0 ? (float)r * (float)S / Sr : 0.0f;
-    if (bad) o.S = o.G = o.share = nan;
+    // a large share goes into the entries' exponents: times an exponential that underflows relative to M it would be lost
+    if (!(r > 0.0)) {
+        o.share = 0.0f;
+    } else if (!(rest.S > 0.0f)) {
+        o.share = INFINITY;
+    } else if (ln_share > 2.8) {
+        const double share = ln_share < 69.0 ? exp64(ln_share) - G : 0.0;
+        o.share = ln_share >= 69.0 ? (float)(-1.4426950408889634 * ln_share)
+                  : share > 16.0 ? (float)(-1.4426950408889634 * log64(share)) : (float)r * (float)S / Sr;
+    } else {
+        o.share = (float)r * (float)S / Sr;
+    }
+    o.to_rest = rest.S > 0.0f ? (float)G * shrink / (float)S - (float)r / rest.S : 0.0f;
+    if (bad) o.S = o.G = o.share = o.to_rest = nan;
     o.loss = bad ? nan : e.bad ? 0.0f : (float)loss;
     o.lse = bad ? nan : empty ? -INFINITY : (float)((double)M * a.inv_tau + l);
     o.zero = e.bad || empty;
-    if (e.bad) { o.G = 0.0f; o.share = 0.0f; }
+    if (e.bad) o.G = o.share = o.to_rest = 0.0f;
+    if (empty) o.to_rest = 0.0f;
     return o;
 }
 __device__ __forceinline__ void row_write(const Args& a, long long t, const RowOut& o, bool bad_id, int lane) {
@@ -354,6 +377,304 @@ distill_forward_kernel(const Args a) {
     }
 }
 
+// ---- loss and gradient, a row in the shared memory of a cluster ------------------------------------------------
+template <int kThreads> struct StepShared {
+    Part part;                                     // of this CTA's slice, listed entries left out
+    float m[kThreads / 32], s[kThreads / 32];
+    float scale;                                   // of the exponentials kept in this CTA's slice
+    unsigned tail_listed;
+};
+
+// The gradient of the listed entries that `here` (a predicate of the vector index) accepts, after everything else of their row.
+template <bool kBf16, int kPer, class F>
+__device__ __forceinline__ void write_listed(char* out, const Listed<kPer>& e, const float (&ej)[kPer], const RowOut& o, float wt, F here) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+        if (e.first[i] && here(e.id[i] >> (kBf16 ? 3 : 2)))
+            Elems<kBf16>::store1(out, e.id[i], o.zero ? 0.0f : wt * (float)((double)(ej[i] / o.S) * (double)o.G - e.p[i] * o.norm));
+}
+// p of entries listed twice, added up; listed_first has to run after the loss has been formed from the single ones.
+template <int kPer> __device__ __forceinline__ void listed_sums(const Args& a, int lane, Listed<kPer>& e) { listed_first<kPer>(a, lane, e, true); }
+
+template <bool kBf16, int kThreads, int kPer>
+__global__ void __launch_bounds__(kThreads + 32)
+distill_step_kernel(const Args a, int log2C, int vec_per_cta) {
+    constexpr int kLog2 = kBf16 ? 3 : 2, kPerVec = 1 << kLog2, kWarps = kThreads / 32;
+    extern __shared__ uint4 slice[];
+    __shared__ StepShared<kThreads> sh;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    wait_for_previous();
+    const long long T = rows_of(a);
+    const int rank = blockIdx.x & ((1 << log2C) - 1);
+    const long long t = (long long)(blockIdx.x >> log2C);
+    if (t >= T) return;                                            // the whole cluster leaves together
+    const char* row = a.logits + t * a.row_bytes;
+    char* out = a.dlogits + t * a.row_bytes;
+    const int nvec = a.V >> kLog2, tail0 = nvec << kLog2;
+    const int v0 = rank * vec_per_cta, nv = max(0, min(vec_per_cta, nvec - v0));
+    const bool last = rank == (1 << log2C) - 1;
+
+    Listed<kPer> e;
+    float lp[kPer];
+    float wt = 0.0f;
+    if (warp < kWarps) {                                           // the slice: every thread's own vectors, then everybody's
+        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(slice);
+        for (int i = tid; i < nv; i += kThreads)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst + (uint32_t)i * 16u), "l"(row + (size_t)(v0 + i) * 16) : "memory");
+        if (tid == 0) sh.tail_listed = 0;
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    } else {
+        listed_ids<kPer>(a, t, lane, e, lp);
+        wt = (float)((a.weight ? (double)a.weight[t] : 1.0) * a.inv_tau);
+        listed_logits<kBf16, kPer>(row, e);
+        listed_probs<kPer>(lp, e);
+        listed_first<kPer>(a, lane, e, false);
+    }
+    __syncthreads();
+    if (warp == kWarps) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int rel = (e.id[i] >> kLog2) - v0;
+            if (e.id[i] < 0) continue;
+            if ((e.id[i] >> kLog2) >= nvec) {
+                if (last) atomicOr(&sh.tail_listed, 1u << (e.id[i] & (kPerVec - 1)));
+            } else if (rel >= 0 && rel < nv) {
+                Elems<kBf16>::store1(slice + rel, e.id[i] & (kPerVec - 1), -INFINITY);
+            }
+        }
+    }
+    __syncthreads();
+
+    // the slice's maximum (NaN where there is one)
+    float m = -INFINITY, ztail = -INFINITY;
+    if (warp < kWarps) {
+        if constexpr (kBf16) {
+            __nv_bfloat162 x = __float2bfloat162_rn(-INFINITY);
+#pragma unroll 4
+            for (int i = tid; i < nv; i += kThreads) {
+                const uint4 q = slice[i];
+                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+                const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(w);
+                x = __hmax2_nan(x, __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3])));
+            }
+            m = max_nan(__low2float(x), __high2float(x));
+        } else {
+#pragma unroll 4
+            for (int i = tid; i < nv; i += kThreads) {
+                const uint4 q = slice[i];
+                m = max_nan(m, max_nan(max_nan(__uint_as_float(q.x), __uint_as_float(q.y)), max_nan(__uint_as_float(q.z), __uint_as_float(q.w))));
+            }
+        }
+        if (last && tail0 + tid < a.V && !(sh.tail_listed >> tid & 1u)) ztail = Elems<kBf16>::load1(row, tail0 + tid);
+        m = max_nan(m, ztail);
+        const bool bad = __any_sync(kAll, !(m < INFINITY));
+        m = bad ? __int_as_float(0x7fffffff) : warp_max_f32(m);
+        if (lane == 0) sh.m[warp] = m;
+    }
+    __syncthreads();
+    m = sh.m[0];
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) m = max_nan(m, sh.m[w]);
+    const bool bad = !(m < INFINITY);
+    m = bad ? 0.0f : fmaxf(m, kLowest);
+
+    // the exponentials, in place, and their sum: in the frame of a running sum (see Sum)
+    Sum acc;
+    sum_init(acc, m, a.c);
+    float etail = 0.0f;
+    if (warp < kWarps) {
+        const f32x2 c2 = pair_of(a.c, a.c), nr2 = pair_of(acc.nr, acc.nr), nm2 = pair_of(-m, -m);
+        auto pass = [&](auto is_quick) {
+            auto e2 = [&](float z0, float z1) {
+                float y0, y1;
+                if constexpr (decltype(is_quick)::value) unpair(fma2(pair_of(z0, z1), c2, nr2), y0, y1);
+                else unpair(mul2(add2(pair_of(z0, z1), nm2), c2), y0, y1);
+                const f32x2 r = pair_of(ex2(y0), ex2(y1));
+                acc.S = add2(acc.S, r);
+                return r;
+            };
+#pragma unroll 2
+            for (int i = tid; i < nv; i += kThreads) {
+                const uint4 q = slice[i];
+                uint32_t w[4] = {q.x, q.y, q.z, q.w};
+                if constexpr (kBf16) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float x0, x1;
+                        unpair(e2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u)), x0, x1);
+                        w[j] = pack_half2(x0, x1);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; j += 2) {
+                        float x0, x1;
+                        unpair(e2(__uint_as_float(w[j]), __uint_as_float(w[j + 1])), x0, x1);
+                        w[j] = __float_as_uint(x0); w[j + 1] = __float_as_uint(x1);
+                    }
+                }
+                slice[i] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            if (ztail > -INFINITY) {
+                float unused;
+                unpair(e2(ztail, -INFINITY), etail, unused);
+            }
+        };
+        if (acc.quick) pass(std::true_type()); else pass(std::false_type());
+        float s0, s1;
+        unpair(acc.S, s0, s1);
+        const float s = warp_sum(s0 + s1);
+        if (lane == 0) sh.s[warp] = s;
+    }
+    __syncthreads();
+    const float back = ex2(-acc.res);                              // the frame's shift, out of what was kept
+    cg::cluster_group cl = cg::this_cluster();
+    if (warp == kWarps) {
+        const float s = warp_sum(lane < kWarps ? sh.s[lane] : 0.0f);
+        Part p = {m, bad ? 0.0f : s * back, bad ? 1 : 0};
+        if (!(p.S > 0.0f)) p.m = kLowest;
+        if (lane == 0) sh.part = p;
+        __syncwarp();
+    }
+    if (log2C > 0) cl.sync();                                      // every CTA's part is in its shared memory
+    RowOut o = {};
+    float ej[kPer];
+    if (warp == kWarps) {
+        Part p = lane < (1 << log2C) ? (log2C > 0 ? *cl.map_shared_rank(&sh.part, lane) : sh.part) : part_none();
+        p = part_warp(p, a.c);
+        o = row_finish<kPer>(a, e, lp, p, ej);
+        // to_rest is relative to the row's unlisted maximum, what is kept to this slice's
+        if (lane == 0) sh.scale = wt * o.to_rest * (p.m > m ? ex2((m - p.m) * a.c) : 1.0f) * back;
+        if (rank == 0) row_write(a, t, o, e.bad, lane);
+        __syncwarp();
+    }
+    if (log2C > 0) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // the parts have been read
+    __syncthreads();
+    const float scale = sh.scale;
+    if (warp < kWarps) {
+        uint4* dst = reinterpret_cast<uint4*>(out) + v0;
+        const f32x2 s2 = pair_of(scale, scale);
+#pragma unroll 2
+        for (int i = tid; i < nv; i += kThreads) {
+            const uint4 q = slice[i];
+            uint4 r;
+            if constexpr (kBf16) {
+                r.x = scale_pair(q.x, s2); r.y = scale_pair(q.y, s2); r.z = scale_pair(q.z, s2); r.w = scale_pair(q.w, s2);
+            } else {
+                float x0, x1, x2, x3;
+                unpair(mul2(pair_of(__uint_as_float(q.x), __uint_as_float(q.y)), s2), x0, x1);
+                unpair(mul2(pair_of(__uint_as_float(q.z), __uint_as_float(q.w)), s2), x2, x3);
+                r = make_uint4(__float_as_uint(x0), __float_as_uint(x1), __float_as_uint(x2), __float_as_uint(x3));
+            }
+            __stcs(dst + i, r);
+        }
+        if (last && tail0 + tid < a.V) Elems<kBf16>::store1(out, tail0 + tid, scale * etail);
+    } else {
+        listed_sums<kPer>(a, lane, e);
+    }
+    __syncthreads();                                               // the listed entries' places have been written
+    let_next_start();
+    if (warp == kWarps) write_listed<kBf16, kPer>(out, e, ej, o, wt, [&](int v) { return v >= nvec ? last : v >= v0 && v < v0 + nv; });
+    __syncwarp();
+    if (log2C > 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// ---- short rows: a warp per row, with or without the gradient --------------------------------------------------
+// The row goes through the warp's shared memory once, where its listed entries are read and masked, and stays in registers.
+template <bool kBf16, int kVecs, int kTeams, bool kGradient, int kPer>
+__global__ void __launch_bounds__(32 * kTeams)
+distill_warp_kernel(const Args a) {
+    constexpr int kLog2 = kBf16 ? 3 : 2, kPerVec = 1 << kLog2;
+    __shared__ uint4 rows[kTeams][kVecs * 32];
+    __shared__ unsigned tails[kTeams];
+    const int lane = threadIdx.x & 31, team = threadIdx.x >> 5;
+    uint4* mine = rows[team];
+    enter_kernel();
+    const long long t = (long long)blockIdx.x * kTeams + team;
+    if (t >= rows_of(a)) return;
+    const char* row = a.logits + t * a.row_bytes;
+    const int nvec = a.V >> kLog2, tail = (nvec << kLog2) + lane;
+    uint4 q[kVecs];
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) q[u] = u * 32 + lane < nvec ? load_vec_rw(row + (size_t)(u * 32 + lane) * 16) : masked_vec<kBf16>();
+    float zt = tail < a.V ? Elems<kBf16>::load1(row, tail) : -INFINITY;
+    Listed<kPer> e;
+    float lp[kPer];
+    listed_ids<kPer>(a, t, lane, e, lp);
+    const float wt = kGradient ? (float)((a.weight ? (double)a.weight[t] : 1.0) * a.inv_tau) : 0.0f;
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) mine[u * 32 + lane] = q[u];
+    if (lane == 0) tails[team] = 0;
+    __syncwarp();
+    listed_probs<kPer>(lp, e);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int v = e.id[i] >> kLog2;
+        e.z[i] = e.id[i] < 0 ? -INFINITY : v >= nvec ? Elems<kBf16>::load1(row, e.id[i]) : Elems<kBf16>::load1(mine, e.id[i]);
+    }
+    listed_first<kPer>(a, lane, e, false);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        if (e.id[i] < 0) continue;
+        if ((e.id[i] >> kLog2) >= nvec) atomicOr(&tails[team], 1u << (e.id[i] & (kPerVec - 1)));
+        else Elems<kBf16>::store1(mine, e.id[i], -INFINITY);
+    }
+    __syncwarp();
+    if (tails[team] >> lane & 1u) zt = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) q[u] = mine[u * 32 + lane];
+    __nv_bfloat162 unused;
+    float m = max_nan(vecs_max<kBf16, kVecs>(q, unused), zt);
+    const bool bad = __any_sync(kAll, !(m < INFINITY));
+    m = bad ? 0.0f : fmaxf(warp_max_f32(m), kLowest);
+    Sum acc;
+    sum_init(acc, m, a.c);
+    f32x2 x[kVecs * kPerVec / 2];                                  // the exponentials
+    float xt = 0.0f;
+    {
+        const f32x2 c2 = pair_of(a.c, a.c), nr2 = pair_of(acc.nr, acc.nr), nm2 = pair_of(-m, -m);
+        const bool quick = acc.quick;
+#pragma unroll
+        for (int u = 0; u < kVecs; ++u) {
+            float f[kPerVec];
+            Elems<kBf16>::unpack(q[u], f);
+#pragma unroll
+            for (int j = 0; j < kPerVec; j += 2) {
+                float y0, y1;
+                unpair(quick ? fma2(pair_of(f[j], f[j + 1]), c2, nr2) : mul2(add2(pair_of(f[j], f[j + 1]), nm2), c2), y0, y1);
+                x[(u * kPerVec + j) / 2] = pair_of(ex2(y0), ex2(y1));
+                acc.S = add2(acc.S, x[(u * kPerVec + j) / 2]);
+            }
+        }
+        xt = ex2(quick ? fmaf(zt, a.c, acc.nr) : (zt - m) * a.c);
+    }
+    const float back = ex2(-acc.res);
+    float s0, s1;
+    unpair(acc.S, s0, s1);
+    Part p = {m, warp_sum(s0 + s1 + xt) * back, bad ? 1 : 0};
+    if (!(p.S > 0.0f)) p.m = kLowest;
+    float ej[kPer];
+    const RowOut o = row_finish<kPer>(a, e, lp, p, ej);
+    row_write(a, t, o, e.bad, lane);
+    if constexpr (kGradient) {
+        char* out = a.dlogits + t * a.row_bytes;
+        const float scale = wt * o.to_rest * back;
+        const f32x2 s2 = pair_of(scale, scale);
+#pragma unroll
+        for (int u = 0; u < kVecs; ++u) {
+            if (u * 32 + lane >= nvec) continue;
+            float f[kPerVec];
+#pragma unroll
+            for (int j = 0; j < kPerVec; j += 2) unpair(mul2(x[(u * kPerVec + j) / 2], s2), f[j], f[j + 1]);
+            __stcs(reinterpret_cast<uint4*>(out) + u * 32 + lane, Elems<kBf16>::pack(f));
+        }
+        if (tail < a.V) Elems<kBf16>::store1(out, tail, scale * xt);
+        listed_sums<kPer>(a, lane, e);
+        __syncwarp();
+        write_listed<kBf16, kPer>(out, e, ej, o, wt, [](int) { return true; });
+    }
+}
+
 // ---- gradient from the forward's statistics ---------------------------------------------------------------
 template <bool kBf16, int kThreads, int kTeams, int kUnroll, int kPer>
 __global__ void __launch_bounds__(kThreads * kTeams)
@@ -386,13 +707,14 @@ distill_backward_kernel(const Args a) {
 
     const bool empty = st.x == -INFINITY;
     const float inv = st.y > 0.0f || st.y != st.y ? 1.0f / st.y : 0.0f;
-    // share = inf: nothing unlisted has a probability, so nothing is multiplied by it
-    const float coef = empty || st.w == INFINITY ? 0.0f : wt * (st.z - st.w) * inv;
+    // share = inf: nothing unlisted has a probability, so nothing is multiplied by it; below 0: its exponent, which the entries' take up
+    const bool far = st.w < 0.0f;
+    const float coef = empty || st.w == INFINITY ? 0.0f : far ? -wt * inv : wt * (st.z - st.w) * inv;
     const bool zero = empty || coef == 0.0f;
     const f32x2 c2 = pair_of(a.c, a.c), g2 = pair_of(coef, coef);
     const float r = st.x * a.c;
-    const bool quick = fabsf(r) <= 1048576.0f && fabsf(st.x) <= 1e37f;             // as in the forward's sum
-    const f32x2 nr2 = pair_of(-r, -r), nm2 = pair_of(-st.x, -st.x);
+    const bool quick = !far && fabsf(r) <= 1048576.0f && fabsf(st.x) <= 1e37f;     // as in the forward's sum
+    const f32x2 nr2 = pair_of(-r, -r), nm2 = pair_of(-st.x, -st.x), up2 = pair_of(-st.w, -st.w);
     const float res = quick ? fmaf(st.x, a.c, -r) : 0.0f;
     const f32x2 gq2 = pair_of(coef * ex2(-res), coef * ex2(-res));
     auto put = [&](const uint4& q, int i, auto is_quick) {
@@ -402,6 +724,7 @@ distill_backward_kernel(const Args a) {
         for (int j = 0; j < kPerVec; j += 2) {
             float y0, y1;
             if constexpr (decltype(is_quick)::value) unpair(fma2(pair_of(z[j], z[j + 1]), c2, nr2), y0, y1);
+            else if (far) unpair(fma2(add2(pair_of(z[j], z[j + 1]), nm2), c2, up2), y0, y1);
             else unpair(mul2(add2(pair_of(z[j], z[j + 1]), nm2), c2), y0, y1);
             unpair(mul2(pair_of(ex2(y0), ex2(y1)), decltype(is_quick)::value ? gq2 : g2), z[j], z[j + 1]);
         }
@@ -434,7 +757,7 @@ distill_backward_kernel(const Args a) {
     }
     if (last && tail0 + tid < a.V) {
         const float z = Elems<kBf16>::load1(row, tail0 + tid);
-        Elems<kBf16>::store1(out, tail0 + tid, zero ? 0.0f : coef * ex2((z - st.x) * a.c));
+        Elems<kBf16>::store1(out, tail0 + tid, zero ? 0.0f : coef * ex2(fmaf(z - st.x, a.c, far ? -st.w : 0.0f)));
     }
     if constexpr (kThreads == 32) __syncwarp(); else __syncthreads();          // the listed entries' places have been written
     if (tid >= 32) return;
@@ -467,6 +790,8 @@ distill_backward_kernel(const Args a) {
 }
 
 // ---- host side -------------------------------------------------------------------------------------------
+template <bool kBf16, bool kGradient, int kPer> static int run_warp(const Args& a, cudaStream_t s);
+
 template <bool kBf16, int kThreads, int kPer, bool kCluster> static int launch_fwd(const Args& a, int C, cudaStream_t s) {
     auto kernel = distill_forward_kernel<kBf16, kThreads, kPer, kCluster>;
     const int nvec = a.V >> (kBf16 ? 3 : 2);
@@ -479,11 +804,51 @@ template <bool kBf16, int kPer> static int run_fwd(const Args& a, cudaStream_t s
     const int nvec = a.V >> (kBf16 ? 3 : 2);
     const long long sms = sm_count();
     int C = 1;
+    if (nvec <= 256) return run_warp<kBf16, false, kPer>(a, s);
     if (nvec > 4096)
         while (C < kMaxCluster && a.T_max * C < 2 * sms) C *= 2;
     if (nvec <= 512) return launch_fwd<kBf16, 128, kPer, false>(a, 1, s);
     if (C == 1) return launch_fwd<kBf16, 128, kPer, false>(a, 1, s);
     return launch_fwd<kBf16, 256, kPer, true>(a, C, s);
+}
+
+template <bool kBf16, int kVecs, bool kGradient, int kPer> static int launch_warp(const Args& a, cudaStream_t s) {
+    constexpr int kTeams = 4;
+    return launch_after("distill_topk launch", distill_warp_kernel<kBf16, kVecs, kTeams, kGradient, kPer>, (a.T_max + kTeams - 1) / kTeams, 32 * kTeams, 0, s, 1, a);
+}
+template <bool kBf16, bool kGradient, int kPer> static int run_warp(const Args& a, cudaStream_t s) {
+    const int nvec = a.V >> (kBf16 ? 3 : 2);
+    if (nvec <= 32) return launch_warp<kBf16, 1, kGradient, kPer>(a, s);
+    if (nvec <= 64) return launch_warp<kBf16, 2, kGradient, kPer>(a, s);
+    if (nvec <= 128) return launch_warp<kBf16, 4, kGradient, kPer>(a, s);
+    return launch_warp<kBf16, 8, kGradient, kPer>(a, s);
+}
+
+constexpr size_t kSliceMax = 220 * 1024;
+template <bool kBf16, int kThreads, int kPer> static int launch_step(const Args& a, int log2C, int vec_per_cta, cudaStream_t s) {
+    auto kernel = distill_step_kernel<kBf16, kThreads, kPer>;
+    static bool raised[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); dev = -1; }
+    if (dev < 0 || !raised[dev]) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSliceMax);
+        if (e != cudaSuccess) { cudaGetLastError(); return cuda_fail(e, "distill_topk: shared memory attribute"); }
+        if (dev >= 0) raised[dev] = true;
+    }
+    if (a.T_max << log2C > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "distill_topk: T_max=%lld needs too large a grid", a.T_max);
+    return launch_after("distill_topk launch", kernel, a.T_max << log2C, kThreads + 32, (size_t)max(vec_per_cta, 1) * 16, s, 1 << log2C, a, log2C, vec_per_cta);
+}
+// The slices of a row: in one CTA up to 44 KB, in two of up to 55 KB, else in four or eight of up to 76 KB, three of which share an SM.
+template <bool kBf16, int kPer> static int run_step(const Args& a, cudaStream_t s, bool* done) {
+    const int nvec = a.V >> (kBf16 ? 3 : 2);
+    *done = true;
+    if (nvec <= 256) return run_warp<kBf16, true, kPer>(a, s);
+    const long long bytes = (long long)nvec * 16;
+    const int log2C = bytes <= 44 << 10 ? 0 : bytes <= 110 << 10 ? 1 : bytes <= 304 << 10 ? 2 : 3;
+    const int vec = (nvec + (1 << log2C) - 1) >> log2C;
+    if ((size_t)vec * 16 > kSliceMax) { *done = false; return DPPO_OK; }
+    if (vec * 16 > (kBf16 ? 28 : 64) << 10) return launch_step<kBf16, 256, kPer>(a, log2C, vec, s);
+    return launch_step<kBf16, 128, kPer>(a, log2C, vec, s);
 }
 
 template <bool kBf16, int kThreads, int kTeams, int kUnroll, int kPer> static int launch_bwd(const Args& a, cudaStream_t s) {
@@ -532,6 +897,15 @@ static Args args_of(const dppo_distill_params* p, const void* logits, const int3
 }
 
 template <bool kBf16> static int run_fwd_k(const Args& a, cudaStream_t s) { return a.k <= 32 ? run_fwd<kBf16, 1>(a, s) : run_fwd<kBf16, 4>(a, s); }
+// Loss and gradient in one kernel where the row fits the shared memory of eight CTAs, else one after the other.
+template <bool kBf16, int kPer> static int run_both(const Args& a, cudaStream_t s) {
+    bool done;
+    int rc = run_step<kBf16, kPer>(a, s, &done);
+    if (rc != DPPO_OK || done) return rc;
+    rc = run_fwd<kBf16, kPer>(a, s);
+    return rc != DPPO_OK ? rc : run_bwd<kBf16, kPer>(a, s);
+}
+template <bool kBf16> static int run_both_k(const Args& a, cudaStream_t s) { return a.k <= 32 ? run_both<kBf16, 1>(a, s) : run_both<kBf16, 4>(a, s); }
 template <bool kBf16> static int run_bwd_k(const Args& a, cudaStream_t s) { return a.k <= 32 ? run_bwd<kBf16, 1>(a, s) : run_bwd<kBf16, 4>(a, s); }
 
 }  // namespace distill
@@ -549,9 +923,8 @@ extern "C" int dppo_distill_topk(const dppo_distill_params* p, const void* logit
     distill::Args a = distill::args_of(p, logits, top_ids, top_logp, n_tokens_dev, weight, dlogits, status);
     a.loss = loss_out; a.lse = lse_out; a.stats = (float4*)stats; a.stats_in = (const float4*)stats;
     cudaStream_t s = (cudaStream_t)stream;
-    const int f = p->dtype == DPPO_BF16 ? distill::run_fwd_k<true>(a, s) : distill::run_fwd_k<false>(a, s);
-    if (f != DPPO_OK || !dlogits) return f;
-    return p->dtype == DPPO_BF16 ? distill::run_bwd_k<true>(a, s) : distill::run_bwd_k<false>(a, s);
+    if (dlogits) return p->dtype == DPPO_BF16 ? distill::run_both_k<true>(a, s) : distill::run_both_k<false>(a, s);
+    return p->dtype == DPPO_BF16 ? distill::run_fwd_k<true>(a, s) : distill::run_fwd_k<false>(a, s);
 }
 
 extern "C" int dppo_distill_topk_backward(const dppo_distill_params* p, const void* logits, const int32_t* top_ids, const float* top_logp,

@@ -7,7 +7,8 @@ has the sum over what is not listed, eR with its own mean.  The loss adds P ln S
     |loss error| <= P eS + r (eS + eR) + u |loss|.
 A gradient entry w (s (G - share) - p): s carries eS + (3 |x| + 4) u, share eS + eR, and G, share, w and the products 8 roundings:
     |error| <= w s (G + share) (eS + eR + (3 |x| + 12) u) + 4 u w p + half a step of the type,
-and 2^-126 w (G + share) where an exponential is below the normal numbers.  The call that returns loss and gradient at once keeps the
+and where an exponential is below the normal numbers, 2^-126 w times what it is multiplied by: at most G + 17, since a share - G above 16
+goes into the exponent.  The call that returns loss and gradient at once keeps the
 exponentials of bf16 rows in 16 bits between its two passes: 2^-11 more relative to s, and, below 2^-14 of the largest unlisted entry
 of the row, 2^-25 of that.
 """
@@ -120,8 +121,11 @@ def check(r, z, V, ids, lp, mode, tau, w=None, rows=None):
         listed[ids[t].cpu().numpy()[ids[t].cpu().numpy() >= 0]] = True
         base = (3 + 6 * n + 16) * U
         eS = base + 3 * U * (e * np.abs(x)).sum() / e.sum()
-        rest = e[~listed].sum()
-        eR = base + (3 * U * (e * np.abs(x))[~listed].sum() / rest if rest > 0 else 0.0)
+        xr = x[~listed & (row > -np.inf)]                            # relative to their own maximum: their sum does not underflow
+        mr = xr.max() if xr.size else 0.0
+        er = np.where(listed | (row == -np.inf), 0.0, np.exp(np.minimum(x - mr, 0.0)))
+        rest = er.sum()
+        eR = base + (3 * U * (er * np.abs(x - mr)).sum() / rest + 3 * U * abs(mr) if rest > 0 else 0.0)
         P, rr = want["P"][t], want["r"][t]
         tol = P * eS + rr * (eS + eR)
         for o in got.values():
@@ -129,16 +133,16 @@ def check(r, z, V, ids, lp, mode, tau, w=None, rows=None):
             assert a == b or abs(a - b) <= tol + U * abs(b), ("loss", t, a, b, tol)
             a, b = o["lse"][t, 0], want["lse"][t]
             assert abs(a - b) <= eS + 4 * U * abs(np.log(e.sum())) + 3 * U * abs(m) / tau + U * abs(b), ("lse", t, a, b)
-        share = rr * e.sum() / rest if rest > 0 and rr > 0 else 0.0
         s, G, ww = e / e.sum(), P + rr, abs(wt[t]) / tau
-        p = np.abs(want["dz"][t] * tau - s * (G - np.where(listed, 0.0, share)))
-        tol = ww * s * (G + share) * (eS + eR + (3 * np.abs(x) + 12) * U) + 4 * U * ww * p + ww * (G + share) * 2.0 ** -126
+        to_rest = rr * er / rest if rest > 0 else er                 # s r / sigma
+        p = np.abs(want["dz"][t] * tau - s * G + to_rest)
+        size = s * G + to_rest
+        tol = ww * size * (eS + eR + (3 * np.abs(x) + 12) * U) + 4 * U * ww * p + ww * (G + 17) * 2.0 ** -126
         b = want["dz"][t] * wt[t]
         for k, g in grads.items():
             more = tol
             if k == "step" and dtype == "bf16":
-                top = (s[~listed]).max() if rest > 0 else 0.0
-                more = tol + ww * (G + share) * (s * 2.0 ** -11 + 2.0 ** -25 * top)
+                more = tol + ww * (size * 2.0 ** -11 + 2.0 ** -25 * size[~listed].max(initial=0.0))
             bad = np.abs(g[t] - b) > more * (1 + half) + half * np.abs(b) + 1e-40
             assert not bad.any(), (k, t, np.flatnonzero(bad)[:5], g[t][bad][:5], b[bad][:5], more[bad][:5] if np.ndim(more) else more)
 
@@ -195,6 +199,17 @@ def test_rows_where_it_can_go_wrong(B, V, dtype, mode, K):
     ids[13, ::2] = -1
     r = Run(B, z, V, ids, lp, mode, 1.0)
     check(r, z, V, ids, lp, mode, 1.0)
+
+
+@pytest.mark.parametrize("V,dtype", [(500, "f32"), (3001, "bf16"), (60001, "f32")])
+@pytest.mark.parametrize("tau", [0.02, 0.004, 30.0])
+def test_far_temperatures(B, V, dtype, tau):
+    """A cold student's unlisted tokens are far below the listed ones (sigma down to e^-2000): the loss and its gradient stay finite."""
+    z, ids, lp = make(6, V, dtype, 6, V)
+    lp -= 0.3                                                        # the teacher leaves a remainder
+    r = Run(B, z, V, ids, lp, 2, tau)
+    assert bool(r.one["loss"][:6].isfinite().all())
+    check(r, z, V, ids, lp, 2, tau)
 
 
 @pytest.mark.parametrize("V,dtype", [(300, "f32"), (70001, "bf16")])
