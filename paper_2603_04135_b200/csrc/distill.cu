@@ -71,17 +71,27 @@ template <int kPer> struct Listed {
     bool bad;                                      // (all lanes) an id outside [-1, V)
 };
 
-template <int kPer> __device__ __forceinline__ void listed_ids(const Args& a, long long t, int lane, Listed<kPer>& e, float (&lp)[kPer]) {
-    bool bad = false;
+// Asked for, and (when they are needed) looked at: ids outside [-1, V) make the row bad and count as no entry.
+template <int kPer> __device__ __forceinline__ void listed_ask(const Args& a, long long t, int lane, Listed<kPer>& e, float (&lp)[kPer]) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int j = i * 32 + lane;
         e.id[i] = j < a.k ? a.ids[t * a.k + j] : -1;
         lp[i] = j < a.k ? a.logp[t * a.k + j] : -INFINITY;
+    }
+}
+template <int kPer> __device__ __forceinline__ void listed_check(const Args& a, Listed<kPer>& e) {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
         bad = bad || e.id[i] < -1 || e.id[i] >= a.V;
         if (e.id[i] < 0 || e.id[i] >= a.V) e.id[i] = -1;
     }
     e.bad = __any_sync(kAll, bad);
+}
+template <int kPer> __device__ __forceinline__ void listed_ids(const Args& a, long long t, int lane, Listed<kPer>& e, float (&lp)[kPer]) {
+    listed_ask<kPer>(a, t, lane, e, lp);
+    listed_check<kPer>(a, e);
 }
 template <bool kBf16, int kPer> __device__ __forceinline__ void listed_logits(const char* row, Listed<kPer>& e) {
 #pragma unroll
@@ -129,88 +139,103 @@ __device__ __forceinline__ double warp_sum_f64(double v) {
 }
 
 // ---- the row's loss from its parts ---------------------------------------------------------------------
-struct RowOut {                                    // in every lane
-    float m, S, G, share;                          // what the backward call reads; share: r / sigma, or -log2(r / sigma - G) where that is above 16
-    float to_rest;                                 // gradient of an unlisted entry: its exponential relative to the unlisted entries' maximum times this
-    double norm;                                   // the listed p times this are the loss's p
-    float loss, lse;
-    bool zero;                                     // no gradient of the listed entries: an empty row or a bad id
+// What the teacher's entries alone say (in every lane): formed while the row is under way.
+struct Mass {
+    double P, lp, z;                               // sums of p, of p ln p and of p (z - zmax)
+    float G, r, norm;                              // the listed p times norm are the loss's p
+    float zmax;
+    bool bad;                                      // a NaN or +inf among the listed logits
 };
-// rest: the row without its listed entries.  The exponentials of the listed ones go to ej.
-template <int kPer> __device__ __forceinline__ RowOut row_finish(const Args& a, const Listed<kPer>& e, const float (&lp)[kPer], const Part& rest, float (&ej)[kPer]) {
-    float zmax = kLowest;
-    bool bad = rest.bad;
+template <int kPer> __device__ __forceinline__ Mass listed_mass(const Args& a, const Listed<kPer>& e, const float (&lp)[kPer]) {
+    Mass m;
+    m.zmax = kLowest;
+    m.P = m.lp = m.z = 0.0;
+    bool bad = false;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         bad = bad || !(e.z[i] < INFINITY);
-        if (e.z[i] < INFINITY) zmax = fmaxf(zmax, e.z[i]);
+        if (e.z[i] < INFINITY) m.zmax = fmaxf(m.zmax, e.z[i]);
     }
-    bad = __any_sync(kAll, bad);
-    const float M = fmaxf(rest.m, warp_max_f32(zmax));
-    // the unlisted sum relative to M may underflow; its logarithm does not
-    const double down = ((double)rest.m - (double)M) * a.inv_tau;
-    const float shrink = rest.S > 0.0f ? ex2((rest.m - M) * a.c) : 0.0f, Sr = rest.S * shrink;
-    float Sl = 0.0f;
-    double P = 0.0, B = 0.0;
+    m.bad = __any_sync(kAll, bad);
+    m.zmax = warp_max_f32(m.zmax);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        const double y = ((double)e.z[i] - (double)M) * a.inv_tau;
-        ej[i] = e.id[i] >= 0 ? ex2((e.z[i] - M) * a.c) : 0.0f;
-        if (e.first[i]) Sl += ej[i];
-        P += e.p[i];
-        if (e.p[i] != 0.0) B += e.p[i] * ((double)lp[i] - y);
+        m.P += e.p[i];
+        if (e.p[i] != 0.0) { m.lp += e.p[i] * (double)lp[i]; m.z += e.p[i] * ((double)e.z[i] - (double)m.zmax); }
     }
-    Sl = warp_sum(Sl); P = warp_sum_f64(P); B = warp_sum_f64(B);
-    const double S = (double)Sr + (double)Sl, l = log64(S);
-    RowOut o;
-    o.norm = 1.0;
-    double G = P, r = 0.0, loss, ln_share = 0.0;
-    const bool empty = !(S > 0.0) && !bad;
+    m.P = warp_sum_f64(m.P); m.lp = warp_sum_f64(m.lp); m.z = warp_sum_f64(m.z);
+    const double r = a.mode == DPPO_DISTILL_REST && 1.0 - m.P > kLeastRest ? 1.0 - m.P : 0.0;
+    m.r = (float)r;
+    m.norm = 1.0f;
     if (a.mode == DPPO_DISTILL_NORMALIZED) {
-        o.norm = P > 0.0 ? inv64(P) : 0.0;
-        G = P > 0.0 ? 1.0 : P;                     // a NaN stays one
-        loss = P > 0.0 ? B * o.norm - log64(P) + l : P;
+        m.norm = m.P > 0.0 ? (float)inv64(m.P) : 0.0f;
+        m.G = m.P > 0.0 ? 1.0f : (float)m.P;       // a NaN stays one
     } else {
-        loss = P != 0.0 ? B + P * l : 0.0;
-        if (a.mode == DPPO_DISTILL_REST) {
-            r = 1.0 - P > kLeastRest ? 1.0 - P : 0.0;
-            G = P + r;
-            if (r > 0.0) {
-                ln_share = rest.S > 0.0f ? log64(r) - (log64((double)rest.S) + down) + l : INFINITY;
-                loss += r * ln_share;
-            }
-        }
+        m.G = (float)(m.P + r);
     }
-    if (empty) loss = P > 0.0 ? INFINITY : P != 0.0 ? P : 0.0;
-    const float nan = __int_as_float(0x7fffffff);
-    o.m = bad ? nan : empty ? -INFINITY : M;
-    o.S = (float)S; o.G = (float)G;
-    // a large share goes into the entries' exponents: times an exponential that underflows relative to M it would be lost
-    if (!(r > 0.0)) {
-        o.share = 0.0f;
-    } else if (!(rest.S > 0.0f)) {
-        o.share = INFINITY;
-    } else if (ln_share > 2.8) {
-        const double share = ln_share < 69.0 ? exp64(ln_share) - G : 0.0;
-        o.share = ln_share >= 69.0 ? (float)(-1.4426950408889634 * ln_share)
-                  : share > 16.0 ? (float)(-1.4426950408889634 * log64(share)) : (float)r * (float)S / Sr;
-    } else {
-        o.share = (float)r * (float)S / Sr;
-    }
-    o.to_rest = rest.S > 0.0f ? (float)G * shrink / (float)S - (float)r / rest.S : 0.0f;
-    if (bad) o.S = o.G = o.share = o.to_rest = nan;
-    o.loss = bad ? nan : e.bad ? 0.0f : (float)loss;
-    o.lse = bad ? nan : empty ? -INFINITY : (float)((double)M * a.inv_tau + l);
-    o.zero = e.bad || empty;
-    if (e.bad) o.G = o.share = o.to_rest = 0.0f;
-    if (empty) o.to_rest = 0.0f;
-    return o;
+    return m;
 }
-__device__ __forceinline__ void row_write(const Args& a, long long t, const RowOut& o, bool bad_id, int lane) {
+
+// The row's sums (in every lane), in a few f32 operations: the gradient waits for nothing else.
+struct RowSums {
+    float M, S, Sr;                                // the largest entry; sums relative to it: all, unlisted
+    float to_rest;                                 // gradient of an unlisted entry: its exponential relative to the unlisted entries' maximum times this
+    bool bad, empty;
+};
+// rest: the row without its listed entries.  The exponentials of the listed ones go to ej.
+template <int kPer> __device__ __forceinline__ RowSums row_sums(const Args& a, const Listed<kPer>& e, const Mass& m, const Part& rest, float (&ej)[kPer]) {
+    RowSums s;
+    s.bad = rest.bad || m.bad;
+    s.M = fmaxf(rest.m, m.zmax);
+    const float shrink = rest.S > 0.0f ? ex2((rest.m - s.M) * a.c) : 0.0f;
+    s.Sr = rest.S * shrink;
+    float Sl = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        ej[i] = e.id[i] >= 0 ? ex2((e.z[i] - s.M) * a.c) : 0.0f;
+        if (e.first[i]) Sl += ej[i];
+    }
+    s.S = s.Sr + warp_sum(Sl);
+    s.empty = !(s.S > 0.0f) && !s.bad;
+    const float nan = __int_as_float(0x7fffffff);
+    if (s.bad) s.S = nan;
+    s.to_rest = s.bad ? nan : rest.S > 0.0f && !e.bad ? m.G * shrink / s.S - m.r / rest.S : 0.0f;
+    return s;
+}
+
+// What is written of a row, by a warp.  share: r / sigma, or -log2(r / sigma - G) where that is above 16: a large share goes into the entries'
+// exponents, since times an exponential that underflows relative to M it would be lost.
+__device__ __forceinline__ void row_write(const Args& a, long long t, const Mass& m, const RowSums& s, const Part& rest, bool bad_id, int lane) {
+    const float nan = __int_as_float(0x7fffffff);
+    const bool shared = m.r > 0.0f && rest.S > 0.0f;
+    // two 64-bit logarithms at once, on two lanes: of S, and of r S / (the unlisted sum relative to its own maximum, which does not underflow)
+    // or of P
+    const double second = shared ? (1.0 - m.P) * (double)s.S * inv64((double)rest.S) : m.P;
+    const double logs = log64(lane == 0 ? (double)s.S : second);
+    const double l = __shfl_sync(kAll, logs, 0), l2 = __shfl_sync(kAll, logs, 1);
+    const double cross = m.lp - (m.z + m.P * ((double)m.zmax - (double)s.M)) * a.inv_tau;      // sum of p (ln p - (z - M) / tau)
+    double loss = a.mode == DPPO_DISTILL_NORMALIZED ? (m.P > 0.0 ? cross * inv64(m.P) - l2 + l : m.P) : (m.P != 0.0 ? cross + m.P * l : 0.0);
+    float share = 0.0f;
+    if (shared) {
+        const double ln_share = l2 + ((double)s.M - (double)rest.m) * a.inv_tau;
+        loss += (1.0 - m.P) * ln_share;
+        share = ln_share < 69.0 ? m.r * s.S / s.Sr : (float)(-1.4426950408889634 * ln_share);
+        if (ln_share > 2.8 && ln_share < 69.0) {
+            const double over = exp64(ln_share) - (double)m.G;
+            if (over > 16.0) share = (float)(-1.4426950408889634 * log64(over));
+        }
+    } else if (m.r > 0.0f) {
+        share = INFINITY;
+        loss = INFINITY;
+    }
     if (lane != 0) return;
-    if (a.loss) a.loss[t] = o.loss;
-    if (a.lse) a.lse[t] = o.lse;
-    if (a.stats) a.stats[t] = make_float4(o.m, o.S, o.G, o.share);
+    if (s.empty) loss = m.P > 0.0 ? INFINITY : m.P != 0.0 ? m.P : 0.0;
+    if (a.loss) a.loss[t] = s.bad ? nan : bad_id ? 0.0f : (float)loss;
+    if (a.lse) a.lse[t] = s.bad ? nan : s.empty ? -INFINITY : (float)((double)s.M * a.inv_tau + l);
+    if (a.stats) {
+        const bool zero = bad_id && !s.bad;
+        a.stats[t] = s.bad ? make_float4(nan, nan, nan, nan) : make_float4(s.empty ? -INFINITY : s.M, s.S, zero ? 0.0f : m.G, zero ? 0.0f : share);
+    }
     if (bad_id) set_status(a.status, DPPO_STATUS_BAD_TARGET);
 }
 
@@ -302,6 +327,7 @@ distill_forward_kernel(const Args a) {
         if (lane == 0) sh.part[warp] = p;
     }
     Part hot = part_none();                                        // the unlisted entries of the marked vectors
+    Mass mass = {};
     if (warp == kWarps) {
         listed_probs<kPer>(lp, e);
         listed_logits<kBf16, kPer>(row, e);
@@ -339,6 +365,7 @@ distill_forward_kernel(const Args a) {
                 if (!(out[i] >> j & 1u)) part_one(hot, f[j], a.c);
         }
         listed_first<kPer>(a, lane, e, false);
+        mass = listed_mass<kPer>(a, e, lp);
     }
     __syncthreads();
     Part rest = part_none();
@@ -372,8 +399,8 @@ distill_forward_kernel(const Args a) {
     let_next_start();
     if (warp == kWarps) {
         float ej[kPer];
-        const RowOut o = row_finish<kPer>(a, e, lp, rest, ej);
-        row_write(a, t, o, e.bad, lane);
+        const RowSums sums = row_sums<kPer>(a, e, mass, rest, ej);
+        row_write(a, t, mass, sums, rest, e.bad, lane);
     }
 }
 
@@ -387,11 +414,12 @@ template <int kThreads> struct StepShared {
 
 // The gradient of the listed entries that `here` (a predicate of the vector index) accepts, after everything else of their row.
 template <bool kBf16, int kPer, class F>
-__device__ __forceinline__ void write_listed(char* out, const Listed<kPer>& e, const float (&ej)[kPer], const RowOut& o, float wt, F here) {
+__device__ __forceinline__ void write_listed(char* out, const Listed<kPer>& e, const float (&ej)[kPer], const Mass& m, const RowSums& s, float wt, F here) {
+    const float inv = 1.0f / s.S;
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
         if (e.first[i] && here(e.id[i] >> (kBf16 ? 3 : 2)))
-            Elems<kBf16>::store1(out, e.id[i], o.zero ? 0.0f : wt * (float)((double)(ej[i] / o.S) * (double)o.G - e.p[i] * o.norm));
+            Elems<kBf16>::store1(out, e.id[i], s.bad ? s.S : s.empty || e.bad ? 0.0f : wt * (float)((double)(ej[i] * inv) * (double)m.G - e.p[i] * (double)m.norm));
 }
 // p of entries listed twice, added up; listed_first has to run after the loss has been formed from the single ones.
 template <int kPer> __device__ __forceinline__ void listed_sums(const Args& a, int lane, Listed<kPer>& e) { listed_first<kPer>(a, lane, e, true); }
@@ -416,6 +444,7 @@ distill_step_kernel(const Args a, int log2C, int vec_per_cta) {
 
     Listed<kPer> e;
     float lp[kPer];
+    Mass mass = {};
     float wt = 0.0f;
     if (warp < kWarps) {                                           // the slice: every thread's own vectors, then everybody's
         const uint32_t dst = (uint32_t)__cvta_generic_to_shared(slice);
@@ -429,6 +458,7 @@ distill_step_kernel(const Args a, int log2C, int vec_per_cta) {
         listed_logits<kBf16, kPer>(row, e);
         listed_probs<kPer>(lp, e);
         listed_first<kPer>(a, lane, e, false);
+        mass = listed_mass<kPer>(a, e, lp);
     }
     __syncthreads();
     if (warp == kWarps) {
@@ -536,15 +566,15 @@ distill_step_kernel(const Args a, int log2C, int vec_per_cta) {
         __syncwarp();
     }
     if (log2C > 0) cl.sync();                                      // every CTA's part is in its shared memory
-    RowOut o = {};
+    RowSums sums = {};
+    Part p = part_none();
     float ej[kPer];
     if (warp == kWarps) {
-        Part p = lane < (1 << log2C) ? (log2C > 0 ? *cl.map_shared_rank(&sh.part, lane) : sh.part) : part_none();
+        p = lane < (1 << log2C) ? (log2C > 0 ? *cl.map_shared_rank(&sh.part, lane) : sh.part) : part_none();
         p = part_warp(p, a.c);
-        o = row_finish<kPer>(a, e, lp, p, ej);
+        sums = row_sums<kPer>(a, e, mass, p, ej);
         // to_rest is relative to the row's unlisted maximum, what is kept to this slice's
-        if (lane == 0) sh.scale = wt * o.to_rest * (p.m > m ? ex2((m - p.m) * a.c) : 1.0f) * back;
-        if (rank == 0) row_write(a, t, o, e.bad, lane);
+        if (lane == 0) sh.scale = wt * sums.to_rest * (p.m > m ? ex2((m - p.m) * a.c) : 1.0f) * back;
         __syncwarp();
     }
     if (log2C > 0) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // the parts have been read
@@ -569,17 +599,20 @@ distill_step_kernel(const Args a, int log2C, int vec_per_cta) {
         }
         if (last && tail0 + tid < a.V) Elems<kBf16>::store1(out, tail0 + tid, scale * etail);
     } else {
+        if (rank == 0) row_write(a, t, mass, sums, p, e.bad, lane);
+        __syncwarp();
         listed_sums<kPer>(a, lane, e);
     }
     __syncthreads();                                               // the listed entries' places have been written
     let_next_start();
-    if (warp == kWarps) write_listed<kBf16, kPer>(out, e, ej, o, wt, [&](int v) { return v >= nvec ? last : v >= v0 && v < v0 + nv; });
+    if (warp == kWarps) write_listed<kBf16, kPer>(out, e, ej, mass, sums, wt, [&](int v) { return v >= nvec ? last : v >= v0 && v < v0 + nv; });
     __syncwarp();
     if (log2C > 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // ---- short rows: a warp per row, with or without the gradient --------------------------------------------------
-// The row goes through the warp's shared memory once, where its listed entries are read and masked, and stays in registers.
+// The row goes through the warp's shared memory once, where its listed entries are read and masked, and stays in registers.  (Several rows
+// per warp, with their 64-bit scalars one row per lane at the end, save instructions and lose as much to their registers.)
 template <bool kBf16, int kVecs, int kTeams, bool kGradient, int kPer>
 __global__ void __launch_bounds__(32 * kTeams)
 distill_warp_kernel(const Args a) {
@@ -654,11 +687,12 @@ distill_warp_kernel(const Args a) {
     Part p = {m, warp_sum(s0 + s1 + xt) * back, bad ? 1 : 0};
     if (!(p.S > 0.0f)) p.m = kLowest;
     float ej[kPer];
-    const RowOut o = row_finish<kPer>(a, e, lp, p, ej);
-    row_write(a, t, o, e.bad, lane);
+    const Mass mass = listed_mass<kPer>(a, e, lp);
+    const RowSums sums = row_sums<kPer>(a, e, mass, p, ej);
+    row_write(a, t, mass, sums, p, e.bad, lane);
     if constexpr (kGradient) {
         char* out = a.dlogits + t * a.row_bytes;
-        const float scale = wt * o.to_rest * back;
+        const float scale = wt * sums.to_rest * back;
         const f32x2 s2 = pair_of(scale, scale);
 #pragma unroll
         for (int u = 0; u < kVecs; ++u) {
@@ -671,17 +705,19 @@ distill_warp_kernel(const Args a) {
         if (tail < a.V) Elems<kBf16>::store1(out, tail, scale * xt);
         listed_sums<kPer>(a, lane, e);
         __syncwarp();
-        write_listed<kBf16, kPer>(out, e, ej, o, wt, [](int) { return true; });
+        write_listed<kBf16, kPer>(out, e, ej, mass, sums, wt, [](int) { return true; });
     }
 }
 
 // ---- gradient from the forward's statistics ---------------------------------------------------------------
+// A warp per row (kThreads = 32, kTeams rows in a CTA), or kThreads threads per piece of a row and a warp for what is listed in it.
 template <bool kBf16, int kThreads, int kTeams, int kUnroll, int kPer>
-__global__ void __launch_bounds__(kThreads * kTeams)
+__global__ void __launch_bounds__(kThreads == 32 ? 32 * kTeams : kThreads + 32)
 distill_backward_kernel(const Args a) {
     constexpr int kPerVec = Elems<kBf16>::kPerVec, kLog2 = kBf16 ? 3 : 2;
     const int team = kTeams == 1 ? 0 : threadIdx.x / kThreads;
     const int tid = kTeams == 1 ? threadIdx.x : threadIdx.x % kThreads, lane = tid & 31;
+    const bool lister = kThreads == 32 || tid >= kThreads, sweeper = tid < kThreads;
     enter_kernel();
     const long long T = rows_of(a);
     const long long item = (long long)blockIdx.x * kTeams + team;
@@ -696,12 +732,17 @@ distill_backward_kernel(const Args a) {
     const float4 st = a.stats_in[t];
     const float wt = (float)((a.weight ? (double)a.weight[t] : 1.0) * a.inv_tau);
 
-    // what is listed in this piece: its ids now, the rest when the sweep is done (in place: its logits before anything is written)
+    // what is listed in this piece: its ids and logits (in place: before anything is written)
     Listed<kPer> e;
     float lp[kPer];
-    if (tid < 32) {
+    bool any = false;
+    auto here = [&](int i) { const int v = e.id[i] >> kLog2; return e.id[i] >= 0 && (v >= nvec ? last : v >= v0 && v < v1); };
+    if (lister) {
         listed_ids<kPer>(a, t, lane, e, lp);
-        if (a.in_place) listed_logits<kBf16, kPer>(row, e);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) any = any || here(i);
+        any = __any_sync(kAll, any);
+        if (any) listed_logits<kBf16, kPer>(row, e);
     }
     if (a.in_place) { if constexpr (kThreads == 32) __syncwarp(); else __syncthreads(); }
 
@@ -748,42 +789,40 @@ distill_backward_kernel(const Args a) {
             }
         }
     };
-    if (zero) {
+    if (!sweeper) {
+    } else if (zero) {
         for (int i = v0 + tid; i < v1; i += kThreads) __stcs(reinterpret_cast<uint4*>(out) + i, make_uint4(0u, 0u, 0u, 0u));
     } else if (quick) {
         sweep(std::true_type());
     } else {
         sweep(std::false_type());
     }
-    if (last && tail0 + tid < a.V) {
+    if (sweeper && last && tail0 + tid < a.V) {
         const float z = Elems<kBf16>::load1(row, tail0 + tid);
         Elems<kBf16>::store1(out, tail0 + tid, zero ? 0.0f : coef * ex2(fmaf(z - st.x, a.c, far ? -st.w : 0.0f)));
     }
+    double norm = 1.0;
+    if (lister && any) {
+        listed_probs<kPer>(lp, e);
+        if (a.mode == DPPO_DISTILL_NORMALIZED) {
+            double P = 0.0;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) P += e.p[i];
+            P = warp_sum_f64(P);
+            norm = P > 0.0 ? inv64(P) : 0.0;
+        }
+        listed_first<kPer>(a, lane, e, true);
+    }
     if constexpr (kThreads == 32) __syncwarp(); else __syncthreads();          // the listed entries' places have been written
-    if (tid >= 32) return;
+    if (!lister) return;
     if (e.bad) {
         if (lane == 0 && chunk == 0) set_status(a.status, DPPO_STATUS_BAD_TARGET);
         return;                                                    // G = 0: the row is zero
     }
-    bool here = false;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) here = here || (e.id[i] >= 0 && ((e.id[i] >> kLog2) >= nvec ? last : (e.id[i] >> kLog2) >= v0 && (e.id[i] >> kLog2) < v1));
-    if (empty || !__any_sync(kAll, here)) return;
-    if (!a.in_place) listed_logits<kBf16, kPer>(row, e);
-    listed_probs<kPer>(lp, e);
-    double norm = 1.0;
-    if (a.mode == DPPO_DISTILL_NORMALIZED) {
-        double P = 0.0;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) P += e.p[i];
-        P = warp_sum_f64(P);
-        norm = P > 0.0 ? inv64(P) : 0.0;
-    }
-    listed_first<kPer>(a, lane, e, true);
+    if (empty || !any) return;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        const int v = e.id[i] >> kLog2;
-        if (!e.first[i] || !(v >= nvec ? last : v >= v0 && v < v1)) continue;
+        if (!e.first[i] || !here(i)) continue;
         const float s = ex2((e.z[i] - st.x) * a.c) * inv;
         Elems<kBf16>::store1(out, e.id[i], wt * (float)((double)s * (double)st.z - e.p[i] * norm));
     }
@@ -813,7 +852,7 @@ template <bool kBf16, int kPer> static int run_fwd(const Args& a, cudaStream_t s
 }
 
 template <bool kBf16, int kVecs, bool kGradient, int kPer> static int launch_warp(const Args& a, cudaStream_t s) {
-    constexpr int kTeams = 4;
+    constexpr int kTeams = 2;
     return launch_after("distill_topk launch", distill_warp_kernel<kBf16, kVecs, kTeams, kGradient, kPer>, (a.T_max + kTeams - 1) / kTeams, 32 * kTeams, 0, s, 1, a);
 }
 template <bool kBf16, bool kGradient, int kPer> static int run_warp(const Args& a, cudaStream_t s) {
@@ -854,16 +893,22 @@ template <bool kBf16, int kPer> static int run_step(const Args& a, cudaStream_t 
 template <bool kBf16, int kThreads, int kTeams, int kUnroll, int kPer> static int launch_bwd(const Args& a, cudaStream_t s) {
     const long long ctas = (a.T_max * a.chunks + kTeams - 1) / kTeams;
     if (ctas > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "distill_topk_backward: T_max=%lld needs too large a grid", a.T_max);
-    return launch_after("distill_topk_backward launch", distill_backward_kernel<kBf16, kThreads, kTeams, kUnroll, kPer>, ctas, kThreads * kTeams, 0, s, 1, a);
+    return launch_after("distill_topk_backward launch", distill_backward_kernel<kBf16, kThreads, kTeams, kUnroll, kPer>, ctas, kThreads == 32 ? 32 * kTeams : kThreads + 32, 0, s, 1, a);
 }
 
 template <bool kBf16, int kPer> static int run_bwd(Args a, cudaStream_t s) {
     const int nvec = a.V >> (kBf16 ? 3 : 2);
     a.chunks = 1; a.chunk_vecs = nvec;
     if (nvec <= 320) return launch_bwd<kBf16, 32, 4, 4, kPer>(a, s);
-    a.chunk_vecs = 512;
-    a.chunks = (nvec + 511) / 512;
-    return launch_bwd<kBf16, 128, 1, 4, kPer>(a, s);
+    // Pieces long enough that the listed entries' chain of loads (id, logit) is over before the sweep is: 8,192 x 151,936 bf16 in 512
+    // vectors by 128 threads 957 us, in 4,096 by 256 768; 2,003 x 50,304 f32 161 and 133.  Where there are too few of those to
+    // go round, shorter ones (64 x 151,936: 9.9 us in 4,096, 8.2 in 1,024).  Rounds of four loads: eight take 1,070 and 138.
+    const long long share = a.T_max * nvec / (8 * sm_count());
+    const int most = share >= 4096 ? 4096 : share >= 2048 ? 2048 : 1024;
+    a.chunks = (nvec + most - 1) / most;
+    a.chunk_vecs = (nvec + a.chunks - 1) / a.chunks;
+    if (most == 1024) return launch_bwd<kBf16, 128, 1, 4, kPer>(a, s);
+    return launch_bwd<kBf16, 256, 1, 4, kPer>(a, s);
 }
 
 // Checks that both calls make; 0 or the error.
