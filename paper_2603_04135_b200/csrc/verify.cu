@@ -8,7 +8,8 @@
 // Two kernels.  The first reduces every row of both policies to {m, S} (one read of all logits: what bounds the call); the second, a
 // cluster of CTAs per sequence, finds the first rejection (a warp, 32 drafts at a time) and races over that one row.
 //
-// Tokens are exact: f32 decides a race only where no second entry's upper bound reaches the winner's lower bound; otherwise
+// The race: an entry counts only if its p / e, by one fma and a logarithm, comes near the best lower bound among the
+// first entries of its CTA, which a few dozen do; only those look at the draft's row, all at once.  Tokens are exact: f32 decides a race only where no second entry's upper bound reaches the winner's lower bound; otherwise
 // the entries within reach are compared in 64 bits, ties to the lower index.
 #include <cooperative_groups.h>
 
@@ -24,6 +25,7 @@ namespace verify {
 using namespace sweep;
 
 constexpr int kMaxCluster = 8;
+constexpr int kCand = 512;
 constexpr uint32_t kAll = 0xffffffffu;
 // Relative error of an f32 probability: 3 roundings and the constant in an exponent of up to 100, the exponential, the sum.
 constexpr float kEps = 1.0f / 65536.0f;
@@ -176,7 +178,10 @@ struct PickShared {
     Field f;
     float2 sp, sq;
     long long row;                        // of the next token
-    int base, n, n_acc, state;            // state: 0 go on, 1 the sequence has no next token, 2 nothing may be written
+    int bound, n_cand;                    // bits of the largest lower bound of the CTA's first entries; entries that come near it
+    float z[kCand], e[kCand];
+    int at[kCand];
+    int n_acc, state;                     // state: 0 go on, 1 the sequence has no next token, 2 nothing may be written
 };
 
 template <int kThreads> __device__ __forceinline__ Race race_cta(Race r, PickShared& sh) {
@@ -194,27 +199,58 @@ template <int kThreads> __device__ __forceinline__ Exact exact_cta(Exact r, Pick
     return exact_warp((threadIdx.x & 31) < kThreads / 32 ? sh.exact[threadIdx.x & 31] : Exact{0.0, 0x7fffffff});
 }
 
-// Calls f(z_p, z_q, e, index) for the entries of vectors [v0, v1) that this thread owns, and for the tail's.
-template <bool kBf16, int kThreads, class F>
-__device__ __forceinline__ void for_field(const Field& w, int v0, int v1, int tail0, int V, F f) {
+// Calls f(z_p, e, index) for those entries of vectors [v0, v1), and of the row's tail, whose log2(p / e) is not below `bound` by more than a
+// margin (far above the errors of its f32 estimate; p relative to its row's sum).  kUnroll vectors' loads under way together.
+template <bool kBf16, int kThreads, int kUnroll, class F>
+__device__ __forceinline__ void for_field(const Field& w, float ct, int v0, int v1, int tail0, int V, float bound, F f) {
     constexpr int kPer = Elems<kBf16>::kPerVec;
+    constexpr float kMargin = 0.01f;
     const int tid = threadIdx.x;
+    auto one = [&](float z, float e, int at) {
+        float l;
+        asm("lg2.approx.f32 %0, %1;" : "=f"(l) : "f"(e));
+        if (fmaf(z - w.mp, ct, -l) > bound - kMargin) f(z, e, at);
+    };
 #pragma unroll 1
-    for (int i = v0 + tid; i < v1; i += kThreads) {
-        float zp[kPer], zq[kPer], e[kPer];
-        const uint4 vp = load_vec(w.p + (size_t)i * 16);
-        const uint4 vq = w.q ? load_vec(w.q + (size_t)i * 16) : masked_vec<kBf16>();
+    for (int i0 = v0 + tid; i0 < v1; i0 += kUnroll * kThreads) {
+        uint4 vp[kUnroll], ve[kUnroll][kPer / 4];
 #pragma unroll
-        for (int j = 0; j < kPer; j += 4) {
-            const uint4 ve = load_vec(w.e + (size_t)i * kPer + j);
-            e[j] = __uint_as_float(ve.x); e[j + 1] = __uint_as_float(ve.y); e[j + 2] = __uint_as_float(ve.z); e[j + 3] = __uint_as_float(ve.w);
+        for (int u = 0; u < kUnroll; ++u) {
+            const int i = i0 + u * kThreads;
+            const bool in = i < v1;
+            vp[u] = in ? load_vec(w.p + (size_t)i * 16) : masked_vec<kBf16>();
+#pragma unroll
+            for (int j = 0; j < kPer / 4; ++j) ve[u][j] = in ? load_vec(w.e + (size_t)i * kPer + 4 * j) : make_uint4(0x3f800000u, 0x3f800000u, 0x3f800000u, 0x3f800000u);
         }
-        Elems<kBf16>::unpack(vp, zp);
-        Elems<kBf16>::unpack(vq, zq);
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) f(zp[j], zq[j], e[j], i * kPer + j);
+        for (int u = 0; u < kUnroll; ++u) {
+            float zp[kPer];
+            Elems<kBf16>::unpack(vp[u], zp);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const uint32_t x[4] = {ve[u][j / 4].x, ve[u][j / 4].y, ve[u][j / 4].z, ve[u][j / 4].w};
+                one(zp[j], __uint_as_float(x[j & 3]), (i0 + u * kThreads) * kPer + j);
+            }
+        }
     }
-    if (tail0 + tid < V) f(Elems<kBf16>::load1(w.p, tail0 + tid), w.q ? Elems<kBf16>::load1(w.q, tail0 + tid) : -INFINITY, w.e[tail0 + tid], tail0 + tid);
+    if (tail0 + tid < V) one(Elems<kBf16>::load1(w.p, tail0 + tid), w.e[tail0 + tid], tail0 + tid);
+}
+// f(z_p, z_q, e, index) for every entry of this thread's vector i, if it is one.
+template <bool kBf16, class F> __device__ __forceinline__ void for_vector(const Field& w, int i, int v1, F f) {
+    constexpr int kPer = Elems<kBf16>::kPerVec;
+    if (i >= v1) return;
+    float zp[kPer], zq[kPer];
+    uint4 ve[kPer / 4];
+    const uint4 vp = load_vec(w.p + (size_t)i * 16), vq = w.q ? load_vec(w.q + (size_t)i * 16) : masked_vec<kBf16>();
+#pragma unroll
+    for (int j = 0; j < kPer / 4; ++j) ve[j] = load_vec(w.e + (size_t)i * kPer + 4 * j);
+    Elems<kBf16>::unpack(vp, zp);
+    Elems<kBf16>::unpack(vq, zq);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const uint32_t x[4] = {ve[j / 4].x, ve[j / 4].y, ve[j / 4].z, ve[j / 4].w};
+        f(zp[j], zq[j], __uint_as_float(x[j & 3]), i * kPer + j);
+    }
 }
 
 template <bool kBf16, int kThreads, bool kCluster> __global__ void __launch_bounds__(kThreads) verify_pick_kernel(const Args a) {
@@ -226,6 +262,15 @@ template <bool kBf16, int kThreads, bool kCluster> __global__ void __launch_boun
     if constexpr (kCluster) { C = cg::this_cluster().num_blocks(); rank = cg::this_cluster().block_rank(); }
     const int log2C = 31 - __clz((int)C);
     const int b = (int)(blockIdx.x >> log2C);
+
+    const int nvec = a.V >> kLog2;
+    const int v0 = (int)((long long)nvec * rank >> log2C), v1 = (int)((long long)nvec * (rank + 1) >> log2C);
+    // the noise does not depend on where the sequence stops: on its way to L2 while that is found
+    {
+        const char* e = reinterpret_cast<const char*>(a.noise + (size_t)b * a.noise_stride);
+        const long long lo = (long long)v0 << kLog2 << 2, hi = (long long)v1 << kLog2 << 2;
+        for (long long at = lo + 128ll * tid; at < hi; at += 128ll * kThreads) asm volatile("prefetch.global.L2 [%0];" :: "l"(e + at));
+    }
 
     // ---- the first rejection, by one warp of every CTA; the first CTA writes
     if (warp == 0) {
@@ -308,13 +353,13 @@ template <bool kBf16, int kThreads, bool kCluster> __global__ void __launch_boun
 
     // ---- the race
     Field f = sh.f;
-    const int nvec = a.V >> kLog2;
-    const int v0 = (int)((long long)nvec * rank >> log2C), v1 = (int)((long long)nvec * (rank + 1) >> log2C);
     const int tail0 = rank == C - 1 ? nvec << kLog2 : a.V;
     int won = -1;
+    const double ln_sum = log64((double)sh.sp.y);
 #pragma unroll 1
     for (int pass = 0; pass < 2 && won < 0; ++pass) {
         Race r = {0.0f, 0.0f, 0.0f, 0x7fffffff};
+        float z_best = 0.0f;
         auto bounds = [&](float zp, float zq, float e, int at, float& hi, float& lo) {
             const float p = ex2((zp - f.mp) * a.ct) * f.ip;
             float w = p, t = p;
@@ -327,13 +372,32 @@ template <bool kBf16, int kThreads, bool kCluster> __global__ void __launch_boun
             hi = fmaf(t, kEps, w) * inv;
             lo = fmaf(t, -kEps, w) * inv;
         };
-        for_field<kBf16, kThreads>(f, v0, v1, tail0, a.V, [&](float zp, float zq, float e, int at) {
+        auto enter = [&](float zp, float zq, float e, int at) {
             float hi, lo;
             bounds(zp, zq, e, at, hi, lo);
-            if (hi > r.hi) { r.second = r.hi; r.hi = hi; r.at = at; }
+            if (hi > r.hi) { r.second = r.hi; r.hi = hi; r.at = at; z_best = zp; }
             else if (hi > r.second) r.second = hi;
             if (lo > r.lo) r.lo = lo;
+        };
+        auto draft_at = [&](int at) { return f.q ? Elems<kBf16>::load1(f.q, at) : -INFINITY; };
+        auto log_bound = [&](float lo) { return lo > 0.0f ? __log2f(lo) + __log2f(sh.sp.y) : -INFINITY; };
+        if (tid == 0) { sh.bound = 0; sh.n_cand = 0; }
+        __syncthreads();
+        for_vector<kBf16>(f, v0 + tid, v1, enter);                 // every thread's first vector
+        if (__any_sync(kAll, r.lo > 0.0f)) {                       // positive floats order as integers do
+            const float best = warp_max_f32(r.lo);
+            if (lane == 0) atomicMax(&sh.bound, __float_as_int(best));
+        }
+        __syncthreads();
+        for_field<kBf16, kThreads, 2>(f, a.ct, v0 + kThreads, v1, tail0, a.V, log_bound(__int_as_float(sh.bound)), [&](float zp, float e, int at) {
+            const int slot = atomicAdd(&sh.n_cand, 1);
+            if (slot < kCand) { sh.z[slot] = zp; sh.e[slot] = e; sh.at[slot] = at; }
+            else enter(zp, draft_at(at), e, at);                   // more than there is room for
         });
+        __syncthreads();
+        for (int i = tid; i < min(sh.n_cand, kCand); i += kThreads) enter(sh.z[i], draft_at(sh.at[i]), sh.e[i], sh.at[i]);
+        const float z_mine = z_best;
+        const int at_mine = r.at;
         r = race_cta<kThreads>(r, sh);
         if constexpr (kCluster) {
             cg::cluster_group cl = cg::this_cluster();
@@ -342,16 +406,25 @@ template <bool kBf16, int kThreads, bool kCluster> __global__ void __launch_boun
             r = race_warp(lane < (int)C ? *cl.map_shared_rank(&sh.mine, lane) : Race{0.0f, 0.0f, 0.0f, 0x7fffffff});
             cl.sync();
         }
-        if (r.lo > 0.0f && r.second < r.lo && r.hi < INFINITY) { won = r.at; break; }
+        if (r.lo > 0.0f && r.second < r.lo && r.hi < INFINITY) {
+            won = r.at;
+            if (at_mine == won) {                                  // one thread of the cluster
+                a.tokens[sh.row] = won;
+                a.logp[sh.row] = (float)(((double)z_mine - (double)sh.sp.x) * a.inv_tau_t - ln_sum);
+            }
+            return;
+        }
         if (r.hi > 0.0f) {                                         // in 64 bits, over the entries within reach
             const double ip = 1.0 / (double)sh.sp.y, iq = f.q ? 1.0 / (double)sh.sq.y : 0.0;
             Exact x = {0.0, 0x7fffffff};
-            for_field<kBf16, kThreads>(f, v0, v1, tail0, a.V, [&](float zp, float zq, float e, int at) {
+            const float bound = log_bound(r.lo);
+            for_field<kBf16, kThreads, 1>(f, a.ct, v0, v1, tail0, a.V, bound, [&](float zp, float e, int at) {
                 float hi, lo;
+                const float zq = draft_at(at);
                 bounds(zp, zq, e, at, hi, lo);
                 if (!(hi >= r.lo) || !(hi > 0.0f) || !(zp > -INFINITY)) return;
                 double w = exp64(((double)zp - (double)f.mp) * a.inv_tau_t) * ip;
-                if (f.q && zq > -INFINITY) w -= exp64(((double)zq - (double)f.mq) * a.inv_tau_d) * iq;
+                if (zq > -INFINITY) w -= exp64(((double)zq - (double)f.mq) * a.inv_tau_d) * iq;
                 if (w > 0.0) x = exact_join({w / (double)e, at}, x);
             });
             x = exact_cta<kThreads>(x, sh);
@@ -371,7 +444,7 @@ template <bool kBf16, int kThreads, bool kCluster> __global__ void __launch_boun
             a.tokens[sh.row] = -1; a.logp[sh.row] = __int_as_float(0x7fffffff);
         } else {
             a.tokens[sh.row] = won;
-            a.logp[sh.row] = (float)(((double)Elems<kBf16>::load1(f.p, won) - (double)sh.sp.x) * a.inv_tau_t - log64((double)sh.sp.y));
+            a.logp[sh.row] = (float)(((double)Elems<kBf16>::load1(f.p, won) - (double)sh.sp.x) * a.inv_tau_t - ln_sum);
         }
     }
 }
@@ -380,20 +453,25 @@ template <bool kBf16, int kThreads, bool kCluster> __global__ void __launch_boun
 template <bool kBf16> static int run(const Args& a, cudaStream_t s) {
     const int nvec = a.V >> (kBf16 ? 3 : 2);
     const long long sms = sm_count(), rows = a.T_max + a.n_seqs + (a.draft ? a.T_max : 0);
+    // Rows: a warp each up to 4 KB; a CTA each where they fill the SMs twice (1,414 x 151,936 bf16: 256 threads 71 us, 128 80; 4,096 x 8,003 f32
+    // 512 threads 36.6, 256 37.2, 128 41.4); else a cluster (9 x 151,936: eight CTAs of 256 threads 5.0 us, four 5.9, one of 512 8.1).
     int rc, C = 1;
     if (nvec > 4096)
         while (C < kMaxCluster && rows * C < 2 * sms) C *= 2;
     if (rows * C > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "verify_drafts: %lld rows need too large a grid", rows);
     if (nvec <= 256) rc = launch_after("verify_drafts launch", verify_rows_warp_kernel<kBf16, 4>, (rows + 3) / 4, 128, 0, s, 1, a, rows);
-    else if (C == 1) rc = launch_after("verify_drafts launch", verify_rows_kernel<kBf16, 128, false>, rows, 128, 0, s, 1, a);
-    else rc = launch_after("verify_drafts launch", verify_rows_kernel<kBf16, 256, true>, rows * C, 256, 0, s, C, a);
+    else if (C > 1) rc = launch_after("verify_drafts launch", verify_rows_kernel<kBf16, 256, true>, rows * C, 256, 0, s, C, a);
+    else if (nvec <= 1024) rc = launch_after("verify_drafts launch", verify_rows_kernel<kBf16, 128, false>, rows, 128, 0, s, 1, a);
+    else rc = launch_after("verify_drafts launch", verify_rows_kernel<kBf16, 256, false>, rows, 256, 0, s, 1, a);
     if (rc != DPPO_OK) return rc;
-    C = 1;
-    if (nvec > 512)
-        while (C < kMaxCluster && (long long)a.n_seqs * C < 2 * sms) C *= 2;
-    if ((long long)a.n_seqs * C > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "verify_drafts: too many sequences");
-    if (C == 1) return launch_after("verify_drafts launch", verify_pick_kernel<kBf16, 256, false>, a.n_seqs, 256, 0, s, 1, a);
-    return launch_after("verify_drafts launch", verify_pick_kernel<kBf16, 256, true>, (long long)a.n_seqs * C, 256, 0, s, C, a);
+    // The race: four CTAs per sequence, of 512 threads where each has an SM to itself (37 x 32,003 f32 47.9 us with the rows; eight 56.5, two 49.5;
+    // 128 x 151,936 bf16 109 with 256 threads, 139 with 512); eight for a few sequences (1: 16.3, four 19.0, sixteen 17.6), fewer for many.
+    C = nvec <= 512 || a.n_seqs > 4 * sms ? 1 : a.n_seqs > 2 * sms ? 2 : 16ll * a.n_seqs > sms ? 4 : 8;
+    const long long ctas = (long long)a.n_seqs * C;
+    if (ctas > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "verify_drafts: too many sequences");
+    if (C == 1) return launch_after("verify_drafts launch", verify_pick_kernel<kBf16, 256, false>, ctas, 256, 0, s, 1, a);
+    if (ctas <= sms) return launch_after("verify_drafts launch", verify_pick_kernel<kBf16, 512, true>, ctas, 512, 0, s, C, a);
+    return launch_after("verify_drafts launch", verify_pick_kernel<kBf16, 256, true>, ctas, 256, 0, s, C, a);
 }
 
 }  // namespace verify
