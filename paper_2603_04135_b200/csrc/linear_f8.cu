@@ -36,7 +36,7 @@ constexpr int kBK = 128;                  // codes of a block = of a stage
 constexpr int kTileM = 128;               // rows of the M side per CTA
 constexpr int kTileN = 256;               // most channels per tile of the pair kernel
 constexpr int kBytesA = kTileM * kBK;
-constexpr int kMaxStages = 9;             // + 2 accumulators + 1 < kSlots
+constexpr int kMaxStages = 6;             // + 2 accumulators + 1 < kSlots
 constexpr int kSlots = 16;                // blocks whose token scales are in shared memory
 constexpr int kEpiWarps = 8;              // pair kernel: two per TMEM lane quarter, half of the tile's channels each
 constexpr int kThreads = 128 + 32 * kEpiWarps;     // producer, MMA, watch and one idle warp before them
@@ -54,7 +54,7 @@ struct Args {
     int32_t* status;
     long long M_max, out_stride, xs_stride, ws_stride;
     int N, n_ksteps, out_bf16;
-    int tile_n;                           // pair kernel: channels per tile, 64, 128 or 256
+    int tile_n;                           // pair kernel: channels per tile, 128 or 256
     int vec_out;                          // out: base and rows on 16 bytes
     unsigned long long wait_limit_ns;
     int test_extra_tx;
@@ -135,25 +135,26 @@ template <bool kBf16> __device__ __forceinline__ void store_piece(const Args& a,
                      :: "r"(stage + (uint32_t)(lane * 64 + ((p ^ (lane >> 1 & 3)) * 16))), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
     }
     __syncwarp();
-    const int c = ch + (lane & 3) * kPer;
-    Out* out = reinterpret_cast<Out*>(a.out) + t0 * a.out_stride + c;
+    // consecutive lanes, consecutive channels; eight loads at a time before their stores
+    constexpr int kCh = 4 * kPer, kBatch = 8;
+    typedef typename std::conditional<kBf16, unsigned short, float>::type Bits;
+    Out* out = reinterpret_cast<Out*>(a.out) + t0 * a.out_stride + ch;
+#pragma unroll 1
+    for (int i0 = 0; i0 < kCh; i0 += kBatch) {
+        Bits v[kBatch];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int t = i * 8 + (lane >> 2);
-        uint4 v;
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                     : "r"(stage + (uint32_t)(t * 64 + (((lane & 3) ^ (t >> 1 & 3)) * 16))) : "memory");
-        if (t0 + t >= T) continue;
-        if (a.vec_out && c + kPer <= a.N) {
-            *reinterpret_cast<uint4*>(out + t * a.out_stride) = v;
-        } else {
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        for (int i = 0; i < kBatch; ++i) {
+            const int t = ((i0 + i) * 32 + lane) / kCh, c = lane % kCh;
+            const uint32_t at = stage + (uint32_t)(t * 64 + (((c / kPer) ^ (t >> 1 & 3)) * 16) + c % kPer * (int)sizeof(Out));
+            if constexpr (kBf16) asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v[i]) : "r"(at) : "memory");
+            else asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[i]) : "r"(at) : "memory");
+        }
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) {
-                if (c + e >= a.N) continue;
-                if constexpr (kBf16) out[t * a.out_stride + e] = __ushort_as_bfloat16((unsigned short)(w[e >> 1] >> (16 * (e & 1))));
-                else out[t * a.out_stride + e] = __uint_as_float(w[e]);
-            }
+        for (int i = 0; i < kBatch; ++i) {
+            const int t = ((i0 + i) * 32 + lane) / kCh, c = lane % kCh;
+            if (t0 + t >= T || ch + c >= a.N) continue;
+            if constexpr (kBf16) out[t * a.out_stride + c] = __ushort_as_bfloat16(v[i]);
+            else out[t * a.out_stride + c] = v[i];
         }
     }
 }
@@ -328,7 +329,8 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         // ------------------------------------------------------------------ epilogue (warps 4..11, both CTAs)
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         const int q = warp & 3, half = (warp - 4) >> 2;                  // TMEM lane quarter of this warp; which half of the channels
-        const int blocks = a.tile_n / 64, first = half * (a.tile_n / 2); // blocks of 32 channels, the first of them
+        const bool wide = a.tile_n == kTileN;                            // 128 channels per warp and token, or 64
+        const int blocks = wide ? 4 : 2, first = half * (a.tile_n / 2);  // blocks of 32 channels, the first of them
         const uint32_t stage = tiles + (uint32_t)kRingBytes + (uint32_t)((warp - 4) * kStageOut);
         uint32_t it = 0;
         int ch, tok;
@@ -352,7 +354,7 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             uint32_t v[2][32];
             handed_on();
             columns_load(v[0], lanes + (it & 1) * kTileN);
-            if (blocks > 1) columns_load(v[1], lanes + (it & 1) * kTileN + 32u);
+            columns_load(v[1], lanes + (it & 1) * kTileN + 32u);
             ask_scale(it);
 #pragma unroll 1
             for (int k = 0; k < a.n_ksteps; ++k, ++it) {
@@ -368,7 +370,7 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 // two blocks of columns under way at a time; the next accumulator's first two before this one's last sums are done
                 columns_wait(v[0]);
                 columns_wait(v[1]);
-                if (blocks == 4) {
+                if (wide) {
                     add(0, v[0]);
                     columns_load(v[0], taddr + 64u);
                     add(1, v[1]);
@@ -385,17 +387,18 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                     handed_on();
                     ask_scale(it + 1);
                 }
-                const uint32_t next = lanes + (b ^ 1) * kTileN;
-                if (blocks == 4) add(2, v[0]); else add(0, v[0]);
+                const uint32_t next = lanes + ((it + 1) & 1) * kTileN;
+                if (wide) add(2, v[0]); else add(0, v[0]);
                 if (more) columns_load(v[0], next);
-                if (blocks == 4) add(3, v[1]); else if (blocks == 2) add(1, v[1]);
-                if (more && blocks > 1) columns_load(v[1], next + 32u);
+                if (wide) add(3, v[1]); else add(1, v[1]);
+                if (more) columns_load(v[1], next + 32u);
             }
-            if (a.vec_out && blocks > 1 && t0 + 32 <= T) {
+            // tiled copies write whole boxes, or boxes cut at the last of M_max rows: at the last channel they are cut on 16 bytes only
+            if (a.vec_out && ch0 + a.tile_n / 2 <= a.N && (t0 + 32 <= T || (t0 < T && T == a.M_max))) {
                 constexpr int kBox = kBf16 ? 64 : 32;                    // channels of a box
 #pragma unroll
                 for (int r = 0; r < (kBf16 ? 1 : 2); ++r) {
-                    if (2 * r * kBox >= a.tile_n / 2 || ch0 + 2 * r * kBox >= a.N) break;
+                    if (2 * r * kBox >= a.tile_n / 2) break;
                     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     __syncwarp();                                        // the boxes before these have been read
                     stage_boxes<kBf16>(lane, acc + 32 * r, stage);
@@ -404,7 +407,7 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                     if (lane == 0) {
 #pragma unroll
                         for (int g = 2 * r; g < 2 * r + 2; ++g)
-                            if (g * kBox < a.tile_n / 2 && ch0 + g * kBox < a.N)
+                            if (g * kBox < a.tile_n / 2)
                                 asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
                                              :: "l"(&map_out), "r"(ch0 + g * kBox), "r"((int)t0), "r"(stage + (uint32_t)((g & 1) * 4096)) : "memory");
                         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
@@ -869,32 +872,40 @@ template <class Kernel> static int raise_smem(Kernel kernel, size_t bytes, bool 
     return DPPO_OK;
 }
 
-// ---- which kernel, which tile: both kernels' times in microseconds ----
-static double pair_time(long long M, int N, int n_ksteps, int* tile) {
+// ---- which kernel, which tile ----
+// Both kernels' times in microseconds, fitted to measurements.
+//
+// Pair kernel: whole waves of tiles.  A block of a tile of 256 channels takes 0.61 us, of 128 channels 0.50 (its way to the epilogue and back);
+// a wave ends with its outputs, which take longer where tiled copies cannot write them.
+static double pair_time(long long M, int N, int n_ksteps, bool bf16, bool tiled, int* tile) {
     const long long n_tok = (M + 255) / 256, pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
+    const double store = !tiled ? 0.027 : bf16 ? 0.010 : 0.016;
     double best = 0.0;
-    for (int tn = kTileN; tn >= 64; tn /= 2) {
+    for (int tn = kTileN; tn >= 128; tn /= 2) {
         const long long tiles = n_tok * ((N + tn - 1) / tn), waves = (tiles + pairs - 1) / pairs;
-        const double slab = tn * 0.0018 > 0.3 ? tn * 0.0018 : 0.3;
-        const double t = 2.9 + (double)waves * (n_ksteps * slab + 0.3 + 0.011 * tn);
+        const double t = 3.4 + (double)waves * (n_ksteps * (tn == 256 ? 0.61 : 0.50) + store * tn);
         if (best == 0.0 || t < best) { best = t; *tile = tn; }
     }
     return best;
 }
+// The other, with the split of the contraction that takes least.  A block costs its latency, or, as far as two CTAs share an SM, what the SM can
+// fetch (75 KB/us); each CTA starts and ends, later with a second one beside it; a join grows with the CTAs that take part and
+// with the tokens.
 static double small_time(long long M, int N, int n_ksteps, int* tokens, int* split) {
     const int nb = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
     const long long tiles = (long long)((N + kTileM - 1) / kTileM) * ((M + nb - 1) / nb), sms = sm_count();
-    const double latency = 0.25 + 0.00075 * nb, fetch = 2 * (16384 + nb * 128) / 75e3;
+    const double latency = 0.30 + 0.0016 * nb, fetch = 2 * (16384 + nb * 128) / 75e3;
+    const int per_sm = nb <= 64 ? 2 : 1;
     double best = 0.0;
     for (int sp = 1, i = 0; sp <= 8; sp *= 2, ++i) {
-        constexpr double kJoin[4] = {0.0, 0.3, 0.4, 0.9};
+        constexpr double kJoin[4] = {0.0, 0.3, 0.4, 0.2}, kPerToken[4] = {0.0, 0.017, 0.017, 0.026};
         const long long ctas = tiles * sp;
-        if (sp > 1 && (ctas > 2 * sms || n_ksteps < sp)) break;
-        const bool two = ctas > sms;
-        const double waves = ctas <= 2 * sms ? 1.0 : (double)ctas / (double)(2 * sms) + 0.4;
-        const double slab = two && fetch > latency ? fetch : latency;
-        const double t = waves * (((n_ksteps + sp - 1) / sp) * slab + 3.0 + 0.0075 * nb) + (two ? 1.8 : 0.0)
-                       + (sp > 1 ? kJoin[i] + 0.017 * nb : 0.0);
+        if (sp > 1 && (ctas > per_sm * sms || n_ksteps < sp)) break;
+        const double shared = per_sm == 1 || ctas <= sms ? 0.0 : ctas >= 2 * sms ? 1.0 : (double)(ctas - sms) / (double)sms;
+        const double waves = ctas <= per_sm * sms ? 1.0 : (double)ctas / (double)(per_sm * sms) + 0.4;
+        const double slab = latency + (fetch > latency ? shared * (fetch - latency) : 0.0);
+        const double t = waves * (((n_ksteps + sp - 1) / sp) * slab + 3.0 + 0.0075 * nb) + 1.8 * shared
+                       + (sp > 1 ? kJoin[i] + kPerToken[i] * nb : 0.0);
         if (best == 0.0 || t < best) { best = t; *split = sp; }
     }
     *tokens = nb;
@@ -989,10 +1000,11 @@ extern "C" int dppo_linear_f8(const dppo_linear_f8_params* p, const uint8_t* x, 
     a.N = p->N; a.n_ksteps = n_blocks; a.out_bf16 = p->out_dtype == DPPO_BF16;
     a.wait_limit_ns = p->variant >= 100 ? kSelfTestWaitLimitNs : kDefaultWaitLimitNs;
     a.test_extra_tx = p->variant >= 100 ? 16 : 0;
-    int nb = 0, split = 1;
-    const double t_pair = f8::pair_time(p->M_max, p->N, n_blocks, &a.tile_n), t_small = f8::small_time(p->M_max, p->N, n_blocks, &nb, &split);
-    const bool pair = variant == 1 || (variant == 0 && t_pair < t_small);
     a.vec_out = ((uintptr_t)out & 15) == 0 && p->out_stride * (a.out_bf16 ? 2 : 4) % 16 == 0 && p->out_stride < (1ll << 36);
+    int nb = 0, split = 1;
+    const double t_pair = f8::pair_time(p->M_max, p->N, n_blocks, a.out_bf16 != 0, a.vec_out != 0, &a.tile_n);
+    const double t_small = f8::small_time(p->M_max, p->N, n_blocks, &nb, &split);
+    const bool pair = variant == 1 || (variant == 0 && t_pair < t_small);
     alignas(64) CUtensorMap mw, mx, ms, mo = {};
     int rc = f8::make_map(&mw, w, p->N, p->K, p->w_stride, pair ? a.tile_n / 2 : f8::kTileM);
     if (rc == DPPO_OK) rc = f8::make_map(&mx, x, p->M_max, p->K, p->x_stride, pair ? f8::kTileM : nb);
