@@ -846,9 +846,9 @@ template <bool kBf16, int kPer> static int run_fwd(const Args& a, cudaStream_t s
     if (nvec <= 256) return run_warp<kBf16, false, kPer>(a, s);
     if (nvec > 4096)
         while (C < kMaxCluster && a.T_max * C < 2 * sms) C *= 2;
-    if (nvec <= 512) return launch_fwd<kBf16, 128, kPer, false>(a, 1, s);
-    if (C == 1) return launch_fwd<kBf16, 128, kPer, false>(a, 1, s);
-    return launch_fwd<kBf16, 256, kPer, true>(a, C, s);
+    if (C > 1) return launch_fwd<kBf16, 256, kPer, true>(a, C, s);
+    if (nvec > 1024 && a.T_max <= 5 * sms) return launch_fwd<kBf16, 256, kPer, false>(a, 1, s);
+    return launch_fwd<kBf16, 128, kPer, false>(a, 1, s);
 }
 
 template <bool kBf16, int kVecs, bool kGradient, int kPer> static int launch_warp(const Args& a, cudaStream_t s) {

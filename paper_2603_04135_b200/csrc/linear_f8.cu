@@ -889,8 +889,8 @@ static double pair_time(long long M, int N, int n_ksteps, bool bf16, bool tiled,
     return best;
 }
 // The other, with the split of the contraction that takes least.  A block costs its latency, or, as far as two CTAs share an SM, what the SM can
-// fetch (75 KB/us); each CTA starts and ends, later with a second one beside it; a join grows with the CTAs that take part and
-// with the tokens.
+// fetch (75 KB/us); each CTA starts and ends, later with a second one beside it; a join grows with the tokens, one of eight CTAs also with how
+// many of them there are.
 static double small_time(long long M, int N, int n_ksteps, int* tokens, int* split) {
     const int nb = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
     const long long tiles = (long long)((N + kTileM - 1) / kTileM) * ((M + nb - 1) / nb), sms = sm_count();
@@ -898,14 +898,13 @@ static double small_time(long long M, int N, int n_ksteps, int* tokens, int* spl
     const int per_sm = nb <= 64 ? 2 : 1;
     double best = 0.0;
     for (int sp = 1, i = 0; sp <= 8; sp *= 2, ++i) {
-        constexpr double kJoin[4] = {0.0, 0.3, 0.4, 0.2}, kPerToken[4] = {0.0, 0.017, 0.017, 0.026};
         const long long ctas = tiles * sp;
+        const double joins[4] = {0.0, 0.3 + 0.017 * nb, 0.4 + 0.017 * nb, 0.2 + nb * (0.002 + 0.040 * (double)ctas / (double)sms)};
         if (sp > 1 && (ctas > per_sm * sms || n_ksteps < sp)) break;
         const double shared = per_sm == 1 || ctas <= sms ? 0.0 : ctas >= 2 * sms ? 1.0 : (double)(ctas - sms) / (double)sms;
-        const double waves = ctas <= per_sm * sms ? 1.0 : (double)ctas / (double)(per_sm * sms) + 0.4;
+        const double waves = per_sm == 1 ? (double)((ctas + sms - 1) / sms) : ctas <= 2 * sms ? 1.0 : (double)ctas / (double)(2 * sms) + 0.4;
         const double slab = latency + (fetch > latency ? shared * (fetch - latency) : 0.0);
-        const double t = waves * (((n_ksteps + sp - 1) / sp) * slab + 3.0 + 0.0075 * nb) + 1.8 * shared
-                       + (sp > 1 ? kJoin[i] + kPerToken[i] * nb : 0.0);
+        const double t = waves * (((n_ksteps + sp - 1) / sp) * slab + 3.0 + 0.0075 * nb) + 1.8 * shared + joins[i];
         if (best == 0.0 || t < best) { best = t; *split = sp; }
     }
     *tokens = nb;
