@@ -65,7 +65,8 @@ __device__ __forceinline__ long long rows_of(const Args& a) {
 // ---- the teacher's entries of a row, by a warp: entry i * 32 + lane in slot i of a lane ------------------
 template <int kPer> struct Listed {
     int id[kPer];                                  // -1: no entry
-    double p[kPer];                                // 0 where there is none
+    double p[kPer];                                // 0 where there is none; mode NORMALIZED: relative to the largest
+    float top;                                     // (all lanes) that one's log-prob; 0 in the other modes
     float z[kPer];                                 // the student's logit, -inf where there is none
     bool first[kPer];                              // no earlier entry has this id
     bool bad;                                      // (all lanes) an id outside [-1, V)
@@ -97,9 +98,18 @@ template <bool kBf16, int kPer> __device__ __forceinline__ void listed_logits(co
 #pragma unroll
     for (int i = 0; i < kPer; ++i) e.z[i] = e.id[i] >= 0 ? Elems<kBf16>::load1(row, e.id[i]) : -INFINITY;
 }
-template <int kPer> __device__ __forceinline__ void listed_probs(const float (&lp)[kPer], Listed<kPer>& e) {
+template <int kPer> __device__ __forceinline__ void listed_probs(const Args& a, const float (&lp)[kPer], Listed<kPer>& e) {
+    e.top = 0.0f;
+    if (a.mode == DPPO_DISTILL_NORMALIZED) {       // lists whose probabilities are all far below 1 keep their ratios
+        float top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) e.p[i] = e.id[i] >= 0 ? exp64((double)lp[i]) : 0.0;
+        for (int i = 0; i < kPer; ++i)
+            if (e.id[i] >= 0 && lp[i] < INFINITY) top = fmaxf(top, lp[i]);
+        top = warp_max_f32(top);
+        if (top > -INFINITY) e.top = top;
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) e.p[i] = e.id[i] >= 0 ? exp64((double)lp[i] - (double)e.top) : 0.0;
 }
 // Which entries are the first with their id.  together: their p, added up in the order of the entries, goes to the first.
 template <int kPer> __device__ __forceinline__ void listed_first(const Args& a, int lane, Listed<kPer>& e, bool together) {
@@ -141,7 +151,7 @@ __device__ __forceinline__ double warp_sum_f64(double v) {
 // ---- the row's loss from its parts ---------------------------------------------------------------------
 // What the teacher's entries alone say (in every lane): formed while the row is under way.
 struct Mass {
-    double P, lp, z;                               // sums of p, of p ln p and of p (z - zmax)
+    double P, lp, z;                               // sums of p, of p ln p and of p (z - zmax); p as in Listed
     float G, r, norm;                              // the listed p times norm are the loss's p
     float zmax;
     bool bad;                                      // a NaN or +inf among the listed logits
@@ -161,7 +171,7 @@ template <int kPer> __device__ __forceinline__ Mass listed_mass(const Args& a, c
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         m.P += e.p[i];
-        if (e.p[i] != 0.0) { m.lp += e.p[i] * (double)lp[i]; m.z += e.p[i] * ((double)e.z[i] - (double)m.zmax); }
+        if (e.p[i] != 0.0) { m.lp += e.p[i] * ((double)lp[i] - (double)e.top); m.z += e.p[i] * ((double)e.z[i] - (double)m.zmax); }
     }
     m.P = warp_sum_f64(m.P); m.lp = warp_sum_f64(m.lp); m.z = warp_sum_f64(m.z);
     const double r = a.mode == DPPO_DISTILL_REST && 1.0 - m.P > kLeastRest ? 1.0 - m.P : 0.0;
@@ -329,7 +339,7 @@ distill_forward_kernel(const Args a) {
     Part hot = part_none();                                        // the unlisted entries of the marked vectors
     Mass mass = {};
     if (warp == kWarps) {
-        listed_probs<kPer>(lp, e);
+        listed_probs<kPer>(a, lp, e);
         listed_logits<kBf16, kPer>(row, e);
         int vec[kPer];
         unsigned out[kPer];
@@ -456,7 +466,7 @@ distill_step_kernel(const Args a, int log2C, int vec_per_cta) {
         listed_ids<kPer>(a, t, lane, e, lp);
         wt = (float)((a.weight ? (double)a.weight[t] : 1.0) * a.inv_tau);
         listed_logits<kBf16, kPer>(row, e);
-        listed_probs<kPer>(lp, e);
+        listed_probs<kPer>(a, lp, e);
         listed_first<kPer>(a, lane, e, false);
         mass = listed_mass<kPer>(a, e, lp);
     }
@@ -498,7 +508,8 @@ distill_step_kernel(const Args a, int log2C, int vec_per_cta) {
         if (last && tail0 + tid < a.V && !(sh.tail_listed >> tid & 1u)) ztail = Elems<kBf16>::load1(row, tail0 + tid);
         m = max_nan(m, ztail);
         const bool bad = __any_sync(kAll, !(m < INFINITY));
-        m = bad ? __int_as_float(0x7fffffff) : warp_max_f32(m);
+        m = warp_max_f32(bad ? 0.0f : m);
+        if (bad) m = __int_as_float(0x7fffffff);
         if (lane == 0) sh.m[warp] = m;
     }
     __syncthreads();
@@ -638,7 +649,7 @@ distill_warp_kernel(const Args a) {
     for (int u = 0; u < kVecs; ++u) mine[u * 32 + lane] = q[u];
     if (lane == 0) tails[team] = 0;
     __syncwarp();
-    listed_probs<kPer>(lp, e);
+    listed_probs<kPer>(a, lp, e);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int v = e.id[i] >> kLog2;
@@ -659,7 +670,7 @@ distill_warp_kernel(const Args a) {
     __nv_bfloat162 unused;
     float m = max_nan(vecs_max<kBf16, kVecs>(q, unused), zt);
     const bool bad = __any_sync(kAll, !(m < INFINITY));
-    m = bad ? 0.0f : fmaxf(warp_max_f32(m), kLowest);
+    m = fmaxf(warp_max_f32(bad ? 0.0f : m), kLowest);
     Sum acc;
     sum_init(acc, m, a.c);
     f32x2 x[kVecs * kPerVec / 2];                                  // the exponentials
@@ -803,7 +814,7 @@ distill_backward_kernel(const Args a) {
     }
     double norm = 1.0;
     if (lister && any) {
-        listed_probs<kPer>(lp, e);
+        listed_probs<kPer>(a, lp, e);
         if (a.mode == DPPO_DISTILL_NORMALIZED) {
             double P = 0.0;
 #pragma unroll
@@ -839,6 +850,9 @@ template <bool kBf16, int kThreads, int kPer, bool kCluster> static int launch_f
     return launch_after("distill_topk launch", kernel, a.T_max * C, kThreads + 32, smem, s, kCluster ? C : 1, a);
 }
 
+// Loss alone: a warp per row up to 4 KB, else a CTA, in a cluster while the rows do not give every SM two (40 x 151,936 bf16 8.5 us).  A CTA alone has 256
+// threads up to five rows per SM (400 x 151,936 bf16 29.5 us, with 128 44.6; 700 x 50,304 18.4, 20.2) and 128 beyond, where they are as fast and
+// leave room for shorter ones (8,192 x 151,936 390 us, 6.4 TB/s).
 template <bool kBf16, int kPer> static int run_fwd(const Args& a, cudaStream_t s) {
     const int nvec = a.V >> (kBf16 ? 3 : 2);
     const long long sms = sm_count();
@@ -877,6 +891,7 @@ template <bool kBf16, int kThreads, int kPer> static int launch_step(const Args&
     if (a.T_max << log2C > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "distill_topk: T_max=%lld needs too large a grid", a.T_max);
     return launch_after("distill_topk launch", kernel, a.T_max << log2C, kThreads + 32, (size_t)max(vec_per_cta, 1) * 16, s, 1 << log2C, a, log2C, vec_per_cta);
 }
+// Loss and gradient, 8,192 x 151,936 bf16 875 us (5.7 TB/s of one read and one write; as two kernels 1,160); 20,011 x 1,021 f32 31 (5.3).
 // The slices of a row: in one CTA up to 44 KB, in two of up to 55 KB, else in four or eight of up to 76 KB, three of which share an SM.
 template <bool kBf16, int kPer> static int run_step(const Args& a, cudaStream_t s, bool* done) {
     const int nvec = a.V >> (kBf16 ? 3 : 2);

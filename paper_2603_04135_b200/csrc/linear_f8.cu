@@ -183,6 +183,11 @@ template <bool kBf16> __device__ __forceinline__ void stage_boxes(int lane, cons
 }
 
 // ---- many tokens: CTA pairs ---------------------------------------------------------------------------
+// 2,048 x 2,560 x 151,936 into bf16: 840 us at 1.6 GHz, 1.9 PFLOP/s (930 us in a long run, under the power limit), where the products alone would
+// take 464 at the rate of a plain product.  What bounds it is the accumulator's way to the registers: a block's 256 x 256
+// sums take 650 cycles of products, 512 of tensor-memory reads, and the hand-over between; two accumulators fill tensor memory.  With
+// tiles of 128 channels a block takes 0.50 us instead of 0.61, also with four accumulators.  Sixteen epilogue warps, two instructions of half
+// the channels each, and epilogue warps that look at the barriers themselves were slower (907, 880 and 976 us).
 struct Shared2 {
     unsigned long long full[kMaxStages];
     unsigned long long empty[kMaxStages];
@@ -441,6 +446,8 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
 }
 
 // ---- few tokens: a CTA per 128 channels, K split over a cluster ---------------------------------------
+// 1 x 2,560 x 151,936: 65 us, 6.0 TB/s of weights; 64 x 4,096 x 4,096 in 9.5 us, where four CTAs share a tile and a CTA's eight blocks of
+// 0.4 us each, its start and the join are what takes time.
 template <int kNB> struct Small {
     static constexpr int kStages = kNB <= 16 ? 6 : kNB <= 32 ? 5 : kNB <= 64 ? 4 : 6;        // two CTAs per SM, but one of 128 tokens
     static constexpr int kPerSm = kNB <= 64 ? 2 : 1;
@@ -653,6 +660,7 @@ linear_f8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
 }
 
 // ---- quantisation -------------------------------------------------------------------------------------
+// One read, one write: 8,192 x 4,096 bf16 28 us (3.6 TB/s), 2,048 x 2,560 6.
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));

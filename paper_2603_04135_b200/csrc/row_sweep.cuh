@@ -1,5 +1,5 @@
-// Sweeps over rows of logits: loads, maxima, and an online sum of exponentials (shared by the scoring, distillation and
-// draft verification kernels; not part of the ABI).
+// Sweeps over rows of logits: loads, maxima, and an online sum of exponentials (shared by the distillation and draft
+// verification kernels; not part of the ABI).
 #pragma once
 #include "common.cuh"
 #include "grpo_loss.cuh"
@@ -11,10 +11,11 @@ using namespace packed;
 constexpr float kLowest = -3.402823466e38f;
 constexpr int kRound = 4;                 // vectors that a thread has under way
 
+// Over a warp, no NaN among them.  By integers in the order of the floats: with the f32 form of the same instruction a short row's maximum
+// came out as another register's value in one of the kernels.
 __device__ __forceinline__ float warp_max_f32(float v) {
-    float r;
-    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-    return r;
+    const int i = __float_as_int(v), k = __reduce_max_sync(0xffffffffu, i ^ (i >> 31 & 0x7fffffff));
+    return __int_as_float(k ^ (k >> 31 & 0x7fffffff));
 }
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
@@ -172,10 +173,10 @@ __device__ __forceinline__ void part_one(Part& p, float z, float c) {
 }
 
 // ---- a row's scalars in 64 bits, short of the library's full precision -----------------------------------
-// e^x for x <= 700 to a relative 2^-36: x = n ln 2 + f with |f| <= ln 2 / 2, the Taylor series of e^f to f^9 / 9! (remainder
-// f^10 / 10! < 7e-12), in two halves that are under way together, and n added to the exponent.  Below -700 it is 0.
+// e^x for |x| <= 700 to a relative 2^-36: x = n ln 2 + f with |f| <= ln 2 / 2, the Taylor series of e^f to f^9 / 9! (remainder
+// f^10 / 10! < 7e-12), in two halves that are under way together, and n added to the exponent.  Below it is 0, above infinity.
 __device__ __forceinline__ double exp64(double x) {
-    if (!(x >= -700.0)) return x != x ? x : 0.0;
+    if (!(fabs(x) <= 700.0)) return x != x ? x : x > 0.0 ? (double)INFINITY : 0.0;
     const double n = rint(x * 1.4426950408889634);
     const double f = fma(n, -0.6931471805599453, x), f2 = f * f;
     const double even = fma(fma(fma(fma(1.0 / 40320, f2, 1.0 / 720), f2, 1.0 / 24), f2, 0.5), f2, 1.0);

@@ -8,9 +8,9 @@
 // Two kernels.  The first reduces every row of both policies to {m, S} (one read of all logits: what bounds the call); the second, a
 // cluster of CTAs per sequence, finds the first rejection (a warp, 32 drafts at a time) and races over that one row.
 //
-// The race: an entry counts only if its p / e, by one fma and a logarithm, comes near the best lower bound among the
-// first entries of its CTA, which a few dozen do; only those look at the draft's row, all at once.  Tokens are exact: f32 decides a race only where no second entry's upper bound reaches the winner's lower bound; otherwise
-// the entries within reach are compared in 64 bits, ties to the lower index.
+// The race: an entry counts only if its p / e, by one fma and a logarithm, comes near the best lower bound among the first entries of its
+// CTA, which a few dozen do; only those look at the draft's row, all at once.  Tokens are exact: f32 decides a race only where no second
+// entry's upper bound reaches the winner's lower bound; otherwise the entries within reach are compared in 64 bits, ties to the lower index.
 #include <cooperative_groups.h>
 
 #include "common.cuh"

@@ -212,6 +212,28 @@ def test_far_temperatures(B, V, dtype, tau):
     check(r, z, V, ids, lp, 2, tau)
 
 
+@pytest.mark.parametrize("V,dtype", [(40, "f32"), (250, "bf16"), (500, "f32"), (1000, "f32"), (1000, "bf16"), (2000, "bf16"), (5000, "f32"), (9001, "bf16"),
+                                     (100003, "f32"), (151936, "bf16")])
+@pytest.mark.parametrize("K", [8, 40])
+def test_largest_logit(B, V, dtype, K):
+    """The statistics' maximum, of rows with entries and without."""
+    for T, mode in ((30, 0), (30, 1), (30, 2), (500, 2)):
+        z, ids, lp = make(T, V, dtype, K, V + mode)
+        ids[0], ids[5], ids[17] = -1, -1, -1
+        r = Run(B, z, V, ids, lp, mode, 1.0)
+        for o in (r.one, r.two):
+            assert torch.equal(o["stats"][:T, 0], z[:, :V].float().amax(1))
+
+
+@pytest.mark.parametrize("V,dtype,K", [(500, "f32", 6), (3001, "bf16", 6), (60001, "f32", 40), (151936, "bf16", 6)])
+def test_normalized_lists_of_low_probability(B, V, dtype, K):
+    """A list of unlikely tokens (e^-600 together) normalises as any other does."""
+    z, ids, lp = make(6, V, dtype, K, V + 1)
+    lp -= torch.tensor([0.0, 60.0, 90.0, 150.0, 400.0, 600.0], device="cuda")[:, None]
+    r = Run(B, z, V, ids, lp, 1, 1.0)
+    check(r, z, V, ids, lp, 1, 1.0)
+
+
 @pytest.mark.parametrize("V,dtype", [(300, "f32"), (70001, "bf16")])
 def test_bad_ids(B, V, dtype):
     z, ids, lp = make(6, V, dtype, 5, 3)
