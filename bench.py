@@ -18,10 +18,13 @@ Side modes (each prints its own lines and is not part of the default run):
                                 (--rows --vocab --dtype --iters --in-place --full-call --back-to-back --variant)
   --profile-case score, linear  the same for the scoring call (--rows --vocab --dtype --top-k --backward --variant) and the
                                 8-bit product (--tokens --hidden --vocab --variant)
+  --profile-case distill, verify, linear-f8   distillation (--rows --vocab --dtype --top-k --backward), verification of 7 drafts
+                                in each of --seqs sequences (--vocab --dtype), the block-scaled 8-bit product
   --profile-case lmhead         the same for the fused LM-head (--tokens --hidden --vocab --iters --backward --variant)
 """
 import argparse
 import json
+import math
 import multiprocessing as mp
 import os
 import statistics
@@ -313,7 +316,8 @@ def time_row_length(dtype, V, rows, dev, iters=8, warmup=3):
 # --------------------------------------------------------------------------------------- profile cases
 def run_score_case(args):
     """`score`: dppo_token_logprobs (or, with --backward, its gradient) on --rows rows of --vocab logits;  `linear`:
-    dppo_quantize_rows_i8 + dppo_linear_i8 on --tokens tokens, --hidden wide, --vocab channels, bf16 out."""
+    dppo_quantize_rows_i8 + dppo_linear_i8 on --tokens tokens, --hidden wide, --vocab channels, bf16 out;  `linear-f8`: the same of
+    dppo_quantize_f8 + dppo_linear_f8;  `distill`: dppo_distill_topk, with --backward loss and gradient;  `verify`: dppo_verify_drafts."""
     from paper_2603_04135_b200 import binding as B
     torch.cuda.set_device(0)
     gen = torch.Generator(device="cuda").manual_seed(0)
@@ -330,6 +334,47 @@ def run_score_case(args):
         def call():
             B.quantize_rows_i8(B.QuantizeParams(M, K, B.BF16, x.shape[1], ld), x, q, qs, status=status)
             B.linear_i8(B.LinearI8Params(M, N, K, ld, ld, N, B.BF16, args.variant), q, qs, w, ws, out, status=status)
+    elif args.profile_case == "linear-f8":
+        M, K, N = args.tokens, args.hidden, args.vocab
+        kb, f8 = -(-K // 128), torch.float8_e4m3fn
+        x = torch.empty(M, -(-K // 8) * 8, device="cuda").normal_(generator=gen).to(torch.bfloat16)
+        w = torch.empty(N, kb * 128, device="cuda").normal_(0.0, 100.0, generator=gen).clamp_(-448.0, 448.0).to(f8)
+        q, qs = torch.zeros(M, kb * 128, dtype=f8, device="cuda"), torch.zeros(kb, -(-M // 4) * 4, device="cuda")
+        ws, out = torch.rand(-(-N // 128), kb, device="cuda", generator=gen), torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+        work, unit = 2.0 * M * N * K, "TOP/s"
+
+        def call():
+            B.quantize_f8(B.QuantizeF8Params(M, K, B.BF16, x.shape[1], kb * 128, qs.shape[1], 1), x, q, qs, status=status)
+            B.linear_f8(B.LinearF8Params(M, N, K, kb * 128, kb * 128, N, qs.shape[1], kb, B.BF16, args.variant), q, qs, w, ws, out, status=status)
+    elif args.profile_case in ("distill", "verify"):
+        V, dt = args.vocab, torch.bfloat16 if args.dtype == "bf16" else torch.float32
+        ld = -(-V // (16 // dt.itemsize)) * (16 // dt.itemsize)
+        code = B.BF16 if dt is torch.bfloat16 else B.F32
+        logits = lambda rows: torch.empty(rows, ld, dtype=dt, device="cuda").normal_(0.0, 2.0, generator=gen)
+        if args.profile_case == "distill":
+            T, k = args.rows, max(args.top_k, 1)
+            z, ids = logits(T), torch.randint(0, V, (T, k), device="cuda", generator=gen, dtype=torch.int32)
+            logp = torch.full((T, k), -math.log(2.0 * k), device="cuda")
+            loss, lse, stats = torch.zeros(T, device="cuda"), torch.zeros(T, device="cuda"), torch.zeros(T, 4, device="cuda")
+            dz = torch.empty_like(z) if args.backward else None
+            prm = B.DistillParams(T, V, code, ld, k, B.DISTILL_REST, 1.0)
+            work, unit = (2.0 if args.backward else 1.0) * T * V * dt.itemsize * 1e-3, "GB/s"
+
+            def call():
+                B.distill_topk(prm, z, ids, logp, None, None, loss, lse, stats, dz, status)
+        else:
+            n, T = args.seqs, 7 * args.seqs
+            target, draft = logits(T + n), logits(T)
+            y, cu = torch.randint(0, V, (T,), device="cuda", generator=gen, dtype=torch.int32), torch.arange(0, T + 1, 7, dtype=torch.int32, device="cuda")
+            u, noise = torch.rand(T, device="cuda", generator=gen), torch.empty(n, -(-V // 4) * 4, device="cuda").exponential_(generator=gen)
+            acc, tok, logp = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(T + n, dtype=torch.int32, device="cuda"), torch.zeros(T + n, device="cuda")
+            prm = B.VerifyParams(T, n, V, code, ld, ld, noise.shape[1], 1.0, 1.0)
+            nbytes = B.verify_drafts_workspace_bytes(prm)
+            scratch = torch.zeros(nbytes, dtype=torch.uint8, device="cuda")
+            work, unit = (2.0 * T + n) * V * dt.itemsize * 1e-3, "GB/s"
+
+            def call():
+                B.verify_drafts(prm, target, draft, y, cu, u, noise, acc, tok, logp, scratch, nbytes, status)
     else:
         T, V, dt = args.rows, args.vocab, torch.bfloat16 if args.dtype == "bf16" else torch.float32
         per16 = 16 // dt.itemsize
@@ -729,7 +774,7 @@ def main():
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--no-lmhead", action="store_true", help="skip the fused LM-head measurement")
     ap.add_argument("--no-modes", action="store_true", help="skip the forward-only / in-place / sequence-ratio timings")
-    ap.add_argument("--profile-case", choices=["loss", "lmhead", "score", "linear"], help="instead of the benchmark: a small self-contained run")
+    ap.add_argument("--profile-case", choices=["loss", "lmhead", "score", "linear", "linear-f8", "distill", "verify"], help="instead of the benchmark: a small self-contained run")
     ap.add_argument("--rows", type=int, default=8192)
     ap.add_argument("--tokens", type=int, default=16384)
     ap.add_argument("--hidden", type=int, default=2560)
@@ -750,7 +795,7 @@ def main():
     args = ap.parse_args()
     if args.prune_pack_sweep:
         sys.exit(run_prune_pack_sweep(args))
-    if args.profile_case in ("score", "linear"):
+    if args.profile_case in ("score", "linear", "linear-f8", "distill", "verify"):
         sys.exit(run_score_case(args))
     if args.profile_case:
         sys.exit(run_profile_case(args))
