@@ -6,8 +6,9 @@
  * factors so that the gradient stays unbiased, packs the retained sequences densely and trains on
  * them.  This library does, per batch:  group advantages -> candidate sets, pruning masks and
  * rescaling factors -> Dense Prompt Packing -> one sweep over the LM-head logits that yields the
- * loss and dlogits; and, for the frozen policies of that loss, the scoring of the sampled tokens (8-bit LM-head
- * product, log-probs with entropy and alternatives).
+ * loss and dlogits; for the frozen policies of that loss, the scoring of the sampled tokens (8-bit LM-head
+ * product, log-probs with entropy and alternatives); and, with a second policy beside the trained one, distillation
+ * from its alternatives, verification of tokens that it drafted, and its LM-head in block-scaled 8-bit floating point.
  *
  * Conventions (all entry points)
  *  - Return value: 0 (DPPO_OK) or a negative dppo_error.  Nothing throws, aborts or prints.

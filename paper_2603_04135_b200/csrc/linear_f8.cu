@@ -660,7 +660,7 @@ linear_f8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
 }
 
 // ---- quantisation -------------------------------------------------------------------------------------
-// One read, one write: 8,192 x 4,096 bf16 28 us (3.6 TB/s), 2,048 x 2,560 6.
+// One read, one write: rows, 8,192 x 4,096 f32 27 us (6.3 TB/s), bf16 23 (4.3, bound by its instructions); 128 x 128, 43 and 29.
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
@@ -687,13 +687,13 @@ __device__ __forceinline__ Scale scale_of(float amax) {
     Scale r;
     r.fine = amax < INFINITY;
     r.s = r.fine ? fmaxf(__fmul_rn(amax, 1.0f / 448.0f), 1.17549435e-38f) : __int_as_float(0x7fffffff);
-    const float inv = __fdiv_rn(1.0f, r.s);
+    const float inv = __fdividef(1.0f, r.s);
     r.lo = inv * (1.0f - 0x1p-21f);
     r.hi = inv * (1.0f + 0x1p-21f);
     return r;
 }
-// The codes of kPer values, 4 per word.  The quotient x / s lies strictly between x lo and x hi (the roundings of 1 / s and of the
-// products are 2^-24 each), and rounding to a code is monotonous: where both ends have the same code, so has the quotient.  A
+// The codes of kPer values, 4 per word.  The quotient x / s lies strictly between x lo and x hi (1 / s is off by 2^-22 of it at most, the
+// roundings of the products by 2^-24 each), and rounding to a code is monotonous: where both ends have the same code, so has the quotient.  A
 // vector where they differ (one in ten thousand) is divided out.
 template <int kPer> __device__ __forceinline__ void codes_of(const float (&f)[kPer], const Scale& sc, uint32_t (&w)[kPer / 4]) {
     uint32_t diff = 0;
@@ -723,13 +723,22 @@ template <bool kBf16> __device__ __forceinline__ uint4 load_part(const char* row
     for (int j = 0; j < kPer; ++j) f[j] = e0 + j < K ? Elems<kBf16>::load1(row, e0 + j) : 0.0f;
     return Elems<kBf16>::pack(f);
 }
-template <bool kBf16> __device__ __forceinline__ float amax_vec(const uint4& v) {
-    constexpr int kPer = Elems<kBf16>::kPerVec;
-    float f[kPer], m = 0.0f;
-    Elems<kBf16>::unpack(v, f);
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) m = max_nan(m, fabsf(f[j]));
-    return m;
+// The largest magnitude of a vector, and of several lanes' (bf16: of each half of a word, joined at the end).
+template <bool kBf16> __device__ __forceinline__ uint32_t amax_join(uint32_t a, uint32_t b) {
+    if constexpr (kBf16) {
+        const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+        return *reinterpret_cast<const uint32_t*>(&m);
+    } else {
+        return __float_as_uint(max_nan(__uint_as_float(a), __uint_as_float(b)));
+    }
+}
+template <bool kBf16> __device__ __forceinline__ uint32_t amax_vec(const uint4& v) {
+    constexpr uint32_t kMag = kBf16 ? 0x7fff7fffu : 0x7fffffffu;
+    return amax_join<kBf16>(amax_join<kBf16>(v.x & kMag, v.y & kMag), amax_join<kBf16>(v.z & kMag, v.w & kMag));
+}
+template <bool kBf16> __device__ __forceinline__ float amax_value(uint32_t m) {
+    if constexpr (kBf16) return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+    else return __uint_as_float(m);
 }
 template <bool kBf16> __device__ __forceinline__ void store_codes(uint8_t* row, int e0, int K, const uint4& v, const Scale& sc) {
     constexpr int kPer = Elems<kBf16>::kPerVec;
@@ -755,25 +764,36 @@ template <bool kBf16, int kUnroll> __global__ void __launch_bounds__(128) quanti
     const long long item = (long long)blockIdx.x * kTeams + threadIdx.x / kTeam;
     const long long t = item / groups;
     const int b0 = (int)(item - t * groups) * kUnroll, l = threadIdx.x % kTeam;
-    const bool live = t < T;
     const char* row = a.x + t * a.x_row_bytes;
+    const bool whole_blocks = __all_sync(0xffffffffu, (b0 + kUnroll) * kBK <= a.K);       // one way for both teams of a warp
+    if (t >= T) return;                                            // a whole team
+    const unsigned team = kTeam == 32 ? 0xffffffffu : 0xffffu << (threadIdx.x & 16);
+    float* scale = a.scale + (long long)b0 * a.scale_stride + t;
+    uint8_t* codes = a.q + t * a.q_stride;
+    auto block = [&](const uint4& v, int u, bool whole) {
+        uint32_t m = amax_vec<kBf16>(v);
+#pragma unroll
+        for (int o = kTeam / 2; o > 0; o >>= 1) m = amax_join<kBf16>(m, __shfl_xor_sync(team, m, o));
+        const Scale sc = scale_of(amax_value<kBf16>(m));
+        const int e0 = (b0 + u) * kBK + l * kPer;
+        if (l == 0) scale[u * a.scale_stride] = sc.s;
+        if (whole || e0 < a.K) store_codes<kBf16>(codes, e0, whole ? e0 + kPer : a.K, v, sc);
+    };
     uint4 v[kUnroll];
+    if (whole_blocks) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-        const int e0 = (b0 + u) * kBK + l * kPer;
-        v[u] = live && b0 + u < a.n_blocks && e0 < a.K ? load_part<kBf16>(row, e0, a.K) : make_uint4(0u, 0u, 0u, 0u);
-    }
+        for (int u = 0; u < kUnroll; ++u) v[u] = *reinterpret_cast<const uint4*>(row + (size_t)((b0 + u) * kBK + l * kPer) * (16 / kPer));
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-        float m = amax_vec<kBf16>(v[u]);
+        for (int u = 0; u < kUnroll; ++u) block(v[u], u, true);
+    } else {
 #pragma unroll
-        for (int o = kTeam / 2; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-        const Scale sc = scale_of(m);
-        const int e0 = (b0 + u) * kBK + l * kPer;
-        if (live && b0 + u < a.n_blocks) {
-            if (l == 0) a.scale[(long long)(b0 + u) * a.scale_stride + t] = sc.s;
-            if (e0 < a.K) store_codes<kBf16>(a.q + t * a.q_stride, e0, a.K, v[u], sc);
+        for (int u = 0; u < kUnroll; ++u) {
+            const int e0 = (b0 + u) * kBK + l * kPer;
+            v[u] = e0 < a.K ? load_part<kBf16>(row, e0, a.K) : make_uint4(0u, 0u, 0u, 0u);
         }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (b0 + u < a.n_blocks) block(v[u], u, false);
     }
 }
 
@@ -787,16 +807,17 @@ template <bool kBf16> __global__ void __launch_bounds__(256) quantize_f8_blocks_
     const int bk = (int)(blockIdx.x - br * a.n_blocks), e0 = bk * kBK + (int)(threadIdx.x % kTeam) * kPer;
     if (br * kBK >= T) return;
     uint4 v[kVecs];
-    float m = 0.0f;
+    uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
         const long long t = r0 + i * kRows;
         v[i] = t < T && e0 < a.K ? load_part<kBf16>(a.x + t * a.x_row_bytes, e0, a.K) : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) m = max_nan(m, amax_vec<kBf16>(v[i]));
+    for (int i = 0; i < kVecs; ++i) most = amax_join<kBf16>(most, amax_vec<kBf16>(v[i]));
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+    for (int o = 16; o > 0; o >>= 1) most = amax_join<kBf16>(most, __shfl_xor_sync(0xffffffffu, most, o));
+    float m = amax_value<kBf16>(most);
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = m;
     __syncthreads();
 #pragma unroll
@@ -811,14 +832,16 @@ template <bool kBf16> __global__ void __launch_bounds__(256) quantize_f8_blocks_
 }
 
 // ---- host side ---------------------------------------------------------------------------------------
+template <bool kBf16, int kUnroll> static int run_quantize_rows(const QuantArgs& a, cudaStream_t s) {
+    constexpr int kTeams = kBf16 ? 8 : 4;
+    const int groups = (a.n_blocks + kUnroll - 1) / kUnroll;
+    const long long ctas = (a.rows_max * groups + kTeams - 1) / kTeams;
+    if (ctas > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "quantize_f8: too many blocks");
+    return launch_after("quantize_f8 launch", quantize_f8_rows_kernel<kBf16, kUnroll>, ctas, 128, 0, s, 1, a, groups);
+}
 template <bool kBf16> static int run_quantize(const QuantArgs& a, int block_rows, cudaStream_t s) {
-    if (block_rows == 1) {
-        constexpr int kUnroll = 4, kTeams = kBf16 ? 8 : 4;
-        const int groups = (a.n_blocks + kUnroll - 1) / kUnroll;
-        const long long ctas = (a.rows_max * groups + kTeams - 1) / kTeams;
-        if (ctas > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "quantize_f8: too many blocks");
-        return launch_after("quantize_f8 launch", quantize_f8_rows_kernel<kBf16, kUnroll>, ctas, 128, 0, s, 1, a, groups);
-    }
+    // Few blocks: one at a time, more CTAs (64 x 4,096 bf16 1.8 us, four at a time 2.9; 2,048 x 2,560 6.5 and 5.6)
+    if (block_rows == 1) return a.rows_max * a.n_blocks <= 100ll * sm_count() ? run_quantize_rows<kBf16, 1>(a, s) : run_quantize_rows<kBf16, 4>(a, s);
     const long long ctas = (a.rows_max + kBK - 1) / kBK * a.n_blocks;
     if (ctas > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "quantize_f8: too many blocks");
     return launch_after("quantize_f8 launch", quantize_f8_blocks_kernel<kBf16>, ctas, 256, 0, s, 1, a);
