@@ -892,13 +892,15 @@ template <bool kBf16, int kThreads, int kPer> static int launch_step(const Args&
     return launch_after("distill_topk launch", kernel, a.T_max << log2C, kThreads + 32, (size_t)max(vec_per_cta, 1) * 16, s, 1 << log2C, a, log2C, vec_per_cta);
 }
 // Loss and gradient, 8,192 x 151,936 bf16 875 us (5.7 TB/s of one read and one write; as two kernels 1,160); 20,011 x 1,021 f32 31 (5.3).
-// The slices of a row: in one CTA up to 44 KB, in two of up to 55 KB, else in four or eight of up to 76 KB, three of which share an SM.
+// The slices of a row: in one CTA up to 44 KB, in two of up to 55 KB, else in four or eight of up to 76 KB, three of which share an SM.  Few
+// rows: more CTAs for each (37 x 151,936 bf16 8.7 us, 10.2 in four; 16 x 20,000 f32 5.1, 5.9 in two).
 template <bool kBf16, int kPer> static int run_step(const Args& a, cudaStream_t s, bool* done) {
     const int nvec = a.V >> (kBf16 ? 3 : 2);
     *done = true;
     if (nvec <= 256) return run_warp<kBf16, true, kPer>(a, s);
     const long long bytes = (long long)nvec * 16;
-    const int log2C = bytes <= 44 << 10 ? 0 : bytes <= 110 << 10 ? 1 : bytes <= 304 << 10 ? 2 : 3;
+    int log2C = bytes <= 44 << 10 ? 0 : bytes <= 110 << 10 ? 1 : bytes <= 304 << 10 ? 2 : 3;
+    while (log2C > 0 && log2C < 3 && a.T_max << (log2C + 1) <= 2ll * sm_count()) ++log2C;
     const int vec = (nvec + (1 << log2C) - 1) >> log2C;
     if ((size_t)vec * 16 > kSliceMax) { *done = false; return DPPO_OK; }
     if (vec * 16 > (kBf16 ? 28 : 64) << 10) return launch_step<kBf16, 256, kPer>(a, log2C, vec, s);
