@@ -76,6 +76,30 @@ __device__ __forceinline__ bool warp_wait(unsigned long long* bar, uint32_t pari
     return __all_sync(0xffffffffu, lm_wait(lm_smem_u32(bar), parity, abort_flag, limit_ns));
 }
 
+// lm_wait for two barriers, looked at together: two looks one after the other are 500 cycles while the tensor cores read shared memory.
+__device__ __forceinline__ bool test_both(uint32_t bar0, uint32_t parity0, uint32_t bar1, uint32_t parity1) {
+    uint32_t d0, d1;
+    asm volatile("{\n\t.reg .pred p, q;\n\t"
+                 "mbarrier.test_wait.parity.shared::cta.b64 p, [%2], %3;\n\t"
+                 "mbarrier.test_wait.parity.shared::cta.b64 q, [%4], %5;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t"
+                 "selp.u32 %1, 1, 0, q;\n\t}"
+                 : "=r"(d0), "=r"(d1) : "r"(bar0), "r"(parity0), "r"(bar1), "r"(parity1) : "memory");
+    return (d0 & d1) != 0;
+}
+__device__ __forceinline__ bool wait_both(uint32_t bar0, uint32_t parity0, uint32_t bar1, uint32_t parity1, volatile int* abort_flag,
+                                          unsigned long long limit_ns) {
+    if (test_both(bar0, parity0, bar1, parity1)) return true;
+    const unsigned long long t0 = lm_global_ns();
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 16; ++i)
+            if (test_both(bar0, parity0, bar1, parity1)) return true;
+        if (*abort_flag) return false;
+        if (lm_global_ns() - t0 > limit_ns) { *abort_flag = 1; return false; }
+    }
+}
+
 // kCount consecutive tokens t0 .. of this lane's channel.
 template <bool kBf16, int kCount> __device__ __forceinline__ void store_tokens(const Args& a, long long t0, long long T, int ch, const float* acc) {
     typedef typename std::conditional<kBf16, __nv_bfloat16, float>::type Out;
@@ -183,10 +207,10 @@ template <bool kBf16> __device__ __forceinline__ void stage_boxes(int lane, cons
 }
 
 // ---- many tokens: CTA pairs ---------------------------------------------------------------------------
-// 2,048 x 2,560 x 151,936 into bf16: 840 us at 1.6 GHz, 1.9 PFLOP/s (930 us in a long run, under the power limit), where the products alone would
+// 2,048 x 2,560 x 151,936 into bf16: 778 us on a rested board, 2.0 PFLOP/s (930 us in a long run, under the power limit), where the products alone would
 // take 464 at the rate of a plain product.  What bounds it is the accumulator's way to the registers: a block's 256 x 256
 // sums take 650 cycles of products, 512 of tensor-memory reads, and the hand-over between; two accumulators fill tensor memory.  With
-// tiles of 128 channels a block takes 0.50 us instead of 0.61, also with four accumulators.  Sixteen epilogue warps, two instructions of half
+// tiles of 128 channels a block takes 0.47 us instead of 0.61, also with four accumulators.  Sixteen epilogue warps, two instructions of half
 // the channels each, and epilogue warps that look at the barriers themselves were slower (907, 880 and 976 us).
 struct Shared2 {
     unsigned long long full[kMaxStages];
@@ -291,8 +315,13 @@ linear_f8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             for (uint32_t j = 0; ok && tile_of(j, n_ch, n_tok, ch, tok) && !*abort_flag; ++j) {
                 for (int k = 0; k < a.n_ksteps; ++k, ++it, s = s + 1 == stages ? 0 : s + 1, use += s == 0 ? 1 : 0) {
                     const uint32_t b = it & 1, use_b = it >> 1;
-                    if (!lm_wait(lm_smem_u32(&sh.full[s]), use & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
-                    if (use_b > 0 && !lm_wait(lm_smem_u32(&sh.acc_empty[b]), (use_b - 1) & 1, abort_flag, a.wait_limit_ns)) { ok = false; break; }
+                    const uint32_t full = lm_smem_u32(&sh.full[s]), empty = lm_smem_u32(&sh.acc_empty[b]);
+                    // Tiles of 128 channels: the looks themselves count (705 x 7,681 x 2,000 31.0 us, 32.9 one after the other); of 256 the
+                    // suspended wait is better (1,024 x 2,560 x 20,000 60.4, both polled 62.7).
+                    if (a.tile_n < kTileN && use_b > 0) ok = wait_both(full, use & 1, empty, (use_b - 1) & 1, abort_flag, a.wait_limit_ns);
+                    else ok = lm_wait(full, use & 1, abort_flag, a.wait_limit_ns)
+                              && (use_b == 0 || lm_wait(empty, (use_b - 1) & 1, abort_flag, a.wait_limit_ns));
+                    if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t d_tmem = tmem_base + b * kTileN;
                     const uint64_t dx = lm_smem_desc_k(tiles + s * stage_bytes), dw = lm_smem_desc_k(tiles + s * stage_bytes + kBytesA);
@@ -906,7 +935,7 @@ template <class Kernel> static int raise_smem(Kernel kernel, size_t bytes, bool 
 // ---- which kernel, which tile ----
 // Both kernels' times in microseconds, fitted to measurements.
 //
-// Pair kernel: whole waves of tiles.  A block of a tile of 256 channels takes 0.61 us, of 128 channels 0.50 (its way to the epilogue and back);
+// Pair kernel: whole waves of tiles.  A block of a tile of 256 channels takes 0.61 us, of 128 channels 0.47 (its way to the epilogue and back);
 // a wave ends with its outputs, which take longer where tiled copies cannot write them.
 static double pair_time(long long M, int N, int n_ksteps, bool bf16, bool tiled, int* tile) {
     const long long n_tok = (M + 255) / 256, pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
@@ -914,7 +943,7 @@ static double pair_time(long long M, int N, int n_ksteps, bool bf16, bool tiled,
     double best = 0.0;
     for (int tn = kTileN; tn >= 128; tn /= 2) {
         const long long tiles = n_tok * ((N + tn - 1) / tn), waves = (tiles + pairs - 1) / pairs;
-        const double t = 3.4 + (double)waves * (n_ksteps * (tn == 256 ? 0.61 : 0.50) + store * tn);
+        const double t = 3.4 + (double)waves * (n_ksteps * (tn == 256 ? 0.61 : 0.47) + store * tn);
         if (best == 0.0 || t < best) { best = t; *tile = tn; }
     }
     return best;
