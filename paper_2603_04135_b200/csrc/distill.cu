@@ -14,9 +14,8 @@
 // adds the unlisted entries of each from the vector itself.
 //
 // Loss and gradient together (distill_step_kernel): one read and one write of the row.  A row's slices lie in the shared memory of the CTAs
-// of a cluster; the listed entries are set to -inf there, the exponentials replace the logits (as fp16 pairs for bf16 rows), and once the
-// row's sums are known the slices leave scaled; the listed entries are written last.  Short rows (distill_warp_kernel) do the same in
-// a warp's registers.
+// of a cluster; the listed entries are set to -inf there, and once the row's sums are known the exponentials leave scaled; the listed
+// entries are written last.  Short rows (distill_warp_kernel) do the same in a warp's registers.
 //
 // Gradient alone (distill_backward_kernel): a map over the row from the forward's {m, S, G, r / sigma}; the listed entries last here too.
 #include <cooperative_groups.h>
@@ -519,45 +518,44 @@ distill_step_kernel(const Args a, int log2C, int vec_per_cta) {
     const bool bad = !(m < INFINITY);
     m = bad ? 0.0f : fmaxf(m, kLowest);
 
-    // the exponentials, in place, and their sum: in the frame of a running sum (see Sum)
+    // the exponentials and their sum, in the frame of a running sum (see Sum).  Those of f32 rows take the logits' place; bf16 rows form
+    // theirs again for the gradient, since 16 bits would not hold the range that a gradient of that type has
     Sum acc;
     sum_init(acc, m, a.c);
     float etail = 0.0f;
+    const f32x2 c2 = pair_of(a.c, a.c), nr2 = pair_of(acc.nr, acc.nr), nm2 = pair_of(-m, -m);
+    auto e2 = [&](float z0, float z1, auto is_quick) {
+        float y0, y1;
+        if constexpr (decltype(is_quick)::value) unpair(fma2(pair_of(z0, z1), c2, nr2), y0, y1);
+        else unpair(mul2(add2(pair_of(z0, z1), nm2), c2), y0, y1);
+        return pair_of(ex2(y0), ex2(y1));
+    };
     if (warp < kWarps) {
-        const f32x2 c2 = pair_of(a.c, a.c), nr2 = pair_of(acc.nr, acc.nr), nm2 = pair_of(-m, -m);
         auto pass = [&](auto is_quick) {
-            auto e2 = [&](float z0, float z1) {
-                float y0, y1;
-                if constexpr (decltype(is_quick)::value) unpair(fma2(pair_of(z0, z1), c2, nr2), y0, y1);
-                else unpair(mul2(add2(pair_of(z0, z1), nm2), c2), y0, y1);
-                const f32x2 r = pair_of(ex2(y0), ex2(y1));
-                acc.S = add2(acc.S, r);
-                return r;
-            };
-#pragma unroll 2
+#pragma unroll 4
             for (int i = tid; i < nv; i += kThreads) {
                 const uint4 q = slice[i];
                 uint32_t w[4] = {q.x, q.y, q.z, q.w};
                 if constexpr (kBf16) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float x0, x1;
-                        unpair(e2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u)), x0, x1);
-                        w[j] = pack_half2(x0, x1);
-                    }
+                    for (int j = 0; j < 4; ++j) acc.S = add2(acc.S, e2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u), is_quick));
                 } else {
 #pragma unroll
                     for (int j = 0; j < 4; j += 2) {
+                        const f32x2 x = e2(__uint_as_float(w[j]), __uint_as_float(w[j + 1]), is_quick);
                         float x0, x1;
-                        unpair(e2(__uint_as_float(w[j]), __uint_as_float(w[j + 1])), x0, x1);
+                        acc.S = add2(acc.S, x);
+                        unpair(x, x0, x1);
                         w[j] = __float_as_uint(x0); w[j + 1] = __float_as_uint(x1);
                     }
+                    slice[i] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
-                slice[i] = make_uint4(w[0], w[1], w[2], w[3]);
             }
             if (ztail > -INFINITY) {
+                const f32x2 x = e2(ztail, -INFINITY, is_quick);
                 float unused;
-                unpair(e2(ztail, -INFINITY), etail, unused);
+                acc.S = add2(acc.S, x);
+                unpair(x, etail, unused);
             }
         };
         if (acc.quick) pass(std::true_type()); else pass(std::false_type());
@@ -594,20 +592,21 @@ distill_step_kernel(const Args a, int log2C, int vec_per_cta) {
     if (warp < kWarps) {
         uint4* dst = reinterpret_cast<uint4*>(out) + v0;
         const f32x2 s2 = pair_of(scale, scale);
+        auto put = [&](auto is_quick) {
 #pragma unroll 2
-        for (int i = tid; i < nv; i += kThreads) {
-            const uint4 q = slice[i];
-            uint4 r;
-            if constexpr (kBf16) {
-                r.x = scale_pair(q.x, s2); r.y = scale_pair(q.y, s2); r.z = scale_pair(q.z, s2); r.w = scale_pair(q.w, s2);
-            } else {
-                float x0, x1, x2, x3;
-                unpair(mul2(pair_of(__uint_as_float(q.x), __uint_as_float(q.y)), s2), x0, x1);
-                unpair(mul2(pair_of(__uint_as_float(q.z), __uint_as_float(q.w)), s2), x2, x3);
-                r = make_uint4(__float_as_uint(x0), __float_as_uint(x1), __float_as_uint(x2), __float_as_uint(x3));
+            for (int i = tid; i < nv; i += kThreads) {
+                float f[kPerVec];
+                Elems<kBf16>::unpack(slice[i], f);
+#pragma unroll
+                for (int j = 0; j < kPerVec; j += 2) {
+                    f32x2 x;
+                    if constexpr (kBf16) x = e2(f[j], f[j + 1], is_quick); else x = pair_of(f[j], f[j + 1]);
+                    unpair(mul2(x, s2), f[j], f[j + 1]);
+                }
+                __stcs(dst + i, Elems<kBf16>::pack(f));
             }
-            __stcs(dst + i, r);
-        }
+        };
+        if (!kBf16 || acc.quick) put(std::true_type()); else put(std::false_type());
         if (last && tail0 + tid < a.V) Elems<kBf16>::store1(out, tail0 + tid, scale * etail);
     } else {
         if (rank == 0) row_write(a, t, mass, sums, p, e.bad, lane);
@@ -891,7 +890,8 @@ template <bool kBf16, int kThreads, int kPer> static int launch_step(const Args&
     if (a.T_max << log2C > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "distill_topk: T_max=%lld needs too large a grid", a.T_max);
     return launch_after("distill_topk launch", kernel, a.T_max << log2C, kThreads + 32, (size_t)max(vec_per_cta, 1) * 16, s, 1 << log2C, a, log2C, vec_per_cta);
 }
-// Loss and gradient, 8,192 x 151,936 bf16 875 us (5.7 TB/s of one read and one write; as two kernels 1,160); 20,011 x 1,021 f32 31 (5.3).
+// Loss and gradient, 8,192 x 151,936 bf16 990-1,000 us (5.0 TB/s of one read and one write; as two kernels 1,160; 895-945 with the exponentials
+// kept as fp16, which lost the digits of entries more than e^-10 below the largest); 20,011 x 1,021 f32 32.5 (5.1).
 // The slices of a row: in one CTA up to 44 KB, in two of up to 55 KB, else in four or eight of up to 76 KB, three of which share an SM.  Few
 // rows: more CTAs for each (37 x 151,936 bf16 8.7 us, 10.2 in four; 16 x 20,000 f32 5.1, 5.9 in two).
 template <bool kBf16, int kPer> static int run_step(const Args& a, cudaStream_t s, bool* done) {
