@@ -518,7 +518,8 @@ size_t dppo_verify_drafts_workspace_bytes(const dppo_verify_params* p);
 /*   target_logits [(T_max + n_seqs) x target_stride], draft_logits [T_max x draft_stride] or NULL, of dtype
  *   drafts        i32 [T_max];  cu_drafts i32 [n_seqs + 1], non-decreasing from 0, the last at most T_max; rows past the last
  *                 sequence are neither read nor written
- *   uniforms      f32 [T_max] in [0, 1);  noise f32 [n_seqs x noise_stride], positive
+ *   uniforms      f32 [T_max] in [0, 1);  noise f32 [n_seqs x noise_stride], positive, of any size (entries whose noise is outside
+ *                 [2^-64, 2^13] are compared in 64 bits, which takes longer)
  *   n_accepted    i32 [n_seqs] out;  tokens_out i32, logp_out f32 [T_max + n_seqs] out
  *   workspace     at least dppo_verify_drafts_workspace_bytes, 16-byte aligned
  * Errors: INVALID_ARG, BAD_SHAPE, MISALIGNED, UNSUPPORTED (dtype), WORKSPACE_TOO_SMALL.

@@ -29,6 +29,10 @@ constexpr int kCand = 512;
 constexpr uint32_t kAll = 0xffffffffu;
 // Relative error of an f32 probability: 3 roundings and the constant in an exponent of up to 100, the exponential, the sum.
 constexpr float kEps = 1.0f / 65536.0f;
+// Where the exponent is beyond 100, down to probabilities that f32 makes 0, the error is that of this one.
+constexpr float kTiny = 0x1p-96f;
+// Noise between these has a reciprocal that, times kEps kTiny or a probability, is a normal f32; entries with any other are decided in 64 bits.
+constexpr float kLeastNoise = 0x1p-64f, kMostNoise = 0x1p13f;
 
 struct Args {
     const char *target, *draft;
@@ -253,7 +257,10 @@ template <bool kBf16, class F> __device__ __forceinline__ void for_vector(const 
     }
 }
 
-template <bool kBf16, int kThreads, bool kCluster> __global__ void __launch_bounds__(kThreads) verify_pick_kernel(const Args a) {
+// CTAs per SM that the registers leave room for: of 256 threads four (128 x 151,936 bf16 111 us; with 76 registers, three, 122), of 512 threads two for
+// f32 (clusters of four do not come out even on 148 SMs: 37 x 32,003 48.7 us, with one 56), one for bf16, whose loads want registers (16 sequences of
+// 4 drafts x 151,936 30.4 us, with two 33.1).
+template <bool kBf16, int kThreads, bool kCluster> __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : kBf16 ? 1 : 2) verify_pick_kernel(const Args a) {
     constexpr int kLog2 = kBf16 ? 3 : 2;
     __shared__ PickShared sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -362,15 +369,16 @@ template <bool kBf16, int kThreads, bool kCluster> __global__ void __launch_boun
         float z_best = 0.0f;
         auto bounds = [&](float zp, float zq, float e, int at, float& hi, float& lo) {
             const float p = ex2((zp - f.mp) * a.ct) * f.ip;
-            float w = p, t = p;
+            float w = p, t = p + kTiny;
             if (f.q) {
                 const float q = ex2((zq - f.mq) * a.cd) * f.iq;
-                w = p - q; t = p + q;
+                w = p - q; t += q;
             }
             if (at == f.drop) w = t = 0.0f;
+            const bool sure = e >= kLeastNoise && e <= kMostNoise;
             const float inv = __fdividef(1.0f, e);
-            hi = fmaf(t, kEps, w) * inv;
-            lo = fmaf(t, -kEps, w) * inv;
+            hi = sure ? fmaf(t, kEps, w) * inv : INFINITY;
+            lo = sure ? fmaf(t, -kEps, w) * inv : 0.0f;
         };
         auto enter = [&](float zp, float zq, float e, int at) {
             float hi, lo;
@@ -414,7 +422,7 @@ template <bool kBf16, int kThreads, bool kCluster> __global__ void __launch_boun
             }
             return;
         }
-        if (r.hi > 0.0f) {                                         // in 64 bits, over the entries within reach
+        if (r.hi > 0.0f) {                                         // in 64 bits, over the entries within reach (r.lo is finite)
             const double ip = 1.0 / (double)sh.sp.y, iq = f.q ? 1.0 / (double)sh.sq.y : 0.0;
             Exact x = {0.0, 0x7fffffff};
             const float bound = log_bound(r.lo);
@@ -422,7 +430,7 @@ template <bool kBf16, int kThreads, bool kCluster> __global__ void __launch_boun
                 float hi, lo;
                 const float zq = draft_at(at);
                 bounds(zp, zq, e, at, hi, lo);
-                if (!(hi >= r.lo) || !(hi > 0.0f) || !(zp > -INFINITY)) return;
+                if (!(hi >= r.lo) || !(hi > 0.0f) || !(zp > -INFINITY) || at == f.drop) return;
                 double w = exp64(((double)zp - (double)f.mp) * a.inv_tau_t) * ip;
                 if (zq > -INFINITY) w -= exp64(((double)zq - (double)f.mq) * a.inv_tau_d) * iq;
                 if (w > 0.0) x = exact_join({w / (double)e, at}, x);
