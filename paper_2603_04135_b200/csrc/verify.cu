@@ -312,7 +312,8 @@ template <bool kBf16, int kThreads, bool kCluster> __global__ void __launch_boun
                         if (zq > -INFINITY && d.y > 0.0f) x = l - (((double)zq - (double)d.x) * a.inv_tau_d - log64((double)d.y));
                         else x = l > -INFINITY ? INFINITY : l;
                     }
-                    accept = l > -INFINITY && (x >= 700.0 || (double)a.u[c0 + j] < exp64(x));
+                    const float u = a.u[c0 + j];                   // 0: whatever is possible, also where exp64 returns 0
+                    accept = l > -INFINITY && (x >= 700.0 || u == 0.0f || (double)u < exp64(x));
                     lp = (float)l;
                 }
             }

@@ -1,4 +1,4 @@
-"""Verification of drafts with noise of any positive size on the GPU against the float64 oracle.
+"""Verification of drafts with noise of any positive size and uniforms of zero, on the GPU against the float64 oracle.
 
 The bounds are those of test_gpu_verify.py; here every sequence has a margin (asserted), so that nothing is left out of the comparison.
 """
@@ -76,3 +76,23 @@ def test_unlikely_token_with_noise_to_match(B):
     assert w["margin"][0] > 0.1 and int(got["tokens"][0]) == 4000
     # the second sequence is a tie: the other tokens are alike, and the clamp has left many of them the same noise
     assert int(got["tokens"][1]) == w["tokens"][1] == int((c.noise[1, :5000] == 0.5).nonzero()[0])
+
+
+@pytest.mark.parametrize("z", [-100.0, -690.0, -720.0, -900.0])
+def test_a_uniform_of_zero_accepts_whatever_is_possible(B, z):
+    """u q < p at u = 0 is 0 < p: true of every token that is not masked, also where p is below the f64 numbers."""
+    V = 300
+    c = Case([2], V, "f32", True, 1.0, 1.0, 12)
+    c.target[:3, :V] = -math.inf
+    c.target[:3, 5] = 0.0
+    c.target[:3, 9] = z
+    c.drafts[:2] = 9
+    c.u[:2] = 0.0
+    out = c.run(B)
+    torch.cuda.synchronize()
+    assert int(out["n"][0]) == 2 and out["tokens"][:3].tolist() == [9, 9, 5]
+    assert out["logp"][:3].tolist() == [z, z, 0.0]
+    c.target[1, 9] = -math.inf
+    out = c.run(B)
+    torch.cuda.synchronize()
+    assert int(out["n"][0]) == 1 and out["tokens"][:3].tolist() == [9, 5, -1]
