@@ -255,11 +255,13 @@ class DppoStep:
     # -- distillation: a teacher's alternatives (score(..., top_k) of its logits) as the target ----------------
     _DISTILL = {"given": B.DISTILL_GIVEN, "normalized": B.DISTILL_NORMALIZED, "rest": B.DISTILL_REST}
 
-    def _distill_params(self, logits, top_ids, mode, row_stride):
+    def _distill_params(self, logits, top_ids, top_logp, mode, row_stride):
         if mode not in self._DISTILL:
             raise ValueError("mode %r: one of %s" % (mode, ", ".join(sorted(self._DISTILL))))
         if top_ids.dim() != 2 or top_ids.shape[0] < self.T_max:
             raise ValueError("top_ids has shape %s, T_max is %d" % (tuple(top_ids.shape), self.T_max))
+        if top_logp.dim() != 2 or top_logp.shape[0] < self.T_max or top_logp.shape[1] != top_ids.shape[1]:
+            raise ValueError("top_logp has shape %s, top_ids %s, T_max is %d" % (tuple(top_logp.shape), tuple(top_ids.shape), self.T_max))
         return B.DistillParams(self.T_max, self.V, self.loss_params.dtype, self.V if row_stride is None else row_stride, top_ids.shape[1],
                                self._DISTILL[mode], self.loss_params.temperature)
 
@@ -269,7 +271,7 @@ class DppoStep:
         mode "given": the log-probs as they stand, "normalized": over their sum, "rest": with the remainder as one more outcome.
         dlogits (`logits` itself for in place): the gradient of sum(weight * loss) in the same call (weight f32 [T_max], None: ones).
         Rows past the token count (the packer's, or n_tokens_dev) are left as they were.  `out`: the dict of an earlier call."""
-        prm = self._distill_params(logits, top_ids, mode, row_stride)
+        prm = self._distill_params(logits, top_ids, top_logp, mode, row_stride)
         T = self.T_max
         if out is None:
             f32 = dict(dtype=torch.float32, device=self.device)
@@ -284,7 +286,7 @@ class DppoStep:
     def distill_backward(self, logits, top_ids, top_logp, distilled, dloss=None, mode="rest", dlogits=None, row_stride=None, n_tokens_dev=None):
         """Gradient with respect to `logits` for the per-token derivatives dloss (f32 [T_max], None: ones); `distilled` is what distill()
         returned for the same arguments.  Returns dlogits (`logits` itself for in place; a new tensor of its shape and strides if None)."""
-        prm = self._distill_params(logits, top_ids, mode, row_stride)
+        prm = self._distill_params(logits, top_ids, top_logp, mode, row_stride)
         if dlogits is None:
             dlogits = self._zeros_like_rows(logits)
         B.distill_topk_backward(prm, logits, top_ids, top_logp, self.counts[3:4] if n_tokens_dev is None else n_tokens_dev,
