@@ -76,6 +76,15 @@ __device__ __forceinline__ float warp_max(float v) {
     for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
+// The same, no NaN among them, in one reduction: by integers in the order of the floats.  The f32 form of that instruction is not used: under
+// a condition, even one that all lanes share (the vote's `bad ? 0 : max`), it returned another register's value for some rows of one
+// kernel; the same kernel with the reduction moved out of the condition was right.
+__device__ __forceinline__ int order_of(float v) {
+    const int i = __float_as_int(v);
+    return i ^ (i >> 31 & 0x7fffffff);
+}
+__device__ __forceinline__ float float_of(int order) { return __int_as_float(order ^ (order >> 31 & 0x7fffffff)); }
+__device__ __forceinline__ float warp_max_f32(float v) { return float_of(__reduce_max_sync(0xffffffffu, order_of(v))); }
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);

@@ -65,11 +65,6 @@ __device__ __forceinline__ void rescale(Part& p, float M, float c) {
     p.m = M;
 }
 // The parts of a warp's lanes as one, in every lane: the maximum first, one rescale per lane, then the sums.
-__device__ __forceinline__ float warp_max_f32(float v) {
-    float r;
-    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-    return r;
-}
 __device__ __forceinline__ Part warp_join(Part p, float c) {
     rescale(p, warp_max_f32(p.m), c);
     p.S = warp_sum(p.S); p.Q = warp_sum(p.Q);
@@ -320,15 +315,16 @@ template <int kPer, int kBits> __device__ __forceinline__ uint32_t kth_largest(c
 // equal go together), else out of the sorted values (a bitonic network over the lanes, 15 exchanges).
 __device__ __forceinline__ float kth_of_lanes(float v, int k, int lane) {
     if (k <= 6) {
-        float m = kLowest;
+        int own = order_of(v), m = 0;
+        const int none = order_of(-INFINITY);
 #pragma unroll 1
         for (int have = 0; have < k;) {
-            m = warp_max_f32(v);
-            if (!(m > kLowest)) return kLowest;
-            have += __popc(__ballot_sync(0xffffffffu, v == m));
-            v = v == m ? -INFINITY : v;
+            m = __reduce_max_sync(0xffffffffu, own);
+            if (m <= order_of(kLowest)) return kLowest;
+            have += __popc(__ballot_sync(0xffffffffu, own == m));
+            own = own == m ? none : own;
         }
-        return m;
+        return float_of(m);
     }
 #pragma unroll
     for (int size = 2; size <= 32; size <<= 1) {

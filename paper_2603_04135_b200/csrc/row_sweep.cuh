@@ -11,12 +11,6 @@ using namespace packed;
 constexpr float kLowest = -3.402823466e38f;
 constexpr int kRound = 4;                 // vectors that a thread has under way
 
-// Over a warp, no NaN among them.  By integers in the order of the floats: with the f32 form of the same instruction a short row's maximum
-// came out as another register's value in one of the kernels.
-__device__ __forceinline__ float warp_max_f32(float v) {
-    const int i = __float_as_int(v), k = __reduce_max_sync(0xffffffffu, i ^ (i >> 31 & 0x7fffffff));
-    return __int_as_float(k ^ (k >> 31 & 0x7fffffff));
-}
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
