@@ -752,7 +752,8 @@ distill_backward_kernel(const Args a) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) any = any || here(i);
         any = __any_sync(kAll, any);
-        if (any) listed_logits<kBf16, kPer>(row, e);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) e.z[i] = here(i) ? Elems<kBf16>::load1(row, e.id[i]) : -INFINITY;      // the other pieces' are being written
     }
     if (a.in_place) { if constexpr (kThreads == 32) __syncwarp(); else __syncthreads(); }
 
