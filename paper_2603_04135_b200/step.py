@@ -10,6 +10,14 @@ from . import binding as B
 from . import dp
 
 
+def _pitch(x):
+    """Elements between the rows of a matrix; of a single row, where nothing lies that far, the next number on 16 bytes."""
+    if x.shape[0] > 1:
+        return x.stride(0)
+    per = 16 // x.element_size()
+    return (max(x.stride(0), x.shape[1]) + per - 1) // per * per
+
+
 def quantize_rows_i8(x, status=None):
     """8-bit codes and scales of the rows of x (bf16 or f32 [M, K] with rows on 16 bytes): (q int8 [M, K], scale f32 [M]), q a
     view of padded rows.  Weights are quantised once this way and kept; see DppoStep.score_hidden_i8."""
@@ -17,8 +25,7 @@ def quantize_rows_i8(x, status=None):
     ld = (K + 127) // 128 * 128            # whole 128-byte lines: the product's slabs then never straddle two
     q = torch.zeros(M, ld, dtype=torch.int8, device=x.device)
     scale = torch.zeros(M, dtype=torch.float32, device=x.device)
-    B.quantize_rows_i8(B.QuantizeParams(M, K, B.BF16 if x.dtype is torch.bfloat16 else B.F32, x.stride(0) if M > 1 else max(x.stride(0), K), ld),
-                       x, q, scale, status=status)
+    B.quantize_rows_i8(B.QuantizeParams(M, K, B.BF16 if x.dtype is torch.bfloat16 else B.F32, _pitch(x), ld), x, q, scale, status=status)
     return q[:, :K], scale
 
 
@@ -30,7 +37,7 @@ def quantize_f8(x, block_rows=128, status=None):
     ld, kb = (K + 127) // 128 * 128, (K + 127) // 128
     q = torch.zeros(M, ld, dtype=torch.float8_e4m3fn, device=x.device)
     scale = torch.zeros(kb, (M + 3) // 4 * 4, device=x.device) if block_rows == 1 else torch.zeros((M + 127) // 128, kb, device=x.device)
-    B.quantize_f8(B.QuantizeF8Params(M, K, B.BF16 if x.dtype is torch.bfloat16 else B.F32, x.stride(0) if M > 1 else max(x.stride(0), K), ld,
+    B.quantize_f8(B.QuantizeF8Params(M, K, B.BF16 if x.dtype is torch.bfloat16 else B.F32, _pitch(x), ld,
                                      scale.stride(0) if scale.numel() else max(kb, 1), block_rows), x, q, scale, status=status)
     return q[:, :K], scale[:, :M] if block_rows == 1 else scale
 
@@ -211,7 +218,7 @@ class DppoStep:
         dtype = B.BF16 if hidden.dtype is torch.bfloat16 else B.F32
         for i, lo in enumerate(range(0, T, C)):
             hi, n = min(lo + C, T), left[i:i + 1]
-            B.quantize_rows_i8(B.QuantizeParams(hi - lo, H, dtype, hidden.stride(0), ldq), hidden[lo:hi], q, q_scale, n, self.status)
+            B.quantize_rows_i8(B.QuantizeParams(hi - lo, H, dtype, _pitch(hidden), ldq), hidden[lo:hi], q, q_scale, n, self.status)
             B.linear_i8(B.LinearI8Params(hi - lo, V, H, ldq, W_q.stride(0), ldv, B.F32), q, q_scale, W_q, W_scale, logits, n,
                         self.status)
             self._score_call(logits, B.F32, V, ldv, None if target is None else target[lo:hi], n, top_k, out, lo, hi)
@@ -246,7 +253,7 @@ class DppoStep:
         dtype = B.BF16 if hidden.dtype is torch.bfloat16 else B.F32
         for i, lo in enumerate(range(0, T, C)):
             hi, n = min(lo + C, T), left[i:i + 1]
-            B.quantize_f8(B.QuantizeF8Params(hi - lo, H, dtype, hidden.stride(0), ldq, lds, 1), hidden[lo:hi], q, q_scale, n, self.status)
+            B.quantize_f8(B.QuantizeF8Params(hi - lo, H, dtype, _pitch(hidden), ldq, lds, 1), hidden[lo:hi], q, q_scale, n, self.status)
             B.linear_f8(B.LinearF8Params(hi - lo, V, H, ldq, W_q.stride(0), ldv, lds, W_scale.stride(0), B.F32), q, q_scale, W_q, W_scale,
                         logits, n, self.status)
             self._score_call(logits, B.F32, V, ldv, None if target is None else target[lo:hi], n, top_k, out, lo, hi)
