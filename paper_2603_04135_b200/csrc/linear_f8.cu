@@ -47,13 +47,12 @@ constexpr int kSlotBytes2 = kTileM * 4;   // pair kernel: of this CTA's tokens
 constexpr size_t kDynSmem2 = (size_t)kRingBytes + kEpiWarps * kStageOut + kSlots * kSlotBytes2 + 1024;
 
 struct Args {
-    const float* x_scale;
     const float* w_scale;
     void* out;
     const int32_t* n_rows_dev;
     int32_t* status;
-    long long M_max, out_stride, xs_stride, ws_stride;
-    int N, n_ksteps, out_bf16;
+    long long M_max, out_stride, ws_stride;
+    int N, n_ksteps;
     int tile_n;                           // pair kernel: channels per tile, 128 or 256
     int vec_out;                          // out: base and rows on 16 bytes
     unsigned long long wait_limit_ns;
@@ -1054,22 +1053,23 @@ extern "C" int dppo_linear_f8(const dppo_linear_f8_params* p, const uint8_t* x, 
         return fail(DPPO_ERR_BAD_SHAPE, "linear_f8: strides of x, w and x_scale must be below 2^40 bytes");
 
     f8::Args a = {};
-    a.x_scale = x_scale; a.w_scale = w_scale; a.out = out; a.n_rows_dev = n_rows_dev; a.status = status;
-    a.M_max = p->M_max; a.out_stride = p->out_stride; a.xs_stride = p->x_scale_stride; a.ws_stride = p->w_scale_stride;
-    a.N = p->N; a.n_ksteps = n_blocks; a.out_bf16 = p->out_dtype == DPPO_BF16;
+    a.w_scale = w_scale; a.out = out; a.n_rows_dev = n_rows_dev; a.status = status;
+    a.M_max = p->M_max; a.out_stride = p->out_stride; a.ws_stride = p->w_scale_stride;
+    a.N = p->N; a.n_ksteps = n_blocks;
+    const bool bf16 = p->out_dtype == DPPO_BF16;
     a.wait_limit_ns = p->variant >= 100 ? kSelfTestWaitLimitNs : kDefaultWaitLimitNs;
     a.test_extra_tx = p->variant >= 100 ? 16 : 0;
-    a.vec_out = ((uintptr_t)out & 15) == 0 && p->out_stride * (a.out_bf16 ? 2 : 4) % 16 == 0 && p->out_stride < (1ll << 36);
+    a.vec_out = ((uintptr_t)out & 15) == 0 && p->out_stride * (bf16 ? 2 : 4) % 16 == 0 && p->out_stride < (1ll << 36);
     int nb = 0, split = 1;
-    const double t_pair = f8::pair_time(p->M_max, p->N, n_blocks, a.out_bf16 != 0, a.vec_out != 0, &a.tile_n);
+    const double t_pair = f8::pair_time(p->M_max, p->N, n_blocks, bf16, a.vec_out != 0, &a.tile_n);
     const double t_small = f8::small_time(p->M_max, p->N, n_blocks, &nb, &split);
     const bool pair = variant == 1 || (variant == 0 && t_pair < t_small);
     alignas(64) CUtensorMap mw, mx, ms, mo = {};
     int rc = f8::make_map(&mw, w, p->N, p->K, p->w_stride, pair ? a.tile_n / 2 : f8::kTileM);
     if (rc == DPPO_OK) rc = f8::make_map(&mx, x, p->M_max, p->K, p->x_stride, pair ? f8::kTileM : nb);
     if (rc == DPPO_OK) rc = f8::make_scale_map(&ms, x_scale, p->M_max, n_blocks, p->x_scale_stride, pair ? f8::kTileM : nb);
-    if (rc == DPPO_OK && pair && a.vec_out) rc = f8::make_out_map(&mo, out, p->M_max, p->N, p->out_stride, a.out_bf16 != 0);
+    if (rc == DPPO_OK && pair && a.vec_out) rc = f8::make_out_map(&mo, out, p->M_max, p->N, p->out_stride, bf16);
     if (rc != DPPO_OK) return rc;
     cudaStream_t s = (cudaStream_t)stream;
-    return a.out_bf16 ? f8::launch<true>(pair, nb, split, mw, mx, ms, mo, a, s) : f8::launch<false>(pair, nb, split, mw, mx, ms, mo, a, s);
+    return bf16 ? f8::launch<true>(pair, nb, split, mw, mx, ms, mo, a, s) : f8::launch<false>(pair, nb, split, mw, mx, ms, mo, a, s);
 }

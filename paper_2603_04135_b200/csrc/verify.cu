@@ -185,7 +185,7 @@ struct PickShared {
     int bound, n_cand;                    // bits of the largest lower bound of the CTA's first entries; entries that come near it
     float z[kCand], e[kCand];
     int at[kCand];
-    int n_acc, state;                     // state: 0 go on, 1 the sequence has no next token, 2 nothing may be written
+    int state;                            // 0 go on, 1 the sequence has no next token, 2 nothing may be written
 };
 
 template <int kThreads> __device__ __forceinline__ Race race_cta(Race r, PickShared& sh) {
@@ -354,7 +354,7 @@ template <bool kBf16, int kThreads, bool kCluster> __global__ void __launch_boun
                 }
             }
         }
-        if (lane == 0) { sh.sp = sp; sh.sq = sq; sh.row = base + n_acc; sh.n_acc = n_acc; sh.state = state; }
+        if (lane == 0) { sh.sp = sp; sh.sq = sq; sh.row = base + n_acc; sh.state = state; }
     }
     __syncthreads();
     if (sh.state != 0) return;                                     // the same in every CTA of the cluster
