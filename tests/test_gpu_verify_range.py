@@ -1,4 +1,4 @@
-"""Verification of drafts with noise of any positive size and uniforms of zero, on the GPU against the float64 oracle.
+"""Verification of drafts with noise of any positive size, uniforms of zero, and single sequences, on the GPU against the float64 oracle.
 
 The bounds are those of test_gpu_verify.py; here every sequence has a margin (asserted), so that nothing is left out of the comparison.
 """
@@ -96,3 +96,12 @@ def test_a_uniform_of_zero_accepts_whatever_is_possible(B, z):
     out = c.run(B)
     torch.cuda.synchronize()
     assert int(out["n"][0]) == 1 and out["tokens"][:3].tolist() == [9, 5, -1]
+
+
+@pytest.mark.parametrize("lens,V,dtype,copied", [([4], 151936, "bf16", False), ([1], 33001, "bf16", False), ([0], 7, "f32", False), ([12], 50304, "f32", False),
+                                                  ([40], 777, "bf16", True), ([2, 9], 5003, "f32", False)])
+@pytest.mark.parametrize("seed", [21, 22, 23])
+def test_single_sequences(B, lens, V, dtype, copied, seed):
+    """Nothing is close here: the margins are asserted, and every count, token and log-prob is compared."""
+    c = Case(lens, V, dtype, copied, 1.0, 1.0, seed * 1000 + V)
+    check_all(c, c.run(B))
