@@ -498,7 +498,7 @@ int dppo_distill_topk_backward(const dppo_distill_params* p, const void* logits,
  *   y_j is accepted while u_j q_j(y_j) < p_j(y_j).
  *   After a first rejection at j the next token is argmax_v max(p_j(v) - q_j(v), 0) / e_b(v) (if p_j <= q_j everywhere:
  *   argmax_v p_j(v) / e_b(v)), after n acceptances argmax_v p_n(v) / e_b(v); ties to the lower index.  With independent u uniform
- *   in [0, 1) and e exponential that is a sample.
+ *   in [0, 1) and e exponential that is a sample.  Softmax sums are f32 (about 1e-6 off); all else is decided as in 64 bits.
  *   tokens_out: the accepted drafts, the next token, then -1;  logp_out: their log-probs under the target, then 0.
  * Logits at -inf are masked.  A draft row that its mask leaves empty has q = 0.  At a row with a NaN or +inf, the target's or the draft's,
  * the sequence ends: next token -1, log-prob NaN.  A target row that its mask leaves empty: next token -1, log-prob -inf.
@@ -560,7 +560,8 @@ int dppo_quantize_f8(const dppo_quantize_f8_params* p, const void* x, uint8_t* q
                      int32_t* status, void* stream);
 
 /*   out[t, n] = sum_B x_scale[B, t] w_scale[n / 128, B] sum_{k in block B} x[t, k] w[n, k], the blocks' sums and their sum in f32,
- * rounded once more to a bf16 out.  The order of the sums is a function of the sizes alone. */
+ * rounded once more to a bf16 out.  The order of the sums is a function of the sizes (M_max, not the true count), of variant, of out's type and of
+ * whether its base and rows lie on 16 bytes. */
 typedef struct {
     int64_t M_max;          /* rows of x / upper bound of tokens (below 2^31)                        */
     int32_t N, K;           /* output channels; contraction length                                   */

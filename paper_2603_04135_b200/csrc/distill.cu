@@ -110,7 +110,9 @@ template <int kPer> __device__ __forceinline__ void listed_probs(const Args& a, 
 #pragma unroll
     for (int i = 0; i < kPer; ++i) e.p[i] = e.id[i] >= 0 ? exp64((double)lp[i] - (double)e.top) : 0.0;
 }
-// Which entries are the first with their id.  together: their p, added up in the order of the entries, goes to the first.
+// Which entries are the first with their id.  together: their p, added up in the order of the entries, goes to the first.  Lists of more than 32
+// walk over all of their entries, which costs more than the sweep from about 64 on (2,048 x 151,936 bf16, loss and gradient: 20 entries 243 us, 33
+// 322, 64 372, 128 512; loss 112, 132, 130, 133; gradient 192, 218, 229, 336).
 template <int kPer> __device__ __forceinline__ void listed_first(const Args& a, int lane, Listed<kPer>& e, bool together) {
     if constexpr (kPer == 1) {                     // mostly no id comes twice
         const unsigned peers = __match_any_sync(kAll, e.id[0]);
@@ -852,7 +854,7 @@ template <bool kBf16, int kThreads, int kPer, bool kCluster> static int launch_f
 
 // Loss alone: a warp per row up to 4 KB, else a CTA, in a cluster while the rows do not give every SM two (40 x 151,936 bf16 8.5 us).  A CTA alone has 256
 // threads up to five rows per SM (400 x 151,936 bf16 29.5 us, with 128 44.6; 700 x 50,304 18.4, 20.2) and 128 beyond, where they are as fast and
-// leave room for shorter ones (8,192 x 151,936 390 us, 6.4 TB/s).
+// leave room for shorter ones (8,192 x 151,936 390-434 us, 6.4-5.7 TB/s: the power limit).
 template <bool kBf16, int kPer> static int run_fwd(const Args& a, cudaStream_t s) {
     const int nvec = a.V >> (kBf16 ? 3 : 2);
     const long long sms = sm_count();
@@ -891,7 +893,7 @@ template <bool kBf16, int kThreads, int kPer> static int launch_step(const Args&
     if (a.T_max << log2C > 0x7fffffffll) return fail(DPPO_ERR_BAD_SHAPE, "distill_topk: T_max=%lld needs too large a grid", a.T_max);
     return launch_after("distill_topk launch", kernel, a.T_max << log2C, kThreads + 32, (size_t)max(vec_per_cta, 1) * 16, s, 1 << log2C, a, log2C, vec_per_cta);
 }
-// Loss and gradient, 8,192 x 151,936 bf16 990-1,000 us (5.0 TB/s of one read and one write; as two kernels 1,160; 895-945 with the exponentials
+// Loss and gradient, 8,192 x 151,936 bf16 990-1,015 us (5.0 TB/s of one read and one write; as two kernels 1,160; 895-945 with the exponentials
 // kept as fp16, which lost the digits of entries more than e^-10 below the largest); 20,011 x 1,021 f32 32.5 (5.1).
 // The slices of a row: in one CTA up to 44 KB, in two of up to 55 KB, else in four or eight of up to 76 KB, three of which share an SM.  Few
 // rows: more CTAs for each (37 x 151,936 bf16 8.7 us, 10.2 in four; 16 x 20,000 f32 5.1, 5.9 in two).

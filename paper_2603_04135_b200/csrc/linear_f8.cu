@@ -207,10 +207,10 @@ template <bool kBf16> __device__ __forceinline__ void stage_boxes(int lane, cons
 
 // ---- many tokens: CTA pairs ---------------------------------------------------------------------------
 // 2,048 x 2,560 x 151,936 into bf16: 778 us on a rested board, 2.0 PFLOP/s (930 us in a long run, under the power limit), where the products alone would
-// take 464 at the rate of a plain product.  What bounds it is the accumulator's way to the registers: a block's 256 x 256
-// sums take 650 cycles of products, 512 of tensor-memory reads, and the hand-over between; two accumulators fill tensor memory.  With
-// tiles of 128 channels a block takes 0.47 us instead of 0.61, also with four accumulators.  Sixteen epilogue warps, two instructions of half
-// the channels each, and epilogue warps that look at the barriers themselves were slower (907, 880 and 976 us).
+// take 464 at the rate of a plain product; into f32 995 in a long run.  What bounds it is the epilogue: each of its eight warps serves every block, one
+// step after the other (barrier, tensor-memory reads, release, sums), 0.61 us for a block of 256 x 256 whose products alone take about 0.35.  With tiles
+// of 128 channels a block takes 0.47 us instead of half of that, with two accumulators or with four, so it is not their number.  Sixteen epilogue
+// warps, two instructions of half the channels each, and epilogue warps that look at the barriers themselves were slower (907, 880 and 976 us).
 struct Shared2 {
     unsigned long long full[kMaxStages];
     unsigned long long empty[kMaxStages];
@@ -688,7 +688,8 @@ linear_f8_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
 }
 
 // ---- quantisation -------------------------------------------------------------------------------------
-// One read, one write: rows, 8,192 x 4,096 f32 27 us (6.3 TB/s), bf16 23 (4.3, bound by its instructions); 128 x 128, 43 and 29.
+// One read, one write: rows, 8,192 x 4,096 f32 27-33 us (6.3-5.1 TB/s), bf16 23-29 (4.3-3.5, bound by its instructions); 128 x 128, 43-51 and 29-34:
+// a CTA loads a block, joins its maximum, writes and leaves, and only other CTAs' loads run under that (once per set of weights).
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));

@@ -9,8 +9,11 @@
 // cluster of CTAs per sequence, finds the first rejection (a warp, 32 drafts at a time) and races over that one row.
 //
 // The race: an entry counts only if its p / e, by one fma and a logarithm, comes near the best lower bound among the first entries of its
-// CTA, which a few dozen do; only those look at the draft's row, all at once.  Tokens are exact: f32 decides a race only where no second
-// entry's upper bound reaches the winner's lower bound; otherwise the entries within reach are compared in 64 bits, ties to the lower index.
+// CTA, which a few dozen do; only those look at the draft's row, all at once.  f32 decides a race only where no second entry's upper bound
+// reaches the winner's lower bound; otherwise the entries within reach are compared in 64 bits, ties to the lower index.
+//
+// What that leaves: the rows' sums S are f32 sums (about 1e-6 of them off), common to all of a race over p alone, but not to both sides of
+// u q < p nor to p and q in p - q.  Decisions whose sides are closer than that may differ from the definition's; they are the same in every call.
 #include <cooperative_groups.h>
 
 #include "common.cuh"
